@@ -302,6 +302,64 @@ dream_status dream_gemm_timing(dream_ctx *ctx, int32_t on, int64_t *launches, do
 dream_status dream_topk_lse_static(const float *logits, int32_t rows, int32_t vocab, int32_t ktop,
                                    float *top_val, int32_t *top_id, float *lse, void *cuda_stream);
 
+/* Calls on rows of logits.  Like dream_topk_lse_static they need no context and allocate nothing; unlike it they need no scratch
+ * either (a row is worked on by one block, or by a cluster of blocks that exchange through shared memory), so calls on
+ * several streams, and captured ones, do not meet.  Common to all:
+ *   logits : device [rows][vocab] of dtype (DREAM_F32 or DREAM_BF16), `ld` elements from one row to the next (ld >= vocab); any
+ *            alignment to its elements and any vocab up to 262144 (DREAM_E_CAPACITY above), fastest where rows start on 16 bytes
+ *   cuda_stream : a cudaStream_t of the current device (NULL = legacy default stream)
+ * Asynchronous; errors are reported through dream_last_error(NULL), before anything is enqueued. */
+
+/* A token per row, drawn from the row's distribution at a temperature, cut to its likely tokens.  With
+ *   w_i = exp((l_i - max l) / temperature), tokens ordered by logit, larger first, then by id, smaller first,
+ * the kept tokens are the first n of the order: at most top_k; only those before which less than top_p of the mass of the top_k has
+ * gone by; only those with w >= min_p; the first one in any case, and never a logit of -inf or NaN.  The token is the
+ * first kept one, in id order, at which the running sum of w exceeds u times the kept tokens' sum: the rule of
+ * dream_accept_sample's final draw.  Sums are exact to about 1e-12 of the row's mass and the same at every run.
+ *   temperature, top_k, top_p, min_p : device [rows], each NULL where the batch does not use it (1, all, 1, 0).  By row:
+ *            temperature <= 0 takes the first of the order; top_k <= 0 or >= vocab, top_p >= 1, min_p <= 0 switch off; NaN reads as
+ *            off (temperature: as 0)
+ *   uniforms : device [rows], numbers in [0, 1) drawn by the caller (others are taken to the nearer end)
+ *   outputs  : device tokens int32 [rows] (-1 for a row of nothing but -inf and NaN), logprob float [rows] or NULL (log of the token's
+ *            probability among the kept), kept int32 [rows] or NULL (how many tokens were kept)
+ * Logits of +inf share the mass equally. */
+dream_status dream_sample(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, const float *temperature,
+                          const int32_t *top_k, const float *top_p, const float *min_p, const float *uniforms, int32_t *tokens,
+                          float *logprob, int32_t *kept, void *cuda_stream);
+
+/* The same cut without the draw: out[r][i] = logits[r][i] where token i is kept, -inf elsewhere.  On the logits of
+ * dream_verify_tree it makes dream_accept_sample, at the same temperature, follow the truncated distribution.
+ *   out  : device [rows][vocab] of the same dtype, out_ld elements from row to row; may be `logits` itself (out_ld = ld then);
+ *          anything between two rows is left as it is
+ *   kept : device int32 [rows] or NULL */
+dream_status dream_truncate_logits(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, const float *temperature,
+                                   const int32_t *top_k, const float *top_p, const float *min_p, void *out, int64_t out_ld,
+                                   int32_t *kept, void *cuda_stream);
+
+/* Distillation of a draft from the target's top logits: Kullback-Leibler divergence of a student's rows from a teacher of which the top
+ * logits were kept (dream_topk_lse_static makes them).  z = logits / temperature, p = softmax(z), lse = log-sum-exp of z.
+ *   teacher_ids int32 [rows][top], teacher_logits float [rows][top] : device, top in 1..128; an id outside [0, vocab) is no entry;
+ *            an id may come twice (its probabilities add up)
+ *   teacher_lse : device float [rows], log-sum-exp of the teacher's whole row at this temperature, or NULL.
+ *            NULL: q = softmax of the entries at this temperature, loss = sum_j q_j (log q_j - log p_j).
+ *            Given: q_j = exp(t_j / temperature - teacher_lse) and the rest of the vocabulary is one bucket, q_r = 1 - sum q (0 if that is
+ *            negative): loss also has q_r (log q_r - log p_r), p_r the student's probability of all ids that are not entries.
+ *   outputs  : device loss float [rows], lse float [rows], log_rest float [rows] = log p_r (with teacher_lse, else NULL)
+ *   grad     : device [rows][vocab] of the logits' dtype, grad_ld elements from row to row, or NULL.  Receives
+ *            row_scale[r] * d loss[r] / d logits[r], in the same pass over the row; may be `logits` itself (grad_ld = ld then)
+ *   row_scale : device float [rows] (what reaches a row's loss from behind), NULL = 1.  A row with 0 is padding: its gradient is zeros
+ *            whatever its logits hold.
+ * A row without an entry has loss 0 and gradient 0; a row without a finite logit loss +inf and gradient 0.  A factor of
+ * temperature^2, where wanted, goes into row_scale. */
+dream_status dream_distill_loss(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, const int32_t *teacher_ids,
+                                const float *teacher_logits, int32_t top, const float *teacher_lse, float temperature, float *loss,
+                                float *lse, float *log_rest, const float *row_scale, void *grad, int64_t grad_ld, void *cuda_stream);
+
+/* The gradient on its own, from the lse (and, with teacher_lse, log_rest) that dream_distill_loss left.  Arguments as there. */
+dream_status dream_distill_grad(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, const int32_t *teacher_ids,
+                                const float *teacher_logits, int32_t top, const float *teacher_lse, float temperature, const float *lse,
+                                const float *log_rest, const float *row_scale, void *grad, int64_t grad_ld, void *cuda_stream);
+
 /* Timeline of the context's stream (a measurement hook; Section 4 times whole steps only).
  * buffer: DEVICE array of 2 + 2 * capacity_entries 64-bit words, or NULL to stop tracing.  While
  * installed, every kernel of the library appends (kernel id, nanosecond timer) at the moment its

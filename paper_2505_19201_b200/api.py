@@ -90,6 +90,10 @@ def lib():
             "dream_poll": [vp],
             "dream_trace": [vp, vp, C.c_int64],
             "dream_topk_lse_static": [vp, i32, i32, i32, vp, vp, vp, vp],
+            "dream_sample": [vp, i32, i32, i32, C.c_int64] + [vp] * 9,
+            "dream_truncate_logits": [vp, i32, i32, i32, C.c_int64] + [vp] * 5 + [C.c_int64, vp, vp],
+            "dream_distill_loss": [vp, i32, i32, i32, C.c_int64, vp, vp, i32, vp, C.c_float] + [vp] * 5 + [C.c_int64, vp],
+            "dream_distill_grad": [vp, i32, i32, i32, C.c_int64, vp, vp, i32, vp, C.c_float] + [vp] * 4 + [C.c_int64, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -151,6 +155,107 @@ def dream_topk_lse_static(logits, ktop, top_val, top_id, lse, stream=None):
     with torch.cuda.device(logits.device):
         _check(None, lib().dream_topk_lse_static(_ptr(logits), rows, vocab, ktop, _ptr(top_val), _ptr(top_id), _ptr(lse),
                                                  C.c_void_p(st.cuda_stream)))
+
+
+_ROW_TYPES = {torch.float32: DREAM_F32, torch.bfloat16: DREAM_BF16}
+
+
+def _bad(msg):
+    raise DreamError(-1, msg)
+
+
+def _rows(name, t, like=None):
+    """A matrix of logits: float32 or bfloat16, two dimensions, rows of consecutive elements on a CUDA device."""
+    if t.dtype not in _ROW_TYPES or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        _bad(f"{name} must be float32 or bfloat16 [rows, vocab] with consecutive elements in a row")
+    if not t.is_cuda:
+        _bad(f"{name} must be a CUDA tensor")
+    if like is not None and (t.dtype != like.dtype or t.shape != like.shape or t.device != like.device):
+        _bad(f"{name} must be {like.dtype} of shape {tuple(like.shape)} on {like.device}")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _side(name, t, dtype, shape, device, optional=True):
+    """The address of a contiguous tensor that goes with the rows, or None."""
+    if t is None:
+        if not optional:
+            _bad(f"{name} is required")
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
+        _bad(f"{name} must be contiguous {dtype} of shape {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _call_rows(fn, device, stream, *args):
+    """Call an entry point on rows of logits with its tensors' device current, on `stream` or that device's current stream."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        _bad(f"the stream belongs to {stream.device}, the tensors to {device}")
+    if torch.cuda.current_device() == device.index:
+        code = fn(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            code = fn(*args, stream.cuda_stream)
+    if code != 0:
+        _check(None, code)
+
+
+def dream_sample(logits, uniforms, tokens, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, kept=None,
+                 stream=None):
+    """A token per row of `logits` [rows, vocab] (float32 or bfloat16; rows may be strided) under temperature, top-k, top-p and
+    min-p by row (CUDA tensors [rows]; None: not used) and one uniform number per row.  Outputs are the caller's tensors: tokens
+    [rows] int32, logprob [rows] float32, kept [rows] int32."""
+    p, ld = _rows("logits", logits)
+    R, V = logits.shape
+    dev, n, f32, i32 = logits.device, (R,), torch.float32, torch.int32
+    _call_rows(lib().dream_sample, dev, stream, p, _ROW_TYPES[logits.dtype], R, V, ld,
+               _side("temperature", temperature, f32, n, dev), _side("top_k", top_k, i32, n, dev), _side("top_p", top_p, f32, n, dev),
+               _side("min_p", min_p, f32, n, dev), _side("uniforms", uniforms, f32, n, dev, False),
+               _side("tokens", tokens, i32, n, dev, False), _side("logprob", logprob, f32, n, dev), _side("kept", kept, i32, n, dev))
+
+
+def dream_truncate_logits(logits, out, temperature=None, top_k=None, top_p=None, min_p=None, kept=None, stream=None):
+    """out = logits where a token is kept under the settings of dream_sample, -inf elsewhere; `out` may be `logits`."""
+    p, ld = _rows("logits", logits)
+    q, out_ld = _rows("out", out, logits)
+    R, V = logits.shape
+    dev, n, f32, i32 = logits.device, (R,), torch.float32, torch.int32
+    _call_rows(lib().dream_truncate_logits, dev, stream, p, _ROW_TYPES[logits.dtype], R, V, ld,
+               _side("temperature", temperature, f32, n, dev), _side("top_k", top_k, i32, n, dev), _side("top_p", top_p, f32, n, dev),
+               _side("min_p", min_p, f32, n, dev), q, out_ld, _side("kept", kept, i32, n, dev))
+
+
+def dream_distill_loss(logits, teacher_ids, teacher_logits, loss, lse, teacher_lse=None, log_rest=None, temperature=1.0,
+                       row_scale=None, grad=None, stream=None):
+    """Distillation loss per row of a student's `logits` [rows, vocab] against a teacher's top logits (teacher_ids int32 and
+    teacher_logits float32, both [rows, K], K <= 128; with teacher_lse [rows] the rest of the vocabulary counts as one bucket and
+    log_rest [rows] is an output).  Writes loss and lse [rows] and, if given, grad [rows, vocab] = row_scale * d loss / d logits."""
+    p, ld = _rows("logits", logits)
+    R, V = logits.shape
+    dev, n, f32 = logits.device, (R,), torch.float32
+    g, grad_ld = (None, 0) if grad is None else _rows("grad", grad, logits)
+    nk = (R, teacher_ids.shape[-1])
+    _call_rows(lib().dream_distill_loss, dev, stream, p, _ROW_TYPES[logits.dtype], R, V, ld,
+               _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), nk[1],
+               _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("loss", loss, f32, n, dev, False),
+               _side("lse", lse, f32, n, dev, False), _side("log_rest", log_rest, f32, n, dev),
+               _side("row_scale", row_scale, f32, n, dev), g, grad_ld)
+
+
+def dream_distill_grad(logits, teacher_ids, teacher_logits, lse, grad, teacher_lse=None, log_rest=None, temperature=1.0,
+                       row_scale=None, stream=None):
+    """The backward pass of dream_distill_loss on its own: grad = row_scale * d loss / d logits from the saved lse (and log_rest).
+    `grad` may be `logits`."""
+    p, ld = _rows("logits", logits)
+    g, grad_ld = _rows("grad", grad, logits)
+    R, V = logits.shape
+    dev, n, f32 = logits.device, (R,), torch.float32
+    nk = (R, teacher_ids.shape[-1])
+    _call_rows(lib().dream_distill_grad, dev, stream, p, _ROW_TYPES[logits.dtype], R, V, ld,
+               _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), nk[1],
+               _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("lse", lse, f32, n, dev, False),
+               _side("log_rest", log_rest, f32, n, dev), _side("row_scale", row_scale, f32, n, dev), g, grad_ld)
 
 
 class Tree:

@@ -16,9 +16,11 @@
 #include "attn_tc.cuh"
 #include "colsum_tc.cuh"
 #include "common.cuh"
+#include "distill.cuh"
 #include "gemm_simt.cuh"
 #include "gemm_tc.cuh"
 #include "rows.cuh"
+#include "sample.cuh"
 #include "tree.cuh"
 
 #define ROW_CHUNK 256          // most rows a decode call holds (max_batch * tree nodes)
@@ -1586,6 +1588,174 @@ extern "C" dream_status dream_topk_lse_static(const float *logits, int32_t rows,
   e = cudaGetLastError();
   if (e != cudaSuccess) return fail(nullptr, DREAM_E_CUDA, "k_topk_lse launch: %s", cudaGetErrorString(e));
   return DREAM_OK;
+}
+
+// ------------------------------------------------------------------------------------- rows of logits: sampling, distillation
+
+// DREAM_PDL=0 serialises every launch of the library (debugging aid).
+static bool pdl_on() {
+  static const bool on = [] { const char *p = getenv("DREAM_PDL"); return !(p && !strcmp(p, "0")); }();
+  return on;
+}
+
+// Launch of `rows` clusters on a caller's stream, of the current device.  Returns null or what went wrong.
+template <typename A>
+static const char *launch_rows(void (*kernel)(A), int rows, int cluster, int threads, size_t smem, cudaStream_t stream, const A &args) {
+  cudaError_t e = smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+  if (e == cudaSuccess) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)rows * (unsigned)cluster); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (cluster > 1) {
+      attr[n].id = cudaLaunchAttributeClusterDimension;
+      attr[n].val.clusterDim.x = (unsigned)cluster; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+      ++n;
+    }
+    if (pdl_on()) {
+      attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      attr[n].val.programmaticStreamSerializationAllowed = 1;
+      ++n;
+    }
+    cfg.attrs = attr; cfg.numAttrs = n;
+    e = cudaLaunchKernelEx(&cfg, kernel, args);
+  }
+  if (e == cudaSuccess) return nullptr;
+  cudaGetLastError();
+  return cudaGetErrorString(e);
+}
+
+// What every entry point on rows of logits asks of its matrix.
+static dream_status check_rows(const char *who, const void *p, int dtype, int rows, int vocab, long long ld, int max_vocab) {
+  if (!p) return fail(nullptr, DREAM_E_ARG, "%s: null buffer", who);
+  if (dtype != DREAM_F32 && dtype != DREAM_BF16) return fail(nullptr, DREAM_E_ARG, "%s: dtype must be DREAM_F32 or DREAM_BF16", who);
+  if (rows < 1 || vocab < 1) return fail(nullptr, DREAM_E_ARG, "%s: rows = %d, vocab = %d: both must be positive", who, rows, vocab);
+  if (vocab > max_vocab) return fail(nullptr, DREAM_E_CAPACITY, "%s: vocab = %d above %d", who, vocab, max_vocab);
+  if (rows > 1 << 24) return fail(nullptr, DREAM_E_CAPACITY, "%s: rows = %d above %d", who, rows, 1 << 24);
+  if (ld < vocab) return fail(nullptr, DREAM_E_ARG, "%s: rows of %d elements, %lld apart", who, vocab, ld);
+  if ((uintptr_t)p & (dtype == DREAM_BF16 ? 1 : 3)) return fail(nullptr, DREAM_E_ARG, "%s: a matrix is not aligned to its elements", who);
+  return DREAM_OK;
+}
+// Whether two matrices of rows x vocab share an element without being the same matrix: rows of one buffer side by side do not.
+static bool rows_collide(const void *p, long long ld, const void *q, long long qld, int dtype, int rows, int vocab) {
+  const long long esz = dtype == DREAM_BF16 ? 2 : 4, a = (long long)((uintptr_t)p / esz), b = (long long)((uintptr_t)q / esz);
+  if (a == b) return ld != qld && rows > 1;
+  if (a + (rows - 1) * ld + vocab <= b || b + (rows - 1) * qld + vocab <= a) return false;
+  if (ld != qld) return true;
+  const long long off = ((b - a) % ld + ld) % ld;
+  return off < vocab || off + vocab > ld;
+}
+static bool rows_of_16(const void *p, int dtype, int rows, long long ld) {
+  return ((uintptr_t)p & 15) == 0 && (rows == 1 || ld * (dtype == DREAM_BF16 ? 2 : 4) % 16 == 0);
+}
+
+// Fills in what follows from the sizes and launches.
+static const char *sample_launch(SampleArgs a, int dtype, int rows, bool truncate, cudaStream_t stream) {
+  a.cluster = 1;
+  while (a.vocab > a.cluster * SAMPLE_CTA_MAX) a.cluster *= 2;
+  const int share = (a.vocab + a.cluster - 1) / a.cluster, line = dtype == DREAM_BF16 ? 256 : 128;
+  const int warps = imin(32, imax(4, (share + line - 1) / line));
+  a.warp_elems = ((share + warps - 1) / warps + line - 1) / line * line;
+  a.frac_bits = imin(50, 62 - ilog2(a.vocab));
+  a.vec = rows_of_16(a.logits, dtype, rows, a.ld);
+  a.out_vec = truncate && rows_of_16(a.out, dtype, rows, a.out_ld);
+  const size_t smem = sizeof(SampleShared) + (size_t)warps * a.warp_elems * (dtype == DREAM_BF16 ? 2 : 4);
+  void (*kernel)(SampleArgs) = dtype == DREAM_BF16 ? (truncate ? k_sample<bf16, true> : k_sample<bf16, false>)
+                                                   : (truncate ? k_sample<float, true> : k_sample<float, false>);
+  return launch_rows(kernel, rows, a.cluster, warps * 32, smem, stream, a);
+}
+
+static SampleArgs sample_args(const void *logits, int vocab, long long ld, const float *temperature, const int32_t *top_k,
+                              const float *top_p, const float *min_p) {
+  SampleArgs a;
+  memset(&a, 0, sizeof(a));
+  a.logits = logits; a.vocab = vocab; a.ld = ld;
+  a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
+  a.t0 = 1.f; a.k0 = 0; a.p0 = 1.f; a.m0 = 0.f;
+  return a;
+}
+
+extern "C" dream_status dream_sample(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, const float *temperature,
+                                     const int32_t *top_k, const float *top_p, const float *min_p, const float *uniforms,
+                                     int32_t *tokens, float *logprob, int32_t *kept, void *cuda_stream) {
+  dream_status s = check_rows("dream_sample", logits, dtype, rows, vocab, ld, SAMPLE_MAX_VOCAB);
+  if (s) return s;
+  if (!uniforms || !tokens) return fail(nullptr, DREAM_E_ARG, "dream_sample: uniforms and tokens are required");
+  SampleArgs a = sample_args(logits, vocab, ld, temperature, top_k, top_p, min_p);
+  a.uniforms = uniforms; a.tokens = tokens; a.logprob = logprob; a.kept = kept;
+  const char *why = sample_launch(a, dtype, rows, false, (cudaStream_t)cuda_stream);
+  return why ? fail(nullptr, DREAM_E_CUDA, "dream_sample: %s", why) : DREAM_OK;
+}
+
+extern "C" dream_status dream_truncate_logits(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld,
+                                              const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                                              void *out, int64_t out_ld, int32_t *kept, void *cuda_stream) {
+  dream_status s = check_rows("dream_truncate_logits", logits, dtype, rows, vocab, ld, SAMPLE_MAX_VOCAB);
+  if (!s) s = check_rows("dream_truncate_logits (out)", out, dtype, rows, vocab, out_ld, SAMPLE_MAX_VOCAB);
+  if (s) return s;
+  if (rows_collide(logits, ld, out, out_ld, dtype, rows, vocab)) return fail(nullptr, DREAM_E_ARG, "dream_truncate_logits: out overlaps logits without being logits");
+  SampleArgs a = sample_args(logits, vocab, ld, temperature, top_k, top_p, min_p);
+  a.out = out; a.out_ld = out_ld; a.kept = kept;
+  const char *why = sample_launch(a, dtype, rows, true, (cudaStream_t)cuda_stream);
+  return why ? fail(nullptr, DREAM_E_CUDA, "dream_truncate_logits: %s", why) : DREAM_OK;
+}
+
+// Arguments that the forward and the backward pass have in common.
+static dream_status distill_args(const char *who, DistillArgs *a, const void *logits, int dtype, int rows, int vocab, long long ld,
+                                 const int32_t *ids, const float *teacher, int top, const float *teacher_lse, float temperature,
+                                 float *lse, float *log_rest, const float *row_scale, void *grad, long long grad_ld) {
+  dream_status s = check_rows(who, logits, dtype, rows, vocab, ld, DISTILL_MAX_VOCAB);
+  if (!s && grad) s = check_rows(who, grad, dtype, rows, vocab, grad_ld, DISTILL_MAX_VOCAB);
+  if (s) return s;
+  if (!ids || !teacher || !lse) return fail(nullptr, DREAM_E_ARG, "%s: teacher_ids, teacher_logits and lse are required", who);
+  if (top < 1 || top > DISTILL_MAX_TOP) return fail(nullptr, DREAM_E_ARG, "%s: top = %d outside 1..%d", who, top, DISTILL_MAX_TOP);
+  if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(nullptr, DREAM_E_ARG, "%s: temperature must be positive and finite", who);
+  if (!teacher_lse != !log_rest) return fail(nullptr, DREAM_E_ARG, "%s: log_rest goes with teacher_lse", who);
+  if (grad && rows_collide(logits, ld, grad, grad_ld, dtype, rows, vocab)) return fail(nullptr, DREAM_E_ARG, "%s: grad overlaps logits without being logits", who);
+  memset(a, 0, sizeof(*a));
+  a->logits = logits; a->vocab = vocab; a->ld = ld; a->ids = ids; a->teacher = teacher; a->top = top; a->teacher_lse = teacher_lse;
+  a->inv_tau = 1.0 / (double)temperature; a->lse = lse; a->log_rest = log_rest; a->row_scale = row_scale;
+  a->grad = grad; a->grad_ld = grad_ld;
+  a->vec = rows_of_16(logits, dtype, rows, ld);
+  a->grad_vec = grad && rows_of_16(grad, dtype, rows, grad_ld);
+  return DREAM_OK;
+}
+
+extern "C" dream_status dream_distill_loss(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld,
+                                           const int32_t *teacher_ids, const float *teacher_logits, int32_t top, const float *teacher_lse,
+                                           float temperature, float *loss, float *lse, float *log_rest, const float *row_scale,
+                                           void *grad, int64_t grad_ld, void *cuda_stream) {
+  DistillArgs a;
+  if (!loss) return fail(nullptr, DREAM_E_ARG, "dream_distill_loss: loss is required");
+  dream_status s = distill_args("dream_distill_loss", &a, logits, dtype, rows, vocab, ld, teacher_ids, teacher_logits, top, teacher_lse,
+                                temperature, lse, log_rest, row_scale, grad, grad_ld);
+  if (s) return s;
+  a.loss = loss;
+  a.cluster = 1;
+  while (vocab > a.cluster * DISTILL_CTA_MAX) a.cluster *= 2;
+  a.cta_elems = ((vocab + a.cluster - 1) / a.cluster + 1023) / 1024 * 1024;
+  const int esz = dtype == DREAM_BF16 ? 2 : 4, per = 16 / esz, threads = a.cta_elems * esz > 65536 ? 1024 : imax(128, imin(512, a.cta_elems / per));
+  const size_t step = (size_t)threads * per, smem = (sizeof(DistillShared) + 15) / 16 * 16 + (grad ? (a.cta_elems + step - 1) / step * step * esz : 0);
+  void (*kernel)(DistillArgs) = dtype == DREAM_BF16 ? (grad ? k_distill<bf16, true> : k_distill<bf16, false>)
+                                                    : (grad ? k_distill<float, true> : k_distill<float, false>);
+  const char *why = launch_rows(kernel, rows, a.cluster, threads, smem, (cudaStream_t)cuda_stream, a);
+  return why ? fail(nullptr, DREAM_E_CUDA, "dream_distill_loss: %s", why) : DREAM_OK;
+}
+
+extern "C" dream_status dream_distill_grad(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld,
+                                           const int32_t *teacher_ids, const float *teacher_logits, int32_t top, const float *teacher_lse,
+                                           float temperature, const float *lse, const float *log_rest, const float *row_scale,
+                                           void *grad, int64_t grad_ld, void *cuda_stream) {
+  DistillArgs a;
+  if (!grad) return fail(nullptr, DREAM_E_ARG, "dream_distill_grad: grad is required");
+  dream_status s = distill_args("dream_distill_grad", &a, logits, dtype, rows, vocab, ld, teacher_ids, teacher_logits, top, teacher_lse,
+                                temperature, const_cast<float *>(lse), const_cast<float *>(log_rest), row_scale, grad, grad_ld);
+  if (s) return s;
+  const int chunk = DISTILL_GRAD_THREADS * DISTILL_GRAD_VECS * (dtype == DREAM_BF16 ? 8 : 4), chunks = (vocab + chunk - 1) / chunk;
+  void (*kernel)(DistillArgs) = dtype == DREAM_BF16 ? k_distill_grad<bf16> : k_distill_grad<float>;
+  if ((long long)rows * chunks > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "dream_distill_grad: %d rows of %d logits in one call", rows, vocab);
+  const char *why = launch_rows(kernel, rows * chunks, 1, DISTILL_GRAD_THREADS, 0, (cudaStream_t)cuda_stream, a);
+  return why ? fail(nullptr, DREAM_E_CUDA, "dream_distill_grad: %s", why) : DREAM_OK;
 }
 
 static const char *const g_trace_names[] = DREAM_TRACE_NAMES;
