@@ -148,6 +148,14 @@ dream_status dream_prefill(dream_ctx *ctx, int32_t seq, const void *visual_embed
 /* Override l* of a prefilled sequence (1-based) before dream_compress_visual. */
 dream_status dream_set_tap(dream_ctx *ctx, int32_t seq, int32_t tap_layer);
 
+/* Draws the first token of a prefilled sequence from its prompt's last logits instead of taking the largest (Section 4 reports
+ * Temp = 1, at which every emitted token is a draw), under the rules of dream_sample with one setting each: temperature > 0
+ * (DREAM_E_ARG otherwise), top_k <= 0, top_p >= 1 and min_p <= 0 switch off.  It replaces the pending token that dream_prefill set; call it
+ * before dream_compress_visual (DREAM_E_STATE otherwise).  uniform: device float[1] in [0, 1).  Outputs (device, may be NULL): first_token
+ * int32[1], logprob float[1].  Vocabularies up to 262144 (DREAM_E_UNSUPPORTED above). */
+dream_status dream_sample_first(dream_ctx *ctx, int32_t seq, float temperature, int32_t top_k, float top_p, float min_p,
+                                const float *uniform, int32_t *first_token, float *logprob);
+
 /* Visual-token compression (Section 3.3): importance of visual token j = attention it
  * receives at layer l* summed over query rows and heads; the k highest are kept.  Builds
  * the draft's compressed context (self-attention K/V from input embeddings, cross-attention

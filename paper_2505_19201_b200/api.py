@@ -90,6 +90,7 @@ def lib():
             "dream_poll": [vp],
             "dream_trace": [vp, vp, C.c_int64],
             "dream_topk_lse_static": [vp, i32, i32, i32, vp, vp, vp, vp],
+            "dream_sample_first": [vp, i32, C.c_float, i32, C.c_float, C.c_float, vp, vp, vp],
             "dream_sample": [vp, i32, i32, i32, C.c_int64] + [vp] * 9,
             "dream_truncate_logits": [vp, i32, i32, i32, C.c_int64] + [vp] * 5 + [C.c_int64, vp, vp],
             "dream_distill_loss": [vp, i32, i32, i32, C.c_int64, vp, vp, i32, vp, C.c_float] + [vp] * 5 + [C.c_int64, vp],
@@ -359,6 +360,11 @@ class Context:
 
     def dream_set_tap(self, seq, layer):
         _check(self.h, lib().dream_set_tap(self.h, seq, layer))
+
+    def dream_sample_first(self, seq, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, first_token=None, logprob=None):
+        """uniform: CUDA float32 tensor with one number in [0, 1)."""
+        _check(self.h, lib().dream_sample_first(self.h, seq, float(temperature), int(top_k), float(top_p), float(min_p), _ptr(uniform),
+                                                _ptr(first_token), _ptr(logprob)))
 
     def dream_compress_visual(self, seq, k, forced_idx=None, kept_idx=None, scores=None):
         _check(self.h, lib().dream_compress_visual(self.h, seq, k, _ptr(forced_idx), _ptr(kept_idx), _ptr(scores)))

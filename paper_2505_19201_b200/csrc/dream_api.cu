@@ -90,6 +90,7 @@ struct dream_ctx {
   int last_verify_n, last_verify_seq[DREAM_MAX_BATCH];   // the sequence list of the last dream_verify_tree
   int cur_seq[DREAM_MAX_BATCH];        // sequences of the call being enqueued, by slot
   int tk_nsplit;                       // most vocabulary blocks of the top-k kernel
+  float *first_logits;                 // of the last prompt row of the latest prefill (dream_sample_first)
   int *top_id, *argmax_i, *accept_len_i, *out_tokens_i, *comp_src_i;
   size_t gout_floats;
   // host side
@@ -410,6 +411,7 @@ static size_t carve(dream_ctx *c, char *base) {
   c->tks.pm = a.take<float>((size_t)ROW_CHUNK * c->tk_nsplit);
   c->tks.pz = a.take<float>((size_t)ROW_CHUNK * c->tk_nsplit);
   c->tks.counter = a.take<int>(ROW_CHUNK);
+  c->first_logits = a.take<float>(f.vocab);
   c->argmax_i = a.take<int>(ROW_CHUNK);
   c->margin_i = a.take<float>(ROW_CHUNK);
   c->accept_len_i = a.take<int>(MB);
@@ -1009,7 +1011,7 @@ static dream_status prefill_impl(dream_ctx *c, int seq, const void *visual, int 
   // first token: LM head on the last prompt row
   norm_rows<T>(c, c->x + (size_t)(n - 1) * d, NO_GEMM, false, c->ln_f, 1, mp);
   GemmOut g = gemm<T>(c, c->lm_head, c->xn, mp, 1, f.vocab, d);
-  TOPK_LAUNCH(c, 1, g, 2, (float *)nullptr);
+  TOPK_LAUNCH(c, 1, g, 2, c->first_logits);
   LAUNCH(c, k_first_token, 1, 32, 0, c->top_id, c->top_val, first_token, first_margin);
   LAUNCH(c, k_set_seq, 1, 32, 0, c->sd, seq, n, c->top_id, -1, -1);
   LAUNCH(c, k_select_tap, 1, 32, 0, c->ae, f.tap_mode, f.tap_layer, f.tap_lo, f.tap_hi, c->sd.tap + seq, tap_layer);
@@ -1698,6 +1700,24 @@ extern "C" dream_status dream_truncate_logits(const void *logits, int32_t dtype,
   a.out = out; a.out_ld = out_ld; a.kept = kept;
   const char *why = sample_launch(a, dtype, rows, true, (cudaStream_t)cuda_stream);
   return why ? fail(nullptr, DREAM_E_CUDA, "dream_truncate_logits: %s", why) : DREAM_OK;
+}
+
+extern "C" dream_status dream_sample_first(dream_ctx *c, int32_t seq, float temperature, int32_t top_k, float top_p, float min_p,
+                                           const float *uniform, int32_t *first_token, float *logprob) {
+  dream_status s = check_seq(c, seq);
+  if (s) return s;
+  if (!uniform) return fail(c, DREAM_E_ARG, "dream_sample_first: uniform is required");
+  if (!(temperature > 0.f)) return fail(c, DREAM_E_ARG, "temperature must be above zero (dream_prefill's own token is the greedy one)");
+  if (c->phase[seq] != PH_PREFILLED || c->prefill_seq != seq) return fail(c, DREAM_E_STATE, "dream_sample_first follows dream_prefill of the same sequence");
+  if (c->cfg.vocab > SAMPLE_MAX_VOCAB) return fail(c, DREAM_E_UNSUPPORTED, "dream_sample_first: vocab above %d", SAMPLE_MAX_VOCAB);
+  SampleArgs a = sample_args(c->first_logits, c->cfg.vocab, c->cfg.vocab, nullptr, nullptr, nullptr, nullptr);
+  a.t0 = temperature; a.k0 = top_k; a.p0 = top_p; a.m0 = min_p;
+  a.uniforms = uniform; a.tokens = c->sd.pending + seq; a.logprob = logprob; a.status = c->status;
+  const char *why = sample_launch(a, DREAM_F32, 1, false, c->stream);
+  if (why) return fail(c, DREAM_E_CUDA, "dream_sample_first: %s", why);
+  c->launches++;
+  if (first_token) LAUNCH(c, k_copy_f32, 1, 32, 0, (const float *)(c->sd.pending + seq), (float *)first_token, 1);
+  return call_done(c);
 }
 
 // Arguments that the forward and the backward pass have in common.

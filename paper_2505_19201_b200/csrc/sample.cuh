@@ -40,6 +40,7 @@ struct SampleArgs {
   int *tokens;
   float *logprob;                      // may be null
   int *kept;                           // may be null
+  int *status;                         // of a context, or null: a row without mass then raises it and gives token 0
   void *out;
   long long out_ld;
 };
@@ -431,7 +432,8 @@ k_sample(const __grid_constant__ SampleArgs a) {
   }
   if (!(m > -INFINITY)) {                                   // nothing to draw from
     if (rank == 0 && threadIdx.x == 0) {
-      a.tokens[row] = -1;
+      a.tokens[row] = a.status ? 0 : -1;
+      if (a.status) atomicMax(a.status, DREAM_DEV_BAD_INDEX);
       if (a.logprob) a.logprob[row] = -INFINITY;
       if (a.kept) a.kept[row] = 0;
     }
