@@ -345,7 +345,8 @@ dream_status dream_truncate_logits(const void *logits, int32_t dtype, int32_t ro
                                    int32_t *kept, void *cuda_stream);
 
 /* Distillation of a draft from the target's top logits: Kullback-Leibler divergence of a student's rows from a teacher of which the top
- * logits were kept (dream_topk_lse_static makes them).  z = logits / temperature, p = softmax(z), lse = log-sum-exp of z.
+ * logits were kept (dream_topk_lse_static makes them).  z = logits / temperature, p = softmax(z), lse = log-sum-exp of z; temperature in
+ * 1e-20..1e20.
  *   teacher_ids int32 [rows][top], teacher_logits float [rows][top] : device, top in 1..128; an id outside [0, vocab) is no entry;
  *            an id may come twice (its probabilities add up)
  *   teacher_lse : device float [rows], log-sum-exp of the teacher's whole row at this temperature, or NULL.

@@ -73,280 +73,377 @@ template <typename T, int VEC> __device__ __forceinline__ void store_vec(T *row,
   for (int e = 0; e < VEC; ++e) if (i + e < n) row[i + e] = t[e];
 }
 
-// The teacher's side of a row, by the first DISTILL_MAX_TOP threads of a block of at least as many.
-struct Teacher {
-  double q[DISTILL_MAX_TOP];           // 0 for no entry
-  int id[DISTILL_MAX_TOP];             // -1 for no entry
-  double part[4][2];
-  double rest, total;                  // q_r and Q
-};
-// Ends in a barrier: q, id, rest and total are there.
-__device__ __forceinline__ void teacher_row(const DistillArgs &a, int row, Teacher &t) {
-  const int j = threadIdx.x, lane = j & 31, warp = j >> 5;
-  double x = -INFINITY, e = 0.0;
-  int id = -1;
-  if (j < DISTILL_MAX_TOP) {
-    if (j < a.top) {
-      id = a.ids[(long long)row * a.top + j];
-      if (id < 0 || id >= a.vocab) id = -1;
-      else x = (double)a.teacher[(long long)row * a.top + j] * a.inv_tau;
-    }
-    t.id[j] = id;
-    if (a.teacher_lse) e = exp(x - (double)a.teacher_lse[row]);
-    else {
-      double m = x;
+// Two sums, products and both at once per instruction.
+__device__ __forceinline__ unsigned long long pair_bits(float2 v) {
+  unsigned long long u;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(u) : "f"(v.x), "f"(v.y));
+  return u;
+}
+__device__ __forceinline__ float2 pair_of(unsigned long long u) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(u));
+  return v;
+}
+__device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+  return pair_of(r);
+}
+__device__ __forceinline__ float2 mul_pair(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+  return pair_of(r);
+}
+__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
+  return pair_of(r);
+}
+// The largest of a vector's elements (NaN does not count).
+template <typename T, int VEC> __device__ __forceinline__ float max_vec(const uint4 &q) {
+  if constexpr (sizeof(T) == 4)
+    return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+  else {
+    const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&q);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+}
+__device__ __forceinline__ double warp_sum_d(double v) {
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if (lane == 0) t.part[warp][0] = m;
-    }
-  }
-  if (!a.teacher_lse) {
-    __syncthreads();
-    if (j < DISTILL_MAX_TOP) {
-      const double m = fmax(fmax(t.part[0][0], t.part[1][0]), fmax(t.part[2][0], t.part[3][0]));
-      e = x > -INFINITY ? exp(x - m) : 0.0;
-    }
-  }
-  if (j < DISTILL_MAX_TOP) {
-    if (id < 0) e = 0.0;
-    double s = e;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) t.part[warp][1] = s;
-  }
-  __syncthreads();
-  const double s = t.part[0][1] + t.part[1][1] + t.part[2][1] + t.part[3][1];
-  const bool tail = a.teacher_lse != nullptr;
-  const bool any = !(s == 0.0);                              // a row with no valid entry has no loss, with or without the rest
-  if (j < DISTILL_MAX_TOP) t.q[j] = tail || !any ? e : e / s;
-  if (j == 0) {
-    t.rest = tail && any ? fmax(0.0, 1.0 - s) : 0.0;
-    t.total = tail ? (any ? s + t.rest : 0.0) : any ? 1.0 : 0.0;
-  }
-  __syncthreads();
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
 }
 
-struct DistillShared {
-  Teacher teacher;
-  uint32_t bits[DISTILL_CTA_MAX / 32];     // ids of this CTA's share that are listed
-  float warp_m[32], warp_s[32];
-  double share[DISTILL_MAX_CLUSTER][4];    // of every CTA: maximum, sum over the others, sum over the listed, sum of q s
-  uint32_t first[DISTILL_MAX_TOP];         // entry j is the one that stands for its id here
-  float m, d2, coef;                       // row maximum, (lse - m / tau) log2 e, factor of e of an id that is not listed
-  double lse, scale;
-  int repeated;
+// The teacher's side of a row: entry j belongs to thread j of the first DISTILL_TOP_WARPS warps.  Each warp leaves its sums relative to its
+// own largest entry, and whoever needs the row's puts the four together.
+#define DISTILL_TOP_WARPS (DISTILL_MAX_TOP / 32)
+struct Entry {
+  int id;                              // -1: no entry
+  double x, e;                         // t / tau; e^(x - the warp's reference), with teacher_lse q itself
 };
+struct TeacherSums {                   // by warp: reference, sum of e, sum of e ln e (with teacher_lse) or e x
+  double ref[DISTILL_TOP_WARPS], sum[DISTILL_TOP_WARPS], log[DISTILL_TOP_WARPS];
+};
+struct TeacherRow {
+  double f[DISTILL_TOP_WARPS];         // q_j = e_j f of its warp
+  double rest, total, shift;           // q_r; Q; sum q ln q = sum of f log, minus shift
+  __device__ __forceinline__ double mine() const {
+    double v = 0.0;
+#pragma unroll
+    for (int w = 0; w < DISTILL_TOP_WARPS; ++w) if (w == (int)(threadIdx.x >> 5)) v = f[w];
+    return v;
+  }
+};
+__device__ __forceinline__ Entry load_entry(const DistillArgs &a, int row) {
+  const int j = threadIdx.x;
+  Entry t = {-1, -INFINITY, 0.0};
+  if (j < a.top) {
+    const int id = a.ids[(long long)row * a.top + j];
+    const float x = a.teacher[(long long)row * a.top + j];
+    if (id >= 0 && id < a.vocab) { t.id = id; t.x = (double)x * a.inv_tau; }
+  }
+  return t;
+}
+// By the first DISTILL_TOP_WARPS warps.
+__device__ __forceinline__ void teacher_sums(const DistillArgs &a, int row, Entry &t, TeacherSums &sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  double ref, y = t.x;
+  if (a.teacher_lse) {
+    ref = (double)a.teacher_lse[row];
+    y = t.x - ref;
+  } else {
+    ref = t.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ref = fmax(ref, __shfl_xor_sync(0xffffffffu, ref, o));
+  }
+  if (t.id >= 0 && t.x != -INFINITY) t.e = exp(t.x - ref);
+  const double s = warp_sum_d(t.e), l = warp_sum_d(t.e == 0.0 ? 0.0 : t.e * y);
+  if (lane == 0) { sh.ref[warp] = ref; sh.sum[warp] = s; sh.log[warp] = l; }
+}
+__device__ __forceinline__ TeacherRow teacher_row(const DistillArgs &a, const TeacherSums &sh) {
+  TeacherRow r;
+  double s = 0.0, m = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < DISTILL_TOP_WARPS; ++w) {
+    r.f[w] = 1.0;
+    if (!a.teacher_lse) m = fmax(m, sh.ref[w]);
+  }
+#pragma unroll
+  for (int w = 0; w < DISTILL_TOP_WARPS; ++w) {
+    if (!a.teacher_lse && sh.ref[w] != m) r.f[w] = exp(sh.ref[w] - m);
+    s += sh.sum[w] * r.f[w];
+  }
+  const bool any = !(s == 0.0);                             // a row with no valid entry has no loss, with or without the rest
+  if (a.teacher_lse) {
+    r.rest = any ? fmax(0.0, 1.0 - s) : 0.0;
+    r.total = any ? s + r.rest : 0.0;
+    r.shift = 0.0;
+  } else {
+#pragma unroll
+    for (int w = 0; w < DISTILL_TOP_WARPS; ++w) r.f[w] = any ? r.f[w] / s : 0.0;
+    r.rest = 0.0;
+    r.total = any ? 1.0 : 0.0;
+    r.shift = any ? m + log(s) : 0.0;
+  }
+  return r;
+}
+
+// A CTA's part in the row's sums, which are of 2^((l - m) ch), ch = log2(e) / tau.  (l ch - m ch in one instruction would overflow on rows
+// masked with the type's lowest value.)
+struct DistillPart {
+  float m, unused;                     // largest logit, -inf without one
+  double others, tops, qz;             // sums over the ids that are not listed, that are; sum of q_j z_j tau
+};
+struct DistillShared {
+  DistillPart part[DISTILL_MAX_CLUSTER];
+  TeacherSums teacher;
+  double q[DISTILL_MAX_TOP], qz[DISTILL_TOP_WARPS], scale, total;
+  float top_m[DISTILL_TOP_WARPS], top_s[DISTILL_TOP_WARPS], warp_m[32], warp_s[32], m, d, coef;
+  int id[DISTILL_MAX_TOP], repeated;
+  uint32_t bits[1];                    // one per id of this CTA's share: is it listed?
+};
+__host__ __device__ inline size_t distill_row_offset(int cta_elems) { return (sizeof(DistillShared) + (size_t)cta_elems / 8 + 15) / 16 * 16; }
 
 // GRAD: the row stays in shared memory and its gradient leaves in the same pass.
+#define DISTILL_THREADS 512
 template <typename T, bool GRAD>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(DISTILL_THREADS, 3)
 k_distill(const __grid_constant__ DistillArgs a) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   DistillShared &sh = *reinterpret_cast<DistillShared *>(smem_raw);
-  uint4 *vals = reinterpret_cast<uint4 *>(smem_raw + (sizeof(DistillShared) + 15) / 16 * 16);
-  constexpr int VEC = 16 / sizeof(T);
+  uint4 *vals = reinterpret_cast<uint4 *>(smem_raw + distill_row_offset(a.cta_elems));
+  constexpr int VEC = 16 / sizeof(T), U = 4;
   cluster_started_arrive(a.cluster);
   kernel_entry(TR_k_distill);
   const int rank = a.cluster > 1 ? (int)cluster_ctarank() : 0, row = blockIdx.x / a.cluster, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5,
-            nw = blockDim.x >> 5, base = rank * a.cta_elems, n = min(a.cta_elems, a.vocab - base);   // n may be negative: an empty share
+            nt = blockDim.x, nw = nt >> 5, base = rank * a.cta_elems, n = max(0, min(a.cta_elems, a.vocab - base));
   const T *src = (const T *)a.logits + row * a.ld + base;
-  T *dst = GRAD ? (T *)a.grad + row * a.grad_ld + base : nullptr;
-  const float c2 = (float)(a.inv_tau * 1.4426950408889634), scale = a.row_scale ? a.row_scale[row] : 1.f;
-  for (int i = tid; i < a.cta_elems / 32; i += blockDim.x) sh.bits[i] = 0;
+  const float ch = (float)(a.inv_tau * 1.4426950408889634);
+  const bool tail = a.teacher_lse != nullptr, top_warp = warp < DISTILL_TOP_WARPS;
+  const int steps = (n + nt * VEC - 1) / (nt * VEC);
+  uint4 q[U];
+#pragma unroll
+  for (int k = 0; k < U; ++k) q[k] = load_vec<T, VEC>(src, (k * nt + tid) * VEC, n, a.vec, -INFINITY);
+  Entry t = {-1, -INFINITY, 0.0};
+  if (top_warp) { t = load_entry(a, row); sh.id[tid] = t.id; }
+  for (int i = tid; i < a.cta_elems / 32; i += nt) sh.bits[i] = 0;
   if (tid == 0) sh.repeated = 0;
-  teacher_row(a, row, sh.teacher);
-  if (tid < DISTILL_MAX_TOP) {
-    const int id = sh.teacher.id[tid] - base;
-    bool mine = sh.teacher.id[tid] >= 0 && id >= 0 && id < n;
-    if (mine && (atomicOr(&sh.bits[id >> 5], 1u << (id & 31)) >> (id & 31) & 1u)) { mine = false; sh.repeated = 1; }
-    sh.first[tid] = mine;
+  __syncthreads();
+  const bool mine = top_warp && t.id >= base && t.id < base + n;
+  float z = -INFINITY;
+  if (mine) {
+    const int i = t.id - base;
+    z = to_f(src[i]);
+    if (atomicOr(&sh.bits[i >> 5], 1u << (i & 31)) >> (i & 31) & 1u) sh.repeated = 1;
   }
   __syncthreads();
-  // running maximum and sum of the ids that are not listed
-  float m = -INFINITY, s = 0.f;
-  const int steps = (max(n, 0) + blockDim.x * VEC - 1) / (blockDim.x * VEC);
-  constexpr int U = 4;
+  bool first = mine;                                        // of the entries of one id the first stands for it
+  if (mine && sh.repeated)
+    for (int j = 0; j < tid; ++j) if (sh.id[j] == t.id) first = false;
+  // running maximum m (ref: the same, 0 without one) and sum of 2^((l - ref) ch); listed ids stay out where the rest is a bucket
+  float m = -INFINITY, ref = 0.f, s = 0.f, s1 = 0.f;
   for (int j0 = 0; j0 < steps; j0 += U) {
-    uint4 q[U];
+    if (j0) {
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const int i = ((j0 + k) * blockDim.x + tid) * VEC;
-      if (j0 + k < steps) q[k] = load_vec<T, VEC>(src, i, n, a.vec, -INFINITY);
+      for (int k = 0; k < U; ++k) q[k] = load_vec<T, VEC>(src, ((j0 + k) * nt + tid) * VEC, n, a.vec, -INFINITY);
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      if (j0 + k >= steps) break;
-      const int i = ((j0 + k) * blockDim.x + tid) * VEC;
-      float l[VEC];
+      const int i = ((j0 + k) * nt + tid) * VEC;
+      if (i >= n) break;
+      if (GRAD) vals[(j0 + k) * nt + tid] = q[k];
+      float l[VEC], v;
+      const uint32_t b = tail ? sh.bits[i >> 5] >> (i & 31) & ((1u << VEC) - 1u) : 0u;
       unpack_vec<T, VEC>(q[k], l);
-      if (GRAD) vals[(j0 + k) * blockDim.x + tid] = q[k];
-      if (i < n) {
-        const uint32_t b = sh.bits[i >> 5] >> (i & 31);
-        if (b & ((1u << VEC) - 1u)) {
+      if (b) {
+        v = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) if (b >> e & 1u) l[e] = -INFINITY;
-        }
-        float v = l[0];
+        for (int e = 0; e < VEC; ++e) { if (b >> e & 1u) l[e] = -INFINITY; v = fmaxf(v, l[e]); }
+      } else v = max_vec<T, VEC>(q[k]);
+      if (v > m) {
+        if (m > -INFINITY) { const float f = ex2((m - v) * ch); s *= f; s1 *= f; }
+        m = ref = v;
+      }
 #pragma unroll
-        for (int e = 1; e < VEC; ++e) v = fmaxf(v, l[e]);
-        if (v > m) { s *= ex2((m - v) * c2); m = v; }
-        if (m > -INFINITY) {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) s += ex2((l[e] - m) * c2);
-        } else {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) if (l[e] != l[e]) s = l[e];      // NaN is not lost where nothing else is there
-        }
+      for (int e = 0; e < VEC; e += 2) {
+        const float2 y = mul_pair(add_pair(make_float2(l[e], l[e + 1]), make_float2(-ref, -ref)), make_float2(ch, ch));
+        s += ex2(y.x); s1 += ex2(y.y);
       }
     }
   }
+  if (top_warp) {
+    teacher_sums(a, row, t, sh.teacher);
+    const float tm = warp_max(z);
+    const float ts = warp_sum(first ? ex2((z - (tm > -INFINITY ? tm : 0.f)) * ch) : 0.f);
+    const double qz = warp_sum_d(mine && !(t.e == 0.0) ? t.e * (double)z : 0.0);
+    if (lane == 0) { sh.top_m[warp] = tm; sh.top_s[warp] = ts; sh.qz[warp] = qz; }
+  }
   {
     const float wm = warp_max(m);
-    s = warp_sum(m > -INFINITY ? s * ex2((m - wm) * c2) : s);          // s is 0, or NaN, without a maximum
+    s = warp_sum((s + s1) * (m > -INFINITY ? ex2((m - wm) * ch) : 1.f));        // without a maximum 0, or NaN
     if (lane == 0) { sh.warp_m[warp] = wm; sh.warp_s[warp] = s; }
   }
   __syncthreads();
   cluster_started_wait(a.cluster);
+  TeacherRow tr;
+  if (top_warp) tr = teacher_row(a, sh.teacher);
   if (warp == 0) {
-    float wm = lane < nw ? sh.warp_m[lane] : -INFINITY, ws = lane < nw ? sh.warp_s[lane] : 0.f;
-    float cm = warp_max(wm), z[DISTILL_MAX_TOP / 32];
-    double qs = 0.0, tops = 0.0;
+    const float wm = lane < nw ? sh.warp_m[lane] : -INFINITY, ws = lane < nw ? sh.warp_s[lane] : 0.f;
+    const float tm = lane < DISTILL_TOP_WARPS ? sh.top_m[lane] : -INFINITY, ts = lane < DISTILL_TOP_WARPS ? sh.top_s[lane] : 0.f;
+    const float cm = warp_max(fmaxf(wm, tm));
+    const double others = warp_sum_d((double)(ws * (wm > -INFINITY ? ex2((wm - cm) * ch) : 1.f)));
+    const double tops = warp_sum_d((double)(ts * (tm > -INFINITY ? ex2((tm - cm) * ch) : 1.f)));
+    double qz = 0.0;
 #pragma unroll
-    for (int k = 0; k < DISTILL_MAX_TOP / 32; ++k) {
-      const int id = sh.teacher.id[k * 32 + lane] - base;
-      const bool mine = sh.teacher.id[k * 32 + lane] >= 0 && id >= 0 && id < n;
-      z[k] = -INFINITY;
-      if (mine) {
-        z[k] = to_f(src[id]);
-        if (sh.teacher.q[k * 32 + lane] > 0.0) qs += sh.teacher.q[k * 32 + lane] * (double)z[k];
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < DISTILL_MAX_TOP / 32; ++k) cm = fmaxf(cm, warp_max(z[k]));
-#pragma unroll
-    for (int k = 0; k < DISTILL_MAX_TOP / 32; ++k)
-      if (z[k] > -INFINITY && sh.first[k * 32 + lane]) tops += exp(((double)z[k] - (double)cm) * a.inv_tau);
-    double others = wm > -INFINITY ? (double)ws * exp(((double)wm - (double)cm) * a.inv_tau) : (double)ws;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      qs += __shfl_xor_sync(0xffffffffu, qs, o);
-      tops += __shfl_xor_sync(0xffffffffu, tops, o);
-      others += __shfl_xor_sync(0xffffffffu, others, o);
-    }
+    for (int w = 0; w < DISTILL_TOP_WARPS; ++w) if (!(sh.qz[w] == 0.0)) qz += sh.qz[w] * tr.f[w];
     if (lane < a.cluster) {
-      const uint32_t to = mapa_of(a.cluster, smem_u32(&sh.share[rank][0]), lane);
-      st_cluster_u64(to, __double_as_longlong((double)cm)); st_cluster_u64(to + 8, __double_as_longlong(others));
-      st_cluster_u64(to + 16, __double_as_longlong(tops)); st_cluster_u64(to + 24, __double_as_longlong(qs));
+      const uint32_t to = mapa_of(a.cluster, smem_u32(&sh.part[rank]), lane);
+      st_cluster_u64(to, (unsigned long long)__float_as_uint(cm));
+      st_cluster_u64(to + 8, __double_as_longlong(others));
+      st_cluster_u64(to + 16, __double_as_longlong(tops));
+      st_cluster_u64(to + 24, __double_as_longlong(qz));
     }
   }
   sync_all_of(a.cluster);
-  const Teacher &t = sh.teacher;
+  // the row's sums, by each warp that needs them
+  float rm = -INFINITY;
+  double others = 0.0, tops = 0.0, qz = 0.0;
   if (warp == 0) {
-    double qlq = 0.0;
-    if (rank == 0) {
-#pragma unroll
-      for (int k = 0; k < DISTILL_MAX_TOP / 32; ++k) { const double q = t.q[k * 32 + lane]; if (q > 0.0) qlq += q * log(q); }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) qlq += __shfl_xor_sync(0xffffffffu, qlq, o);
+    for (int c = 0; c < a.cluster; ++c) rm = fmaxf(rm, sh.part[c].m);
+    for (int c = 0; c < a.cluster; ++c) {
+      const DistillPart &p = sh.part[c];
+      const double f = p.m > -INFINITY ? (double)ex2((p.m - rm) * ch) : 1.0;
+      others += p.others * f; tops += p.tops * f; qz += p.qz;
     }
-    if (lane == 0) {
-      double rm = -INFINITY, others = 0.0, tops = 0.0, qs = 0.0;
-      for (int q = 0; q < a.cluster; ++q) rm = fmax(rm, sh.share[q][0]);
-      for (int q = 0; q < a.cluster; ++q) {
-        const double f = sh.share[q][0] > -INFINITY ? exp((sh.share[q][0] - rm) * a.inv_tau) : 1.0;
-        others += sh.share[q][1] * f; tops += sh.share[q][2] * f; qs += sh.share[q][3];
+    if (!tail) tops = 0.0;                                  // they are among the others
+  }
+  const double total = others + tops;
+  const bool none = total == 0.0;                           // no finite logit
+  if (GRAD) {
+    if (top_warp && mine) sh.q[tid] = t.e * tr.mine();
+    if (tid == 0) {
+      const double scale = none || tr.total == 0.0 ? 0.0 : (double)(a.row_scale ? a.row_scale[row] : 1.f) * a.inv_tau;
+      sh.scale = scale;
+      sh.m = none ? 0.f : rm; sh.d = log2f((float)total);
+      sh.coef = scale == 0.0 ? 0.f : (float)(scale * (tr.total - (tr.rest > 0.0 && others > 0.0 ? tr.rest * (total / others) : 0.0)));
+    }
+    __syncthreads();
+    const double scale = sh.scale;
+    const float ref = sh.m, d = sh.d, coef = sh.coef;
+    T *dst = (T *)a.grad + row * a.grad_ld + base;
+    if (scale == 0.0) {                                     // padding: zeros, whatever the logits hold
+      for (int i = tid * VEC; i < n; i += nt * VEC) store_vec<T, VEC>(dst, i, n, a.grad_vec, make_uint4(0u, 0u, 0u, 0u));
+    } else {
+      for (int j = 0; j < steps; ++j) {
+        const int i = (j * nt + tid) * VEC;
+        if (i >= n) break;
+        float l[VEC], g[VEC];
+        unpack_vec<T, VEC>(vals[j * nt + tid], l);
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) {
+          const float2 y = fma_pair(add_pair(make_float2(l[e], l[e + 1]), make_float2(-ref, -ref)), make_float2(ch, ch), make_float2(-d, -d));
+          const float2 o = mul_pair(make_float2(ex2(y.x), ex2(y.y)), make_float2(coef, coef));
+          g[e] = o.x; g[e + 1] = o.y;
+        }
+        store_vec<T, VEC>(dst, i, n, a.grad_vec, pack_vec<T, VEC>(g));
       }
-      const double total = others + tops, lz = log(total);               // relative to the row's maximum
-      const double lse = rm * a.inv_tau + lz;
+      __syncthreads();                                      // the listed ids' own gradients replace what was written
+      if (first) {
+        double qj = sh.q[tid];
+        if (sh.repeated) {
+          qj = 0.0;
+          for (int j = 0; j < a.top; ++j) if (sh.id[j] == t.id) qj += sh.q[j];
+        }
+        dst[t.id - base] = from_f<T>((float)(scale * (tr.total * (double)ex2(fmaf(z - ref, ch, -d)) - qj)));
+      }
+    }
+  }
+  if (rank == 0 && tid == 0) {
+    const double lse = (double)rm * a.inv_tau + log(total);
+    double loss = -tr.shift - qz * a.inv_tau + (tr.total - tr.rest) * lse;
+#pragma unroll
+    for (int w = 0; w < DISTILL_TOP_WARPS; ++w) if (!(sh.teacher.log[w] == 0.0)) loss += sh.teacher.log[w] * tr.f[w];
+    if (tail) {
       const double log_rest = others > 0.0 ? -log1p(tops / others) : others == 0.0 ? -INFINITY : others;
-      const bool none = total == 0.0;                                    // no finite logit
-      if (rank == 0) {
-        double loss = qlq - qs * a.inv_tau + (t.total - t.rest) * lse;
-        if (t.rest > 0.0) loss += t.rest * (log(t.rest) - log_rest);
-        if (none) loss = t.total > 0.0 ? INFINITY : 0.0;
-        if (t.total == 0.0) loss = 0.0;
-        a.loss[row] = (float)loss;
-        a.lse[row] = none ? -INFINITY : (float)lse;
-        if (a.teacher_lse) a.log_rest[row] = none ? -INFINITY : (float)log_rest;
-      }
-      if (GRAD) {
-        const double sc = none ? 0.0 : (double)scale * a.inv_tau;
-        sh.m = none ? 0.f : (float)rm;
-        sh.d2 = none ? 0.f : (float)(lz * 1.4426950408889634);
-        sh.lse = lse;
-        sh.scale = t.total == 0.0 ? 0.0 : sc;
-        sh.coef = t.total == 0.0 || sc == 0.0 ? 0.f : (float)(sc * (t.total - (t.rest > 0.0 && others > 0.0 ? t.rest * (total / others) : 0.0)));
-      }
+      if (tr.rest > 0.0) loss += tr.rest * (log(tr.rest) - log_rest);
+      a.log_rest[row] = none ? -INFINITY : (float)log_rest;
     }
-  }
-  if (!GRAD) return;
-  __syncthreads();
-  const float rm = sh.m, d2 = sh.d2, coef = sh.coef;
-  const bool zero = sh.scale == 0.0;                                     // padding: zeros, whatever the logits hold
-  for (int j = 0; j < steps; ++j) {
-    const int i = (j * blockDim.x + tid) * VEC;
-    float l[VEC], g[VEC];
-    unpack_vec<T, VEC>(vals[j * blockDim.x + tid], l);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) g[e] = zero ? 0.f : coef * ex2(fmaf(l[e] - rm, c2, -d2));
-    if (i < n) store_vec<T, VEC>(dst, i, n, a.grad_vec, pack_vec<T, VEC>(g));
-  }
-  if (zero) return;
-  __syncthreads();                                                       // the listed ids' own gradients replace what was written
-  if (tid < DISTILL_MAX_TOP && sh.first[tid]) {
-    const int id = t.id[tid];
-    double q = t.q[tid];
-    if (sh.repeated) {
-      q = 0.0;
-      for (int j = 0; j < a.top; ++j) if (t.id[j] == id) q += t.q[j];
-    }
-    const double z = (double)to_f(reinterpret_cast<const T *>(vals)[id - base]) * a.inv_tau;
-    dst[id - base] = from_f<T>((float)(sh.scale * (t.total * exp(z - sh.lse) - q)));
+    a.loss[row] = (float)(tr.total == 0.0 ? 0.0 : none ? (double)INFINITY : loss);
+    a.lse[row] = none ? -INFINITY : (float)lse;
   }
 }
 
-// The gradient from a saved log-sum-exp (and, with teacher_lse, log_rest): a CTA takes DISTILL_GRAD_VECS vectors per thread of a row.
+// The gradient from a saved log-sum-exp (and, with teacher_lse, log_rest).  A CTA walks `cta_elems` logits of a row, the next loads always on
+// their way.
 #define DISTILL_GRAD_THREADS 256
-#define DISTILL_GRAD_VECS 4
 template <typename T>
-__global__ void __launch_bounds__(DISTILL_GRAD_THREADS)
+__global__ void __launch_bounds__(DISTILL_GRAD_THREADS, 4)
 k_distill_grad(const __grid_constant__ DistillArgs a) {
-  __shared__ Teacher t;
-  constexpr int VEC = 16 / sizeof(T), CHUNK = DISTILL_GRAD_THREADS * DISTILL_GRAD_VECS * VEC;
+  __shared__ TeacherSums teacher;
+  __shared__ double sq[DISTILL_MAX_TOP];
+  __shared__ int sid[DISTILL_MAX_TOP];
+  constexpr int VEC = 16 / sizeof(T), U = 4, STEP = DISTILL_GRAD_THREADS * VEC;
   kernel_entry(TR_k_distill_grad);
-  const int chunks = (a.vocab + CHUNK - 1) / CHUNK, row = blockIdx.x / chunks, base = (blockIdx.x - row * chunks) * CHUNK,
-            n = min(CHUNK, a.vocab - base), tid = threadIdx.x;
+  const int parts = (a.vocab + a.cta_elems - 1) / a.cta_elems, row = blockIdx.x / parts, base = (blockIdx.x - row * parts) * a.cta_elems,
+            n = min(a.cta_elems, a.vocab - base), tid = threadIdx.x;
   const T *src = (const T *)a.logits + row * a.ld + base;
   T *dst = (T *)a.grad + row * a.grad_ld + base;
-  const bool pad = a.row_scale && a.row_scale[row] == 0.f;               // a row of padding is not read
-  const double lse = (double)a.lse[row], scale = (a.row_scale ? (double)a.row_scale[row] : 1.0) * a.inv_tau;
-  const float c2 = (float)(a.inv_tau * 1.4426950408889634);
-  uint4 q[DISTILL_GRAD_VECS];
+  const float rs = a.row_scale ? a.row_scale[row] : 1.f;
+  if (rs == 0.f || a.lse[row] == -INFINITY) {               // a row of padding is not read
+    for (int i = tid * VEC; i < n; i += STEP) store_vec<T, VEC>(dst, i, n, a.grad_vec, make_uint4(0u, 0u, 0u, 0u));
+    return;
+  }
+  uint4 q[2][U];
+  auto fetch = [&](uint4 (&b)[U], int i0) {
 #pragma unroll
-  for (int k = 0; k < DISTILL_GRAD_VECS; ++k) q[k] = load_vec<T, VEC>(src, (k * DISTILL_GRAD_THREADS + tid) * VEC, pad ? 0 : n, a.vec, -INFINITY);
-  teacher_row(a, row, t);
-  const bool zero = scale == 0.0 || t.total == 0.0 || lse == -INFINITY;
-  const double tail = t.rest > 0.0 ? t.rest * exp(-(double)a.log_rest[row]) : 0.0;
-  // s near tau lse, so that the difference that the exponential sees is small where p is not
-  const float ref = (float)(lse / a.inv_tau), d2 = (float)((lse - (double)ref * a.inv_tau) * 1.4426950408889634), coef = (float)(scale * (t.total - tail));
-  // listed ids of this chunk: their logits are read before any gradient is written (the two may be one buffer)
-  const int id = tid < DISTILL_MAX_TOP ? t.id[tid] - base : -1;
-  const bool mine = tid < DISTILL_MAX_TOP && t.id[tid] >= 0 && id >= 0 && id < n && !zero;
-  float g_top = 0.f;
-  if (mine) {
-    double qj = 0.0;
-    for (int j = 0; j < a.top; ++j) if (t.id[j] == t.id[tid]) qj += t.q[j];     // every entry of an id computes the same value
-    g_top = (float)(scale * (t.total * exp((double)to_f(src[id]) * a.inv_tau - lse) - qj));
+    for (int k = 0; k < U; ++k) b[k] = load_vec<T, VEC>(src, i0 + (k * DISTILL_GRAD_THREADS + tid) * VEC, n, a.vec, -INFINITY);
+  };
+  fetch(q[0], 0);
+  const double lse = (double)a.lse[row];
+  Entry t = {-1, -INFINITY, 0.0};
+  if (tid < DISTILL_MAX_TOP) {
+    t = load_entry(a, row);
+    teacher_sums(a, row, t, teacher);
   }
   __syncthreads();
+  const TeacherRow tr = teacher_row(a, teacher);
+  const double scale = tr.total == 0.0 ? 0.0 : (double)rs * a.inv_tau;
+  const double tail = tr.rest > 0.0 ? tr.rest * exp(-(double)a.log_rest[row]) : 0.0;
+  // logits relative to tau lse, so that the difference that the exponential sees is small where p is not
+  const float ch = (float)(a.inv_tau * 1.4426950408889634), ref = (float)(lse / a.inv_tau),
+              d = (float)((lse - (double)ref * a.inv_tau) * 1.4426950408889634), coef = (float)(scale * (tr.total - tail));
+  const int id = t.id - base;
+  const bool mine = t.id >= 0 && id >= 0 && id < n && scale != 0.0;
+  float g_top = 0.f;
+  if (tid < DISTILL_MAX_TOP) { sq[tid] = t.e * tr.mine(); sid[tid] = t.id; }
+  __syncthreads();
+  if (mine) {                                               // every entry of an id computes the same value
+    double qj = 0.0;
+    for (int j = 0; j < a.top; ++j) if (sid[j] == t.id) qj += sq[j];
+    g_top = (float)(scale * (tr.total * exp((double)to_f(src[id]) * a.inv_tau - lse) - qj));
+  }
+  __syncthreads();                                          // before any gradient is written: the two may be one buffer
+  auto turn = [&](const uint4 (&b)[U], int i0) {
 #pragma unroll
-  for (int k = 0; k < DISTILL_GRAD_VECS; ++k) {
-    const int i = (k * DISTILL_GRAD_THREADS + tid) * VEC;
-    float l[VEC], g[VEC];
-    unpack_vec<T, VEC>(q[k], l);
+    for (int k = 0; k < U; ++k) {
+      const int i = i0 + (k * DISTILL_GRAD_THREADS + tid) * VEC;
+      float l[VEC], g[VEC];
+      unpack_vec<T, VEC>(b[k], l);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) g[e] = zero ? 0.f : coef * ex2(fmaf(l[e] - ref, c2, -d2));
-    if (i < n) store_vec<T, VEC>(dst, i, n, a.grad_vec, pack_vec<T, VEC>(g));
+      for (int e = 0; e < VEC; e += 2) {
+        const float2 y = fma_pair(add_pair(make_float2(l[e], l[e + 1]), make_float2(-ref, -ref)), make_float2(ch, ch), make_float2(-d, -d));
+        const float2 o = mul_pair(make_float2(ex2(y.x), ex2(y.y)), make_float2(coef, coef));
+        g[e] = o.x; g[e + 1] = o.y;
+      }
+      if (i < n) store_vec<T, VEC>(dst, i, n, a.grad_vec, pack_vec<T, VEC>(g));
+    }
+  };
+  for (int i0 = 0; i0 < n; i0 += 2 * U * STEP) {
+    if (i0 + U * STEP < n) fetch(q[1], i0 + U * STEP);
+    turn(q[0], i0);
+    if (i0 + 2 * U * STEP < n) fetch(q[0], i0 + 2 * U * STEP);
+    if (i0 + U * STEP < n) turn(q[1], i0 + U * STEP);
   }
   __syncthreads();
   if (mine) dst[id] = from_f<T>(g_top);

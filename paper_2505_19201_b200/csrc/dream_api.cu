@@ -1729,7 +1729,7 @@ static dream_status distill_args(const char *who, DistillArgs *a, const void *lo
   if (s) return s;
   if (!ids || !teacher || !lse) return fail(nullptr, DREAM_E_ARG, "%s: teacher_ids, teacher_logits and lse are required", who);
   if (top < 1 || top > DISTILL_MAX_TOP) return fail(nullptr, DREAM_E_ARG, "%s: top = %d outside 1..%d", who, top, DISTILL_MAX_TOP);
-  if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(nullptr, DREAM_E_ARG, "%s: temperature must be positive and finite", who);
+  if (!(temperature >= 1e-20f && temperature <= 1e20f)) return fail(nullptr, DREAM_E_ARG, "%s: temperature must lie in 1e-20..1e20", who);
   if (!teacher_lse != !log_rest) return fail(nullptr, DREAM_E_ARG, "%s: log_rest goes with teacher_lse", who);
   if (grad && rows_collide(logits, ld, grad, grad_ld, dtype, rows, vocab)) return fail(nullptr, DREAM_E_ARG, "%s: grad overlaps logits without being logits", who);
   memset(a, 0, sizeof(*a));
@@ -1751,11 +1751,13 @@ extern "C" dream_status dream_distill_loss(const void *logits, int32_t dtype, in
                                 temperature, lse, log_rest, row_scale, grad, grad_ld);
   if (s) return s;
   a.loss = loss;
+  // 64 KB of the row per CTA where a cluster of eight can hold it so: three CTAs per SM then take turns at loading, summing and writing
+  const int esz = dtype == DREAM_BF16 ? 2 : 4, per = 16 / esz;
   a.cluster = 1;
-  while (vocab > a.cluster * DISTILL_CTA_MAX) a.cluster *= 2;
-  a.cta_elems = ((vocab + a.cluster - 1) / a.cluster + 1023) / 1024 * 1024;
-  const int esz = dtype == DREAM_BF16 ? 2 : 4, per = 16 / esz, threads = a.cta_elems * esz > 65536 ? 1024 : imax(128, imin(512, a.cta_elems / per));
-  const size_t step = (size_t)threads * per, smem = (sizeof(DistillShared) + 15) / 16 * 16 + (grad ? (a.cta_elems + step - 1) / step * step * esz : 0);
+  while (vocab > a.cluster * (65536 / esz) && a.cluster < DISTILL_MAX_CLUSTER) a.cluster *= 2;
+  a.cta_elems = ((vocab + a.cluster - 1) / a.cluster + 31) / 32 * 32;
+  const int threads = imax(DISTILL_MAX_TOP, imin(DISTILL_THREADS, (a.cta_elems / per + 31) / 32 * 32));
+  const size_t step = (size_t)threads * per, smem = distill_row_offset(a.cta_elems) + (grad ? (a.cta_elems + step - 1) / step * step * esz : 0);
   void (*kernel)(DistillArgs) = dtype == DREAM_BF16 ? (grad ? k_distill<bf16, true> : k_distill<bf16, false>)
                                                     : (grad ? k_distill<float, true> : k_distill<float, false>);
   const char *why = launch_rows(kernel, rows, a.cluster, threads, smem, (cudaStream_t)cuda_stream, a);
@@ -1771,7 +1773,11 @@ extern "C" dream_status dream_distill_grad(const void *logits, int32_t dtype, in
   dream_status s = distill_args("dream_distill_grad", &a, logits, dtype, rows, vocab, ld, teacher_ids, teacher_logits, top, teacher_lse,
                                 temperature, const_cast<float *>(lse), const_cast<float *>(log_rest), row_scale, grad, grad_ld);
   if (s) return s;
-  const int chunk = DISTILL_GRAD_THREADS * DISTILL_GRAD_VECS * (dtype == DREAM_BF16 ? 8 : 4), chunks = (vocab + chunk - 1) / chunk;
+  // as much of a row per CTA as leaves every SM some eight of them, in whole rounds of a CTA's loads
+  const int round = DISTILL_GRAD_THREADS * 4 * (dtype == DREAM_BF16 ? 8 : 4), rounds = (vocab + round - 1) / round;
+  const int parts_wanted = imax(1, imin(rounds, (148 * 8 + rows - 1) / rows));
+  a.cta_elems = (rounds + parts_wanted - 1) / parts_wanted * round;
+  const int chunks = (vocab + a.cta_elems - 1) / a.cta_elems;
   void (*kernel)(DistillArgs) = dtype == DREAM_BF16 ? k_distill_grad<bf16> : k_distill_grad<float>;
   if ((long long)rows * chunks > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "dream_distill_grad: %d rows of %d logits in one call", rows, vocab);
   const char *why = launch_rows(kernel, rows * chunks, 1, DISTILL_GRAD_THREADS, 0, (cudaStream_t)cuda_stream, a);

@@ -49,7 +49,7 @@ def test_matrix(call, bad, code):
     (sample, dict(uniforms=None)), (sample, dict(tokens=None)),
     (truncate, dict(out=None)), (truncate, dict(out_ld=50)), (truncate, dict(out=C.c_void_p((1 << 40) + 1))),
     (loss, dict(ids=None)), (loss, dict(top_logits=None)), (loss, dict(loss=None)), (loss, dict(lse=None)), (loss, dict(top=0)), (loss, dict(top=129)),
-    (loss, dict(tau=0.0)), (loss, dict(tau=-1.0)), (loss, dict(tau=float("nan"))), (loss, dict(tau=float("inf"))),
+    (loss, dict(tau=0.0)), (loss, dict(tau=-1.0)), (loss, dict(tau=float("nan"))), (loss, dict(tau=float("inf"))), (loss, dict(tau=1e-30)), (grad, dict(tau=1e30)),
     (loss, dict(tl=Q)), (loss, dict(rest=Q)), (loss, dict(grad=Q, grad_ld=99)),
     (grad, dict(grad=None)), (grad, dict(lse=None)), (grad, dict(tl=Q)), (grad, dict(rest=Q)), (grad, dict(top=129)), (grad, dict(tau=0.0)),
 ])
