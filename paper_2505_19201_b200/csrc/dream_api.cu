@@ -1736,8 +1736,6 @@ static dream_status distill_args(const char *who, DistillArgs *a, const void *lo
   a->logits = logits; a->vocab = vocab; a->ld = ld; a->ids = ids; a->teacher = teacher; a->top = top; a->teacher_lse = teacher_lse;
   a->inv_tau = 1.0 / (double)temperature; a->lse = lse; a->log_rest = log_rest; a->row_scale = row_scale;
   a->grad = grad; a->grad_ld = grad_ld;
-  a->vec = rows_of_16(logits, dtype, rows, ld);
-  a->grad_vec = grad && rows_of_16(grad, dtype, rows, grad_ld);
   return DREAM_OK;
 }
 
@@ -1751,13 +1749,14 @@ extern "C" dream_status dream_distill_loss(const void *logits, int32_t dtype, in
                                 temperature, lse, log_rest, row_scale, grad, grad_ld);
   if (s) return s;
   a.loss = loss;
-  // 64 KB of the row per CTA where a cluster of eight can hold it so: three CTAs per SM then take turns at loading, summing and writing
-  const int esz = dtype == DREAM_BF16 ? 2 : 4, per = 16 / esz;
+  // With a gradient a CTA keeps its share of the row, 64 KB where a cluster of eight can hold the row so: three CTAs per SM then take turns at
+  // loading, summing and writing.  Without one it needs a ring and a byte per vector, and as few CTAs per row as keep the SMs busy.
+  const int vecs = imax(1, vocab / (dtype == DREAM_BF16 ? 8 : 4)), most = grad ? 4096 : 16384;
   a.cluster = 1;
-  while (vocab > a.cluster * (65536 / esz) && a.cluster < DISTILL_MAX_CLUSTER) a.cluster *= 2;
-  a.cta_elems = ((vocab + a.cluster - 1) / a.cluster + 31) / 32 * 32;
-  const int threads = imax(DISTILL_MAX_TOP, imin(DISTILL_THREADS, (a.cta_elems / per + 31) / 32 * 32));
-  const size_t step = (size_t)threads * per, smem = distill_row_offset(a.cta_elems) + (grad ? (a.cta_elems + step - 1) / step * step * esz : 0);
+  while (a.cluster < DISTILL_MAX_CLUSTER && (vecs > a.cluster * most || (!grad && rows * a.cluster < 148 * 3 * 4 && vecs > a.cluster * 2048))) a.cluster *= 2;
+  a.cta_vecs = (vecs + a.cluster - 1) / a.cluster;
+  const int slots = grad ? (a.cta_vecs + DISTILL_THREADS - 1) / DISTILL_THREADS : DISTILL_RING, threads = DISTILL_THREADS;
+  const size_t smem = (sizeof(DistillShared) + 15) / 16 * 16 + distill_flag_bytes(a.cta_vecs) + (size_t)slots * threads * 16;
   void (*kernel)(DistillArgs) = dtype == DREAM_BF16 ? (grad ? k_distill<bf16, true> : k_distill<bf16, false>)
                                                     : (grad ? k_distill<float, true> : k_distill<float, false>);
   const char *why = launch_rows(kernel, rows, a.cluster, threads, smem, (cudaStream_t)cuda_stream, a);
@@ -1773,14 +1772,14 @@ extern "C" dream_status dream_distill_grad(const void *logits, int32_t dtype, in
   dream_status s = distill_args("dream_distill_grad", &a, logits, dtype, rows, vocab, ld, teacher_ids, teacher_logits, top, teacher_lse,
                                 temperature, const_cast<float *>(lse), const_cast<float *>(log_rest), row_scale, grad, grad_ld);
   if (s) return s;
-  // as much of a row per CTA as leaves every SM some eight of them, in whole rounds of a CTA's loads
-  const int round = DISTILL_GRAD_THREADS * 4 * (dtype == DREAM_BF16 ? 8 : 4), rounds = (vocab + round - 1) / round;
-  const int parts_wanted = imax(1, imin(rounds, (148 * 8 + rows - 1) / rows));
-  a.cta_elems = (rounds + parts_wanted - 1) / parts_wanted * round;
-  const int chunks = (vocab + a.cta_elems - 1) / a.cta_elems;
+  // as much of a row per CTA as leaves every SM some twelve of them
+  const int vecs = imax(1, vocab / (dtype == DREAM_BF16 ? 8 : 4));
+  const int steps = (vecs + DISTILL_THREADS - 1) / DISTILL_THREADS, parts = imax(1, imin((steps + 3) / 4, (148 * 12 + rows - 1) / rows));
+  a.cta_vecs = (steps + parts - 1) / parts * DISTILL_THREADS;
+  a.cluster = (vecs + a.cta_vecs - 1) / a.cta_vecs;
   void (*kernel)(DistillArgs) = dtype == DREAM_BF16 ? k_distill_grad<bf16> : k_distill_grad<float>;
-  if ((long long)rows * chunks > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "dream_distill_grad: %d rows of %d logits in one call", rows, vocab);
-  const char *why = launch_rows(kernel, rows * chunks, 1, DISTILL_GRAD_THREADS, 0, (cudaStream_t)cuda_stream, a);
+  if ((long long)rows * a.cluster > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "dream_distill_grad: %d rows of %d logits in one call", rows, vocab);
+  const char *why = launch_rows(kernel, rows * a.cluster, 1, DISTILL_THREADS, DISTILL_GRAD_RING * DISTILL_THREADS * 16, (cudaStream_t)cuda_stream, a);
   return why ? fail(nullptr, DREAM_E_CUDA, "dream_distill_grad: %s", why) : DREAM_OK;
 }
 

@@ -90,14 +90,14 @@ def run_all(x, ids, top, teacher_lse, scale, tau=1.0):
     g3 = x.clone()
     api.dream_distill_loss(g3, ids, top, new(), new(), teacher_lse=teacher_lse, log_rest=rest(), temperature=tau, row_scale=scale, grad=g3)
     torch.cuda.synchronize()
-    assert torch.equal(loss, loss2) and torch.equal(lse, lse2) and (lr is None or torch.equal(lr, lr2))
-    assert torch.equal(g, g3)
     a, b, c, d, size = formula(x, ids, top, teacher_lse, tau, V)
-    close_rows(loss, a, "loss")
-    close_rows(lse, b, "lse")
-    if lr is not None:
-        close_rows(lr, c, "log_rest")
+    for x1, x2, x3 in ((loss, lse, lr), (loss2, lse2, lr2)):  # the two may share a row differently among blocks
+        close_rows(x1, a, "loss")
+        close_rows(x2, b, "lse")
+        if lr is not None:
+            close_rows(x3, c, "log_rest")
     close_grad(g, d, size, scale, x.dtype)
+    close_grad(g3, d, size, scale, x.dtype)
     _, _, _, d, size = formula(x, ids, top, teacher_lse, tau, V, lse, lr)
     close_grad(g2, d, size, scale, x.dtype)
     return loss, g, g2
