@@ -21,7 +21,7 @@
 struct DistillArgs {
   const void *logits;
   long long ld;
-  int vocab, cluster, cta_vecs, top;
+  int rows, vocab, cluster, cta_vecs, top;
   const int *ids;                      // [rows][top]; outside [0, vocab): no entry
   const float *teacher;                // [rows][top]
   const float *teacher_lse;            // [rows] or null
@@ -178,18 +178,24 @@ struct DistillPart {
   float m, unused;                     // largest logit, -inf without one
   double others, tops, qz;             // sums over the ids that are not listed, that are; sum of q_j z_j tau
 };
-#define DISTILL_PAIRS (DISTILL_THREADS / 32 + DISTILL_TOP_WARPS)
-struct DistillShared {
-  DistillPart part[DISTILL_MAX_CLUSTER];
-  TeacherSums teacher;
-  double q[DISTILL_MAX_TOP], qz[DISTILL_TOP_WARPS], qz_row, entropy;
-  float2 pair[DISTILL_PAIRS];          // (maximum, sum): of every warp's vectors, of its listed ids
-  float total, rest;                   // Q, q_r
-  int id[DISTILL_MAX_TOP], repeated;
+// What the side warp knows of a row before its sums.
+struct DistillSide {
+  float total, rest, top_m, tops;      // Q; q_r; largest listed logit of this share and the listed ids' sum relative to it
+  double qz, entropy;                  // sum of q_j z_j tau in this share; sum of q ln q, the bucket's too
 };
-// Shared memory behind it: a byte per vector of the CTA's share, whose bits say which ids are listed, 16 bytes of such bits for the ids
-// at the row's ends, then the vectors.
-__host__ __device__ inline int distill_flag_bytes(int cta_vecs) { return (cta_vecs + 15) / 16 * 16 + 16; }
+template <int SW> struct DistillShared {
+  DistillPart part[2][DISTILL_MAX_CLUSTER];
+  DistillSide side[2];
+  float2 pair[2][SW];                  // (maximum, sum) of every stream warp
+  float q[DISTILL_MAX_TOP];            // for ids that are listed twice
+  int id[2][DISTILL_MAX_TOP];
+};
+// Shared memory behind it, twice: a byte per vector of the CTA's share, whose bits say which ids are listed, and 16 bytes of such bits for the
+// ids at the row's ends.  Then the ring of vectors.
+#define DISTILL_PER 16                 // vectors of a thread in a block of the share
+__host__ __device__ inline int distill_flag_bytes(int cta_vecs, int threads) {
+  return (cta_vecs + DISTILL_PER * threads - 1) / (DISTILL_PER * threads) * (DISTILL_PER * threads) + 16;
+}
 
 __device__ __forceinline__ void cp_async16(void *dst, const void *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
@@ -212,27 +218,38 @@ template <typename T> struct RowShare {
     mine = row + id0 + tid * VEC;
     edge = rank == 0 && tid < head ? tid : rank == cluster - 1 && tid >= 16 && tid < 16 + rest ? vocab - rest + tid - 16 : -1;
   }
-  // Where a listed id is in the share: a bit of a byte per vector, or of the bytes of the edges behind them; -1 elsewhere.
-  __device__ __forceinline__ int flag_bit(int id, int vocab, int rank, int cluster) const {
+  // Where a listed id is in the share: a bit of its vector's byte, a thread's DISTILL_PER vectors of a block side by side, or of the bytes of the
+  // edges from byte `edges` on; -1 elsewhere.
+  template <int NT> __device__ __forceinline__ int flag_bit(int id, int rank, int cluster, int edges) const {
     const int at = id - id0;
     if (id < 0) return -1;
-    if (at >= 0 && at < nv * VEC) return at / VEC * 8 + at % VEC;
-    const int n = flag_bytes(nv) * 8;
-    if (at < 0) return rank == 0 && id0 < VEC ? n + id : -1;                          // in front of the first boundary
-    return rank == cluster - 1 ? n + 16 + at - nv * VEC : -1;                         // behind the last
+    if (at >= 0 && at < nv * VEC) {
+      const int v = at / VEC, in = v % (DISTILL_PER * NT);
+      return (((v / (DISTILL_PER * NT) * NT + in % NT) * DISTILL_PER + in / NT) << 3) + at % VEC;
+    }
+    if (at < 0) return rank == 0 && id0 < VEC ? edges * 8 + id : -1;                  // in front of the first boundary
+    return rank == cluster - 1 ? edges * 8 + 16 + at - nv * VEC : -1;                 // behind the last
   }
-  __host__ __device__ static int flag_bytes(int nv) { return (nv + 15) / 16 * 16; }
 };
 
-// The gradient coef * 2^((l - ref) ch - d) of the thread's vectors, get(k) being the k-th's logits, and of its single id's logit le (where
-// `edge`).  Nothing is got where it is zero.  listed(g): bits of the elements of vector g that somebody else writes.
-template <typename T, typename F, typename L>
-__device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool zero, F get, L listed, bool edge, float le, float ref, float ch, float d, float coef) {
+// A vector of a gradient, without the elements in `listed`, which somebody else writes.
+template <typename T> __device__ __forceinline__ void store_unlisted(T *p, bool vec, const uint4 &q, uint32_t listed) {
+  if (vec && !listed) { *reinterpret_cast<uint4 *>(p) = q; return; }
+  constexpr int VEC = 16 / sizeof(T);
+  T t[VEC];
+  memcpy(t, &q, 16);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) if (!(listed >> e & 1u)) p[e] = t[e];
+}
+// The gradient coef * 2^((l - ref) ch - d) of the thread's vectors, get(k) being the k-th's logits, and of its single id's logit le.  Nothing is
+// got where it is zero.
+template <typename T, typename F>
+__device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool zero, F get, float le, float ref, float ch, float d, float coef) {
   constexpr int VEC = 16 / sizeof(T), NT = DISTILL_THREADS;
   const float2 r2 = make_float2(-ref, -ref), c2 = make_float2(ch, ch), d2 = make_float2(-d, -d), o2 = make_float2(coef, coef);
   T *p = dst + sr.id0 + threadIdx.x * VEC;
   const bool vec = ((uintptr_t)p & 15) == 0;
-  if (edge) dst[sr.edge] = from_f<T>(zero ? 0.f : coef * ex2(fmaf(le - ref, ch, -d)));
+  if (sr.edge >= 0) dst[sr.edge] = from_f<T>(zero ? 0.f : coef * ex2(fmaf(le - ref, ch, -d)));
   for (int k = 0, g = threadIdx.x; g < sr.nv; ++k, g += NT, p += NT * VEC) {
     uint4 q = make_uint4(0u, 0u, 0u, 0u);
     if (!zero) {
@@ -246,126 +263,278 @@ __device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool ze
       }
       q = pack_vec<T, VEC>(l);
     }
-    const uint32_t not_mine = listed(g);
-    if (vec && !not_mine) *reinterpret_cast<uint4 *>(p) = q;
-    else {
-      T u[VEC];
-      memcpy(u, &q, 16);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) if (!(not_mine >> e & 1u)) p[e] = u[e];
-    }
+    store_unlisted<T>(p, vec, q, 0u);
   }
 }
 
-// A thread has the same vectors of the share in every pass over it, so its copies into shared memory need no barrier: DISTILL_RING of them are
-// on their way at a time, in groups of DISTILL_BATCH.  GRAD: the whole share stays there and its gradient leaves in the same call.
-#define DISTILL_RING 16
-#define DISTILL_BATCH 2
+// Rows in a loop: cluster c takes the rows c, c + clusters, ..  SW stream warps walk a row's vectors, once for its sums and, with GRAD, once
+// more for its gradient; one side warp does meanwhile what is left: the listed ids of the next row and the loss of the last.
+// A stream thread has the same vectors in both passes, so its copies into shared memory need no barrier.  It walks blocks of 16 vectors of its own
+// (with GRAD a share is one block), and a vector's place is taken by the next block's, or the next row's, as soon as its gradient is
+// out (without GRAD: as soon as it has been added), so loads are always on their way.  (With a block per row and its own 64 KB the turnaround
+// of the blocks cost as much as everything else: 4096 rows of 32000 bf16 with gradient took 152 us, 99 of them with both passes left out.)
 #define DISTILL_GRAD_RING 8
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(DISTILL_THREADS, 3)
-k_distill(const __grid_constant__ DistillArgs a) {
-  extern __shared__ __align__(16) unsigned char smem_raw[];
-  DistillShared &sh = *reinterpret_cast<DistillShared *>(smem_raw);
-  uint8_t *flags = smem_raw + (sizeof(DistillShared) + 15) / 16 * 16;
-  constexpr int VEC = 16 / sizeof(T), NT = DISTILL_THREADS, NW = NT / 32, B = DISTILL_BATCH, AHEAD = DISTILL_RING / B;
-  cluster_started_arrive(a.cluster);
-  kernel_entry(TR_k_distill);
-  const int rank = a.cluster > 1 ? (int)cluster_ctarank() : 0, row = blockIdx.x / a.cluster, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const RowShare<T> sr(a.logits, a.ld, row, a.vocab, rank, a.cluster, a.cta_vecs);
-  uint4 *vals = reinterpret_cast<uint4 *>(flags + distill_flag_bytes(a.cta_vecs)) + tid;
-  const float ch = (float)(a.inv_tau * 1.4426950408889634);
-  const bool tail = a.teacher_lse != nullptr, top_warp = warp < teacher_warps(a);
-  const int nb = (sr.nv + B * NT - 1) / (B * NT);           // batches
-  for (int b = 0; b < (GRAD ? max(nb, AHEAD) : AHEAD); ++b) {
+template <int THREADS> __device__ __forceinline__ void block_barrier() { asm volatile("barrier.sync 0, %0;" ::"n"(THREADS) : "memory"); }
+
+template <typename T, bool GRAD, int SW>
+struct DistillBlock {
+  static constexpr int VEC = 16 / sizeof(T), NT = SW * 32, THREADS = NT + 32, PER = DISTILL_PER,
+                       B = sizeof(T) == 4 ? 4 : 2, TURNS = PER / B;       // vectors of a thread per turn, turns of a block
+  const DistillArgs &a;
+  DistillShared<SW> &sh;
+  uint8_t *flags;                      // [2][distill_flag_bytes(cta_vecs)]
+  int rank, first_row, clusters;
+  float ch;
+  __device__ __forceinline__ uint8_t *flags_of(int p) const { return flags + p * distill_flag_bytes(a.cta_vecs, NT); }
+  __device__ __forceinline__ RowShare<T> share(int row) const { return RowShare<T>(a.logits, a.ld, row, a.vocab, rank, a.cluster, a.cta_vecs); }
+  __device__ __forceinline__ int edge_byte() const { return distill_flag_bytes(a.cta_vecs, NT) - 16; }
+  __device__ __forceinline__ float scaled(float m, float s, float to) const { return m > -INFINITY ? s * ex2((m - to) * ch) : s; }
+  // The row's largest logit and its sums, from this CTA's warps or the cluster's parts.
+  template <typename R> __device__ __forceinline__ void sums(int p, float &rm, R &others, R &tops, double *qz) const {
+    rm = -INFINITY; others = 0; tops = 0;
+    if (a.cluster > 1) {
+      for (int c = 0; c < a.cluster; ++c) rm = fmaxf(rm, sh.part[p][c].m);
+      for (int c = 0; c < a.cluster; ++c) {
+        const DistillPart &x = sh.part[p][c];
+        const float f = x.m > -INFINITY ? ex2((x.m - rm) * ch) : 1.f;
+        others += x.others * f; tops += x.tops * f;
+        if (qz) *qz += x.qz;
+      }
+    } else {
+      own_sums(p, rm, others, tops);
+      if (qz) *qz = sh.side[p].qz;
+    }
+  }
+  template <typename R> __device__ __forceinline__ void own_sums(int p, float &rm, R &others, R &tops) const {
+    rm = sh.side[p].top_m;
+#pragma unroll
+    for (int w = 0; w < SW; ++w) rm = fmaxf(rm, sh.pair[p][w].x);
+#pragma unroll
+    for (int w = 0; w < SW; ++w) others += scaled(sh.pair[p][w].x, sh.pair[p][w].y, rm);
+    if (a.teacher_lse) tops += scaled(sh.side[p].top_m, sh.side[p].tops, rm);   // without the bucket they are among the others
+  }
+  // What the gradient of a row needs.
+  struct Slope { float ref, d, scale, coef; };
+  __device__ __forceinline__ Slope slope(int p, float rs) const {
+    Slope g;
+    float rm, others, tops;
+    sums(p, rm, others, tops, nullptr);
+    const float total = others + tops, q = sh.side[p].total, rest = sh.side[p].rest;
+    g.ref = rm > -INFINITY ? rm : 0.f;
+    g.d = __log2f(total);
+    g.scale = total == 0.f || q == 0.f ? 0.f : rs * (float)a.inv_tau;         // 0: padding, or nothing to learn from
+    g.coef = g.scale * (q - (rest > 0.f && others > 0.f ? rest * __fdividef(total, others) : 0.f));
+    return g;
+  }
+
+  // ---- the side warp: lane's entries are lane, lane + 32, ..
+  static constexpr int E = DISTILL_MAX_TOP / 32;
+  struct Entries { int id[E]; float t[E], z[E], q[E]; bool first[E]; };
+  __device__ __forceinline__ void load_entries(int row, Entries &n) const {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int j = lane + 32 * i;
+      n.id[i] = -1; n.t[i] = -INFINITY;
+      if (j < a.top && row < a.rows) {
+        const int id = a.ids[(long long)row * a.top + j];
+        n.t[i] = a.teacher[(long long)row * a.top + j];
+        n.id[i] = id >= 0 && id < a.vocab ? id : -1;
+      }
+    }
+  }
+  // Marks the row's listed ids, and leaves sh.side[p].
+  __device__ __forceinline__ void prepare(int row, int p, Entries &n) const {
+    if (row >= a.rows) return;
+    const int lane = threadIdx.x & 31;
+    const RowShare<T> sr = share(row);
+    uint32_t *words = reinterpret_cast<uint32_t *>(flags_of(p));
+    double x[E], e[E], ref = -INFINITY, s = 0.0, l = 0.0, qz = 0.0;
+    int bit[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      bit[i] = sr.template flag_bit<NT>(n.id[i], rank, a.cluster, edge_byte());
+      n.z[i] = bit[i] >= 0 ? to_f(sr.row[n.id[i]]) : -INFINITY;
+      n.first[i] = bit[i] >= 0;
+      x[i] = n.id[i] >= 0 ? (double)n.t[i] * a.inv_tau : -INFINITY;
+      sh.id[p][lane + 32 * i] = n.id[i];
+    }
+    bool twice = false;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (bit[i] >= 0 && (atomicOr(words + (bit[i] >> 5), 1u << (bit[i] & 31)) >> (bit[i] & 31) & 1u)) twice = true;
+    twice = __any_sync(0xffffffffu, twice);
+    __syncwarp();
+    if (twice) {                                            // of the entries of one id the first stands for it
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        for (int j = 0; j < lane + 32 * i; ++j) if (sh.id[p][j] == n.id[i]) n.first[i] = false;
+    }
+    if (a.teacher_lse) ref = (double)a.teacher_lse[row];
+    else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) ref = fmax(ref, x[i]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) ref = fmax(ref, __shfl_xor_sync(0xffffffffu, ref, o));
+    }
+    float tm = -INFINITY, ts = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      e[i] = 0.0;
+      if (i * 32 < a.top) {
+        if (n.id[i] >= 0 && x[i] != -INFINITY) e[i] = exp(x[i] - ref);
+        s += e[i];
+        if (!(e[i] == 0.0)) {
+          l += e[i] * (a.teacher_lse ? x[i] - ref : x[i]);
+          if (bit[i] >= 0) qz += e[i] * (double)n.z[i];
+        }
+        tm = fmaxf(tm, n.z[i]);
+      }
+    }
+    tm = warp_max(tm);
+#pragma unroll
+    for (int i = 0; i < E; ++i) if (n.first[i]) ts += ex2((n.z[i] - (tm > -INFINITY ? tm : 0.f)) * ch);
+    ts = warp_sum(ts); s = warp_sum_d(s); l = warp_sum_d(l); qz = warp_sum_d(qz);
+    const bool any = !(s == 0.0);                           // a row with no valid entry has no loss, with or without the rest
+    DistillSide d;
+    double f = 1.0;
+    if (a.teacher_lse) {
+      const double rest = any ? fmax(0.0, 1.0 - s) : 0.0;
+      d.rest = (float)rest;
+      d.total = any ? (float)(s + rest) : 0.f;
+      d.entropy = l + (rest > 0.0 ? rest * log(rest) : 0.0);
+    } else {
+      f = any ? 1.0 / s : 0.0;
+      d.rest = 0.f;
+      d.total = any ? 1.f : 0.f;
+      d.entropy = any ? l * f - (ref + log(s)) : 0.0;
+    }
+    d.qz = qz == 0.0 ? 0.0 : qz * f;
+    d.top_m = tm; d.tops = ts;
+#pragma unroll
+    for (int i = 0; i < E; ++i) n.q[i] = (float)(e[i] * f);
+    if (twice) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) sh.q[lane + 32 * i] = n.q[i];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (n.first[i]) {
+          n.q[i] = 0.f;
+          for (int j = 0; j < a.top; ++j) if (sh.id[p][j] == n.id[i]) n.q[i] += sh.q[j];
+        }
+      __syncwarp();
+    }
+    if (lane == 0) sh.side[p] = d;
+  }
+  __device__ __forceinline__ void finish(int row, int p) const {
+    if (rank || row < 0) return;
+    float rm;
+    double others, tops, qz = 0.0;
+    sums(p, rm, others, tops, &qz);
+    const DistillSide &d = sh.side[p];
+    const double total = others + tops, lse = (double)rm * a.inv_tau + log(total);
+    const bool none = total == 0.0;                         // no finite logit
+    double loss = d.entropy - qz * a.inv_tau + ((double)d.total - (double)d.rest) * lse, log_rest = 0.0;
+    if (a.teacher_lse) {
+      log_rest = others > 0.0 ? -log1p(tops / others) : others == 0.0 ? -INFINITY : others;
+      if (d.rest > 0.f) loss -= (double)d.rest * log_rest;
+    }
+    if ((threadIdx.x & 31) == 0) {
+      if (a.teacher_lse) a.log_rest[row] = none ? -INFINITY : (float)log_rest;
+      a.loss[row] = (float)(d.total == 0.f ? 0.0 : none ? (double)INFINITY : loss);
+      a.lse[row] = none ? -INFINITY : (float)lse;
+    }
+  }
+  __device__ __forceinline__ void side_warp() const {
+    Entries n;
+    load_entries(first_row, n);
+    for (int i = threadIdx.x & 31; i < distill_flag_bytes(a.cta_vecs, NT) * 2 / 4; i += 32) reinterpret_cast<uint32_t *>(flags)[i] = 0;
+    __syncwarp();
+    prepare(first_row, 0, n);
+    cluster_started_wait(a.cluster);
+    block_barrier<THREADS>();
+    int p = 0, last = -1;
+    for (int row = first_row; row < a.rows; row += clusters, p ^= 1) {
+      Entries next;
+      load_entries(row + clusters, next);
+      const float rs = GRAD && a.row_scale ? a.row_scale[row] : 1.f;
+      finish(last, p ^ 1);
+      block_barrier<THREADS>();                             // the row's pairs are there
+      if (a.cluster > 1) {
+        const int lane = threadIdx.x & 31;
+        if (lane < a.cluster) {
+          float rm;
+          double others = 0.0, tops = 0.0;
+          own_sums(p, rm, others, tops);
+          const uint32_t to = mapa(smem_u32(&sh.part[p][rank]), lane);
+          st_cluster_u64(to, (unsigned long long)__float_as_uint(rm));
+          st_cluster_u64(to + 8, __double_as_longlong(others));
+          st_cluster_u64(to + 16, __double_as_longlong(tops));
+          st_cluster_u64(to + 24, __double_as_longlong(sh.side[p].qz));
+        }
+        cluster_sync_all();
+      }
+      if (GRAD) {
+        const Slope g = slope(p, rs);
+        T *dst = (T *)a.grad + row * a.grad_ld;
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (n.first[i]) dst[n.id[i]] = from_f<T>(g.scale == 0.f ? 0.f : g.scale * fmaf(sh.side[p].total, ex2(fmaf(n.z[i] - g.ref, ch, -g.d)), -n.q[i]));
+      }
+      last = row;
+      if (row != first_row) unmark_row(row - clusters, p ^ 1);
+      prepare(row + clusters, p ^ 1, next);
+      n = next;
+      block_barrier<THREADS>();
+    }
+    finish(last, p ^ 1);
+  }
+  __device__ __forceinline__ void unmark_row(int row, int p) const {
+    const RowShare<T> sr = share(row);
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int j = lane + 32 * i, bit = j < a.top ? sr.template flag_bit<NT>(sh.id[p][j], rank, a.cluster, edge_byte()) : -1;
+      if (bit >= 0) flags_of(p)[bit >> 3] = 0;
+    }
+    __syncwarp();
+  }
+
+  // ---- the stream warps
+  // The next block's vectors of a turn, where the block has them (left: ids of vectors from the thread's first on), as one group of copies.
+  __device__ __forceinline__ void fetch(int turn, const T *from, int left, uint4 *ring) const {
 #pragma unroll
     for (int k = 0; k < B; ++k)
-      if ((b * B + k) * NT + tid < sr.nv) cp_async16(vals + (b * B + k) * NT, sr.mine + (size_t)(b * B + k) * NT * VEC);
+      if ((turn * B + k) * NT < left) cp_async16(ring + (turn * B + k) * NT, from + (turn * B + k) * NT * VEC);
     cp_async_commit();
   }
-  // while they are on their way: the teacher's side, and the listed ids' logits
-  Entry t = {-1, -INFINITY, 0.0};
-  if (top_warp) { t = load_entry(a, row); sh.id[tid] = t.id; }
-  const float le = sr.edge >= 0 ? to_f(sr.row[sr.edge]) : -INFINITY, rs = GRAD && a.row_scale ? a.row_scale[row] : 1.f;
-  for (int i = tid; i < distill_flag_bytes(sr.nv) / 4; i += NT) reinterpret_cast<uint32_t *>(flags)[i] = 0;
-  if (tid == 0) sh.repeated = 0;
-  if (tid < DISTILL_TOP_WARPS) sh.pair[NW + tid] = make_float2(-INFINITY, 0.f);
-  const int bit = top_warp ? sr.flag_bit(t.id, a.vocab, rank, a.cluster) : -1;
-  const bool mine = bit >= 0;
-  const float z = mine ? to_f(sr.row[t.id]) : -INFINITY;
-  __syncthreads();
-  bool first = mine;                                        // of the entries of one id the first stands for it
-  auto listed_pair = [&]() {
-    const float tm = warp_max(z), ts = warp_sum(first ? ex2((z - (tm > -INFINITY ? tm : 0.f)) * ch) : 0.f);
-    if (lane == 0) sh.pair[NW + warp] = make_float2(tm, ts);
-  };
-  if (top_warp) {
-    if (mine && (atomicOr(reinterpret_cast<uint32_t *>(flags) + (bit >> 5), 1u << (bit & 31)) >> (bit & 31) & 1u)) sh.repeated = 1;
-    teacher_sums(a, row, t, sh.teacher);
-    const double qz = warp_sum_d(mine && !(t.e == 0.0) ? t.e * (double)z : 0.0);
-    if (lane == 0) sh.qz[warp] = qz;
-    listed_pair();
-  }
-  __syncthreads();
-  TeacherRow tr;
-  double qj = 0.0;
-  if (top_warp) {
-    tr = teacher_row(a, sh.teacher);
-    sh.q[tid] = qj = t.e * tr.mine();
-    if (sh.repeated) {
-      for (int j = 0; j < tid; ++j) if (sh.id[j] == t.id) first = false;
-      listed_pair();
-    }
-    if (tid == 0) {
-      double qz = 0.0, en = -(tr.ref + log(tr.sum));        // sum q ln q, the bucket's too
-      for (int w = 0; w < teacher_warps(a); ++w) {
-        if (!(sh.qz[w] == 0.0)) qz += sh.qz[w] * tr.f[w];
-        if (!(sh.teacher.log[w] == 0.0)) en += sh.teacher.log[w] * tr.f[w];
-      }
-      if (tr.rest > 0.0) en += tr.rest * log(tr.rest);
-      sh.qz_row = qz; sh.entropy = en;
-      sh.total = (float)tr.total; sh.rest = (float)tr.rest;
-    }
-  }
-  // running maximum m (ref: the same, 0 without one) and sum of 2^((l - ref) ch); listed ids stay out where the rest is a bucket
-  float m = -INFINITY, ref = 0.f, s = 0.f, s1 = 0.f;
-  const bool listed_edge = sr.edge >= 0 && (flags[RowShare<T>::flag_bytes(sr.nv) + (tid >> 3)] >> (tid & 7) & 1u);
-  if (sr.edge >= 0 && !(tail && listed_edge)) {
-    if (le > m) { m = ref = le; s = 1.f; }
-    else if (le != le) s = le;
-  }
-  for (int b = 0; b < nb; ++b) {
-    cp_async_wait<AHEAD - 1>();
+  template <int TURN> __device__ __forceinline__ void add_turn(const uint4 *ring, int left, const uint4 &marks, float &m, float &ref, float2 &s) const {
     uint4 q[B];
-    uint32_t listed = 0;
 #pragma unroll
     for (int k = 0; k < B; ++k) {
-      const int g = (b * B + k) * NT + tid, slot = GRAD ? b * B + k : b % AHEAD * B + k;
-      if (g < sr.nv) {
-        q[k] = vals[slot * NT];
-        if (tail) listed |= (uint32_t)flags[g] << k * VEC;
-      } else {
-        const uint32_t u = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;       // -inf
-        q[k] = make_uint4(u, u, u, u);
-      }
-      if (!GRAD && g + DISTILL_RING * NT < sr.nv) cp_async16(vals + slot * NT, sr.mine + (size_t)((b + AHEAD) * B + k) * NT * VEC);
+      const uint32_t u = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;            // -inf
+      q[k] = make_uint4(u, u, u, u);
+      if ((TURN * B + k) * NT < left) q[k] = ring[(TURN * B + k) * NT];
     }
-    cp_async_commit();
     float l[B][VEC], v = max_vec<T, VEC>(q[0]);
 #pragma unroll
     for (int k = 0; k < B; ++k) unpack_vec<T, VEC>(q[k], l[k]);
 #pragma unroll
     for (int k = 1; k < B; ++k) v = fmaxf(v, max_vec<T, VEC>(q[k]));
+    const uint32_t listed = turn_marks<TURN>(marks);
     if (listed) {
       v = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < B * VEC; ++e) {
-        if (listed >> e & 1u) l[e / VEC][e % VEC] = -INFINITY;
-        v = fmaxf(v, l[e / VEC][e % VEC]);
-      }
+      for (int k = 0; k < B; ++k)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          if (listed >> (k * 8 + e) & 1u) l[k][e] = -INFINITY;
+          v = fmaxf(v, l[k][e]);
+        }
     }
     if (v > m) {
-      if (m > -INFINITY) { const float f = ex2((m - v) * ch); s *= f; s1 *= f; }
+      if (m > -INFINITY) { const float f = ex2((m - v) * ch); s.x *= f; s.y *= f; }
       m = ref = v;
     }
     const float2 r2 = make_float2(-ref, -ref), c2 = make_float2(ch, ch);
@@ -374,82 +543,128 @@ k_distill(const __grid_constant__ DistillArgs a) {
 #pragma unroll
       for (int e = 0; e < VEC; e += 2) {
         const float2 y = mul_pair(add_pair(make_float2(l[k][e], l[k][e + 1]), r2), c2);
-        s += ex2(y.x); s1 += ex2(y.y);
+        s = add_pair(s, make_float2(ex2(y.x), ex2(y.y)));
       }
   }
-  {
-    const float wm = warp_max(m);
-    s = warp_sum((s + s1) * (m > -INFINITY ? ex2((m - wm) * ch) : 1.f));        // without a maximum 0, or NaN
-    if (lane == 0) sh.pair[warp] = make_float2(wm, s);
+  template <int TURN> static __device__ __forceinline__ uint32_t turn_marks(const uint4 &m) {     // B bytes
+    constexpr int w = TURN * B / 4;
+    const uint32_t u = w == 0 ? m.x : w == 1 ? m.y : w == 2 ? m.z : m.w;
+    return B == 4 ? u : TURN & 1 ? u >> 16 : u & 0xffffu;
   }
-  __syncthreads();
-  // the CTA's sums out of the warps' (each thread that needs them by itself), in the precision asked for
-  float rm = -INFINITY;
+  template <int TURN> __device__ __forceinline__ void write_turn(const uint4 *ring, int left, const uint4 &marks, T *out, bool vec, const Slope &g) const {
+    const float2 r2 = make_float2(-g.ref, -g.ref), c2 = make_float2(ch, ch), d2 = make_float2(-g.d, -g.d), o2 = make_float2(g.coef, g.coef);
+    const uint32_t listed = turn_marks<TURN>(marks);
 #pragma unroll
-  for (int w = 0; w < DISTILL_PAIRS; ++w) rm = fmaxf(rm, sh.pair[w].x);
-  auto join = [&](auto &others, auto &tops) {
+    for (int k = 0; k < B; ++k)
+      if ((TURN * B + k) * NT < left) {
+        float l[VEC];
+        unpack_vec<T, VEC>(ring[(TURN * B + k) * NT], l);
 #pragma unroll
-    for (int w = 0; w < DISTILL_PAIRS; ++w) {
-      const float2 p = sh.pair[w];
-      const float v = p.x > -INFINITY ? p.y * ex2((p.x - rm) * ch) : p.y;
-      if (w < NW) others += v;
-      else if (tail) tops += v;                             // without the bucket they are among the others
+        for (int e = 0; e < VEC; e += 2) {
+          const float2 y = fma_pair(add_pair(make_float2(l[e], l[e + 1]), r2), c2, d2);
+          const float2 o = mul_pair(make_float2(ex2(y.x), ex2(y.y)), o2);
+          l[e] = o.x; l[e + 1] = o.y;
+        }
+        store_unlisted<T>(out + (TURN * B + k) * NT * VEC, vec, pack_vec<T, VEC>(l), listed >> (k * 8) & 0xffu);
+      }
+  }
+  template <int TURN> __device__ __forceinline__ void add_turns(uint4 *ring, int left, const uint4 &marks, float &m, float &ref, float2 &s, const T *from, int from_left) const {
+    if constexpr (TURN < TURNS) {
+      cp_async_wait<GRAD ? TURNS - 1 - TURN : TURNS - 1>();
+      if (TURN * B * NT < left) add_turn<TURN>(ring, left, marks, m, ref, s);
+      if (!GRAD) fetch(TURN, from, from_left, ring);
+      add_turns<TURN + 1>(ring, left, marks, m, ref, s, from, from_left);
     }
-  };
-  auto join_parts = [&](auto &others, auto &tops, double &qz) {
-    for (int c = 0; c < a.cluster; ++c) {
-      const DistillPart &p = sh.part[c];
-      const float f = p.m > -INFINITY ? ex2((p.m - rm) * ch) : 1.f;
-      others += p.others * f; tops += p.tops * f; qz += p.qz;
+  }
+  template <int TURN> __device__ __forceinline__ void write_turns(uint4 *ring, int left, const uint4 &marks, T *out, bool vec, const Slope &g, const T *from, int from_left) const {
+    if constexpr (TURN < TURNS) {
+      if (TURN * B * NT < left) write_turn<TURN>(ring, left, marks, out, vec, g);
+      fetch(TURN, from, from_left, ring);
+      write_turns<TURN + 1>(ring, left, marks, out, vec, g, from, from_left);
     }
-  };
-  if (a.cluster > 1) {
+  }
+  __device__ __forceinline__ void stream_warp(uint4 *ring) const {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool tail = a.teacher_lse != nullptr;
+    const uint4 unmarked = make_uint4(0u, 0u, 0u, 0u);
+    RowShare<T> sr = share(first_row), next = sr;
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) fetch(t, sr.mine, sr.nv - tid, ring);
+    float le = sr.edge >= 0 ? to_f(sr.row[sr.edge]) : -INFINITY;
     cluster_started_wait(a.cluster);
-    if (tid < a.cluster) {
-      double others = 0.0, tops = 0.0;
-      join(others, tops);
-      const uint32_t to = mapa(smem_u32(&sh.part[rank]), tid);
-      st_cluster_u64(to, (unsigned long long)__float_as_uint(rm));
-      st_cluster_u64(to + 8, __double_as_longlong(others));
-      st_cluster_u64(to + 16, __double_as_longlong(tops));
-      st_cluster_u64(to + 24, __double_as_longlong(sh.qz_row));
-    }
-    cluster_sync_all();
-    for (int c = 0; c < a.cluster; ++c) rm = fmaxf(rm, sh.part[c].m);
-  }
-  if (GRAD) {
-    float others = 0.f, tops = 0.f;
-    double unused = 0.0;
-    if (a.cluster > 1) join_parts(others, tops, unused);
-    else join(others, tops);
-    const float total = others + tops, ref = rm > -INFINITY ? rm : 0.f, d = __log2f(total), scale = total == 0.f || sh.total == 0.f ? 0.f : rs * (float)a.inv_tau,
-                coef = scale * (sh.total - (sh.rest > 0.f && others > 0.f ? sh.rest * __fdividef(total, others) : 0.f));
-    T *dst = (T *)a.grad + row * a.grad_ld;
-    // a scale of zero: padding, or nothing to learn from; zeros, whatever the logits hold
-    if (first) {
-      if (sh.repeated) {
-        qj = 0.0;
-        for (int j = 0; j < a.top; ++j) if (sh.id[j] == t.id) qj += sh.q[j];
+    block_barrier<THREADS>();
+    int p = 0;
+#pragma unroll 1
+    for (int row = first_row; row < a.rows; row += clusters, p ^= 1) {
+      const uint8_t *fl = flags_of(p);
+      const bool more = row + clusters < a.rows;
+      if (more) next = share(row + clusters);
+      // running maximum m (ref: the same, 0 without one) and sum of 2^((l - ref) ch); listed ids stay out where the rest is a bucket
+      float m = -INFINITY, ref = 0.f;
+      float2 s = make_float2(0.f, 0.f);
+      const bool listed_edge = sr.edge >= 0 && (fl[edge_byte() + (tid >> 3)] >> (tid & 7) & 1u);
+      if (sr.edge >= 0 && !(tail && listed_edge)) {
+        if (le > m) { m = ref = le; s.x = 1.f; }
+        else if (le != le) s.x = le;
       }
-      dst[t.id] = from_f<T>(scale == 0.f ? 0.f : (float)((double)scale * (tr.total * (double)ex2(fmaf(z - ref, ch, -d)) - qj)));
+      const float rs = GRAD && a.row_scale ? a.row_scale[row] : 1.f;
+      const T *from = sr.mine;
+      int left = sr.nv - tid, block = 0;
+#pragma unroll 1
+      do {
+        const uint4 marks = tail ? reinterpret_cast<const uint4 *>(fl)[block * NT + tid] : unmarked;
+        const bool last = GRAD || sr.nv <= (block + 1) * PER * NT;
+        from = last ? next.mine : from + PER * NT * VEC;
+        const int from_left = last ? (more ? next.nv - tid : 0) : left - PER * NT;
+        add_turns<0>(ring, left, marks, m, ref, s, from, from_left);
+        left -= PER * NT;
+        ++block;
+      } while (!GRAD && sr.nv > block * PER * NT);
+      const float wm = warp_max(m);
+      s.x = warp_sum((s.x + s.y) * (m > -INFINITY ? ex2((m - wm) * ch) : 1.f));       // without a maximum 0, or NaN
+      if (lane == 0) sh.pair[p][warp] = make_float2(wm, s.x);
+      block_barrier<THREADS>();
+      if (a.cluster > 1) cluster_sync_all();
+      const float le_now = le;
+      if (more) le = next.edge >= 0 ? to_f(next.row[next.edge]) : -INFINITY;
+      if (GRAD) {
+        const Slope g = slope(p, rs);
+        T *dst = (T *)a.grad + row * a.grad_ld, *out = dst + sr.id0 + tid * VEC;
+        const bool vec = ((uintptr_t)out & 15) == 0;
+        const int from_left = more ? next.nv - tid : 0;
+        left = sr.nv - tid;
+        if (sr.edge >= 0 && !listed_edge) dst[sr.edge] = from_f<T>(g.scale == 0.f ? 0.f : g.coef * ex2(fmaf(le_now - g.ref, ch, -g.d)));
+        const uint4 marks = reinterpret_cast<const uint4 *>(fl)[tid];
+        if (g.scale == 0.f) {                               // zeros, whatever the logits hold
+#pragma unroll 1
+          for (int j = 0; j < PER; ++j) {
+            const uint32_t u = j < 4 ? marks.x : j < 8 ? marks.y : j < 12 ? marks.z : marks.w;
+            if (j * NT < left) store_unlisted<T>(out + j * NT * VEC, vec, unmarked, u >> (j % 4 * 8) & 0xffu);
+          }
+#pragma unroll
+          for (int t = 0; t < TURNS; ++t) fetch(t, next.mine, from_left, ring);
+        } else write_turns<0>(ring, left, marks, out, vec, g, next.mine, from_left);
+      }
+      sr = next;
+      block_barrier<THREADS>();
     }
-    write_row<T>(sr, dst, scale == 0.f, [&](int k) { return vals[k * NT]; }, [&](int g) { return (uint32_t)flags[g]; }, sr.edge >= 0 && !listed_edge, le, ref, ch, d, coef);
+    cp_async_wait<0>();
   }
-  if (rank == 0 && warp == NW - 1 && lane == 0) {
-    double others = 0.0, tops = 0.0, qz = 0.0;
-    if (a.cluster > 1) join_parts(others, tops, qz);
-    else { join(others, tops); qz = sh.qz_row; }
-    const double total = others + tops, lse = (double)rm * a.inv_tau + log(total);
-    const bool none = total == 0.0;                         // no finite logit
-    double loss = sh.entropy - qz * a.inv_tau + ((double)sh.total - (double)sh.rest) * lse;
-    if (tail) {
-      const double log_rest = others > 0.0 ? -log1p(tops / others) : others == 0.0 ? -INFINITY : others;
-      if (sh.rest > 0.f) loss -= (double)sh.rest * log_rest;
-      a.log_rest[row] = none ? -INFINITY : (float)log_rest;
-    }
-    a.loss[row] = (float)(sh.total == 0.f ? 0.0 : none ? (double)INFINITY : loss);
-    a.lse[row] = none ? -INFINITY : (float)lse;
-  }
+};
+
+// GRAD: the gradient leaves in the same call.
+template <typename T, bool GRAD, int SW>
+__global__ void __launch_bounds__((SW + 1) * 32, SW == 8 ? 3 : 1)
+k_distill(const __grid_constant__ DistillArgs a) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  DistillShared<SW> &sh = *reinterpret_cast<DistillShared<SW> *>(smem_raw);
+  uint8_t *flags = smem_raw + (sizeof(DistillShared<SW>) + 15) / 16 * 16;
+  cluster_started_arrive(a.cluster);
+  kernel_entry(TR_k_distill);
+  const DistillBlock<T, GRAD, SW> blk = {a, sh, flags, a.cluster > 1 ? (int)cluster_ctarank() : 0, (int)blockIdx.x / a.cluster, (int)gridDim.x / a.cluster,
+                                         (float)(a.inv_tau * 1.4426950408889634)};
+  if (threadIdx.x >= SW * 32) blk.side_warp();
+  else blk.stream_warp(reinterpret_cast<uint4 *>(flags + 2 * distill_flag_bytes(a.cta_vecs, SW * 32)) + threadIdx.x);
 }
 
 // The gradient from a saved log-sum-exp (and, with teacher_lse, log_rest).  A CTA walks `cta_vecs` vectors of a row with a ring of copies ahead
@@ -469,9 +684,8 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   T *dst = (T *)a.grad + row * a.grad_ld;
   const float rs = a.row_scale ? a.row_scale[row] : 1.f;
   auto none = [](int) { return make_uint4(0u, 0u, 0u, 0u); };
-  auto nobody = [](int) { return 0u; };
   if (rs == 0.f || a.lse[row] == -INFINITY) {               // a row of padding is not read
-    write_row<T>(sr, dst, true, none, nobody, sr.edge >= 0, 0.f, 0.f, 0.f, 0.f, 0.f);
+    write_row<T>(sr, dst, true, none, 0.f, 0.f, 0.f, 0.f, 0.f);
     return;
   }
   auto fetch = [&](int k) {
@@ -494,7 +708,7 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   // logits relative to tau lse, so that the difference that the exponential sees is small where p is not
   const float ch = (float)(a.inv_tau * 1.4426950408889634), ref = (float)(lse / a.inv_tau),
               d = (float)((lse - (double)ref * a.inv_tau) * 1.4426950408889634), coef = (float)(scale * (tr.total - tail));
-  const bool mine = sr.flag_bit(t.id, a.vocab, blockIdx.x - row * a.cluster, a.cluster) >= 0 && scale != 0.0;
+  const bool mine = sr.template flag_bit<NT>(t.id, blockIdx.x - row * a.cluster, a.cluster, 0) >= 0 && scale != 0.0;
   float g_top = 0.f;
   if (tid < DISTILL_MAX_TOP) { sq[tid] = t.e * tr.mine(); sid[tid] = t.id; }
   __syncthreads();
@@ -509,7 +723,7 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
     const uint4 q = vals[k % DISTILL_GRAD_RING * NT];
     fetch(k + DISTILL_GRAD_RING);
     return q;
-  }, nobody, sr.edge >= 0, le, ref, ch, d, coef);
+  }, le, ref, ch, d, coef);
   cp_async_wait<0>();
   __syncthreads();
   if (mine) dst[t.id] = from_f<T>(g_top);

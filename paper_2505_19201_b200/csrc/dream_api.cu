@@ -1627,6 +1627,39 @@ static const char *launch_rows(void (*kernel)(A), int rows, int cluster, int thr
   return cudaGetErrorString(e);
 }
 
+// How many clusters (blocks, where cluster is 1) of a kernel are resident on the current device at once: what a kernel that loops over rows is
+// launched with, since a cluster that had to wait for a place would start when the others are done.  The GPU's SMs come in groups that a
+// cluster does not cross, so this is less than SMs times blocks: 48 clusters of eight with three blocks per SM, not 55.
+template <typename A>
+static int resident_clusters(void (*kernel)(A), int cluster, int threads, size_t smem) {
+  struct Known { const void *kernel; int device, cluster, threads, n; size_t smem; };
+  static thread_local Known known[16];
+  static thread_local int next = 0;
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); return 1; }
+  for (const Known &k : known)
+    if (k.kernel == (const void *)kernel && k.device == device && k.cluster == cluster && k.threads == threads && k.smem == smem) return k.n;
+  int n = 0, sms = 0, per = 0;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (cluster > 1) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)cluster * 1024); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+  } else {
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, threads, smem);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    n = per * sms;
+  }
+  if (e != cudaSuccess || n < 1) { cudaGetLastError(); return 1; }      // the launch will say what is wrong
+  known[next] = {(const void *)kernel, device, cluster, threads, n, smem};
+  next = (next + 1) % 16;
+  return n;
+}
+
 // What every entry point on rows of logits asks of its matrix.
 static dream_status check_rows(const char *who, const void *p, int dtype, int rows, int vocab, long long ld, int max_vocab) {
   if (!p) return fail(nullptr, DREAM_E_ARG, "%s: null buffer", who);
@@ -1733,7 +1766,7 @@ static dream_status distill_args(const char *who, DistillArgs *a, const void *lo
   if (!teacher_lse != !log_rest) return fail(nullptr, DREAM_E_ARG, "%s: log_rest goes with teacher_lse", who);
   if (grad && rows_collide(logits, ld, grad, grad_ld, dtype, rows, vocab)) return fail(nullptr, DREAM_E_ARG, "%s: grad overlaps logits without being logits", who);
   memset(a, 0, sizeof(*a));
-  a->logits = logits; a->vocab = vocab; a->ld = ld; a->ids = ids; a->teacher = teacher; a->top = top; a->teacher_lse = teacher_lse;
+  a->logits = logits; a->rows = rows; a->vocab = vocab; a->ld = ld; a->ids = ids; a->teacher = teacher; a->top = top; a->teacher_lse = teacher_lse;
   a->inv_tau = 1.0 / (double)temperature; a->lse = lse; a->log_rest = log_rest; a->row_scale = row_scale;
   a->grad = grad; a->grad_ld = grad_ld;
   return DREAM_OK;
@@ -1749,17 +1782,17 @@ extern "C" dream_status dream_distill_loss(const void *logits, int32_t dtype, in
                                 temperature, lse, log_rest, row_scale, grad, grad_ld);
   if (s) return s;
   a.loss = loss;
-  // With a gradient a CTA keeps its share of the row, 64 KB where a cluster of eight can hold the row so: three CTAs per SM then take turns at
-  // loading, summing and writing.  Without one it needs a ring and a byte per vector, and as few CTAs per row as keep the SMs busy.
-  const int vecs = imax(1, vocab / (dtype == DREAM_BF16 ? 8 : 4)), most = grad ? 4096 : 16384;
+  // With a gradient the ring holds a CTA's share of a row, 64 KB, in the widest fp32 rows 128 KB; without one the share is bounded by its byte per
+  // vector.  More CTAs to a row where there are few rows.  Three CTAs per SM.
+  const int vecs = imax(1, vocab / (dtype == DREAM_BF16 ? 8 : 4)), wide = grad && vecs > DISTILL_MAX_CLUSTER * 4096, most = grad ? (wide ? 8192 : 4096) : 8192;
   a.cluster = 1;
-  while (a.cluster < DISTILL_MAX_CLUSTER && (vecs > a.cluster * most || (!grad && rows * a.cluster < 148 * 3 * 4 && vecs > a.cluster * 2048))) a.cluster *= 2;
+  while (a.cluster < DISTILL_MAX_CLUSTER && (vecs > a.cluster * most || (rows * a.cluster < 148 * 2 && vecs > a.cluster * 1024))) a.cluster *= 2;
   a.cta_vecs = (vecs + a.cluster - 1) / a.cluster;
-  const int slots = grad ? (a.cta_vecs + DISTILL_THREADS - 1) / DISTILL_THREADS : DISTILL_RING, threads = DISTILL_THREADS;
-  const size_t smem = (sizeof(DistillShared) + 15) / 16 * 16 + distill_flag_bytes(a.cta_vecs) + (size_t)slots * threads * 16;
-  void (*kernel)(DistillArgs) = dtype == DREAM_BF16 ? (grad ? k_distill<bf16, true> : k_distill<bf16, false>)
-                                                    : (grad ? k_distill<float, true> : k_distill<float, false>);
-  const char *why = launch_rows(kernel, rows, a.cluster, threads, smem, (cudaStream_t)cuda_stream, a);
+  const int warps = wide ? 16 : 8;
+  const size_t smem = ((wide ? sizeof(DistillShared<16>) : sizeof(DistillShared<8>)) + 15) / 16 * 16 + 2 * (size_t)distill_flag_bytes(a.cta_vecs, warps * 32) + (size_t)DISTILL_PER * warps * 32 * 16;
+  void (*kernel)(DistillArgs) = wide ? k_distill<float, true, 16>
+                              : dtype == DREAM_BF16 ? (grad ? k_distill<bf16, true, 8> : k_distill<bf16, false, 8>) : (grad ? k_distill<float, true, 8> : k_distill<float, false, 8>);
+  const char *why = launch_rows(kernel, imin(rows, resident_clusters(kernel, a.cluster, warps * 32 + 32, smem)), a.cluster, warps * 32 + 32, smem, (cudaStream_t)cuda_stream, a);
   return why ? fail(nullptr, DREAM_E_CUDA, "dream_distill_loss: %s", why) : DREAM_OK;
 }
 
