@@ -502,27 +502,29 @@ struct DistillBlock {
   }
 
   // ---- the stream warps
-  // The next block's vectors of a turn, where the block has them (left: ids of vectors from the thread's first on), as one group of copies.
+  // The vectors of a turn of the next block, where the block has them (left: ids of vectors from the thread's first on), as one group of copies.
+  // The passes are loops over turns whose body is as short as it gets: unrolled over a block they waited for instructions more than
+  // for anything else.
   __device__ __forceinline__ void fetch(int turn, const T *from, int left, uint4 *ring) const {
 #pragma unroll
     for (int k = 0; k < B; ++k)
       if ((turn * B + k) * NT < left) cp_async16(ring + (turn * B + k) * NT, from + (turn * B + k) * NT * VEC);
     cp_async_commit();
   }
-  template <int TURN> __device__ __forceinline__ void add_turn(const uint4 *ring, int left, const uint4 &marks, float &m, float &ref, float2 &s) const {
+  // ring, left and marks are the turn's own.
+  __device__ __forceinline__ void add_turn(const uint4 *ring, int left, uint32_t listed, float &m, float &ref, float2 &s) const {
     uint4 q[B];
 #pragma unroll
     for (int k = 0; k < B; ++k) {
       const uint32_t u = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;            // -inf
       q[k] = make_uint4(u, u, u, u);
-      if ((TURN * B + k) * NT < left) q[k] = ring[(TURN * B + k) * NT];
+      if (k * NT < left) q[k] = ring[k * NT];
     }
     float l[B][VEC], v = max_vec<T, VEC>(q[0]);
 #pragma unroll
     for (int k = 0; k < B; ++k) unpack_vec<T, VEC>(q[k], l[k]);
 #pragma unroll
     for (int k = 1; k < B; ++k) v = fmaxf(v, max_vec<T, VEC>(q[k]));
-    const uint32_t listed = turn_marks<TURN>(marks);
     if (listed) {
       v = -INFINITY;
 #pragma unroll
@@ -546,47 +548,40 @@ struct DistillBlock {
         s = add_pair(s, make_float2(ex2(y.x), ex2(y.y)));
       }
   }
-  template <int TURN> static __device__ __forceinline__ uint32_t turn_marks(const uint4 &m) {     // B bytes
-    constexpr int w = TURN * B / 4;
-    const uint32_t u = w == 0 ? m.x : w == 1 ? m.y : w == 2 ? m.z : m.w;
-    return B == 4 ? u : TURN & 1 ? u >> 16 : u & 0xffffu;
-  }
-  template <int TURN> __device__ __forceinline__ void write_turn(const uint4 *ring, int left, const uint4 &marks, T *out, bool vec, const Slope &g) const {
+  __device__ __forceinline__ void write_turn(const uint4 *ring, int left, uint32_t listed, T *out, bool vec, const Slope &g) const {
     const float2 r2 = make_float2(-g.ref, -g.ref), c2 = make_float2(ch, ch), d2 = make_float2(-g.d, -g.d), o2 = make_float2(g.coef, g.coef);
-    const uint32_t listed = turn_marks<TURN>(marks);
+    uint4 q[B];
 #pragma unroll
-    for (int k = 0; k < B; ++k)
-      if ((TURN * B + k) * NT < left) {
-        float l[VEC];
-        unpack_vec<T, VEC>(ring[(TURN * B + k) * NT], l);
+    for (int k = 0; k < B; ++k) {
+      q[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (k * NT < left) q[k] = ring[k * NT];
+    }
 #pragma unroll
-        for (int e = 0; e < VEC; e += 2) {
-          const float2 y = fma_pair(add_pair(make_float2(l[e], l[e + 1]), r2), c2, d2);
-          const float2 o = mul_pair(make_float2(ex2(y.x), ex2(y.y)), o2);
-          l[e] = o.x; l[e + 1] = o.y;
-        }
-        store_unlisted<T>(out + (TURN * B + k) * NT * VEC, vec, pack_vec<T, VEC>(l), listed >> (k * 8) & 0xffu);
+    for (int k = 0; k < B; ++k) {
+      float l[VEC];
+      unpack_vec<T, VEC>(q[k], l);
+#pragma unroll
+      for (int e = 0; e < VEC; e += 2) {
+        const float2 y = fma_pair(add_pair(make_float2(l[e], l[e + 1]), r2), c2, d2);
+        const float2 o = mul_pair(make_float2(ex2(y.x), ex2(y.y)), o2);
+        l[e] = o.x; l[e + 1] = o.y;
       }
-  }
-  template <int TURN> __device__ __forceinline__ void add_turns(uint4 *ring, int left, const uint4 &marks, float &m, float &ref, float2 &s, const T *from, int from_left) const {
-    if constexpr (TURN < TURNS) {
-      cp_async_wait<GRAD ? TURNS - 1 - TURN : TURNS - 1>();
-      if (TURN * B * NT < left) add_turn<TURN>(ring, left, marks, m, ref, s);
-      if (!GRAD) fetch(TURN, from, from_left, ring);
-      add_turns<TURN + 1>(ring, left, marks, m, ref, s, from, from_left);
+      q[k] = pack_vec<T, VEC>(l);
+    }
+    if (vec && !listed) {
+#pragma unroll
+      for (int k = 0; k < B; ++k) if (k * NT < left) *reinterpret_cast<uint4 *>(out + k * NT * VEC) = q[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < B; ++k) if (k * NT < left) store_unlisted<T>(out + k * NT * VEC, vec, q[k], listed >> (k * 8) & 0xffu);
     }
   }
-  template <int TURN> __device__ __forceinline__ void write_turns(uint4 *ring, int left, const uint4 &marks, T *out, bool vec, const Slope &g, const T *from, int from_left) const {
-    if constexpr (TURN < TURNS) {
-      if (TURN * B * NT < left) write_turn<TURN>(ring, left, marks, out, vec, g);
-      fetch(TURN, from, from_left, ring);
-      write_turns<TURN + 1>(ring, left, marks, out, vec, g, from, from_left);
-    }
+  static __device__ __forceinline__ uint32_t turn_marks(const uint8_t *f) {      // of the thread's B vectors
+    return B == 4 ? *reinterpret_cast<const uint32_t *>(f) : *reinterpret_cast<const uint16_t *>(f);
   }
   __device__ __forceinline__ void stream_warp(uint4 *ring) const {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const bool tail = a.teacher_lse != nullptr;
-    const uint4 unmarked = make_uint4(0u, 0u, 0u, 0u);
     RowShare<T> sr = share(first_row), next = sr;
 #pragma unroll
     for (int t = 0; t < TURNS; ++t) fetch(t, sr.mine, sr.nv - tid, ring);
@@ -612,11 +607,19 @@ struct DistillBlock {
       int left = sr.nv - tid, block = 0;
 #pragma unroll 1
       do {
-        const uint4 marks = tail ? reinterpret_cast<const uint4 *>(fl)[block * NT + tid] : unmarked;
+        const uint8_t *marks = fl + (block * NT + tid) * PER;
         const bool last = GRAD || sr.nv <= (block + 1) * PER * NT;
         from = last ? next.mine : from + PER * NT * VEC;
         const int from_left = last ? (more ? next.nv - tid : 0) : left - PER * NT;
-        add_turns<0>(ring, left, marks, m, ref, s, from, from_left);
+#pragma unroll 1
+        for (int t = 0; t < TURNS; ++t) {
+          if (!GRAD) cp_async_wait<TURNS - 1>();
+          else if (t == 0) cp_async_wait<TURNS / 2>();
+          else if (t == TURNS / 2) cp_async_wait<0>();
+          const int here = left - t * B * NT;
+          if (here > 0) add_turn(ring + t * B * NT, here, tail ? turn_marks(marks + t * B) : 0u, m, ref, s);
+          if (!GRAD) fetch(t, from, from_left, ring);
+        }
         left -= PER * NT;
         ++block;
       } while (!GRAD && sr.nv > block * PER * NT);
@@ -634,16 +637,18 @@ struct DistillBlock {
         const int from_left = more ? next.nv - tid : 0;
         left = sr.nv - tid;
         if (sr.edge >= 0 && !listed_edge) dst[sr.edge] = from_f<T>(g.scale == 0.f ? 0.f : g.coef * ex2(fmaf(le_now - g.ref, ch, -g.d)));
-        const uint4 marks = reinterpret_cast<const uint4 *>(fl)[tid];
-        if (g.scale == 0.f) {                               // zeros, whatever the logits hold
+        const uint8_t *marks = fl + tid * PER;
 #pragma unroll 1
-          for (int j = 0; j < PER; ++j) {
-            const uint32_t u = j < 4 ? marks.x : j < 8 ? marks.y : j < 12 ? marks.z : marks.w;
-            if (j * NT < left) store_unlisted<T>(out + j * NT * VEC, vec, unmarked, u >> (j % 4 * 8) & 0xffu);
+        for (int t = 0; t < TURNS; ++t) {
+          const int here = left - t * B * NT;
+          if (here > 0) {
+            if (g.scale != 0.f) write_turn(ring + t * B * NT, here, turn_marks(marks + t * B), out + t * B * NT * VEC, vec, g);
+            else                                            // zeros, whatever the logits hold
+              for (int k = 0; k < B; ++k)
+                if (k * NT < here) store_unlisted<T>(out + (t * B + k) * NT * VEC, vec, make_uint4(0u, 0u, 0u, 0u), marks[t * B + k]);
           }
-#pragma unroll
-          for (int t = 0; t < TURNS; ++t) fetch(t, next.mine, from_left, ring);
-        } else write_turns<0>(ring, left, marks, out, vec, g, next.mine, from_left);
+          fetch(t, next.mine, from_left, ring);
+        }
       }
       sr = next;
       block_barrier<THREADS>();
