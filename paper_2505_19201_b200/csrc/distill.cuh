@@ -185,10 +185,10 @@ struct DistillSide {
 };
 template <int SW> struct DistillShared {
   DistillPart part[2][DISTILL_MAX_CLUSTER];
-  DistillSide side[2];
+  DistillSide side[4];
   float2 pair[2][SW];                  // (maximum, sum) of every stream warp
   float q[DISTILL_MAX_TOP];            // for ids that are listed twice
-  int id[2][DISTILL_MAX_TOP];
+  int id[DISTILL_MAX_TOP];
 };
 // Shared memory behind it, twice: a byte per vector of the CTA's share, whose bits say which ids are listed, and 16 bytes of such bits for the
 // ids at the row's ends.  Then the ring of vectors.
@@ -232,14 +232,14 @@ template <typename T> struct RowShare {
   }
 };
 
-// A vector of a gradient, without the elements in `listed`, which somebody else writes.
-template <typename T> __device__ __forceinline__ void store_unlisted(T *p, bool vec, const uint4 &q, uint32_t listed) {
-  if (vec && !listed) { *reinterpret_cast<uint4 *>(p) = q; return; }
+// A vector of a gradient; vec: it lies on a 16-byte boundary.
+template <typename T> __device__ __forceinline__ void store_vec(T *p, bool vec, const uint4 &q) {
+  if (vec) { *reinterpret_cast<uint4 *>(p) = q; return; }
   constexpr int VEC = 16 / sizeof(T);
   T t[VEC];
   memcpy(t, &q, 16);
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) if (!(listed >> e & 1u)) p[e] = t[e];
+  for (int e = 0; e < VEC; ++e) p[e] = t[e];
 }
 // The gradient coef * 2^((l - ref) ch - d) of the thread's vectors, get(k) being the k-th's logits, and of its single id's logit le.  Nothing is
 // got where it is zero.
@@ -263,7 +263,7 @@ __device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool ze
       }
       q = pack_vec<T, VEC>(l);
     }
-    store_unlisted<T>(p, vec, q, 0u);
+    store_vec<T>(p, vec, q);
   }
 }
 
@@ -290,36 +290,36 @@ struct DistillBlock {
   __device__ __forceinline__ int edge_byte() const { return distill_flag_bytes(a.cta_vecs, NT) - 16; }
   __device__ __forceinline__ float scaled(float m, float s, float to) const { return m > -INFINITY ? s * ex2((m - to) * ch) : s; }
   // The row's largest logit and its sums, from this CTA's warps or the cluster's parts.
-  template <typename R> __device__ __forceinline__ void sums(int p, float &rm, R &others, R &tops, double *qz) const {
+  template <typename R> __device__ __forceinline__ void sums(int i, float &rm, R &others, R &tops, double *qz) const {
     rm = -INFINITY; others = 0; tops = 0;
     if (a.cluster > 1) {
-      for (int c = 0; c < a.cluster; ++c) rm = fmaxf(rm, sh.part[p][c].m);
+      for (int c = 0; c < a.cluster; ++c) rm = fmaxf(rm, sh.part[i & 1][c].m);
       for (int c = 0; c < a.cluster; ++c) {
-        const DistillPart &x = sh.part[p][c];
+        const DistillPart &x = sh.part[i & 1][c];
         const float f = x.m > -INFINITY ? ex2((x.m - rm) * ch) : 1.f;
         others += x.others * f; tops += x.tops * f;
         if (qz) *qz += x.qz;
       }
     } else {
-      own_sums(p, rm, others, tops);
-      if (qz) *qz = sh.side[p].qz;
+      own_sums(i, rm, others, tops);
+      if (qz) *qz = sh.side[i & 3].qz;
     }
   }
-  template <typename R> __device__ __forceinline__ void own_sums(int p, float &rm, R &others, R &tops) const {
-    rm = sh.side[p].top_m;
+  template <typename R> __device__ __forceinline__ void own_sums(int i, float &rm, R &others, R &tops) const {
+    rm = sh.side[i & 3].top_m;
 #pragma unroll
-    for (int w = 0; w < SW; ++w) rm = fmaxf(rm, sh.pair[p][w].x);
+    for (int w = 0; w < SW; ++w) rm = fmaxf(rm, sh.pair[i & 1][w].x);
 #pragma unroll
-    for (int w = 0; w < SW; ++w) others += scaled(sh.pair[p][w].x, sh.pair[p][w].y, rm);
-    if (a.teacher_lse) tops += scaled(sh.side[p].top_m, sh.side[p].tops, rm);   // without the bucket they are among the others
+    for (int w = 0; w < SW; ++w) others += scaled(sh.pair[i & 1][w].x, sh.pair[i & 1][w].y, rm);
+    if (a.teacher_lse) tops += scaled(sh.side[i & 3].top_m, sh.side[i & 3].tops, rm);   // without the bucket they are among the others
   }
   // What the gradient of a row needs.
   struct Slope { float ref, d, scale, coef; };
-  __device__ __forceinline__ Slope slope(int p, float rs) const {
+  __device__ __forceinline__ Slope slope(int i, float rs) const {
     Slope g;
     float rm, others, tops;
-    sums(p, rm, others, tops, nullptr);
-    const float total = others + tops, q = sh.side[p].total, rest = sh.side[p].rest;
+    sums(i, rm, others, tops, nullptr);
+    const float total = others + tops, q = sh.side[i & 3].total, rest = sh.side[i & 3].rest;
     g.ref = rm > -INFINITY ? rm : 0.f;
     g.d = __log2f(total);
     g.scale = total == 0.f || q == 0.f ? 0.f : rs * (float)a.inv_tau;         // 0: padding, or nothing to learn from
@@ -329,46 +329,47 @@ struct DistillBlock {
 
   // ---- the side warp: lane's entries are lane, lane + 32, ..
   static constexpr int E = DISTILL_MAX_TOP / 32;
-  struct Entries { int id[E]; float t[E], z[E], q[E]; bool first[E]; };
-  __device__ __forceinline__ void load_entries(int row, Entries &n) const {
+  struct Entries { int id[E], bit[E]; float z[E], q[E]; bool first[E]; };      // bit: its mark's place, -1 outside the share
+  __device__ __forceinline__ void load_entries(int row, int (&id)[E], float (&t)[E]) const {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int j = lane + 32 * i;
-      n.id[i] = -1; n.t[i] = -INFINITY;
+      id[i] = -1; t[i] = -INFINITY;
       if (j < a.top && row < a.rows) {
-        const int id = a.ids[(long long)row * a.top + j];
-        n.t[i] = a.teacher[(long long)row * a.top + j];
-        n.id[i] = id >= 0 && id < a.vocab ? id : -1;
+        id[i] = a.ids[(long long)row * a.top + j];
+        t[i] = a.teacher[(long long)row * a.top + j];
+        if (id[i] < 0 || id[i] >= a.vocab) id[i] = -1;
       }
     }
   }
-  // Marks the row's listed ids, and leaves sh.side[p].
-  __device__ __forceinline__ void prepare(int row, int p, Entries &n) const {
+  // Marks the listed ids of a row, the i-th of the block, whose entries are id and t, and leaves sh.side[i & 3].
+  __device__ __forceinline__ void prepare(int row, int i_row, const int (&id)[E], const float (&t)[E], Entries &n) const {
+#pragma unroll
+    for (int i = 0; i < E; ++i) { n.id[i] = id[i]; n.bit[i] = -1; n.first[i] = false; n.z[i] = -INFINITY; n.q[i] = 0.f; }
     if (row >= a.rows) return;
     const int lane = threadIdx.x & 31;
     const RowShare<T> sr = share(row);
-    uint32_t *words = reinterpret_cast<uint32_t *>(flags_of(p));
+    uint32_t *words = reinterpret_cast<uint32_t *>(flags_of(i_row & 1));
     double x[E], e[E], ref = -INFINITY, s = 0.0, l = 0.0, qz = 0.0;
-    int bit[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      bit[i] = sr.template flag_bit<NT>(n.id[i], rank, a.cluster, edge_byte());
-      n.z[i] = bit[i] >= 0 ? to_f(sr.row[n.id[i]]) : -INFINITY;
-      n.first[i] = bit[i] >= 0;
-      x[i] = n.id[i] >= 0 ? (double)n.t[i] * a.inv_tau : -INFINITY;
-      sh.id[p][lane + 32 * i] = n.id[i];
+      n.bit[i] = sr.template flag_bit<NT>(n.id[i], rank, a.cluster, edge_byte());
+      if (n.bit[i] >= 0) n.z[i] = to_f(sr.row[n.id[i]]);
+      n.first[i] = n.bit[i] >= 0;
+      x[i] = n.id[i] >= 0 ? (double)t[i] * a.inv_tau : -INFINITY;
+      sh.id[lane + 32 * i] = n.id[i];
     }
     bool twice = false;
 #pragma unroll
     for (int i = 0; i < E; ++i)
-      if (bit[i] >= 0 && (atomicOr(words + (bit[i] >> 5), 1u << (bit[i] & 31)) >> (bit[i] & 31) & 1u)) twice = true;
+      if (n.bit[i] >= 0 && (atomicOr(words + (n.bit[i] >> 5), 1u << (n.bit[i] & 31)) >> (n.bit[i] & 31) & 1u)) twice = true;
     twice = __any_sync(0xffffffffu, twice);
     __syncwarp();
     if (twice) {                                            // of the entries of one id the first stands for it
 #pragma unroll
       for (int i = 0; i < E; ++i)
-        for (int j = 0; j < lane + 32 * i; ++j) if (sh.id[p][j] == n.id[i]) n.first[i] = false;
+        for (int j = 0; j < lane + 32 * i; ++j) if (sh.id[j] == n.id[i]) n.first[i] = false;
     }
     if (a.teacher_lse) ref = (double)a.teacher_lse[row];
     else {
@@ -386,7 +387,7 @@ struct DistillBlock {
         s += e[i];
         if (!(e[i] == 0.0)) {
           l += e[i] * (a.teacher_lse ? x[i] - ref : x[i]);
-          if (bit[i] >= 0) qz += e[i] * (double)n.z[i];
+          if (n.bit[i] >= 0) qz += e[i] * (double)n.z[i];
         }
         tm = fmaxf(tm, n.z[i]);
       }
@@ -421,18 +422,19 @@ struct DistillBlock {
       for (int i = 0; i < E; ++i)
         if (n.first[i]) {
           n.q[i] = 0.f;
-          for (int j = 0; j < a.top; ++j) if (sh.id[p][j] == n.id[i]) n.q[i] += sh.q[j];
+          for (int j = 0; j < a.top; ++j) if (sh.id[j] == n.id[i]) n.q[i] += sh.q[j];
         }
       __syncwarp();
     }
-    if (lane == 0) sh.side[p] = d;
+    if (lane == 0) sh.side[i_row & 3] = d;
+    __syncwarp();
   }
-  __device__ __forceinline__ void finish(int row, int p) const {
-    if (rank || row < 0) return;
+  __device__ __forceinline__ void finish(int row, int i) const {
+    if (rank) return;
     float rm;
     double others, tops, qz = 0.0;
-    sums(p, rm, others, tops, &qz);
-    const DistillSide &d = sh.side[p];
+    sums(i, rm, others, tops, &qz);
+    const DistillSide &d = sh.side[i & 3];
     const double total = others + tops, lse = (double)rm * a.inv_tau + log(total);
     const bool none = total == 0.0;                         // no finite logit
     double loss = d.entropy - qz * a.inv_tau + ((double)d.total - (double)d.rest) * lse, log_rest = 0.0;
@@ -446,59 +448,68 @@ struct DistillBlock {
       a.lse[row] = none ? -INFINITY : (float)lse;
     }
   }
+  // One barrier to a row, when its sums are there.  Behind it the stream warps write the row's gradient and go on to the next row, while this warp
+  // replaces the gradients of the listed ids of the row before, whose others are all out by now, computes this row's, finishes its loss and
+  // prepares the row after the next, whose marks take the place of this row's.
   __device__ __forceinline__ void side_warp() const {
-    Entries n;
-    load_entries(first_row, n);
+    Entries n, next;
+    int id[E];
+    float t[E], g_top[E];
+    load_entries(first_row, id, t);
     for (int i = threadIdx.x & 31; i < distill_flag_bytes(a.cta_vecs, NT) * 2 / 4; i += 32) reinterpret_cast<uint32_t *>(flags)[i] = 0;
     __syncwarp();
-    prepare(first_row, 0, n);
+    prepare(first_row, 0, id, t, n);
+    load_entries(first_row + clusters, id, t);
+    prepare(first_row + clusters, 1, id, t, next);
     cluster_started_wait(a.cluster);
     block_barrier<THREADS>();
-    int p = 0, last = -1;
-    for (int row = first_row; row < a.rows; row += clusters, p ^= 1) {
-      Entries next;
-      load_entries(row + clusters, next);
+    int i_row = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) { g_top[i] = 0.f; id[i] = -1; }             // id: of the row before, where this warp has something to write
+#pragma unroll 1
+    for (int row = first_row; row < a.rows; row += clusters, ++i_row) {
       const float rs = GRAD && a.row_scale ? a.row_scale[row] : 1.f;
-      finish(last, p ^ 1);
-      block_barrier<THREADS>();                             // the row's pairs are there
+      block_barrier<THREADS>();
       if (a.cluster > 1) {
         const int lane = threadIdx.x & 31;
         if (lane < a.cluster) {
           float rm;
           double others = 0.0, tops = 0.0;
-          own_sums(p, rm, others, tops);
-          const uint32_t to = mapa(smem_u32(&sh.part[p][rank]), lane);
+          own_sums(i_row, rm, others, tops);
+          const uint32_t to = mapa(smem_u32(&sh.part[i_row & 1][rank]), lane);
           st_cluster_u64(to, (unsigned long long)__float_as_uint(rm));
           st_cluster_u64(to + 8, __double_as_longlong(others));
           st_cluster_u64(to + 16, __double_as_longlong(tops));
-          st_cluster_u64(to + 24, __double_as_longlong(sh.side[p].qz));
+          st_cluster_u64(to + 24, __double_as_longlong(sh.side[i_row & 3].qz));
         }
         cluster_sync_all();
       }
+      int ahead[E];
+      load_entries(row + 2 * clusters, ahead, t);
       if (GRAD) {
-        const Slope g = slope(p, rs);
-        T *dst = (T *)a.grad + row * a.grad_ld;
+        if (i_row) write_listed(row - clusters, id, g_top);
+        const Slope g = slope(i_row, rs);
+        const float q = sh.side[i_row & 3].total;
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-          if (n.first[i]) dst[n.id[i]] = from_f<T>(g.scale == 0.f ? 0.f : g.scale * fmaf(sh.side[p].total, ex2(fmaf(n.z[i] - g.ref, ch, -g.d)), -n.q[i]));
+        for (int i = 0; i < E; ++i) {
+          id[i] = n.first[i] ? n.id[i] : -1;
+          g_top[i] = g.scale == 0.f ? 0.f : g.scale * fmaf(q, ex2(fmaf(n.z[i] - g.ref, ch, -g.d)), -n.q[i]);
+        }
       }
-      last = row;
-      if (row != first_row) unmark_row(row - clusters, p ^ 1);
-      prepare(row + clusters, p ^ 1, next);
-      n = next;
-      block_barrier<THREADS>();
-    }
-    finish(last, p ^ 1);
-  }
-  __device__ __forceinline__ void unmark_row(int row, int p) const {
-    const RowShare<T> sr = share(row);
-    const int lane = threadIdx.x & 31;
+      finish(row, i_row);
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const int j = lane + 32 * i, bit = j < a.top ? sr.template flag_bit<NT>(sh.id[p][j], rank, a.cluster, edge_byte()) : -1;
-      if (bit >= 0) flags_of(p)[bit >> 3] = 0;
+      for (int i = 0; i < E; ++i) if (n.bit[i] >= 0) flags_of(i_row & 1)[n.bit[i] >> 3] = 0;
+      __syncwarp();
+      n = next;
+      prepare(row + 2 * clusters, i_row + 2, ahead, t, next);
     }
-    __syncwarp();
+    block_barrier<THREADS>();
+    if (GRAD) write_listed(first_row + (i_row - 1) * clusters, id, g_top);
+  }
+  __device__ __forceinline__ void write_listed(int row, const int (&id)[E], const float (&g_top)[E]) const {
+    T *dst = (T *)a.grad + row * a.grad_ld;
+#pragma unroll
+    for (int i = 0; i < E; ++i) if (id[i] >= 0) dst[id[i]] = from_f<T>(g_top[i]);
   }
 
   // ---- the stream warps
@@ -548,7 +559,7 @@ struct DistillBlock {
         s = add_pair(s, make_float2(ex2(y.x), ex2(y.y)));
       }
   }
-  __device__ __forceinline__ void write_turn(const uint4 *ring, int left, uint32_t listed, T *out, bool vec, const Slope &g) const {
+  __device__ __forceinline__ void write_turn(const uint4 *ring, int left, T *out, bool vec, const Slope &g) const {
     const float2 r2 = make_float2(-g.ref, -g.ref), c2 = make_float2(ch, ch), d2 = make_float2(-g.d, -g.d), o2 = make_float2(g.coef, g.coef);
     uint4 q[B];
 #pragma unroll
@@ -568,13 +579,8 @@ struct DistillBlock {
       }
       q[k] = pack_vec<T, VEC>(l);
     }
-    if (vec && !listed) {
 #pragma unroll
-      for (int k = 0; k < B; ++k) if (k * NT < left) *reinterpret_cast<uint4 *>(out + k * NT * VEC) = q[k];
-    } else {
-#pragma unroll
-      for (int k = 0; k < B; ++k) if (k * NT < left) store_unlisted<T>(out + k * NT * VEC, vec, q[k], listed >> (k * 8) & 0xffu);
-    }
+    for (int k = 0; k < B; ++k) if (k * NT < left) store_vec<T>(out + k * NT * VEC, vec, q[k]);
   }
   static __device__ __forceinline__ uint32_t turn_marks(const uint8_t *f) {      // of the thread's B vectors
     return B == 4 ? *reinterpret_cast<const uint32_t *>(f) : *reinterpret_cast<const uint16_t *>(f);
@@ -588,17 +594,16 @@ struct DistillBlock {
     float le = sr.edge >= 0 ? to_f(sr.row[sr.edge]) : -INFINITY;
     cluster_started_wait(a.cluster);
     block_barrier<THREADS>();
-    int p = 0;
+    int i_row = 0;
 #pragma unroll 1
-    for (int row = first_row; row < a.rows; row += clusters, p ^= 1) {
-      const uint8_t *fl = flags_of(p);
+    for (int row = first_row; row < a.rows; row += clusters, ++i_row) {
+      const uint8_t *fl = flags_of(i_row & 1);
       const bool more = row + clusters < a.rows;
       if (more) next = share(row + clusters);
       // running maximum m (ref: the same, 0 without one) and sum of 2^((l - ref) ch); listed ids stay out where the rest is a bucket
       float m = -INFINITY, ref = 0.f;
       float2 s = make_float2(0.f, 0.f);
-      const bool listed_edge = sr.edge >= 0 && (fl[edge_byte() + (tid >> 3)] >> (tid & 7) & 1u);
-      if (sr.edge >= 0 && !(tail && listed_edge)) {
+      if (sr.edge >= 0 && !(tail && (fl[edge_byte() + (tid >> 3)] >> (tid & 7) & 1u))) {
         if (le > m) { m = ref = le; s.x = 1.f; }
         else if (le != le) s.x = le;
       }
@@ -625,34 +630,33 @@ struct DistillBlock {
       } while (!GRAD && sr.nv > block * PER * NT);
       const float wm = warp_max(m);
       s.x = warp_sum((s.x + s.y) * (m > -INFINITY ? ex2((m - wm) * ch) : 1.f));       // without a maximum 0, or NaN
-      if (lane == 0) sh.pair[p][warp] = make_float2(wm, s.x);
+      if (lane == 0) sh.pair[i_row & 1][warp] = make_float2(wm, s.x);
       block_barrier<THREADS>();
       if (a.cluster > 1) cluster_sync_all();
       const float le_now = le;
       if (more) le = next.edge >= 0 ? to_f(next.row[next.edge]) : -INFINITY;
       if (GRAD) {
-        const Slope g = slope(p, rs);
+        const Slope g = slope(i_row, rs);
         T *dst = (T *)a.grad + row * a.grad_ld, *out = dst + sr.id0 + tid * VEC;
         const bool vec = ((uintptr_t)out & 15) == 0;
         const int from_left = more ? next.nv - tid : 0;
         left = sr.nv - tid;
-        if (sr.edge >= 0 && !listed_edge) dst[sr.edge] = from_f<T>(g.scale == 0.f ? 0.f : g.coef * ex2(fmaf(le_now - g.ref, ch, -g.d)));
-        const uint8_t *marks = fl + tid * PER;
+        if (sr.edge >= 0) dst[sr.edge] = from_f<T>(g.scale == 0.f ? 0.f : g.coef * ex2(fmaf(le_now - g.ref, ch, -g.d)));
 #pragma unroll 1
         for (int t = 0; t < TURNS; ++t) {
           const int here = left - t * B * NT;
           if (here > 0) {
-            if (g.scale != 0.f) write_turn(ring + t * B * NT, here, turn_marks(marks + t * B), out + t * B * NT * VEC, vec, g);
+            if (g.scale != 0.f) write_turn(ring + t * B * NT, here, out + t * B * NT * VEC, vec, g);
             else                                            // zeros, whatever the logits hold
               for (int k = 0; k < B; ++k)
-                if (k * NT < here) store_unlisted<T>(out + (t * B + k) * NT * VEC, vec, make_uint4(0u, 0u, 0u, 0u), marks[t * B + k]);
+                if (k * NT < here) store_vec<T>(out + (t * B + k) * NT * VEC, vec, make_uint4(0u, 0u, 0u, 0u));
           }
           fetch(t, next.mine, from_left, ring);
         }
       }
       sr = next;
-      block_barrier<THREADS>();
     }
+    block_barrier<THREADS>();
     cp_async_wait<0>();
   }
 };
