@@ -21,7 +21,7 @@
 struct DistillArgs {
   const void *logits;
   long long ld;
-  int rows, vocab, cluster, cta_vecs, top;
+  int rows, vocab, cluster, cta_vecs, top, alike;      // alike: all rows lie alike on 16-byte boundaries
   const int *ids;                      // [rows][top]; outside [0, vocab): no entry
   const float *teacher;                // [rows][top]
   const float *teacher_lse;            // [rows] or null
@@ -279,7 +279,7 @@ template <int THREADS> __device__ __forceinline__ void block_barrier() { asm vol
 template <typename T, bool GRAD, int SW>
 struct DistillBlock {
   static constexpr int VEC = 16 / sizeof(T), NT = SW * 32, THREADS = NT + 32, PER = DISTILL_PER,
-                       B = sizeof(T) == 4 ? 4 : 2, TURNS = PER / B;       // vectors of a thread per turn, turns of a block
+                       B = 4, TURNS = PER / B;       // vectors of a thread per turn, turns of a block
   const DistillArgs &a;
   DistillShared<SW> &sh;
   uint8_t *flags;                      // [2][distill_flag_bytes(cta_vecs)]
@@ -288,37 +288,47 @@ struct DistillBlock {
   __device__ __forceinline__ uint8_t *flags_of(int p) const { return flags + p * distill_flag_bytes(a.cta_vecs, NT); }
   __device__ __forceinline__ RowShare<T> share(int row) const { return RowShare<T>(a.logits, a.ld, row, a.vocab, rank, a.cluster, a.cta_vecs); }
   __device__ __forceinline__ int edge_byte() const { return distill_flag_bytes(a.cta_vecs, NT) - 16; }
-  __device__ __forceinline__ float scaled(float m, float s, float to) const { return m > -INFINITY ? s * ex2((m - to) * ch) : s; }
-  // The row's largest logit and its sums, from this CTA's warps or the cluster's parts.
-  template <typename R> __device__ __forceinline__ void sums(int i, float &rm, R &others, R &tops, double *qz) const {
-    rm = -INFINITY; others = 0; tops = 0;
-    if (a.cluster > 1) {
-      for (int c = 0; c < a.cluster; ++c) rm = fmaxf(rm, sh.part[i & 1][c].m);
-      for (int c = 0; c < a.cluster; ++c) {
-        const DistillPart &x = sh.part[i & 1][c];
-        const float f = x.m > -INFINITY ? ex2((x.m - rm) * ch) : 1.f;
-        others += x.others * f; tops += x.tops * f;
-        if (qz) *qz += x.qz;
-      }
-    } else {
-      own_sums(i, rm, others, tops);
+  // The largest logit and the sums of row i of the block, by a whole warp: of this CTA's warps (own), or of the cluster.
+  template <typename R> __device__ __forceinline__ void sums(int i, bool own, float &rm, R &others, R &tops, double *qz) const {
+    const int lane = threadIdx.x & 31;
+    const bool tail = a.teacher_lse != nullptr;
+    float m = -INFINITY;
+    R o = 0, t = 0;
+    if (own || a.cluster == 1) {
+      float v = 0.f;
+      if (lane < SW) { m = sh.pair[i & 1][lane].x; v = sh.pair[i & 1][lane].y; }
+      else if (lane == SW) { m = sh.side[i & 3].top_m; v = tail ? sh.side[i & 3].tops : 0.f; }   // without the bucket they are among the others
+      rm = warp_max(m);
+      v = m > -INFINITY ? v * ex2((m - rm) * ch) : v;
+      if (lane < SW) o = v; else t = v;
       if (qz) *qz = sh.side[i & 3].qz;
+    } else {
+      double z = 0.0;
+      if (lane < a.cluster) { const DistillPart &x = sh.part[i & 1][lane]; m = x.m; o = (R)x.others; t = (R)x.tops; z = x.qz; }
+      rm = warp_max(m);
+      const float f = m > -INFINITY ? ex2((m - rm) * ch) : 1.f;
+      o *= f; t *= f;
+      if (qz) *qz = warp_sum_d(z);
     }
-  }
-  template <typename R> __device__ __forceinline__ void own_sums(int i, float &rm, R &others, R &tops) const {
-    rm = sh.side[i & 3].top_m;
 #pragma unroll
-    for (int w = 0; w < SW; ++w) rm = fmaxf(rm, sh.pair[i & 1][w].x);
+    for (int x = 16; x > 0; x >>= 1) o += __shfl_xor_sync(0xffffffffu, o, x);
+    others = o;
+    tops = 0;
+    if (tail) {
+      if (own || a.cluster == 1) tops = __shfl_sync(0xffffffffu, t, SW);
+      else {
 #pragma unroll
-    for (int w = 0; w < SW; ++w) others += scaled(sh.pair[i & 1][w].x, sh.pair[i & 1][w].y, rm);
-    if (a.teacher_lse) tops += scaled(sh.side[i & 3].top_m, sh.side[i & 3].tops, rm);   // without the bucket they are among the others
+        for (int x = 16; x > 0; x >>= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
+        tops = t;
+      }
+    }
   }
   // What the gradient of a row needs.
   struct Slope { float ref, d, scale, coef; };
   __device__ __forceinline__ Slope slope(int i, float rs) const {
     Slope g;
     float rm, others, tops;
-    sums(i, rm, others, tops, nullptr);
+    sums(i, false, rm, others, tops, nullptr);
     const float total = others + tops, q = sh.side[i & 3].total, rest = sh.side[i & 3].rest;
     g.ref = rm > -INFINITY ? rm : 0.f;
     g.d = __log2f(total);
@@ -354,6 +364,8 @@ struct DistillBlock {
     double x[E], e[E], ref = -INFINITY, s = 0.0, l = 0.0, qz = 0.0;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
+      x[i] = -INFINITY;
+      if (i * 32 >= a.top) continue;
       n.bit[i] = sr.template flag_bit<NT>(n.id[i], rank, a.cluster, edge_byte());
       if (n.bit[i] >= 0) n.z[i] = to_f(sr.row[n.id[i]]);
       n.first[i] = n.bit[i] >= 0;
@@ -433,7 +445,7 @@ struct DistillBlock {
     if (rank) return;
     float rm;
     double others, tops, qz = 0.0;
-    sums(i, rm, others, tops, &qz);
+    sums(i, false, rm, others, tops, &qz);
     const DistillSide &d = sh.side[i & 3];
     const double total = others + tops, lse = (double)rm * a.inv_tau + log(total);
     const bool none = total == 0.0;                         // no finite logit
@@ -472,10 +484,10 @@ struct DistillBlock {
       block_barrier<THREADS>();
       if (a.cluster > 1) {
         const int lane = threadIdx.x & 31;
+        float rm;
+        double others, tops;
+        sums(i_row, true, rm, others, tops, nullptr);
         if (lane < a.cluster) {
-          float rm;
-          double others = 0.0, tops = 0.0;
-          own_sums(i_row, rm, others, tops);
           const uint32_t to = mapa(smem_u32(&sh.part[i_row & 1][rank]), lane);
           st_cluster_u64(to, (unsigned long long)__float_as_uint(rm));
           st_cluster_u64(to + 8, __double_as_longlong(others));
@@ -498,7 +510,7 @@ struct DistillBlock {
       }
       finish(row, i_row);
 #pragma unroll
-      for (int i = 0; i < E; ++i) if (n.bit[i] >= 0) flags_of(i_row & 1)[n.bit[i] >> 3] = 0;
+      for (int i = 0; i < E; ++i) if (i * 32 < a.top && n.bit[i] >= 0) flags_of(i_row & 1)[n.bit[i] >> 3] = 0;
       __syncwarp();
       n = next;
       prepare(row + 2 * clusters, i_row + 2, ahead, t, next);
@@ -522,51 +534,53 @@ struct DistillBlock {
       if ((turn * B + k) * NT < left) cp_async16(ring + (turn * B + k) * NT, from + (turn * B + k) * NT * VEC);
     cp_async_commit();
   }
-  // ring, left and marks are the turn's own.
+  // A turn's vectors; without one -inf.  ring and left are the turn's own.
+  __device__ __forceinline__ void take(const uint4 *ring, int left, uint4 (&q)[B]) const {
+    if ((B - 1) * NT < left) {
+#pragma unroll
+      for (int k = 0; k < B; ++k) q[k] = ring[k * NT];
+    } else {
+      const uint32_t u = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+#pragma unroll
+      for (int k = 0; k < B; ++k) q[k] = k * NT < left ? ring[k * NT] : make_uint4(u, u, u, u);
+    }
+  }
   __device__ __forceinline__ void add_turn(const uint4 *ring, int left, uint32_t listed, float &m, float &ref, float2 &s) const {
     uint4 q[B];
+    take(ring, left, q);
+    if (listed) {
 #pragma unroll
-    for (int k = 0; k < B; ++k) {
-      const uint32_t u = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;            // -inf
-      q[k] = make_uint4(u, u, u, u);
-      if (k * NT < left) q[k] = ring[k * NT];
+      for (int k = 0; k < B; ++k) {
+        T t[VEC];
+        memcpy(t, &q[k], 16);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) if (listed >> (k * 8 + e) & 1u) t[e] = from_f<T>(-INFINITY);
+        memcpy(&q[k], t, 16);
+      }
     }
-    float l[B][VEC], v = max_vec<T, VEC>(q[0]);
-#pragma unroll
-    for (int k = 0; k < B; ++k) unpack_vec<T, VEC>(q[k], l[k]);
+    float v = max_vec<T, VEC>(q[0]);
 #pragma unroll
     for (int k = 1; k < B; ++k) v = fmaxf(v, max_vec<T, VEC>(q[k]));
-    if (listed) {
-      v = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < B; ++k)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          if (listed >> (k * 8 + e) & 1u) l[k][e] = -INFINITY;
-          v = fmaxf(v, l[k][e]);
-        }
-    }
     if (v > m) {
       if (m > -INFINITY) { const float f = ex2((m - v) * ch); s.x *= f; s.y *= f; }
       m = ref = v;
     }
     const float2 r2 = make_float2(-ref, -ref), c2 = make_float2(ch, ch);
 #pragma unroll
-    for (int k = 0; k < B; ++k)
+    for (int k = 0; k < B; ++k) {
+      float l[VEC];
+      unpack_vec<T, VEC>(q[k], l);
 #pragma unroll
       for (int e = 0; e < VEC; e += 2) {
-        const float2 y = mul_pair(add_pair(make_float2(l[k][e], l[k][e + 1]), r2), c2);
+        const float2 y = mul_pair(add_pair(make_float2(l[e], l[e + 1]), r2), c2);
         s = add_pair(s, make_float2(ex2(y.x), ex2(y.y)));
       }
+    }
   }
   __device__ __forceinline__ void write_turn(const uint4 *ring, int left, T *out, bool vec, const Slope &g) const {
     const float2 r2 = make_float2(-g.ref, -g.ref), c2 = make_float2(ch, ch), d2 = make_float2(-g.d, -g.d), o2 = make_float2(g.coef, g.coef);
     uint4 q[B];
-#pragma unroll
-    for (int k = 0; k < B; ++k) {
-      q[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (k * NT < left) q[k] = ring[k * NT];
-    }
+    take(ring, left, q);
 #pragma unroll
     for (int k = 0; k < B; ++k) {
       float l[VEC];
@@ -577,13 +591,8 @@ struct DistillBlock {
         const float2 o = mul_pair(make_float2(ex2(y.x), ex2(y.y)), o2);
         l[e] = o.x; l[e + 1] = o.y;
       }
-      q[k] = pack_vec<T, VEC>(l);
+      if (k * NT < left) store_vec<T>(out + k * NT * VEC, vec, pack_vec<T, VEC>(l));
     }
-#pragma unroll
-    for (int k = 0; k < B; ++k) if (k * NT < left) store_vec<T>(out + k * NT * VEC, vec, q[k]);
-  }
-  static __device__ __forceinline__ uint32_t turn_marks(const uint8_t *f) {      // of the thread's B vectors
-    return B == 4 ? *reinterpret_cast<const uint32_t *>(f) : *reinterpret_cast<const uint16_t *>(f);
   }
   __device__ __forceinline__ void stream_warp(uint4 *ring) const {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -599,7 +608,10 @@ struct DistillBlock {
     for (int row = first_row; row < a.rows; row += clusters, ++i_row) {
       const uint8_t *fl = flags_of(i_row & 1);
       const bool more = row + clusters < a.rows;
-      if (more) next = share(row + clusters);
+      if (more) {
+        if (a.alike) { next.row += clusters * a.ld; next.mine += clusters * a.ld; }
+        else next = share(row + clusters);
+      }
       // running maximum m (ref: the same, 0 without one) and sum of 2^((l - ref) ch); listed ids stay out where the rest is a bucket
       float m = -INFINITY, ref = 0.f;
       float2 s = make_float2(0.f, 0.f);
@@ -622,7 +634,7 @@ struct DistillBlock {
           else if (t == 0) cp_async_wait<TURNS / 2>();
           else if (t == TURNS / 2) cp_async_wait<0>();
           const int here = left - t * B * NT;
-          if (here > 0) add_turn(ring + t * B * NT, here, tail ? turn_marks(marks + t * B) : 0u, m, ref, s);
+          if (here > 0) add_turn(ring + t * B * NT, here, tail ? *reinterpret_cast<const uint32_t *>(marks + t * B) : 0u, m, ref, s);
           if (!GRAD) fetch(t, from, from_left, ring);
         }
         left -= PER * NT;

@@ -1769,6 +1769,7 @@ static dream_status distill_args(const char *who, DistillArgs *a, const void *lo
   a->logits = logits; a->rows = rows; a->vocab = vocab; a->ld = ld; a->ids = ids; a->teacher = teacher; a->top = top; a->teacher_lse = teacher_lse;
   a->inv_tau = 1.0 / (double)temperature; a->lse = lse; a->log_rest = log_rest; a->row_scale = row_scale;
   a->grad = grad; a->grad_ld = grad_ld;
+  a->alike = ld * (dtype == DREAM_BF16 ? 2 : 4) % 16 == 0;
   return DREAM_OK;
 }
 
