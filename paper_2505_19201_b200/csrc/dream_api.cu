@@ -1680,21 +1680,16 @@ static bool rows_collide(const void *p, long long ld, const void *q, long long q
   const long long off = ((b - a) % ld + ld) % ld;
   return off < vocab || off + vocab > ld;
 }
-static bool rows_of_16(const void *p, int dtype, int rows, long long ld) {
-  return ((uintptr_t)p & 15) == 0 && (rows == 1 || ld * (dtype == DREAM_BF16 ? 2 : 4) % 16 == 0);
-}
-
 // Fills in what follows from the sizes and launches.
 static const char *sample_launch(SampleArgs a, int dtype, int rows, bool truncate, cudaStream_t stream) {
+  // 64 KB of the row per CTA, two CTAs per SM, where a cluster of eight holds it so; more CTAs to a row where there are few rows
+  const int esz = dtype == DREAM_BF16 ? 2 : 4;
   a.cluster = 1;
-  while (a.vocab > a.cluster * SAMPLE_CTA_MAX) a.cluster *= 2;
-  const int share = (a.vocab + a.cluster - 1) / a.cluster, line = dtype == DREAM_BF16 ? 256 : 128;
-  const int warps = imin(32, imax(4, (share + line - 1) / line));
+  while (a.cluster < SAMPLE_MAX_CLUSTER && (a.vocab > a.cluster * (65536 / esz) || (rows * a.cluster < 148 && a.vocab > a.cluster * 4096))) a.cluster *= 2;
+  const int share = (a.vocab + 16 / esz - 1 + a.cluster - 1) / a.cluster, line = dtype == DREAM_BF16 ? 256 : 128, warps = SAMPLE_THREADS / 32;
   a.warp_elems = ((share + warps - 1) / warps + line - 1) / line * line;
   a.frac_bits = imin(50, 62 - ilog2(a.vocab));
-  a.vec = rows_of_16(a.logits, dtype, rows, a.ld);
-  a.out_vec = truncate && rows_of_16(a.out, dtype, rows, a.out_ld);
-  const size_t smem = sizeof(SampleShared) + (size_t)warps * a.warp_elems * (dtype == DREAM_BF16 ? 2 : 4);
+  const size_t smem = (sizeof(SampleShared) + 15) / 16 * 16 + (size_t)warps * a.warp_elems * esz;
   void (*kernel)(SampleArgs) = dtype == DREAM_BF16 ? (truncate ? k_sample<bf16, true> : k_sample<bf16, false>)
                                                    : (truncate ? k_sample<float, true> : k_sample<float, false>);
   return launch_rows(kernel, rows, a.cluster, warps * 32, smem, stream, a);

@@ -10,9 +10,12 @@
 // therefore taken in double (to 3e-13) and summed as 64-bit integers of 2^-s (s such that a whole row of ones fits), whose sums do
 // not depend on their order: histograms by atomics, shares of a cluster and scans all agree bit for bit.
 //
-// The cut is a pair (key, id): an order-preserving 32-bit key of the logit and the last id kept among its ties.  It is found by a radix
-// selection over the keys, eleven bits a level, by count (top_k) or by mass (top_p), so it needs no sort and no assumption on the
-// values: rows masked with the type's lowest value, infinities and rows of ties take the same three levels.
+// The cut is a pair (key, id): an order-preserving 32-bit key of the logit and the last id kept among its ties.  Three ways to it:
+//   few tokens (top_k up to 256, greedy): the k-th largest of the threads' own maxima is a bound that little more than k logits pass; those
+//     are listed, and one block settles order, masses, cut and draw on the list.
+//   many: one pass sorts the row into bins of 1 / 128 nat with counts and masses; the bin where top_k or top_p ends is listed and settled.
+//   neither list fits (masked rows, rows of ties, logits of an odd scale): a radix selection over the keys, eleven bits a level, by count or by
+//     mass, which assumes nothing about the values.
 #pragma once
 #include "common.cuh"
 #include "rows.cuh"
@@ -22,7 +25,10 @@
 #define SAMPLE_MAX_VOCAB (SAMPLE_MAX_CLUSTER * SAMPLE_CTA_MAX)
 #define SAMPLE_BINS 2048
 #define SAMPLE_CHUNKS 32               // of SAMPLE_BINS / 32 bins, a lane each
-#define SAMPLE_EXCHANGES 8
+#define SAMPLE_EXCHANGES 10
+#define SAMPLE_LIST 512                // listed tokens one block settles
+#define SAMPLE_SMALL_K 256
+#define SAMPLE_THREADS 512
 
 typedef unsigned long long u64;
 
@@ -31,7 +37,6 @@ struct SampleArgs {
   long long ld;                        // elements from one row to the next
   int vocab, cluster, warp_elems;      // logits per warp, a multiple of 32 vectors of 16 bytes
   int frac_bits;                       // s: weights are integers of 2^-s
-  int vec, out_vec;                    // rows (of the output) start on 16-byte boundaries
   const float *temperature;            // [rows] each, or null: the values below for every row
   const int *top_k;
   const float *top_p, *min_p, *uniforms;
@@ -48,16 +53,22 @@ struct SampleArgs {
 struct SampleShared {
   u64 xch[SAMPLE_EXCHANGES][SAMPLE_MAX_CLUSTER];   // one 64-bit word from every CTA of the cluster
   u64 warp_tot[32];
-  u64 coarse_mass[2][SAMPLE_CHUNKS];
-  uint32_t coarse_cnt[2][SAMPLE_CHUNKS];
+  u64 coarse_mass[SAMPLE_CHUNKS];
+  uint32_t coarse_cnt[SAMPLE_CHUNKS];
   uint32_t warp_cnt[32];
-  float warp_f[32];
+  float2 warp_f[32];
   // what a selection level found
   int bin;
   uint32_t bin_cnt;
   u64 before_cnt, before_mass, total;
-  // histograms of two levels: while one is read by the cluster the next is filled
-  uint32_t cnt[2][SAMPLE_BINS], lo[2][SAMPLE_BINS], hi[2][SAMPLE_BINS];
+  // listed tokens (of the whole cluster, in its first CTA) and what they settle
+  uint32_t list_n[3];                  // a counter for each list a row may need
+  float list_l[SAMPLE_LIST], cut_l;
+  int list_id[SAMPLE_LIST], min_id;
+  u64 list_w[SAMPLE_LIST];
+  double table[256];                   // of the weights (Weigher)
+  int cut_id;
+  uint32_t cnt[SAMPLE_BINS], lo[SAMPLE_BINS], hi[SAMPLE_BINS];
 };
 
 __device__ __forceinline__ u64 warp_sum_u64(u64 v) {
@@ -75,28 +86,24 @@ __device__ __forceinline__ u64 warp_scan_u64(u64 v) {            // inclusive
   return v;
 }
 
-// exp((l - m) / T) as an integer of 2^-s.  2^y by the textbook reduction y = n + r, |r| <= 1/2, and the Taylor series of
-// e^(r ln 2) to its tenth power (remainder 2.2e-13 at the ends); both roundings to integers are additions of a number so large that its
-// last bit is the unit wanted.
+// exp((l - m) / T) as an integer of 2^-s.  2^y by table, as in Tang's table-driven exponential: y = n + j / 256 + r, |r| <= 1 / 512, and 2^r by the
+// Taylor series of e^(r ln 2) to its third power (remainder 1.4e-13).  Both roundings to integers are additions of a number so large
+// that its last bit is the unit wanted.  Nine operations in double, where a series without a table takes fifteen.
+#define SAMPLE_TABLE 256
 struct Weigher {
   double m, c2, unit;                  // row maximum, log2(e) / T, 2^(52 - s)
   float cut;                           // below it a weight is less than half a unit
+  const double *table;                 // 2^(j / 256), in shared memory
   __device__ __forceinline__ u64 operator()(float l) const {
     const double d = (double)fminf(fmaxf(l, cut), 3.402823466e38f) - m;
-    const double big = 6755399441055744.0;         // 1.5 * 2^52
+    const double big = 6755399441055744.0 / SAMPLE_TABLE;       // 1.5 * 2^52 / 256: its last bit is 1 / 256
     const double t = fma(d, c2, big), r = fma(d, c2, -(t - big));
-    double p = 7.054911620801121e-09;              // ln(2)^k / k!, k = 10 .. 0
-    p = fma(p, r, 1.0178086009239696e-07);
-    p = fma(p, r, 1.3215486790144305e-06);
-    p = fma(p, r, 1.5252733804059838e-05);
-    p = fma(p, r, 1.5403530393381606e-04);
-    p = fma(p, r, 1.3333558146428441e-03);
-    p = fma(p, r, 9.618129107628477e-03);
-    p = fma(p, r, 5.5504108664821576e-02);
-    p = fma(p, r, 2.402265069591007e-01);
-    p = fma(p, r, 6.931471805599453e-01);
-    p = fma(p, r, 1.0);
-    p = __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
+    const int n = __double2loint(t);
+    const double e = table[n & (SAMPLE_TABLE - 1)];
+    double p = fma(r, 0.05550410866482158, 0.2402265069591007);  // ln(2)^k / k!, k = 3, 2, 1
+    p = fma(p, r, 0.6931471805599453);
+    p = fma(e, p * r, e);
+    p = __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
     const u64 w = (u64)__double_as_longlong(p + unit) - (u64)__double_as_longlong(unit);
     return l >= cut ? w : 0ull;
   }
@@ -104,13 +111,12 @@ struct Weigher {
   __device__ __forceinline__ double least(double temp) const { return cut == INFINITY ? INFINITY : m - 744.0 * temp; }
 };
 
-// A cut of the order: tokens in front of it stay.  Its key is never below that of -inf, which no cut keeps (nor NaN).
+// A cut of the order: larger logits stay, and equal ones up to an id; -inf and NaN never do.
 struct Cut {
-  uint32_t key;
+  float l;
   int id;
-  __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= id); }
+  __device__ __forceinline__ bool keeps(float x, int i) const { return x > l || (x == l && i <= id); }
 };
-#define KEY_NEG_INF 0x007fffffu          // topk_key(-inf); NaN is 0
 
 template <typename T>
 struct SampleRow {
@@ -118,8 +124,7 @@ struct SampleRow {
   const SampleArgs &a;
   SampleShared &sh;
   uint4 *vals;                           // this CTA's logits, as they came
-  int rank, nw, warp, lane, steps, base; // base: id of the warp's first logit
-  mutable int turn;                      // which of the two histograms is next
+  int rank, nw, warp, lane, steps, base; // base: id of the warp's first logit; vectors lie on 16-byte boundaries, so the row's first may begin below 0
 
   __device__ __forceinline__ void unpack(const uint4 &q, float (&l)[VEC]) const {
     if constexpr (sizeof(T) == 4) {
@@ -141,14 +146,25 @@ struct SampleRow {
       for (int e = 0; e < VEC; ++e) f(l[e], base + (j * 32 + lane) * VEC + e);
     }
   }
+  // f(logits, id of the first) for the thread's vectors
+  template <typename F> __device__ __forceinline__ void each_vec(F f) const {
+    const uint4 *p = vals + (size_t)warp * steps * 32 + lane;
+#pragma unroll 1
+    for (int j = 0; j < steps; ++j) {
+      float l[VEC];
+      unpack(p[j * 32], l);
+      f(l, base + (j * 32 + lane) * VEC);
+    }
+  }
   // One word from every CTA to every CTA; ends in a barrier of the cluster.
   __device__ __forceinline__ void exchange(int slot, u64 v) const {
     if (threadIdx.x < a.cluster) st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[slot][rank]), threadIdx.x), v);
     sync_all_of(a.cluster);
   }
 
-  // The row into shared memory; returns its maximum (NaN does not count).  Past the row's end: -inf.
-  __device__ __forceinline__ float load(int row) const {
+  // The row into shared memory.  own: the thread's largest logit (NaN does not count; past the row's end: -inf); most, least: the
+  // largest and the smallest of those that are not -inf.
+  __device__ __forceinline__ void load(int row, float &own, float &most, float &least) const {
     const T *src = (const T *)a.logits + row * a.ld;
     const T neg = from_f<T>(-INFINITY);
     uint4 *p = vals + (size_t)warp * steps * 32 + lane;
@@ -159,11 +175,11 @@ struct SampleRow {
 #pragma unroll
       for (int k = 0; k < U; ++k) {
         const int i = base + ((j0 + k) * 32 + lane) * VEC;
-        if (j0 + k < steps && a.vec && i + VEC <= a.vocab) q[k] = __ldg(reinterpret_cast<const uint4 *>(src + i));
+        if (j0 + k < steps && i >= 0 && i + VEC <= a.vocab) q[k] = *reinterpret_cast<const uint4 *>(src + i);
         else {
           T t[VEC];
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) t[e] = j0 + k < steps && i + e < a.vocab ? src[i + e] : neg;
+          for (int e = 0; e < VEC; ++e) t[e] = j0 + k < steps && i + e >= 0 && i + e < a.vocab ? src[i + e] : neg;
           memcpy(&q[k], t, 16);
         }
       }
@@ -177,45 +193,58 @@ struct SampleRow {
           p[(j0 + k) * 32] = q[k];
         }
     }
-    m = warp_max(m);
-    if (lane == 0) sh.warp_f[warp] = m;
+    own = m;
+    most = warp_max(m);
+    least = -warp_max(m > -INFINITY ? -m : -INFINITY);
+    if (lane == 0) sh.warp_f[warp] = make_float2(most, least);
+    if (threadIdx.x == 0) { sh.list_n[0] = sh.list_n[1] = sh.list_n[2] = 0; sh.min_id = 0x7fffffff; }
     __syncthreads();
-    m = warp_max(lane < nw ? sh.warp_f[lane] : -INFINITY);
     cluster_started_wait(a.cluster);
-    exchange(0, (u64)__float_as_uint(m));
-    for (int q = 0; q < a.cluster; ++q) m = fmaxf(m, __uint_as_float((uint32_t)sh.xch[0][q]));
-    return m;
+    const float2 w = lane < nw ? sh.warp_f[lane] : make_float2(-INFINITY, INFINITY);
+    most = warp_max(w.x);
+    least = -warp_max(-w.y);
+    exchange(0, (u64)__float_as_uint(most) | (u64)__float_as_uint(least) << 32);
+    for (int q = 0; q < a.cluster; ++q) {
+      most = fmaxf(most, __uint_as_float((uint32_t)sh.xch[0][q]));
+      least = fminf(least, __uint_as_float((uint32_t)(sh.xch[0][q] >> 32)));
+    }
   }
 
-  // One level of the selection: among the tokens that f gives a bin (>= 0) and a mass, the bin, from the top, in which the running
-  // count (MASS false) or mass reaches `goal(total)`.  Leaves it in sh.bin .. sh.total; false, and nothing found, where the total is not
-  // above the goal by count.
-  template <bool MASS, typename F, typename G> __device__ __forceinline__ bool level(int lev, F f, G goal) const {
-    const int b = turn++ & 1;
+  // One level of the selection.  walk(put) hands put(bin, mass) the tokens, or one value a thread; of the bins, from the top, that one is
+  // found in which the running count (MASS false) or mass reaches goal(total), and left in sh.bin .. sh.total.  enough: false, and nothing
+  // found, where the goal is not below the total.  Bin 0 may hold most of a row, so it is added up in registers first.
+  template <bool MASS, typename F, typename G> __device__ __forceinline__ bool level(bool first, bool enough, F walk, G goal) const {
+    if (!first) sync_all_of(a.cluster);                     // nobody still reads the bins of the level before
     for (int i = threadIdx.x; i < SAMPLE_BINS; i += blockDim.x) {
-      sh.cnt[b][i] = 0;
-      if (MASS) { sh.lo[b][i] = 0; sh.hi[b][i] = 0; }
+      sh.cnt[i] = 0;
+      if (MASS) { sh.lo[i] = 0; sh.hi[i] = 0; }
     }
     __syncthreads();
-    each([&](float l, int id) {
-      u64 w = 0;
-      const int bin = f(l, id, w);
-      if (bin < 0) return;
-      atomicAdd(&sh.cnt[b][bin], 1u);
+    uint32_t n0 = 0;
+    u64 w0 = 0;
+    auto add = [&](int bin, uint32_t n, u64 w) {
+      atomicAdd(&sh.cnt[bin], n);
       if (MASS && w) {
-        const uint32_t add = (uint32_t)w, old = atomicAdd(&sh.lo[b][bin], add), carry = old + add < old ? 1u : 0u;
-        const uint32_t up = (uint32_t)(w >> 32) + carry;
-        if (up) atomicAdd(&sh.hi[b][bin], up);
+        const uint32_t low = (uint32_t)w, old = atomicAdd(&sh.lo[bin], low), up = (uint32_t)(w >> 32) + (old + low < old ? 1u : 0u);
+        if (up) atomicAdd(&sh.hi[bin], up);
       }
+    };
+    walk([&](int bin, u64 w) {
+      if (bin > 0) add(bin, 1u, w);
+      n0 += bin == 0 ? 1u : 0u;
+      if (MASS) w0 += bin == 0 ? w : 0ull;
     });
+    n0 = __reduce_add_sync(0xffffffffu, n0);
+    if (MASS) w0 = warp_sum_u64(w0);
+    if (lane == 0 && n0) add(0, n0, w0);
     __syncthreads();
     for (int ch = warp; ch < SAMPLE_CHUNKS; ch += nw) {
       const int i = ch * (SAMPLE_BINS / SAMPLE_CHUNKS) + lane;
-      uint32_t c = sh.cnt[b][i] + sh.cnt[b][i + 32];
+      uint32_t c = sh.cnt[i] + sh.cnt[i + 32];
       c = __reduce_add_sync(0xffffffffu, c);
       u64 w = 0;
-      if (MASS) w = warp_sum_u64(bin_mass(b, i) + bin_mass(b, i + 32));
-      if (lane == 0) { sh.coarse_cnt[b][ch] = c; if (MASS) sh.coarse_mass[b][ch] = w; }
+      if (MASS) w = warp_sum_u64(bin_mass(i) + bin_mass(i + 32));
+      if (lane == 0) { sh.coarse_cnt[ch] = c; if (MASS) sh.coarse_mass[ch] = w; }
     }
     sync_all_of(a.cluster);
     if (warp == 0) {
@@ -223,13 +252,13 @@ struct SampleRow {
       const int ch = SAMPLE_CHUNKS - 1 - lane;
       u64 c = 0, w = 0;
       for (int q = 0; q < a.cluster; ++q) {
-        c += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.coarse_cnt[b][ch]), q));
-        if (MASS) w += ld_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.coarse_mass[b][ch]), q));
+        c += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.coarse_cnt[ch]), q));
+        if (MASS) w += ld_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.coarse_mass[ch]), q));
       }
       const u64 ic = warp_scan_u64(c), iw = MASS ? warp_scan_u64(w) : 0;
       const u64 total = __shfl_sync(0xffffffffu, MASS ? iw : ic, 31), want = goal(total);
       const unsigned hit = __ballot_sync(0xffffffffu, (MASS ? iw : ic) >= want);
-      if (!hit || (!MASS && want >= total && lev == 0)) { if (lane == 0) sh.bin = -1; }
+      if (!hit || (enough && want >= total)) { if (lane == 0) sh.bin = -1; }
       else {
         const int at = __ffs(hit) - 1;                                   // the chunk
         const u64 bc = __shfl_sync(0xffffffffu, ic - c, at), bw = __shfl_sync(0xffffffffu, iw - w, at);
@@ -239,8 +268,8 @@ struct SampleRow {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {                                  // lane's bins, descending: top - 2 lane, then the next
             const int i = top - 2 * lane - k;
-            c2[k] += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[b][i]), q));
-            if (MASS) w2[k] += (u64)ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[b][i]), q)) + ((u64)ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[b][i]), q)) << 32);
+            c2[k] += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
+            if (MASS) w2[k] += (u64)ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)) + ((u64)ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[i]), q)) << 32);
           }
         const u64 sc = bc + warp_scan_u64(c2[0] + c2[1]), sw = bw + (MASS ? warp_scan_u64(w2[0] + w2[1]) : 0);
         const unsigned h2 = __ballot_sync(0xffffffffu, (MASS ? sw : sc) >= want);
@@ -258,13 +287,14 @@ struct SampleRow {
     __syncthreads();
     return sh.bin >= 0;
   }
-  __device__ __forceinline__ u64 bin_mass(int b, int i) const { return (u64)sh.lo[b][i] + ((u64)sh.hi[b][i] << 32); }
+  __device__ __forceinline__ u64 bin_mass(int i) const { return (u64)sh.lo[i] + ((u64)sh.hi[i] << 32); }
 
   // The first token in id order at which the running sum of val exceeds goal(total): found(logit, id, total) runs in the one thread that
-  // holds it.  Two exchange slots (the second carries `side`, summed over the threads); returns the total.
-  template <typename V, typename G, typename H> __device__ __forceinline__ u64 locate(int slot, V val, G goal, uint32_t side, H found) const {
+  // holds it.  Two exchange slots (the second carries the sum of count over the tokens); returns the total.
+  template <typename V, typename G, typename C, typename H> __device__ __forceinline__ u64 locate(int slot, V val, G goal, C count, H found) const {
     u64 s = 0;
-    each([&](float l, int id) { s += val(l, id); });
+    uint32_t side = 0;
+    each([&](float l, int id) { s += val(l, id); side += count(l, id); });
     s = warp_sum_u64(s);
     side = __reduce_add_sync(0xffffffffu, side);
     __syncthreads();
@@ -309,34 +339,37 @@ struct SampleRow {
     return total;
   }
 
-  // The last of the first r ties of `key` in id order, to every CTA.
-  __device__ __forceinline__ int nth_tie(uint32_t key, u64 r) const {
-    locate(2, [&](float l, int) { return (u64)(topk_key(l) == key); }, [&](u64) { return r - 1; }, 0u,
+  // The last of the first r tokens of a logit in id order, to every CTA.
+  __device__ __forceinline__ int nth_tie(float tie, u64 r) const {
+    locate(2, [&](float l, int) { return (u64)(l == tie); }, [&](u64) { return r - 1; }, [](float, int) { return 0u; },
            [&](float, int id, u64) { for (int q = 0; q < a.cluster; ++q) st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[4][0]), q), (u64)id); });
     sync_all_of(a.cluster);
     return (int)sh.xch[4][0];
   }
 
-  // Three levels down to one key.  By count: the `want` first; by mass: until top_p of the mass is reached.
-  template <bool MASS> __device__ __forceinline__ Cut select(Cut cut, u64 want, double top_p, const Weigher &weigh) const {
+  static __device__ __forceinline__ u64 mass_goal(double top_p, u64 total) {     // masses below it stay; the first token always does
+    const u64 g = (u64)ceil(top_p * (double)total);
+    return g < 1 ? (u64)1 : g > total ? total : g;
+  }
+  // Radix selection, three levels down to one key.  By count: the `want` first; by mass: until top_p of the mass is reached.
+  template <bool MASS> __device__ __forceinline__ Cut radix(Cut cut, u64 want, double top_p, const Weigher &weigh) const {
     uint32_t prefix = 0;
     u64 goal = want, ties = 0;
+#pragma unroll 1
     for (int lev = 0; lev < 3; ++lev) {
       const int shift = lev == 0 ? 21 : lev == 1 ? 10 : 0, width = lev == 2 ? 1023 : 2047;
       const uint32_t above = lev == 0 ? 0u : lev == 1 ? 0xffe00000u : 0xfffffc00u;
-      const bool any = level<MASS>(lev,
-          [&](float l, int id, u64 &w) {
-            const uint32_t k = topk_key(l);
-            if ((k & above) != prefix || !cut.keeps(k, id)) return -1;
-            if (MASS) w = weigh(l);
-            return (int)((k >> shift) & width);
+      if (!level<MASS>(false, !MASS && lev == 0,
+          [&](auto put) {
+            each([&](float l, int id) {
+              const uint32_t k = topk_key(l);
+              if ((k & above) != prefix || !cut.keeps(l, id)) return;
+              put((int)((k >> shift) & width), MASS ? weigh(l) : 0ull);
+            });
           },
-          [&](u64 total) {
-            if (MASS && lev == 0) { const u64 g = (u64)ceil(top_p * (double)total); return g < 1 ? (u64)1 : g > total ? total : g; }
-            return goal;
-          });
-      if (!any) return cut;                                 // fewer tokens than top_k
-      if (MASS && lev == 0) { const u64 g = (u64)ceil(top_p * (double)sh.total); goal = g < 1 ? (u64)1 : g > sh.total ? sh.total : g; }
+          [&](u64 total) { return MASS && lev == 0 ? mass_goal(top_p, total) : goal; }))
+        return cut;                                         // fewer tokens than top_k
+      if (MASS && lev == 0) goal = mass_goal(top_p, sh.total);
       goal -= MASS ? sh.before_mass : sh.before_cnt;
       prefix |= (uint32_t)sh.bin << shift;
       ties = sh.bin_cnt;
@@ -347,52 +380,213 @@ struct SampleRow {
       const u64 w = weigh(topk_value(prefix));
       r = (goal + w - 1) / w;
     }
-    Cut found = {prefix, 0x7fffffff};
+    Cut found = {topk_value(prefix), 0x7fffffff};
     if (r < ties) {
-      found.id = nth_tie(prefix, r);
+      found.id = nth_tie(found.l, r);
       __syncthreads();
     }
-    if (prefix == cut.key && cut.id < found.id) found.id = cut.id;
+    if (found.l == cut.l && cut.id < found.id) found.id = cut.id;
+    return found;
+  }
+
+  // ---- lists.  Tokens that want(logit) to the list of the cluster's first CTA; returns how many there are, which may be more than fit.
+  template <typename F> __device__ __forceinline__ uint32_t list(int which, F want) const {
+    const uint32_t counter = mapa_of(a.cluster, smem_u32(&sh.list_n[which]), 0);
+    each([&](float l, int id) {
+      if (!want(l)) return;
+      uint32_t at;
+      asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(counter) : "memory");
+      if (at < SAMPLE_LIST) {
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_of(a.cluster, smem_u32(sh.list_l + at), 0)), "r"(__float_as_uint(l)) : "memory");
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_of(a.cluster, smem_u32(sh.list_id + at), 0)), "r"((uint32_t)id) : "memory");
+      }
+    });
+    sync_all_of(a.cluster);
+    return ld_cluster_u32(counter);
+  }
+  __device__ __forceinline__ u64 block_sum_u64(u64 v) const {
+    v = warp_sum_u64(v);
+    __syncthreads();
+    if (lane == 0) sh.warp_tot[warp] = v;
+    __syncthreads();
+    return warp_sum_u64(lane < nw ? sh.warp_tot[lane] : 0ull);
+  }
+  // What became of the list, in the first CTA.  `share` threads have an entry together, the one with part 0 holds what became of it.
+  struct Settled {
+    int entry, share, part, id;        // entry: -1 without one
+    float l;
+    bool stays;
+    u64 w, n, mass;                    // its weight (0 if it is cut); how many stay, and their mass
+  };
+  // Settles the n listed tokens, which follow tokens that all stay: top_k more of them stay, of these those before which the mass is below
+  // goal(their mass), of these those with logits from least_l on; the first of the order does in any case if `one`.  Each entry counts the
+  // entries in front of it; threads share an entry so that all of the block works.
+  template <typename G> __device__ __forceinline__ Settled settle(uint32_t n, u64 top_k, G goal, float least_l, bool one, const Weigher &weigh) const {
+    const int tid = threadIdx.x;
+    Settled r;
+    r.share = SAMPLE_THREADS;
+    for (uint32_t m = 1; m < n; m *= 2) r.share /= 2;
+    r.share = max(1, min(32, r.share));
+    r.part = tid % r.share;
+    r.entry = tid / r.share < (int)n ? tid / r.share : -1;
+    for (uint32_t i = tid; i < n; i += SAMPLE_THREADS) sh.list_w[i] = weigh(sh.list_l[i]);
+    __syncthreads();
+    r.l = r.entry >= 0 ? sh.list_l[r.entry] : 0.f;
+    r.id = r.entry >= 0 ? sh.list_id[r.entry] : 0;
+    const u64 w = r.entry >= 0 ? sh.list_w[r.entry] : 0ull;
+    uint32_t rank = 0;
+    u64 before = 0;
+    for (uint32_t j = r.part; j < n; j += r.share) {
+      const float lj = sh.list_l[j];
+      if (lj > r.l || (lj == r.l && sh.list_id[j] < r.id)) { ++rank; before += sh.list_w[j]; }
+    }
+    for (int o = r.share >> 1; o > 0; o >>= 1) { rank += __shfl_xor_sync(0xffffffffu, rank, o); before += __shfl_xor_sync(0xffffffffu, before, o); }
+    const bool mine = r.entry >= 0 && r.part == 0, in_k = rank < top_k;
+    const u64 want = goal(block_sum_u64(mine && in_k ? w : 0ull));
+    r.stays = mine && ((in_k && before < want && r.l >= least_l) || (one && rank == 0));
+    r.w = r.stays ? w : 0ull;
+    r.mass = block_sum_u64(r.w);
+    r.n = block_sum_u64(r.stays ? 1ull : 0ull);
+    if (r.stays && rank + 1 == r.n) { sh.cut_l = r.l; sh.cut_id = r.id; }
+    __syncthreads();
+    return r;
+  }
+  // The kept entry at which the running mass in id order exceeds goal(their mass); u == 0: the first with any mass at all.  found(logit, id, mass)
+  // runs in the thread that holds it.
+  template <typename G, typename H> __device__ __forceinline__ void draw_settled(const Settled &r, uint32_t n, float u, double least, G goal, H found) const {
+    const bool stays = __shfl_sync(0xffffffffu, (int)r.stays, (int)(threadIdx.x & 31) / r.share * r.share);
+    if (r.entry >= 0 && r.part == 0) sh.list_w[r.entry] = r.w;             // cut tokens weigh nothing from here on
+    if (r.stays && u == 0.f && (double)r.l >= least) atomicMin(&sh.min_id, r.id);
+    __syncthreads();
+    u64 before = 0;
+    if (stays)
+      for (uint32_t j = r.part; j < n; j += r.share) if (sh.list_id[j] < r.id) before += sh.list_w[j];
+    for (int o = r.share >> 1; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+    const u64 t = goal(r.mass);
+    if (r.stays && (u == 0.f ? r.id == sh.min_id : before <= t && t - before < r.w)) found(r.l, r.id, r.mass);
+  }
+  // The first CTA's cut to all.
+  __device__ __forceinline__ Cut share_cut(int slot) const {
+    if (rank == 0 && threadIdx.x < a.cluster)
+      st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[slot][0]), threadIdx.x), (u64)__float_as_uint(sh.cut_l) << 32 | (uint32_t)sh.cut_id);
+    sync_all_of(a.cluster);
+    return {__uint_as_float((uint32_t)(sh.xch[slot][0] >> 32)), (int)(uint32_t)sh.xch[slot][0]};
+  }
+
+  // Many tokens, by count (top_k) or by mass (top_p) within the cut.  Bins of 1 / 128 nat below the row's maximum; what is 16 nats below or more
+  // is in bin 0.
+  template <bool MASS> __device__ __forceinline__ Cut select(Cut cut, u64 top_k, double top_p, const Weigher &weigh, float m, float temp, int slot) const {
+    const float scale = 128.f / temp;
+    auto nat_bin = [&](float l) { return (SAMPLE_BINS - 1) - (int)fminf((m - l) * scale, (float)(SAMPLE_BINS - 1)); };
+    if (!level<MASS>(false, !MASS,
+          [&](auto put) {
+            // weights first, without a branch among them: most of a row is in bin 0
+            each_vec([&](const float (&l)[VEC], int i0) {
+              u64 w[VEC];
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) w[e] = MASS ? weigh(l[e]) : 0ull;
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) put(cut.keeps(l[e], i0 + e) ? nat_bin(l[e]) : -1, w[e]);
+            });
+          },
+          [&](u64 total) { return MASS ? mass_goal(top_p, total) : top_k; }))
+      return cut;
+    const int bin = sh.bin;
+    const u64 left = (MASS ? mass_goal(top_p, sh.total) : top_k) - (MASS ? sh.before_mass : sh.before_cnt);
+    // bin 0 and bins of too many are for the radix selection; an infinite scale has everything in bin 0
+    if (bin == 0 || sh.bin_cnt > SAMPLE_LIST || !(scale < INFINITY) || m == INFINITY) return radix<MASS>(cut, top_k, top_p, weigh);
+    __syncthreads();
+    const uint32_t n = list(MASS ? 2 : 1, [&](float l) { return l >= cut.l && l > -INFINITY && nat_bin(l) == bin; });
+    if (rank == 0) {
+      // ties of the present cut's key behind its id are listed too: they come last, behind all that this cut can keep
+      if (n <= SAMPLE_LIST) settle(n, MASS ? (u64)n : left, [&](u64) { return MASS ? left : ~0ull; }, -INFINITY, false, weigh);
+      else {
+        if (threadIdx.x == 0) { sh.cut_l = INFINITY; sh.cut_id = -1; }
+        __syncthreads();
+      }
+    }
+    Cut found = share_cut(slot);
+    if (found.id < 0) return radix<MASS>(cut, top_k, top_p, weigh);
+    if (found.l == cut.l && cut.id < found.id) found.id = cut.id;
     return found;
   }
 };
 
 template <typename T, bool TRUNCATE>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(SAMPLE_THREADS, 2)
 k_sample(const __grid_constant__ SampleArgs a) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   SampleShared &sh = *reinterpret_cast<SampleShared *>(smem_raw);
   constexpr int VEC = SampleRow<T>::VEC;
   cluster_started_arrive(a.cluster);
   kernel_entry(TRUNCATE ? TR_k_truncate : TR_k_sample);
-  const int rank = a.cluster > 1 ? (int)cluster_ctarank() : 0, row = blockIdx.x / a.cluster, nw = blockDim.x >> 5, warp = threadIdx.x >> 5;
-  const SampleRow<T> R = {a, sh, reinterpret_cast<uint4 *>(smem_raw + sizeof(SampleShared)), rank, nw, warp, (int)(threadIdx.x & 31),
-                          a.warp_elems / (32 * VEC), (rank * nw + warp) * a.warp_elems, 0};
+  const int rank = a.cluster > 1 ? (int)cluster_ctarank() : 0, row = blockIdx.x / a.cluster, nw = SAMPLE_THREADS / 32, warp = threadIdx.x >> 5;
+  const SampleRow<T> R = {a, sh, reinterpret_cast<uint4 *>(smem_raw + (sizeof(SampleShared) + 15) / 16 * 16), rank, nw, warp, (int)(threadIdx.x & 31),
+                          a.warp_elems / (32 * VEC),
+                          (rank * nw + warp) * a.warp_elems - (int)((uintptr_t)((const T *)a.logits + row * a.ld) / sizeof(T) % VEC)};
   float temp = a.temperature ? a.temperature[row] : a.t0;
   int k = a.top_k ? a.top_k[row] : a.k0;
-  const float top_p = a.top_p ? a.top_p[row] : a.p0, min_p = a.min_p ? a.min_p[row] : a.m0;
+  float top_p = a.top_p ? a.top_p[row] : a.p0;
+  const float min_p = a.min_p ? a.min_p[row] : a.m0, u = TRUNCATE ? 0.f : fmaxf(a.uniforms[row], 0.f);
   if (!(temp > 0.f)) { temp = 1.f; k = 1; }                 // greedy
-  const float m = R.load(row);
-  Cut cut = {KEY_NEG_INF, -1};                              // every token above -inf
+  if (threadIdx.x < SAMPLE_TABLE) sh.table[threadIdx.x] = exp2((double)threadIdx.x / SAMPLE_TABLE);
+  float own, m, lowest;
+  R.load(row, own, m, lowest);
+  Cut cut = {-INFINITY, (int)0x80000000};                   // every token above -inf
   Weigher weigh;
+  weigh.table = sh.table;
   weigh.m = (double)m; weigh.c2 = 1.4426950408889634 / (double)temp; weigh.unit = __longlong_as_double((long long)(1023 + 52 - a.frac_bits) << 52);
   weigh.cut = fmaxf(__double2float_rd(weigh.m - (double)(a.frac_bits + 2) * 0.69314718055994531 * (double)temp), -3.402823466e38f);
   if (m == INFINITY) { weigh.m = (double)3.402823466e38f; weigh.cut = INFINITY; }   // the infinite ones share the mass
+  auto target = [&](u64 total) { const u64 t = (u64)((double)u * (double)total); return t < total ? t : total - 1; };
+  auto draw = [&](float l, int id, u64 total) {
+    a.tokens[row] = id;
+    if (a.logprob) a.logprob[row] = (float)((m == INFINITY ? 0.0 : ((double)l - weigh.m) / (double)temp) - log(ldexp((double)total, -a.frac_bits)));
+  };
   if (m > -INFINITY) {
-    if (k > 0 && k < a.vocab) cut = R.template select<false>(cut, (u64)k, 0.0, weigh);
-    if (top_p < 1.f) cut = R.template select<true>(cut, 0, (double)top_p, weigh);
-    if (min_p > 0.f) {                      // w >= min_p; the first of the order always stays
-      const double least = weigh.m + log((double)min_p) * (double)temp;
-      const float edge = m == INFINITY ? m : fminf(__double2float_ru(least), m);
-      Cut c = {topk_key(edge), 0x7fffffff};
-      if (min_p > 1.f) c = R.template select<false>(cut, 1, 0.0, weigh);
-      if (c.key > cut.key) cut = c;
-      else if (c.key == cut.key && c.id < cut.id) cut = c;
+    float least_l = -INFINITY;
+    if (min_p > 0.f) {                                      // w >= min_p
+      if (min_p > 1.f) k = 1;                               // nothing but the first of the order
+      else least_l = m == INFINITY ? m : fminf(__double2float_ru(weigh.m + log((double)min_p) * (double)temp), m);
     }
+    if (k > 0 && k < a.vocab) {
+      // Few tokens: a bin of the threads' own maxima, in 2047 steps from the smallest (or 256 below the largest) to the largest, down to which
+      // there are k of them.
+      const float low = fmaxf(lowest, m - 256.f), scale = (float)(SAMPLE_BINS - 1) / (m - low);
+      auto bin_of = [&](float l) { return l >= low ? (int)((l - low) * scale) : 0; };
+      bool listed = false;
+      if (k <= SAMPLE_SMALL_K && scale > 0.f && scale < INFINITY) {
+        R.template level<false>(true, false, [&](auto put) { put(bin_of(own), 0ull); }, [&](u64) { return (u64)k; });
+        const int bin = sh.bin;
+        __syncthreads();
+        uint32_t n = SAMPLE_LIST + 1;
+        if (bin > 0) n = R.list(0, [&](float l) { return bin_of(l) >= bin; });
+        listed = n <= SAMPLE_LIST;
+        if (listed) {
+          if (rank == 0) {
+            const auto r = R.settle(n, (u64)k, [&](u64 mass) { return top_p < 1.f ? SampleRow<T>::mass_goal((double)top_p, mass) : ~0ull; }, least_l, true, weigh);
+            if (!TRUNCATE) {
+              R.draw_settled(r, n, u, weigh.least((double)temp), target, draw);
+              if (threadIdx.x == 0 && a.kept) a.kept[row] = (int)r.n;
+            }
+          }
+          if (!TRUNCATE) {                                  // the first CTA stays until the others have read how long its list is
+            sync_all_of(a.cluster);
+            return;
+          }
+          cut = R.share_cut(8);
+          top_p = 1.f; least_l = -INFINITY;                      // settled with the list
+        }
+      }
+      if (!listed) cut = R.template select<false>(cut, (u64)k, 0.0, weigh, m, temp, 8);
+    }
+    if (top_p < 1.f) cut = R.template select<true>(cut, 0, (double)top_p, weigh, m, temp, 9);
+    if (least_l > cut.l) cut = {least_l, 0x7fffffff};       // the largest logit passes it: a first one always stays
   }
   uint32_t n = 0;
   if (TRUNCATE) {
     T *dst = (T *)a.out + row * a.out_ld;
+    const bool out_vec = ((uintptr_t)(dst + R.base) & 15) == 0;          // the output lies on its boundaries like the row
     const uint4 *p = R.vals + (size_t)warp * R.steps * 32 + R.lane;
 #pragma unroll 1
     for (int j = 0; j < R.steps; ++j) {
@@ -402,17 +596,17 @@ k_sample(const __grid_constant__ SampleArgs a) {
       T t[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const bool on = cut.keeps(topk_key(l[e]), i0 + e);
+        const bool on = cut.keeps(l[e], i0 + e);
         n += on ? 1u : 0u;
         t[e] = from_f<T>(on ? l[e] : -INFINITY);
       }
-      if (a.out_vec && i0 + VEC <= a.vocab) {
+      if (out_vec && i0 >= 0 && i0 + VEC <= a.vocab) {
         uint4 q;
         memcpy(&q, t, 16);
         *reinterpret_cast<uint4 *>(dst + i0) = q;
       } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) if (i0 + e < a.vocab) dst[i0 + e] = t[e];
+        for (int e = 0; e < VEC; ++e) if (i0 + e >= 0 && i0 + e < a.vocab) dst[i0 + e] = t[e];
       }
     }
     if (a.kept) {
@@ -439,17 +633,10 @@ k_sample(const __grid_constant__ SampleArgs a) {
     }
     return;
   }
-  R.each([&](float l, int id) { n += cut.keeps(topk_key(l), id) ? 1u : 0u; });
-  const float u = fmaxf(a.uniforms[row], 0.f);
-  auto draw = [&](float l, int id, u64 total) {
-    a.tokens[row] = id;
-    if (a.logprob) a.logprob[row] = (float)((m == INFINITY ? 0.0 : ((double)l - weigh.m) / (double)temp) - log(ldexp((double)total, -a.frac_bits)));
-  };
-  const u64 total = R.locate(6, [&](float l, int id) { return cut.keeps(topk_key(l), id) ? weigh(l) : 0ull; },
-                             [&](u64 total) { const u64 t = (u64)((double)u * (double)total); return t < total ? t : total - 1; }, n,
-                             [&](float l, int id, u64 total) { if (u > 0.f) draw(l, id, total); });
+  const u64 total = R.locate(6, [&](float l, int id) { return cut.keeps(l, id) ? weigh(l) : 0ull; }, target,
+                             [&](float l, int id) { return cut.keeps(l, id) ? 1u : 0u; }, [&](float l, int id, u64 total) { if (u > 0.f) draw(l, id, total); });
   if (u == 0.f)                                             // the first kept id with any mass, be it less than a unit
-    R.locate(2, [&](float l, int id) { return (u64)(cut.keeps(topk_key(l), id) && l >= weigh.least((double)temp)); }, [](u64) { return 0ull; }, 0u,
+    R.locate(2, [&](float l, int id) { return (u64)(cut.keeps(l, id) && l >= weigh.least((double)temp)); }, [](u64) { return 0ull; }, [](float, int) { return 0u; },
              [&](float l, int id, u64) { draw(l, id, total); });
   if (rank == 0 && threadIdx.x == 0 && a.kept) {
     u64 all = 0;
