@@ -25,7 +25,7 @@
 #define SAMPLE_MAX_VOCAB (SAMPLE_MAX_CLUSTER * SAMPLE_CTA_MAX)
 #define SAMPLE_BINS 2048
 #define SAMPLE_CHUNKS 32               // of SAMPLE_BINS / 32 bins, a lane each
-#define SAMPLE_EXCHANGES 10
+#define SAMPLE_EXCHANGES 11
 #define SAMPLE_LIST 512                // listed tokens one block settles
 #define SAMPLE_SMALL_K 256
 #define SAMPLE_THREADS 512
@@ -71,31 +71,37 @@ struct SampleShared {
   uint32_t cnt[SAMPLE_BINS], lo[SAMPLE_BINS], hi[SAMPLE_BINS];
 };
 
-__device__ __forceinline__ u64 warp_sum_u64(u64 v) {
+// Sums and inclusive running sums over a warp, of u64 or double.
+template <typename A> __device__ __forceinline__ A warp_total(A v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ u64 warp_scan_u64(u64 v) {            // inclusive
+template <typename A> __device__ __forceinline__ A warp_scan(A v) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const u64 t = __shfl_up_sync(0xffffffffu, v, o);
+    const A t = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += t;
   }
   return v;
 }
+__device__ __forceinline__ u64 as_bits(u64 v) { return v; }
+__device__ __forceinline__ u64 as_bits(double v) { return (u64)__double_as_longlong(v); }
+template <typename A> __device__ __forceinline__ A of_bits(u64 v);
+template <> __device__ __forceinline__ u64 of_bits<u64>(u64 v) { return v; }
+template <> __device__ __forceinline__ double of_bits<double>(u64 v) { return __longlong_as_double((long long)v); }
 
-// exp((l - m) / T) as an integer of 2^-s.  2^y by table, as in Tang's table-driven exponential: y = n + j / 256 + r, |r| <= 1 / 512, and 2^r by the
-// Taylor series of e^(r ln 2) to its third power (remainder 1.4e-13).  Both roundings to integers are additions of a number so large
-// that its last bit is the unit wanted.  Nine operations in double, where a series without a table takes fifteen.
+// exp((l - m) / T), also as an integer of 2^-s.  2^y by table, as in Tang's table-driven exponential: y = n + j / 256 + r, |r| <= 1 / 512, and 2^r by the
+// Taylor series of e^(r ln 2) to its third power (remainder 1.4e-13).  Roundings to integers are additions of a number so large that its
+// last bit is the unit wanted.  Eight operations in double, where a series without a table takes fourteen.
 #define SAMPLE_TABLE 256
 struct Weigher {
   double m, c2, unit;                  // row maximum, log2(e) / T, 2^(52 - s)
   float cut;                           // below it a weight is less than half a unit
   const double *table;                 // 2^(j / 256), in shared memory
-  __device__ __forceinline__ u64 operator()(float l) const {
-    const double d = (double)fminf(fmaxf(l, cut), 3.402823466e38f) - m;
+  __device__ __forceinline__ double raw(float l) const {
+    const double d = (double)fminf(l, 3.402823466e38f) - m;
     const double big = 6755399441055744.0 / SAMPLE_TABLE;       // 1.5 * 2^52 / 256: its last bit is 1 / 256
     const double t = fma(d, c2, big), r = fma(d, c2, -(t - big));
     const int n = __double2loint(t);
@@ -103,12 +109,15 @@ struct Weigher {
     double p = fma(r, 0.05550410866482158, 0.2402265069591007);  // ln(2)^k / k!, k = 3, 2, 1
     p = fma(p, r, 0.6931471805599453);
     p = fma(e, p * r, e);
-    p = __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
-    const u64 w = (u64)__double_as_longlong(p + unit) - (u64)__double_as_longlong(unit);
+    return __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
+  }
+  __device__ __forceinline__ double exact(float l) const { const double p = raw(l); return l >= cut ? p : 0.0; }
+  __device__ __forceinline__ u64 units(float l) const {
+    const u64 w = (u64)__double_as_longlong(raw(l) + unit) - (u64)__double_as_longlong(unit);
     return l >= cut ? w : 0ull;
   }
   // The smallest logit whose weight is above zero in double.
-  __device__ __forceinline__ double least(double temp) const { return cut == INFINITY ? INFINITY : m - 744.0 * temp; }
+  __device__ __forceinline__ double least(double temp) const { return m - 744.0 * temp; }
 };
 
 // A cut of the order: larger logits stay, and equal ones up to an id; -inf and NaN never do.
@@ -210,40 +219,43 @@ struct SampleRow {
     }
   }
 
-  // One level of the selection.  walk(put) hands put(bin, mass) the tokens, or one value a thread; of the bins, from the top, that one is
-  // found in which the running count (MASS false) or mass reaches goal(total), and left in sh.bin .. sh.total.  enough: false, and nothing
+  // One level of the selection.  walk(put) hands put(bin, term) the tokens, or one value a thread; of the bins, from the top, that one is
+  // found in which the running count or mass reaches goal(total), and left in sh.bin .. sh.total.  enough: false, and nothing
   // found, where the goal is not below the total.  Bin 0 may hold most of a row, so it is added up in registers first.
-  template <bool MASS, typename F, typename G> __device__ __forceinline__ bool level(bool first, bool enough, F walk, G goal) const {
+  template <int KIND, typename F, typename G> __device__ __forceinline__ bool level(bool first, bool enough, F walk, G goal) const {
+    constexpr bool MASS = KIND != COUNT, UNITS = KIND == UNITS_OF_MASS;
     if (!first) sync_all_of(a.cluster);                     // nobody still reads the bins of the level before
     for (int i = threadIdx.x; i < SAMPLE_BINS; i += blockDim.x) {
       sh.cnt[i] = 0;
-      if (MASS) { sh.lo[i] = 0; sh.hi[i] = 0; }
+      if (UNITS) { sh.lo[i] = 0; sh.hi[i] = 0; }
     }
     __syncthreads();
     uint32_t n0 = 0;
     u64 w0 = 0;
     auto add = [&](int bin, uint32_t n, u64 w) {
       atomicAdd(&sh.cnt[bin], n);
-      if (MASS && w) {
+      if (UNITS && w) {
         const uint32_t low = (uint32_t)w, old = atomicAdd(&sh.lo[bin], low), up = (uint32_t)(w >> 32) + (old + low < old ? 1u : 0u);
         if (up) atomicAdd(&sh.hi[bin], up);
       }
     };
     walk([&](int bin, u64 w) {
-      if (bin > 0) add(bin, 1u, w);
-      n0 += bin == 0 ? 1u : 0u;
-      if (MASS) w0 += bin == 0 ? w : 0ull;
+      if (bin > 0) add(bin, KIND == NATS_OF_MASS ? (uint32_t)w : 1u, w);
+      if (KIND != NATS_OF_MASS) n0 += bin == 0 ? 1u : 0u;
+      if (UNITS) w0 += bin == 0 ? w : 0ull;
     });
-    n0 = __reduce_add_sync(0xffffffffu, n0);
-    if (MASS) w0 = warp_sum_u64(w0);
-    if (lane == 0 && n0) add(0, n0, w0);
+    if (KIND != NATS_OF_MASS) {
+      n0 = __reduce_add_sync(0xffffffffu, n0);
+      if (UNITS) w0 = warp_total<u64>(w0);
+      if (lane == 0 && n0) add(0, n0, w0);
+    }
     __syncthreads();
     for (int ch = warp; ch < SAMPLE_CHUNKS; ch += nw) {
       const int i = ch * (SAMPLE_BINS / SAMPLE_CHUNKS) + lane;
       uint32_t c = sh.cnt[i] + sh.cnt[i + 32];
       c = __reduce_add_sync(0xffffffffu, c);
       u64 w = 0;
-      if (MASS) w = warp_sum_u64(bin_mass(i) + bin_mass(i + 32));
+      if (MASS) w = warp_total<u64>(bin_mass<KIND>(i, sh.cnt[i], UNITS ? sh.lo[i] : 0u, UNITS ? sh.hi[i] : 0u) + bin_mass<KIND>(i + 32, sh.cnt[i + 32], UNITS ? sh.lo[i + 32] : 0u, UNITS ? sh.hi[i + 32] : 0u));
       if (lane == 0) { sh.coarse_cnt[ch] = c; if (MASS) sh.coarse_mass[ch] = w; }
     }
     sync_all_of(a.cluster);
@@ -255,7 +267,7 @@ struct SampleRow {
         c += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.coarse_cnt[ch]), q));
         if (MASS) w += ld_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.coarse_mass[ch]), q));
       }
-      const u64 ic = warp_scan_u64(c), iw = MASS ? warp_scan_u64(w) : 0;
+      const u64 ic = warp_scan<u64>(c), iw = MASS ? warp_scan<u64>(w) : 0;
       const u64 total = __shfl_sync(0xffffffffu, MASS ? iw : ic, 31), want = goal(total);
       const unsigned hit = __ballot_sync(0xffffffffu, (MASS ? iw : ic) >= want);
       if (!hit || (enough && want >= total)) { if (lane == 0) sh.bin = -1; }
@@ -268,10 +280,12 @@ struct SampleRow {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {                                  // lane's bins, descending: top - 2 lane, then the next
             const int i = top - 2 * lane - k;
-            c2[k] += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
-            if (MASS) w2[k] += (u64)ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)) + ((u64)ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[i]), q)) << 32);
+            const uint32_t n = ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
+            c2[k] += n;
+            if (MASS) w2[k] += bin_mass<KIND>(i, n, UNITS ? ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)) : 0u,
+                                              UNITS ? ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[i]), q)) : 0u);
           }
-        const u64 sc = bc + warp_scan_u64(c2[0] + c2[1]), sw = bw + (MASS ? warp_scan_u64(w2[0] + w2[1]) : 0);
+        const u64 sc = bc + warp_scan<u64>(c2[0] + c2[1]), sw = bw + (MASS ? warp_scan<u64>(w2[0] + w2[1]) : 0);
         const unsigned h2 = __ballot_sync(0xffffffffu, (MASS ? sw : sc) >= want);
         if (lane == __ffs(h2) - 1) {
           const u64 c0 = sc - c2[0] - c2[1], w0 = sw - w2[0] - w2[1];
@@ -287,53 +301,79 @@ struct SampleRow {
     __syncthreads();
     return sh.bin >= 0;
   }
-  __device__ __forceinline__ u64 bin_mass(int i) const { return (u64)sh.lo[i] + ((u64)sh.hi[i] << 32); }
+  // UNITS_OF_MASS: exact, a 64-bit sum in two words.  NATS_OF_MASS: bin i is the i-th of 1 / 128 nat from the bottom of SAMPLE_BINS, n the sum of
+  // its weights relative to its upper edge's in 1 / 4096; mass in units of 2^-32, good to a few 1e-5.
+  enum { COUNT, UNITS_OF_MASS, NATS_OF_MASS };
+  template <int KIND> static __device__ __forceinline__ u64 bin_mass(int i, uint32_t n, uint32_t lo, uint32_t hi) {
+    if (KIND == UNITS_OF_MASS) return (u64)lo + ((u64)hi << 32);
+    return (u64)((float)n * ex2((float)(i - (SAMPLE_BINS - 1)) * (1.44269504f / 128.f) + 20.f));
+  }
 
-  // The first token in id order at which the running sum of val exceeds goal(total): found(logit, id, total) runs in the one thread that
-  // holds it.  Two exchange slots (the second carries the sum of count over the tokens); returns the total.
-  template <typename V, typename G, typename C, typename H> __device__ __forceinline__ u64 locate(int slot, V val, G goal, C count, H found) const {
-    u64 s = 0;
-    uint32_t side = 0;
-    each([&](float l, int id) { s += val(l, id); side += count(l, id); });
-    s = warp_sum_u64(s);
-    side = __reduce_add_sync(0xffffffffu, side);
+  // The first token in id order at which the running sum of vals exceeds goal(total): found(logit, id, total) runs in the one thread that
+  // holds it.  vals(logits, first id, v) gives a vector's terms and returns how many tokens they count for.  Two exchange slots (the second
+  // carries the count); returns the total.  In double as in integers the sums have one order, and neighbours see the same border between them.
+  template <typename A, typename V, typename G, typename H> __device__ __forceinline__ A locate(int slot, V vals_of, G goal, H found) const {
+    A s = 0;
+    uint32_t n = 0;
+    each_vec([&](const float (&l)[VEC], int i0) {
+      A v[VEC];
+      n += vals_of(l, i0, v);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s += v[e];
+    });
+    s = warp_total<A>(s);
+    n = __reduce_add_sync(0xffffffffu, n);
     __syncthreads();
-    if (lane == 0) { sh.warp_tot[warp] = s; sh.warp_cnt[warp] = side; }
+    if (lane == 0) { sh.warp_tot[warp] = as_bits(s); sh.warp_cnt[warp] = n; }
     __syncthreads();
-    const u64 mine = lane < nw ? sh.warp_tot[lane] : 0, inc = warp_scan_u64(mine), all = __shfl_sync(0xffffffffu, inc, 31);
-    const u64 n = __reduce_add_sync(0xffffffffu, lane < nw ? sh.warp_cnt[lane] : 0u);
-    if (threadIdx.x < a.cluster) st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[slot + 1][rank]), threadIdx.x), n);
-    exchange(slot, all);
-    u64 before = 0, total = 0;
-    for (int q = 0; q < a.cluster; ++q) { const u64 x = sh.xch[slot][q]; total += x; if (q < rank) before += x; }
-    const u64 want = goal(total);
-    before += __shfl_sync(0xffffffffu, inc - mine, warp);
-    if (total && want >= before && want - before < s) {                 // a warp at most
-      u64 left = want - before;
+    const A inc = warp_scan<A>(lane < nw ? of_bits<A>(sh.warp_tot[lane]) : (A)0), all = __shfl_sync(0xffffffffu, inc, nw - 1);
+    n = __reduce_add_sync(0xffffffffu, lane < nw ? sh.warp_cnt[lane] : 0u);
+    if (threadIdx.x < a.cluster) st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[slot + 1][rank]), threadIdx.x), (u64)n);
+    exchange(slot, as_bits(all));
+    A before = 0, total = 0;
+    for (int q = 0; q < a.cluster; ++q) {
+      if (q == rank) before = total;
+      total += of_bits<A>(sh.xch[slot][q]);
+    }
+    const A want = goal(total), up = __shfl_sync(0xffffffffu, inc, max(warp, 1) - 1), start = warp ? before + up : before,
+            end = before + __shfl_sync(0xffffffffu, inc, warp);
+    if (want >= start && want < end) {                      // a warp at most
+      A left = want - start;
+      int last = -1;                                        // with a term of its own, for a rounding that puts the goal behind the warp's end
+      float last_l = 0.f;
+      bool done = false;
       const uint4 *p = vals + (size_t)warp * steps * 32 + lane;
 #pragma unroll 1
-      for (int j = 0; j < steps; ++j) {
+      for (int j = 0; j < steps && !done; ++j) {
         float l[VEC];
         unpack(p[j * 32], l);
         const int i0 = base + (j * 32 + lane) * VEC;
-        u64 v[VEC], sum = 0;
+        A v[VEC], sum = 0;
+        vals_of(l, i0, v);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) { v[e] = val(l[e], i0 + e); sum += v[e]; }
-        const u64 in = warp_scan_u64(sum), group = __shfl_sync(0xffffffffu, in, 31);
-        if (left < group) {
-          const unsigned hit = __ballot_sync(0xffffffffu, in > left);
+        for (int e = 0; e < VEC; ++e) { sum += v[e]; if (v[e] > (A)0) { last = i0 + e; last_l = l[e]; } }
+        const A in = warp_scan<A>(sum), group = __shfl_sync(0xffffffffu, in, 31);
+        const unsigned hit = __ballot_sync(0xffffffffu, in > left);
+        if (hit) {
+          const A front = __shfl_up_sync(0xffffffffu, in, 1);
           if (lane == __ffs(hit) - 1) {
-            u64 run = in - sum;
-            bool done = false;
+            A run = lane ? front : (A)0;
+            bool mine = false;
+            int id = last;
+            float x = last_l;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
               run += v[e];
-              if (!done && run > left) { done = true; found(l[e], i0 + e, total); }
+              if (!mine && run > left) { mine = true; id = i0 + e; x = l[e]; }
             }
+            found(x, id, total);
           }
-          break;
-        }
-        left -= group;
+          done = true;
+        } else left -= group;
+      }
+      if (!done) {
+        const int id = __reduce_max_sync(0xffffffffu, last);
+        if (id >= 0 && id == last) found(last_l, id, total);
       }
     }
     return total;
@@ -341,10 +381,14 @@ struct SampleRow {
 
   // The last of the first r tokens of a logit in id order, to every CTA.
   __device__ __forceinline__ int nth_tie(float tie, u64 r) const {
-    locate(2, [&](float l, int) { return (u64)(l == tie); }, [&](u64) { return r - 1; }, [](float, int) { return 0u; },
-           [&](float, int id, u64) { for (int q = 0; q < a.cluster; ++q) st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[4][0]), q), (u64)id); });
+    locate<u64>(2, [&](const float (&l)[VEC], int, u64 (&v)[VEC]) {
+#pragma unroll
+                  for (int e = 0; e < VEC; ++e) v[e] = (u64)(l[e] == tie);
+                  return 0u;
+                }, [&](u64) { return r - 1; },
+           [&](float, int id, u64) { for (int q = 0; q < a.cluster; ++q) st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[10][0]), q), (u64)id); });
     sync_all_of(a.cluster);
-    return (int)sh.xch[4][0];
+    return (int)sh.xch[10][0];
   }
 
   static __device__ __forceinline__ u64 mass_goal(double top_p, u64 total) {     // masses below it stay; the first token always does
@@ -359,12 +403,12 @@ struct SampleRow {
     for (int lev = 0; lev < 3; ++lev) {
       const int shift = lev == 0 ? 21 : lev == 1 ? 10 : 0, width = lev == 2 ? 1023 : 2047;
       const uint32_t above = lev == 0 ? 0u : lev == 1 ? 0xffe00000u : 0xfffffc00u;
-      if (!level<MASS>(false, !MASS && lev == 0,
+      if (!level<MASS ? UNITS_OF_MASS : COUNT>(false, !MASS && lev == 0,
           [&](auto put) {
             each([&](float l, int id) {
               const uint32_t k = topk_key(l);
               if ((k & above) != prefix || !cut.keeps(l, id)) return;
-              put((int)((k >> shift) & width), MASS ? weigh(l) : 0ull);
+              put((int)((k >> shift) & width), MASS ? weigh.units(l) : 0ull);
             });
           },
           [&](u64 total) { return MASS && lev == 0 ? mass_goal(top_p, total) : goal; }))
@@ -377,7 +421,7 @@ struct SampleRow {
     }
     u64 r = goal;                                           // ties of the key that stay
     if (MASS) {
-      const u64 w = weigh(topk_value(prefix));
+      const u64 w = weigh.units(topk_value(prefix));
       r = (goal + w - 1) / w;
     }
     Cut found = {topk_value(prefix), 0x7fffffff};
@@ -389,11 +433,11 @@ struct SampleRow {
     return found;
   }
 
-  // ---- lists.  Tokens that want(logit) to the list of the cluster's first CTA; returns how many there are, which may be more than fit.
-  template <typename F> __device__ __forceinline__ uint32_t list(int which, F want) const {
+  // ---- lists.  Tokens that want(logit, id) to the list of the cluster's first CTA; returns how many there are, which may be more than fit.
+  template <typename F, typename P> __device__ __forceinline__ uint32_t list(int which, F want, P before_barrier) const {
     const uint32_t counter = mapa_of(a.cluster, smem_u32(&sh.list_n[which]), 0);
     each([&](float l, int id) {
-      if (!want(l)) return;
+      if (!want(l, id)) return;
       uint32_t at;
       asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(counter) : "memory");
       if (at < SAMPLE_LIST) {
@@ -401,15 +445,16 @@ struct SampleRow {
         asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_of(a.cluster, smem_u32(sh.list_id + at), 0)), "r"((uint32_t)id) : "memory");
       }
     });
+    before_barrier();
     sync_all_of(a.cluster);
     return ld_cluster_u32(counter);
   }
   __device__ __forceinline__ u64 block_sum_u64(u64 v) const {
-    v = warp_sum_u64(v);
+    v = warp_total<u64>(v);
     __syncthreads();
     if (lane == 0) sh.warp_tot[warp] = v;
     __syncthreads();
-    return warp_sum_u64(lane < nw ? sh.warp_tot[lane] : 0ull);
+    return warp_total<u64>(lane < nw ? sh.warp_tot[lane] : 0ull);
   }
   // What became of the list, in the first CTA.  `share` threads have an entry together, the one with part 0 holds what became of it.
   struct Settled {
@@ -429,7 +474,7 @@ struct SampleRow {
     r.share = max(1, min(32, r.share));
     r.part = tid % r.share;
     r.entry = tid / r.share < (int)n ? tid / r.share : -1;
-    for (uint32_t i = tid; i < n; i += SAMPLE_THREADS) sh.list_w[i] = weigh(sh.list_l[i]);
+    for (uint32_t i = tid; i < n; i += SAMPLE_THREADS) sh.list_w[i] = weigh.units(sh.list_l[i]);
     __syncthreads();
     r.l = r.entry >= 0 ? sh.list_l[r.entry] : 0.f;
     r.id = r.entry >= 0 ? sh.list_id[r.entry] : 0;
@@ -473,41 +518,86 @@ struct SampleRow {
     return {__uint_as_float((uint32_t)(sh.xch[slot][0] >> 32)), (int)(uint32_t)sh.xch[slot][0]};
   }
 
-  // Many tokens, by count (top_k) or by mass (top_p) within the cut.  Bins of 1 / 128 nat below the row's maximum; what is 16 nats below or more
-  // is in bin 0.
-  template <bool MASS> __device__ __forceinline__ Cut select(Cut cut, u64 top_k, double top_p, const Weigher &weigh, float m, float temp, int slot) const {
-    const float scale = 128.f / temp;
-    auto nat_bin = [&](float l) { return (SAMPLE_BINS - 1) - (int)fminf((m - l) * scale, (float)(SAMPLE_BINS - 1)); };
-    if (!level<MASS>(false, !MASS,
-          [&](auto put) {
-            // weights first, without a branch among them: most of a row is in bin 0
-            each_vec([&](const float (&l)[VEC], int i0) {
-              u64 w[VEC];
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) w[e] = MASS ? weigh(l[e]) : 0ull;
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) put(cut.keeps(l[e], i0 + e) ? nat_bin(l[e]) : -1, w[e]);
-            });
-          },
-          [&](u64 total) { return MASS ? mass_goal(top_p, total) : top_k; }))
-      return cut;
-    const int bin = sh.bin;
-    const u64 left = (MASS ? mass_goal(top_p, sh.total) : top_k) - (MASS ? sh.before_mass : sh.before_cnt);
-    // bin 0 and bins of too many are for the radix selection; an infinite scale has everything in bin 0
-    if (bin == 0 || sh.bin_cnt > SAMPLE_LIST || !(scale < INFINITY) || m == INFINITY) return radix<MASS>(cut, top_k, top_p, weigh);
+  __device__ __forceinline__ double block_sum(double v) const {
+    v = warp_total<double>(v);
     __syncthreads();
-    const uint32_t n = list(MASS ? 2 : 1, [&](float l) { return l >= cut.l && l > -INFINITY && nat_bin(l) == bin; });
+    if (lane == 0) sh.warp_tot[warp] = as_bits(v);
+    __syncthreads();
+    return warp_total<double>(lane < nw ? of_bits<double>(sh.warp_tot[lane]) : 0.0);
+  }
+  __device__ __forceinline__ void push(int slot, double v) const {       // to every CTA; there behind the next barrier of the cluster
+    if (threadIdx.x < a.cluster) st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[slot][rank]), threadIdx.x), as_bits(v));
+  }
+  __device__ __forceinline__ double pushed(int slot) const {
+    double v = 0.0;
+    for (int q = 0; q < a.cluster; ++q) v += of_bits<double>(sh.xch[slot][q]);
+    return v;
+  }
+  // Many tokens, by count (top_k) or by mass (top_p) within the cut.  Bins of 1 / 128 nat below the row's maximum; what is 16 nats below or more
+  // is in bin 0.  By mass the bins are approximate and only say where to look: the mass in front of the bin's upper neighbour is then summed
+  // exactly, and the three bins are listed.
+  template <bool MASS> __device__ __forceinline__ Cut select(Cut cut, u64 top_k, double top_p, const Weigher &weigh, float m, float temp) const {
+    const float scale = 128.f / temp;
+    auto depth = [&](float l) { return fminf((m - l) * scale, (float)(SAMPLE_BINS - 1)); };
+    auto nat_bin = [&](float l) { return (SAMPLE_BINS - 1) - (int)depth(l); };
+    double z = 0.0;
+    const bool found_bin = level<MASS ? NATS_OF_MASS : COUNT>(false, !MASS,
+          [&](auto put) {
+            if (!MASS) {
+              each([&](float l, int id) { if (cut.keeps(l, id)) put(nat_bin(l), 0ull); });
+              return;
+            }
+            double s = 0.0;
+            each_vec([&](const float (&l)[VEC], int i0) {
+              double w[VEC];
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) w[e] = weigh.exact(l[e]);
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) {
+                const bool on = cut.keeps(l[e], i0 + e);
+                s += on ? w[e] : 0.0;
+                const float x = depth(l[e]), below = floorf(x), y = (x - below) * (1.f / 128.f);
+                if (on && x < (float)(SAMPLE_BINS - 1)) put((SAMPLE_BINS - 1) - (int)below, (u64)(uint32_t)(4096.5f - 4096.f * (y - 0.5f * y * y)));
+              }
+            });
+            push(8, block_sum(s));
+          },
+          [&](u64) {
+            if (!MASS) return top_k;
+            z = pushed(8);
+            return (u64)fmax(1.0, top_p * z * 4294967296.0);
+          });
+    if (!MASS && !found_bin && sh.bin == -1) return cut;    // no more tokens than top_k
+    z = MASS ? pushed(8) : 0.0;
+    const int bin = sh.bin;
+    const u64 left = MASS ? 0ull : top_k - sh.before_cnt;
+    // bin 0, or none, is for the radix selection; an infinite scale has everything there
+    if (!found_bin || bin == 0 || !(scale < INFINITY)) return radix<MASS>(cut, top_k, top_p, weigh);
+    __syncthreads();
+    double s = 0.0;
+    const uint32_t n = list(MASS ? 2 : 1, [&](float l, int id) {
+          if (!cut.keeps(l, id)) return false;
+          const int b = nat_bin(l);
+          if (MASS && b > bin + 1) s += weigh.exact(l);
+          return MASS ? b >= bin - 1 && b <= bin + 1 : b == bin;
+        }, [&] { if (MASS) push(9, block_sum(s)); });
     if (rank == 0) {
-      // ties of the present cut's key behind its id are listed too: they come last, behind all that this cut can keep
-      if (n <= SAMPLE_LIST) settle(n, MASS ? (u64)n : left, [&](u64) { return MASS ? left : ~0ull; }, -INFINITY, false, weigh);
-      else {
-        if (threadIdx.x == 0) { sh.cut_l = INFINITY; sh.cut_id = -1; }
-        __syncthreads();
+      bool good = n <= SAMPLE_LIST;
+      if (good) {
+        const double rest = MASS ? top_p * z - pushed(9) : 0.0;            // of the listed tokens' mass
+        const u64 units = MASS ? (u64)fmax(0.0, ceil(rest * (4503599627370496.0 / weigh.unit))) : 0ull;
+        const auto r = settle(n, MASS ? (u64)n : left, [&](u64 mass) {
+            if (MASS && (rest <= 0.0 || units > mass)) sh.bin = -2;        // the bins were too coarse: the cut is not among them
+            return MASS ? units : ~0ull;
+          }, -INFINITY, false, weigh);
+        good = sh.bin != -2 && r.n > 0;
       }
+      __syncthreads();
+      if (!good && threadIdx.x == 0) { sh.cut_l = INFINITY; sh.cut_id = -1; }
+      __syncthreads();
     }
-    Cut found = share_cut(slot);
-    if (found.id < 0) return radix<MASS>(cut, top_k, top_p, weigh);
-    if (found.l == cut.l && cut.id < found.id) found.id = cut.id;
+    const Cut found = share_cut(MASS ? 7 : 6);
+    if (found.l == INFINITY && found.id < 0) return radix<MASS>(cut, top_k, top_p, weigh);
     return found;
   }
 };
@@ -534,20 +624,21 @@ k_sample(const __grid_constant__ SampleArgs a) {
   R.load(row, own, m, lowest);
   Cut cut = {-INFINITY, (int)0x80000000};                   // every token above -inf
   Weigher weigh;
+  const bool infinite = m == INFINITY;                      // the infinite ones share the mass
   weigh.table = sh.table;
   weigh.m = (double)m; weigh.c2 = 1.4426950408889634 / (double)temp; weigh.unit = __longlong_as_double((long long)(1023 + 52 - a.frac_bits) << 52);
   weigh.cut = fmaxf(__double2float_rd(weigh.m - (double)(a.frac_bits + 2) * 0.69314718055994531 * (double)temp), -3.402823466e38f);
-  if (m == INFINITY) { weigh.m = (double)3.402823466e38f; weigh.cut = INFINITY; }   // the infinite ones share the mass
+  if (infinite) { weigh.m = (double)3.402823466e38f; weigh.cut = INFINITY; }
   auto target = [&](u64 total) { const u64 t = (u64)((double)u * (double)total); return t < total ? t : total - 1; };
-  auto draw = [&](float l, int id, u64 total) {
+  auto draw = [&](float l, int id, double total) {
     a.tokens[row] = id;
-    if (a.logprob) a.logprob[row] = (float)((m == INFINITY ? 0.0 : ((double)l - weigh.m) / (double)temp) - log(ldexp((double)total, -a.frac_bits)));
+    if (a.logprob) a.logprob[row] = (float)((infinite ? 0.0 : ((double)l - weigh.m) / (double)temp) - log(total));
   };
   if (m > -INFINITY) {
     float least_l = -INFINITY;
     if (min_p > 0.f) {                                      // w >= min_p
       if (min_p > 1.f) k = 1;                               // nothing but the first of the order
-      else least_l = m == INFINITY ? m : fminf(__double2float_ru(weigh.m + log((double)min_p) * (double)temp), m);
+      else least_l = infinite ? m : fminf(__double2float_ru(weigh.m + log((double)min_p) * (double)temp), m);
     }
     if (k > 0 && k < a.vocab) {
       // Few tokens: a bin of the threads' own maxima, in 2047 steps from the smallest (or 256 below the largest) to the largest, down to which
@@ -556,17 +647,17 @@ k_sample(const __grid_constant__ SampleArgs a) {
       auto bin_of = [&](float l) { return l >= low ? (int)((l - low) * scale) : 0; };
       bool listed = false;
       if (k <= SAMPLE_SMALL_K && scale > 0.f && scale < INFINITY) {
-        R.template level<false>(true, false, [&](auto put) { put(bin_of(own), 0ull); }, [&](u64) { return (u64)k; });
+        R.template level<SampleRow<T>::COUNT>(true, false, [&](auto put) { put(bin_of(own), 0ull); }, [&](u64) { return (u64)k; });
         const int bin = sh.bin;
         __syncthreads();
         uint32_t n = SAMPLE_LIST + 1;
-        if (bin > 0) n = R.list(0, [&](float l) { return bin_of(l) >= bin; });
+        if (bin > 0) n = R.list(0, [&](float l, int) { return bin_of(l) >= bin; }, [] {});
         listed = n <= SAMPLE_LIST;
         if (listed) {
           if (rank == 0) {
             const auto r = R.settle(n, (u64)k, [&](u64 mass) { return top_p < 1.f ? SampleRow<T>::mass_goal((double)top_p, mass) : ~0ull; }, least_l, true, weigh);
             if (!TRUNCATE) {
-              R.draw_settled(r, n, u, weigh.least((double)temp), target, draw);
+              R.draw_settled(r, n, u, weigh.least((double)temp), target, [&](float l, int id, u64 total) { draw(l, id, ldexp((double)total, -a.frac_bits)); });
               if (threadIdx.x == 0 && a.kept) a.kept[row] = (int)r.n;
             }
           }
@@ -574,13 +665,13 @@ k_sample(const __grid_constant__ SampleArgs a) {
             sync_all_of(a.cluster);
             return;
           }
-          cut = R.share_cut(8);
+          cut = R.share_cut(6);
           top_p = 1.f; least_l = -INFINITY;                      // settled with the list
         }
       }
-      if (!listed) cut = R.template select<false>(cut, (u64)k, 0.0, weigh, m, temp, 8);
+      if (!listed) cut = R.template select<false>(cut, (u64)k, 0.0, weigh, m, temp);
     }
-    if (top_p < 1.f) cut = R.template select<true>(cut, 0, (double)top_p, weigh, m, temp, 9);
+    if (top_p < 1.f) cut = R.template select<true>(cut, 0, fmax((double)top_p, 1e-30), weigh, m, temp);
     if (least_l > cut.l) cut = {least_l, 0x7fffffff};       // the largest logit passes it: a first one always stays
   }
   uint32_t n = 0;
@@ -615,10 +706,10 @@ k_sample(const __grid_constant__ SampleArgs a) {
       if (R.lane == 0) sh.warp_cnt[warp] = n;
       __syncthreads();
       n = __reduce_add_sync(0xffffffffu, R.lane < nw ? sh.warp_cnt[R.lane] : 0u);
-      R.exchange(6, (u64)n);
+      R.exchange(1, (u64)n);
       if (rank == 0 && threadIdx.x == 0) {
         u64 all = 0;
-        for (int q = 0; q < a.cluster; ++q) all += sh.xch[6][q];
+        for (int q = 0; q < a.cluster; ++q) all += sh.xch[1][q];
         a.kept[row] = (int)all;
       }
     } else sync_all_of(a.cluster);                          // no CTA leaves while another may still read its histograms
@@ -633,14 +724,35 @@ k_sample(const __grid_constant__ SampleArgs a) {
     }
     return;
   }
-  const u64 total = R.locate(6, [&](float l, int id) { return cut.keeps(l, id) ? weigh(l) : 0ull; }, target,
-                             [&](float l, int id) { return cut.keeps(l, id) ? 1u : 0u; }, [&](float l, int id, u64 total) { if (u > 0.f) draw(l, id, total); });
-  if (u == 0.f)                                             // the first kept id with any mass, be it less than a unit
-    R.locate(2, [&](float l, int id) { return (u64)(cut.keeps(l, id) && l >= weigh.least((double)temp)); }, [](u64) { return 0ull; }, [](float, int) { return 0u; },
-             [&](float l, int id, u64) { draw(l, id, total); });
+  const bool whole = cut.l == -INFINITY;                    // nothing is cut: no comparison and no branch among the weights
+  auto weights = [&](const float (&l)[VEC], int i0, double (&v)[VEC]) {
+    uint32_t n = 0;
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) { v[e] = weigh.exact(l[e]); n += l[e] > -INFINITY ? 1u : 0u; }
+    } else {
+      bool on[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) { on[e] = cut.keeps(l[e], i0 + e); v[e] = 0.0; n += on[e] ? 1u : 0u; }
+      if (n) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) if (on[e]) v[e] = weigh.exact(l[e]);
+      }
+    }
+    return n;
+  };
+  const double total = R.template locate<double>(4, weights, [&](double total) { return fmin((double)u * total, total * 0.9999999999999999); },
+                                                 [&](float l, int id, double total) { if (u > 0.f) draw(l, id, total); });
+  if (u == 0.f)                                             // the first kept id with any mass, be it less than a weight can be
+    R.template locate<u64>(2, [&](const float (&l)[VEC], int i0, u64 (&v)[VEC]) {
+                             const double least = weigh.least((double)temp);
+#pragma unroll
+                             for (int e = 0; e < VEC; ++e) v[e] = (u64)(cut.keeps(l[e], i0 + e) && (double)l[e] >= least);
+                             return 0u;
+                           }, [](u64) { return 0ull; }, [&](float l, int id, u64) { draw(l, id, total); });
   if (rank == 0 && threadIdx.x == 0 && a.kept) {
     u64 all = 0;
-    for (int q = 0; q < a.cluster; ++q) all += sh.xch[7][q];
+    for (int q = 0; q < a.cluster; ++q) all += sh.xch[5][q];
     a.kept[row] = (int)all;
   }
 }
