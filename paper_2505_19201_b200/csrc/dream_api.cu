@@ -1604,6 +1604,7 @@ static bool pdl_on() {
 template <typename A>
 static const char *launch_rows(void (*kernel)(A), int rows, int cluster, int threads, size_t smem, cudaStream_t stream, const A &args) {
   cudaError_t e = smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+  if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)rows * (unsigned)cluster); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
@@ -1685,7 +1686,8 @@ static const char *sample_launch(SampleArgs a, int dtype, int rows, bool truncat
   // 64 KB of the row per CTA, two CTAs per SM, where a cluster of eight holds it so; more CTAs to a row where there are few rows
   const int esz = dtype == DREAM_BF16 ? 2 : 4;
   a.cluster = 1;
-  while (a.cluster < SAMPLE_MAX_CLUSTER && (a.vocab > a.cluster * (65536 / esz) || (rows * a.cluster < 148 && a.vocab > a.cluster * 4096))) a.cluster *= 2;
+  while (a.cluster < 8 && (a.vocab > a.cluster * (65536 / esz) || (rows * a.cluster < 148 && a.vocab > a.cluster * 4096))) a.cluster *= 2;
+  if (a.cluster == 8 && rows <= 9 && a.vocab > 8 * 8192) a.cluster = 16;
   const int share = (a.vocab + 16 / esz - 1 + a.cluster - 1) / a.cluster, line = dtype == DREAM_BF16 ? 256 : 128, warps = SAMPLE_THREADS / 32;
   a.warp_elems = ((share + warps - 1) / warps + line - 1) / line * line;
   a.frac_bits = imin(50, 62 - ilog2(a.vocab));

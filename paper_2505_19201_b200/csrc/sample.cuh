@@ -20,12 +20,11 @@
 #include "common.cuh"
 #include "rows.cuh"
 
-#define SAMPLE_MAX_CLUSTER 8
-#define SAMPLE_CTA_MAX 32768           // logits of a row one CTA holds (128 KB as fp32)
-#define SAMPLE_MAX_VOCAB (SAMPLE_MAX_CLUSTER * SAMPLE_CTA_MAX)
+#define SAMPLE_MAX_CLUSTER 16          // above 8 where rows are few: the kernel opts in
+#define SAMPLE_MAX_VOCAB 262144
 #define SAMPLE_BINS 2048
 #define SAMPLE_CHUNKS 32               // of SAMPLE_BINS / 32 bins, a lane each
-#define SAMPLE_EXCHANGES 11
+#define SAMPLE_EXCHANGES 12
 #define SAMPLE_LIST 512                // listed tokens one block settles
 #define SAMPLE_SMALL_K 256
 #define SAMPLE_THREADS 512
@@ -222,7 +221,7 @@ struct SampleRow {
   // One level of the selection.  walk(put) hands put(bin, term) the tokens, or one value a thread; of the bins, from the top, that one is
   // found in which the running count or mass reaches goal(total), and left in sh.bin .. sh.total.  enough: false, and nothing
   // found, where the goal is not below the total.  Bin 0 may hold most of a row, so it is added up in registers first.
-  template <int KIND, typename F, typename G> __device__ __forceinline__ bool level(bool first, bool enough, F walk, G goal) const {
+  template <int KIND, typename F, typename G> __device__ __forceinline__ bool level(bool first, bool enough, F walk, G goal, float slope = 0.f) const {
     constexpr bool MASS = KIND != COUNT, UNITS = KIND == UNITS_OF_MASS;
     if (!first) sync_all_of(a.cluster);                     // nobody still reads the bins of the level before
     for (int i = threadIdx.x; i < SAMPLE_BINS; i += blockDim.x) {
@@ -240,7 +239,7 @@ struct SampleRow {
       }
     };
     walk([&](int bin, u64 w) {
-      if (bin > 0) add(bin, KIND == NATS_OF_MASS ? (uint32_t)w : 1u, w);
+      if (bin > 0 && bin < SAMPLE_BINS) add(bin, KIND == NATS_OF_MASS ? (uint32_t)w : 1u, w);
       if (KIND != NATS_OF_MASS) n0 += bin == 0 ? 1u : 0u;
       if (UNITS) w0 += bin == 0 ? w : 0ull;
     });
@@ -255,7 +254,7 @@ struct SampleRow {
       uint32_t c = sh.cnt[i] + sh.cnt[i + 32];
       c = __reduce_add_sync(0xffffffffu, c);
       u64 w = 0;
-      if (MASS) w = warp_total<u64>(bin_mass<KIND>(i, sh.cnt[i], UNITS ? sh.lo[i] : 0u, UNITS ? sh.hi[i] : 0u) + bin_mass<KIND>(i + 32, sh.cnt[i + 32], UNITS ? sh.lo[i + 32] : 0u, UNITS ? sh.hi[i + 32] : 0u));
+      if (MASS) w = warp_total<u64>(bin_mass<KIND>(slope, i, sh.cnt[i], UNITS ? sh.lo[i] : 0u, UNITS ? sh.hi[i] : 0u) + bin_mass<KIND>(slope, i + 32, sh.cnt[i + 32], UNITS ? sh.lo[i + 32] : 0u, UNITS ? sh.hi[i + 32] : 0u));
       if (lane == 0) { sh.coarse_cnt[ch] = c; if (MASS) sh.coarse_mass[ch] = w; }
     }
     sync_all_of(a.cluster);
@@ -282,7 +281,7 @@ struct SampleRow {
             const int i = top - 2 * lane - k;
             const uint32_t n = ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
             c2[k] += n;
-            if (MASS) w2[k] += bin_mass<KIND>(i, n, UNITS ? ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)) : 0u,
+            if (MASS) w2[k] += bin_mass<KIND>(slope, i, n, UNITS ? ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)) : 0u,
                                               UNITS ? ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[i]), q)) : 0u);
           }
         const u64 sc = bc + warp_scan<u64>(c2[0] + c2[1]), sw = bw + (MASS ? warp_scan<u64>(w2[0] + w2[1]) : 0);
@@ -301,12 +300,12 @@ struct SampleRow {
     __syncthreads();
     return sh.bin >= 0;
   }
-  // UNITS_OF_MASS: exact, a 64-bit sum in two words.  NATS_OF_MASS: bin i is the i-th of 1 / 128 nat from the bottom of SAMPLE_BINS, n the sum of
-  // its weights relative to its upper edge's in 1 / 4096; mass in units of 2^-32, good to a few 1e-5.
+  // UNITS_OF_MASS: exact, a 64-bit sum in two words.  NATS_OF_MASS: n is the sum of a bin's weights in 2^-17 of the weight at its upper edge
+  // (slope 1: bins of 1 / 128 nat) or at that of all bins (0); mass in units of 2^-32 of the top bin's edge, good to a few 1e-6.
   enum { COUNT, UNITS_OF_MASS, NATS_OF_MASS };
-  template <int KIND> static __device__ __forceinline__ u64 bin_mass(int i, uint32_t n, uint32_t lo, uint32_t hi) {
+  template <int KIND> static __device__ __forceinline__ u64 bin_mass(float slope, int i, uint32_t n, uint32_t lo, uint32_t hi) {
     if (KIND == UNITS_OF_MASS) return (u64)lo + ((u64)hi << 32);
-    return (u64)((float)n * ex2((float)(i - (SAMPLE_BINS - 1)) * (1.44269504f / 128.f) + 20.f));
+    return (u64)((float)n * ex2((float)(i - (SAMPLE_BINS - 1)) * (slope * (1.44269504f / 128.f)) + 15.f));
   }
 
   // The first token in id order at which the running sum of vals exceeds goal(total): found(logit, id, total) runs in the one thread that
@@ -533,58 +532,83 @@ struct SampleRow {
     for (int q = 0; q < a.cluster; ++q) v += of_bits<double>(sh.xch[slot][q]);
     return v;
   }
-  // Many tokens, by count (top_k) or by mass (top_p) within the cut.  Bins of 1 / 128 nat below the row's maximum; what is 16 nats below or more
-  // is in bin 0.  By mass the bins are approximate and only say where to look: the mass in front of the bin's upper neighbour is then summed
-  // exactly, and the three bins are listed.
-  template <bool MASS> __device__ __forceinline__ Cut select(Cut cut, u64 top_k, double top_p, const Weigher &weigh, float m, float temp) const {
+  // Many tokens, by count (top_k) or by mass (top_p) within the cut.  Bins of 1 / 128 nat below the row's maximum, up to 16 nats; where the bin in
+  // which the cut falls holds too many to list, once more with bins a fraction as wide.  By mass the bins are approximate and only
+  // say where to look: the mass in front of the bin's upper neighbour is then summed exactly, and the three bins are listed.
+  // fresh: nobody has used the bins yet.
+  template <bool MASS> __device__ __forceinline__ Cut select(bool fresh, Cut cut, u64 top_k, double top_p, const Weigher &weigh, float m, float temp) const {
+    constexpr int LAST = SAMPLE_BINS - 1;
     const float scale = 128.f / temp;
-    auto depth = [&](float l) { return fminf((m - l) * scale, (float)(SAMPLE_BINS - 1)); };
-    auto nat_bin = [&](float l) { return (SAMPLE_BINS - 1) - (int)depth(l); };
+    float x0 = 0.f, fine = 1.f;                             // where the bins begin, and how many to 1 / 128 nat
+    auto depth = [&](float l) { return (m - l) * scale - x0; };
+    auto place = [&](float x) { return (int)floorf(fminf(x * fine, (float)LAST)); };       // NaN: the last
     double z = 0.0;
-    const bool found_bin = level<MASS ? NATS_OF_MASS : COUNT>(false, !MASS,
-          [&](auto put) {
-            if (!MASS) {
-              each([&](float l, int id) { if (cut.keeps(l, id)) put(nat_bin(l), 0ull); });
-              return;
-            }
-            double s = 0.0;
-            each_vec([&](const float (&l)[VEC], int i0) {
-              double w[VEC];
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) w[e] = weigh.exact(l[e]);
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) {
-                const bool on = cut.keeps(l[e], i0 + e);
-                s += on ? w[e] : 0.0;
-                const float x = depth(l[e]), below = floorf(x), y = (x - below) * (1.f / 128.f);
-                if (on && x < (float)(SAMPLE_BINS - 1)) put((SAMPLE_BINS - 1) - (int)below, (u64)(uint32_t)(4096.5f - 4096.f * (y - 0.5f * y * y)));
+    u64 left = top_k;
+    int at = 0;
+    if (!(scale < INFINITY)) return radix<MASS>(cut, top_k, top_p, weigh);      // everything in one place
+#pragma unroll 1
+    for (int lev = 0;; ++lev) {
+      const bool found_bin = level<MASS ? NATS_OF_MASS : COUNT>(fresh && lev == 0, !MASS && lev == 0,
+            [&](auto put) {
+              if (!MASS) {
+                each([&](float l, int id) {
+                  const int i = place(depth(l));
+                  if (cut.keeps(l, id) && i >= 0) put(LAST - i, 0ull);
+                });
+                return;
               }
-            });
-            push(8, block_sum(s));
-          },
-          [&](u64) {
-            if (!MASS) return top_k;
-            z = pushed(8);
-            return (u64)fmax(1.0, top_p * z * 4294967296.0);
-          });
-    if (!MASS && !found_bin && sh.bin == -1) return cut;    // no more tokens than top_k
-    z = MASS ? pushed(8) : 0.0;
-    const int bin = sh.bin;
-    const u64 left = MASS ? 0ull : top_k - sh.before_cnt;
-    // bin 0, or none, is for the radix selection; an infinite scale has everything there
-    if (!found_bin || bin == 0 || !(scale < INFINITY)) return radix<MASS>(cut, top_k, top_p, weigh);
-    __syncthreads();
+              double s = 0.0;                               // of the row; then of what lies in front of the finer bins
+              each_vec([&](const float (&l)[VEC], int i0) {
+                bool sum[VEC], any = false;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                  const bool on = cut.keeps(l[e], i0 + e);
+                  const float x = depth(l[e]);
+                  const int i = place(x);
+                  sum[e] = on && (lev == 0 || i < 0);
+                  any = any || sum[e];
+                  if (on && i >= 0 && i < LAST) {
+                    const float y = (lev ? x : x - (float)i) * (1.f / 128.f);
+                    put(LAST - i, (u64)(uint32_t)(131072.5f - 131072.f * y * (1.f - y * (0.5f - y * (1.f / 6.f)))));
+                  }
+                }
+                if (any) {
+#pragma unroll
+                  for (int e = 0; e < VEC; ++e) { const double w = weigh.exact(l[e]); s += sum[e] ? w : 0.0; }
+                }
+              });
+              push(lev ? 9 : 8, block_sum(s));
+            },
+            [&](u64) {
+              if (!MASS) return left;
+              z = pushed(8);
+              const double goal = lev ? (top_p * z - pushed(9)) * exp((double)x0 / 128.0) : top_p * z;
+              return (u64)fmin(fmax(1.0, goal * 4294967296.0), 9e18);
+            }, lev ? 0.f : 1.f);
+      if (!MASS && lev == 0 && !found_bin) return cut;      // no more tokens than top_k
+      if (MASS) z = pushed(8);
+      at = LAST - sh.bin;
+      const uint32_t n = MASS ? 3 * (sh.bin_cnt >> 17) : sh.bin_cnt;
+      if (!found_bin || at >= LAST) return radix<MASS>(cut, top_k, top_p, weigh);
+      if (!MASS) left -= sh.before_cnt;
+      __syncthreads();
+      if (lev || n <= SAMPLE_LIST - 100) break;
+      x0 = MASS ? fmaxf((float)(at - 1), 0.f) : (float)at;
+      fine = MASS ? (float)LAST / 3.f : (float)LAST;
+    }
+    // the mass in front of the list: after a second look only what lies between the finer bins' first and the list is new
+    const bool twice = x0 > 0.f || fine != 1.f;
     double s = 0.0;
     const uint32_t n = list(MASS ? 2 : 1, [&](float l, int id) {
           if (!cut.keeps(l, id)) return false;
-          const int b = nat_bin(l);
-          if (MASS && b > bin + 1) s += weigh.exact(l);
-          return MASS ? b >= bin - 1 && b <= bin + 1 : b == bin;
-        }, [&] { if (MASS) push(9, block_sum(s)); });
+          const int i = place(depth(l));
+          if (MASS && i < at - 1 && (!twice || i >= 0)) s += weigh.exact(l);
+          return MASS ? i >= at - 1 && i <= at + 1 : i == at;
+        }, [&] { if (MASS) push(11, block_sum(s)); });
     if (rank == 0) {
       bool good = n <= SAMPLE_LIST;
       if (good) {
-        const double rest = MASS ? top_p * z - pushed(9) : 0.0;            // of the listed tokens' mass
+        const double rest = MASS ? top_p * z - (twice ? pushed(9) + pushed(11) : pushed(11)) : 0.0;        // of the listed tokens' mass
         const u64 units = MASS ? (u64)fmax(0.0, ceil(rest * (4503599627370496.0 / weigh.unit))) : 0ull;
         const auto r = settle(n, MASS ? (u64)n : left, [&](u64 mass) {
             if (MASS && (rest <= 0.0 || units > mass)) sh.bin = -2;        // the bins were too coarse: the cut is not among them
@@ -636,6 +660,7 @@ k_sample(const __grid_constant__ SampleArgs a) {
   };
   if (m > -INFINITY) {
     float least_l = -INFINITY;
+    bool tried = false;                                     // the bins have been used
     if (min_p > 0.f) {                                      // w >= min_p
       if (min_p > 1.f) k = 1;                               // nothing but the first of the order
       else least_l = infinite ? m : fminf(__double2float_ru(weigh.m + log((double)min_p) * (double)temp), m);
@@ -647,6 +672,7 @@ k_sample(const __grid_constant__ SampleArgs a) {
       auto bin_of = [&](float l) { return l >= low ? (int)((l - low) * scale) : 0; };
       bool listed = false;
       if (k <= SAMPLE_SMALL_K && scale > 0.f && scale < INFINITY) {
+        tried = true;
         R.template level<SampleRow<T>::COUNT>(true, false, [&](auto put) { put(bin_of(own), 0ull); }, [&](u64) { return (u64)k; });
         const int bin = sh.bin;
         __syncthreads();
@@ -669,9 +695,12 @@ k_sample(const __grid_constant__ SampleArgs a) {
           top_p = 1.f; least_l = -INFINITY;                      // settled with the list
         }
       }
-      if (!listed) cut = R.template select<false>(cut, (u64)k, 0.0, weigh, m, temp);
+      if (!listed) {
+        cut = R.template select<false>(!tried, cut, (u64)k, 0.0, weigh, m, temp);
+        tried = true;
+      }
     }
-    if (top_p < 1.f) cut = R.template select<true>(cut, 0, fmax((double)top_p, 1e-30), weigh, m, temp);
+    if (top_p < 1.f) cut = R.template select<true>(!tried, cut, 0, fmax((double)top_p, 1e-30), weigh, m, temp);
     if (least_l > cut.l) cut = {least_l, 0x7fffffff};       // the largest logit passes it: a first one always stays
   }
   uint32_t n = 0;
@@ -734,9 +763,9 @@ k_sample(const __grid_constant__ SampleArgs a) {
       bool on[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) { on[e] = cut.keeps(l[e], i0 + e); v[e] = 0.0; n += on[e] ? 1u : 0u; }
-      if (n) {
+      if (n) {                                              // all of a vector: a branch per token would cost more
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) if (on[e]) v[e] = weigh.exact(l[e]);
+        for (int e = 0; e < VEC; ++e) { const double w = weigh.exact(l[e]); v[e] = on[e] ? w : 0.0; }
       }
     }
     return n;
