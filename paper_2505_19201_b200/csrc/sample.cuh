@@ -57,7 +57,7 @@ struct SampleShared {
   uint32_t warp_cnt[32];
   float2 warp_f[32];
   // what a selection level found
-  int bin;
+  int bin, chunk;
   uint32_t bin_cnt;
   u64 before_cnt, before_mass, total;
   // listed tokens (of the whole cluster, in its first CTA) and what they settle
@@ -65,9 +65,13 @@ struct SampleShared {
   float list_l[SAMPLE_LIST], cut_l;
   int list_id[SAMPLE_LIST], min_id;
   u64 list_w[SAMPLE_LIST];
-  double table[256];                   // of the weights (Weigher)
+  double table[32];                    // of the weights (Weigher)
+  double c2;                           // of the row
   int cut_id;
-  uint32_t cnt[SAMPLE_BINS], lo[SAMPLE_BINS], hi[SAMPLE_BINS];
+  alignas(16) uint32_t cnt[SAMPLE_BINS], lo[SAMPLE_BINS], hi[SAMPLE_BINS];
+  // where there are no exact masses, 64 words from every CTA are gathered in their place
+  __device__ uint32_t *part_cnt() { return lo; }
+  __device__ u64 *part_mass() { return reinterpret_cast<u64 *>(hi); }
 };
 
 // Sums and inclusive running sums over a warp, of u64 or double.
@@ -91,24 +95,25 @@ template <typename A> __device__ __forceinline__ A of_bits(u64 v);
 template <> __device__ __forceinline__ u64 of_bits<u64>(u64 v) { return v; }
 template <> __device__ __forceinline__ double of_bits<double>(u64 v) { return __longlong_as_double((long long)v); }
 
-// exp((l - m) / T), also as an integer of 2^-s.  2^y by table, as in Tang's table-driven exponential: y = n + j / 256 + r, |r| <= 1 / 512, and 2^r by the
-// Taylor series of e^(r ln 2) to its third power (remainder 1.4e-13).  Roundings to integers are additions of a number so large that its
-// last bit is the unit wanted.  Eight operations in double, where a series without a table takes fourteen.
-#define SAMPLE_TABLE 256
+// exp((l - m) / T), also as an integer of 2^-s.  2^y by table, as in Tang's table-driven exponential: y = n + j / 32 + r, |r| <= 1 / 64, and 2^r by the
+// Taylor series of e^(r ln 2) to its fourth power (remainder 1.3e-12).  Roundings to integers are additions of a number so large that its
+// last bit is the unit wanted.  Nine operations in double, where a series without a table takes fourteen.
+#define SAMPLE_TABLE 32
 struct Weigher {
   double m, c2, unit;                  // row maximum, log2(e) / T, 2^(52 - s)
   float cut;                           // below it a weight is less than half a unit
-  const double *table;                 // 2^(j / 256), in shared memory
+  const double *table;                 // 2^(j / 32), in shared memory
   __device__ __forceinline__ double raw(float l) const {
     const double d = (double)fminf(l, 3.402823466e38f) - m;
-    const double big = 6755399441055744.0 / SAMPLE_TABLE;       // 1.5 * 2^52 / 256: its last bit is 1 / 256
+    const double big = 6755399441055744.0 / SAMPLE_TABLE;       // 1.5 * 2^52 / 32: its last bit is 1 / 32
     const double t = fma(d, c2, big), r = fma(d, c2, -(t - big));
     const int n = __double2loint(t);
     const double e = table[n & (SAMPLE_TABLE - 1)];
-    double p = fma(r, 0.05550410866482158, 0.2402265069591007);  // ln(2)^k / k!, k = 3, 2, 1
+    double p = fma(r, 0.009618129107628477, 0.05550410866482158);          // ln(2)^k / k!, k = 4, 3, 2, 1
+    p = fma(p, r, 0.2402265069591007);
     p = fma(p, r, 0.6931471805599453);
     p = fma(e, p * r, e);
-    return __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
+    return __hiloint2double(__double2hiint(p) + ((n >> 5) << 20), __double2loint(p));
   }
   __device__ __forceinline__ double exact(float l) const { const double p = raw(l); return l >= cut ? p : 0.0; }
   __device__ __forceinline__ u64 units(float l) const {
@@ -258,43 +263,76 @@ struct SampleRow {
       if (lane == 0) { sh.coarse_cnt[ch] = c; if (MASS) sh.coarse_mass[ch] = w; }
     }
     sync_all_of(a.cluster);
+    // Every warp reads a CTA's chunks, then its bins of the chunk in question, and the first warp adds them up: read one after the other the
+    // round trips to the other CTAs took longer than all else.  (Exact masses, the rare case, have their own arrays in the way.)
+    if (!UNITS) {
+      for (int q = warp; q < a.cluster; q += nw) {
+        sh.part_cnt()[q * 64 + lane] = ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.coarse_cnt[SAMPLE_CHUNKS - 1 - lane]), q));
+        if (MASS) sh.part_mass()[q * 64 + lane] = ld_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.coarse_mass[SAMPLE_CHUNKS - 1 - lane]), q));
+      }
+      __syncthreads();
+    }
+    u64 bc = 0, bw = 0, want = 0, total = 0;
     if (warp == 0) {
       // lane 0 has the top chunk
       const int ch = SAMPLE_CHUNKS - 1 - lane;
       u64 c = 0, w = 0;
       for (int q = 0; q < a.cluster; ++q) {
-        c += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.coarse_cnt[ch]), q));
-        if (MASS) w += ld_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.coarse_mass[ch]), q));
+        if (UNITS) {
+          c += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.coarse_cnt[ch]), q));
+          w += ld_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.coarse_mass[ch]), q));
+        } else {
+          c += sh.part_cnt()[q * 64 + lane];
+          if (MASS) w += sh.part_mass()[q * 64 + lane];
+        }
       }
       const u64 ic = warp_scan<u64>(c), iw = MASS ? warp_scan<u64>(w) : 0;
-      const u64 total = __shfl_sync(0xffffffffu, MASS ? iw : ic, 31), want = goal(total);
+      total = __shfl_sync(0xffffffffu, MASS ? iw : ic, 31);
+      want = goal(total);
       const unsigned hit = __ballot_sync(0xffffffffu, (MASS ? iw : ic) >= want);
-      if (!hit || (enough && want >= total)) { if (lane == 0) sh.bin = -1; }
-      else {
-        const int at = __ffs(hit) - 1;                                   // the chunk
-        const u64 bc = __shfl_sync(0xffffffffu, ic - c, at), bw = __shfl_sync(0xffffffffu, iw - w, at);
-        const int top = (SAMPLE_CHUNKS - at) * (SAMPLE_BINS / SAMPLE_CHUNKS) - 1;
-        u64 c2[2] = {0, 0}, w2[2] = {0, 0};
-        for (int q = 0; q < a.cluster; ++q)
+      const int at = !hit || (enough && want >= total) ? -1 : __ffs(hit) - 1;            // the chunk
+      bc = __shfl_sync(0xffffffffu, ic - c, max(at, 0)); bw = __shfl_sync(0xffffffffu, iw - w, max(at, 0));
+      if (lane == 0) { sh.chunk = at; if (at < 0) sh.bin = -1; }
+    }
+    __syncthreads();
+    const int at = sh.chunk;
+    if (at < 0) return false;
+    const int top = (SAMPLE_CHUNKS - at) * (SAMPLE_BINS / SAMPLE_CHUNKS) - 1;            // bins descending from here, two to a lane
+    if (!UNITS) {
+      for (int q = warp; q < a.cluster; q += nw)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {                                  // lane's bins, descending: top - 2 lane, then the next
-            const int i = top - 2 * lane - k;
-            const uint32_t n = ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
-            c2[k] += n;
-            if (MASS) w2[k] += bin_mass<KIND>(slope, i, n, UNITS ? ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)) : 0u,
-                                              UNITS ? ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[i]), q)) : 0u);
-          }
-        const u64 sc = bc + warp_scan<u64>(c2[0] + c2[1]), sw = bw + (MASS ? warp_scan<u64>(w2[0] + w2[1]) : 0);
-        const unsigned h2 = __ballot_sync(0xffffffffu, (MASS ? sw : sc) >= want);
-        if (lane == __ffs(h2) - 1) {
-          const u64 c0 = sc - c2[0] - c2[1], w0 = sw - w2[0] - w2[1];
-          const int k = (MASS ? w0 + w2[0] : c0 + c2[0]) >= want ? 0 : 1;
-          sh.bin = top - 2 * lane - k;
-          sh.before_cnt = c0 + (k ? c2[0] : 0);
-          sh.before_mass = w0 + (k ? w2[0] : 0);
-          sh.bin_cnt = (uint32_t)c2[k];
-          sh.total = total;
+        for (int k = 0; k < 2; ++k) {
+          const int i = top - 2 * lane - k;
+          const uint32_t n = ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
+          sh.part_cnt()[q * 64 + 2 * lane + k] = n;
+          if (MASS) sh.part_mass()[q * 64 + 2 * lane + k] = bin_mass<KIND>(slope, i, n, 0u, 0u);
         }
+      __syncthreads();
+    }
+    if (warp == 0) {
+      u64 c2[2] = {0, 0}, w2[2] = {0, 0};
+      for (int q = 0; q < a.cluster; ++q)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int i = top - 2 * lane - k;
+          if (UNITS) {
+            c2[k] += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
+            w2[k] += bin_mass<KIND>(slope, i, 0u, ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)), ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[i]), q)));
+          } else {
+            c2[k] += sh.part_cnt()[q * 64 + 2 * lane + k];
+            if (MASS) w2[k] += sh.part_mass()[q * 64 + 2 * lane + k];
+          }
+        }
+      const u64 sc = bc + warp_scan<u64>(c2[0] + c2[1]), sw = bw + (MASS ? warp_scan<u64>(w2[0] + w2[1]) : 0);
+      const unsigned h2 = __ballot_sync(0xffffffffu, (MASS ? sw : sc) >= want);
+      if (lane == __ffs(h2) - 1) {
+        const u64 c0 = sc - c2[0] - c2[1], w0 = sw - w2[0] - w2[1];
+        const int k = (MASS ? w0 + w2[0] : c0 + c2[0]) >= want ? 0 : 1;
+        sh.bin = top - 2 * lane - k;
+        sh.before_cnt = c0 + (k ? c2[0] : 0);
+        sh.before_mass = w0 + (k ? w2[0] : 0);
+        sh.bin_cnt = (uint32_t)c2[k];
+        sh.total = total;
       }
     }
     __syncthreads();
@@ -643,14 +681,16 @@ k_sample(const __grid_constant__ SampleArgs a) {
   float top_p = a.top_p ? a.top_p[row] : a.p0;
   const float min_p = a.min_p ? a.min_p[row] : a.m0, u = TRUNCATE ? 0.f : fmaxf(a.uniforms[row], 0.f);
   if (!(temp > 0.f)) { temp = 1.f; k = 1; }                 // greedy
-  if (threadIdx.x < SAMPLE_TABLE) sh.table[threadIdx.x] = exp2((double)threadIdx.x / SAMPLE_TABLE);
+  // what takes many instructions is one warp's
+  if (warp == 0) sh.table[threadIdx.x] = exp2((double)threadIdx.x / SAMPLE_TABLE);
+  else if (warp == 1) { const double c2 = 1.4426950408889634 / (double)temp; if (threadIdx.x == 32) sh.c2 = c2; }
   float own, m, lowest;
   R.load(row, own, m, lowest);
   Cut cut = {-INFINITY, (int)0x80000000};                   // every token above -inf
   Weigher weigh;
   const bool infinite = m == INFINITY;                      // the infinite ones share the mass
   weigh.table = sh.table;
-  weigh.m = (double)m; weigh.c2 = 1.4426950408889634 / (double)temp; weigh.unit = __longlong_as_double((long long)(1023 + 52 - a.frac_bits) << 52);
+  weigh.m = (double)m; weigh.c2 = sh.c2; weigh.unit = __longlong_as_double((long long)(1023 + 52 - a.frac_bits) << 52);
   weigh.cut = fmaxf(__double2float_rd(weigh.m - (double)(a.frac_bits + 2) * 0.69314718055994531 * (double)temp), -3.402823466e38f);
   if (infinite) { weigh.m = (double)3.402823466e38f; weigh.cut = INFINITY; }
   auto target = [&](u64 total) { const u64 t = (u64)((double)u * (double)total); return t < total ? t : total - 1; };
