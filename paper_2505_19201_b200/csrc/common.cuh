@@ -324,3 +324,14 @@ __device__ __forceinline__ float block_sum(float v, float *sh /* >= 33 floats */
 __device__ __forceinline__ bool better(float va, int ia, float vb, int ib) {
   return va > vb || (va == vb && ia < ib);
 }
+
+// The largest of a vector's elements (NaN does not count).
+template <typename T, int VEC> __device__ __forceinline__ float max_vec(const uint4 &q) {
+  if constexpr (sizeof(T) == 4)
+    return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+  else {
+    const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&q);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+}

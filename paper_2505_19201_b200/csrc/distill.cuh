@@ -81,16 +81,6 @@ __device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
   return pair_of(r);
 }
-// The largest of a vector's elements (NaN does not count).
-template <typename T, int VEC> __device__ __forceinline__ float max_vec(const uint4 &q) {
-  if constexpr (sizeof(T) == 4)
-    return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
-  else {
-    const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&q);
-    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-    return fmaxf(__low2float(m), __high2float(m));
-  }
-}
 __device__ __forceinline__ double warp_sum_d(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -52,14 +52,13 @@ struct SampleArgs {
 struct SampleShared {
   u64 xch[SAMPLE_EXCHANGES][SAMPLE_MAX_CLUSTER];   // one 64-bit word from every CTA of the cluster
   u64 warp_tot[32];
-  u64 coarse_mass[SAMPLE_CHUNKS];
-  uint32_t coarse_cnt[SAMPLE_CHUNKS];
+  u64 coarse[SAMPLE_CHUNKS];
   uint32_t warp_cnt[32];
   float2 warp_f[32];
   // what a selection level found
   int bin, chunk;
   uint32_t bin_cnt;
-  u64 before_cnt, before_mass, total;
+  u64 before, total;
   // listed tokens (of the whole cluster, in its first CTA) and what they settle
   uint32_t list_n[3];                  // a counter for each list a row may need
   float list_l[SAMPLE_LIST], cut_l;
@@ -68,10 +67,8 @@ struct SampleShared {
   double table[32];                    // of the weights (Weigher)
   double c2;                           // of the row
   int cut_id;
-  alignas(16) uint32_t cnt[SAMPLE_BINS], lo[SAMPLE_BINS], hi[SAMPLE_BINS];
-  // where there are no exact masses, 64 words from every CTA are gathered in their place
-  __device__ uint32_t *part_cnt() { return lo; }
-  __device__ u64 *part_mass() { return reinterpret_cast<u64 *>(hi); }
+  uint32_t cnt[SAMPLE_BINS], lo[SAMPLE_BINS], hi[SAMPLE_BINS];
+  __device__ uint32_t *part() { return lo; }       // 64 words from every CTA, where there are no exact masses
 };
 
 // Sums and inclusive running sums over a warp, of u64 or double.
@@ -148,26 +145,23 @@ struct SampleRow {
       for (int i = 0; i < 4; ++i) { l[2 * i] = __uint_as_float(u[i] << 16); l[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
     }
   }
-  // f(logit, id) for the thread's logits, ascending ids inside a thread
-  template <typename F> __device__ __forceinline__ void each(F f) const {
-    const uint4 *p = vals + (size_t)warp * steps * 32 + lane;
-#pragma unroll 1
-    for (int j = 0; j < steps; ++j) {
-      float l[VEC];
-      unpack(p[j * 32], l);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) f(l[e], base + (j * 32 + lane) * VEC + e);
-    }
-  }
   // f(logits, id of the first) for the thread's vectors
   template <typename F> __device__ __forceinline__ void each_vec(F f) const {
     const uint4 *p = vals + (size_t)warp * steps * 32 + lane;
+    int i0 = base + lane * VEC;
 #pragma unroll 1
-    for (int j = 0; j < steps; ++j) {
+    for (int j = 0; j < steps; ++j, p += 32, i0 += 32 * VEC) {
       float l[VEC];
-      unpack(p[j * 32], l);
-      f(l, base + (j * 32 + lane) * VEC);
+      unpack(*p, l);
+      f(l, i0);
     }
+  }
+  // f(logit, id) for the thread's logits, ascending ids inside a thread
+  template <typename F> __device__ __forceinline__ void each(F f) const {
+    each_vec([&](const float (&l)[VEC], int i0) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f(l[e], i0 + e);
+    });
   }
   // One word from every CTA to every CTA; ends in a barrier of the cluster.
   __device__ __forceinline__ void exchange(int slot, u64 v) const {
@@ -179,32 +173,35 @@ struct SampleRow {
   // largest and the smallest of those that are not -inf.
   __device__ __forceinline__ void load(int row, float &own, float &most, float &least) const {
     const T *src = (const T *)a.logits + row * a.ld;
-    const T neg = from_f<T>(-INFINITY);
     uint4 *p = vals + (size_t)warp * steps * 32 + lane;
     float m = -INFINITY;
+    const int first = base + lane * VEC;
     constexpr int U = 8;
-    for (int j0 = 0; j0 < steps; j0 += U) {
-      uint4 q[U];
+    int j = 0;
+    if (base >= 0) {                                        // whole vectors, as many at once as there are
+      const uint4 *s = reinterpret_cast<const uint4 *>(src + first);
+      const int whole = max(0, min(steps, (a.vocab - base) / (32 * VEC)));
+      for (; j + U <= whole; j += U) {
+        uint4 q[U];
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int i = base + ((j0 + k) * 32 + lane) * VEC;
-        if (j0 + k < steps && i >= 0 && i + VEC <= a.vocab) q[k] = *reinterpret_cast<const uint4 *>(src + i);
-        else {
-          T t[VEC];
+        for (int k = 0; k < U; ++k) q[k] = s[(j + k) * 32];
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) t[e] = j0 + k < steps && i + e >= 0 && i + e < a.vocab ? src[i + e] : neg;
-          memcpy(&q[k], t, 16);
-        }
+        for (int k = 0; k < U; ++k) { m = fmaxf(m, max_vec<T, VEC>(q[k])); p[(j + k) * 32] = q[k]; }
       }
+    }
+#pragma unroll 2
+    for (; j < steps; ++j) {
+      const int i = first + j * 32 * VEC;
+      uint4 q;
+      if (i >= 0 && i + VEC <= a.vocab) q = *reinterpret_cast<const uint4 *>(src + i);
+      else {
+        T t[VEC];
 #pragma unroll
-      for (int k = 0; k < U; ++k)
-        if (j0 + k < steps) {
-          float l[VEC];
-          unpack(q[k], l);
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) m = fmaxf(m, l[e]);
-          p[(j0 + k) * 32] = q[k];
-        }
+        for (int e = 0; e < VEC; ++e) t[e] = i + e >= 0 && i + e < a.vocab ? src[i + e] : from_f<T>(-INFINITY);
+        memcpy(&q, t, 16);
+      }
+      m = fmaxf(m, max_vec<T, VEC>(q));
+      p[j * 32] = q;
     }
     own = m;
     most = warp_max(m);
@@ -217,133 +214,122 @@ struct SampleRow {
     most = warp_max(w.x);
     least = -warp_max(-w.y);
     exchange(0, (u64)__float_as_uint(most) | (u64)__float_as_uint(least) << 32);
-    for (int q = 0; q < a.cluster; ++q) {
-      most = fmaxf(most, __uint_as_float((uint32_t)sh.xch[0][q]));
-      least = fminf(least, __uint_as_float((uint32_t)(sh.xch[0][q] >> 32)));
-    }
+    const u64 x = sh.xch[0][min(lane, a.cluster - 1)];
+    most = warp_max(__uint_as_float((uint32_t)x));
+    least = -warp_max(-__uint_as_float((uint32_t)(x >> 32)));
   }
 
   // One level of the selection.  walk(put) hands put(bin, term) the tokens, or one value a thread; of the bins, from the top, that one is
-  // found in which the running count or mass reaches goal(total), and left in sh.bin .. sh.total.  enough: false, and nothing
-  // found, where the goal is not below the total.  Bin 0 may hold most of a row, so it is added up in registers first.
+  // found in which the running sum reaches goal(total), and left in sh.bin, with what is in front of it and how much of cnt it holds.  enough: false,
+  // and nothing found, where the goal is not below the total.  Bin 0 may hold most of a row, so it is added up in registers first.
+  //   COUNT: tokens.  UNITS: exact mass, a 64-bit sum in two words.  NATS: approximate mass; a bin holds weights in 2^-17 of the weight at its upper
+  //   edge (slope 1: bins of 1 / 128 nat) or at that of the top bin (0), good to a few 1e-6 of a bin.
+  enum { COUNT, UNITS, NATS };
+  template <int KIND> __device__ __forceinline__ auto bin_sum(float slope, int i, uint32_t n, uint32_t lo, uint32_t hi) const {
+    if constexpr (KIND == COUNT) return n;
+    else if constexpr (KIND == UNITS) return (u64)lo + ((u64)hi << 32);
+    else return (float)n * ex2((float)(i - (SAMPLE_BINS - 1)) * (slope * (1.44269504f / 128.f)) - 17.f);
+  }
   template <int KIND, typename F, typename G> __device__ __forceinline__ bool level(bool first, bool enough, F walk, G goal, float slope = 0.f) const {
-    constexpr bool MASS = KIND != COUNT, UNITS = KIND == UNITS_OF_MASS;
+    constexpr bool EXACT = KIND == UNITS;
+    typedef decltype(bin_sum<KIND>(0.f, 0, 0u, 0u, 0u)) A;
     if (!first) sync_all_of(a.cluster);                     // nobody still reads the bins of the level before
-    for (int i = threadIdx.x; i < SAMPLE_BINS; i += blockDim.x) {
+    for (int i = threadIdx.x; i < SAMPLE_BINS; i += SAMPLE_THREADS) {
       sh.cnt[i] = 0;
-      if (UNITS) { sh.lo[i] = 0; sh.hi[i] = 0; }
+      if (EXACT) { sh.lo[i] = 0; sh.hi[i] = 0; }
     }
     __syncthreads();
     uint32_t n0 = 0;
     u64 w0 = 0;
     auto add = [&](int bin, uint32_t n, u64 w) {
       atomicAdd(&sh.cnt[bin], n);
-      if (UNITS && w) {
+      if (EXACT && w) {
         const uint32_t low = (uint32_t)w, old = atomicAdd(&sh.lo[bin], low), up = (uint32_t)(w >> 32) + (old + low < old ? 1u : 0u);
         if (up) atomicAdd(&sh.hi[bin], up);
       }
     };
     walk([&](int bin, u64 w) {
-      if (bin > 0 && bin < SAMPLE_BINS) add(bin, KIND == NATS_OF_MASS ? (uint32_t)w : 1u, w);
-      if (KIND != NATS_OF_MASS) n0 += bin == 0 ? 1u : 0u;
-      if (UNITS) w0 += bin == 0 ? w : 0ull;
+      if (bin > 0 && bin < SAMPLE_BINS) add(bin, KIND == NATS ? (uint32_t)w : 1u, w);
+      if (KIND != NATS) n0 += bin == 0 ? 1u : 0u;
+      if (EXACT) w0 += bin == 0 ? w : 0ull;
     });
-    if (KIND != NATS_OF_MASS) {
+    if (KIND != NATS) {
       n0 = __reduce_add_sync(0xffffffffu, n0);
-      if (UNITS) w0 = warp_total<u64>(w0);
+      if (EXACT) w0 = warp_total<u64>(w0);
       if (lane == 0 && n0) add(0, n0, w0);
     }
     __syncthreads();
+    A *coarse = reinterpret_cast<A *>(sh.coarse);
     for (int ch = warp; ch < SAMPLE_CHUNKS; ch += nw) {
-      const int i = ch * (SAMPLE_BINS / SAMPLE_CHUNKS) + lane;
-      uint32_t c = sh.cnt[i] + sh.cnt[i + 32];
-      c = __reduce_add_sync(0xffffffffu, c);
-      u64 w = 0;
-      if (MASS) w = warp_total<u64>(bin_mass<KIND>(slope, i, sh.cnt[i], UNITS ? sh.lo[i] : 0u, UNITS ? sh.hi[i] : 0u) + bin_mass<KIND>(slope, i + 32, sh.cnt[i + 32], UNITS ? sh.lo[i + 32] : 0u, UNITS ? sh.hi[i + 32] : 0u));
-      if (lane == 0) { sh.coarse_cnt[ch] = c; if (MASS) sh.coarse_mass[ch] = w; }
+      const int i = ch * 64 + lane;
+      A w = bin_sum<KIND>(slope, i, sh.cnt[i], EXACT ? sh.lo[i] : 0u, EXACT ? sh.hi[i] : 0u) + bin_sum<KIND>(slope, i + 32, sh.cnt[i + 32], EXACT ? sh.lo[i + 32] : 0u, EXACT ? sh.hi[i + 32] : 0u);
+      if constexpr (KIND == COUNT) w = __reduce_add_sync(0xffffffffu, w);
+      else w = warp_total<A>(w);
+      if (lane == 0) coarse[ch] = w;
     }
     sync_all_of(a.cluster);
-    // Every warp reads a CTA's chunks, then its bins of the chunk in question, and the first warp adds them up: read one after the other the
-    // round trips to the other CTAs took longer than all else.  (Exact masses, the rare case, have their own arrays in the way.)
-    if (!UNITS) {
-      for (int q = warp; q < a.cluster; q += nw) {
-        sh.part_cnt()[q * 64 + lane] = ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.coarse_cnt[SAMPLE_CHUNKS - 1 - lane]), q));
-        if (MASS) sh.part_mass()[q * 64 + lane] = ld_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.coarse_mass[SAMPLE_CHUNKS - 1 - lane]), q));
-      }
+    // Each warp reads a CTA's chunks, then its bins of the chunk in question, and the first warp adds them up: read one after the other the
+    // round trips to the other CTAs took longer than all else.  (Exact masses, the rare case, are in the way and are read one by one.)
+    auto of_chunk = [&](int q) -> A {                       // lane 0 has the top chunk
+      const uint32_t from = mapa_of(a.cluster, smem_u32(coarse + SAMPLE_CHUNKS - 1 - lane), q);
+      if constexpr (EXACT) return (A)ld_cluster_u64(from);
+      else if constexpr (KIND == NATS) return ld_cluster(from);
+      else return (A)ld_cluster_u32(from);
+    };
+    if constexpr (!EXACT) {
+      for (int q = warp; q < a.cluster; q += nw) reinterpret_cast<A *>(sh.part())[q * 64 + lane] = of_chunk(q);
       __syncthreads();
     }
-    u64 bc = 0, bw = 0, want = 0, total = 0;
+    A before = 0, want = 0;
     if (warp == 0) {
-      // lane 0 has the top chunk
-      const int ch = SAMPLE_CHUNKS - 1 - lane;
-      u64 c = 0, w = 0;
+      A c = 0;
       for (int q = 0; q < a.cluster; ++q) {
-        if (UNITS) {
-          c += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.coarse_cnt[ch]), q));
-          w += ld_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.coarse_mass[ch]), q));
-        } else {
-          c += sh.part_cnt()[q * 64 + lane];
-          if (MASS) w += sh.part_mass()[q * 64 + lane];
-        }
+        if constexpr (EXACT) c += of_chunk(q);
+        else c += reinterpret_cast<A *>(sh.part())[q * 64 + lane];
       }
-      const u64 ic = warp_scan<u64>(c), iw = MASS ? warp_scan<u64>(w) : 0;
-      total = __shfl_sync(0xffffffffu, MASS ? iw : ic, 31);
+      const A run = warp_scan<A>(c), total = __shfl_sync(0xffffffffu, run, 31);
       want = goal(total);
-      const unsigned hit = __ballot_sync(0xffffffffu, (MASS ? iw : ic) >= want);
-      const int at = !hit || (enough && want >= total) ? -1 : __ffs(hit) - 1;            // the chunk
-      bc = __shfl_sync(0xffffffffu, ic - c, max(at, 0)); bw = __shfl_sync(0xffffffffu, iw - w, max(at, 0));
-      if (lane == 0) { sh.chunk = at; if (at < 0) sh.bin = -1; }
+      const unsigned hit = __ballot_sync(0xffffffffu, run >= want);
+      const int at = !hit || (enough && want >= total) ? -1 : __ffs(hit) - 1;
+      before = __shfl_sync(0xffffffffu, run - c, max(at, 0));
+      if (lane == 0) { sh.chunk = at; if (at < 0) sh.bin = -1; if (KIND != NATS) sh.total = (u64)total; }
     }
     __syncthreads();
     const int at = sh.chunk;
     if (at < 0) return false;
-    const int top = (SAMPLE_CHUNKS - at) * (SAMPLE_BINS / SAMPLE_CHUNKS) - 1;            // bins descending from here, two to a lane
-    if (!UNITS) {
+    const int top = (SAMPLE_CHUNKS - at) * 64 - 1;          // bins descending from here, two to a lane
+    if (!EXACT) {
       for (int q = warp; q < a.cluster; q += nw)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int i = top - 2 * lane - k;
-          const uint32_t n = ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
-          sh.part_cnt()[q * 64 + 2 * lane + k] = n;
-          if (MASS) sh.part_mass()[q * 64 + 2 * lane + k] = bin_mass<KIND>(slope, i, n, 0u, 0u);
-        }
+        for (int k = 0; k < 2; ++k) sh.part()[q * 64 + 2 * lane + k] = ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[top - 2 * lane - k]), q));
       __syncthreads();
     }
     if (warp == 0) {
-      u64 c2[2] = {0, 0}, w2[2] = {0, 0};
+      A w[2] = {0, 0};
+      uint32_t n[2] = {0, 0};
       for (int q = 0; q < a.cluster; ++q)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const int i = top - 2 * lane - k;
-          if (UNITS) {
-            c2[k] += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
-            w2[k] += bin_mass<KIND>(slope, i, 0u, ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)), ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[i]), q)));
-          } else {
-            c2[k] += sh.part_cnt()[q * 64 + 2 * lane + k];
-            if (MASS) w2[k] += sh.part_mass()[q * 64 + 2 * lane + k];
-          }
+          if constexpr (EXACT) {
+            n[k] += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.cnt[i]), q));
+            w[k] += ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.lo[i]), q)) + ((u64)ld_cluster_u32(mapa_of(a.cluster, smem_u32(&sh.hi[i]), q)) << 32);
+          } else n[k] += sh.part()[q * 64 + 2 * lane + k];
         }
-      const u64 sc = bc + warp_scan<u64>(c2[0] + c2[1]), sw = bw + (MASS ? warp_scan<u64>(w2[0] + w2[1]) : 0);
-      const unsigned h2 = __ballot_sync(0xffffffffu, (MASS ? sw : sc) >= want);
-      if (lane == __ffs(h2) - 1) {
-        const u64 c0 = sc - c2[0] - c2[1], w0 = sw - w2[0] - w2[1];
-        const int k = (MASS ? w0 + w2[0] : c0 + c2[0]) >= want ? 0 : 1;
+      if (!EXACT) for (int k = 0; k < 2; ++k) w[k] = bin_sum<KIND>(slope, top - 2 * lane - k, n[k], 0u, 0u);
+      const A run = before + warp_scan<A>(w[0] + w[1]);
+      const unsigned hit = __ballot_sync(0xffffffffu, run >= want);
+      // a sum in float may fall a rounding short of its chunk's: the chunk's last bin then
+      if (lane == (hit ? __ffs(hit) - 1 : 31)) {
+        const A front = run - w[0] - w[1];
+        const int k = front + w[0] >= want ? 0 : 1;
         sh.bin = top - 2 * lane - k;
-        sh.before_cnt = c0 + (k ? c2[0] : 0);
-        sh.before_mass = w0 + (k ? w2[0] : 0);
-        sh.bin_cnt = (uint32_t)c2[k];
-        sh.total = total;
+        if (KIND != NATS) sh.before = (u64)(front + (k ? w[0] : (A)0));
+        sh.bin_cnt = n[k];
       }
     }
     __syncthreads();
     return sh.bin >= 0;
-  }
-  // UNITS_OF_MASS: exact, a 64-bit sum in two words.  NATS_OF_MASS: n is the sum of a bin's weights in 2^-17 of the weight at its upper edge
-  // (slope 1: bins of 1 / 128 nat) or at that of all bins (0); mass in units of 2^-32 of the top bin's edge, good to a few 1e-6.
-  enum { COUNT, UNITS_OF_MASS, NATS_OF_MASS };
-  template <int KIND> static __device__ __forceinline__ u64 bin_mass(float slope, int i, uint32_t n, uint32_t lo, uint32_t hi) {
-    if (KIND == UNITS_OF_MASS) return (u64)lo + ((u64)hi << 32);
-    return (u64)((float)n * ex2((float)(i - (SAMPLE_BINS - 1)) * (slope * (1.44269504f / 128.f)) + 15.f));
   }
 
   // The first token in id order at which the running sum of vals exceeds goal(total): found(logit, id, total) runs in the one thread that
@@ -440,7 +426,7 @@ struct SampleRow {
     for (int lev = 0; lev < 3; ++lev) {
       const int shift = lev == 0 ? 21 : lev == 1 ? 10 : 0, width = lev == 2 ? 1023 : 2047;
       const uint32_t above = lev == 0 ? 0u : lev == 1 ? 0xffe00000u : 0xfffffc00u;
-      if (!level<MASS ? UNITS_OF_MASS : COUNT>(false, !MASS && lev == 0,
+      if (!level<MASS ? UNITS : COUNT>(false, !MASS && lev == 0,
           [&](auto put) {
             each([&](float l, int id) {
               const uint32_t k = topk_key(l);
@@ -448,10 +434,10 @@ struct SampleRow {
               put((int)((k >> shift) & width), MASS ? weigh.units(l) : 0ull);
             });
           },
-          [&](u64 total) { return MASS && lev == 0 ? mass_goal(top_p, total) : goal; }))
+          [&](auto total) { return (decltype(total))(MASS && lev == 0 ? mass_goal(top_p, (u64)total) : goal); }))
         return cut;                                         // fewer tokens than top_k
       if (MASS && lev == 0) goal = mass_goal(top_p, sh.total);
-      goal -= MASS ? sh.before_mass : sh.before_cnt;
+      goal -= sh.before;
       prefix |= (uint32_t)sh.bin << shift;
       ties = sh.bin_cnt;
       __syncthreads();
@@ -586,7 +572,7 @@ struct SampleRow {
     if (!(scale < INFINITY)) return radix<MASS>(cut, top_k, top_p, weigh);      // everything in one place
 #pragma unroll 1
     for (int lev = 0;; ++lev) {
-      const bool found_bin = level<MASS ? NATS_OF_MASS : COUNT>(fresh && lev == 0, !MASS && lev == 0,
+      const bool found_bin = level<MASS ? NATS : COUNT>(fresh && lev == 0, !MASS && lev == 0,
             [&](auto put) {
               if (!MASS) {
                 each([&](float l, int id) {
@@ -617,18 +603,18 @@ struct SampleRow {
               });
               push(lev ? 9 : 8, block_sum(s));
             },
-            [&](u64) {
-              if (!MASS) return left;
+            [&](auto total) {
+              typedef decltype(total) A;
+              if (!MASS) return (A)left;
               z = pushed(8);
-              const double goal = lev ? (top_p * z - pushed(9)) * exp((double)x0 / 128.0) : top_p * z;
-              return (u64)fmin(fmax(1.0, goal * 4294967296.0), 9e18);
+              return (A)fmax(1e-30, lev ? (top_p * z - pushed(9)) * exp((double)x0 / 128.0) : top_p * z);
             }, lev ? 0.f : 1.f);
       if (!MASS && lev == 0 && !found_bin) return cut;      // no more tokens than top_k
       if (MASS) z = pushed(8);
       at = LAST - sh.bin;
       const uint32_t n = MASS ? 3 * (sh.bin_cnt >> 17) : sh.bin_cnt;
       if (!found_bin || at >= LAST) return radix<MASS>(cut, top_k, top_p, weigh);
-      if (!MASS) left -= sh.before_cnt;
+      if (!MASS) left -= sh.before;
       __syncthreads();
       if (lev || n <= SAMPLE_LIST - 100) break;
       x0 = MASS ? fmaxf((float)(at - 1), 0.f) : (float)at;
@@ -713,7 +699,7 @@ k_sample(const __grid_constant__ SampleArgs a) {
       bool listed = false;
       if (k <= SAMPLE_SMALL_K && scale > 0.f && scale < INFINITY) {
         tried = true;
-        R.template level<SampleRow<T>::COUNT>(true, false, [&](auto put) { put(bin_of(own), 0ull); }, [&](u64) { return (u64)k; });
+        R.template level<SampleRow<T>::COUNT>(true, false, [&](auto put) { put(bin_of(own), 0ull); }, [&](uint32_t) { return (uint32_t)k; });
         const int bin = sh.bin;
         __syncthreads();
         uint32_t n = SAMPLE_LIST + 1;
@@ -793,13 +779,15 @@ k_sample(const __grid_constant__ SampleArgs a) {
     }
     return;
   }
-  const bool whole = cut.l == -INFINITY;                    // nothing is cut: no comparison and no branch among the weights
+  auto whole = [&](const float (&l)[VEC], int, double (&v)[VEC]) {         // nothing is cut: no comparison and no branch among the weights
+    uint32_t n = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) { v[e] = weigh.exact(l[e]); n += l[e] > -INFINITY ? 1u : 0u; }
+    return n;
+  };
   auto weights = [&](const float (&l)[VEC], int i0, double (&v)[VEC]) {
     uint32_t n = 0;
-    if (whole) {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) { v[e] = weigh.exact(l[e]); n += l[e] > -INFINITY ? 1u : 0u; }
-    } else {
+    {
       bool on[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) { on[e] = cut.keeps(l[e], i0 + e); v[e] = 0.0; n += on[e] ? 1u : 0u; }
@@ -810,8 +798,9 @@ k_sample(const __grid_constant__ SampleArgs a) {
     }
     return n;
   };
-  const double total = R.template locate<double>(4, weights, [&](double total) { return fmin((double)u * total, total * 0.9999999999999999); },
-                                                 [&](float l, int id, double total) { if (u > 0.f) draw(l, id, total); });
+  auto goal = [&](double total) { return fmin((double)u * total, total * 0.9999999999999999); };
+  auto found = [&](float l, int id, double total) { if (u > 0.f) draw(l, id, total); };
+  const double total = cut.l == -INFINITY ? R.template locate<double>(4, whole, goal, found) : R.template locate<double>(4, weights, goal, found);
   if (u == 0.f)                                             // the first kept id with any mass, be it less than a weight can be
     R.template locate<u64>(2, [&](const float (&l)[VEC], int i0, u64 (&v)[VEC]) {
                              const double least = weigh.least((double)temp);
