@@ -166,38 +166,49 @@ def _bad(msg):
 
 
 def _rows(name, t, like=None):
-    """A matrix of logits: float32 or bfloat16, two dimensions, rows of consecutive elements on a CUDA device."""
-    if t.dtype not in _ROW_TYPES or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        _bad(f"{name} must be float32 or bfloat16 [rows, vocab] with consecutive elements in a row")
-    if not t.is_cuda:
+    """A matrix of logits: float32 or bfloat16, two dimensions, rows of consecutive elements on a CUDA device.  Returns its address, rows,
+    row length, elements from row to row, type and device ordinal."""
+    kind, shape = _ROW_TYPES.get(t.dtype), t.shape
+    if kind is None or len(shape) != 2:
+        _bad(f"{name} must be float32 or bfloat16 [rows, vocab]")
+    dev, (ld, step), (R, V) = t.get_device(), t.stride(), shape
+    if dev < 0:
         _bad(f"{name} must be a CUDA tensor")
-    if like is not None and (t.dtype != like.dtype or t.shape != like.shape or t.device != like.device):
-        _bad(f"{name} must be {like.dtype} of shape {tuple(like.shape)} on {like.device}")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if step != 1 and V > 1:
+        _bad(f"{name} must have consecutive elements in a row")
+    if like is not None and (kind, (R, V), dev) != like:
+        _bad(f"{name} must have the type, shape and device of logits")
+    return t.data_ptr(), R, V, ld if R > 1 else V, kind, dev
 
 
-def _side(name, t, dtype, shape, device, optional=True):
-    """The address of a contiguous tensor that goes with the rows, or None."""
+def _side(name, t, dtype, shape, dev):
+    """The address of a contiguous tensor that goes with the rows; None stays None.  (These few lines run up to nine times a call, and a call for
+    one row is over on the GPU in about ten microseconds.)"""
     if t is None:
-        if not optional:
-            _bad(f"{name} is required")
         return None
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
-        _bad(f"{name} must be contiguous {dtype} of shape {tuple(shape)} on {device}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _bad(f"{name} must be contiguous {dtype} of shape {tuple(shape)} on cuda:{dev}")
     return t.data_ptr()
 
 
-def _call_rows(fn, device, stream, *args):
+def _need(name, t):
+    if t is None:
+        _bad(f"{name} is required")
+
+
+def _call_rows(fn, dev, stream, *args):
     """Call an entry point on rows of logits with its tensors' device current, on `stream` or that device's current stream."""
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif stream.device != device:
-        _bad(f"the stream belongs to {stream.device}, the tensors to {device}")
-    if torch.cuda.current_device() == device.index:
-        code = fn(*args, stream.cuda_stream)
+        raw = torch._C._cuda_getCurrentRawStream(dev)
+    elif stream.device_index != dev:
+        _bad(f"the stream belongs to cuda:{stream.device_index}, the tensors to cuda:{dev}")
     else:
-        with torch.cuda.device(device):
-            code = fn(*args, stream.cuda_stream)
+        raw = stream.cuda_stream
+    if torch._C._cuda_getDevice() == dev:
+        code = fn(*args, raw)
+    else:
+        with torch.cuda.device(dev):
+            code = fn(*args, raw)
     if code != 0:
         _check(None, code)
 
@@ -207,22 +218,22 @@ def dream_sample(logits, uniforms, tokens, temperature=None, top_k=None, top_p=N
     """A token per row of `logits` [rows, vocab] (float32 or bfloat16; rows may be strided) under temperature, top-k, top-p and
     min-p by row (CUDA tensors [rows]; None: not used) and one uniform number per row.  Outputs are the caller's tensors: tokens
     [rows] int32, logprob [rows] float32, kept [rows] int32."""
-    p, ld = _rows("logits", logits)
-    R, V = logits.shape
-    dev, n, f32, i32 = logits.device, (R,), torch.float32, torch.int32
-    _call_rows(lib().dream_sample, dev, stream, p, _ROW_TYPES[logits.dtype], R, V, ld,
+    p, R, V, ld, kind, dev = _rows("logits", logits)
+    _need("uniforms", uniforms)
+    _need("tokens", tokens)
+    n, f32, i32 = (R,), torch.float32, torch.int32
+    _call_rows(lib().dream_sample, dev, stream, p, kind, R, V, ld,
                _side("temperature", temperature, f32, n, dev), _side("top_k", top_k, i32, n, dev), _side("top_p", top_p, f32, n, dev),
-               _side("min_p", min_p, f32, n, dev), _side("uniforms", uniforms, f32, n, dev, False),
-               _side("tokens", tokens, i32, n, dev, False), _side("logprob", logprob, f32, n, dev), _side("kept", kept, i32, n, dev))
+               _side("min_p", min_p, f32, n, dev), _side("uniforms", uniforms, f32, n, dev), _side("tokens", tokens, i32, n, dev),
+               _side("logprob", logprob, f32, n, dev), _side("kept", kept, i32, n, dev))
 
 
 def dream_truncate_logits(logits, out, temperature=None, top_k=None, top_p=None, min_p=None, kept=None, stream=None):
     """out = logits where a token is kept under the settings of dream_sample, -inf elsewhere; `out` may be `logits`."""
-    p, ld = _rows("logits", logits)
-    q, out_ld = _rows("out", out, logits)
-    R, V = logits.shape
-    dev, n, f32, i32 = logits.device, (R,), torch.float32, torch.int32
-    _call_rows(lib().dream_truncate_logits, dev, stream, p, _ROW_TYPES[logits.dtype], R, V, ld,
+    p, R, V, ld, kind, dev = _rows("logits", logits)
+    q, _, _, out_ld, _, _ = _rows("out", out, (kind, (R, V), dev))
+    n, f32, i32 = (R,), torch.float32, torch.int32
+    _call_rows(lib().dream_truncate_logits, dev, stream, p, kind, R, V, ld,
                _side("temperature", temperature, f32, n, dev), _side("top_k", top_k, i32, n, dev), _side("top_p", top_p, f32, n, dev),
                _side("min_p", min_p, f32, n, dev), q, out_ld, _side("kept", kept, i32, n, dev))
 
@@ -232,30 +243,27 @@ def dream_distill_loss(logits, teacher_ids, teacher_logits, loss, lse, teacher_l
     """Distillation loss per row of a student's `logits` [rows, vocab] against a teacher's top logits (teacher_ids int32 and
     teacher_logits float32, both [rows, K], K <= 128; with teacher_lse [rows] the rest of the vocabulary counts as one bucket and
     log_rest [rows] is an output).  Writes loss and lse [rows] and, if given, grad [rows, vocab] = row_scale * d loss / d logits."""
-    p, ld = _rows("logits", logits)
-    R, V = logits.shape
-    dev, n, f32 = logits.device, (R,), torch.float32
-    g, grad_ld = (None, 0) if grad is None else _rows("grad", grad, logits)
-    nk = (R, teacher_ids.shape[-1])
-    _call_rows(lib().dream_distill_loss, dev, stream, p, _ROW_TYPES[logits.dtype], R, V, ld,
+    p, R, V, ld, kind, dev = _rows("logits", logits)
+    g, grad_ld = None, 0
+    if grad is not None:
+        g, _, _, grad_ld, _, _ = _rows("grad", grad, (kind, (R, V), dev))
+    n, f32, nk = (R,), torch.float32, (R, teacher_ids.shape[-1])
+    _call_rows(lib().dream_distill_loss, dev, stream, p, kind, R, V, ld,
                _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), nk[1],
-               _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("loss", loss, f32, n, dev, False),
-               _side("lse", lse, f32, n, dev, False), _side("log_rest", log_rest, f32, n, dev),
-               _side("row_scale", row_scale, f32, n, dev), g, grad_ld)
+               _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("loss", loss, f32, n, dev), _side("lse", lse, f32, n, dev),
+               _side("log_rest", log_rest, f32, n, dev), _side("row_scale", row_scale, f32, n, dev), g, grad_ld)
 
 
 def dream_distill_grad(logits, teacher_ids, teacher_logits, lse, grad, teacher_lse=None, log_rest=None, temperature=1.0,
                        row_scale=None, stream=None):
     """The backward pass of dream_distill_loss on its own: grad = row_scale * d loss / d logits from the saved lse (and log_rest).
     `grad` may be `logits`."""
-    p, ld = _rows("logits", logits)
-    g, grad_ld = _rows("grad", grad, logits)
-    R, V = logits.shape
-    dev, n, f32 = logits.device, (R,), torch.float32
-    nk = (R, teacher_ids.shape[-1])
-    _call_rows(lib().dream_distill_grad, dev, stream, p, _ROW_TYPES[logits.dtype], R, V, ld,
+    p, R, V, ld, kind, dev = _rows("logits", logits)
+    g, _, _, grad_ld, _, _ = _rows("grad", grad, (kind, (R, V), dev))
+    n, f32, nk = (R,), torch.float32, (R, teacher_ids.shape[-1])
+    _call_rows(lib().dream_distill_grad, dev, stream, p, kind, R, V, ld,
                _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), nk[1],
-               _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("lse", lse, f32, n, dev, False),
+               _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("lse", lse, f32, n, dev),
                _side("log_rest", log_rest, f32, n, dev), _side("row_scale", row_scale, f32, n, dev), g, grad_ld)
 
 

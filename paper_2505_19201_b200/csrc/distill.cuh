@@ -415,7 +415,7 @@ struct DistillBlock {
     d.qz = qz == 0.0 ? 0.0 : qz * f;
     d.top_m = tm; d.tops = ts;
 #pragma unroll
-    for (int i = 0; i < E; ++i) n.q[i] = (float)(e[i] * f);
+    for (int i = 0; i < E; ++i) n.q[i] = (float)(e[i] * f);     // in single precision: doubles for two rows spill (8 % of a step)
     if (twice) {
 #pragma unroll
       for (int i = 0; i < E; ++i) sh.q[lane + 32 * i] = n.q[i];
@@ -491,11 +491,11 @@ struct DistillBlock {
       if (GRAD) {
         if (i_row) write_listed(row - clusters, id, g_top);
         const Slope g = slope(i_row, rs);
-        const float q = sh.side[i_row & 3].total;
+        const double q = (double)sh.side[i_row & 3].total, scale = (double)rs * a.inv_tau;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           id[i] = n.first[i] ? n.id[i] : -1;
-          g_top[i] = g.scale == 0.f ? 0.f : g.scale * fmaf(q, ex2(fmaf(n.z[i] - g.ref, ch, -g.d)), -n.q[i]);
+          g_top[i] = g.scale == 0.f ? 0.f : (float)(scale * (q * (double)ex2(fmaf(n.z[i] - g.ref, ch, -g.d)) - (double)n.q[i]));
         }
       }
       finish(row, i_row);

@@ -1600,11 +1600,29 @@ static bool pdl_on() {
   return on;
 }
 
+// A kernel may use all of a block's shared memory, and clusters above eight, from now on: asked for once per device by a thread that calls again
+// and again, and always for the same, so that threads do not take it from each other.
+#define MAX_BLOCK_SHARED (227 * 1024)
+template <typename A>
+static cudaError_t allow(void (*kernel)(A), int cluster, size_t smem) {
+  struct Allowed { const void *kernel; int device; };
+  static thread_local Allowed allowed[16];
+  static thread_local int next = 0;
+  if (smem <= 48 * 1024 && cluster <= 8) return cudaSuccess;
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  for (const Allowed &k : allowed) if (k.kernel == (const void *)kernel && k.device == device) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_BLOCK_SHARED);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) { allowed[next] = {(const void *)kernel, device}; next = (next + 1) % 16; }
+  return e;
+}
+
 // Launch of `rows` clusters on a caller's stream, of the current device.  Returns null or what went wrong.
 template <typename A>
 static const char *launch_rows(void (*kernel)(A), int rows, int cluster, int threads, size_t smem, cudaStream_t stream, const A &args) {
-  cudaError_t e = smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
-  if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  cudaError_t e = allow(kernel, cluster, smem);
   if (e == cudaSuccess) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)rows * (unsigned)cluster); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
@@ -1641,7 +1659,7 @@ static int resident_clusters(void (*kernel)(A), int cluster, int threads, size_t
   for (const Known &k : known)
     if (k.kernel == (const void *)kernel && k.device == device && k.cluster == cluster && k.threads == threads && k.smem == smem) return k.n;
   int n = 0, sms = 0, per = 0;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = allow(kernel, cluster, smem);
   if (cluster > 1) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)cluster * 1024); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
