@@ -165,13 +165,15 @@ __device__ __forceinline__ TeacherRow teacher_row(const DistillArgs &a, const Te
 // A CTA's part in the row's sums, which are of 2^((l - m) ch), ch = log2(e) / tau.  (l ch - m ch in one instruction would overflow on rows
 // masked with the type's lowest value.)
 struct DistillPart {
-  float m, unused;                     // largest logit, -inf without one
-  double others, tops, qz;             // sums over the ids that are not listed, that are; sum of q_j z_j tau
+  float m, top_m;                      // largest logit that is not listed, that is; -inf without one
+  double others, tops, qz;             // sums relative to these; sum of q_j z_j tau
 };
 // What the side warp knows of a row before its sums.
 struct DistillSide {
-  float total, rest, top_m, tops;      // Q; q_r; largest listed logit of this share and the listed ids' sum relative to it
+  float total, rest, top_m;            // Q; q_r; largest listed logit of this share
+  double tops;                         // the listed ids' sum relative to it, in double: see sums()
   double qz, entropy;                  // sum of q_j z_j tau in this share; sum of q ln q, the bucket's too
+  double listed, left;                 // sum of q_j, and q_r: in the loss they multiply logarithms that all but cancel
 };
 template <int SW> struct DistillShared {
   DistillPart part[2][DISTILL_MAX_CLUSTER];
@@ -231,15 +233,19 @@ template <typename T> __device__ __forceinline__ void store_vec(T *p, bool vec, 
 #pragma unroll
   for (int e = 0; e < VEC; ++e) p[e] = t[e];
 }
-// The gradient coef * 2^((l - ref) ch - d) of the thread's vectors, get(k) being the k-th's logits, and of its single id's logit le.  Nothing is
-// got where it is zero.
+// The gradient coef * 2^((l - ref) log2(e) / tau - d) of the thread's vectors, get(k) being the k-th's logits, and of its single id's logit le.
+// Nothing is got where it is zero.  In fp32 the factor is two floats: what one is off by, 3e-8 of an exponent of 13, is the same for most of
+// a row of 8192.  The first is rounded down, so that both are above 0 and a logit of -inf gives -inf.
 template <typename T, typename F>
-__device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool zero, F get, float le, float ref, float ch, float d, float coef) {
+__device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool zero, F get, float le, float ref, double factor, float d, float coef) {
   constexpr int VEC = 16 / sizeof(T), NT = DISTILL_THREADS;
-  const float2 r2 = make_float2(-ref, -ref), c2 = make_float2(ch, ch), d2 = make_float2(-d, -d), o2 = make_float2(coef, coef);
+  constexpr bool FULL = sizeof(T) == 4;
+  const float ch = FULL ? __double2float_rz(factor * (1.0 - 0x1p-25)) : (float)factor, cl = (float)(factor - (double)ch);
+  const float2 r2 = make_float2(-ref, -ref), c2 = make_float2(ch, ch), cl2 = make_float2(cl, cl), d2 = make_float2(-d, -d),
+               o2 = make_float2(coef, coef);
   T *p = dst + sr.id0 + threadIdx.x * VEC;
   const bool vec = ((uintptr_t)p & 15) == 0;
-  if (sr.edge >= 0) dst[sr.edge] = from_f<T>(zero ? 0.f : coef * ex2(fmaf(le - ref, ch, -d)));
+  if (sr.edge >= 0) dst[sr.edge] = from_f<T>(zero ? 0.f : coef * ex2(fmaf(le - ref, ch, FULL ? fmaf(le - ref, cl, -d) : -d)));
   for (int k = 0, g = threadIdx.x; g < sr.nv; ++k, g += NT, p += NT * VEC) {
     uint4 q = make_uint4(0u, 0u, 0u, 0u);
     if (!zero) {
@@ -247,7 +253,7 @@ __device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool ze
       unpack_vec<T, VEC>(get(k), l);
 #pragma unroll
       for (int e = 0; e < VEC; e += 2) {
-        const float2 y = fma_pair(add_pair(make_float2(l[e], l[e + 1]), r2), c2, d2);
+        const float2 x = add_pair(make_float2(l[e], l[e + 1]), r2), y = fma_pair(x, c2, FULL ? fma_pair(x, cl2, d2) : d2);
         const float2 o = mul_pair(make_float2(ex2(y.x), ex2(y.y)), o2);
         l[e] = o.x; l[e + 1] = o.y;
       }
@@ -274,56 +280,70 @@ struct DistillBlock {
   DistillShared<SW> &sh;
   uint8_t *flags;                      // [2][distill_flag_bytes(cta_vecs)]
   int rank, first_row, clusters;
+  // log2(e) / tau as a float, and 1 / tau as that float has it: the student's temperature in all of a row, off by up to 6e-8.  With q being
+  // exact that changes the loss by 6e-8 of sum (q - p) z / tau; were tau itself taken in parts of it, by 6e-8 of sum p z / tau.
   float ch;
+  double inv_tau;
   __device__ __forceinline__ uint8_t *flags_of(int p) const { return flags + p * distill_flag_bytes(a.cta_vecs, NT); }
   __device__ __forceinline__ RowShare<T> share(int row) const { return RowShare<T>(a.logits, a.ld, row, a.vocab, rank, a.cluster, a.cta_vecs); }
   __device__ __forceinline__ int edge_byte() const { return distill_flag_bytes(a.cta_vecs, NT) - 16; }
-  // The largest logit and the sums of row i of the block, by a whole warp: of this CTA's warps (own), or of the cluster.
-  template <typename R> __device__ __forceinline__ void sums(int i, bool own, float &rm, R &others, R &tops, double *qz) const {
+  // The largest logit and the sums of row i of the block, by a whole warp.  The exponentials of the others are all off in one direction by some
+  // 1e-7.  Where the listed ids' sum is exact, such an error e changes the loss by e times the difference of the teacher's and the student's
+  // share of the listed ids; with the same error there it would change it by e times the share itself, which in rows that nearly agree
+  // is much of the loss.  So with R = double, for the loss, the listed ids are summed and scaled by exp in double.
+  template <typename R> __device__ __forceinline__ R listed_sum(float m, double s, float rm) const {
+    if (s == 0.0) return 0;
+    if constexpr (sizeof(R) == 8) return s * exp(((double)m - (double)rm) * inv_tau);
+    else return (float)s * ex2((m - rm) * ch);
+  }
+  __device__ __forceinline__ void own_pairs(int i, float &m, double &others) const {
     const int lane = threadIdx.x & 31;
-    const bool tail = a.teacher_lse != nullptr;
-    float m = -INFINITY;
-    R o = 0, t = 0;
-    if (own || a.cluster == 1) {
-      float v = 0.f;
-      if (lane < SW) { m = sh.pair[i & 1][lane].x; v = sh.pair[i & 1][lane].y; }
-      else if (lane == SW) { m = sh.side[i & 3].top_m; v = tail ? sh.side[i & 3].tops : 0.f; }   // without the bucket they are among the others
-      rm = warp_max(m);
-      v = m > -INFINITY ? v * ex2((m - rm) * ch) : v;
-      if (lane < SW) o = v; else t = v;
+    const float2 p = lane < SW ? sh.pair[i & 1][lane] : make_float2(-INFINITY, 0.f);
+    m = warp_max(p.x);
+    others = warp_sum_d((double)(p.x > -INFINITY ? p.y * ex2((p.x - m) * ch) : p.y));
+  }
+  template <typename R> __device__ __forceinline__ void sums(int i, float &rm, R &others, R &tops, double *qz) const {
+    const int lane = threadIdx.x & 31;
+    const bool tail = a.teacher_lse != nullptr;             // without the bucket the listed ids are among the others
+    R o = 0;
+    tops = 0;
+    if (a.cluster == 1) {
+      const float2 p = lane < SW ? sh.pair[i & 1][lane] : make_float2(-INFINITY, 0.f);
+      const float tm = sh.side[i & 3].top_m;
+      rm = fmaxf(warp_max(p.x), tm);
+      o = p.x > -INFINITY ? p.y * ex2((p.x - rm) * ch) : p.y;
+      if (tail) tops = listed_sum<R>(tm, sh.side[i & 3].tops, rm);
       if (qz) *qz = sh.side[i & 3].qz;
     } else {
-      double z = 0.0;
-      if (lane < a.cluster) { const DistillPart &x = sh.part[i & 1][lane]; m = x.m; o = (R)x.others; t = (R)x.tops; z = x.qz; }
-      rm = warp_max(m);
-      const float f = m > -INFINITY ? ex2((m - rm) * ch) : 1.f;
-      o *= f; t *= f;
+      float m = -INFINITY, tm = -INFINITY;
+      double t = 0.0, z = 0.0;
+      if (lane < a.cluster) { const DistillPart &x = sh.part[i & 1][lane]; m = x.m; tm = x.top_m; o = (R)x.others; t = x.tops; z = x.qz; }
+      rm = warp_max(fmaxf(m, tm));
+      if (m > -INFINITY) o *= ex2((m - rm) * ch);
+      if (tail) {
+        tops = listed_sum<R>(tm, t, rm);
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) tops += __shfl_xor_sync(0xffffffffu, tops, x);
+      }
       if (qz) *qz = warp_sum_d(z);
     }
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) o += __shfl_xor_sync(0xffffffffu, o, x);
     others = o;
-    tops = 0;
-    if (tail) {
-      if (own || a.cluster == 1) tops = __shfl_sync(0xffffffffu, t, SW);
-      else {
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
-        tops = t;
-      }
-    }
   }
   // What the gradient of a row needs.
-  struct Slope { float ref, d, scale, coef; };
+  struct Slope { float ref, scale, coef; double total; };          // coef: of 2^((l - ref) ch)
   __device__ __forceinline__ Slope slope(int i, float rs) const {
     Slope g;
     float rm, others, tops;
-    sums(i, false, rm, others, tops, nullptr);
-    const float total = others + tops, q = sh.side[i & 3].total, rest = sh.side[i & 3].rest;
+    sums(i, rm, others, tops, nullptr);
+    const float total = others + tops, q = sh.side[i & 3].total, rest = sh.side[i & 3].rest, listed = (float)sh.side[i & 3].listed;
     g.ref = rm > -INFINITY ? rm : 0.f;
-    g.d = __log2f(total);
+    g.total = (double)total;
     g.scale = total == 0.f || q == 0.f ? 0.f : rs * (float)a.inv_tau;         // 0: padding, or nothing to learn from
-    g.coef = g.scale * (q - (rest > 0.f && others > 0.f ? rest * __fdividef(total, others) : 0.f));
+    // Q - q_r / p_r, without the 1 that both begin with
+    g.coef = g.scale * (rest > 0.f && others > 0.f ? listed - rest * (tops / others) : q) / total;
+    if (g.scale == 0.f) g.coef = 0.f;
     return g;
   }
 
@@ -380,7 +400,8 @@ struct DistillBlock {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) ref = fmax(ref, __shfl_xor_sync(0xffffffffu, ref, o));
     }
-    float tm = -INFINITY, ts = 0.f;
+    float tm = -INFINITY;
+    double ts = 0.0;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       e[i] = 0.0;
@@ -396,22 +417,24 @@ struct DistillBlock {
     }
     tm = warp_max(tm);
 #pragma unroll
-    for (int i = 0; i < E; ++i) if (n.first[i]) ts += ex2((n.z[i] - (tm > -INFINITY ? tm : 0.f)) * ch);
-    ts = warp_sum(ts); s = warp_sum_d(s); l = warp_sum_d(l); qz = warp_sum_d(qz);
+    for (int i = 0; i < E; ++i)
+      if (i * 32 < a.top && a.teacher_lse && n.first[i] && n.z[i] != -INFINITY) ts += exp(((double)n.z[i] - (double)tm) * inv_tau);
+    ts = warp_sum_d(ts); s = warp_sum_d(s); l = warp_sum_d(l); qz = warp_sum_d(qz);
     const bool any = !(s == 0.0);                           // a row with no valid entry has no loss, with or without the rest
     DistillSide d;
-    double f = 1.0;
+    double f = 1.0, rest = 0.0;
     if (a.teacher_lse) {
-      const double rest = any ? fmax(0.0, 1.0 - s) : 0.0;
-      d.rest = (float)rest;
+      rest = any ? fmax(0.0, 1.0 - s) : 0.0;
       d.total = any ? (float)(s + rest) : 0.f;
       d.entropy = l + (rest > 0.0 ? rest * log(rest) : 0.0);
     } else {
       f = any ? 1.0 / s : 0.0;
-      d.rest = 0.f;
       d.total = any ? 1.f : 0.f;
       d.entropy = any ? l * f - (ref + log(s)) : 0.0;
     }
+    d.rest = (float)rest;
+    d.left = rest;
+    d.listed = any ? s * f : 0.0;
     d.qz = qz == 0.0 ? 0.0 : qz * f;
     d.top_m = tm; d.tops = ts;
 #pragma unroll
@@ -435,14 +458,15 @@ struct DistillBlock {
     if (rank) return;
     float rm;
     double others, tops, qz = 0.0;
-    sums(i, false, rm, others, tops, &qz);
+    sums(i, rm, others, tops, &qz);
+    others *= 1.0 + 5.1e-8;                                 // ex2.approx is that much below 2^x in the mean, measured over -28 < x < 0
     const DistillSide &d = sh.side[i & 3];
-    const double total = others + tops, lse = (double)rm * a.inv_tau + log(total);
+    const double total = others + tops, lse = (double)rm * inv_tau + log(total);
     const bool none = total == 0.0;                         // no finite logit
-    double loss = d.entropy - qz * a.inv_tau + ((double)d.total - (double)d.rest) * lse, log_rest = 0.0;
+    double loss = d.entropy - qz * inv_tau + d.listed * lse, log_rest = 0.0;
     if (a.teacher_lse) {
       log_rest = others > 0.0 ? -log1p(tops / others) : others == 0.0 ? -INFINITY : others;
-      if (d.rest > 0.f) loss -= (double)d.rest * log_rest;
+      if (d.left > 0.0) loss -= d.left * log_rest;
     }
     if ((threadIdx.x & 31) == 0) {
       if (a.teacher_lse) a.log_rest[row] = none ? -INFINITY : (float)log_rest;
@@ -474,14 +498,14 @@ struct DistillBlock {
       block_barrier<THREADS>();
       if (a.cluster > 1) {
         const int lane = threadIdx.x & 31;
-        float rm;
-        double others, tops;
-        sums(i_row, true, rm, others, tops, nullptr);
+        float m;
+        double others;
+        own_pairs(i_row, m, others);
         if (lane < a.cluster) {
           const uint32_t to = mapa(smem_u32(&sh.part[i_row & 1][rank]), lane);
-          st_cluster_u64(to, (unsigned long long)__float_as_uint(rm));
+          st_cluster_u64(to, (unsigned long long)__float_as_uint(m) | (unsigned long long)__float_as_uint(sh.side[i_row & 3].top_m) << 32);
           st_cluster_u64(to + 8, __double_as_longlong(others));
-          st_cluster_u64(to + 16, __double_as_longlong(tops));
+          st_cluster_u64(to + 16, __double_as_longlong(sh.side[i_row & 3].tops));
           st_cluster_u64(to + 24, __double_as_longlong(sh.side[i_row & 3].qz));
         }
         cluster_sync_all();
@@ -495,7 +519,8 @@ struct DistillBlock {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           id[i] = n.first[i] ? n.id[i] : -1;
-          g_top[i] = g.scale == 0.f ? 0.f : (float)(scale * (q * (double)ex2(fmaf(n.z[i] - g.ref, ch, -g.d)) - (double)n.q[i]));
+          g_top[i] = 0.f;
+          if (i * 32 < a.top && g.scale != 0.f) g_top[i] = (float)(scale * (q * exp(((double)n.z[i] - (double)g.ref) * inv_tau) / g.total - (double)n.q[i]));
         }
       }
       finish(row, i_row);
@@ -568,7 +593,7 @@ struct DistillBlock {
     }
   }
   __device__ __forceinline__ void write_turn(const uint4 *ring, int left, T *out, bool vec, const Slope &g) const {
-    const float2 r2 = make_float2(-g.ref, -g.ref), c2 = make_float2(ch, ch), d2 = make_float2(-g.d, -g.d), o2 = make_float2(g.coef, g.coef);
+    const float2 r2 = make_float2(-g.ref, -g.ref), c2 = make_float2(ch, ch), o2 = make_float2(g.coef, g.coef);
     uint4 q[B];
     take(ring, left, q);
 #pragma unroll
@@ -577,7 +602,7 @@ struct DistillBlock {
       unpack_vec<T, VEC>(q[k], l);
 #pragma unroll
       for (int e = 0; e < VEC; e += 2) {
-        const float2 y = fma_pair(add_pair(make_float2(l[e], l[e + 1]), r2), c2, d2);
+        const float2 y = mul_pair(add_pair(make_float2(l[e], l[e + 1]), r2), c2);
         const float2 o = mul_pair(make_float2(ex2(y.x), ex2(y.y)), o2);
         l[e] = o.x; l[e + 1] = o.y;
       }
@@ -643,7 +668,7 @@ struct DistillBlock {
         const bool vec = ((uintptr_t)out & 15) == 0;
         const int from_left = more ? next.nv - tid : 0;
         left = sr.nv - tid;
-        if (sr.edge >= 0) dst[sr.edge] = from_f<T>(g.scale == 0.f ? 0.f : g.coef * ex2(fmaf(le_now - g.ref, ch, -g.d)));
+        if (sr.edge >= 0) dst[sr.edge] = from_f<T>(g.scale == 0.f ? 0.f : g.coef * ex2((le_now - g.ref) * ch));
 #pragma unroll 1
         for (int t = 0; t < TURNS; ++t) {
           const int here = left - t * B * NT;
@@ -673,7 +698,7 @@ k_distill(const __grid_constant__ DistillArgs a) {
   cluster_started_arrive(a.cluster);
   kernel_entry(TR_k_distill);
   const DistillBlock<T, GRAD, SW> blk = {a, sh, flags, a.cluster > 1 ? (int)cluster_ctarank() : 0, (int)blockIdx.x / a.cluster, (int)gridDim.x / a.cluster,
-                                         (float)(a.inv_tau * 1.4426950408889634)};
+                                         (float)(a.inv_tau * 1.4426950408889634), (double)(float)(a.inv_tau * 1.4426950408889634) * 0.6931471805599453};
   if (threadIdx.x >= SW * 32) blk.side_warp();
   else blk.stream_warp(reinterpret_cast<uint4 *>(flags + 2 * distill_flag_bytes(a.cta_vecs, SW * 32)) + threadIdx.x);
 }
@@ -696,7 +721,7 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   const float rs = a.row_scale ? a.row_scale[row] : 1.f;
   auto none = [](int) { return make_uint4(0u, 0u, 0u, 0u); };
   if (rs == 0.f || a.lse[row] == -INFINITY) {               // a row of padding is not read
-    write_row<T>(sr, dst, true, none, 0.f, 0.f, 0.f, 0.f, 0.f);
+    write_row<T>(sr, dst, true, none, 0.f, 0.f, 0.0, 0.f, 0.f);
     return;
   }
   auto fetch = [&](int k) {
@@ -717,7 +742,7 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   const double scale = tr.total == 0.0 ? 0.0 : (double)rs * a.inv_tau;
   const double tail = tr.rest > 0.0 ? tr.rest * exp(-(double)a.log_rest[row]) : 0.0;
   // logits relative to tau lse, so that the difference that the exponential sees is small where p is not
-  const float ch = (float)(a.inv_tau * 1.4426950408889634), ref = (float)(lse / a.inv_tau),
+  const float ref = (float)(lse / a.inv_tau),
               d = (float)((lse - (double)ref * a.inv_tau) * 1.4426950408889634), coef = (float)(scale * (tr.total - tail));
   const bool mine = sr.template flag_bit<NT>(t.id, blockIdx.x - row * a.cluster, a.cluster, 0) >= 0 && scale != 0.0;
   float g_top = 0.f;
@@ -734,7 +759,7 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
     const uint4 q = vals[k % DISTILL_GRAD_RING * NT];
     fetch(k + DISTILL_GRAD_RING);
     return q;
-  }, le, ref, ch, d, coef);
+  }, le, ref, a.inv_tau * 1.4426950408889634, d, coef);
   cp_async_wait<0>();
   __syncthreads();
   if (mine) dst[t.id] = from_f<T>(g_top);
