@@ -201,9 +201,9 @@ template <typename T> struct RowShare {
   static constexpr int VEC = 16 / sizeof(T);
   const T *row, *mine;                 // the row; the thread's first vector
   int id0, nv, edge;                   // id of the share's first whole vector, how many there are, the thread's single id or -1
-  __device__ __forceinline__ RowShare(const void *p, long long ld, int r, int vocab, int rank, int cluster, int cta_vecs) {
+  __device__ __forceinline__ RowShare(const void *p, long long ld, int r, int vocab, int rank, int cluster, int cta_vecs, int tid) {
     row = (const T *)p + r * ld;
-    const int tid = threadIdx.x, head = min(vocab, (VEC - (int)((uintptr_t)row / sizeof(T) % VEC)) % VEC), all = (vocab - head) / VEC,
+    const int head = min(vocab, (VEC - (int)((uintptr_t)row / sizeof(T) % VEC)) % VEC), all = (vocab - head) / VEC,
               rest = vocab - head - all * VEC, v0 = min(all, rank * cta_vecs);
     id0 = head + v0 * VEC;
     nv = min(cta_vecs, all - v0);
@@ -285,71 +285,79 @@ struct DistillBlock {
   float ch;
   double inv_tau;
   __device__ __forceinline__ uint8_t *flags_of(int p) const { return flags + p * distill_flag_bytes(a.cta_vecs, NT); }
-  __device__ __forceinline__ RowShare<T> share(int row) const { return RowShare<T>(a.logits, a.ld, row, a.vocab, rank, a.cluster, a.cta_vecs); }
+  __device__ __forceinline__ RowShare<T> share(int row) const { return RowShare<T>(a.logits, a.ld, row, a.vocab, rank, a.cluster, a.cta_vecs, (int)threadIdx.x - 32); }
   __device__ __forceinline__ int edge_byte() const { return distill_flag_bytes(a.cta_vecs, NT) - 16; }
-  // The largest logit and the sums of row i of the block, by a whole warp.  The exponentials of the others are all off in one direction by some
-  // 1e-7.  Where the listed ids' sum is exact, such an error e changes the loss by e times the difference of the teacher's and the student's
-  // share of the listed ids; with the same error there it would change it by e times the share itself, which in rows that nearly agree
-  // is much of the loss.  So with R = double, for the loss, the listed ids are summed and scaled by exp in double.
-  template <typename R> __device__ __forceinline__ R listed_sum(float m, double s, float rm) const {
-    if (s == 0.0) return 0;
-    if constexpr (sizeof(R) == 8) return s * exp(((double)m - (double)rm) * inv_tau);
-    else return (float)s * ex2((m - rm) * ch);
-  }
+  // The sums of row i of the block, by a whole warp: of the others relative to their largest logit m, with the bucket of the listed ids relative
+  // to theirs (without it the listed ids are among the others, and tops is 0).  Each keeps its own reference: between the two may lie more
+  // than a float's range, at a low temperature in any row.
+  // The exponentials of the others are all off in one direction by some 1e-7.  Where the listed ids' sum is exact, such an error e changes
+  // the loss by e times the difference of the teacher's and the student's share of the listed ids; with the same error there it would change
+  // it by e times the share itself, which in rows that nearly agree is much of the loss.  So the listed ids are summed by exp in double.
+  template <typename R> struct Sums {
+    float m, top_m;
+    R others, tops;
+    double qz;                           // where R is double
+  };
   __device__ __forceinline__ void own_pairs(int i, float &m, double &others) const {
     const int lane = threadIdx.x & 31;
     const float2 p = lane < SW ? sh.pair[i & 1][lane] : make_float2(-INFINITY, 0.f);
     m = warp_max(p.x);
     others = warp_sum_d((double)(p.x > -INFINITY ? p.y * ex2((p.x - m) * ch) : p.y));
   }
-  template <typename R> __device__ __forceinline__ void sums(int i, float &rm, R &others, R &tops, double *qz) const {
+  template <typename R> __device__ __forceinline__ Sums<R> sums(int i) const {
     const int lane = threadIdx.x & 31;
-    const bool tail = a.teacher_lse != nullptr;             // without the bucket the listed ids are among the others
-    R o = 0;
-    tops = 0;
+    const bool tail = a.teacher_lse != nullptr;
+    Sums<R> r;
+    R o = 0, t = 0;
+    double z = 0.0;
+    float m = -INFINITY, tm = -INFINITY;
     if (a.cluster == 1) {
       const float2 p = lane < SW ? sh.pair[i & 1][lane] : make_float2(-INFINITY, 0.f);
-      const float tm = sh.side[i & 3].top_m;
-      rm = fmaxf(warp_max(p.x), tm);
-      o = p.x > -INFINITY ? p.y * ex2((p.x - rm) * ch) : p.y;
-      if (tail) tops = listed_sum<R>(tm, sh.side[i & 3].tops, rm);
-      if (qz) *qz = sh.side[i & 3].qz;
+      m = p.x; o = (R)p.y;
+      r.top_m = tail ? sh.side[i & 3].top_m : -INFINITY;
+      r.tops = tail ? (R)sh.side[i & 3].tops : (R)0;
+      r.qz = sh.side[i & 3].qz;
     } else {
-      float m = -INFINITY, tm = -INFINITY;
-      double t = 0.0, z = 0.0;
-      if (lane < a.cluster) { const DistillPart &x = sh.part[i & 1][lane]; m = x.m; tm = x.top_m; o = (R)x.others; t = x.tops; z = x.qz; }
-      rm = warp_max(fmaxf(m, tm));
-      if (m > -INFINITY) o *= ex2((m - rm) * ch);
+      if (lane < a.cluster) { const DistillPart &x = sh.part[i & 1][lane]; m = x.m; tm = x.top_m; o = (R)x.others; t = (R)x.tops; z = x.qz; }
+      r.top_m = tail ? warp_max(tm) : -INFINITY;
+      r.tops = 0;
       if (tail) {
-        tops = listed_sum<R>(tm, t, rm);
+        if (tm > -INFINITY) {
+          if constexpr (sizeof(R) == 8) t *= exp(((double)tm - (double)r.top_m) * inv_tau);
+          else t *= ex2((tm - r.top_m) * ch);
+        }
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) tops += __shfl_xor_sync(0xffffffffu, tops, x);
+        for (int x = 16; x > 0; x >>= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
+        r.tops = t;
       }
-      if (qz) *qz = warp_sum_d(z);
+      if constexpr (sizeof(R) == 8) r.qz = warp_sum_d(z);
     }
+    r.m = warp_max(m);
+    if (m > -INFINITY) o *= ex2((m - r.m) * ch);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) o += __shfl_xor_sync(0xffffffffu, o, x);
-    others = o;
+    r.others = o;
+    return r;
   }
-  // What the gradient of a row needs.
-  struct Slope { float ref, scale, coef; double total; };          // coef: of 2^((l - ref) ch)
+  // The gradient of an id that is not listed is coef * 2^((l - ref) ch), ref the largest of their logits.
+  struct Slope { float ref, scale, coef; };
   __device__ __forceinline__ Slope slope(int i, float rs) const {
     Slope g;
-    float rm, others, tops;
-    sums(i, rm, others, tops, nullptr);
-    const float total = others + tops, q = sh.side[i & 3].total, rest = sh.side[i & 3].rest, listed = (float)sh.side[i & 3].listed;
-    g.ref = rm > -INFINITY ? rm : 0.f;
-    g.total = (double)total;
+    const Sums<float> s = sums<float>(i);
+    const float rm = fmaxf(s.m, s.top_m), o = s.m > -INFINITY ? s.others * ex2((s.m - rm) * ch) : s.others,
+                t = s.top_m > -INFINITY ? s.tops * ex2((s.top_m - rm) * ch) : s.tops, total = o + t,
+                q = sh.side[i & 3].total, rest = sh.side[i & 3].rest, listed = (float)sh.side[i & 3].listed;
+    g.ref = s.m > -INFINITY ? s.m : 0.f;
     g.scale = total == 0.f || q == 0.f ? 0.f : rs * (float)a.inv_tau;         // 0: padding, or nothing to learn from
-    // Q - q_r / p_r, without the 1 that both begin with
-    g.coef = g.scale * (rest > 0.f && others > 0.f ? listed - rest * (tops / others) : q) / total;
-    if (g.scale == 0.f) g.coef = 0.f;
+    // p_r Q - q_r, without the p_r q_r that both have
+    g.coef = g.scale == 0.f || s.others == 0.f ? 0.f : g.scale * (listed * (o / total) - rest * (t / total)) / s.others;
     return g;
   }
 
   // ---- the side warp: lane's entries are lane, lane + 32, ..
   static constexpr int E = DISTILL_MAX_TOP / 32;
-  struct Entries { int id[E], bit[E]; float z[E], q[E]; bool first[E]; };      // bit: its mark's place, -1 outside the share
+  struct Entries { int id[E], bit[E]; float q[E]; bool first[E]; double w[E]; };      // bit: its mark's place, -1 outside the share; w: e^(z / tau)
+                                                                                      // relative to the largest listed logit of the share
   __device__ __forceinline__ void load_entries(int row, int (&id)[E], float (&t)[E]) const {
     const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -366,18 +374,19 @@ struct DistillBlock {
   // Marks the listed ids of a row, the i-th of the block, whose entries are id and t, and leaves sh.side[i & 3].
   __device__ __forceinline__ void prepare(int row, int i_row, const int (&id)[E], const float (&t)[E], Entries &n) const {
 #pragma unroll
-    for (int i = 0; i < E; ++i) { n.id[i] = id[i]; n.bit[i] = -1; n.first[i] = false; n.z[i] = -INFINITY; n.q[i] = 0.f; }
+    for (int i = 0; i < E; ++i) { n.id[i] = id[i]; n.bit[i] = -1; n.first[i] = false; n.w[i] = 0.0; n.q[i] = 0.f; }
     if (row >= a.rows) return;
     const int lane = threadIdx.x & 31;
     const RowShare<T> sr = share(row);
     uint32_t *words = reinterpret_cast<uint32_t *>(flags_of(i_row & 1));
     double x[E], e[E], ref = -INFINITY, s = 0.0, l = 0.0, qz = 0.0;
+    float z[E], tm = -INFINITY;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      x[i] = -INFINITY;
+      x[i] = -INFINITY; z[i] = -INFINITY;
       if (i * 32 >= a.top) continue;
       n.bit[i] = sr.template flag_bit<NT>(n.id[i], rank, a.cluster, edge_byte());
-      if (n.bit[i] >= 0) n.z[i] = to_f(sr.row[n.id[i]]);
+      if (n.bit[i] >= 0) z[i] = to_f(sr.row[n.id[i]]);
       n.first[i] = n.bit[i] >= 0;
       x[i] = n.id[i] >= 0 ? (double)t[i] * a.inv_tau : -INFINITY;
       sh.id[lane + 32 * i] = n.id[i];
@@ -400,8 +409,6 @@ struct DistillBlock {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) ref = fmax(ref, __shfl_xor_sync(0xffffffffu, ref, o));
     }
-    float tm = -INFINITY;
-    double ts = 0.0;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       e[i] = 0.0;
@@ -410,15 +417,19 @@ struct DistillBlock {
         s += e[i];
         if (!(e[i] == 0.0)) {
           l += e[i] * (a.teacher_lse ? x[i] - ref : x[i]);
-          if (n.bit[i] >= 0) qz += e[i] * (double)n.z[i];
+          if (n.bit[i] >= 0) qz += e[i] * (double)z[i];
         }
-        tm = fmaxf(tm, n.z[i]);
+        tm = fmaxf(tm, z[i]);
       }
     }
     tm = warp_max(tm);
+    double ts = 0.0;
 #pragma unroll
     for (int i = 0; i < E; ++i)
-      if (i * 32 < a.top && a.teacher_lse && n.first[i] && n.z[i] != -INFINITY) ts += exp(((double)n.z[i] - (double)tm) * inv_tau);
+      if (i * 32 < a.top && (GRAD || a.teacher_lse)) {
+        if (n.first[i] && z[i] != -INFINITY) n.w[i] = exp(((double)z[i] - (double)tm) * inv_tau);
+        ts += n.w[i];
+      }
     ts = warp_sum_d(ts); s = warp_sum_d(s); l = warp_sum_d(l); qz = warp_sum_d(qz);
     const bool any = !(s == 0.0);                           // a row with no valid entry has no loss, with or without the rest
     DistillSide d;
@@ -454,25 +465,34 @@ struct DistillBlock {
     if (lane == 0) sh.side[i_row & 3] = d;
     __syncwarp();
   }
-  __device__ __forceinline__ void finish(int row, int i) const {
-    if (rank) return;
-    float rm;
-    double others, tops, qz = 0.0;
-    sums(i, rm, others, tops, &qz);
-    others *= 1.0 + 5.1e-8;                                 // ex2.approx is that much below 2^x in the mean, measured over -28 < x < 0
+  // The row's results; returns what turns the weights of the listed ids of this share into Q p.  The few functions in double are of this warp's
+  // time between two rows' barriers, and a chain of them one by one (two logarithms, a quotient and five exponentials) was a tenth of all, so
+  // the lanes take each an argument of their own.
+  __device__ __forceinline__ double finish(int row, int i, bool &none) const {
+    const int lane = threadIdx.x & 31;
+    Sums<double> s = sums<double>(i);
     const DistillSide &d = sh.side[i & 3];
-    const double total = others + tops, lse = (double)rm * inv_tau + log(total);
-    const bool none = total == 0.0;                         // no finite logit
-    double loss = d.entropy - qz * inv_tau + d.listed * lse, log_rest = 0.0;
-    if (a.teacher_lse) {
-      log_rest = others > 0.0 ? -log1p(tops / others) : others == 0.0 ? -INFINITY : others;
-      if (d.left > 0.0) loss -= d.left * log_rest;
+    s.others *= 1.0 + 5.1e-8;                               // ex2.approx is that much below 2^x in the mean, measured over -28 < x < 0
+    const float rm = fmaxf(s.m, s.top_m);
+    // relative to rm: 0 the others, 1 the listed ids, 4 those of this share; the listed to the others: 2, 3
+    const double from = (double)(lane == 0 ? s.m : lane == 4 ? d.top_m : s.top_m), to = (double)(lane == 2 || lane == 3 ? s.m : rm),
+                 gap = (from - to) * (lane == 3 ? a.inv_tau : inv_tau), e = exp(fmin(gap, 600.0));
+    const double total = s.others * __shfl_sync(0xffffffffu, e, 0) + s.tops * __shfl_sync(0xffffffffu, e, 1);
+    none = total == 0.0;                                    // no finite logit
+    if (rank == 0) {
+      // ln total, and ln (1 + listed / others) = -ln p_r
+      const double lg = log1p(lane < 2 ? total - 1.0 : s.tops / s.others * e) + (lane >= 2 && gap > 600.0 ? gap - 600.0 : 0.0);
+      const double log_total = __shfl_sync(0xffffffffu, lg, 0), p_r = __shfl_sync(0xffffffffu, lg, 2), log_rest = __shfl_sync(0xffffffffu, lg, 3),
+                   no_rest = s.others == 0.0 ? INFINITY : s.others;            // or NaN
+      double loss = d.entropy - s.qz * inv_tau + d.listed * ((double)rm * inv_tau + log_total);
+      if (d.left > 0.0) loss += d.left * (s.others > 0.0 ? p_r : no_rest);
+      if (lane == 0) {
+        if (a.teacher_lse) a.log_rest[row] = none ? -INFINITY : (float)-(s.others > 0.0 ? log_rest : no_rest);
+        a.loss[row] = (float)(d.total == 0.f ? 0.0 : none ? (double)INFINITY : loss);
+        a.lse[row] = none ? -INFINITY : (float)((double)rm * a.inv_tau + log_total);
+      }
     }
-    if ((threadIdx.x & 31) == 0) {
-      if (a.teacher_lse) a.log_rest[row] = none ? -INFINITY : (float)log_rest;
-      a.loss[row] = (float)(d.total == 0.f ? 0.0 : none ? (double)INFINITY : loss);
-      a.lse[row] = none ? -INFINITY : (float)lse;
-    }
+    return none ? 0.0 : __shfl_sync(0xffffffffu, e, 4) * (double)d.total / total;
   }
   // One barrier to a row, when its sums are there.  Behind it the stream warps write the row's gradient and go on to the next row, while this warp
   // replaces the gradients of the listed ids of the row before, whose others are all out by now, computes this row's, finishes its loss and
@@ -512,18 +532,18 @@ struct DistillBlock {
       }
       int ahead[E];
       load_entries(row + 2 * clusters, ahead, t);
+      if (GRAD && i_row) write_listed(row - clusters, id, g_top);
+      double p = 0.0;
+      bool none = false;
+      if (GRAD || rank == 0) p = finish(row, i_row, none);
       if (GRAD) {
-        if (i_row) write_listed(row - clusters, id, g_top);
-        const Slope g = slope(i_row, rs);
-        const double q = (double)sh.side[i_row & 3].total, scale = (double)rs * a.inv_tau;
+        const double scale = none || sh.side[i_row & 3].total == 0.f ? 0.0 : (double)rs * a.inv_tau;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           id[i] = n.first[i] ? n.id[i] : -1;
-          g_top[i] = 0.f;
-          if (i * 32 < a.top && g.scale != 0.f) g_top[i] = (float)(scale * (q * exp(((double)n.z[i] - (double)g.ref) * inv_tau) / g.total - (double)n.q[i]));
+          g_top[i] = scale == 0.0 ? 0.f : (float)(scale * (p * n.w[i] - (double)n.q[i]));
         }
       }
-      finish(row, i_row);
 #pragma unroll
       for (int i = 0; i < E; ++i) if (i * 32 < a.top && n.bit[i] >= 0) flags_of(i_row & 1)[n.bit[i] >> 3] = 0;
       __syncwarp();
@@ -610,7 +630,7 @@ struct DistillBlock {
     }
   }
   __device__ __forceinline__ void stream_warp(uint4 *ring) const {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = (int)threadIdx.x - 32, lane = tid & 31, warp = tid >> 5;
     const bool tail = a.teacher_lse != nullptr;
     RowShare<T> sr = share(first_row), next = sr;
 #pragma unroll
@@ -699,8 +719,8 @@ k_distill(const __grid_constant__ DistillArgs a) {
   kernel_entry(TR_k_distill);
   const DistillBlock<T, GRAD, SW> blk = {a, sh, flags, a.cluster > 1 ? (int)cluster_ctarank() : 0, (int)blockIdx.x / a.cluster, (int)gridDim.x / a.cluster,
                                          (float)(a.inv_tau * 1.4426950408889634), (double)(float)(a.inv_tau * 1.4426950408889634) * 0.6931471805599453};
-  if (threadIdx.x >= SW * 32) blk.side_warp();
-  else blk.stream_warp(reinterpret_cast<uint4 *>(flags + 2 * distill_flag_bytes(a.cta_vecs, SW * 32)) + threadIdx.x);
+  if (threadIdx.x < 32) blk.side_warp();
+  else blk.stream_warp(reinterpret_cast<uint4 *>(flags + 2 * distill_flag_bytes(a.cta_vecs, SW * 32)) + threadIdx.x - 32);
 }
 
 // The gradient from a saved log-sum-exp (and, with teacher_lse, log_rest).  A CTA walks `cta_vecs` vectors of a row with a ring of copies ahead
@@ -715,7 +735,7 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   constexpr int VEC = 16 / sizeof(T), NT = DISTILL_THREADS;
   kernel_entry(TR_k_distill_grad);
   const int row = blockIdx.x / a.cluster, tid = threadIdx.x;
-  const RowShare<T> sr(a.logits, a.ld, row, a.vocab, blockIdx.x - row * a.cluster, a.cluster, a.cta_vecs);
+  const RowShare<T> sr(a.logits, a.ld, row, a.vocab, blockIdx.x - row * a.cluster, a.cluster, a.cta_vecs, tid);
   uint4 *vals = reinterpret_cast<uint4 *>(smem_raw) + tid;
   T *dst = (T *)a.grad + row * a.grad_ld;
   const float rs = a.row_scale ? a.row_scale[row] : 1.f;
@@ -740,10 +760,11 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   __syncthreads();
   const TeacherRow tr = teacher_row(a, teacher);
   const double scale = tr.total == 0.0 ? 0.0 : (double)rs * a.inv_tau;
-  const double tail = tr.rest > 0.0 ? tr.rest * exp(-(double)a.log_rest[row]) : 0.0;
-  // logits relative to tau lse, so that the difference that the exponential sees is small where p is not
-  const float ref = (float)(lse / a.inv_tau),
-              d = (float)((lse - (double)ref * a.inv_tau) * 1.4426950408889634), coef = (float)(scale * (tr.total - tail));
+  // (p_r Q - q_r) times the id's part of the others, which is no more than 1 however small p_r is: logits relative to tau (lse + ln p_r)
+  const double rest_log = a.teacher_lse && a.log_rest[row] != -INFINITY ? (double)a.log_rest[row] : 0.0, base = lse + rest_log;
+  const float ref = (float)(base / a.inv_tau),
+              d = (float)((base - (double)ref * a.inv_tau) * 1.4426950408889634),
+              coef = (float)(scale * (a.teacher_lse && a.log_rest[row] == -INFINITY ? 0.0 : tr.total * exp(rest_log) - tr.rest));
   const bool mine = sr.template flag_bit<NT>(t.id, blockIdx.x - row * a.cluster, a.cluster, 0) >= 0 && scale != 0.0;
   float g_top = 0.f;
   if (tid < DISTILL_MAX_TOP) { sq[tid] = t.e * tr.mine(); sid[tid] = t.id; }

@@ -53,13 +53,13 @@ def formula(s, ids, top, teacher_lse, tau, V, lse=None, log_rest=None):
     zt = torch.gather(z, 1, at)
     loss = torch.where(q > 0, q * (torch.log(q.clamp(min=1e-300)) - zt + lse[:, None]), 0.0).sum(1)
     total = q.sum(1) + qr
-    rest = total.clone()
+    bucket = torch.zeros_like(p)                             # q_r p_i / p_r
     if tail:
         loss = loss + torch.where(qr > 0, qr * (torch.log(qr.clamp(min=1e-300)) - log_rest), 0.0)
-        rest = total - torch.where(qr > 0, qr * torch.exp(-log_rest), 0.0)
-    grad = torch.where(listed, total[:, None] * p - target, p * rest[:, None]) / tau
+        bucket = torch.where((qr > 0)[:, None] & (z > NEG), qr[:, None] * torch.exp(z - (lse + log_rest)[:, None]), 0.0)
+    grad = torch.where(listed, total[:, None] * p - target, total[:, None] * p - bucket) / tau
     # what an error of 1 in every p (relative) makes of it
-    size = torch.where(listed, total[:, None] * p, p * (total + (total - rest).abs())[:, None]) / tau
+    size = torch.where(listed, total[:, None] * p, total[:, None] * p + bucket) / tau
     return loss, lse, log_rest, grad, size
 
 
@@ -226,6 +226,40 @@ def test_a_sure_student_keeps_the_rest_exact():
     x, ids, top, tl, scale = make(3, 20000, 4, seed=8, tail=True)
     x.scatter_(1, ids.long(), 35.0)
     run_all(x, ids, top, tl, scale)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,tau", [(5000, 1.0), (5000, 0.01), (150001, 0.3)])
+@pytest.mark.parametrize("gap", [-3000.0, -95.0, 40.0, 95.0, 400.0, 3000.0])
+def test_listed_ids_far_from_the_others(gap, V, tau, dtype):
+    """Between the listed ids and the others lie `gap` units of the temperature, more than a float's exponential reaches.  The loss may be off by
+    more than elsewhere: the student's 1 / tau is a float's, off by 2^-24, which changes it by 2^-24 of |sum (p - q) z / tau|, at most
+    loss + 2 ln V (loss = sum q ln q + H(p) + sum (p - q) z / tau): 2^-24 (|loss| + 25), beside the 1.7e-5 and half a step of its own.
+    A gradient's p_i are off by as much as elsewhere, each group's being taken relative to its own largest; ids that are `gap` below the
+    other group have next to no p (2^-24 * 95 = 5.7e-6 of e^-95)."""
+    from paper_2505_19201_b200 import api
+    R, K = 3, 8
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = (torch.randn(R, V, device="cuda", generator=g) * tau).to(dtype)
+    ids = torch.stack([torch.randperm(V, device="cuda", generator=g)[:K] for _ in range(R)]).int()
+    x.scatter_add_(1, ids.long(), torch.full((R, K), gap * tau, device="cuda").to(dtype))
+    top = torch.randn(R, K, device="cuda", generator=g) * tau
+    tl = (torch.logsumexp(top.double() / tau, 1) + torch.tensor([0.3, 1.0, 3.0], device="cuda", dtype=torch.float64)).float()
+    scale = torch.rand(R, device="cuda", generator=g) + 0.5
+    out = [torch.full((R,), 5.0, device="cuda") for _ in range(3)]
+    grad = torch.full_like(x, 3.0)
+    api.dream_distill_loss(x, ids, top, out[0], out[1], teacher_lse=tl, log_rest=out[2], temperature=tau, row_scale=scale, grad=grad)
+    back = torch.full_like(x, 3.0)
+    api.dream_distill_grad(x, ids, top, out[1], back, teacher_lse=tl, log_rest=out[2], temperature=tau, row_scale=scale)
+    tau = float(torch.tensor(tau, dtype=torch.float32))      # as the call has it
+    loss, lse, log_rest, want, size = formula(x, ids, top, tl, tau, V)
+    assert bool(((out[0].double().cpu() - loss).abs() <= 1.7e-5 + 2 ** -24 * (2 * loss.abs() + 25)).all())
+    close_rows(out[1], lse, "lse")
+    close_rows(out[2], log_rest, "log_rest")
+    close_grad(grad, want, size, scale, dtype)
+    # the separate call starts from the rounded lse and log_rest
+    _, _, _, want, size = formula(x, ids, top, tl, tau, V, out[1], out[2])
+    close_grad(back, want, size, scale, dtype)
 
 
 @pytest.mark.parametrize("tail", [False, True])
