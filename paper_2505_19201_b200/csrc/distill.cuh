@@ -81,6 +81,12 @@ __device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
   return pair_of(r);
 }
+// The largest of a warp's floats, NaN passed over.
+__device__ __forceinline__ float max_of_warp(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
 __device__ __forceinline__ double warp_sum_d(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -293,6 +299,7 @@ struct DistillBlock {
   // The exponentials of the others are all off in one direction by some 1e-7.  Where the listed ids' sum is exact, such an error e changes
   // the loss by e times the difference of the teacher's and the student's share of the listed ids; with the same error there it would change
   // it by e times the share itself, which in rows that nearly agree is much of the loss.  So the listed ids are summed by exp in double.
+  // Every group of G lanes holds the G values, so that log2(G) exchanges add them up.
   template <typename R> struct Sums {
     float m, top_m;
     R others, tops;
@@ -300,43 +307,47 @@ struct DistillBlock {
   };
   __device__ __forceinline__ void own_pairs(int i, float &m, double &others) const {
     const int lane = threadIdx.x & 31;
-    const float2 p = lane < SW ? sh.pair[i & 1][lane] : make_float2(-INFINITY, 0.f);
-    m = warp_max(p.x);
-    others = warp_sum_d((double)(p.x > -INFINITY ? p.y * ex2((p.x - m) * ch) : p.y));
+    const float2 p = sh.pair[i & 1][lane % SW];
+    m = max_of_warp(p.x);
+    others = group_sum<SW>((double)(p.x > -INFINITY ? p.y * ex2((p.x - m) * ch) : p.y));
+  }
+  template <int G, typename R> static __device__ __forceinline__ R group_sum(R v) {
+#pragma unroll
+    for (int x = G / 2; x > 0; x >>= 1) v += __shfl_xor_sync(0xffffffffu, v, x);
+    return v;
   }
   template <typename R> __device__ __forceinline__ Sums<R> sums(int i) const {
     const int lane = threadIdx.x & 31;
     const bool tail = a.teacher_lse != nullptr;
     Sums<R> r;
-    R o = 0, t = 0;
-    double z = 0.0;
-    float m = -INFINITY, tm = -INFINITY;
+    r.top_m = -INFINITY; r.tops = 0;
     if (a.cluster == 1) {
-      const float2 p = lane < SW ? sh.pair[i & 1][lane] : make_float2(-INFINITY, 0.f);
-      m = p.x; o = (R)p.y;
-      r.top_m = tail ? sh.side[i & 3].top_m : -INFINITY;
-      r.tops = tail ? (R)sh.side[i & 3].tops : (R)0;
+      const float2 p = sh.pair[i & 1][lane % SW];
+      if (tail) { r.top_m = sh.side[i & 3].top_m; r.tops = (R)sh.side[i & 3].tops; }
       r.qz = sh.side[i & 3].qz;
+      r.m = max_of_warp(p.x);
+      r.others = group_sum<SW>((R)(p.x > -INFINITY ? p.y * ex2((p.x - r.m) * ch) : p.y));
     } else {
-      if (lane < a.cluster) { const DistillPart &x = sh.part[i & 1][lane]; m = x.m; tm = x.top_m; o = (R)x.others; t = (R)x.tops; z = x.qz; }
-      r.top_m = tail ? warp_max(tm) : -INFINITY;
-      r.tops = 0;
+      constexpr int G = DISTILL_MAX_CLUSTER;
+      const bool on = lane % G < a.cluster;
+      const DistillPart &x = sh.part[i & 1][lane % G];
+      const float m = on ? x.m : -INFINITY;
+      r.m = max_of_warp(m);
+      R o = on ? (R)x.others : (R)0;
+      if (m > -INFINITY) o *= ex2((m - r.m) * ch);
+      r.others = group_sum<G>(o);
       if (tail) {
+        const float tm = on ? x.top_m : -INFINITY;
+        r.top_m = max_of_warp(tm);
+        R t = on ? (R)x.tops : (R)0;
         if (tm > -INFINITY) {
           if constexpr (sizeof(R) == 8) t *= exp(((double)tm - (double)r.top_m) * inv_tau);
           else t *= ex2((tm - r.top_m) * ch);
         }
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
-        r.tops = t;
+        r.tops = group_sum<G>(t);
       }
-      if constexpr (sizeof(R) == 8) r.qz = warp_sum_d(z);
+      if constexpr (sizeof(R) == 8) r.qz = group_sum<G>(on ? x.qz : 0.0);
     }
-    r.m = warp_max(m);
-    if (m > -INFINITY) o *= ex2((m - r.m) * ch);
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) o += __shfl_xor_sync(0xffffffffu, o, x);
-    r.others = o;
     return r;
   }
   // The gradient of an id that is not listed is coef * 2^((l - ref) ch), ref the largest of their logits.
@@ -344,13 +355,17 @@ struct DistillBlock {
   __device__ __forceinline__ Slope slope(int i, float rs) const {
     Slope g;
     const Sums<float> s = sums<float>(i);
-    const float rm = fmaxf(s.m, s.top_m), o = s.m > -INFINITY ? s.others * ex2((s.m - rm) * ch) : s.others,
-                t = s.top_m > -INFINITY ? s.tops * ex2((s.top_m - rm) * ch) : s.tops, total = o + t,
-                q = sh.side[i & 3].total, rest = sh.side[i & 3].rest, listed = (float)sh.side[i & 3].listed;
+    const float q = sh.side[i & 3].total;
+    float total = s.others, part = q;                       // Q - q_r / p_r, times p_r
+    if (a.teacher_lse) {                                    // p_r Q - q_r, without the p_r q_r that both have
+      const float rm = fmaxf(s.m, s.top_m), o = s.m > -INFINITY ? s.others * ex2((s.m - rm) * ch) : s.others,
+                  t = s.top_m > -INFINITY ? s.tops * ex2((s.top_m - rm) * ch) : s.tops;
+      total = o + t;
+      part = __fdividef((float)sh.side[i & 3].listed * o - sh.side[i & 3].rest * t, total);
+    }
     g.ref = s.m > -INFINITY ? s.m : 0.f;
     g.scale = total == 0.f || q == 0.f ? 0.f : rs * (float)a.inv_tau;         // 0: padding, or nothing to learn from
-    // p_r Q - q_r, without the p_r q_r that both have
-    g.coef = g.scale == 0.f || s.others == 0.f ? 0.f : g.scale * (listed * (o / total) - rest * (t / total)) / s.others;
+    g.coef = g.scale == 0.f || s.others == 0.f ? 0.f : g.scale * __fdividef(part, s.others);
     return g;
   }
 
@@ -422,7 +437,7 @@ struct DistillBlock {
         tm = fmaxf(tm, z[i]);
       }
     }
-    tm = warp_max(tm);
+    tm = max_of_warp(tm);
     double ts = 0.0;
 #pragma unroll
     for (int i = 0; i < E; ++i)
@@ -474,16 +489,25 @@ struct DistillBlock {
     const DistillSide &d = sh.side[i & 3];
     s.others *= 1.0 + 5.1e-8;                               // ex2.approx is that much below 2^x in the mean, measured over -28 < x < 0
     const float rm = fmaxf(s.m, s.top_m);
-    // relative to rm: 0 the others, 1 the listed ids, 4 those of this share; the listed to the others: 2, 3
-    const double from = (double)(lane == 0 ? s.m : lane == 4 ? d.top_m : s.top_m), to = (double)(lane == 2 || lane == 3 ? s.m : rm),
-                 gap = (from - to) * (lane == 3 ? a.inv_tau : inv_tau), e = exp(fmin(gap, 600.0));
-    const double total = s.others * __shfl_sync(0xffffffffu, e, 0) + s.tops * __shfl_sync(0xffffffffu, e, 1);
+    double total = s.others, log_total = 0.0, p_r = 0.0, log_rest = 0.0, own = 0.0;
+    if (a.teacher_lse) {
+      // relative to rm: 0 the others, 1 the listed ids, 4 those of this share; the listed to the others: 2, 3
+      const double from = (double)(lane == 0 ? s.m : lane == 4 ? d.top_m : s.top_m), to = (double)(lane == 2 || lane == 3 ? s.m : rm),
+                   gap = (from - to) * (lane == 3 ? a.inv_tau : inv_tau), e = exp(fmin(gap, 600.0));
+      total = s.others * __shfl_sync(0xffffffffu, e, 0) + s.tops * __shfl_sync(0xffffffffu, e, 1);
+      own = __shfl_sync(0xffffffffu, e, 4);
+      // ln total, and ln (1 + listed / others) = -ln p_r
+      if (rank == 0) {
+        const double lg = log1p(lane < 2 ? total - 1.0 : s.tops / s.others * e) + (lane >= 2 && gap > 600.0 ? gap - 600.0 : 0.0);
+        log_total = __shfl_sync(0xffffffffu, lg, 0); p_r = __shfl_sync(0xffffffffu, lg, 2); log_rest = __shfl_sync(0xffffffffu, lg, 3);
+      }
+    } else {
+      if (rank == 0) log_total = log(total);
+      if (GRAD) own = exp(((double)d.top_m - (double)rm) * inv_tau);
+    }
     none = total == 0.0;                                    // no finite logit
     if (rank == 0) {
-      // ln total, and ln (1 + listed / others) = -ln p_r
-      const double lg = log1p(lane < 2 ? total - 1.0 : s.tops / s.others * e) + (lane >= 2 && gap > 600.0 ? gap - 600.0 : 0.0);
-      const double log_total = __shfl_sync(0xffffffffu, lg, 0), p_r = __shfl_sync(0xffffffffu, lg, 2), log_rest = __shfl_sync(0xffffffffu, lg, 3),
-                   no_rest = s.others == 0.0 ? INFINITY : s.others;            // or NaN
+      const double no_rest = s.others == 0.0 ? INFINITY : s.others;         // or NaN
       double loss = d.entropy - s.qz * inv_tau + d.listed * ((double)rm * inv_tau + log_total);
       if (d.left > 0.0) loss += d.left * (s.others > 0.0 ? p_r : no_rest);
       if (lane == 0) {
@@ -492,7 +516,7 @@ struct DistillBlock {
         a.lse[row] = none ? -INFINITY : (float)((double)rm * a.inv_tau + log_total);
       }
     }
-    return none ? 0.0 : __shfl_sync(0xffffffffu, e, 4) * (double)d.total / total;
+    return none ? 0.0 : own * (double)d.total / total;
   }
   // One barrier to a row, when its sums are there.  Behind it the stream warps write the row's gradient and go on to the next row, while this warp
   // replaces the gradients of the listed ids of the row before, whose others are all out by now, computes this row's, finishes its loss and
@@ -675,7 +699,7 @@ struct DistillBlock {
         left -= PER * NT;
         ++block;
       } while (!GRAD && sr.nv > block * PER * NT);
-      const float wm = warp_max(m);
+      const float wm = max_of_warp(m);
       s.x = warp_sum((s.x + s.y) * (m > -INFINITY ? ex2((m - wm) * ch) : 1.f));       // without a maximum 0, or NaN
       if (lane == 0) sh.pair[i_row & 1][warp] = make_float2(wm, s.x);
       block_barrier<THREADS>();
@@ -726,7 +750,7 @@ k_distill(const __grid_constant__ DistillArgs a) {
 // The gradient from a saved log-sum-exp (and, with teacher_lse, log_rest).  A CTA walks `cta_vecs` vectors of a row with a ring of copies ahead
 // of it.
 template <typename T>
-__global__ void __launch_bounds__(DISTILL_THREADS)
+__global__ void __launch_bounds__(DISTILL_THREADS, 5)
 k_distill_grad(const __grid_constant__ DistillArgs a) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   __shared__ TeacherSums teacher;
@@ -764,7 +788,7 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   const double rest_log = a.teacher_lse && a.log_rest[row] != -INFINITY ? (double)a.log_rest[row] : 0.0, base = lse + rest_log;
   const float ref = (float)(base / a.inv_tau),
               d = (float)((base - (double)ref * a.inv_tau) * 1.4426950408889634),
-              coef = (float)(scale * (a.teacher_lse && a.log_rest[row] == -INFINITY ? 0.0 : tr.total * exp(rest_log) - tr.rest));
+              coef = (float)(scale * (!a.teacher_lse ? tr.total : a.log_rest[row] == -INFINITY ? 0.0 : tr.total * exp(rest_log) - tr.rest));
   const bool mine = sr.template flag_bit<NT>(t.id, blockIdx.x - row * a.cluster, a.cluster, 0) >= 0 && scale != 0.0;
   float g_top = 0.f;
   if (tid < DISTILL_MAX_TOP) { sq[tid] = t.e * tr.mine(); sid[tid] = t.id; }

@@ -1619,9 +1619,11 @@ static cudaError_t allow(void (*kernel)(A), int cluster, size_t smem) {
   return e;
 }
 
-// Launch of `rows` clusters on a caller's stream, of the current device.  Returns null or what went wrong.
+// Launch of `rows` clusters on a caller's stream, of the current device.  Returns null or what went wrong.  early: the kernel may take its places
+// while the one before it still runs.  One that loops and fills the GPU with clusters may not: the places come free one by one and not in whole
+// clusters, some of its own then wait until others are done, and 1000 rows of 131072 took 142 us back to back instead of 105.
 template <typename A>
-static const char *launch_rows(void (*kernel)(A), int rows, int cluster, int threads, size_t smem, cudaStream_t stream, const A &args) {
+static const char *launch_rows(void (*kernel)(A), int rows, int cluster, int threads, size_t smem, cudaStream_t stream, const A &args, bool early = true) {
   cudaError_t e = allow(kernel, cluster, smem);
   if (e == cudaSuccess) {
     cudaLaunchConfig_t cfg = {};
@@ -1633,7 +1635,7 @@ static const char *launch_rows(void (*kernel)(A), int rows, int cluster, int thr
       attr[n].val.clusterDim.x = (unsigned)cluster; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
       ++n;
     }
-    if (pdl_on()) {
+    if (early && pdl_on()) {
       attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
       attr[n].val.programmaticStreamSerializationAllowed = 1;
       ++n;
@@ -1808,7 +1810,8 @@ extern "C" dream_status dream_distill_loss(const void *logits, int32_t dtype, in
   const size_t smem = ((wide ? sizeof(DistillShared<16>) : sizeof(DistillShared<8>)) + 15) / 16 * 16 + 2 * (size_t)distill_flag_bytes(a.cta_vecs, warps * 32) + (size_t)DISTILL_PER * warps * 32 * 16;
   void (*kernel)(DistillArgs) = wide ? k_distill<float, true, 16>
                               : dtype == DREAM_BF16 ? (grad ? k_distill<bf16, true, 8> : k_distill<bf16, false, 8>) : (grad ? k_distill<float, true, 8> : k_distill<float, false, 8>);
-  const char *why = launch_rows(kernel, imin(rows, resident_clusters(kernel, a.cluster, warps * 32 + 32, smem)), a.cluster, warps * 32 + 32, smem, (cudaStream_t)cuda_stream, a);
+  const int places = resident_clusters(kernel, a.cluster, warps * 32 + 32, smem);
+  const char *why = launch_rows(kernel, imin(rows, places), a.cluster, warps * 32 + 32, smem, (cudaStream_t)cuda_stream, a, a.cluster == 1 || rows < 2 * places);
   return why ? fail(nullptr, DREAM_E_CUDA, "dream_distill_loss: %s", why) : DREAM_OK;
 }
 
