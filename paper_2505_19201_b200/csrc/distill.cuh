@@ -9,7 +9,11 @@
 //
 // Bound by memory: a row is read once (and its gradient written once).  p_r would lose its digits as a difference of sums where the
 // listed ids hold nearly everything, so the ids are marked in a bitmap and the others summed by themselves; the few numbers of the listed
-// ids and of the row are in double.
+// ids and of the row are in double.  At 6.45 TB/s of a copy:
+//   4096 rows of 32000 bf16, 16 listed, with gradient: 117 us, 4.5 TB/s; 1024 rows of 262144 bf16: 274 us, 3.9 TB/s
+//   loss alone, 1000 rows of 131072 fp32: 100 us, 5.3 TB/s; 256 rows of 32000 bf16: 11.9 us, a launch and a row's chain of steps
+//   gradient alone, 2048 rows of 32000 bf16, a fifth of them padding: 45 us, 5.4 TB/s; 777 rows of 49155 fp32: 60 us, 5.1 TB/s
+// Between 4.5 and 6.45 TB/s stand the turnaround from a row's sums to its gradient and the exponentials (45 % of their units' rate).
 #pragma once
 #include "common.cuh"
 
@@ -275,6 +279,8 @@ __device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool ze
 // (with GRAD a share is one block), and a vector's place is taken by the next block's, or the next row's, as soon as its gradient is
 // out (without GRAD: as soon as it has been added), so loads are always on their way.  (With a block per row and its own 64 KB the turnaround
 // of the blocks cost as much as everything else: 4096 rows of 32000 bf16 with gradient took 152 us, 99 of them with both passes left out.)
+// The side warp is the block's first: of the warps that could go on the oldest does, and as the last one it got a turn every 30 cycles and held
+// the others up (127 us instead of 117).
 #define DISTILL_GRAD_RING 8
 template <int THREADS> __device__ __forceinline__ void block_barrier() { asm volatile("barrier.sync 0, %0;" ::"n"(THREADS) : "memory"); }
 

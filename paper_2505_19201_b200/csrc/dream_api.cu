@@ -1703,7 +1703,9 @@ static bool rows_collide(const void *p, long long ld, const void *q, long long q
 }
 // Fills in what follows from the sizes and launches.
 static const char *sample_launch(SampleArgs a, int dtype, int rows, bool truncate, cudaStream_t stream) {
-  // 64 KB of the row per CTA, two CTAs per SM, where a cluster of eight holds it so; more CTAs to a row where there are few rows
+  // 64 KB of the row per CTA, two CTAs per SM, where a cluster of eight holds it so; more CTAs to a row where there are few rows (61 rows of
+  // 32003 bf16 of mixed settings: 41 us, by one CTA each 70).  Sixteen: one row of 262144 at top_p 0.95 takes 65 us, in eight 88; eight rows
+  // 92 and 100; more than nine clusters of sixteen do not fit at once.
   const int esz = dtype == DREAM_BF16 ? 2 : 4;
   a.cluster = 1;
   while (a.cluster < 8 && (a.vocab > a.cluster * (65536 / esz) || (rows * a.cluster < 148 && a.vocab > a.cluster * 4096))) a.cluster *= 2;
@@ -1801,10 +1803,12 @@ extern "C" dream_status dream_distill_loss(const void *logits, int32_t dtype, in
   if (s) return s;
   a.loss = loss;
   // With a gradient the ring holds a CTA's share of a row, 64 KB, in the widest fp32 rows 128 KB; without one the share is bounded by its byte per
-  // vector.  More CTAs to a row where there are few rows.  Three CTAs per SM.
+  // vector.  More CTAs to a row where there are few rows, while all are resident at once, three per SM: 40 rows of 131072 bf16 take 8.7 us in
+  // clusters of eight and 11.7 in as few as hold a row (with gradient 12.3 and 15.5), but 256 rows of 32000 12.2 us in pairs and 10.3 by
+  // one CTA each (18.4 and 15.2).
   const int vecs = imax(1, vocab / (dtype == DREAM_BF16 ? 8 : 4)), wide = grad && vecs > DISTILL_MAX_CLUSTER * 4096, most = grad ? (wide ? 8192 : 4096) : 8192;
   a.cluster = 1;
-  while (a.cluster < DISTILL_MAX_CLUSTER && (vecs > a.cluster * most || (rows * a.cluster < 148 * 2 && vecs > a.cluster * 1024))) a.cluster *= 2;
+  while (a.cluster < DISTILL_MAX_CLUSTER && (vecs > a.cluster * most || (2 * (long long)rows * a.cluster <= 148 * 3 && vecs > a.cluster * 1024))) a.cluster *= 2;
   a.cta_vecs = (vecs + a.cluster - 1) / a.cluster;
   const int warps = wide ? 16 : 8;
   const size_t smem = ((wide ? sizeof(DistillShared<16>) : sizeof(DistillShared<8>)) + 15) / 16 * 16 + 2 * (size_t)distill_flag_bytes(a.cta_vecs, warps * 32) + (size_t)DISTILL_PER * warps * 32 * 16;
@@ -1824,7 +1828,8 @@ extern "C" dream_status dream_distill_grad(const void *logits, int32_t dtype, in
   dream_status s = distill_args("dream_distill_grad", &a, logits, dtype, rows, vocab, ld, teacher_ids, teacher_logits, top, teacher_lse,
                                 temperature, const_cast<float *>(lse), const_cast<float *>(log_rest), row_scale, grad, grad_ld);
   if (s) return s;
-  // as much of a row per CTA as leaves every SM some twelve of them
+  // as much of a row per CTA as leaves every SM some twelve of them: 40 rows of 131072 bf16 9.3 us, a CTA to a row 14.6; 256 rows of 32000
+  // 12.4 and 13.1
   const int vecs = imax(1, vocab / (dtype == DREAM_BF16 ? 8 : 4));
   const int steps = (vecs + DISTILL_THREADS - 1) / DISTILL_THREADS, parts = imax(1, imin((steps + 3) / 4, (148 * 12 + rows - 1) / rows));
   a.cta_vecs = (steps + parts - 1) / parts * DISTILL_THREADS;

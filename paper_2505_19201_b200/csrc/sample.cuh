@@ -7,20 +7,31 @@
 //
 // A token is a whole number, so a row's sums have to be exact enough that no rounding moves a border: an error of 1e-7 of the
 // total, what 32-bit exponentials leave, moves the token of one row in ten where 100000 tokens share the mass.  Weights are
-// therefore taken in double (to 3e-13) and summed as 64-bit integers of 2^-s (s such that a whole row of ones fits), whose sums do
-// not depend on their order: histograms by atomics, shares of a cluster and scans all agree bit for bit.
+// therefore taken in double (to 1.3e-12, Weigher).  Lists and histograms add them as 64-bit integers of 2^-s (s such that a whole row of
+// ones fits), whose sums do not depend on their order; the draw and the mass in front of a list add them in double, in one fixed order.
 //
-// The cut is a pair (key, id): an order-preserving 32-bit key of the logit and the last id kept among its ties.  Three ways to it:
-//   few tokens (top_k up to 256, greedy): the k-th largest of the threads' own maxima is a bound that little more than k logits pass; those
+// A row is read once into shared memory, by one block or a cluster of up to 16 whose blocks exchange through shared memory.  The cut is
+// a logit and the last id kept among its ties.  Ways to it:
+//   few tokens (top_k up to 256, greedy; one row of 32000 at top_k 50: 9.8 us, through the bins below 20): the k-th largest of the threads' own maxima is a bound that little more than k logits pass; those
 //     are listed, and one block settles order, masses, cut and draw on the list.
-//   many: one pass sorts the row into bins of 1 / 128 nat with counts and masses; the bin where top_k or top_p ends is listed and settled.
-//   neither list fits (masked rows, rows of ties, logits of an odd scale): a radix selection over the keys, eleven bits a level, by count or by
-//     mass, which assumes nothing about the values.
+//   many: a pass sorts the row into bins of 1 / 128 nat, with counts (top_k) or approximate masses (top_p); the bin in which the cut falls is
+//     listed (a full one is divided once more) and settled exactly, the mass in front of it being summed exactly: the bins only say where to look.
+//   neither list fits (masked rows, rows of ties, logits of an odd scale), or the exact mass contradicts the bins: a radix selection over
+//     order-preserving keys, eleven bits a level, by count or by exact mass, which assumes nothing about the values.
+//
+// What bounds it: not the row's bytes but instructions and, in few rows, the chain of barriers of a cluster.  A temperature alone
+// costs 29 instructions per logit (nine of them in double), a nucleus about 96, every call some 700 to 1600 per warp besides.
+//   1 row of 32000, top_k 50, top_p 0.9: 9.8 us, a launch and a chain of cluster barriers (44 with radix levels alone)
+//   8 rows of 262144 fp32, top_p 0.95: 54 to 95 us, by how often the bins have to be divided
+//   61 rows of 32003 bf16, settings mixed by row: 40 us
+//   256 rows of 131072, a temperature alone: 107 us (1.25 TB/s; 159 with weights by series)
+//   61 rows of 32000 truncated at top_k 40, top_p 0.95: 13.8 us; 244 rows of 131072 at top_p 0.9, min_p 0.002: 278 us
+// 512 threads and two blocks per SM: one block's barriers pass while the other computes.
 #pragma once
 #include "common.cuh"
 #include "rows.cuh"
 
-#define SAMPLE_MAX_CLUSTER 16          // above 8 where rows are few: the kernel opts in
+#define SAMPLE_MAX_CLUSTER 16          // above 8 for up to 9 rows
 #define SAMPLE_MAX_VOCAB 262144
 #define SAMPLE_BINS 2048
 #define SAMPLE_CHUNKS 32               // of SAMPLE_BINS / 32 bins, a lane each
