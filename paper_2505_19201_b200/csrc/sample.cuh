@@ -575,7 +575,9 @@ struct SampleRow {
     constexpr int LAST = SAMPLE_BINS - 1;
     const float scale = 128.f / temp;
     float x0 = 0.f, fine = 1.f;                             // where the bins begin, and how many to 1 / 128 nat
-    auto depth = [&](float l) { return (m - l) * scale - x0; };
+    // Product and difference rounded apart: both looks then see one product, and where it is x0 or more the difference is exact.  Fused, the second
+    // look would take a product that rounds up to x0 for less, and its token, which the first look did not count in front, would be lost to the count.
+    auto depth = [&](float l) { return __fsub_rn(__fmul_rn(m - l, scale), x0); };
     auto place = [&](float x) { return (int)floorf(fminf(x * fine, (float)LAST)); };       // NaN: the last
     double z = 0.0;
     u64 left = top_k;
