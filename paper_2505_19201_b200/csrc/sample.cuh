@@ -109,7 +109,8 @@ template <> __device__ __forceinline__ double of_bits<double>(u64 v) { return __
 #define SAMPLE_TABLE 32
 struct Weigher {
   double m, c2, unit;                  // row maximum, log2(e) / T, 2^(52 - s)
-  float cut;                           // below it a weight is less than half a unit
+  float cut;                           // below it a weight is less than half a unit; rounded up: raw() has no weights for what lies far below, at
+                                       // a very low temperature the very next float
   const double *table;                 // 2^(j / 32), in shared memory
   __device__ __forceinline__ double raw(float l) const {
     const double d = (double)fminf(l, 3.402823466e38f) - m;
@@ -690,7 +691,7 @@ k_sample(const __grid_constant__ SampleArgs a) {
   const bool infinite = m == INFINITY;                      // the infinite ones share the mass
   weigh.table = sh.table;
   weigh.m = (double)m; weigh.c2 = sh.c2; weigh.unit = __longlong_as_double((long long)(1023 + 52 - a.frac_bits) << 52);
-  weigh.cut = fmaxf(__double2float_rd(weigh.m - (double)(a.frac_bits + 2) * 0.69314718055994531 * (double)temp), -3.402823466e38f);
+  weigh.cut = fmaxf(__double2float_ru(weigh.m - (double)(a.frac_bits + 2) * 0.69314718055994531 * (double)temp), -3.402823466e38f);
   if (infinite) { weigh.m = (double)3.402823466e38f; weigh.cut = INFINITY; }
   auto target = [&](u64 total) { const u64 t = (u64)((double)u * (double)total); return t < total ? t : total - 1; };
   auto draw = [&](float l, int id, double total) {

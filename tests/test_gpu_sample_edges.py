@@ -35,3 +35,19 @@ def test_many_kept_at_a_temperature(V, t):
     for seed in range(4):
         check(rows(8, V, seed=seed, sigma=1.0), [0.05, 0.3, 0.5, 0.6, 0.7, 0.8, 0.9, 0.99], t=[t] * 8,
               k=torch.randint(300, V * 3 // 4, (8,), generator=g).tolist())
+
+
+@pytest.mark.parametrize("t", [1e-4, 1e-6, 2e-9, 1e-10, 1e-12, 1e-15])
+@pytest.mark.parametrize("m", [3.7, 20.0, 3000.0, -3.7, 1e6])
+def test_neighbouring_floats_at_low_temperatures(m, t):
+    """A step of a float below the largest logit may be a thousand temperatures and more."""
+    V = 20000
+    x = torch.minimum(rows(5, V, seed=20), torch.tensor(m - 1.0, device="cuda")).contiguous()
+    top = torch.tensor(m)
+    next_ = torch.nextafter(top, torch.tensor(-1e9))
+    for i, at in enumerate((3, 700, 9000, 15000, 19999)):
+        x[:, at] = next_ if i % 2 == 0 else top
+        x[i, at] = top if i < 3 else next_
+    x[3, 4000:4600] = next_
+    for s in ({}, dict(k=[1, 2, 3, 50, 4]), dict(k=[300, 1000, 5000, 400, 19000]), dict(p=[0.1, 0.4, 0.7, 0.9, 0.999]), dict(mp=[0.9, 0.5, 0.1, 0.01, 1e-6])):
+        check(x, [0.05, 0.3, 0.6, 0.85, 0.99], t=[t] * 5, **s)
