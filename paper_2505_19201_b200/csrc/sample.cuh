@@ -346,7 +346,9 @@ struct SampleRow {
 
   // The first token in id order at which the running sum of vals exceeds goal(total): found(logit, id, total) runs in the one thread that
   // holds it.  vals(logits, first id, v) gives a vector's terms and returns how many tokens they count for.  Two exchange slots (the second
-  // carries the count); returns the total.  In double as in integers the sums have one order, and neighbours see the same border between them.
+  // carries the count); returns the total.  In double as in integers the sums have one order, and neighbours see the same border between them: warps
+  // and blocks are added up one by one, so their borders never fall and a warp without a term has no room between its own, whatever is rounded.
+  // (By a scan a border could fall by a rounding; a goal on it, as half the mass of a row of two equal halves, was two warps' or nobody's.)
   template <typename A, typename V, typename G, typename H> __device__ __forceinline__ A locate(int slot, V vals_of, G goal, H found) const {
     A s = 0;
     uint32_t n = 0;
@@ -361,7 +363,12 @@ struct SampleRow {
     __syncthreads();
     if (lane == 0) { sh.warp_tot[warp] = as_bits(s); sh.warp_cnt[warp] = n; }
     __syncthreads();
-    const A inc = warp_scan<A>(lane < nw ? of_bits<A>(sh.warp_tot[lane]) : (A)0), all = __shfl_sync(0xffffffffu, inc, nw - 1);
+    A all = 0, front = 0, own = 0;                          // of the CTA, up to this warp, with this warp
+    for (int q = 0; q < nw; ++q) {
+      if (q == warp) front = all;
+      all += of_bits<A>(sh.warp_tot[q]);
+      if (q == warp) own = all;
+    }
     n = __reduce_add_sync(0xffffffffu, lane < nw ? sh.warp_cnt[lane] : 0u);
     if (threadIdx.x < a.cluster) st_cluster_u64(mapa_of(a.cluster, smem_u32(&sh.xch[slot + 1][rank]), threadIdx.x), (u64)n);
     exchange(slot, as_bits(all));
@@ -370,11 +377,10 @@ struct SampleRow {
       if (q == rank) before = total;
       total += of_bits<A>(sh.xch[slot][q]);
     }
-    const A want = goal(total), up = __shfl_sync(0xffffffffu, inc, max(warp, 1) - 1), start = warp ? before + up : before,
-            end = before + __shfl_sync(0xffffffffu, inc, warp);
+    const A want = goal(total), start = before + front, end = before + own;
     if (want >= start && want < end) {                      // a warp at most
       A left = want - start;
-      int last = -1;                                        // with a term of its own, for a rounding that puts the goal behind the warp's end
+      int last = -1;                                        // with a term of its own, for a rounding that puts the goal behind the lane's end or the warp's
       float last_l = 0.f;
       bool done = false;
       const uint4 *p = vals + (size_t)warp * steps * 32 + lane;
@@ -390,18 +396,24 @@ struct SampleRow {
         const A in = warp_scan<A>(sum), group = __shfl_sync(0xffffffffu, in, 31);
         const unsigned hit = __ballot_sync(0xffffffffu, in > left);
         if (hit) {
-          const A front = __shfl_up_sync(0xffffffffu, in, 1);
-          if (lane == __ffs(hit) - 1) {
-            A run = lane ? front : (A)0;
-            bool mine = false;
-            int id = last;
-            float x = last_l;
+          const A up = __shfl_up_sync(0xffffffffu, in, 1);
+          const int at = __ffs(hit) - 1;
+          bool mine = false;
+          if (lane == at) {
+            A run = lane ? up : (A)0;
+            int id = -1;
+            float x = 0.f;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
               run += v[e];
               if (!mine && run > left) { mine = true; id = i0 + e; x = l[e]; }
             }
-            found(x, id, total);
+            if (mine) found(x, id, total);
+          }
+          // the lanes' sums reach the goal and their terms one by one do not: the last term up to there
+          if (!__any_sync(0xffffffffu, mine)) {
+            const int id = __reduce_max_sync(0xffffffffu, lane <= at ? last : -1);
+            if (lane <= at && id >= 0 && id == last) found(last_l, id, total);
           }
           done = true;
         } else left -= group;

@@ -51,3 +51,36 @@ def test_neighbouring_floats_at_low_temperatures(m, t):
     x[3, 4000:4600] = next_
     for s in ({}, dict(k=[1, 2, 3, 50, 4]), dict(k=[300, 1000, 5000, 400, 19000]), dict(p=[0.1, 0.4, 0.7, 0.9, 0.999]), dict(mp=[0.9, 0.5, 0.1, 0.01, 1e-6])):
         check(x, [0.05, 0.3, 0.6, 0.85, 0.99], t=[t] * 5, **s)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [400, 1074, 3704, 20000, 70002, 200000])
+@pytest.mark.parametrize("min_p", [None, 0.2])
+@pytest.mark.parametrize("mirrored", [False, True])
+def test_goal_on_a_border(mirrored, min_p, V, dtype):
+    """Rows of two halves with the same weights and u = 1 / 2: the goal is the border between them to a rounding, so the token is the last of the first
+    half or the first of the second; it is written, and the same at every run."""
+    from paper_2505_19201_b200 import api
+    R, h = 96, V // 2
+    g = torch.Generator().manual_seed(V)
+    half = torch.where(torch.rand(R, h, generator=g) < torch.rand(R, 1, generator=g) * 0.3, torch.rand(R, h, generator=g) * -3.0, float("-inf"))
+    half[:, h // 2:] = float("-inf")                          # whole warps without a token between the halves
+    half[:, 0] = 0.0
+    x = torch.cat([half, half.flip(1) if mirrored else half], 1).to(dtype).cuda()
+    u = torch.full((R,), 0.5, device="cuda")
+    mp = None if min_p is None else torch.full((R,), min_p, device="cuda")
+    out = []
+    for _ in range(2):
+        tok, lp = torch.full((R,), -9, dtype=torch.int32, device="cuda"), torch.full((R,), 9.0, device="cuda")
+        api.dream_sample(x, u, tok, min_p=mp, logprob=lp)
+        out.append((tok.tolist(), lp.tolist()))
+    assert out[0] == out[1]
+    w = torch.exp(x.cpu().double())
+    w = torch.where(w >= (min_p or 0.0), w, 0.0)
+    for r in range(R):
+        ids = w[r].nonzero()[:, 0]
+        at = ids.numel() // 2
+        tok, lp = out[0][0][r], out[0][1][r]
+        assert tok in (int(ids[at - 1]), int(ids[at])), (r, tok)
+        want = float(torch.log(w[r, tok] / w[r].sum()))
+        assert abs(lp - want) <= abs(want) * 2 ** -24 + 1e-10
