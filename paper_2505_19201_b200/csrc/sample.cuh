@@ -653,7 +653,7 @@ struct SampleRow {
           if (!cut.keeps(l, id)) return false;
           const int i = place(depth(l));
           if (MASS && i < at - 1 && (!twice || i >= 0)) s += weigh.exact(l);
-          return MASS ? i >= at - 1 && i <= at + 1 : i == at;
+          return MASS ? i >= max(at - 1, 0) && i <= at + 1 : i == at;          // what lies in front of the bins is in the mass in front already
         }, [&] { if (MASS) push(11, block_sum(s)); });
     if (rank == 0) {
       bool good = n <= SAMPLE_LIST;

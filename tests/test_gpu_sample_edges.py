@@ -84,3 +84,20 @@ def test_goal_on_a_border(mirrored, min_p, V, dtype):
         assert tok in (int(ids[at - 1]), int(ids[at])), (r, tok)
         want = float(torch.log(w[r, tok] / w[r].sum()))
         assert abs(lp - want) <= abs(want) * 2 ** -24 + 1e-10
+
+
+def test_cut_at_the_first_of_the_finer_bins():
+    """Hundreds of thousands of ties whose approximate mass falls short by a token's weight, a few tokens just in front of a bin's edge, one behind it in
+    which the cut falls, and a full bin after: the first look takes the bin after, and the finer bins' first is where the cut is."""
+    import numpy as np
+    V, step = 262144, np.float32(-1.0 / 128.0)
+    tie = np.float32(-0.78850514)                              # 100.93 bins below the largest: there 2^-17 rounds down the most, by 3.8e-6
+    x, p = np.full((9, V), -np.inf, np.float32), []
+    for r in range(9):
+        n = (240000, 255000, 261000)[r // 3]
+        row = np.concatenate([[0.0], np.full(n, tie), [step * (128 - 0.0004 - 0.00005 * j) for j in range(10)], [step * 128.0005],
+                              [step * (129.1 + 0.003 * j) for j in range(200)]]).astype(np.float32)
+        w = np.exp(row.astype(np.float64))
+        p.append((w[:n + 11].sum() + (0.2, 0.5, 0.8)[r % 3] * w[n + 11]) / w.sum())
+        x[r, :row.size] = np.roll(row, 1000 * r)
+    check(torch.from_numpy(x).cuda(), [0.0, 0.3, 0.5, 0.9, 0.99, 0.1, 0.2, 0.7, 0.8], p=p)
