@@ -323,7 +323,8 @@ dream_status dream_topk_lse_static(const float *logits, int32_t rows, int32_t vo
  * the kept tokens are the first n of the order: at most top_k; only those before which less than top_p of the mass of the top_k has
  * gone by; only those with w >= min_p; the first one in any case, and never a logit of -inf or NaN.  The token is the
  * first kept one, in id order, at which the running sum of w exceeds u times the kept tokens' sum: the rule of
- * dream_accept_sample's final draw.  Sums are exact to about 1e-12 of the row's mass and the same at every run.
+ * dream_accept_sample's final draw.  Sums are good to 2e-12 of the row's mass and the same at every run, weights below e^-700
+ * of the largest counting as none.
  *   temperature, top_k, top_p, min_p : device [rows], each NULL where the batch does not use it (1, all, 1, 0).  By row:
  *            temperature <= 0 takes the first of the order; top_k <= 0 or >= vocab, top_p >= 1, min_p <= 0 switch off; NaN reads as
  *            off (temperature: as 0)

@@ -1712,7 +1712,6 @@ static const char *sample_launch(SampleArgs a, int dtype, int rows, bool truncat
   if (a.cluster == 8 && rows <= 9 && a.vocab > 8 * 8192) a.cluster = 16;
   const int share = (a.vocab + 16 / esz - 1 + a.cluster - 1) / a.cluster, line = dtype == DREAM_BF16 ? 256 : 128, warps = SAMPLE_THREADS / 32;
   a.warp_elems = ((share + warps - 1) / warps + line - 1) / line * line;
-  a.frac_bits = imin(50, 62 - ilog2(a.vocab));
   const size_t smem = (sizeof(SampleShared) + 15) / 16 * 16 + (size_t)warps * a.warp_elems * esz;
   void (*kernel)(SampleArgs) = dtype == DREAM_BF16 ? (truncate ? k_sample<bf16, true> : k_sample<bf16, false>)
                                                    : (truncate ? k_sample<float, true> : k_sample<float, false>);

@@ -7,8 +7,10 @@
 //
 // A token is a whole number, so a row's sums have to be exact enough that no rounding moves a border: an error of 1e-7 of the
 // total, what 32-bit exponentials leave, moves the token of one row in ten where 100000 tokens share the mass.  Weights are
-// therefore taken in double (to 1.3e-12, Weigher).  Lists and histograms add them as 64-bit integers of 2^-s (s such that a whole row of
-// ones fits), whose sums do not depend on their order; the draw and the mass in front of a list add them in double, in one fixed order.
+// therefore taken in double (to 1.3e-12, Weigher).  Lists and histograms add them as 64-bit integers, whose sums do not depend on their order: of
+// 2^-53 of the largest weight in a list (512 of them, half a unit off each: 2.8e-14), in histograms of as small a part as lets the row's mass fit (2^-43
+// of the mass at most).  The draw and the mass in front of a list add them in double, in one fixed order.  All told a border is good to some
+// 2e-12 of the row's mass.
 //
 // A row is read once into shared memory, by one block or a cluster of up to 16 whose blocks exchange through shared memory.  The cut is
 // a logit and the last id kept among its ties.  Ways to it:
@@ -46,7 +48,6 @@ struct SampleArgs {
   const void *logits;
   long long ld;                        // elements from one row to the next
   int vocab, cluster, warp_elems;      // logits per warp, a multiple of 32 vectors of 16 bytes
-  int frac_bits;                       // s: weights are integers of 2^-s
   const float *temperature;            // [rows] each, or null: the values below for every row
   const int *top_k;
   const float *top_p, *min_p, *uniforms;
@@ -103,14 +104,14 @@ template <typename A> __device__ __forceinline__ A of_bits(u64 v);
 template <> __device__ __forceinline__ u64 of_bits<u64>(u64 v) { return v; }
 template <> __device__ __forceinline__ double of_bits<double>(u64 v) { return __longlong_as_double((long long)v); }
 
-// exp((l - m) / T), also as an integer of 2^-s.  2^y by table, as in Tang's table-driven exponential: y = n + j / 32 + r, |r| <= 1 / 64, and 2^r by the
-// Taylor series of e^(r ln 2) to its fourth power (remainder 1.3e-12).  Roundings to integers are additions of a number so large that its
-// last bit is the unit wanted.  Nine operations in double, where a series without a table takes fourteen.
+// exp((l - m) / T), also as an integer.  2^y by table, as in Tang's table-driven exponential: y = n + j / 32 + r, |r| <= 1 / 64, and 2^r by the
+// Taylor series of e^(r ln 2) to its fourth power (remainder 1.3e-12).  The rounding to 1 / 32 is an addition of a number so large that its
+// last bit is 1 / 32.  Nine operations in double, where a series without a table takes fourteen.
 #define SAMPLE_TABLE 32
 struct Weigher {
-  double m, c2, unit;                  // row maximum, log2(e) / T, 2^(52 - s)
-  float cut;                           // below it a weight is less than half a unit; rounded up: raw() has no weights for what lies far below, at
-                                       // a very low temperature the very next float
+  double m, c2, one;                   // row maximum, log2(e) / T, what a weight of 1 is as an integer
+  float cut;                           // below it a weight is less than e^-700 and counts as zero; rounded up: raw() has no weights for what lies
+                                       // farther below, at a very low temperature the very next float
   const double *table;                 // 2^(j / 32), in shared memory
   __device__ __forceinline__ double raw(float l) const {
     const double d = (double)fminf(l, 3.402823466e38f) - m;
@@ -126,7 +127,7 @@ struct Weigher {
   }
   __device__ __forceinline__ double exact(float l) const { const double p = raw(l); return l >= cut ? p : 0.0; }
   __device__ __forceinline__ u64 units(float l) const {
-    const u64 w = (u64)__double_as_longlong(raw(l) + unit) - (u64)__double_as_longlong(unit);
+    const u64 w = __double2ull_rn(raw(l) * one);
     return l >= cut ? w : 0ull;
   }
   // The smallest logit whose weight is above zero in double.
@@ -442,8 +443,17 @@ struct SampleRow {
     return g < 1 ? (u64)1 : g > total ? total : g;
   }
   // Radix selection, three levels down to one key.  By count: the `want` first; by mass: until top_p of the mass is reached.
-  template <bool MASS> __device__ __forceinline__ Cut radix(Cut cut, u64 want, double top_p, const Weigher &weigh) const {
+  template <bool MASS> __device__ __forceinline__ Cut radix(Cut cut, u64 want, double top_p, Weigher weigh, double z = 0.0) const {
     uint32_t prefix = 0;
+    if (MASS) {                                             // z, where it is known: the mass within the cut
+      if (z == 0.0) {
+        each([&](float l, int id) { const double w = weigh.exact(l); z += cut.keeps(l, id) ? w : 0.0; });
+        push(8, block_sum(z));
+        sync_all_of(a.cluster);
+        z = pushed(8);
+      }
+      weigh.one = __hiloint2double((2 * 1023 + 60 - (__double2hiint(z) >> 20)) << 20, 0);      // z units are below 2^61
+    }
     u64 goal = want, ties = 0;
 #pragma unroll 1
     for (int lev = 0; lev < 3; ++lev) {
@@ -638,7 +648,7 @@ struct SampleRow {
       if (MASS) z = pushed(8);
       at = LAST - sh.bin;
       const uint32_t n = MASS ? 3 * (sh.bin_cnt >> 17) : sh.bin_cnt;
-      if (!found_bin || at >= LAST) return radix<MASS>(cut, top_k, top_p, weigh);
+      if (!found_bin || at >= LAST) return radix<MASS>(cut, top_k, top_p, weigh, z);
       if (!MASS) left -= sh.before;
       __syncthreads();
       if (lev || n <= SAMPLE_LIST - 100) break;
@@ -658,7 +668,7 @@ struct SampleRow {
       bool good = n <= SAMPLE_LIST;
       if (good) {
         const double rest = MASS ? top_p * z - (twice ? pushed(9) + pushed(11) : pushed(11)) : 0.0;        // of the listed tokens' mass
-        const u64 units = MASS ? (u64)fmax(0.0, ceil(rest * (4503599627370496.0 / weigh.unit))) : 0ull;
+        const u64 units = MASS ? (u64)fmax(0.0, ceil(rest * weigh.one)) : 0ull;
         const auto r = settle(n, MASS ? (u64)n : left, [&](u64 mass) {
             if (MASS && (rest <= 0.0 || units > mass)) sh.bin = -2;        // the bins were too coarse: the cut is not among them
             return MASS ? units : ~0ull;
@@ -670,7 +680,7 @@ struct SampleRow {
       __syncthreads();
     }
     const Cut found = share_cut(MASS ? 7 : 6);
-    if (found.l == INFINITY && found.id < 0) return radix<MASS>(cut, top_k, top_p, weigh);
+    if (found.l == INFINITY && found.id < 0) return radix<MASS>(cut, top_k, top_p, weigh, z);
     return found;
   }
 };
@@ -701,8 +711,8 @@ k_sample(const __grid_constant__ SampleArgs a) {
   Weigher weigh;
   const bool infinite = m == INFINITY;                      // the infinite ones share the mass
   weigh.table = sh.table;
-  weigh.m = (double)m; weigh.c2 = sh.c2; weigh.unit = __longlong_as_double((long long)(1023 + 52 - a.frac_bits) << 52);
-  weigh.cut = fmaxf(__double2float_ru(weigh.m - (double)(a.frac_bits + 2) * 0.69314718055994531 * (double)temp), -3.402823466e38f);
+  weigh.m = (double)m; weigh.c2 = sh.c2; weigh.one = 0x1p53;      // SAMPLE_LIST ones fit
+  weigh.cut = fmaxf(__double2float_ru(weigh.m - 700.0 * (double)temp), -3.402823466e38f);
   if (infinite) { weigh.m = (double)3.402823466e38f; weigh.cut = INFINITY; }
   auto target = [&](u64 total) { const u64 t = (u64)((double)u * (double)total); return t < total ? t : total - 1; };
   auto draw = [&](float l, int id, double total) {
@@ -734,7 +744,7 @@ k_sample(const __grid_constant__ SampleArgs a) {
           if (rank == 0) {
             const auto r = R.settle(n, (u64)k, [&](u64 mass) { return top_p < 1.f ? SampleRow<T>::mass_goal((double)top_p, mass) : ~0ull; }, least_l, true, weigh);
             if (!TRUNCATE) {
-              R.draw_settled(r, n, u, weigh.least((double)temp), target, [&](float l, int id, u64 total) { draw(l, id, ldexp((double)total, -a.frac_bits)); });
+              R.draw_settled(r, n, u, weigh.least((double)temp), target, [&](float l, int id, u64 total) { draw(l, id, (double)total * 0x1p-53); });
               if (threadIdx.x == 0 && a.kept) a.kept[row] = (int)r.n;
             }
           }
@@ -826,7 +836,7 @@ k_sample(const __grid_constant__ SampleArgs a) {
   auto goal = [&](double total) { return fmin((double)u * total, total * 0.9999999999999999); };
   auto found = [&](float l, int id, double total) { if (u > 0.f) draw(l, id, total); };
   const double total = cut.l == -INFINITY ? R.template locate<double>(4, whole, goal, found) : R.template locate<double>(4, weights, goal, found);
-  if (u == 0.f)                                             // the first kept id with any mass, be it less than a weight can be
+  if (u == 0.f)                                             // the first kept id with any mass in double, be it below e^-700
     R.template locate<u64>(2, [&](const float (&l)[VEC], int i0, u64 (&v)[VEC]) {
                              const double least = weigh.least((double)temp);
 #pragma unroll

@@ -1,5 +1,9 @@
 """Rows and settings at which dream_sample and dream_truncate_logits could go wrong by a rounding, against the definition in float64.  Tokens,
 kept counts and kept sets are equal, not close; logprob within what tests/test_gpu_sample.py derives."""
+import decimal
+import fractions
+import math
+
 import pytest
 import torch
 
@@ -101,3 +105,60 @@ def test_cut_at_the_first_of_the_finer_bins():
         p.append((w[:n + 11].sum() + (0.2, 0.5, 0.8)[r % 3] * w[n + 11]) / w.sum())
         x[r, :row.size] = np.roll(row, 1000 * r)
     check(torch.from_numpy(x).cuda(), [0.0, 0.3, 0.5, 0.9, 0.99, 0.1, 0.2, 0.7, 0.8], p=p)
+
+
+def _exp(x):
+    """e^x as a fraction, to 60 digits."""
+    with decimal.localcontext() as c:
+        c.prec = 60
+        return fractions.Fraction(decimal.Decimal(x).exp())
+
+
+@pytest.mark.parametrize("V", [131072, 200001, 262144])
+@pytest.mark.parametrize("gap,p", [(22, 0.99999), (25, 0.999999), (25, 0.99999994), (19, 0.9999)])
+def test_cut_in_a_far_tail(gap, p, V):
+    """One logit and V - 1 ties far below it that hold little of the mass: r tokens stay where 1 + (r - 2) w < p Z <= 1 + (r - 1) w, all of it in
+    fractions.  The kernel's p Z - 1 may be off by 2e-12 of the mass (half of the borders' room below)."""
+    from paper_2505_19201_b200 import api
+    p = float(torch.tensor(p))
+    w, P = _exp(-gap), fractions.Fraction(p)
+    Z = 1 + (V - 1) * w
+    room = fractions.Fraction(4, 10 ** 12) * Z / w
+    at = (P * Z - 1) / w
+    kept = 1 + max(0, math.ceil(at))
+    assert 1 < kept < V
+    x = torch.zeros(2, V, device="cuda")
+    x[0, V // 3] = x[1, V - 1] = float(gap)
+    n, out, n2 = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros_like(x), torch.zeros(2, dtype=torch.int32, device="cuda")
+    tok = torch.zeros(2, dtype=torch.int32, device="cuda")
+    top_p = torch.full((2,), p, device="cuda")
+    api.dream_sample(x, torch.full((2,), 0.5, device="cuda"), tok, top_p=top_p, kept=n)
+    api.dream_truncate_logits(x, out, top_p=top_p, kept=n2)
+    assert n.tolist() == n2.tolist() and tok.tolist() == [V // 3, V - 1]
+    for r in range(2):
+        assert abs(int(n[r]) - kept) <= math.ceil(room), (int(n[r]), kept)
+        ids = (out[r] > float("-inf")).nonzero()[:, 0].tolist()
+        big = tok.tolist()[r]
+        assert ids == sorted([big] + [i for i in range(int(n[r])) if i != big][:int(n[r]) - 1])
+
+
+@pytest.mark.parametrize("k", [None, 200000])
+@pytest.mark.parametrize("gap,u", [(32, 1e-9), (32, 3e-9), (28, 1e-9), (40, 5e-13), (60, 1e-21)])
+def test_draw_from_a_far_tail(gap, u, k):
+    """The largest logit is the last id, so a small enough u falls among the ties in front of it: token floor(u Z / w).  (Where
+    fewer stay than that, the goal lies in the last one's own weight.)  Sums in double of at most
+    2^18 terms, a thread's 128 in turn: the token's place is good to 1e-12 of itself for the weights and 2^-53 (128 + 16 + 5 + 16) for the sums."""
+    from paper_2505_19201_b200 import api
+    V = 262144
+    u = float(torch.tensor(u))
+    n = (k or V) - 1                                           # ties that stay: the first of them
+    w = _exp(-gap)
+    place = fractions.Fraction(u) * (1 + n * w) / w
+    want = math.floor(place) if place < n else V - 1
+    assert 1e-6 < place % 1 < 1 - 1e-6
+    x = torch.zeros(3, V, device="cuda")
+    x[:, V - 1] = float(gap)
+    tok = torch.zeros(3, dtype=torch.int32, device="cuda")
+    tk = None if k is None else torch.full((3,), k, dtype=torch.int32, device="cuda")
+    api.dream_sample(x, torch.full((3,), u, device="cuda"), tok, top_k=tk)
+    assert tok.tolist() == [want] * 3
