@@ -724,7 +724,8 @@ k_sample(const __grid_constant__ SampleArgs a) {
     bool tried = false;                                     // the bins have been used
     if (min_p > 0.f) {                                      // w >= min_p
       if (min_p > 1.f) k = 1;                               // nothing but the first of the order
-      else least_l = infinite ? m : fminf(__double2float_ru(weigh.m + log((double)min_p) * (double)temp), m);
+      else if (infinite) least_l = m;
+      else if (temp < INFINITY) least_l = fminf(__double2float_ru(weigh.m + log((double)min_p) * (double)temp), m);      // beyond, all weigh 1
     }
     if (k > 0 && k < a.vocab) {
       // Few tokens: a bin of the threads' own maxima, in 2047 steps from the smallest (or 256 below the largest) to the largest, down to which

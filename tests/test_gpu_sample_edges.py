@@ -162,3 +162,16 @@ def test_draw_from_a_far_tail(gap, u, k):
     tk = None if k is None else torch.full((3,), k, dtype=torch.int32, device="cuda")
     api.dream_sample(x, torch.full((3,), u, device="cuda"), tok, top_k=tk)
     assert tok.tolist() == [want] * 3
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [40, 33000])
+def test_min_p_at_an_infinite_temperature(V, dtype):
+    """Every finite logit weighs 1 there, so min_p up to 1 cuts nothing; beside +inf nothing weighs anything."""
+    x = rows(6, V, dtype, seed=21).clone()
+    x[3, ::2] = float("-inf")
+    x[4] = float("-inf")
+    x[5, 3] = float("inf")
+    inf = float("inf")
+    for s in ({}, dict(k=[30, 300, 10, 0, 5, 9]), dict(p=[0.3, 0.9, 0.999, 0.5, 0.5, 0.5])):
+        check(x, [0.1, 0.4, 0.8, 0.5, 0.3, 0.7], t=[inf] * 6, mp=[1.0, 0.3, 1.0, 1.0, 1.0, 1.0], **s)
