@@ -130,8 +130,8 @@ struct Weigher {
     const u64 w = __double2ull_rn(raw(l) * one);
     return l >= cut ? w : 0ull;
   }
-  // The smallest logit whose weight is above zero in double.
-  __device__ __forceinline__ double least(double temp) const { return m - 744.0 * temp; }
+  // The smallest logit whose weight is above zero in double; beside +inf nothing else has any.
+  __device__ __forceinline__ double least(double temp) const { return cut == INFINITY ? (double)INFINITY : m - 744.0 * temp; }
 };
 
 // A cut of the order: larger logits stay, and equal ones up to an id; -inf and NaN never do.

@@ -175,3 +175,15 @@ def test_min_p_at_an_infinite_temperature(V, dtype):
     inf = float("inf")
     for s in ({}, dict(k=[30, 300, 10, 0, 5, 9]), dict(p=[0.3, 0.9, 0.999, 0.5, 0.5, 0.5])):
         check(x, [0.1, 0.4, 0.8, 0.5, 0.3, 0.7], t=[inf] * 6, mp=[1.0, 0.3, 1.0, 1.0, 1.0, 1.0], **s)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [40, 33000])
+def test_the_smallest_draw_beside_infinities(V, dtype):
+    """u = 0 takes the first token with mass, which finite logits have none of where one is +inf, the type's largest value and any temperature included."""
+    inf = float("inf")
+    x = rows(5, V, dtype, seed=22).clone()
+    x[:, 1] = torch.finfo(dtype).max
+    x[:, V // 2] = x[:, V - 1] = inf
+    for s in ({}, dict(k=[1, 2, 5, 30, 300]), dict(k=[10] * 5, mp=[0.5] * 5), dict(p=[0.4, 0.5, 0.6, 0.9, 0.999])):
+        check(x, [0.0] * 5, t=[1.0, 1e30, 1e36, 3e38, inf], **s)
