@@ -365,7 +365,10 @@ dream_status dream_distill_loss(const void *logits, int32_t dtype, int32_t rows,
                                 const float *teacher_logits, int32_t top, const float *teacher_lse, float temperature, float *loss,
                                 float *lse, float *log_rest, const float *row_scale, void *grad, int64_t grad_ld, void *cuda_stream);
 
-/* The gradient on its own, from the lse (and, with teacher_lse, log_rest) that dream_distill_loss left.  Arguments as there. */
+/* The gradient on its own, from the lse (and, with teacher_lse, log_rest) that dream_distill_loss left.  Arguments as there.  Both are floats:
+ * probabilities are off by up to 2^-24 |lse| (and 2^-24 |log_rest| where the rest is one bucket), relative.  Beyond 2^24 they say nothing any
+ * more: a row with such an lse has gradient 0, and with log_rest below -2^24 (all ids that are not entries masked with -1e9, say) those ids
+ * have gradient 0.  dream_distill_loss's own gradient has neither limit. */
 dream_status dream_distill_grad(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, const int32_t *teacher_ids,
                                 const float *teacher_logits, int32_t top, const float *teacher_lse, float temperature, const float *lse,
                                 const float *log_rest, const float *row_scale, void *grad, int64_t grad_ld, void *cuda_stream);

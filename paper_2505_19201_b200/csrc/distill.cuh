@@ -282,6 +282,7 @@ __device__ __forceinline__ void write_row(const RowShare<T> &sr, T *dst, bool ze
 // The side warp is the block's first: of the warps that could go on the oldest does, and as the last one it got a turn every 30 cycles and held
 // the others up (127 us instead of 117).
 #define DISTILL_GRAD_RING 8
+#define DISTILL_SAVED_MAX 16777216.f
 template <int THREADS> __device__ __forceinline__ void block_barrier() { asm volatile("barrier.sync 0, %0;" ::"n"(THREADS) : "memory"); }
 
 template <typename T, bool GRAD, int SW>
@@ -753,7 +754,9 @@ k_distill(const __grid_constant__ DistillArgs a) {
   else blk.stream_warp(reinterpret_cast<uint4 *>(flags + 2 * distill_flag_bytes(a.cta_vecs, SW * 32)) + threadIdx.x - 32);
 }
 
-// The gradient from a saved log-sum-exp (and, with teacher_lse, log_rest).  A CTA walks `cta_vecs` vectors of a row with a ring of copies ahead
+// The gradient from a saved log-sum-exp (and, with teacher_lse, log_rest).  Both are floats, whose rounding, 2^-25 to 2^-24 of their size, is the
+// exponents' error.  Beyond 2^24 that is more than 1/2: a float of -1e9 is off by up to 32, and e^32 of a row that is masked with it would be its
+// gradient.  (The call that makes both in one pass has the sums themselves.)  A CTA walks `cta_vecs` vectors of a row with a ring of copies ahead
 // of it.
 template <typename T>
 __global__ void __launch_bounds__(DISTILL_THREADS, 5)
@@ -770,7 +773,8 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   T *dst = (T *)a.grad + row * a.grad_ld;
   const float rs = a.row_scale ? a.row_scale[row] : 1.f;
   auto none = [](int) { return make_uint4(0u, 0u, 0u, 0u); };
-  if (rs == 0.f || a.lse[row] == -INFINITY) {               // a row of padding is not read
+  // A row of padding is not read; nor is one of which the saved lse says nothing (rows of nothing but logits masked with -1e9, say).
+  if (rs == 0.f || fabsf(a.lse[row]) > DISTILL_SAVED_MAX) {
     write_row<T>(sr, dst, true, none, 0.f, 0.f, 0.0, 0.f, 0.f);
     return;
   }
@@ -791,10 +795,11 @@ k_distill_grad(const __grid_constant__ DistillArgs a) {
   const TeacherRow tr = teacher_row(a, teacher);
   const double scale = tr.total == 0.0 ? 0.0 : (double)rs * a.inv_tau;
   // (p_r Q - q_r) times the id's part of the others, which is no more than 1 however small p_r is: logits relative to tau (lse + ln p_r)
-  const double rest_log = a.teacher_lse && a.log_rest[row] != -INFINITY ? (double)a.log_rest[row] : 0.0, base = lse + rest_log;
+  const bool rest = a.teacher_lse && !(a.log_rest[row] < -DISTILL_SAVED_MAX);
+  const double rest_log = rest ? (double)a.log_rest[row] : 0.0, base = lse + rest_log;
   const float ref = (float)(base / a.inv_tau),
               d = (float)((base - (double)ref * a.inv_tau) * 1.4426950408889634),
-              coef = (float)(scale * (!a.teacher_lse ? tr.total : a.log_rest[row] == -INFINITY ? 0.0 : tr.total * exp(rest_log) - tr.rest));
+              coef = (float)(scale * (!a.teacher_lse ? tr.total : !rest ? 0.0 : tr.total * exp(rest_log) - tr.rest));
   const bool mine = sr.template flag_bit<NT>(t.id, blockIdx.x - row * a.cluster, a.cluster, 0) >= 0 && scale != 0.0;
   float g_top = 0.f;
   if (tid < DISTILL_MAX_TOP) { sq[tid] = t.e * tr.mine(); sid[tid] = t.id; }

@@ -1,0 +1,78 @@
+"""Rows at which the distillation could go wrong: masks by a large finite number, sure students, infinities, against closed forms in float64.
+Tolerances are those that tests/test_gpu_distill.py derives, where nothing else is said."""
+import pytest
+import torch
+
+from tests.test_gpu_distill import close_grad, close_rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("mask", [-1e8, -1e9, None])
+@pytest.mark.parametrize("V,K", [(5, 2), (700, 9), (40000, 31)])
+@pytest.mark.parametrize("tau", [1.0, 0.7, 2.6733145])
+def test_all_but_the_listed_ids_masked_by_a_number(tau, V, K, mask, dtype):
+    """The teacher leaves q_r to ids that the student masks, all alike: p of a listed id is its softmax among the listed, q_r / p_r p_i is q_r over the
+    number of the others.  From a saved log_rest, which is a float, the others' gradient is 0."""
+    from paper_2505_19201_b200 import api
+    R = 6
+    mask = torch.finfo(dtype).min if mask is None else mask
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.full((R, V), mask, dtype=dtype, device="cuda")
+    ids = torch.stack([torch.randperm(V, device="cuda", generator=g)[:K] for _ in range(R)])
+    z = torch.randn(R, K, device="cuda", generator=g).to(dtype)
+    x.scatter_(1, ids, z)
+    top = torch.randn(R, K, device="cuda", generator=g)
+    tau = float(torch.tensor(tau))
+    tl = (torch.logsumexp(top.double() / tau, 1) + 0.8).float()
+    scale = torch.rand(R, device="cuda", generator=g) + 0.5
+    loss, lse, rest = (torch.zeros(R, device="cuda") for _ in range(3))
+    step, back = torch.full_like(x, 3.0), torch.full_like(x, 3.0)
+    api.dream_distill_loss(x, ids.int(), top, loss, lse, teacher_lse=tl, log_rest=rest, temperature=tau, row_scale=scale, grad=step)
+    api.dream_distill_grad(x, ids.int(), top, lse, back, teacher_lse=tl, log_rest=rest, temperature=tau, row_scale=scale)
+    q = torch.exp(top.double() / tau - tl.double()[:, None])
+    qr = 1 - q.sum(1, keepdim=True)
+    p = torch.softmax(z.double() / tau, 1)
+    others = -qr / (V - K) / tau
+    want = others.expand(R, V).clone().scatter_(1, ids, (p - q) / tau).cpu()
+    size = others.abs().expand(R, V).clone().scatter_(1, ids, p / tau).cpu()
+    close_grad(step, want, size, scale, dtype)
+    listed = torch.zeros(R, V, dtype=torch.bool).scatter_(1, ids.cpu(), True)
+    assert not bool(back.cpu()[~listed].any())
+    p = torch.exp(z.double() / tau - lse.double()[:, None])
+    want = torch.zeros(R, V, dtype=torch.float64, device="cuda").scatter_(1, ids, (p - q) / tau).cpu()
+    close_grad(back, want, torch.where(listed, size, 0.0), scale, dtype)
+    close_rows(lse, torch.logsumexp(z.double() / tau, 1).cpu(), "lse")
+    assert bool((loss > 1e7).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("mask", [-1e8, -1e9, None])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("V", [5, 700, 40000])
+def test_every_logit_masked_by_a_number(V, tail, mask, dtype):
+    """The student is uniform; from a saved lse, which is a float, the row has gradient 0."""
+    from paper_2505_19201_b200 import api
+    R, K, tau = 4, 3, 0.7
+    mask = torch.finfo(dtype).min if mask is None else mask
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.full((R, V), mask, dtype=dtype, device="cuda")
+    ids = torch.stack([torch.randperm(V, device="cuda", generator=g)[:K] for _ in range(R)])
+    top = torch.randn(R, K, device="cuda", generator=g)
+    tau = float(torch.tensor(tau))
+    tl = (torch.logsumexp(top.double() / tau, 1) + 0.8).float() if tail else None
+    scale = torch.rand(R, device="cuda", generator=g) + 0.5
+    loss, lse = (torch.zeros(R, device="cuda") for _ in range(2))
+    rest = torch.zeros(R, device="cuda") if tail else None
+    step, back = torch.full_like(x, 3.0), torch.full_like(x, 3.0)
+    api.dream_distill_loss(x, ids.int(), top, loss, lse, teacher_lse=tl, log_rest=rest, temperature=tau, row_scale=scale, grad=step)
+    api.dream_distill_grad(x, ids.int(), top, lse, back, teacher_lse=tl, log_rest=rest, temperature=tau, row_scale=scale)
+    q = torch.exp(top.double() / tau - tl.double()[:, None]) if tail else torch.softmax(top.double() / tau, 1)
+    qr = 1 - q.sum(1, keepdim=True) if tail else torch.zeros(R, 1, dtype=torch.float64, device="cuda")
+    others = (1.0 / V - qr / (V - K)) / tau
+    size = ((1.0 / V + qr / (V - K)) / tau).expand(R, V).clone().scatter_(1, ids, torch.full((R, K), 1.0 / V / tau, dtype=torch.float64, device="cuda"))
+    close_grad(step, others.expand(R, V).clone().scatter_(1, ids, (1.0 / V - q) / tau).cpu(), size.cpu(), scale, dtype)
+    assert not bool(back.any())
+    if tail:
+        close_rows(rest, torch.log(torch.full((R,), (V - K) / V, dtype=torch.float64)), "log_rest")
