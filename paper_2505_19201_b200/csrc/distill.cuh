@@ -494,7 +494,8 @@ struct DistillBlock {
     const int lane = threadIdx.x & 31;
     Sums<double> s = sums<double>(i);
     const DistillSide &d = sh.side[i & 3];
-    s.others *= 1.0 + 5.1e-8;                               // ex2.approx is that much below 2^x in the mean, measured over -28 < x < 0
+    // ex2.approx is 5.1e-8 below 2^x in the mean, measured over -28 < x < 0; the largest logit's own term is 1 and exact
+    s.others += 5.1e-8 * fmax(s.others - 1.0, 0.0);
     const float rm = fmaxf(s.m, s.top_m);
     double total = s.others, log_total = 0.0, p_r = 0.0, log_rest = 0.0, own = 0.0;
     if (a.teacher_lse) {

@@ -76,3 +76,21 @@ def test_every_logit_masked_by_a_number(V, tail, mask, dtype):
     assert not bool(back.any())
     if tail:
         close_rows(rest, torch.log(torch.full((R,), (V - K) / V, dtype=torch.float64)), "log_rest")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,gap,spot", [(1, 0, 0), (2, 40, 1), (5000, 30, 7), (5000, 90, 4999), (150000, 40, 77777)])
+def test_a_student_that_is_sure(V, gap, spot, dtype):
+    """One logit holds the row and the teacher lists it alone: loss = log1p((V - 1) e^-gap).  In the kernel the sum is 1, to which terms below 2^-25
+    are lost within a thread or added by the others: the loss is off by no more than they all are, (V - 1) e^-gap (1 + 2^-20), and the rounding of a sum
+    at 1 in float (2^-24 for each of a warp's five steps, were any of the terms above 2^-25, which none is)."""
+    from paper_2505_19201_b200 import api
+    x = torch.full((3, V), 2.0 - gap, dtype=dtype, device="cuda")
+    x[:, spot] = 2.0
+    ids, top = torch.full((3, 1), spot, dtype=torch.int32, device="cuda"), torch.full((3, 1), 1.0, device="cuda")
+    loss, lse, grad = torch.zeros(3, device="cuda"), torch.zeros(3, device="cuda"), torch.zeros_like(x)
+    rest = (V - 1) * float(torch.exp(torch.tensor(-float(gap), dtype=torch.float64)))
+    for g in (None, grad):
+        api.dream_distill_loss(x, ids, top, loss, lse, grad=g)
+        assert float((loss.double() - rest).abs().max()) <= rest * (1 + 2 ** -20), loss.tolist()
+        assert bool(((lse.double() - 2.0 - rest).abs() <= rest + 2 ** -23).all())
