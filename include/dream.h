@@ -313,6 +313,7 @@ dream_status dream_topk_lse_static(const float *logits, int32_t rows, int32_t vo
 /* Calls on rows of logits.  Like dream_topk_lse_static they need no context and allocate nothing; unlike it they need no scratch
  * either (a row is worked on by one block, or by a cluster of blocks that exchange through shared memory), so calls on
  * several streams, and captured ones, do not meet.  Common to all:
+ *   rows, vocab : at least 1 each (DREAM_E_ARG otherwise: a batch without rows is the caller's to skip)
  *   logits : device [rows][vocab] of dtype (DREAM_F32 or DREAM_BF16), `ld` elements from one row to the next (ld >= vocab); any
  *            alignment to its elements and any vocab up to 262144 (DREAM_E_CAPACITY above), fastest where rows start on 16 bytes
  *   cuda_stream : a cudaStream_t of the current device (NULL = legacy default stream)

@@ -165,9 +165,15 @@ def _bad(msg):
     raise DreamError(-1, msg)
 
 
+def _need(name, t):
+    if t is None:
+        _bad(f"{name} is required")
+
+
 def _rows(name, t, like=None):
     """A matrix of logits: float32 or bfloat16, two dimensions, rows of consecutive elements on a CUDA device.  Returns its address, rows,
     row length, elements from row to row, type and device ordinal."""
+    _need(name, t)
     kind, shape = _ROW_TYPES.get(t.dtype), t.shape
     if kind is None or len(shape) != 2:
         _bad(f"{name} must be float32 or bfloat16 [rows, vocab]")
@@ -191,9 +197,13 @@ def _side(name, t, dtype, shape, dev):
     return t.data_ptr()
 
 
-def _need(name, t):
-    if t is None:
-        _bad(f"{name} is required")
+def _listed(teacher_ids, teacher_logits):
+    """How many entries the teacher has in a row."""
+    _need("teacher_ids", teacher_ids)
+    _need("teacher_logits", teacher_logits)
+    if teacher_ids.dim() != 2:
+        _bad("teacher_ids must be [rows, K]")
+    return teacher_ids.shape[1]
 
 
 def _call_rows(fn, dev, stream, *args):
@@ -218,9 +228,9 @@ def dream_sample(logits, uniforms, tokens, temperature=None, top_k=None, top_p=N
     """A token per row of `logits` [rows, vocab] (float32 or bfloat16; rows may be strided) under temperature, top-k, top-p and
     min-p by row (CUDA tensors [rows]; None: not used) and one uniform number per row.  Outputs are the caller's tensors: tokens
     [rows] int32, logprob [rows] float32, kept [rows] int32."""
-    p, R, V, ld, kind, dev = _rows("logits", logits)
     _need("uniforms", uniforms)
     _need("tokens", tokens)
+    p, R, V, ld, kind, dev = _rows("logits", logits)
     n, f32, i32 = (R,), torch.float32, torch.int32
     _call_rows(lib().dream_sample, dev, stream, p, kind, R, V, ld,
                _side("temperature", temperature, f32, n, dev), _side("top_k", top_k, i32, n, dev), _side("top_p", top_p, f32, n, dev),
@@ -243,13 +253,14 @@ def dream_distill_loss(logits, teacher_ids, teacher_logits, loss, lse, teacher_l
     """Distillation loss per row of a student's `logits` [rows, vocab] against a teacher's top logits (teacher_ids int32 and
     teacher_logits float32, both [rows, K], K <= 128; with teacher_lse [rows] the rest of the vocabulary counts as one bucket and
     log_rest [rows] is an output).  Writes loss and lse [rows] and, if given, grad [rows, vocab] = row_scale * d loss / d logits."""
+    K = _listed(teacher_ids, teacher_logits)
     p, R, V, ld, kind, dev = _rows("logits", logits)
     g, grad_ld = None, 0
     if grad is not None:
         g, _, _, grad_ld, _, _ = _rows("grad", grad, (kind, (R, V), dev))
-    n, f32, nk = (R,), torch.float32, (R, teacher_ids.shape[-1])
+    n, f32, nk = (R,), torch.float32, (R, K)
     _call_rows(lib().dream_distill_loss, dev, stream, p, kind, R, V, ld,
-               _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), nk[1],
+               _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), K,
                _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("loss", loss, f32, n, dev), _side("lse", lse, f32, n, dev),
                _side("log_rest", log_rest, f32, n, dev), _side("row_scale", row_scale, f32, n, dev), g, grad_ld)
 
@@ -258,11 +269,12 @@ def dream_distill_grad(logits, teacher_ids, teacher_logits, lse, grad, teacher_l
                        row_scale=None, stream=None):
     """The backward pass of dream_distill_loss on its own: grad = row_scale * d loss / d logits from the saved lse (and log_rest).
     `grad` may be `logits`."""
+    K = _listed(teacher_ids, teacher_logits)
     p, R, V, ld, kind, dev = _rows("logits", logits)
     g, _, _, grad_ld, _, _ = _rows("grad", grad, (kind, (R, V), dev))
-    n, f32, nk = (R,), torch.float32, (R, teacher_ids.shape[-1])
+    n, f32, nk = (R,), torch.float32, (R, K)
     _call_rows(lib().dream_distill_grad, dev, stream, p, kind, R, V, ld,
-               _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), nk[1],
+               _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), K,
                _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("lse", lse, f32, n, dev),
                _side("log_rest", log_rest, f32, n, dev), _side("row_scale", row_scale, f32, n, dev), g, grad_ld)
 
