@@ -346,8 +346,10 @@ dream_status dream_truncate_logits(const void *logits, int32_t dtype, int32_t ro
                                    const int32_t *top_k, const float *top_p, const float *min_p, void *out, int64_t out_ld,
                                    int32_t *kept, void *cuda_stream);
 
-/* Distillation of a draft from the target's top logits: Kullback-Leibler divergence of a student's rows from a teacher of which the top
- * logits were kept (dream_topk_lse_static makes them).  z = logits / temperature, p = softmax(z), lse = log-sum-exp of z; temperature in
+/* Distillation of a draft from the target's top logits: the Kullback-Leibler divergence KL(teacher || student) over the teacher's kept logits.
+ * (The paper's own recipe, Eqs. 3-4, is not built; its divergence runs the other way, over the whole vocabulary.)  Of up to 128 fp32 rows
+ * dream_topk_lse_static makes up to 16 entries, and a log-sum-exp at temperature 1; longer lists, and the log-sum-exp at another temperature, are
+ * the caller's to make from the target's logits.  z = logits / temperature, p = softmax(z), lse = log-sum-exp of z; temperature in
  * 1e-20..1e20.
  *   teacher_ids int32 [rows][top], teacher_logits float [rows][top] : device, top in 1..128; an id outside [0, vocab) is no entry;
  *            an id may come twice (its probabilities add up)
@@ -360,7 +362,8 @@ dream_status dream_truncate_logits(const void *logits, int32_t dtype, int32_t ro
  *            row_scale[r] * d loss[r] / d logits[r], in the same pass over the row; may be `logits` itself (grad_ld = ld then)
  *   row_scale : device float [rows] (what reaches a row's loss from behind), NULL = 1.  A row with 0 is padding: its gradient is zeros
  *            whatever its logits hold.
- * A row without an entry has loss 0 and gradient 0; a row without a finite logit loss +inf and gradient 0.  A factor of
+ * A row whose entries have no mass at all (no id in range, or nothing but -inf) has loss 0 and gradient 0, with or without teacher_lse; a row
+ * of nothing but -inf loss +inf and gradient 0; a row with a logit of +inf or NaN has loss, lse and gradient NaN.  A factor of
  * temperature^2, where wanted, goes into row_scale. */
 dream_status dream_distill_loss(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, const int32_t *teacher_ids,
                                 const float *teacher_logits, int32_t top, const float *teacher_lse, float temperature, float *loss,

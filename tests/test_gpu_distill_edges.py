@@ -94,3 +94,29 @@ def test_a_student_that_is_sure(V, gap, spot, dtype):
         api.dream_distill_loss(x, ids, top, loss, lse, grad=g)
         assert float((loss.double() - rest).abs().max()) <= rest * (1 + 2 ** -20), loss.tolist()
         assert bool(((lse.double() - 2.0 - rest).abs() <= rest + 2 ** -23).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("V", [60, 20000, 200000])
+def test_rows_with_nan_or_infinity(V, tail, bad, dtype):
+    """They have loss, lse and gradient NaN, wherever the logit stands; the rows beside them are as without them."""
+    from paper_2505_19201_b200 import api
+    from tests.test_gpu_distill import make
+    x, ids, top, tl, scale = make(6, V, 7, dtype, seed=30, tail=tail)
+    outs = []
+    for hurt in (False, True):
+        if hurt:
+            x[1, V - 1] = bad
+            x[3, ids[3, 2].long()] = bad
+            x[4, 0] = bad
+        loss, lse = torch.zeros(6, device="cuda"), torch.zeros(6, device="cuda")
+        rest = torch.zeros(6, device="cuda") if tail else None
+        step, back = torch.full_like(x, 3.0), torch.full_like(x, 3.0)
+        api.dream_distill_loss(x, ids, top, loss, lse, teacher_lse=tl, log_rest=rest, row_scale=scale, grad=step)
+        api.dream_distill_grad(x, ids, top, lse, back, teacher_lse=tl, log_rest=rest, row_scale=scale)
+        outs.append((loss, lse, step, back))
+    for a, b in zip(*outs):
+        assert torch.equal(a[[0, 2, 5]], b[[0, 2, 5]])
+        assert bool(torch.isnan(b[[1, 3, 4]]).all())
