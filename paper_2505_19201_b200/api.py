@@ -382,7 +382,10 @@ class Context:
         _check(self.h, lib().dream_set_tap(self.h, seq, layer))
 
     def dream_sample_first(self, seq, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, first_token=None, logprob=None):
-        """uniform: CUDA float32 tensor with one number in [0, 1)."""
+        """uniform: CUDA float32 tensor with one number in [0, 1).  first_token (int32) and logprob (float32), if given, receive one each."""
+        for name, t, dtype in (("uniform", uniform, torch.float32), ("first_token", first_token, torch.int32), ("logprob", logprob, torch.float32)):
+            if t is not None and (t.dtype is not dtype or t.numel() < 1 or t.device != self.arena.device):
+                _bad(f"{name} must be {dtype} on {self.arena.device}")
         _check(self.h, lib().dream_sample_first(self.h, seq, float(temperature), int(top_k), float(top_p), float(min_p), _ptr(uniform),
                                                 _ptr(first_token), _ptr(logprob)))
 

@@ -22,6 +22,17 @@ def test_what_is_missing_is_named(call, args, name):
     assert e.value.code == -1 and name in str(e.value)
 
 
+@pytest.mark.parametrize("bad", [dict(uniform=U.double()), dict(uniform=U[:0]), dict(uniform=U.to("meta")), dict(first_token=U), dict(logprob=N),
+                                 dict(logprob=U.to("meta"))])
+def test_first_token_checks_its_tensors(bad):
+    from types import SimpleNamespace
+    from paper_2505_19201_b200 import api
+    ctx = SimpleNamespace(h=None, arena=U)
+    with pytest.raises(api.DreamError) as e:
+        api.Context.dream_sample_first(ctx, 0, **{"uniform": U, **bad})
+    assert e.value.code == -1 and next(iter(bad)) in str(e.value)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("call", ["dream_truncate_logits", "dream_distill_loss", "dream_distill_grad"])
 def test_missing_outputs(call):
