@@ -14,8 +14,11 @@
 //
 // A row is read once into shared memory, by one block or a cluster of up to 16 whose blocks exchange through shared memory.  The cut is
 // a logit and the last id kept among its ties.  Ways to it:
-//   few tokens (top_k up to 256, greedy; one row of 32000 at top_k 50: 9.8 us, through the bins below 20): the k-th largest of the threads' own maxima is a bound that little more than k logits pass; those
-//     are listed, and one block settles order, masses, cut and draw on the list.
+//   few tokens (top_k up to 112, greedy): the k-th largest of the threads' own maxima is a bound that little more than k logits pass; those
+//     are listed, and one block settles order, masses, cut and draw on the list.  Against the bins below, by top_k alone: one row of 32000 takes
+//     9.4 us at 50, 10.5 at 64, 13.5 at 112, 19.2 at 128 and 55.7 at 256, through the bins 11.5 to 12.0; 61 rows 13.2, 15.0, 18.2, 25.0 and 66.4,
+//     through the bins 18.2 to 19.7; 64 rows of 131072 30.7, 33.9, 40.3, 53.7 and 132, through the bins 52 to 55.  With a top_p behind it the
+//     bins take half as long again, and the list wins up to 112 everywhere (12.7 against 19.6 us at 96 in one row of 32000).
 //   many: a pass sorts the row into bins of 1 / 128 nat, with counts (top_k) or approximate masses (top_p); the bin in which the cut falls is
 //     listed (a full one is divided once more) and settled exactly, the mass in front of it being summed exactly: the bins only say where to look.
 //   neither list fits (masked rows, rows of ties, logits of an odd scale), or the exact mass contradicts the bins: a radix selection over
@@ -39,7 +42,7 @@
 #define SAMPLE_CHUNKS 32               // of SAMPLE_BINS / 32 bins, a lane each
 #define SAMPLE_EXCHANGES 12
 #define SAMPLE_LIST 512                // listed tokens one block settles
-#define SAMPLE_SMALL_K 256
+#define SAMPLE_SMALL_K 112             // above, the list of what passes the bound is too long to settle
 #define SAMPLE_THREADS 512
 
 typedef unsigned long long u64;

@@ -187,3 +187,12 @@ def test_the_smallest_draw_beside_infinities(V, dtype):
     x[:, V // 2] = x[:, V - 1] = inf
     for s in ({}, dict(k=[1, 2, 5, 30, 300]), dict(k=[10] * 5, mp=[0.5] * 5), dict(p=[0.4, 0.5, 0.6, 0.9, 0.999])):
         check(x, [0.0] * 5, t=[1.0, 1e30, 1e36, 3e38, inf], **s)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [300, 32000, 131072])
+def test_top_k_on_both_sides_of_the_short_list(V, dtype):
+    k = [1, 111, 112, 113, 127, 128, 129, 255, 256, 257]
+    x, u = rows(10, V, dtype, seed=23), [0.05, 0.2, 0.3, 0.4, 0.5, 0.6, 0.7, 0.8, 0.9, 0.97]
+    check(x, u, k=k)
+    check(x, u, k=k, t=[0.7] * 10, p=[0.9] * 10, mp=[0.01] * 10)
