@@ -1,4 +1,4 @@
-"""Calls on rows of logits from several threads at once, each on its own stream: what the library keeps per thread does not mix."""
+"""Calls on rows of logits from several threads at once, each on its own stream: what the library keeps per thread does not mix.  And rows far apart."""
 import threading
 
 import pytest
@@ -48,3 +48,32 @@ def test_threads():
     assert not failed
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_beyond_32_bits(dtype):
+    """Three rows 2^30 elements and a little apart: offsets pass 2^31 elements.  The same as of three rows side by side, bit by bit."""
+    from paper_2505_19201_b200 import api
+    R, V, ld = 3, 20008, 2 ** 30 + 64
+    if torch.cuda.mem_get_info()[0] < 26 << 30:
+        pytest.skip("less than 26 GB free on the device")
+    far = [torch.empty(2 * ld + V, dtype=dtype, device="cuda").as_strided((R, V), (ld, 1)) for _ in range(2)]
+    near = [torch.empty(R, V, dtype=dtype, device="cuda") for _ in range(2)]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(R, V, device="cuda", generator=g) * 2
+    u, tk = torch.rand(R, device="cuda", generator=g), torch.full((R,), 40, dtype=torch.int32, device="cuda")
+    top, ids = torch.topk(x, 9, dim=1)
+    res = []
+    for src, dst in (far, near):
+        src.copy_(x)
+        tok, lp = torch.zeros(R, dtype=torch.int32, device="cuda"), torch.zeros(R, device="cuda")
+        loss, lse = torch.zeros(R, device="cuda"), torch.zeros(R, device="cuda")
+        api.dream_sample(src, u, tok, logprob=lp)
+        out = [tok, lp, loss, lse]
+        for call in (lambda: api.dream_truncate_logits(src, dst, top_k=tk), lambda: api.dream_distill_loss(src, ids.int(), top, loss, lse, grad=dst),
+                     lambda: api.dream_distill_grad(src, ids.int(), top, lse, dst)):
+            dst.fill_(7.0)
+            call()
+            out.append(dst.clone().contiguous())
+        res.append([t.cpu() for t in out])
+    assert all(torch.equal(a, b) for a, b in zip(*res))
