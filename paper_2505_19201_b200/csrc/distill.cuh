@@ -10,8 +10,8 @@
 // Bound by memory: a row is read once (and its gradient written once).  p_r would lose its digits as a difference of sums where the
 // listed ids hold nearly everything, so the ids are marked in a bitmap and the others summed by themselves; the few numbers of the listed
 // ids and of the row are in double.  At 6.45 TB/s of a copy:
-//   4096 rows of 32000 bf16, 16 listed, with gradient: 117 us, 4.5 TB/s; 1024 rows of 262144 bf16: 274 us, 3.9 TB/s
-//   loss alone, 1000 rows of 131072 fp32: 100 us, 5.3 TB/s; 256 rows of 32000 bf16: 10.1 us, a launch and a row's chain of steps
+//   4096 rows of 32000 bf16, 16 listed, with gradient: 116 us, 4.5 TB/s; 1024 rows of 262144 bf16: 270 us, 4.0 TB/s, fp32: 594 us, 3.6 TB/s
+//   loss alone, 1000 rows of 131072 fp32: 102 us, 5.1 TB/s; 256 rows of 32000 bf16: 10.1 us, a launch and a row's chain of steps
 //   gradient alone, 2048 rows of 32000 bf16, a fifth of them padding: 45 us, 5.4 TB/s; 777 rows of 49155 fp32: 60 us, 5.1 TB/s
 // Between 4.5 and 6.45 TB/s stand the turnaround from a row's sums to its gradient and the exponentials (45 % of their units' rate).
 #pragma once

@@ -1704,8 +1704,10 @@ static bool rows_collide(const void *p, long long ld, const void *q, long long q
 // Fills in what follows from the sizes and launches.
 static const char *sample_launch(SampleArgs a, int dtype, int rows, bool truncate, cudaStream_t stream) {
   // 64 KB of the row per CTA, two CTAs per SM, where a cluster of eight holds it so; more CTAs to a row where there are few rows (61 rows of
-  // 32003 bf16 of mixed settings: 41 us, by one CTA each 70).  Sixteen: one row of 262144 at top_p 0.95 takes 65 us, in eight 88; eight rows
-  // 92 and 100; more than nine clusters of sixteen do not fit at once.
+  // 32003 bf16 of mixed settings: 41 us, by one CTA each 70).  Sixteen against eight, us at top_p 0.95: one row of 70000 19.5 and 22.5, of 131072
+  // 28.5 and 35.5, of 262144 38 and 53; eight rows 27.7 and 30.2, 60.7 and 68.7, 80.4 and 89.4; at top_k 50 one row of 70000 10.1 and 10.2, of
+  // 262144 11.6 and 13.2, but eight rows 12.4 and 11.3, 15.7 and 14.3: settings are on the device, and the longer call counts more.  More
+  // than nine clusters of sixteen do not fit at once.
   const int esz = dtype == DREAM_BF16 ? 2 : 4;
   a.cluster = 1;
   while (a.cluster < 8 && (a.vocab > a.cluster * (65536 / esz) || (rows * a.cluster < 148 && a.vocab > a.cluster * 4096))) a.cluster *= 2;

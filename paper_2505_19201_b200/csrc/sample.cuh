@@ -24,13 +24,16 @@
 //   neither list fits (masked rows, rows of ties, logits of an odd scale), or the exact mass contradicts the bins: a radix selection over
 //     order-preserving keys, eleven bits a level, by count or by exact mass, which assumes nothing about the values.
 //
-// What bounds it: not the row's bytes but instructions and, in few rows, the chain of barriers of a cluster.  A temperature alone
-// costs 29 instructions per logit (nine of them in double), a nucleus about 96, every call some 700 to 1600 per warp besides.
+// What bounds it: no unit, but a block's steps one after the other (load, maximum over the cluster, bins, list, weights, draw), of which two blocks
+// per SM overlap part.  Warp instructions for 32 logits, all told, and how often a scheduler issued: a temperature alone 52 (29 in the two passes,
+// nine of them in double; the other 23 are a warp's 730 around its 1024 logits), 49 % of the time; 244 rows cut by top_p 144, 52 %; a nucleus over
+// eight wide rows 185, 32 %.
 //   1 row of 32000, top_k 50, top_p 0.9: 9.8 us, a launch and a chain of cluster barriers (44 with radix levels alone)
-//   8 rows of 262144 fp32, top_p 0.95: 54 to 95 us, by how often the bins have to be divided
-//   61 rows of 32003 bf16, settings mixed by row: 40 us
+//   8 rows of 262144 fp32, top_p 0.95: 64 to 95 us, by how often the bins have to be divided
+//   61 rows of 32003 bf16, settings mixed by row: 37 to 43 us
+//   64 rows of 131072 at top_k 50, top_p 0.9: 31 us, in bf16 19; at top_k 5000: 65 us
 //   256 rows of 131072, a temperature alone: 107 us (1.25 TB/s; 159 with weights by series)
-//   61 rows of 32000 truncated at top_k 40, top_p 0.95: 13.8 us; 244 rows of 131072 at top_p 0.9, min_p 0.002: 278 us
+//   61 rows of 32000 truncated at top_k 40, top_p 0.95: 13.8 us; 244 rows of 131072 at top_p 0.9, min_p 0.002: 264 to 294 us
 // 512 threads and two blocks per SM: one block's barriers pass while the other computes.
 #pragma once
 #include "common.cuh"
@@ -42,7 +45,7 @@
 #define SAMPLE_CHUNKS 32               // of SAMPLE_BINS / 32 bins, a lane each
 #define SAMPLE_EXCHANGES 12
 #define SAMPLE_LIST 512                // listed tokens one block settles
-#define SAMPLE_SMALL_K 112             // above, the list of what passes the bound is too long to settle
+#define SAMPLE_SMALL_K 112             // above, settling the list takes longer than the bins do
 #define SAMPLE_THREADS 512
 
 typedef unsigned long long u64;
