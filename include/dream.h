@@ -51,7 +51,7 @@ enum {
   DREAM_E_DEVICE_TIMEOUT = -6, /* a bounded device-side wait expired */
   DREAM_E_UNSUPPORTED = -7     /* shape or dtype outside what the kernels handle */
 };
-enum { DREAM_F32 = 0, DREAM_BF16 = 1 };
+enum { DREAM_F32 = 0, DREAM_BF16 = 1, DREAM_F16 = 2 };   /* DREAM_F16: the calls on a paged cache only */
 enum { DREAM_TAP_FIXED = 0, DREAM_TAP_ENTROPY_MIN = 1, DREAM_TAP_ENTROPY_MAX = 2 };
 
 /* Shapes and hyper-parameters; plain data, copied by dream_init. */
@@ -376,6 +376,92 @@ dream_status dream_distill_loss(const void *logits, int32_t dtype, int32_t rows,
 dream_status dream_distill_grad(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, const int32_t *teacher_ids,
                                 const float *teacher_logits, int32_t top, const float *teacher_lse, float temperature, const float *lse,
                                 const float *log_rest, const float *row_scale, void *grad, int64_t grad_ld, void *cuda_stream);
+
+/* Calls on a paged cache.  Keys and values that a program keeps itself, in pages of its own, without a context: the rows of a step are appended
+ * (rotated to their positions on the way), and queries attend to them, densely or to selected pages.  Two things that serving a VLM needs and
+ * that dream_verify_tree, whose sequences have nothing in common, does not do: a batch of questions on one image reads the image's keys
+ * once for all (dream_cache_attn, shared_pages), and a query behind a very long context reads only the pages that matter to it (dream_cache_select,
+ * dream_cache_attn_pages).  Common to all:
+ *   cache : HOST struct, copied; its members are device pointers and plain numbers.  Token t of page p, KV head h is head_dim consecutive
+ *            elements at p * page_stride + h * head_stride + t * token_stride of k (v).  Strides are in elements, multiples of 8, in any order, and may leave
+ *            room; k and v 16-byte aligned; no two tokens may share an element.  head_dim 64, 128 or 256; page_tokens a power of two, 16..256; dtype
+ *            DREAM_BF16 or DREAM_F16 (DREAM_E_UNSUPPORTED otherwise).  Token i of sequence s lies in page
+ *            page_table[s * table_stride + i / page_tokens], its place i % page_tokens; entries behind a sequence's last token are not looked at.  A
+ *            sequence holds up to pages_per_seq * page_tokens tokens.  Several sequences may name one page.
+ *   bounds : per page and KV head the smallest and the largest value of each key channel, [n_pages][n_kv_heads][2][head_dim] of dtype, or NULL
+ *            (dream_cache_select needs it).  dream_cache_append writes a page's bounds when it writes the page's last token, from all its tokens as
+ *            they are then; until then they are not looked at, so a page may be rewritten as often as drafted tokens are refused.
+ *   rows, n_heads : at least 1 each; query head h reads KV head h / (n_heads / n_kv_heads); n_heads a multiple of n_kv_heads, at most 128 times it
+ *   q, k_new, v_new, q_out, out : device, rows of heads x head_dim consecutive elements of the cache's dtype, `*_ld` elements from row to row (a multiple
+ *            of 8, at least the row), 16-byte aligned: parts of a fused projection's rows will do
+ *   workspace : device, 256-byte aligned, of the size that dream_cache_attn_bytes (dream_cache_select_bytes) says; what it holds does not
+ *            outlive the call, and two calls that may run at the same time need one each (so do two captured graphs that may)
+ *   status : device int32[2], zeroed by the caller once, or NULL.  Word 0 becomes 1 when a bounded wait in a kernel ran out (word 1: which), 2
+ *            when a sequence, token, position or page number was out of range.  What such a number stands for is left out: rows are not written, keys not seen.
+ *   cuda_stream : a cudaStream_t of the current device (NULL = legacy default stream)
+ * Asynchronous; nothing is allocated; errors are reported through dream_last_error(NULL), before anything is enqueued. */
+typedef struct {
+  void *k, *v;
+  void *bounds;
+  const int32_t *page_table;
+  int64_t page_stride, head_stride, token_stride;
+  int64_t table_stride;
+  int32_t dtype, n_pages, page_tokens, n_kv_heads, head_dim;
+  int32_t n_seqs, pages_per_seq;  /* rows of the page table (at most 4096), and pages in one of them */
+} dream_cache;
+
+/* Rotary factors: table[p][i] = (cos, sin)(p * theta^(-2 i / rot_dim)), float [n_pos][rot_dim / 2][2] on the device, from angles taken in 64 bits. */
+dream_status dream_rope_table(float *table, int32_t n_pos, int32_t rot_dim, float theta, void *cuda_stream);
+
+/* Appends rows: row r is token slots[r] of sequence row_seq[r] (device int32 [rows]; a negative sequence is padding, its row is skipped).  Its queries are
+ * rotated to q_out, its keys rotated into the cache, its values copied there.  The order of the rows is free; no sequence's slot comes twice.
+ *   q, q_out : n_heads x head_dim per row, or both NULL with n_heads = 0; q_out may be q itself (q_out_ld = q_ld then)
+ *   rope : device float [n_pos][rot_dim / 2][2] as dream_rope_table makes it, or NULL (no rotation).  The first rot_dim channels of a head are rotated (a
+ *            multiple of 16, at most head_dim): (a, b) -> (a cos - b sin, b cos + a sin), where a, b are channels i and i + rot_dim / 2, or with
+ *            interleaved != 0 channels 2 i and 2 i + 1; in 32 bits, rounded once.
+ *   positions : device int32 [rows] into rope, NULL = slots (a tree's rows have the position of their depth) */
+dream_status dream_cache_append(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, const void *k_new, int64_t k_ld,
+                                const void *v_new, int64_t v_ld, int32_t rows, const int32_t *row_seq, const int32_t *slots,
+                                const int32_t *positions, const float *rope, int32_t n_pos, int32_t rot_dim, int32_t interleaved,
+                                void *q_out, int64_t q_out_ld, int32_t *status, void *cuda_stream);
+
+/* Bytes of workspace of dream_cache_attn and dream_cache_attn_pages for this many rows.  Host-only. */
+dream_status dream_cache_attn_bytes(const dream_cache *cache, int32_t n_heads, int32_t rows, size_t *bytes);
+
+/* Attention of a ragged batch: out = softmax(scale q K^T) V.  The rows of sequence s are q_start[s] .. q_start[s + 1] - 1 (device int32 [n_seqs + 1],
+ * ascending from 0), T of them, and stand for its last T tokens; kv_len[s] (device int32 [n_seqs]) counts all its tokens, those included.  Row i sees the
+ * tokens up to its own, kv_len - T + i; with tree_mask (device uint32 [rows][4], the layout of dream_tree.mask; T <= 128) the tokens in front of the
+ * T and those of the T whose bit is set.  Rows behind q_start[n_seqs] are left as they were.  A row that sees nothing gets zeros.
+ *   shared_pages : the first so many entries of the page table are the same in every sequence (those of sequence 0 are read): their keys are
+ *            read once for all rows instead of once per sequence.  0: nothing is shared.
+ *   scale : finite, above zero (as a rule head_dim^-1/2)
+ *   lse : device float [rows][n_heads], log-sum-exp of the scaled scores (-inf for a row that sees nothing), or NULL
+ * What lies in a page behind a sequence's last token may be anything, NaN included; the tokens themselves are finite. */
+dream_status dream_cache_attn(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *q_start,
+                              const int32_t *kv_len, int32_t shared_pages, const uint32_t *tree_mask, float scale, void *out, int64_t out_ld,
+                              float *lse, void *workspace, size_t workspace_bytes, int32_t *status, void *cuda_stream);
+
+/* Bytes of workspace of dream_cache_select for this many rows.  Host-only. */
+dream_status dream_cache_select_bytes(const dream_cache *cache, int32_t rows, size_t *bytes);
+
+/* The pages a query attends to.  Row r is token row_pos[r] of sequence row_seq[r] (device int32 [rows]; a negative one is padding: its ids are all -1),
+ * whose own page is row_pos / page_tokens.  Of the pages up to its own it keeps the first keep_first, the last keep_last (at least 1: its own, which may
+ * not be full) and, up to `budget` in all, those with the highest score, which for page p and KV head h is the largest over the group's query heads of
+ *   sum_d max(q_d lo_d, q_d hi_d),  lo and hi the page's bounds: no key of the page has a larger product with q.
+ * Scores are summed in 64 bits and rounded to 32; equal ones go to the lower page.  ids: device int32 [rows][n_kv_heads][budget], ascending, -1 behind the
+ * last.  budget at least keep_first + keep_last, at most 4096; pages_per_seq at most 32768 (DREAM_E_CAPACITY above); cache->bounds is required. */
+dream_status dream_cache_select(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *row_seq,
+                                const int32_t *row_pos, int32_t budget, int32_t keep_first, int32_t keep_last, int32_t *ids,
+                                void *workspace, size_t workspace_bytes, int32_t *status, void *cuda_stream);
+
+/* Attention of each row to the listed pages of its sequence, per KV head: the tokens of these pages up to the row's own, row_pos[r].  ids as
+ * dream_cache_select leaves them, or a program's own: ascending; an id that is negative, past the row's page or not above the one in front of it is no
+ * entry.  A row that sees nothing gets zeros; rows with a negative row_seq are left as they were.  scale, out, lse, workspace as in dream_cache_attn; the tokens in
+ * front of a row's own are finite, what lies behind it in its page may be anything. */
+dream_status dream_cache_attn_pages(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows,
+                                    const int32_t *row_seq, const int32_t *row_pos, const int32_t *ids, int32_t budget, float scale,
+                                    void *out, int64_t out_ld, float *lse, void *workspace, size_t workspace_bytes, int32_t *status,
+                                    void *cuda_stream);
 
 /* Timeline of the context's stream (a measurement hook; Section 4 times whole steps only).
  * buffer: DEVICE array of 2 + 2 * capacity_entries 64-bit words, or NULL to stop tracing.  While

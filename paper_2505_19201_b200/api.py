@@ -13,7 +13,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 
-DREAM_F32, DREAM_BF16 = 0, 1
+DREAM_F32, DREAM_BF16, DREAM_F16 = 0, 1, 2
 MAX_DEPTH = 15
 
 ERRORS = {0: "OK", -1: "E_ARG", -2: "E_STATE", -3: "E_NOMEM", -4: "E_CAPACITY", -5: "E_CUDA",
@@ -42,6 +42,12 @@ class dream_target_weights(C.Structure):
                [("ln_f", C.c_void_p), ("lm_head", C.c_void_p)]
 
 
+class dream_cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "bounds", "page_table")] + \
+               [(n, C.c_int64) for n in ("page_stride", "head_stride", "token_stride", "table_stride")] + \
+               [(n, C.c_int32) for n in ("dtype", "n_pages", "page_tokens", "n_kv_heads", "head_dim", "n_seqs", "pages_per_seq")]
+
+
 DRAFT_TENSORS = ("ln1", "wqkv", "wo", "lnx", "xq", "xkv", "xo", "ln2", "wgu", "wd")
 DRAFT_TENSORS_3 = ("i_ln2", "i_wgu", "i_wd", "f_ln1", "f_wqkv", "f_wo", "f_ln2", "f_wgu", "f_wd")   # draft_blocks = 3 only
 
@@ -63,7 +69,7 @@ def lib():
             raise ImportError(f"{path} is missing: build it with `python -m paper_2505_19201_b200.build` "
                               "(there is no fallback path)")
         L = C.CDLL(path)
-        vp, i32, i32p = C.c_void_p, C.c_int32, C.POINTER(C.c_int32)
+        vp, i32, i64, i32p = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(C.c_int32)
         sig = {
             "dream_tree_nodes": [C.POINTER(dream_config), i32p],
             "dream_arena_bytes": [C.POINTER(dream_config), C.POINTER(C.c_size_t)],
@@ -95,6 +101,13 @@ def lib():
             "dream_truncate_logits": [vp, i32, i32, i32, C.c_int64] + [vp] * 5 + [C.c_int64, vp, vp],
             "dream_distill_loss": [vp, i32, i32, i32, C.c_int64, vp, vp, i32, vp, C.c_float] + [vp] * 5 + [C.c_int64, vp],
             "dream_distill_grad": [vp, i32, i32, i32, C.c_int64, vp, vp, i32, vp, C.c_float] + [vp] * 4 + [C.c_int64, vp],
+            "dream_rope_table": [vp, i32, i32, C.c_float, vp],
+            "dream_cache_append": [vp, vp, i64, i32, vp, i64, vp, i64, i32] + [vp] * 4 + [i32, i32, i32, vp, i64, vp, vp],
+            "dream_cache_attn_bytes": [vp, i32, i32, C.POINTER(C.c_size_t)],
+            "dream_cache_attn": [vp, vp, i64, i32, i32, vp, vp, i32, vp, C.c_float, vp, i64, vp, vp, C.c_size_t, vp, vp],
+            "dream_cache_select_bytes": [vp, i32, C.POINTER(C.c_size_t)],
+            "dream_cache_select": [vp, vp, i64, i32, i32, vp, vp, i32, i32, i32, vp, vp, C.c_size_t, vp, vp],
+            "dream_cache_attn_pages": [vp, vp, i64, i32, i32, vp, vp, vp, i32, C.c_float, vp, i64, vp, vp, C.c_size_t, vp, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -168,6 +181,7 @@ def _bad(msg):
 def _need(name, t):
     if t is None:
         _bad(f"{name} is required")
+    return t
 
 
 def _rows(name, t, like=None):
@@ -277,6 +291,162 @@ def dream_distill_grad(logits, teacher_ids, teacher_logits, lse, grad, teacher_l
                _side("teacher_ids", teacher_ids, torch.int32, nk, dev), _side("teacher_logits", teacher_logits, f32, nk, dev), K,
                _side("teacher_lse", teacher_lse, f32, n, dev), temperature, _side("lse", lse, f32, n, dev),
                _side("log_rest", log_rest, f32, n, dev), _side("row_scale", row_scale, f32, n, dev), g, grad_ld)
+
+
+_CACHE_TYPES = {torch.bfloat16: DREAM_BF16, torch.float16: DREAM_F16}
+
+
+class Cache:
+    """A paged cache that the caller keeps: k and v [n_pages, kv heads, page_tokens, head_dim] (bfloat16 or float16; any strides but the last's, the same
+    in both, so a pool laid out [n_pages, page_tokens, kv heads, head_dim] is passed as its permutation), page_table [n_seqs, pages_per_seq]
+    int32, bounds [n_pages, kv heads, 2, head_dim] or None.  Keeps the tensors alive and the C struct that points at them; the tensors' contents are read
+    by every call anew."""
+
+    def __init__(self, k, v, page_table, bounds=None):
+        for name, t in (("k", k), ("v", v), ("page_table", page_table)):
+            _need(name, t)
+        kind, dev = _CACHE_TYPES.get(k.dtype), k.get_device()
+        if kind is None or k.dim() != 4 or k.stride(3) != 1:
+            _bad("k must be bfloat16 or float16 [n_pages, kv heads, page_tokens, head_dim] with consecutive elements in a head")
+        if dev < 0:
+            _bad("k must be a CUDA tensor")
+        if v.dtype is not k.dtype or v.shape != k.shape or v.get_device() != dev or v.stride() != k.stride():
+            _bad("v must have the type, shape, strides and device of k")
+        if page_table.dtype is not torch.int32 or page_table.dim() != 2 or page_table.get_device() != dev or \
+                (page_table.stride(1) != 1 and page_table.shape[1] > 1):
+            _bad(f"page_table must be int32 [n_seqs, pages_per_seq] on cuda:{dev} with consecutive entries in a row")
+        n, h, pt, d = k.shape
+        self.k, self.v, self.page_table, self.bounds, self.device = k, v, page_table, bounds, dev
+        b = _side("bounds", bounds, k.dtype, (n, h, 2, d), dev)
+        self.heads, self.dim, self.seqs = h, d, page_table.shape[0]
+        self.c = dream_cache(k.data_ptr(), v.data_ptr(), b, page_table.data_ptr(), k.stride(0), k.stride(1), k.stride(2), page_table.stride(0),
+                             kind, n, pt, h, d, page_table.shape[0], page_table.shape[1])
+        self.p = C.addressof(self.c)
+
+    def rows(self, name, t, heads=None):
+        """Address, elements from row to row, rows and heads of a tensor [rows, heads, head_dim] whose heads are consecutive."""
+        _need(name, t)
+        if t.dtype is not self.k.dtype or t.get_device() != self.device or t.dim() != 3:
+            _bad(f"{name} must be {self.k.dtype} [rows, heads, head_dim] on cuda:{self.device}")
+        (R, H, d), (ld, hs, es) = t.shape, t.stride()
+        if d != self.dim or (heads is not None and H != heads):
+            _bad(f"{name} must have {'heads' if heads is None else heads} x {self.dim} elements in a row")
+        if es != 1 or (hs != d and H > 1):
+            _bad(f"{name} must have consecutive heads in a row")
+        return t.data_ptr(), ld if R > 1 else H * d, R, H
+
+
+def _cache(cache):
+    if not isinstance(cache, Cache):
+        _bad("cache must be a Cache")
+    return cache
+
+
+def _workspace(t, dev):
+    _need("workspace", t)
+    if t.get_device() != dev or not t.is_contiguous():
+        _bad(f"workspace must be contiguous on cuda:{dev}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def dream_rope_table(table, theta=10000.0, stream=None):
+    """Fills table [n_pos, rot_dim / 2, 2] float32 with (cos, sin) of p * theta^(-2 i / rot_dim)."""
+    _need("table", table)
+    if table.dtype is not torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous() or table.get_device() < 0:
+        _bad("table must be a contiguous CUDA float32 tensor [n_pos, rot_dim / 2, 2]")
+    _call_rows(lib().dream_rope_table, table.get_device(), stream, table.data_ptr(), table.shape[0], 2 * table.shape[1], theta)
+
+
+def dream_cache_append(cache, q, k_new, v_new, row_seq, slots, q_out, positions=None, rope=None, interleaved=False, status=None, stream=None):
+    """Row r becomes token slots[r] of sequence row_seq[r] (int32 [rows]; a negative sequence is padding): k_new and v_new [rows, kv heads,
+    head_dim] go to the cache, keys rotated by `rope` [n_pos, rot_dim / 2, 2] float32 at positions[r] (None: slots), and q [rows, heads, head_dim],
+    rotated the same, to q_out (q and q_out may be None, or one tensor)."""
+    c = _cache(cache)
+    dev, i32 = c.device, torch.int32
+    kp, k_ld, R, _ = c.rows("k_new", k_new, c.heads)
+    vp, v_ld, Rv, _ = c.rows("v_new", v_new, c.heads)
+    qp = op = None
+    q_ld = o_ld = H = 0
+    if q is not None or q_out is not None:
+        qp, q_ld, Rq, H = c.rows("q", q)
+        op, o_ld, Ro, _ = c.rows("q_out", q_out, H)
+        if Rq != R or Ro != R:
+            _bad("q and q_out must have as many rows as k_new")
+    if Rv != R:
+        _bad("v_new must have as many rows as k_new")
+    n_pos = rot = 0
+    if rope is not None:
+        if rope.dim() != 3 or rope.shape[2] != 2:
+            _bad("rope must be [n_pos, rot_dim / 2, 2]")
+        n_pos, rot = rope.shape[0], 2 * rope.shape[1]
+    _call_rows(lib().dream_cache_append, dev, stream, c.p, qp, q_ld, H, kp, k_ld, vp, v_ld, R, _side("row_seq", _need("row_seq", row_seq), i32, (R,), dev),
+               _side("slots", _need("slots", slots), i32, (R,), dev), _side("positions", positions, i32, (R,), dev),
+               _side("rope", rope, torch.float32, (n_pos, rot // 2, 2), dev), n_pos, rot, int(interleaved), op, o_ld,
+               _side("status", status, i32, (2,), dev))
+
+
+def dream_cache_attn_bytes(cache, rows, n_heads):
+    """Bytes of workspace that dream_cache_attn and dream_cache_attn_pages need for so many rows."""
+    n = C.c_size_t()
+    _check(None, lib().dream_cache_attn_bytes(_cache(cache).p, n_heads, rows, C.byref(n)))
+    return n.value
+
+
+def dream_cache_attn(cache, q, q_start, kv_len, out, workspace, shared_pages=0, tree_mask=None, scale=None, lse=None, status=None, stream=None):
+    """Attention of a ragged batch: rows q_start[s] .. q_start[s + 1] - 1 of q [rows, heads, head_dim] are the last tokens of sequence s, which has
+    kv_len[s] in all; causal, or under tree_mask [rows, 4] int32.  The first shared_pages pages are the same in every sequence and are read once.  out like
+    q; lse [rows, heads] float32 or None; workspace: a CUDA tensor of dream_cache_attn_bytes bytes; scale: head_dim^-1/2 unless given."""
+    c = _cache(cache)
+    dev, i32 = c.device, torch.int32
+    qp, q_ld, R, H = c.rows("q", q)
+    op, o_ld, Ro, _ = c.rows("out", out, H)
+    if Ro != R:
+        _bad("out must have as many rows as q")
+    wp, wn = _workspace(workspace, dev)
+    _call_rows(lib().dream_cache_attn, dev, stream, c.p, qp, q_ld, H, R, _side("q_start", _need("q_start", q_start), i32, (c.seqs + 1,), dev),
+               _side("kv_len", _need("kv_len", kv_len), i32, (c.seqs,), dev), shared_pages, _side("tree_mask", tree_mask, i32, (R, 4), dev),
+               c.dim ** -0.5 if scale is None else scale, op, o_ld, _side("lse", lse, torch.float32, (R, H), dev), wp, wn,
+               _side("status", status, i32, (2,), dev))
+
+
+def dream_cache_select_bytes(cache, rows):
+    """Bytes of workspace that dream_cache_select needs for so many rows."""
+    n = C.c_size_t()
+    _check(None, lib().dream_cache_select_bytes(_cache(cache).p, rows, C.byref(n)))
+    return n.value
+
+
+def dream_cache_select(cache, q, row_seq, row_pos, ids, workspace, keep_first=1, keep_last=1, status=None, stream=None):
+    """The pages that each row of q, token row_pos[r] of sequence row_seq[r], attends to: ids [rows, kv heads, budget] int32, ascending, -1 behind the
+    last; the first keep_first pages, the last keep_last, and those whose bounds allow the largest scores."""
+    c = _cache(cache)
+    dev, i32 = c.device, torch.int32
+    qp, q_ld, R, H = c.rows("q", q)
+    _need("ids", ids)
+    if ids.dim() != 3:
+        _bad("ids must be [rows, kv heads, budget]")
+    wp, wn = _workspace(workspace, dev)
+    _call_rows(lib().dream_cache_select, dev, stream, c.p, qp, q_ld, H, R, _side("row_seq", _need("row_seq", row_seq), i32, (R,), dev),
+               _side("row_pos", _need("row_pos", row_pos), i32, (R,), dev), ids.shape[2], keep_first, keep_last,
+               _side("ids", ids, i32, (R, c.heads, ids.shape[2]), dev), wp, wn, _side("status", status, i32, (2,), dev))
+
+
+def dream_cache_attn_pages(cache, q, row_seq, row_pos, ids, out, workspace, scale=None, lse=None, status=None, stream=None):
+    """Attention of each row, token row_pos[r] of sequence row_seq[r], to the tokens up to its own in the pages ids [rows, kv heads, budget] lists."""
+    c = _cache(cache)
+    dev, i32 = c.device, torch.int32
+    qp, q_ld, R, H = c.rows("q", q)
+    op, o_ld, Ro, _ = c.rows("out", out, H)
+    if Ro != R:
+        _bad("out must have as many rows as q")
+    _need("ids", ids)
+    if ids.dim() != 3:
+        _bad("ids must be [rows, kv heads, budget]")
+    wp, wn = _workspace(workspace, dev)
+    _call_rows(lib().dream_cache_attn_pages, dev, stream, c.p, qp, q_ld, H, R, _side("row_seq", _need("row_seq", row_seq), i32, (R,), dev),
+               _side("row_pos", _need("row_pos", row_pos), i32, (R,), dev), _side("ids", ids, i32, (R, c.heads, ids.shape[2]), dev), ids.shape[2],
+               c.dim ** -0.5 if scale is None else scale, op, o_ld, _side("lse", lse, torch.float32, (R, H), dev), wp, wn,
+               _side("status", status, i32, (2,), dev))
 
 
 class Tree:

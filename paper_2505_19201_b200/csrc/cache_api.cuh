@@ -1,0 +1,249 @@
+// Entry points on a paged cache that a program holds itself (dream.h): checks on the host, then launches.  Part of dream_api.cu.
+#pragma once
+#include "cache_attn.cuh"
+#include "cache_rows.cuh"
+
+#define CACHE_MAX_ROWS (1 << 20)
+#define CACHE_MAX_SEQS 4096
+#define CACHE_MAX_BUDGET 4096
+#define CACHE_MAX_SELECT 32768             // pages of a sequence that dream_cache_select chooses from
+
+// The view of a cache, or what is wrong with it.
+static dream_status cache_view(const char *who, const dream_cache *c, CacheView *v) {
+  if (!c) return fail(nullptr, DREAM_E_ARG, "%s: null cache", who);
+  if (c->dtype != DREAM_BF16 && c->dtype != DREAM_F16) return fail(nullptr, DREAM_E_UNSUPPORTED, "%s: the cache's dtype must be DREAM_BF16 or DREAM_F16", who);
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return fail(nullptr, DREAM_E_UNSUPPORTED, "%s: head_dim must be 64, 128 or 256", who);
+  if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1)))
+    return fail(nullptr, DREAM_E_UNSUPPORTED, "%s: page_tokens must be a power of two in 16..256", who);
+  if (!c->k || !c->v || !c->page_table) return fail(nullptr, DREAM_E_ARG, "%s: null k, v or page_table", who);
+  if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->bounds) & 15) return fail(nullptr, DREAM_E_ARG, "%s: k, v and bounds must be 16-byte aligned", who);
+  if ((uintptr_t)c->page_table & 3) return fail(nullptr, DREAM_E_ARG, "%s: page_table is not aligned to its elements", who);
+  if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_seqs < 1 || c->pages_per_seq < 1) return fail(nullptr, DREAM_E_ARG, "%s: n_pages, n_kv_heads, n_seqs and pages_per_seq must be positive", who);
+  if (c->n_seqs > CACHE_MAX_SEQS) return fail(nullptr, DREAM_E_CAPACITY, "%s: n_seqs above %d", who, CACHE_MAX_SEQS);
+  if (c->n_kv_heads > 1024) return fail(nullptr, DREAM_E_CAPACITY, "%s: n_kv_heads above 1024", who);
+  if (c->pages_per_seq > (1 << 30) / c->page_tokens) return fail(nullptr, DREAM_E_CAPACITY, "%s: a sequence of more than 2^30 tokens", who);
+  if (c->n_seqs > 1 && c->table_stride < c->pages_per_seq) return fail(nullptr, DREAM_E_ARG, "%s: rows of the page table overlap", who);
+  // tokens of head_dim elements each in three directions, none of which may step into what the ones below it hold
+  long long stride[3] = {c->token_stride, c->head_stride, c->page_stride}, count[3] = {c->page_tokens, c->n_kv_heads, c->n_pages};
+  for (int i = 0; i < 3; ++i) {
+    if (count[i] == 1) stride[i] = 0;                    // never stepped along
+    else if (stride[i] < 1 || stride[i] % 8 || stride[i] >= 1LL << 38) return fail(nullptr, DREAM_E_ARG, "%s: strides must be positive multiples of 8 elements", who);
+  }
+  for (int i = 1; i < 3; ++i)
+    for (int j = i; j > 0 && stride[j] < stride[j - 1]; --j) {
+      long long t = stride[j]; stride[j] = stride[j - 1]; stride[j - 1] = t;
+      t = count[j]; count[j] = count[j - 1]; count[j - 1] = t;
+    }
+  long long room = c->head_dim;
+  for (int i = 0; i < 3; ++i) {
+    if (count[i] == 1) continue;
+    if (stride[i] < room) return fail(nullptr, DREAM_E_ARG, "%s: the strides make tokens overlap", who);
+    room = stride[i] * (count[i] - 1) + room;
+  }
+  v->k = c->k; v->v = c->v; v->bounds = c->bounds; v->page_table = c->page_table;
+  v->page_stride = c->n_pages > 1 ? c->page_stride : room; v->head_stride = c->n_kv_heads > 1 ? c->head_stride : c->head_dim;
+  v->token_stride = c->token_stride; v->table_stride = c->table_stride;
+  v->n_pages = c->n_pages; v->page_tokens = c->page_tokens; v->hkv = c->n_kv_heads; v->n_seqs = c->n_seqs; v->pages_per_seq = c->pages_per_seq;
+  v->page_shift = 0;
+  while (1 << v->page_shift < c->page_tokens) ++v->page_shift;
+  return DREAM_OK;
+}
+static dream_status cache_heads(const char *who, const dream_cache *c, int rows, int n_heads) {
+  if (rows < 1) return fail(nullptr, DREAM_E_ARG, "%s: rows = %d must be positive", who, rows);
+  if (rows > CACHE_MAX_ROWS) return fail(nullptr, DREAM_E_CAPACITY, "%s: rows = %d above %d", who, rows, CACHE_MAX_ROWS);
+  if (n_heads < 1 || n_heads % c->n_kv_heads) return fail(nullptr, DREAM_E_ARG, "%s: n_heads = %d is no multiple of n_kv_heads = %d", who, n_heads, c->n_kv_heads);
+  if (n_heads / c->n_kv_heads > 128) return fail(nullptr, DREAM_E_UNSUPPORTED, "%s: more than 128 query heads per KV head", who);
+  return DREAM_OK;
+}
+// A matrix of rows of heads x head_dim elements.
+static dream_status cache_rows(const char *who, const char *name, const void *p, long long ld, long long width) {
+  if (!p) return fail(nullptr, DREAM_E_ARG, "%s: %s is required", who, name);
+  if ((uintptr_t)p & 15) return fail(nullptr, DREAM_E_ARG, "%s: %s must be 16-byte aligned", who, name);
+  if (ld < width || ld % 8 || ld >= 1LL << 38) return fail(nullptr, DREAM_E_ARG, "%s: %s has rows of %lld elements, %lld apart (a multiple of 8, at least the row)", who, name, width, ld);
+  return DREAM_OK;
+}
+static dream_status cache_ints(const char *who, const char *name, const void *p, bool needed) {
+  if (!p && needed) return fail(nullptr, DREAM_E_ARG, "%s: %s is required", who, name);
+  if ((uintptr_t)p & 3) return fail(nullptr, DREAM_E_ARG, "%s: %s is not aligned to its elements", who, name);
+  return DREAM_OK;
+}
+static dream_status cache_workspace(const char *who, const void *p, size_t have, size_t need) {
+  if (!p && need) return fail(nullptr, DREAM_E_ARG, "%s: workspace is required", who);
+  if ((uintptr_t)p & 255) return fail(nullptr, DREAM_E_ARG, "%s: workspace must be 256-byte aligned", who);
+  if (have < need) return fail(nullptr, DREAM_E_NOMEM, "%s: workspace needs %zu bytes, got %zu", who, need, have);
+  return DREAM_OK;
+}
+template <typename A>
+static const char *cache_launch(void (*kernel)(A), dim3 grid, int threads, size_t smem, cudaStream_t stream, const A &args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = pdl_on() ? 1 : 0;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args);
+  if (e == cudaSuccess) return nullptr;
+  cudaGetLastError();
+  return cudaGetErrorString(e);
+}
+
+extern "C" dream_status dream_rope_table(float *table, int32_t n_pos, int32_t rot_dim, float theta, void *cuda_stream) {
+  if (!table || (uintptr_t)table & 15) return fail(nullptr, DREAM_E_ARG, "dream_rope_table: table must be 16-byte aligned device memory");
+  if (n_pos < 1 || rot_dim < 16 || rot_dim > 256 || rot_dim % 16) return fail(nullptr, DREAM_E_ARG, "dream_rope_table: n_pos must be positive and rot_dim a multiple of 16 in 16..256");
+  if (!(theta > 0.f) || isinf(theta)) return fail(nullptr, DREAM_E_ARG, "dream_rope_table: theta must be finite and above zero");
+  k_rope_table<<<n_pos, 128, 0, (cudaStream_t)cuda_stream>>>((float2 *)table, rot_dim, theta);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? fail(nullptr, DREAM_E_CUDA, "dream_rope_table: %s", cudaGetErrorString(e)) : DREAM_OK;
+}
+
+extern "C" dream_status dream_cache_append(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, const void *k_new, int64_t k_ld,
+                                           const void *v_new, int64_t v_ld, int32_t rows, const int32_t *row_seq, const int32_t *slots,
+                                           const int32_t *positions, const float *rope, int32_t n_pos, int32_t rot_dim, int32_t interleaved,
+                                           void *q_out, int64_t q_out_ld, int32_t *status, void *cuda_stream) {
+  static const char who[] = "dream_cache_append";
+  CacheAppendArgs a = {};
+  dream_status s = cache_view(who, cache, &a.c);
+  if (s) return s;
+  const int hd = cache->head_dim;
+  if (!q != !q_out || (n_heads == 0) != !q) return fail(nullptr, DREAM_E_ARG, "%s: q, q_out and n_heads go together", who);
+  s = cache_heads(who, cache, rows, q ? n_heads : cache->n_kv_heads);
+  if (!s && q) s = cache_rows(who, "q", q, q_ld, (long long)n_heads * hd);
+  if (!s && q) s = cache_rows(who, "q_out", q_out, q_out_ld, (long long)n_heads * hd);
+  if (!s) s = cache_rows(who, "k_new", k_new, k_ld, (long long)cache->n_kv_heads * hd);
+  if (!s) s = cache_rows(who, "v_new", v_new, v_ld, (long long)cache->n_kv_heads * hd);
+  if (!s) s = cache_ints(who, "row_seq", row_seq, true);
+  if (!s) s = cache_ints(who, "slots", slots, true);
+  if (!s) s = cache_ints(who, "positions", positions, false);
+  if (!s) s = cache_ints(who, "status", status, false);
+  if (s) return s;
+  if (rope) {
+    if ((uintptr_t)rope & 15) return fail(nullptr, DREAM_E_ARG, "%s: rope must be 16-byte aligned", who);
+    if (n_pos < 1) return fail(nullptr, DREAM_E_ARG, "%s: n_pos must be positive", who);
+    if (rot_dim < 16 || rot_dim > hd || rot_dim % 16) return fail(nullptr, DREAM_E_ARG, "%s: rot_dim must be a multiple of 16 up to head_dim", who);
+  }
+  if (q && rows_collide(q, q_ld, q_out, q_out_ld, DREAM_BF16, rows, n_heads * hd)) return fail(nullptr, DREAM_E_ARG, "%s: q_out overlaps q without being q", who);
+  a.q = q; a.q_ld = q_ld; a.k_new = k_new; a.k_ld = k_ld; a.v_new = v_new; a.v_ld = v_ld; a.q_out = q_out; a.q_out_ld = q_out_ld;
+  a.row_seq = row_seq; a.slots = slots; a.positions = positions; a.rope = (const float2 *)rope; a.rows = rows; a.heads = q ? n_heads : 0; a.hd = hd;
+  a.n_pos = n_pos; a.rot = rope ? rot_dim : 0; a.interleaved = interleaved != 0; a.status = status;
+  a.main_blocks = ((a.heads + 2 * a.c.hkv) * (hd / 16) + CACHE_THREADS - 1) / CACHE_THREADS;
+  const char *why = cache_launch(cache->dtype == DREAM_BF16 ? k_cache_append<bf16> : k_cache_append<f16>,
+                                 dim3(rows, a.main_blocks + (a.c.bounds ? a.c.hkv : 0)), CACHE_THREADS, 0, (cudaStream_t)cuda_stream, a);
+  return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
+}
+
+extern "C" dream_status dream_cache_select_bytes(const dream_cache *cache, int32_t rows, size_t *bytes) {
+  CacheView v;
+  dream_status s = cache_view("dream_cache_select_bytes", cache, &v);
+  if (!s) s = cache_heads("dream_cache_select_bytes", cache, rows, cache->n_kv_heads);
+  if (s) return s;
+  if (!bytes) return fail(nullptr, DREAM_E_ARG, "dream_cache_select_bytes: null argument");
+  *bytes = (size_t)rows * v.hkv * v.pages_per_seq * sizeof(uint32_t);
+  return DREAM_OK;
+}
+
+extern "C" dream_status dream_cache_select(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *row_seq,
+                                           const int32_t *row_pos, int32_t budget, int32_t keep_first, int32_t keep_last, int32_t *ids,
+                                           void *workspace, size_t workspace_bytes, int32_t *status, void *cuda_stream) {
+  static const char who[] = "dream_cache_select";
+  CacheSelectArgs a = {};
+  size_t need = 0;
+  dream_status s = cache_view(who, cache, &a.c);
+  if (!s) s = cache_heads(who, cache, rows, n_heads);
+  if (!s) s = cache_rows(who, "q", q, q_ld, (long long)n_heads * cache->head_dim);
+  if (!s) s = cache_ints(who, "row_seq", row_seq, true);
+  if (!s) s = cache_ints(who, "row_pos", row_pos, true);
+  if (!s) s = cache_ints(who, "ids", ids, true);
+  if (!s) s = cache_ints(who, "status", status, false);
+  if (s) return s;
+  if (!cache->bounds) return fail(nullptr, DREAM_E_ARG, "%s: the cache has no bounds", who);
+  if (keep_first < 0 || keep_last < 1 || keep_first > CACHE_MAX_BUDGET || keep_last > CACHE_MAX_BUDGET || budget < keep_first + keep_last)
+    return fail(nullptr, DREAM_E_ARG, "%s: budget = %d must hold keep_first = %d >= 0 and keep_last = %d >= 1", who, budget, keep_first, keep_last);
+  if (budget > CACHE_MAX_BUDGET) return fail(nullptr, DREAM_E_CAPACITY, "%s: budget above %d", who, CACHE_MAX_BUDGET);
+  if (cache->pages_per_seq > CACHE_MAX_SELECT) return fail(nullptr, DREAM_E_CAPACITY, "%s: pages_per_seq above %d", who, CACHE_MAX_SELECT);
+  s = dream_cache_select_bytes(cache, rows, &need);
+  if (!s) s = cache_workspace(who, workspace, workspace_bytes, need);
+  if (s) return s;
+  a.q = q; a.q_ld = q_ld; a.row_seq = row_seq; a.row_pos = row_pos; a.group = n_heads / a.c.hkv; a.hd = cache->head_dim;
+  a.budget = budget; a.keep_first = keep_first; a.keep_last = keep_last; a.keys = (uint32_t *)workspace; a.ids = ids; a.status = status;
+  const char *why = nullptr;
+  if (a.c.pages_per_seq > budget)
+    why = cache_launch(cache->dtype == DREAM_BF16 ? k_cache_scores<bf16> : k_cache_scores<f16>,
+                       dim3(rows * a.c.hkv, (a.c.pages_per_seq + SCORE_PAGES - 1) / SCORE_PAGES), CACHE_THREADS, 0, (cudaStream_t)cuda_stream, a);
+  if (!why) why = cache_launch(k_cache_select, dim3(rows * a.c.hkv), SELECT_THREADS, 0, (cudaStream_t)cuda_stream, a);
+  return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
+}
+
+extern "C" dream_status dream_cache_attn_bytes(const dream_cache *cache, int32_t n_heads, int32_t rows, size_t *bytes) {
+  CacheView v;
+  dream_status s = cache_view("dream_cache_attn_bytes", cache, &v);
+  if (!s) s = cache_heads("dream_cache_attn_bytes", cache, rows, n_heads);
+  if (s) return s;
+  if (!bytes) return fail(nullptr, DREAM_E_ARG, "dream_cache_attn_bytes: null argument");
+  *bytes = 256;
+  return DREAM_OK;
+}
+
+// What both attention calls ask for.
+static dream_status cache_attn_args(const char *who, const dream_cache *cache, CacheAttnArgs *a, const void *q, long long q_ld, int n_heads, int rows, float scale,
+                                    void *out, long long out_ld, float *lse, const void *workspace, size_t workspace_bytes, int *status) {
+  size_t need = 0;
+  dream_status s = cache_view(who, cache, &a->c);
+  if (!s) s = cache_heads(who, cache, rows, n_heads);
+  if (!s) s = cache_rows(who, "q", q, q_ld, (long long)n_heads * cache->head_dim);
+  if (!s) s = cache_rows(who, "out", out, out_ld, (long long)n_heads * cache->head_dim);
+  if (!s) s = cache_ints(who, "lse", lse, false);
+  if (!s) s = cache_ints(who, "status", status, false);
+  if (s) return s;
+  if (!(scale > 0.f) || isinf(scale)) return fail(nullptr, DREAM_E_ARG, "%s: scale must be finite and above zero", who);
+  if (rows_collide(q, q_ld, out, out_ld, DREAM_BF16, rows, n_heads * cache->head_dim) || q == out)
+    return fail(nullptr, DREAM_E_ARG, "%s: out overlaps q", who);
+  s = dream_cache_attn_bytes(cache, n_heads, rows, &need);
+  if (!s) s = cache_workspace(who, workspace, workspace_bytes, need);
+  if (s) return s;
+  a->q = q; a->q_ld = q_ld; a->out = out; a->out_ld = out_ld; a->lse = lse; a->rows = rows; a->heads = n_heads; a->group = n_heads / a->c.hkv;
+  a->scale_log2 = scale * 1.4426950408889634f; a->status = status;
+  return DREAM_OK;
+}
+template <bool PAGES>
+static const char *cache_attn_launch(const dream_cache *cache, const CacheAttnArgs &a, cudaStream_t stream) {
+  void (*kernel)(CacheAttnArgs) = nullptr;
+  const bool b = cache->dtype == DREAM_BF16;
+  if (cache->head_dim == 64) kernel = b ? k_cache_attn<bf16, 64, PAGES> : k_cache_attn<f16, 64, PAGES>;
+  else if (cache->head_dim == 128) kernel = b ? k_cache_attn<bf16, 128, PAGES> : k_cache_attn<f16, 128, PAGES>;
+  else kernel = b ? k_cache_attn<bf16, 256, PAGES> : k_cache_attn<f16, 256, PAGES>;
+  return cache_launch(kernel, dim3(a.rows, a.heads), 128, 0, stream, a);
+}
+
+extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *q_start,
+                                         const int32_t *kv_len, int32_t shared_pages, const uint32_t *tree_mask, float scale, void *out, int64_t out_ld,
+                                         float *lse, void *workspace, size_t workspace_bytes, int32_t *status, void *cuda_stream) {
+  static const char who[] = "dream_cache_attn";
+  CacheAttnArgs a = {};
+  dream_status s = cache_attn_args(who, cache, &a, q, q_ld, n_heads, rows, scale, out, out_ld, lse, workspace, workspace_bytes, status);
+  if (!s) s = cache_ints(who, "q_start", q_start, true);
+  if (!s) s = cache_ints(who, "kv_len", kv_len, true);
+  if (!s) s = cache_ints(who, "tree_mask", tree_mask, false);
+  if (s) return s;
+  if (shared_pages < 0 || shared_pages > cache->pages_per_seq) return fail(nullptr, DREAM_E_ARG, "%s: shared_pages = %d outside 0..pages_per_seq = %d", who, shared_pages, cache->pages_per_seq);
+  a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask;
+  const char *why = cache_attn_launch<false>(cache, a, (cudaStream_t)cuda_stream);
+  return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
+}
+
+extern "C" dream_status dream_cache_attn_pages(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows,
+                                               const int32_t *row_seq, const int32_t *row_pos, const int32_t *ids, int32_t budget, float scale,
+                                               void *out, int64_t out_ld, float *lse, void *workspace, size_t workspace_bytes, int32_t *status,
+                                               void *cuda_stream) {
+  static const char who[] = "dream_cache_attn_pages";
+  CacheAttnArgs a = {};
+  dream_status s = cache_attn_args(who, cache, &a, q, q_ld, n_heads, rows, scale, out, out_ld, lse, workspace, workspace_bytes, status);
+  if (!s) s = cache_ints(who, "row_seq", row_seq, true);
+  if (!s) s = cache_ints(who, "row_pos", row_pos, true);
+  if (!s) s = cache_ints(who, "ids", ids, true);
+  if (s) return s;
+  if (budget < 1) return fail(nullptr, DREAM_E_ARG, "%s: budget = %d must be positive", who, budget);
+  if (budget > CACHE_MAX_BUDGET) return fail(nullptr, DREAM_E_CAPACITY, "%s: budget above %d", who, CACHE_MAX_BUDGET);
+  a.row_seq = row_seq; a.row_pos = row_pos; a.ids = ids; a.budget = budget;
+  const char *why = cache_attn_launch<true>(cache, a, (cudaStream_t)cuda_stream);
+  return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
+}

@@ -2,10 +2,12 @@
 // reductions, the split-output descriptor every GEMM consumer reads through.
 #pragma once
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
 typedef __nv_bfloat16 bf16;
+typedef __half f16;                   // the calls on a paged cache only
 
 #define DREAM_MAX_BATCH 8          // sequences one call may list
 
@@ -28,6 +30,8 @@ __device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
 template <typename T> __device__ __forceinline__ T from_f(float v);
 template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16_rn(v); }
+__device__ __forceinline__ float to_f(f16 v) { return __half2float(v); }
+template <> __device__ __forceinline__ f16 from_f<f16>(float v) { return __float2half_rn(v); }
 
 // Programmatic dependent launch: a kernel may start while its predecessor in the stream is still
 // running; pdl_wait() blocks until the predecessor has completed and its writes are visible, and
@@ -87,9 +91,14 @@ enum {
   TR_k_truncate,
   TR_k_distill,
   TR_k_distill_grad,
+  TR_k_cache_append,
+  TR_k_cache_attn,
+  TR_k_cache_merge,
+  TR_k_cache_scores,
+  TR_k_cache_select,
   TR_count
 };
-#define DREAM_TRACE_NAMES {"none", "k_embed", "k_build_prompt", "k_resid", "k_qkv_post_target", "k_qkv_post_draft", "k_gemm_to_q", "k_mem_append", "k_silu_mul", "k_gather_rows", "k_topk_lse", "k_attn_prefill", "k_entropy_mean", "k_colsum", "k_attn_tree", "k_attn_draft", "k_attn_tc", "k_attn_combine", "k_draft_begin", "k_tree_expand", "k_tree_finalize", "k_verify_setup", "k_accept", "k_compact_kv", "k_accept_rows", "k_select_tap", "k_select_visual", "k_ctx_rows", "k_gemm_simt", "k_iota_rows", "k_set_seq", "k_set_int", "k_set_pages", "k_first_token", "k_argmax_out", "k_copy_f32", "k_split_rows", "k_gemm_collect", "k_gemm_tc", "k_sample", "k_truncate", "k_distill", "k_distill_grad"}
+#define DREAM_TRACE_NAMES {"none", "k_embed", "k_build_prompt", "k_resid", "k_qkv_post_target", "k_qkv_post_draft", "k_gemm_to_q", "k_mem_append", "k_silu_mul", "k_gather_rows", "k_topk_lse", "k_attn_prefill", "k_entropy_mean", "k_colsum", "k_attn_tree", "k_attn_draft", "k_attn_tc", "k_attn_combine", "k_draft_begin", "k_tree_expand", "k_tree_finalize", "k_verify_setup", "k_accept", "k_compact_kv", "k_accept_rows", "k_select_tap", "k_select_visual", "k_ctx_rows", "k_gemm_simt", "k_iota_rows", "k_set_seq", "k_set_int", "k_set_pages", "k_first_token", "k_argmax_out", "k_copy_f32", "k_split_rows", "k_gemm_collect", "k_gemm_tc", "k_sample", "k_truncate", "k_distill", "k_distill_grad", "k_cache_append", "k_cache_attn", "k_cache_merge", "k_cache_scores", "k_cache_select"}
 // The buffer's address is asked for at a kernel's entry, by the one thread that will use it (trace_open), and looked at behind the grid
 // dependency.  Asked for behind the dependency, as it first was, every kernel began with a round trip to L2 or, behind a GEMM's weight
 // stream, to HBM, in the block that the others then waited for (SmolVLM-shaped round 2315 -> 2290 us, fp32 toy request 4900 -> 4856).

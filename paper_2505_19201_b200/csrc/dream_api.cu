@@ -1904,3 +1904,7 @@ extern "C" dream_status dream_debug_read(dream_ctx *c, int32_t seq, int32_t what
   return c->cfg.dtype == DREAM_BF16 ? debug_read_impl<bf16>(c, seq, what, layer, index, dst)
                                     : debug_read_impl<float>(c, seq, what, layer, index, dst);
 }
+
+// ------------------------------------------------------------------------------------- a paged cache of the caller's own
+
+#include "cache_api.cuh"
