@@ -1,11 +1,15 @@
 // Entry points on a paged cache that a program holds itself (dream.h): checks on the host, then launches.  Part of dream_api.cu.
 #pragma once
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include "cache_attn.cuh"
 #include "cache_rows.cuh"
 
 #define CACHE_MAX_ROWS (1 << 20)
 #define CACHE_MAX_SEQS 4096
 #define CACHE_MAX_BUDGET 4096
+#define CACHE_MAX_CTAS 320                 // most CTAs of the attention
 #define CACHE_MAX_SELECT 32768             // pages of a sequence that dream_cache_select chooses from
 
 // The view of a cache, or what is wrong with it.
@@ -73,15 +77,15 @@ static dream_status cache_workspace(const char *who, const void *p, size_t have,
   if (have < need) return fail(nullptr, DREAM_E_NOMEM, "%s: workspace needs %zu bytes, got %zu", who, need, have);
   return DREAM_OK;
 }
-template <typename A>
-static const char *cache_launch(void (*kernel)(A), dim3 grid, int threads, size_t smem, cudaStream_t stream, const A &args) {
+template <typename... A>
+static const char *cache_launch(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const A &...args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = pdl_on() ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
   if (e == cudaSuccess) return nullptr;
   cudaGetLastError();
   return cudaGetErrorString(e);
@@ -173,13 +177,23 @@ extern "C" dream_status dream_cache_select(const dream_cache *cache, const void 
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
 }
 
+// The parts of the attention's workspace; how many bytes they are.
+static size_t cache_attn_room(const dream_cache *c, int n_heads, int rows, void *workspace, CacheAttnArgs *a) {
+  const size_t n = 2 * (size_t)rows * n_heads, hd = c->head_dim;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { char *p = (char *)workspace + at; at += (bytes + 255) / 256 * 256; return p; };
+  char *po = take(n * hd * 4), *pm = take(n * 16), *co = take((size_t)CACHE_MAX_CTAS * 128 * hd * 4), *cm = take((size_t)CACHE_MAX_CTAS * 128 * 16);
+  if (a) { a->part_o = (float *)po; a->part_ml = (float4 *)pm; a->cont_o = (float *)co; a->cont_ml = (float4 *)cm; }
+  return at;
+}
+
 extern "C" dream_status dream_cache_attn_bytes(const dream_cache *cache, int32_t n_heads, int32_t rows, size_t *bytes) {
   CacheView v;
   dream_status s = cache_view("dream_cache_attn_bytes", cache, &v);
   if (!s) s = cache_heads("dream_cache_attn_bytes", cache, rows, n_heads);
   if (s) return s;
   if (!bytes) return fail(nullptr, DREAM_E_ARG, "dream_cache_attn_bytes: null argument");
-  *bytes = 256;
+  *bytes = cache_attn_room(cache, n_heads, rows, nullptr, nullptr);
   return DREAM_OK;
 }
 
@@ -201,17 +215,59 @@ static dream_status cache_attn_args(const char *who, const dream_cache *cache, C
   if (!s) s = cache_workspace(who, workspace, workspace_bytes, need);
   if (s) return s;
   a->q = q; a->q_ld = q_ld; a->out = out; a->out_ld = out_ld; a->lse = lse; a->rows = rows; a->heads = n_heads; a->group = n_heads / a->c.hkv;
-  a->scale_log2 = scale * 1.4426950408889634f; a->status = status;
+  a->scale_log2 = scale * 1.4426950408889634f; a->status = status; a->tile_rows = 128 / a->group;
+  cache_attn_room(cache, n_heads, rows, const_cast<void *>(workspace), a);
   return DREAM_OK;
 }
+// K or V as the copies take it: 64 columns x the keys of one page that go into a unit, and all panels of columns where that is the whole unit.
+static const char *cache_map(const dream_cache *c, const CacheView &v, const void *base, CUtensorMap *out) {
+  static PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
+  if (!encode) {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult qr;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qr) != cudaSuccess || !fn) return "cuTensorMapEncodeTiled not available";
+    encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
+  }
+  const int sub = c->page_tokens < CA_BLK ? c->page_tokens : CA_BLK, panels = c->head_dim / 64;
+  const cuuint64_t dims[5] = {64, (cuuint64_t)c->page_tokens, (cuuint64_t)panels, (cuuint64_t)c->n_kv_heads, (cuuint64_t)c->n_pages};
+  const cuuint64_t strides[4] = {(cuuint64_t)v.token_stride * 2, 128, (cuuint64_t)v.head_stride * 2, (cuuint64_t)v.page_stride * 2};
+  const cuuint32_t box[5] = {64, (cuuint32_t)sub, (cuuint32_t)(sub == CA_BLK ? panels : 1), 1, 1}, step[5] = {1, 1, 1, 1, 1};
+  const CUresult r = encode(out, c->dtype == DREAM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void *>(base), dims, strides,
+                            box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? nullptr : "the cache's strides make no tensor map";
+}
+template <typename T, int HD, bool PAGES>
+static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
+  struct Ready { int device, sms; };
+  static thread_local Ready ready[8];          // devices on which the kernel may use its shared memory, and their SMs
+  static thread_local int n_ready = 0;
+  auto *kernel = k_cache_attn<T, HD, PAGES>;
+  const size_t smem = CaShape<HD>::SMEM;
+  int device = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  for (int i = 0; i < n_ready && i < 8; ++i) if (ready[i].device == device) sms = ready[i].sms;
+  if (e == cudaSuccess && !sms) {
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e == cudaSuccess) ready[n_ready++ % 8] = {device, sms};
+  }
+  if (e != cudaSuccess) { cudaGetLastError(); return cudaGetErrorString(e); }
+  CUtensorMap mk, mv;
+  const char *why = cache_map(cache, a.c, a.c.k, &mk);
+  if (!why) why = cache_map(cache, a.c, a.c.v, &mv);
+  if (why) return why;
+  a.n_ctas = imin(sms * CaShape<HD>::CTAS_PER_SM, CACHE_MAX_CTAS);
+  why = cache_launch(kernel, dim3(a.n_ctas), CA_THREADS, smem, stream, mk, mv, a);
+  const long long merge = (long long)a.rows * a.heads * (HD / 8);
+  return why ? why : cache_launch(k_cache_merge<T, HD, PAGES>, dim3((unsigned)((merge + 255) / 256)), 256, 0, stream, a);
+}
 template <bool PAGES>
-static const char *cache_attn_launch(const dream_cache *cache, const CacheAttnArgs &a, cudaStream_t stream) {
-  void (*kernel)(CacheAttnArgs) = nullptr;
+static const char *cache_attn_launch(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
   const bool b = cache->dtype == DREAM_BF16;
-  if (cache->head_dim == 64) kernel = b ? k_cache_attn<bf16, 64, PAGES> : k_cache_attn<f16, 64, PAGES>;
-  else if (cache->head_dim == 128) kernel = b ? k_cache_attn<bf16, 128, PAGES> : k_cache_attn<f16, 128, PAGES>;
-  else kernel = b ? k_cache_attn<bf16, 256, PAGES> : k_cache_attn<f16, 256, PAGES>;
-  return cache_launch(kernel, dim3(a.rows, a.heads), 128, 0, stream, a);
+  if (cache->head_dim == 64) return b ? cache_attn_run<bf16, 64, PAGES>(cache, a, stream) : cache_attn_run<f16, 64, PAGES>(cache, a, stream);
+  if (cache->head_dim == 128) return b ? cache_attn_run<bf16, 128, PAGES>(cache, a, stream) : cache_attn_run<f16, 128, PAGES>(cache, a, stream);
+  return b ? cache_attn_run<bf16, 256, PAGES>(cache, a, stream) : cache_attn_run<f16, 256, PAGES>(cache, a, stream);
 }
 
 extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *q_start,
@@ -225,7 +281,11 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   if (!s) s = cache_ints(who, "tree_mask", tree_mask, false);
   if (s) return s;
   if (shared_pages < 0 || shared_pages > cache->pages_per_seq) return fail(nullptr, DREAM_E_ARG, "%s: shared_pages = %d outside 0..pages_per_seq = %d", who, shared_pages, cache->pages_per_seq);
-  a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask;
+  a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask; a.shared_tokens = shared_pages * cache->page_tokens;
+  // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits
+  const long long units = (long long)((cache->pages_per_seq * (long long)cache->page_tokens + CA_BLK - 1) / CA_BLK) * cache->n_kv_heads;
+  if (units > 0x7fffffffLL || (shared_pages && (units * shared_pages / cache->pages_per_seq + cache->n_kv_heads) * ((rows + a.tile_rows - 1) / a.tile_rows) > 0x7fffffffLL))
+    return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows over sequences of %d pages in one call", who, rows, cache->pages_per_seq);
   const char *why = cache_attn_launch<false>(cache, a, (cudaStream_t)cuda_stream);
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
 }
@@ -243,6 +303,7 @@ extern "C" dream_status dream_cache_attn_pages(const dream_cache *cache, const v
   if (s) return s;
   if (budget < 1) return fail(nullptr, DREAM_E_ARG, "%s: budget = %d must be positive", who, budget);
   if (budget > CACHE_MAX_BUDGET) return fail(nullptr, DREAM_E_CAPACITY, "%s: budget above %d", who, CACHE_MAX_BUDGET);
+  if ((long long)rows * cache->n_kv_heads > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows in one call", who, rows);
   a.row_seq = row_seq; a.row_pos = row_pos; a.ids = ids; a.budget = budget;
   const char *why = cache_attn_launch<true>(cache, a, (cudaStream_t)cuda_stream);
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
