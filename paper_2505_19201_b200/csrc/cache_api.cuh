@@ -219,8 +219,8 @@ static dream_status cache_attn_args(const char *who, const dream_cache *cache, C
   cache_attn_room(cache, n_heads, rows, const_cast<void *>(workspace), a);
   return DREAM_OK;
 }
-// K or V as the copies take it: 64 columns x the keys of one page that go into a unit, and all panels of columns where that is the whole unit.
-static const char *cache_map(const dream_cache *c, const CacheView &v, const void *base, CUtensorMap *out) {
+// A tensor of five dimensions as the copies take it, 64 columns (128 bytes, swizzled) at a time.
+static const char *cache_map(int dtype, const void *base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4], const cuuint32_t (&box)[5], CUtensorMap *out) {
   static PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
   if (!encode) {
     void *fn = nullptr;
@@ -228,13 +228,22 @@ static const char *cache_map(const dream_cache *c, const CacheView &v, const voi
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qr) != cudaSuccess || !fn) return "cuTensorMapEncodeTiled not available";
     encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
   }
-  const int sub = c->page_tokens < CA_BLK ? c->page_tokens : CA_BLK, panels = c->head_dim / 64;
-  const cuuint64_t dims[5] = {64, (cuuint64_t)c->page_tokens, (cuuint64_t)panels, (cuuint64_t)c->n_kv_heads, (cuuint64_t)c->n_pages};
-  const cuuint64_t strides[4] = {(cuuint64_t)v.token_stride * 2, 128, (cuuint64_t)v.head_stride * 2, (cuuint64_t)v.page_stride * 2};
-  const cuuint32_t box[5] = {64, (cuuint32_t)sub, (cuuint32_t)(sub == CA_BLK ? panels : 1), 1, 1}, step[5] = {1, 1, 1, 1, 1};
-  const CUresult r = encode(out, c->dtype == DREAM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void *>(base), dims, strides,
-                            box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? nullptr : "the cache's strides make no tensor map";
+  const cuuint32_t step[5] = {1, 1, 1, 1, 1};
+  const CUresult r = encode(out, dtype == DREAM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void *>(base), dims, strides, box,
+                            step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? nullptr : "the strides make no tensor map";
+}
+// K or V: the keys of one page that go into a unit, and all panels of columns where they are the whole unit.
+static const char *cache_kv_map(const dream_cache *c, const CacheView &v, const void *base, CUtensorMap *out) {
+  const cuuint32_t sub = c->page_tokens < CA_BLK ? c->page_tokens : CA_BLK, panels = c->head_dim / 64;
+  return cache_map(c->dtype, base, {64, (cuuint64_t)c->page_tokens, panels, (cuuint64_t)c->n_kv_heads, (cuuint64_t)c->n_pages},
+                   {(cuuint64_t)v.token_stride * 2, 128, (cuuint64_t)v.head_stride * 2, (cuuint64_t)v.page_stride * 2}, {64, sub, sub == CA_BLK ? panels : 1, 1, 1}, out);
+}
+// Q: a panel of so many rows' heads of one group, row after row, as a tile has its entries.
+static const char *cache_q_map(const dream_cache *c, const CacheAttnArgs &a, int rows, CUtensorMap *out) {
+  const cuuint64_t hd = c->head_dim;
+  return cache_map(c->dtype, a.q, {64, hd / 64, (cuuint64_t)a.group, (cuuint64_t)c->n_kv_heads, (cuuint64_t)a.rows},
+                   {128, hd * 2, a.group * hd * 2, (cuuint64_t)a.q_ld * 2}, {64, 1, (cuuint32_t)a.group, 1, (cuuint32_t)rows}, out);
 }
 template <typename T, int HD, bool PAGES>
 static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
@@ -250,15 +259,22 @@ static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cu
     e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    cudaFuncAttributes fa = {};
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, kernel);
+    if (e == cudaSuccess && CaShape<HD>::SPLIT && fa.numRegs != 80) return "the attention's warps share out 80 registers per thread and it was compiled with another number";
     if (e == cudaSuccess) ready[n_ready++ % 8] = {device, sms};
   }
   if (e != cudaSuccess) { cudaGetLastError(); return cudaGetErrorString(e); }
-  CUtensorMap mk, mv;
-  const char *why = cache_map(cache, a.c, a.c.k, &mk);
-  if (!why) why = cache_map(cache, a.c, a.c.v, &mv);
+  CUtensorMap mk, mv, mq, ms;
+  const char *why = cache_kv_map(cache, a.c, a.c.k, &mk);
+  if (!why) why = cache_kv_map(cache, a.c, a.c.v, &mv);
+  // a copy takes a whole tile of query entries, or 16 where a segment has no more
+  a.q_small = a.group < 16 ? 16 / a.group : 1;
+  if (!why) why = cache_q_map(cache, a, a.tile_rows, &mq);
+  if (!why) why = cache_q_map(cache, a, a.q_small, &ms);
   if (why) return why;
   a.n_ctas = imin(sms * CaShape<HD>::CTAS_PER_SM, CACHE_MAX_CTAS);
-  why = cache_launch(kernel, dim3(a.n_ctas), CA_THREADS, smem, stream, mk, mv, a);
+  why = cache_launch(kernel, dim3(a.n_ctas), CA_THREADS, smem, stream, mk, mv, mq, ms, a);
   const long long merge = (long long)a.rows * a.heads * (HD / 8);
   return why ? why : cache_launch(k_cache_merge<T, HD, PAGES>, dim3((unsigned)((merge + 255) / 256)), 256, 0, stream, a);
 }

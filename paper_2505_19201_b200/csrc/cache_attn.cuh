@@ -5,32 +5,40 @@
 // units of 64 keys.  Shared pages: the rows of all sequences stand together, in tiles of 128 entries, so that the prefix is read once for all of them (once per
 // tile).  A sequence's own tokens: its rows, tile by tile.  Listed pages: one row.  The units of all items, one behind the other, are dealt out to
 // the CTAs in equal contiguous ranges, by arithmetic on the lengths that each CTA does for itself (they are on the device), so long contexts
-// with few rows fill the GPU and short ones do not leave a tail.  A range is a few segments, each in one item.  A segment leaves (m, l, O) of its keys; k_cache_merge adds up the
+// with few rows fill the GPU and short ones do not leave a tail.  An item counts CA_START units more than it has, for what starting and ending it costs.  A
+// range is a few segments, each in one item.  A segment leaves (m, l, O) of its keys; k_cache_merge adds up the
 // segments of a row, always in the same order.  The segment that starts an item has its place by row and head, a CTA's continuation
 // of an item the CTA's own.
 //
-// A segment.  S = Q K^T (128 x 64, fp32 in TMEM, two buffers), softmax by 128 threads, a row each: one pass with a running reference m that follows the
+// A segment.  S = Q K^T (128 x 64, fp32 in TMEM, two to four buffers), softmax by eight warps of 16 rows each, the four lanes of a quad to a row (and to the
+// one eight further on): one pass with a running reference m that follows the
 // row's maximum only when that has outgrown it (the accumulator is then rescaled, seldom), P = 2^(s - m) rounded to the cache's type into the columns
 // its scores came from, O += P V with P as the TMEM operand.  l sums the rounded P, so that the weights add up to 1 whatever their rounding, which
 // then moves the result by at most half a step of sum w |v - out|; the log-sum-exp has a sum of its own, of P as it was.  K and V come by TMA in two rings that
-// run on from segment to segment, so that the next one's keys are under way while one ends; its queries are fetched before the accumulator is read out.
-// Warps: 0 TMA, 1 matrix instructions and TMEM, 2..5 softmax and epilogue.
+// run on from segment to segment, so that the next one's keys are under way while one ends.  The producer alone works out what the segments are, ahead of
+// everybody else, and leaves them in a ring in shared memory.
+// Warps: 0 TMA and segments, 1 S, Q and TMEM, 2 O, 3 nothing, 4..11 softmax and epilogue.  Two CTAs share an SM's registers: 80 for each thread, of which
+// the first four warps leave the others a part.
 #pragma once
 #include "attn_tc.cuh"
 #include "cache_rows.cuh"
 
-#define CA_THREADS 192
+#define CA_THREADS 384
+#define CA_WARPS (CA_THREADS / 32)
 #define CA_BLK 64                        // keys of a unit
-#define CA_MASKS 16                      // ring of the units' key masks: more than the K ring's stages and two
+#define CA_RING 16                       // units' key masks, and segments, that are known at once: more than the stages and the buffers of S together
+#define CA_START 1                       // units that starting and ending an item is worth
 
 template <int HD> struct CaShape {
   static constexpr int KP = HD / 64;                                   // 64-column panels of a row
   static constexpr int STAGES = HD == 64 ? 5 : 2;                      // units of K (and of V) in shared memory
-  static constexpr int TMEM_COLS = HD + 2 * CA_BLK <= 256 ? 256 : 512;
+  static constexpr int S_BUFS = HD == 64 ? 3 : HD == 128 ? 2 : 4;      // what the TMEM columns hold beside O
+  static constexpr int TMEM_COLS = HD + S_BUFS * CA_BLK <= 256 ? 256 : 512;
   static constexpr int CTAS_PER_SM = HD == 256 ? 1 : 2;                // one walks its keys while the other starts or ends a segment
   static constexpr int Q_BYTES = 128 * HD * 2, Q_PANEL = 128 * 128;
   static constexpr int STAGE = CA_BLK * HD * 2, PANEL = CA_BLK * 128;
-  static constexpr size_t SMEM = 1024 + Q_BYTES + 2 * STAGES * STAGE + 512;
+  static constexpr bool SPLIT = CTAS_PER_SM == 2;                      // registers are moved between the warps: 4 x 32 x 64 + 8 x 32 x 88 = 384 x 80
+  static constexpr size_t SMEM = 1024 + Q_BYTES + 2 * STAGES * STAGE + 1536;
 };
 
 struct CacheAttnArgs {
@@ -50,6 +58,7 @@ struct CacheAttnArgs {
   float *cont_o;                           // [CTA][128][HD], [CTA][128]: the segments that continue one
   float4 *cont_ml;
   int n_ctas;
+  int q_small;                             // query rows that the smaller of the two copies of Q takes
   int *status;
 };
 
@@ -73,14 +82,12 @@ __device__ __forceinline__ void mma_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uin
       "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
       ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+// 16 lanes x 32 columns: lane 4 i + j of the warp puts r[2 c] into column 4 c + j of TMEM lane i, r[2 c + 1] into that of lane i + 8.
+__device__ __forceinline__ void tmem_st16x32(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-        "r"(r[30]), "r"(r[31]) : "memory");
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
 // A sequence as the call gives it, held within the buffers whatever its numbers say.
@@ -98,9 +105,18 @@ struct CaSeq {
   __device__ __forceinline__ int units(const CacheAttnArgs &a, int t) const { return max(1, (end(a, t) - a.shared_tokens + CA_BLK - 1) / CA_BLK); }
   __device__ __forceinline__ long long all_units(const CacheAttnArgs &a) const {
     long long sum = 0;
-    for (int t = tiles(a) - 1; t >= 0; --t) sum += units(a, t);
+    for (int t = tiles(a) - 1; t >= 0; --t) sum += units(a, t) + CA_START;
     return sum * a.c.hkv;
   }
+};
+
+// A segment, as the producer leaves it for the others.
+struct CaSeg {
+  int row0, rows, kvh, seq;                // rows row0 .. row0 + rows - 1 against KV head kvh (phase 1: of sequence seq)
+  int phase;                               // 0: shared keys; 1: the rows' own
+  int end;                                 // keys from here on are nobody's (pages: the row's position)
+  int b0, n, key0;                         // units b0 .. b0 + n - 1 of the item, whose first key is key0; n = 0: there are no more segments
+  int follow;                              // CTAs that continue the item (of the segment that starts it)
 };
 
 // What a CTA has to do: units [u, u_end) of the call, as segments.
@@ -111,43 +127,44 @@ template <bool PAGES> struct CaWalk {
   int prefix_tiles, prefix_blocks, prefix_rows;
   int seq, tile;
   long long at;                            // where the units behind the prefix stand: those of (seq, tile) start here
-  // the segment
-  int phase, row0, rows, kvh, end;         // rows row0 .. row0 + rows - 1; keys from `end` on are nobody's
-  int b0, b1, key0;                        // units of the item, whose first key is key0
-  int follow;                              // CTAs that continue the item (of the segment that starts it)
-  __device__ __forceinline__ void cut(long long item, int blocks) {
-    b0 = (int)(u - item);
-    b1 = b0 + (int)min((long long)(blocks - b0), u_end - u);
-    follow = (int)(item + blocks - 1 - u_first) / upc;
-    u += b1 - b0;
+  // The part of this CTA in an item of so many blocks: behind CA_START units that stand for its start.  False where the range ends in front of the first.
+  __device__ __forceinline__ bool cut(CaSeg &s, long long item, int blocks) {
+    const int off = (int)(u - item) - CA_START;
+    s.b0 = max(off, 0);
+    const int b1 = (int)min((long long)blocks, u_end - item - CA_START);
+    s.n = b1 - s.b0;
+    s.follow = (int)(item + CA_START + blocks - 1 - u_first) / upc;
+    u = min(u_end, item + CA_START + blocks);
+    return s.n > 0;
   }
-  __device__ __forceinline__ bool next(const CacheAttnArgs &a) {
-    if (u >= u_end) return false;
+  __device__ __forceinline__ bool next(const CacheAttnArgs &a, CaSeg &s) {
     if (PAGES) {
-      const int blocks = prefix_blocks, item = (int)(u / blocks);
-      phase = 1; row0 = item / a.c.hkv; rows = 1; kvh = item - row0 * a.c.hkv; seq = a.row_seq[row0]; key0 = 0; end = a.row_pos[row0];
-      cut((long long)item * blocks, blocks);
-      return true;
+      while (u < u_end) {
+        const int blocks = prefix_blocks, item = (int)(u / (blocks + CA_START));
+        s.phase = 1; s.row0 = item / a.c.hkv; s.rows = 1; s.kvh = item - s.row0 * a.c.hkv; s.seq = a.row_seq[s.row0]; s.key0 = 0; s.end = a.row_pos[s.row0];
+        if (cut(s, (long long)item * (blocks + CA_START), blocks)) return true;
+      }
+      return false;
     }
-    if (u < prefix_units) {
-      const int item = (int)u / prefix_blocks;
-      phase = 0; kvh = item / prefix_tiles;
-      row0 = (item - kvh * prefix_tiles) * a.tile_rows; rows = min(a.tile_rows, prefix_rows - row0);
-      end = a.shared_tokens; key0 = 0;
-      cut(item * prefix_blocks, prefix_blocks);
-      return true;
+    while (u < min(u_end, prefix_units)) {
+      const int item = (int)u / (prefix_blocks + CA_START);
+      s.phase = 0; s.seq = 0; s.kvh = item / prefix_tiles;
+      s.row0 = (item - s.kvh * prefix_tiles) * a.tile_rows; s.rows = min(a.tile_rows, prefix_rows - s.row0);
+      s.end = a.shared_tokens; s.key0 = 0;
+      if (cut(s, (long long)item * (prefix_blocks + CA_START), prefix_blocks)) return true;
     }
-    for (; seq < a.c.n_seqs; ++seq, tile = 0) {
-      const CaSeq s(a, seq);
-      for (const int tiles = s.tiles(a); tile < tiles; ++tile) {
-        const int blocks = s.units(a, tile), sum = blocks * a.c.hkv;
-        if (u < at + sum) {
-          phase = 1; kvh = (int)(u - at) / blocks;
-          row0 = s.q0 + tile * a.tile_rows; rows = min(a.tile_rows, s.n - tile * a.tile_rows);
-          end = s.end(a, tile); key0 = a.shared_tokens;
-          cut(at + kvh * blocks, blocks);
-          return true;
+    for (; u < u_end && seq < a.c.n_seqs; ++seq, tile = 0) {
+      const CaSeq q(a, seq);
+      for (const int tiles = q.tiles(a); tile < tiles; ++tile) {
+        const int blocks = q.units(a, tile), each = blocks + CA_START;
+        const long long sum = (long long)each * a.c.hkv;
+        while (u < u_end && u < at + sum) {
+          s.phase = 1; s.seq = seq; s.kvh = (int)(u - at) / each;
+          s.row0 = q.q0 + tile * a.tile_rows; s.rows = min(a.tile_rows, q.n - tile * a.tile_rows);
+          s.end = q.end(a, tile); s.key0 = a.shared_tokens;
+          if (cut(s, at + (long long)s.kvh * each, blocks)) return true;
         }
+        if (u >= u_end) return false;
         at += sum;
       }
     }
@@ -157,38 +174,48 @@ template <bool PAGES> struct CaWalk {
 
 template <typename T, int HD, bool PAGES>
 __global__ void __launch_bounds__(CA_THREADS, (CaShape<HD>::CTAS_PER_SM))
-k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CacheAttnArgs a) {
+k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q,
+             const __grid_constant__ CUtensorMap map_q_small, const __grid_constant__ CacheAttnArgs a) {
   using Sh = CaShape<HD>;
-  constexpr int STAGES = Sh::STAGES, KP = Sh::KP;
+  constexpr int STAGES = Sh::STAGES, KP = Sh::KP, SB = Sh::S_BUFS;
   extern __shared__ uint8_t ca_smem_raw[];
   uint8_t *smem = (uint8_t *)(((uintptr_t)ca_smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t *q_s = smem, *k_s = q_s + Sh::Q_BYTES, *v_s = k_s + STAGES * Sh::STAGE;
   uint64_t *bars = (uint64_t *)(v_s + STAGES * Sh::STAGE);
   uint64_t *k_full = bars, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES;
-  uint64_t *s_full = v_empty + STAGES, *p_full = s_full + 2, *o_done = p_full + 2, *q_full = o_done + 2, *o_free = q_full + 1;
-  volatile uint64_t *masks = (volatile uint64_t *)(o_free + 1);            // [CA_MASKS] which keys of a unit there are
-  uint32_t *tmem_base_p = (uint32_t *)(masks + CA_MASKS);
+  uint64_t *s_full = v_empty + STAGES, *p_full = s_full + SB, *o_done = p_full + SB, *q_full = o_done + SB, *o_free = q_full + 1, *seg_full = o_free + 1;
+  volatile uint64_t *masks = (volatile uint64_t *)(seg_full + CA_RING);    // [CA_RING] which keys of a unit there are
+  CaSeg *segs = (CaSeg *)(masks + CA_RING);                                // [CA_RING]
+  uint32_t *tmem_base_p = (uint32_t *)(segs + CA_RING);
   volatile int *abort_flag = (volatile int *)(tmem_base_p + 1);
-  __shared__ long long sh_sum[CA_THREADS / 32], sh_at;
+  __shared__ long long sh_sum[CA_WARPS], sh_at;
   __shared__ int sh_seq, sh_partial, sh_status[2];
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, cta = blockIdx.x;
   unsigned long long *tr = trace_open();
   if (warp == 0) {
     if (lane < STAGES) { mbar_init(k_full + lane, 1); mbar_init(k_empty + lane, 1); mbar_init(v_full + lane, 1); mbar_init(v_empty + lane, 1); }
-    else if (lane >= 8 && lane < 10) { mbar_init(s_full + lane - 8, 1); mbar_init(p_full + lane - 8, 4); mbar_init(o_done + lane - 8, 1); }
-    else if (lane == 16) { mbar_init(q_full, 4); mbar_init(o_free, 4); *abort_flag = 0; }
-    else if (lane == 17) { sh_partial = 0; sh_seq = 0; sh_at = 0; sh_status[0] = sh_status[1] = 0; }
+    else if (lane >= 8 && lane < 8 + SB) { mbar_init(s_full + lane - 8, 1); mbar_init(p_full + lane - 8, 8); mbar_init(o_done + lane - 8, 1); }
+    else if (lane >= 16) mbar_init(seg_full + lane - 16, 1);
+    if (lane == 12) { mbar_init(q_full, 1); mbar_init(o_free, 8); *abort_flag = 0; }
+    else if (lane == 13) { sh_partial = 0; sh_seq = 0; sh_at = 0; sh_status[0] = sh_status[1] = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 2 && lane == 0) {
+  if (warp == 3 && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q_small) : "memory");
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_base_p)), "r"((uint32_t)Sh::TMEM_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  static_assert(CA_RING == 16, "a lane inits each of the segments' barriers");
+  static_assert(CA_RING > STAGES + SB, "what the producer leaves is read until a unit's P is done");
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
   pdl_wait();
   trace_stamp(tr, TR_k_cache_attn);
   int *status = a.status ? a.status : sh_status;
@@ -196,92 +223,114 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   // ---- this CTA's units
   CaWalk<PAGES> w;
   long long total;
+  w.seq = w.tile = 0;
+  w.at = 0;
   if (PAGES) {
     w.prefix_blocks = max(1, (a.budget * a.c.page_tokens + CA_BLK - 1) / CA_BLK);
-    total = (long long)a.rows * a.c.hkv * w.prefix_blocks;
-    w.prefix_units = 0;
+    total = (long long)a.rows * a.c.hkv * (w.prefix_blocks + CA_START);
+    w.upc = (int)max(1ll, (total + a.n_ctas - 1) / a.n_ctas);
   } else {
     w.prefix_rows = min(max(a.q_start[a.c.n_seqs], 0), a.rows);
-    w.prefix_tiles = (w.prefix_rows + a.tile_rows - 1) / a.tile_rows;
     w.prefix_blocks = (a.shared_tokens + CA_BLK - 1) / CA_BLK;
-    w.prefix_units = (long long)w.prefix_tiles * w.prefix_blocks * a.c.hkv;
-    long long sum = 0;
+    w.prefix_tiles = w.prefix_blocks ? (w.prefix_rows + a.tile_rows - 1) / a.tile_rows : 0;
+    w.prefix_units = (long long)w.prefix_tiles * (w.prefix_blocks + CA_START) * a.c.hkv;
+    // units in front of each sequence's, a sequence per thread at a time; once around for most batches, twice where there are more sequences than threads
+    const bool once = a.c.n_seqs <= CA_THREADS;
+    long long own = 0, sum = 0;
     for (int s = threadIdx.x; s < a.c.n_seqs; s += CA_THREADS) {
       const CaSeq q(a, s);
-      sum += q.all_units(a);
+      own = q.all_units(a);
+      sum += own;
       if (q.n && q.len - q.n + (a.tree ? 0 : 1) < a.shared_tokens) sh_partial = 1;       // a row that does not see the whole prefix
       if (cta == 0 && (q.q0 != a.q_start[s] || q.q0 + q.n != a.q_start[s + 1] || q.len != a.kv_len[s])) cache_bad_index(status);
     }
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) sh_sum[warp] = sum;
+    for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
+    if (lane == 31) sh_sum[warp] = sum;
     __syncthreads();
     total = w.prefix_units;
-    for (int i = 0; i < CA_THREADS / 32; ++i) total += sh_sum[i];
+    long long before = w.prefix_units + sum - own;
+    for (int i = 0; i < CA_WARPS; ++i) { if (i < warp) before += sh_sum[i]; total += sh_sum[i]; }
+    w.upc = (int)max(1ll, (total + a.n_ctas - 1) / a.n_ctas);
+    // the sequence in which the units behind the prefix start for this CTA
+    const long long goal = max(min((long long)cta * w.upc, total), w.prefix_units);
+    if (once) {
+      if (goal >= before && goal < before + own) { sh_seq = threadIdx.x; sh_at = before; }
+    } else {
+      long long at = w.prefix_units;
+      for (int s0 = 0; s0 < a.c.n_seqs && at <= goal; s0 += CA_THREADS) {
+        const int s = s0 + threadIdx.x;
+        own = s < a.c.n_seqs ? CaSeq(a, s).all_units(a) : 0ll;
+        sum = own;
+        for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
+        __syncthreads();
+        if (lane == 31) sh_sum[warp] = sum;
+        __syncthreads();
+        before = at + sum - own;
+        for (int i = 0; i < CA_WARPS; ++i) { if (i < warp) before += sh_sum[i]; at += sh_sum[i]; }
+        if (goal >= before && goal < before + own) { sh_seq = s; sh_at = before; }
+      }
+    }
+    __syncthreads();
+    w.seq = sh_seq; w.at = sh_at;
   }
-  w.upc = (int)max(1ll, (total + a.n_ctas - 1) / a.n_ctas);
   w.u_first = (long long)cta * w.upc;
   w.u = min(w.u_first, total);
   w.u_end = min(w.u + w.upc, total);
-  if (!PAGES && w.u < w.u_end) {
-    // the sequence in which the units behind the prefix start for this CTA
-    const long long goal = max(w.u, w.prefix_units);
-    long long at = w.prefix_units;
-    for (int s0 = 0; s0 < a.c.n_seqs && at <= goal; s0 += CA_THREADS) {
-      const int s = s0 + threadIdx.x;
-      const long long own = s < a.c.n_seqs ? CaSeq(a, s).all_units(a) : 0ll;
-      long long sum = own;
-      for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
-      __syncthreads();
-      if (lane == 31) sh_sum[warp] = sum;
-      __syncthreads();
-      long long before = at;
-      for (int i = 0; i < CA_THREADS / 32; ++i) { if (i < warp) before += sh_sum[i]; at += sh_sum[i]; }
-      before += sum - own;
-      if (goal >= before && goal < before + own) { sh_seq = s; sh_at = before; }
-    }
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
   const uint32_t tmem_base = *tmem_base_p;
-  w.seq = sh_seq; w.tile = 0; w.at = sh_at;
   int gave_up = WAIT_none;
+  // Units of segment number i, once the producer has left it; 0: there is none, or a wait ran out.
+  auto segment = [&](int i, int where) {
+    if (!mbar_wait_warp(seg_full + i % CA_RING, (uint32_t)(i / CA_RING) & 1u, abort_flag)) { gave_up = where; return 0; }
+    return segs[i % CA_RING].n;
+  };
 
+  if (Sh::SPLIT) {
+    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
+  }
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
     const uint64_t pol = policy_evict_normal();
     const int sub = min(CA_BLK, a.c.page_tokens), n_sub = CA_BLK / sub;     // keys of one copy, copies of a unit
-    int ks = 0, vs = 0, g = 0;
+    int ks = 0, vs = 0, g = 0, n_seg = 0;
     uint32_t kph = 1, vph = 1;
-    while (!gave_up && w.next(a)) {
+    for (;; ++n_seg) {
+      CaSeg s;
+      if (!w.next(a, s)) s.n = 0;
+      if (elect_one()) {
+        segs[n_seg % CA_RING] = s;
+        mbar_arrive(seg_full + n_seg % CA_RING);
+      }
+      __syncwarp();
+      if (!s.n) break;
       // lane l holds the page of part p0 + l of the item's keys, and the first of these keys in the sequence
       int p0 = -64, page = 0, token = 0;
-      for (int blk = w.b0; blk < w.b1 && !gave_up; ++blk, ++g) {
+      for (int blk = s.b0; blk < s.b0 + s.n && !gave_up; ++blk, ++g) {
         const int part = blk * n_sub;
         if (part < p0 || part + n_sub > p0 + 32) {
           p0 = part;
           const int first = (p0 + lane) * sub;             // key of the item
           page = -1;
+          token = 0;
           bool bad = false;
           if (PAGES) {
             const int e = first >> a.c.page_shift;
-            const int *ids = a.ids + ((long long)w.row0 * a.c.hkv + w.kvh) * a.budget;
-            token = 0;
-            if (w.seq >= 0 && w.end >= 0) {
-              if (!a.c.token_ok(w.seq, w.end)) bad = true;
+            const int *ids = a.ids + ((long long)s.row0 * a.c.hkv + s.kvh) * a.budget;
+            if (s.seq >= 0 && s.end >= 0) {
+              if (!a.c.token_ok(s.seq, s.end)) bad = true;
               else if (e < a.budget) {
                 const int id = ids[e], before = e ? ids[e - 1] : -1;
-                if (id > before && id >= 0 && id <= w.end >> a.c.page_shift) {
+                if (id > before && id >= 0 && id <= s.end >> a.c.page_shift) {
                   token = (id << a.c.page_shift) + (first & (a.c.page_tokens - 1));
-                  page = a.c.page(w.seq, id);
+                  page = a.c.page(s.seq, id);
                   bad = page < 0;
                 }
               }
             }
           } else {
-            token = w.key0 + first;
-            if (token < w.end) {
-              page = a.c.page(w.phase ? w.seq : 0, token >> a.c.page_shift);
+            token = s.key0 + first;
+            if (token < s.end) {
+              page = a.c.page(s.seq, token >> a.c.page_shift);
               bad = page < 0;
             }
           }
@@ -291,7 +340,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         uint32_t m0 = 0, m1 = 0;
         const int i = lane - (part - p0);
         if (i >= 0 && i < n_sub && page >= 0) {
-          const int n = min(sub, max(0, (PAGES ? w.end + 1 : w.end) - token));
+          const int n = min(sub, max(0, (PAGES ? s.end + 1 : s.end) - token));
           const uint64_t m = (n >= 64 ? ~0ull : (1ull << n) - 1ull) << (i * sub);
           m0 = (uint32_t)m; m1 = (uint32_t)(m >> 32);
         }
@@ -305,23 +354,24 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           const CUtensorMap *map = which ? &map_v : &map_k;
           if (!mbar_wait_warp((which ? v_empty : k_empty) + st, ph, abort_flag)) { gave_up = WAIT_cache_kv_ring; break; }
           if (elect_one()) {
-            if (!which) masks[g % CA_MASKS] = (uint64_t)m0 | (uint64_t)m1 << 32;
+            if (!which) masks[g % CA_RING] = (uint64_t)m0 | (uint64_t)m1 << 32;
             mbar_expect_tx(full, (uint32_t)Sh::STAGE);
           }
           __syncwarp();
-          for (int s = 0; s < n_sub; ++s) {
+          for (int j = 0; j < n_sub; ++j) {
             // a part without a page is filled with zeros: its page number is past the last
-            const int pg = __shfl_sync(0xffffffffu, page, part - p0 + s), tk = __shfl_sync(0xffffffffu, token, part - p0 + s) & (a.c.page_tokens - 1);
+            const int pg = __shfl_sync(0xffffffffu, page, part - p0 + j), tk = __shfl_sync(0xffffffffu, token, part - p0 + j) & (a.c.page_tokens - 1);
             if (elect_one()) {
-              if (n_sub == 1) tma_load_5d(dst, map, full, 0, tk, 0, w.kvh, pg < 0 ? a.c.n_pages : pg, pol);
+              if (n_sub == 1) tma_load_5d(dst, map, full, 0, tk, 0, s.kvh, pg < 0 ? a.c.n_pages : pg, pol);
               else
-                for (int kp = 0; kp < KP; ++kp) tma_load_5d(dst + kp * Sh::PANEL + s * sub * 128, map, full, 0, tk, kp, w.kvh, pg < 0 ? a.c.n_pages : pg, pol);
+                for (int kp = 0; kp < KP; ++kp) tma_load_5d(dst + kp * Sh::PANEL + j * sub * 128, map, full, 0, tk, kp, s.kvh, pg < 0 ? a.c.n_pages : pg, pol);
             }
             __syncwarp();
           }
           if (++st == STAGES) { st = 0; ph ^= 1u; }
         }
       }
+      if (gave_up) break;
     }
     // Until the last releases have arrived: one that came in after this CTA has left would land in the shared memory of the next.
 #pragma unroll 1
@@ -331,70 +381,86 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       if (++vs == STAGES) { vs = 0; vph ^= 1u; }
     }
   } else if (warp == 1) {
-    // ------------------------------------------------------------------ matrix instructions: S of a unit, then O of the one before
-    constexpr uint32_t id_s = (1u << 4) | CaType<T>::IDESC | ((uint32_t)(CA_BLK >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-    constexpr uint32_t id_o = (1u << 4) | CaType<T>::IDESC | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-    const uint64_t qd = smem_desc(smem_u32(q_s)), kd = smem_desc(smem_u32(k_s)), vd = smem_desc_mn(smem_u32(v_s), Sh::PANEL);
+    // ------------------------------------------------------------------ queries, and S = Q K^T: both operands K-major, N = 64
+    constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | ((uint32_t)(CA_BLK >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    const uint64_t qd = smem_desc(smem_u32(q_s)), kd = smem_desc(smem_u32(k_s));
     const uint32_t s_addr = tmem_base + HD;
-    int ks = 0, vs = 0, g = 0, seg = 0;
-    uint32_t kph = 0, vph = 0;
-    // O of unit x (counted over the CTA's life), the first of its segment or not
-    auto issue_o = [&](int x, bool first) {
-      if (first && seg > 0 && !mbar_wait_warp(o_free, (uint32_t)(seg - 1) & 1u, abort_flag)) { gave_up = WAIT_cache_o; return; }
-      if (!__all_sync(0xffffffffu, mbar_wait(v_full + vs, vph, abort_flag) && mbar_wait(p_full + (x & 1), (uint32_t)(x >> 1) & 1u, abort_flag))) { gave_up = WAIT_cache_p_v; return; }
-      const uint64_t m = masks[x % CA_MASKS];
-      if (m != ~0ull) {
-        // values that are nobody's may be anything, and 0 times that not 0
-        uint8_t *dst = v_s + vs * Sh::STAGE;
-        for (int i = lane; i < CA_BLK * KP * 8; i += 32) {
-          const int key = (i >> 3) & (CA_BLK - 1);
-          if (!(m >> key & 1ull)) *reinterpret_cast<uint4 *>(dst + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-      }
-      tc_fence_after();
+    const uint64_t pol = policy_evict_normal();
+    int ks = 0, g = 0, sb = 0;
+    uint32_t kph = 0, sph = 1;                              // sph: parity of the buffer's last O (1: none yet)
+    for (int seg = 0, n; (n = segment(seg, WAIT_cache_q)) > 0; ++seg) {
       if (elect_one()) {
-        const uint64_t bd = vd + (uint64_t)((vs * Sh::STAGE) >> 4);
-#pragma unroll
-        for (int k = 0; k < CA_BLK / 16; ++k)                               // 16 keys: eight columns of P, two groups of eight rows of V
-          mma_tmem_a(tmem_base, s_addr + (uint32_t)((x & 1) * CA_BLK + k * 8), bd + (uint64_t)(k * 128), id_o, (!first || k > 0) ? 1u : 0u);
-        mma_commit(v_empty + vs);
-        mma_commit(o_done + (x & 1));
+        const CaSeg &s = segs[seg % CA_RING];
+        const bool small = s.rows <= a.q_small;
+        mbar_expect_tx(q_full, (uint32_t)((small ? a.q_small : a.tile_rows) * a.group * 128 * KP));
+        for (int kp = 0; kp < KP; ++kp) tma_load_5d(q_s + kp * Sh::Q_PANEL, small ? &map_q_small : &map_q, q_full, 0, kp, 0, s.kvh, s.row0, pol);
       }
       __syncwarp();
-      if (++vs == STAGES) { vs = 0; vph ^= 1u; }
-    };
-    while (!gave_up && w.next(a)) {
-      const int n = w.b1 - w.b0;
       if (!mbar_wait_warp(q_full, (uint32_t)seg & 1u, abort_flag)) { gave_up = WAIT_cache_q; break; }
-      for (int i = 0; i <= n && !gave_up; ++i) {
-        if (i < n) {
-          // (the buffer of S is free: O of the unit before last, which read P there, was issued before)
-          if (!mbar_wait_warp(k_full + ks, kph, abort_flag)) { gave_up = WAIT_cache_k; break; }
-          tc_fence_after();
-          if (elect_one()) {
+#pragma unroll 1
+      for (int i = 0; i < n; ++i, ++g) {
+        if (!__all_sync(0xffffffffu, mbar_wait(o_done + sb, sph, abort_flag) && mbar_wait(k_full + ks, kph, abort_flag))) { gave_up = WAIT_cache_k; break; }
+        tc_fence_after();
+        if (elect_one()) {
 #pragma unroll
-            for (int kp = 0; kp < KP; ++kp)
+          for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                mma_bf16(s_addr + (uint32_t)(((g + i) & 1) * CA_BLK), qd + (uint64_t)((kp * Sh::Q_PANEL + k * 32) >> 4),
-                         kd + (uint64_t)((ks * Sh::STAGE + kp * Sh::PANEL + k * 32) >> 4), id_s, (kp > 0 || k > 0) ? 1u : 0u);
-            mma_commit(k_empty + ks);
-            mma_commit(s_full + ((g + i) & 1));
-          }
-          __syncwarp();
-          if (++ks == STAGES) { ks = 0; kph ^= 1u; }
+            for (int k = 0; k < 4; ++k)
+              mma_bf16(s_addr + (uint32_t)(sb * CA_BLK), qd + (uint64_t)((kp * Sh::Q_PANEL + k * 32) >> 4),
+                       kd + (uint64_t)((ks * Sh::STAGE + kp * Sh::PANEL + k * 32) >> 4), idesc, (kp > 0 || k > 0) ? 1u : 0u);
+          mma_commit(k_empty + ks);
+          mma_commit(s_full + sb);
         }
-        if (i > 0) issue_o(g + i - 1, i == 1);
+        __syncwarp();
+        if (++ks == STAGES) { ks = 0; kph ^= 1u; }
+        if (++sb == SB) { sb = 0; sph ^= 1u; }
       }
-      g += n;
-      ++seg;
+      if (gave_up) break;
+      // the next queries take these ones' place when S of the last unit is done
+      if (!mbar_wait_warp(s_full + (g - 1) % SB, (uint32_t)((g - 1) / SB) & 1u, abort_flag)) { gave_up = WAIT_cache_k; break; }
     }
-  } else {
-    // ------------------------------------------------------------------ softmax and epilogue: a row of the tile per thread
-    const int quarter = warp & 3, e = quarter * 32 + lane;                  // TMEM lanes this warp may access; entry of the tile
-    const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+  } else if (warp == 2) {
+    // ------------------------------------------------------------------ O += P V: P in TMEM, V MN-major, N = head_dim
+    constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    const uint64_t vd = smem_desc_mn(smem_u32(v_s), Sh::PANEL);
+    const uint32_t p_addr = tmem_base + HD;
+    int vs = 0, g = 0, sb = 0;
+    uint32_t vph = 0, pph = 0;
+    for (int seg = 0, n; (n = segment(seg, WAIT_cache_o)) > 0; ++seg) {
+      if (seg > 0 && !mbar_wait_warp(o_free, (uint32_t)(seg - 1) & 1u, abort_flag)) { gave_up = WAIT_cache_o; break; }
+#pragma unroll 1
+      for (int i = 0; i < n; ++i, ++g) {
+        if (!__all_sync(0xffffffffu, mbar_wait(v_full + vs, vph, abort_flag) && mbar_wait(p_full + sb, pph, abort_flag))) { gave_up = WAIT_cache_p_v; break; }
+        const uint64_t m = masks[g % CA_RING];
+        if (m != ~0ull) {
+          // values that are nobody's may be anything, and 0 times that not 0
+          uint8_t *dst = v_s + vs * Sh::STAGE;
+#pragma unroll 1
+          for (int j = lane; j < CA_BLK * KP * 8; j += 32)
+            if (!(m >> ((j >> 3) & (CA_BLK - 1)) & 1ull)) *reinterpret_cast<uint4 *>(dst + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t bd = vd + (uint64_t)((vs * Sh::STAGE) >> 4);
+#pragma unroll
+          for (int k = 0; k < CA_BLK / 16; ++k)                             // 16 keys: eight columns of P, two groups of eight rows of V
+            mma_tmem_a(tmem_base, p_addr + (uint32_t)(sb * CA_BLK + k * 8), bd + (uint64_t)(k * 128), idesc, (i > 0 || k > 0) ? 1u : 0u);
+          mma_commit(v_empty + vs);
+          mma_commit(o_done + sb);
+        }
+        __syncwarp();
+        if (++vs == STAGES) { vs = 0; vph ^= 1u; }
+        if (++sb == SB) { sb = 0; pph ^= 1u; }
+      }
+      if (gave_up) break;
+    }
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------------ softmax and epilogue: warps 4..7 and 8..11 each take 16 lanes of a quarter; a
+    // lane has 16 of a unit's 64 keys for two rows of the tile, e[0] and e[1] = e[0] + 8
+    const int base = (warp & 3) * 32 + (warp >= 8 ? 16 : 0), quad = lane >> 2, ql = lane & 3;
+    const uint32_t lane_addr = tmem_base + ((uint32_t)base << 16);
     bool ok = true;
     auto wait = [&](uint64_t *bar, uint32_t parity) {                       // one lane polls for the warp
       int v = 1;
@@ -405,175 +471,171 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
     };
     const float scale = a.scale_log2;
-    int g = 0;
-    bool more = w.next(a);
-    // the queries of the segment ahead, this warp's 32 rows of the tile
-    auto load_q = [&]() {
-      const int n = w.rows * a.group;
-      if (quarter * 32 < n) {
-        constexpr int V = HD / 8;
-#pragma unroll 4
-        for (int i = lane; i < 32 * V; i += 32) {
-          const int row = quarter * 32 + i / V, vec = i % V;
-          if (row < n) {
-            const int r = row / a.group, h = w.kvh * a.group + row - r * a.group;
-            const uint4 x = *reinterpret_cast<const uint4 *>((const T *)a.q + (long long)(w.row0 + r) * a.q_ld + (long long)h * HD + vec * 8);
-            *reinterpret_cast<uint4 *>(q_s + (vec >> 3) * Sh::Q_PANEL + row * 128 + (((vec & 7) ^ (row & 7)) << 4)) = x;
+    const bool tree = !PAGES && a.tree;
+    int g = 0, sb = 0;
+    uint32_t sph = 0;
+    for (int seg = 0, n; (n = segment(seg, WAIT_cache_softmax)) > 0; ++seg) {
+      const CaSeg &s = segs[seg % CA_RING];              // read where it is needed: registers are short
+      const int n_entries = s.rows * a.group;
+      const bool active = base < n_entries, mine[2] = {base + quad < n_entries, base + quad + 8 < n_entries};
+      // a row sees the keys below vis (of the item's first, units counted from the segment's first), and in a tree its own ones as the mask has them
+      int vis[2] = {0x7fffffff, 0x7fffffff};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (!PAGES && mine[k] && (s.phase || sh_partial)) {
+          const int r = s.row0 + (base + quad + 8 * k) / a.group;
+          int sq = s.seq;
+          if (!s.phase) {                                                   // the sequence that has the row
+            int lo = 0, hi = a.c.n_seqs;
+            while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (a.q_start[m] <= r) lo = m; else hi = m; }
+            sq = lo;
           }
-        }
-        fence_proxy_async_smem();
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_full);
-    };
-    if (more) load_q();
-    while (more) {
-      const int n_entries = w.rows * a.group, n = w.b1 - w.b0, b0 = w.b0, key0 = w.key0, kvh = w.kvh, phase = w.phase, follow = w.follow;
-      const bool active = quarter * 32 < n_entries, mine = e < n_entries, starts = b0 == 0;
-      const int r = w.row0 + e / a.group, h = kvh * a.group + e % a.group;
-      // what the row sees: keys below vis, and key tail0 + j where bit j of the mask is set
-      int vis = 0x7fffffff, tail0 = 0;
-      unsigned long long mlo = 0ull, mhi = 0ull;
-      const bool row_on = !PAGES || w.seq >= 0;
-      if (!PAGES && mine && (phase || sh_partial)) {
-        int s = w.seq;
-        if (!phase) {                                                       // the sequence that has the row
-          int lo = 0, hi = a.c.n_seqs;
-          while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (a.q_start[m] <= r) lo = m; else hi = m; }
-          s = lo;
-        }
-        const CaSeq q(a, s);
-        tail0 = q.len - q.n;
-        vis = a.tree ? tail0 : tail0 + (r - q.q0) + 1;
-        if (a.tree) {
-          const uint32_t *t = a.tree + (long long)r * 4;
-          mlo = t[0] | (unsigned long long)t[1] << 32;
-          mhi = t[2] | (unsigned long long)t[3] << 32;
+          const CaSeq q(a, sq);
+          vis[k] = q.len - q.n + (tree ? 0 : r - q.q0 + 1) - (s.key0 + s.b0 * CA_BLK);
         }
       }
-      const bool tree = !PAGES && a.tree;
-      float m_ref = -INFINITY, l = 0.f, l_true = 0.f;
+      float m_ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, l_true[2] = {0.f, 0.f};      // l: this lane's share of the sums
 #pragma unroll 1
-      for (int i = 0; i < n; ++i) {
-        const int x = g + i, j0 = key0 + (b0 + i) * CA_BLK;
-        wait(s_full + (x & 1), (uint32_t)(x >> 1) & 1u);
-        // A wait is for a phase whose predecessor is known to be over: O of the unit before last, whose barrier this unit's O has too, is waited for here
-        // (it was issued before S).
-        if (x > 1) wait(o_done + (x & 1), (uint32_t)((x >> 1) - 1) & 1u);
+      for (int i = 0; i < n; ++i, ++g) {
+        wait(s_full + sb, sph);
         if (active) {
           tc_fence_after();
-          const uint32_t s_col = lane_addr + (uint32_t)(HD + (x & 1) * CA_BLK);
-          uint32_t s0[32], s1[32];
-          tmem_ld32(s_col, s0);
-          tmem_ld32(s_col + 32, s1);
-          uint64_t vm = masks[x % CA_MASKS];
-          if (!PAGES) {
-            const int npre = min(64, max(0, vis - j0));
-            unsigned long long m = npre >= 64 ? ~0ull : (1ull << npre) - 1ull;
-            if (tree && npre < 64) {
-              const int sh = j0 - tail0;                                    // node of key j0
-              if (sh < 0) m |= sh > -64 ? mlo << (-sh) : 0ull;
-              else if (sh < 64) m |= (mlo >> sh) | (sh ? mhi << (64 - sh) : 0ull);
-              else m |= sh < 128 ? mhi >> (sh - 64) : 0ull;
-            }
-            vm &= m;
-          }
+          const uint32_t s_col = lane_addr + (uint32_t)(HD + sb * CA_BLK);
+          uint32_t sr[32];                                                  // sr[4 c + 2 k + j]: row k, key 8 c + 2 ql + j
+          tmem_ld16x64(s_col, sr);
+          const uint64_t um = masks[g % CA_RING];
+          const bool all = um == ~0ull && vis[0] - i * CA_BLK >= CA_BLK && vis[1] - i * CA_BLK >= CA_BLK;
           tmem_ld_wait();
-          if (__any_sync(0xffffffffu, vm != ~0ull)) {
-            const uint32_t v0 = (uint32_t)vm, v1 = (uint32_t)(vm >> 32);
+          if (!__all_sync(0xffffffffu, all)) {
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              s0[c] = v0 >> c & 1u ? s0[c] : 0xff800000u;
-              s1[c] = v1 >> c & 1u ? s1[c] : 0xff800000u;
+            for (int k = 0; k < 2; ++k) {
+              const int left = vis[k] - i * CA_BLK, npre = min(64, max(0, left));
+              unsigned long long m = npre >= 64 ? ~0ull : (1ull << npre) - 1ull;
+              if (tree && npre < 64 && mine[k]) {
+                const uint32_t *t = a.tree + (long long)(s.row0 + (base + quad + 8 * k) / a.group) * 4;
+                const unsigned long long mlo = t[0] | (unsigned long long)t[1] << 32, mhi = t[2] | (unsigned long long)t[3] << 32;
+                const int sh = -left;                                       // node of the unit's first key
+                if (sh < 0) m |= sh > -64 ? mlo << (-sh) : 0ull;
+                else if (sh < 64) m |= (mlo >> sh) | (sh ? mhi << (64 - sh) : 0ull);
+                else m |= sh < 128 ? mhi >> (sh - 64) : 0ull;
+              }
+              m = (m & um) >> (2 * ql);
+              const uint32_t v0 = (uint32_t)m, v1 = (uint32_t)(m >> 32);
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                const uint32_t v = c < 4 ? v0 >> (8 * c) : v1 >> (8 * c - 32);
+                sr[4 * c + 2 * k] = v & 1u ? sr[4 * c + 2 * k] : 0xff800000u;
+                sr[4 * c + 2 * k + 1] = v & 2u ? sr[4 * c + 2 * k + 1] : 0xff800000u;
+              }
             }
           }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float bm[2];
+          bool grow[2];
 #pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            mx[0] = fmaxf(mx[0], __uint_as_float(s0[c])); mx[1] = fmaxf(mx[1], __uint_as_float(s0[c + 1]));
-            mx[2] = fmaxf(mx[2], __uint_as_float(s1[c])); mx[3] = fmaxf(mx[3], __uint_as_float(s1[c + 1]));
+          for (int k = 0; k < 2; ++k) {
+            float x = -INFINITY, y = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) { x = fmaxf(x, __uint_as_float(sr[4 * c + 2 * k])); y = fmaxf(y, __uint_as_float(sr[4 * c + 2 * k + 1])); }
+            x = fmaxf(x, y);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            bm[k] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2)) * scale;
+            grow[k] = mine[k] && bm[k] > m_ref[k] + CaType<T>::RESCALE && m_ref[k] != -INFINITY;
           }
-          const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-          const bool grow = mine && bm > m_ref + CaType<T>::RESCALE && m_ref != -INFINITY;
-          if (__any_sync(0xffffffffu, grow)) {
+          if (__any_sync(0xffffffffu, grow[0] || grow[1])) {
             // the accumulator takes the new reference, behind the O of every earlier unit
-            wait(o_done + ((x - 1) & 1), (uint32_t)((x - 1) >> 1) & 1u);
+            wait(o_done + (g - 1) % SB, (uint32_t)((g - 1) / SB) & 1u);
             tc_fence_after();
-            const float corr = grow ? ex2(m_ref - bm) : 1.f;
+            const float corr0 = grow[0] ? ex2(m_ref[0] - bm[0]) : 1.f, corr1 = grow[1] ? ex2(m_ref[1] - bm[1]) : 1.f;
 #pragma unroll 1
-            for (int c0 = 0; c0 < HD; c0 += 32) {
+            for (int c0 = 0; c0 < HD; c0 += 64) {
               uint32_t o[32];
-              tmem_ld32(lane_addr + (uint32_t)c0, o);
+              tmem_ld16x64(lane_addr + (uint32_t)c0, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
-              tmem_st32(lane_addr + (uint32_t)c0, o);
+              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * (c & 2 ? corr1 : corr0));
+              tmem_st16x64(lane_addr + (uint32_t)c0, o);
             }
-            if (grow) { l *= corr; l_true *= corr; m_ref = bm; }
+            tmem_st_wait();
+            if (grow[0]) { l[0] *= corr0; l_true[0] *= corr0; m_ref[0] = bm[0]; }
+            if (grow[1]) { l[1] *= corr1; l_true[1] *= corr1; m_ref[1] = bm[1]; }
           }
-          if (m_ref == -INFINITY) m_ref = bm;
-          const float nbase = (m_ref == -INFINITY ? 0.f : -m_ref) + CaType<T>::SHIFT;
-          uint32_t p[32];
-          float sum[2] = {0.f, 0.f}, sum_true[2] = {0.f, 0.f};
+          uint32_t p[16];
 #pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            const float p0 = ex2(fmaf(__uint_as_float(s0[c]), scale, nbase)), p1 = ex2(fmaf(__uint_as_float(s0[c + 1]), scale, nbase));
-            const float p2 = ex2(fmaf(__uint_as_float(s1[c]), scale, nbase)), p3 = ex2(fmaf(__uint_as_float(s1[c + 1]), scale, nbase));
-            p[c / 2] = pack2(p0, p1, T());
-            p[16 + c / 2] = pack2(p2, p3, T());
-            const float2 u = unpack2(p[c / 2], T()), v = unpack2(p[16 + c / 2], T());
-            sum[0] += u.x + u.y; sum[1] += v.x + v.y;
-            sum_true[0] += p0 + p1; sum_true[1] += p2 + p3;
+          for (int k = 0; k < 2; ++k) {
+            if (m_ref[k] == -INFINITY) m_ref[k] = bm[k];
+            const float nbase = (m_ref[k] == -INFINITY ? 0.f : -m_ref[k]) + CaType<T>::SHIFT;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              const float p0 = ex2(fmaf(__uint_as_float(sr[4 * c + 2 * k]), scale, nbase)), p1 = ex2(fmaf(__uint_as_float(sr[4 * c + 2 * k + 1]), scale, nbase));
+              p[2 * c + k] = pack2(p0, p1, T());
+              const float2 f = unpack2(p[2 * c + k], T());
+              l[k] += f.x + f.y;
+              l_true[k] += p0 + p1;
+            }
           }
-          l += sum[0] + sum[1];
-          l_true += sum_true[0] + sum_true[1];
-          tmem_st32(s_col, p);
+          tmem_st16x32(s_col, p);
           tmem_st_wait();
           tc_fence_before();
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + (x & 1));
+        if (lane == 0) mbar_arrive(p_full + sb);
+        if (++sb == SB) { sb = 0; sph ^= 1u; }
       }
-      g += n;
-      more = w.next(a);
-      if (more) load_q();                                                   // (S of the last unit is done: nobody reads the queries any more)
-      wait(o_done + ((g - 1) & 1), (uint32_t)((g - 1) >> 1) & 1u);
+      // ---- epilogue
+      const bool starts = s.b0 == 0, final = starts && !s.follow && (PAGES || !a.shared_tokens), row_on = !PAGES || s.seq >= 0;
+      float inv[2];
+      long long at[2];
+      int r[2], h[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
+        l_true[k] += __shfl_xor_sync(0xffffffffu, l_true[k], 1);
+        l_true[k] += __shfl_xor_sync(0xffffffffu, l_true[k], 2);
+        inv[k] = l[k] > 0.f ? 1.f / l[k] : 0.f;
+        const int e = base + quad + 8 * k;
+        r[k] = s.row0 + e / a.group;
+        h[k] = s.kvh * a.group + e % a.group;
+        const long long rh = (long long)r[k] * a.heads + h[k];
+        at[k] = starts ? (PAGES ? rh : (long long)s.phase * a.rows * a.heads + rh) : (long long)cta * 128 + e;
+        if (mine[k] && ql == 0) {
+          const float m = m_ref[k] == -INFINITY ? m_ref[k] : m_ref[k] - CaType<T>::SHIFT;
+          if (starts) {
+            a.part_ml[at[k]] = make_float4(m, l[k], l_true[k], pack_follow(e, final || !row_on ? CA_DONE : s.follow, cta + 1));
+            if (final && row_on && a.lse) a.lse[rh] = l[k] > 0.f ? (m + log2f(l_true[k])) * 0.6931471805599453f : -INFINITY;
+          } else a.cont_ml[at[k]] = make_float4(m, l[k], l_true[k], 0.f);
+        }
+      }
+      wait(o_done + (g - 1) % SB, (uint32_t)((g - 1) / SB) & 1u);
       if (active && ok) {
         tc_fence_after();
-        const float m = m_ref == -INFINITY ? m_ref : m_ref - CaType<T>::SHIFT;
-        const long long rh = (long long)r * a.heads + h;
-        const bool final = starts && !follow && (PAGES || !a.shared_tokens);
-        const long long at = starts ? (PAGES ? rh : (long long)phase * a.rows * a.heads + rh) : (long long)cta * 128 + e;
-        float *po = (starts ? a.part_o : a.cont_o) + at * HD;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        T *out = (T *)a.out + (long long)r * a.out_ld + (long long)h * HD;
 #pragma unroll 1
-        for (int c0 = 0; c0 < HD; c0 += 32) {
-          uint32_t o[32];
-          tmem_ld32(lane_addr + (uint32_t)c0, o);
+        for (int c0 = 0; c0 < HD; c0 += 64) {
+          uint32_t o[32];                                                   // o[4 c + 2 k + j]: row k, column c0 + 8 c + 2 ql + j
+          tmem_ld16x64(lane_addr + (uint32_t)c0, o);
           tmem_ld_wait();
-          if (!mine) continue;
           if (final) {
-            if (row_on) {
-              const float f = l > 0.f ? inv : 0.f;
 #pragma unroll
-              for (int c = 0; c < 32; c += 8) {
+            for (int k = 0; k < 2; ++k) {
+              T *out = (T *)a.out + (long long)r[k] * a.out_ld + (long long)h[k] * HD + c0;
+#pragma unroll
+              for (int b = 0; b < 2; ++b) {
                 uint32_t z[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) z[k] = pack2(__uint_as_float(o[c + 2 * k]) * f, __uint_as_float(o[c + 2 * k + 1]) * f, T());
-                *reinterpret_cast<uint4 *>(out + c0 + c) = make_uint4(z[0], z[1], z[2], z[3]);
+                for (int c = 0; c < 4; ++c) z[c] = pack2(__uint_as_float(o[16 * b + 4 * c + 2 * k]) * inv[k], __uint_as_float(o[16 * b + 4 * c + 2 * k + 1]) * inv[k], T());
+                quad_transpose(z, lane);                                    // a lane now has eight columns that stand side by side
+                if (mine[k] && row_on) *reinterpret_cast<uint4 *>(out + 32 * b + 8 * ql) = make_uint4(z[0], z[1], z[2], z[3]);
               }
             }
           } else {
 #pragma unroll
-            for (int c = 0; c < 32; c += 4) *reinterpret_cast<uint4 *>(po + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+            for (int k = 0; k < 2; ++k) {
+              if (!mine[k]) continue;
+              float *po = (starts ? a.part_o : a.cont_o) + at[k] * HD + c0 + 2 * ql;
+#pragma unroll
+              for (int c = 0; c < 8; ++c) *reinterpret_cast<uint2 *>(po + 8 * c) = make_uint2(o[4 * c + 2 * k], o[4 * c + 2 * k + 1]);
+            }
           }
-        }
-        if (mine) {
-          if (starts) {
-            a.part_ml[at] = make_float4(m, l, l_true, pack_follow(e, final || !row_on ? CA_DONE : follow, cta + 1));
-            if (final && row_on && a.lse) a.lse[rh] = l > 0.f ? (m + log2f(l_true)) * 0.6931471805599453f : -INFINITY;
-          } else a.cont_ml[at] = make_float4(m, l, l_true, 0.f);
         }
       }
       tc_fence_before();
@@ -592,8 +654,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   }
 }
 
-// The segments of a (row, head), from the first to the last: out = sum w O / sum w l with w = 2^(m - max m).  A thread takes eight columns.  PHASES: 1, or 2 where
-// the shared pages have partials of their own.
+// The segments of a (row, head), from the first to the last: out = sum w O / sum w l with w = 2^(m - max m).  A thread takes eight columns, and of the segments four
+// at a time, so that their loads are under way together.
 template <typename T, int HD, bool PAGES>
 __global__ void __launch_bounds__(256)
 k_cache_merge(const __grid_constant__ CacheAttnArgs a) {
@@ -603,29 +665,44 @@ k_cache_merge(const __grid_constant__ CacheAttnArgs a) {
   const int c0 = (int)(i % V) * 8, r = (int)(rh / a.heads);
   if (r >= a.rows || (!PAGES && r >= a.q_start[a.c.n_seqs])) return;
   float M = -INFINITY, L = 0.f, Lt = 0.f, acc[8] = {};
-  const int first = PAGES || a.shared_tokens ? 0 : 1;
-  for (int phase = first; phase < (PAGES ? 1 : 2); ++phase) {
-    const long long at = (long long)phase * a.rows * a.heads + rh;
-    float4 ml = a.part_ml[at];
-    const int f = __float_as_int(ml.w), entry = f & 127, cta = f >> 18 & 0x3ff;
+  auto add = [&](const float4 &ml, const float4 &x, const float4 &y) {
+    if (ml.x == -INFINITY) return;
+    const float Mn = fmaxf(M, ml.x), sc = ex2(M - Mn), w = ex2(ml.x - Mn);
+    L = L * sc + ml.y * w; Lt = Lt * sc + ml.z * w;
+    acc[0] = acc[0] * sc + x.x * w; acc[1] = acc[1] * sc + x.y * w; acc[2] = acc[2] * sc + x.z * w; acc[3] = acc[3] * sc + x.w * w;
+    acc[4] = acc[4] * sc + y.x * w; acc[5] = acc[5] * sc + y.y * w; acc[6] = acc[6] * sc + y.z * w; acc[7] = acc[7] * sc + y.w * w;
+    M = Mn;
+  };
+  // what starts the row's items, shared and own
+  const int first = PAGES || a.shared_tokens ? 0 : 1, last = PAGES ? 0 : 1;
+  float4 ml[2], x[2], y[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const long long at = (long long)k * a.rows * a.heads + rh;
+    const bool on = k >= first && k <= last;
+    ml[k] = on ? a.part_ml[at] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    x[k] = on ? *reinterpret_cast<const float4 *>(a.part_o + at * HD + c0) : make_float4(0.f, 0.f, 0.f, 0.f);
+    y[k] = on ? *reinterpret_cast<const float4 *>(a.part_o + at * HD + c0 + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (k < first || k > last) continue;
+    const int f = __float_as_int(ml[k].w), entry = f & 127, cta = f >> 18 & 0x3ff;
     int n = f >> 7 & 0x7ff;
     if (n == CA_DONE) return;
     n = min(n, a.n_ctas - cta);
-    const float *po = a.part_o + at * HD;
-    for (int k = 0;; ++k) {
-      const float Mn = fmaxf(M, ml.x);
-      if (ml.x != -INFINITY) {
-        const float sc = ex2(M - Mn), w = ex2(ml.x - Mn);
-        const float4 x = *reinterpret_cast<const float4 *>(po + c0), y = *reinterpret_cast<const float4 *>(po + c0 + 4);
-        L = L * sc + ml.y * w; Lt = Lt * sc + ml.z * w;
-        acc[0] = acc[0] * sc + x.x * w; acc[1] = acc[1] * sc + x.y * w; acc[2] = acc[2] * sc + x.z * w; acc[3] = acc[3] * sc + x.w * w;
-        acc[4] = acc[4] * sc + y.x * w; acc[5] = acc[5] * sc + y.y * w; acc[6] = acc[6] * sc + y.z * w; acc[7] = acc[7] * sc + y.w * w;
-        M = Mn;
+    add(ml[k], x[k], y[k]);
+    for (int j = 0; j < n; j += 4) {
+      float4 cm[4], cx[4], cy[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const long long c = (long long)(cta + min(j + q, n - 1)) * 128 + entry;
+        cm[q] = a.cont_ml[c];
+        cx[q] = *reinterpret_cast<const float4 *>(a.cont_o + c * HD + c0);
+        cy[q] = *reinterpret_cast<const float4 *>(a.cont_o + c * HD + c0 + 4);
       }
-      if (k >= n) break;
-      const long long c = (long long)(cta + k) * 128 + entry;
-      ml = a.cont_ml[c];
-      po = a.cont_o + c * HD;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) if (j + q < n) add(cm[q], cx[q], cy[q]);
     }
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
