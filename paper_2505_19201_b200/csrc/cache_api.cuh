@@ -129,9 +129,20 @@ extern "C" dream_status dream_cache_append(const dream_cache *cache, const void 
   a.q = q; a.q_ld = q_ld; a.k_new = k_new; a.k_ld = k_ld; a.v_new = v_new; a.v_ld = v_ld; a.q_out = q_out; a.q_out_ld = q_out_ld;
   a.row_seq = row_seq; a.slots = slots; a.positions = positions; a.rope = (const float2 *)rope; a.rows = rows; a.heads = q ? n_heads : 0; a.hd = hd;
   a.n_pos = n_pos; a.rot = rope ? rot_dim : 0; a.interleaved = interleaved != 0; a.status = status;
-  a.main_blocks = ((a.heads + 2 * a.c.hkv) * (hd / 16) + CACHE_THREADS - 1) / CACHE_THREADS;
-  const char *why = cache_launch(cache->dtype == DREAM_BF16 ? k_cache_append<bf16> : k_cache_append<f16>,
-                                 dim3(rows, a.main_blocks + (a.c.bounds ? a.c.hkv : 0)), CACHE_THREADS, 0, (cudaStream_t)cuda_stream, a);
+  // Four units a thread where that fills the GPU; else one, so that more threads share the latency.
+  const long long units = (long long)rows * (a.heads + 2 * a.c.hkv) * (hd / 16);
+  const int deep = units >= 4LL * CACHE_THREADS * 148 * 4 ? 4 : 1;
+  const long long blocks = (units + CACHE_THREADS * deep - 1) / (CACHE_THREADS * deep);
+  if (a.c.bounds) {
+    // a block looks over so many rows for full pages: few where there are few rows, all of which may fill one at once
+    a.bound_rows = (int)((long long)rows * a.c.hkv / (148 * 4));
+    a.bound_rows = a.bound_rows < 1 ? 1 : a.bound_rows > 32 ? 32 : a.bound_rows;
+    a.bound_blocks = (rows + a.bound_rows - 1) / a.bound_rows * a.c.hkv;
+  }
+  if (blocks + a.bound_blocks > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows of %d heads in one call", who, rows, a.heads);
+  void (*kernel)(CacheAppendArgs) = cache->dtype == DREAM_BF16 ? (deep > 1 ? k_cache_append<bf16, 4> : k_cache_append<bf16, 1>)
+                                                               : (deep > 1 ? k_cache_append<f16, 4> : k_cache_append<f16, 1>);
+  const char *why = cache_launch(kernel, dim3((unsigned)(blocks + a.bound_blocks)), CACHE_THREADS, 0, (cudaStream_t)cuda_stream, a);
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
 }
 
@@ -143,6 +154,18 @@ extern "C" dream_status dream_cache_select_bytes(const dream_cache *cache, int32
   if (!bytes) return fail(nullptr, DREAM_E_ARG, "dream_cache_select_bytes: null argument");
   *bytes = (size_t)rows * v.hkv * v.pages_per_seq * sizeof(uint32_t);
   return DREAM_OK;
+}
+
+template <typename T, int HD>
+static const char *cache_scores_run(const CacheSelectArgs &a, int rows, cudaStream_t stream) {
+  // as many heads of the group at a time as it has, up to four
+  void (*kernel)(CacheSelectArgs) = a.group == 1 ? k_cache_scores<T, HD, 1> : a.group == 2 ? k_cache_scores<T, HD, 2> : k_cache_scores<T, HD, 4>;
+  const int block = CACHE_THREADS / 32 * (32 / (HD / 8)) * SCORE_DEEP;
+  return cache_launch(kernel, dim3(rows * a.c.hkv, (a.c.pages_per_seq + block - 1) / block), CACHE_THREADS, 0, stream, a);
+}
+template <typename T>
+static const char *cache_scores(const CacheSelectArgs &a, int hd, int rows, cudaStream_t stream) {
+  return hd == 64 ? cache_scores_run<T, 64>(a, rows, stream) : hd == 128 ? cache_scores_run<T, 128>(a, rows, stream) : cache_scores_run<T, 256>(a, rows, stream);
 }
 
 extern "C" dream_status dream_cache_select(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *row_seq,
@@ -164,16 +187,22 @@ extern "C" dream_status dream_cache_select(const dream_cache *cache, const void 
     return fail(nullptr, DREAM_E_ARG, "%s: budget = %d must hold keep_first = %d >= 0 and keep_last = %d >= 1", who, budget, keep_first, keep_last);
   if (budget > CACHE_MAX_BUDGET) return fail(nullptr, DREAM_E_CAPACITY, "%s: budget above %d", who, CACHE_MAX_BUDGET);
   if (cache->pages_per_seq > CACHE_MAX_SELECT) return fail(nullptr, DREAM_E_CAPACITY, "%s: pages_per_seq above %d", who, CACHE_MAX_SELECT);
+  if ((long long)rows * cache->n_kv_heads > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows in one call", who, rows);
   s = dream_cache_select_bytes(cache, rows, &need);
   if (!s) s = cache_workspace(who, workspace, workspace_bytes, need);
   if (s) return s;
-  a.q = q; a.q_ld = q_ld; a.row_seq = row_seq; a.row_pos = row_pos; a.group = n_heads / a.c.hkv; a.hd = cache->head_dim;
+  a.q = q; a.q_ld = q_ld; a.row_seq = row_seq; a.row_pos = row_pos; a.group = n_heads / a.c.hkv;
   a.budget = budget; a.keep_first = keep_first; a.keep_last = keep_last; a.keys = (uint32_t *)workspace; a.ids = ids; a.status = status;
   const char *why = nullptr;
-  if (a.c.pages_per_seq > budget)
-    why = cache_launch(cache->dtype == DREAM_BF16 ? k_cache_scores<bf16> : k_cache_scores<f16>,
-                       dim3(rows * a.c.hkv, (a.c.pages_per_seq + SCORE_PAGES - 1) / SCORE_PAGES), CACHE_THREADS, 0, (cudaStream_t)cuda_stream, a);
-  if (!why) why = cache_launch(k_cache_select, dim3(rows * a.c.hkv), SELECT_THREADS, 0, (cudaStream_t)cuda_stream, a);
+  if (a.c.pages_per_seq > budget) why = cache->dtype == DREAM_BF16 ? cache_scores<bf16>(a, cache->head_dim, rows, (cudaStream_t)cuda_stream)
+                                                                  : cache_scores<f16>(a, cache->head_dim, rows, (cudaStream_t)cuda_stream);
+  // the keys of as many pages as a sequence may have are held in shared memory
+  const size_t smem = a.c.pages_per_seq > budget ? (size_t)a.c.pages_per_seq * sizeof(uint32_t) : 0;
+  if (!why && smem > 32 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(k_cache_select, cudaFuncAttributeMaxDynamicSharedMemorySize, CACHE_MAX_SELECT * (int)sizeof(uint32_t));
+    if (e != cudaSuccess) { cudaGetLastError(); why = cudaGetErrorString(e); }
+  }
+  if (!why) why = cache_launch(k_cache_select, dim3(rows * a.c.hkv), SELECT_THREADS, smem, (cudaStream_t)cuda_stream, a);
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
 }
 

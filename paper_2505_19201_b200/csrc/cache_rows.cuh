@@ -34,6 +34,10 @@ template <typename T> __device__ __forceinline__ uint4 pack8(const float (&f)[8]
   return q;
 }
 
+template <typename T> struct CaInf;
+template <> struct CaInf<bf16> { static constexpr uint32_t BITS = 0x7f80u; };
+template <> struct CaInf<f16> { static constexpr uint32_t BITS = 0x7c00u; };
+
 struct CacheAppendArgs {
   CacheView c;
   const void *q, *k_new, *v_new;
@@ -42,7 +46,7 @@ struct CacheAppendArgs {
   const int *row_seq, *slots, *positions;
   const float2 *rope;                      // [n_pos][rot / 2], or null (rot = 0 then)
   int rows, heads, hd, n_pos, rot, interleaved;
-  int main_blocks;                         // blocks per row that move it; behind them one per KV head for the bounds
+  int bound_blocks, bound_rows;            // blocks that look for full pages, and rows of one of them
   int *status;
 };
 
@@ -53,13 +57,16 @@ __device__ __forceinline__ void append_unit(const CacheAppendArgs &a, int u, int
   ia = split ? u * 8 : u * 16;
   ib = split ? u * 8 + a.rot / 2 : u * 16 + 8;
 }
-// The rotation of unit u, in 32 bits; rounded once, by whoever stores.
-__device__ __forceinline__ void append_rotate(const CacheAppendArgs &a, int u, int pos, float (&x)[8], float (&y)[8]) {
+// The rotation of unit u, in 32 bits, rounded once.
+template <typename T>
+__device__ __forceinline__ void append_rotate(const CacheAppendArgs &a, int u, int pos, uint4 &va, uint4 &vb) {
   if (u * 16 >= a.rot) return;
   const float4 *t = reinterpret_cast<const float4 *>(a.rope + (long long)pos * (a.rot / 2) + u * 8);
-  float cs[16];
+  float x[8], y[8], cs[16];
 #pragma unroll
   for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(cs + 4 * i) = t[i];
+  unpack8<T>(va, x);
+  unpack8<T>(vb, y);
   if (!a.interleaved) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -76,74 +83,32 @@ __device__ __forceinline__ void append_rotate(const CacheAppendArgs &a, int u, i
       q = q0 * c + p0 * s;
     }
   }
+  va = pack8<T>(x);
+  vb = pack8<T>(y);
 }
 
-// grid (rows, main_blocks + KV heads with bounds).  Blocks below main_blocks: a thread takes one unit of one head of the row, queries first, then
-// keys, then values.  The others: where the row fills its page, the bounds of one KV head of the page, from the rows of this call
-// (rotated once more: the same values) and, for tokens that came earlier, from the cache.
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b, bf16) { __nv_bfloat162 r = __hmin2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b)); return *reinterpret_cast<uint32_t *>(&r); }
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b, bf16) { __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b)); return *reinterpret_cast<uint32_t *>(&r); }
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b, f16) { __half2 r = __hmin2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b)); return *reinterpret_cast<uint32_t *>(&r); }
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b, f16) { __half2 r = __hmax2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b)); return *reinterpret_cast<uint32_t *>(&r); }
+
+// The bounds of one KV head of the page that row r fills, by a whole block: from the rows of this call (rotated once more: the same
+// values) and, for tokens that came earlier, from the cache.
 template <typename T>
-__global__ void __launch_bounds__(CACHE_THREADS)
-k_cache_append(const __grid_constant__ CacheAppendArgs a) {
-  kernel_entry(TR_k_cache_append);
-  const int r = blockIdx.x, seq = a.row_seq[r], slot = a.slots[r], units = a.hd / 16;
-  if (seq < 0) return;
-  const int pos = a.positions ? a.positions[r] : slot;
-  const bool ok = a.c.token_ok(seq, slot) && (!a.rot || (unsigned)pos < (unsigned)a.n_pos);
-  if ((int)blockIdx.y < a.main_blocks) {
-    const int i = blockIdx.y * CACHE_THREADS + threadIdx.x, hh = i / units, u = i - hh * units;
-    if (!ok) {
-      if (i == 0) cache_bad_index(a.status);
-      return;
-    }
-    if (hh >= a.heads + 2 * a.c.hkv) return;
-    int ia, ib;
-    append_unit(a, u, ia, ib);
-    const T *src;
-    T *dst = nullptr;
-    const bool is_v = hh >= a.heads + a.c.hkv;
-    if (hh < a.heads) {
-      src = (const T *)a.q + r * a.q_ld + (long long)hh * a.hd;
-      dst = (T *)a.q_out + r * a.q_out_ld + (long long)hh * a.hd;
-    } else {
-      const int kvh = hh - a.heads - (is_v ? a.c.hkv : 0), page = a.c.page(seq, slot >> a.c.page_shift);
-      src = is_v ? (const T *)a.v_new + r * a.v_ld + (long long)kvh * a.hd : (const T *)a.k_new + r * a.k_ld + (long long)kvh * a.hd;
-      if (page < 0) {
-        if (u == 0) cache_bad_index(a.status);
-        return;
-      }
-      dst = (T *)(is_v ? a.c.v : a.c.k) + a.c.at(page, kvh, slot & (a.c.page_tokens - 1));
-    }
-    uint4 va = *reinterpret_cast<const uint4 *>(src + ia), vb = *reinterpret_cast<const uint4 *>(src + ib);
-    if (!is_v && u * 16 < a.rot) {
-      float x[8], y[8];
-      unpack8<T>(va, x);
-      unpack8<T>(vb, y);
-      append_rotate(a, u, pos, x, y);
-      va = pack8<T>(x);
-      vb = pack8<T>(y);
-    }
-    *reinterpret_cast<uint4 *>(dst + ia) = va;
-    *reinterpret_cast<uint4 *>(dst + ib) = vb;
-    return;
-  }
-  // ---- bounds
-  const int pt = a.c.page_tokens;
-  if (!ok || (slot & (pt - 1)) != pt - 1) return;
-  __shared__ int from[256];                  // row of this call that holds the page's token, -1: it is in the cache already
-  __shared__ float red[2][CACHE_THREADS / 32][256];
-  __shared__ int missing;
-  const int kvh = blockIdx.y - a.main_blocks, first = slot - (pt - 1), tid = threadIdx.x, page = a.c.page(seq, slot >> a.c.page_shift);
-  if (page < 0) return;
-  if (tid == 0) missing = 0;
+__device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, int kvh, int *from, uint32_t (*red)[CACHE_THREADS / 32][128], int *missing) {
+  const int pt = a.c.page_tokens, seq = a.row_seq[r], slot = a.slots[r], first = slot - (pt - 1), tid = threadIdx.x, units = a.hd / 16;
+  const int page = a.c.page(seq, slot >> a.c.page_shift);
+  __syncthreads();                           // (the row before may still be read from)
+  if (tid == 0) *missing = 0;
   __syncthreads();
   for (int t = tid; t < pt; t += CACHE_THREADS) {       // as a rule the rows of a sequence stand in order
     const int rr = r - (pt - 1) + t;
     const bool here = rr >= 0 && a.row_seq[rr] == seq && a.slots[rr] == first + t;
-    from[t] = here ? rr : -1;
-    if (!here) missing = 1;
+    from[t] = here ? rr : -1;                // -1: it is in the cache already
+    if (!here) *missing = 1;
   }
   __syncthreads();
-  if (missing) {
+  if (*missing) {
     for (int rr = tid; rr < a.rows; rr += CACHE_THREADS)
       if (a.row_seq[rr] == seq && a.slots[rr] >= first && a.slots[rr] <= slot) from[a.slots[rr] - first] = rr;
     __syncthreads();
@@ -151,52 +116,124 @@ k_cache_append(const __grid_constant__ CacheAppendArgs a) {
   const int u = tid % units, groups = CACHE_THREADS / units;
   int ia, ib;
   append_unit(a, u, ia, ib);
-  float lo[16], hi[16];
+  uint32_t lo[8], hi[8];
+  const uint32_t plus = CaInf<T>::BITS * 0x10001u;         // two infinities
 #pragma unroll
-  for (int i = 0; i < 16; ++i) { lo[i] = INFINITY; hi[i] = -INFINITY; }
+  for (int i = 0; i < 8; ++i) { lo[i] = plus; hi[i] = plus | 0x80008000u; }
   for (int t = tid / units; t < pt; t += groups) {
     const int rr = from[t];
-    float x[8], y[8];
+    uint4 va, vb;
     if (rr >= 0) {
       const int p = a.positions ? a.positions[rr] : first + t;
       if (a.rot && (unsigned)p >= (unsigned)a.n_pos) continue;         // a row that is not written
       const T *src = (const T *)a.k_new + rr * a.k_ld + (long long)kvh * a.hd;
-      unpack8<T>(*reinterpret_cast<const uint4 *>(src + ia), x);
-      unpack8<T>(*reinterpret_cast<const uint4 *>(src + ib), y);
-      append_rotate(a, u, p, x, y);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { x[i] = to_f(from_f<T>(x[i])); y[i] = to_f(from_f<T>(y[i])); }
+      va = *reinterpret_cast<const uint4 *>(src + ia);
+      vb = *reinterpret_cast<const uint4 *>(src + ib);
+      append_rotate<T>(a, u, p, va, vb);
     } else {
       const T *src = (const T *)a.c.k + a.c.at(page, kvh, t);
-      unpack8<T>(*reinterpret_cast<const uint4 *>(src + ia), x);
-      unpack8<T>(*reinterpret_cast<const uint4 *>(src + ib), y);
+      va = *reinterpret_cast<const uint4 *>(src + ia);
+      vb = *reinterpret_cast<const uint4 *>(src + ib);
     }
+    const uint32_t w[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      lo[i] = fminf(lo[i], x[i]); hi[i] = fmaxf(hi[i], x[i]);
-      lo[8 + i] = fminf(lo[8 + i], y[i]); hi[8 + i] = fmaxf(hi[8 + i], y[i]);
-    }
+    for (int i = 0; i < 8; ++i) { lo[i] = min_pair(lo[i], w[i], T()); hi[i] = max_pair(hi[i], w[i], T()); }
   }
   for (int o = units; o < 32; o <<= 1)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      lo[i] = fminf(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
-      hi[i] = fmaxf(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
+    for (int i = 0; i < 8; ++i) {
+      lo[i] = min_pair(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o), T());
+      hi[i] = max_pair(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o), T());
     }
   if ((tid & 31) < units)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int d = i < 8 ? ia + i : ib + i - 8;
+    for (int i = 0; i < 8; ++i) {
+      const int d = (i < 4 ? ia + 2 * i : ib + 2 * i - 8) / 2;
       red[0][tid >> 5][d] = lo[i];
       red[1][tid >> 5][d] = hi[i];
     }
   __syncthreads();
-  T *out = (T *)a.c.bounds + ((long long)page * a.c.hkv + kvh) * 2 * a.hd;
-  for (int i = tid; i < 2 * a.hd; i += CACHE_THREADS) {
-    const int which = i >= a.hd, d = i - which * a.hd;
-    float m = red[which][0][d];
-    for (int w = 1; w < CACHE_THREADS / 32; ++w) m = which ? fmaxf(m, red[1][w][d]) : fminf(m, red[0][w][d]);
-    out[i] = from_f<T>(m);
+  uint32_t *out = reinterpret_cast<uint32_t *>((T *)a.c.bounds + ((long long)page * a.c.hkv + kvh) * 2 * a.hd);
+  for (int i = tid; i < a.hd; i += CACHE_THREADS) {
+    const int which = i >= a.hd / 2, d = i - which * (a.hd / 2);
+    uint32_t m = red[which][0][d];
+    for (int w = 1; w < CACHE_THREADS / 32; ++w) m = which ? max_pair(m, red[1][w][d], T()) : min_pair(m, red[0][w][d], T());
+    out[i] = m;
+  }
+}
+
+// Bound by HBM, or by latency where there are few rows.  Blocks from bound_blocks on move rows: a thread takes U units of the heads of consecutive rows (queries,
+// then keys, then values), whose loads are under way together; rows, positions and pages are looked up behind them.  The first
+// bound_blocks blocks look for rows that fill a page, a few rows and one KV head each.  One unit a thread and a block of 256 per row and part of it, 88 registers:
+// 5871 rows of 32 heads of 256 215 us.
+template <typename T, int U>
+__global__ void __launch_bounds__(CACHE_THREADS, 4)
+k_cache_append(const __grid_constant__ CacheAppendArgs a) {
+  kernel_entry(TR_k_cache_append);
+  if ((int)blockIdx.x < a.bound_blocks) {
+    __shared__ int from[256], missing;
+    __shared__ uint32_t red[2][CACHE_THREADS / 32][128];
+    const int kvh = blockIdx.x % a.c.hkv, r0 = blockIdx.x / a.c.hkv * a.bound_rows, lane = threadIdx.x & 31, pt = a.c.page_tokens;
+    // which of the rows fill a page: the same in every warp
+    const int r = r0 + lane;
+    bool fills = false;
+    if (lane < a.bound_rows && r < a.rows) {
+      const int seq = a.row_seq[r], slot = a.slots[r], pos = a.positions ? a.positions[r] : slot;
+      fills = seq >= 0 && a.c.token_ok(seq, slot) && (slot & (pt - 1)) == pt - 1 && (!a.rot || (unsigned)pos < (unsigned)a.n_pos) && a.c.page(seq, slot >> a.c.page_shift) >= 0;
+    }
+    for (unsigned left = __ballot_sync(0xffffffffu, fills); left; left &= left - 1) append_bounds<T>(a, r0 + __ffs(left) - 1, kvh, from, red, &missing);
+    return;
+  }
+  const int units = a.hd / 16, per_row = (a.heads + 2 * a.c.hkv) * units;
+  const long long first = (long long)(blockIdx.x - a.bound_blocks) * (CACHE_THREADS * U), row0 = first / per_row;
+  const unsigned off = (unsigned)(first - row0 * per_row) + threadIdx.x;
+  uint4 va[U], vb[U];
+  int row[U], hh[U], u[U], ia[U], ib[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const unsigned i = off + j * CACHE_THREADS, rr = i / (unsigned)per_row, w = i - rr * (unsigned)per_row;
+    row[j] = (int)(row0 + rr);
+    hh[j] = (int)(w / (unsigned)units);
+    u[j] = (int)w - hh[j] * units;
+    ia[j] = u[j] * 16; ib[j] = ia[j] + 8;
+    if (hh[j] < a.heads + a.c.hkv) append_unit(a, u[j], ia[j], ib[j]);
+    if (row[j] < a.rows) {
+      const T *src = hh[j] < a.heads ? (const T *)a.q + row[j] * a.q_ld + (long long)hh[j] * a.hd
+                     : hh[j] < a.heads + a.c.hkv ? (const T *)a.k_new + row[j] * a.k_ld + (long long)(hh[j] - a.heads) * a.hd
+                                                 : (const T *)a.v_new + row[j] * a.v_ld + (long long)(hh[j] - a.heads - a.c.hkv) * a.hd;
+      va[j] = *reinterpret_cast<const uint4 *>(src + ia[j]);
+      vb[j] = *reinterpret_cast<const uint4 *>(src + ib[j]);
+    }
+  }
+  int seq[U], slot[U], pos[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const bool on = row[j] < a.rows;
+    seq[j] = on ? a.row_seq[row[j]] : -1;
+    slot[j] = on ? a.slots[row[j]] : 0;
+    pos[j] = on && a.positions ? a.positions[row[j]] : slot[j];
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    if (seq[j] < 0) continue;
+    if (!a.c.token_ok(seq[j], slot[j]) || (a.rot && (unsigned)pos[j] >= (unsigned)a.n_pos)) {
+      if (u[j] == 0) cache_bad_index(a.status);
+      continue;
+    }
+    T *dst;
+    if (hh[j] < a.heads) dst = (T *)a.q_out + row[j] * a.q_out_ld + (long long)hh[j] * a.hd;
+    else {
+      const bool is_v = hh[j] >= a.heads + a.c.hkv;
+      const int page = a.c.page(seq[j], slot[j] >> a.c.page_shift);
+      if (page < 0) {
+        if (u[j] == 0) cache_bad_index(a.status);
+        continue;
+      }
+      dst = (T *)(is_v ? a.c.v : a.c.k) + a.c.at(page, hh[j] - a.heads - (is_v ? a.c.hkv : 0), slot[j] & (a.c.page_tokens - 1));
+    }
+    if (hh[j] < a.heads + a.c.hkv) append_rotate<T>(a, u[j], pos[j], va[j], vb[j]);
+    *reinterpret_cast<uint4 *>(dst + ia[j]) = va[j];
+    *reinterpret_cast<uint4 *>(dst + ib[j]) = vb[j];
   }
 }
 
@@ -209,7 +246,7 @@ struct CacheSelectArgs {
   const void *q;
   long long q_ld;
   const int *row_seq, *row_pos;
-  int group, hd, budget, keep_first, keep_last;
+  int group, budget, keep_first, keep_last;
   uint32_t *keys;                          // [row][KV head][pages_per_seq]
   int *ids;
   int *status;
@@ -223,99 +260,231 @@ __device__ __forceinline__ uint32_t order_key(float v) {
 __device__ __forceinline__ int select_pages(const CacheSelectArgs &a, int seq, int pos) {
   return seq >= 0 && pos >= 0 && a.c.token_ok(seq, pos) ? (pos >> a.c.page_shift) + 1 : 0;
 }
+// The high word of a 64-bit number that is 2^-896 (bf16) or 2^-1008 (fp16) times the 16-bit one, exactly, subnormal ones included: its exponent and fraction moved into
+// place; the low word is 0.  x: the number in the upper 16 bits.  (A conversion instruction takes four times the time.)  The query's side of the product gets the
+// factor back.  Infinite numbers count as the next power of two above the largest.
+template <typename T> struct CaWide;
+template <> struct CaWide<bf16> {
+  static constexpr int UP = 896;
+  static __device__ __forceinline__ int high(uint32_t x) { return (int)((uint32_t)((int)x >> 3) & 0x8fffe000u); }
+};
+template <> struct CaWide<f16> {
+  static constexpr int UP = 1008;
+  static __device__ __forceinline__ int high(uint32_t x) { return (int)((x & 0x80000000u) | (x >> 6 & 0x01fffc00u)); }
+};
 
-#define SCORE_PAGES 64                       // pages of a block
-#define SELECT_THREADS 256
-
-// grid (rows * KV heads, ceil(pages_per_seq / SCORE_PAGES)).  A warp takes page after page, its lanes the channels.
-template <typename T>
+// Bound by HBM, by arithmetic where many query heads share a KV head.  HD / 8 lanes take a page, eight channels each; a warp has SCORE_DEEP pages per lane under way at a time.  Every
+// product is exact in 64 bits (8 and 8, or 11 and 11, digits), and so is nearly every sum: in another order it comes out the same.  GC heads of the group at a time: a
+// lane has SCORE_DEEP * GC partial sums, which are added up across the lanes by halves, each step with half as many of them, and then compared.
+#define SCORE_DEEP 4
+template <typename T, int HD, int GC>
 __global__ void __launch_bounds__(CACHE_THREADS)
 k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
+  constexpr int LANES = HD / 8, PAGES = 32 / LANES, NV = SCORE_DEEP * GC, BLOCK = CACHE_THREADS / 32 * PAGES * SCORE_DEEP;
+  __shared__ double2 q_s[GC][4][LANES];
   kernel_entry(TR_k_cache_scores);
   const int r = blockIdx.x / a.c.hkv, kvh = blockIdx.x % a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos);
-  if (n <= a.budget) return;                 // all of them are kept
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, end = min(n - a.keep_last, (int)(blockIdx.y + 1) * SCORE_PAGES);
-  uint32_t *keys = a.keys + (long long)blockIdx.x * a.c.pages_per_seq;
-  for (int p = max(a.keep_first, (int)blockIdx.y * SCORE_PAGES) + warp; p < end; p += CACHE_THREADS / 32) {
-    const int page = a.c.page(seq, p);
-    if (page < 0) {
-      if (lane == 0) { cache_bad_index(a.status); keys[p] = 0u; }
-      continue;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LANES, end = n - a.keep_last;
+  const int p0 = blockIdx.y * BLOCK + warp * PAGES * SCORE_DEEP + lane / LANES;       // pages p0, p0 + PAGES, ...
+  if (n <= a.budget || (int)(blockIdx.y * BLOCK) >= end) return;                       // all are kept, or there are none here
+  uint4 lo[SCORE_DEEP], hi[SCORE_DEEP];
+  bool bad[SCORE_DEEP];
+#pragma unroll
+  for (int j = 0; j < SCORE_DEEP; ++j) {
+    const int p = p0 + j * PAGES;
+    const bool on = p >= a.keep_first && p < end;
+    const int page = on ? a.c.page(seq, p) : -1;
+    bad[j] = page < 0;
+    if (on && bad[j] && l == 0) cache_bad_index(a.status);
+    lo[j] = hi[j] = make_uint4(0u, 0u, 0u, 0u);
+    if (page >= 0) {
+      const uint4 *b = reinterpret_cast<const uint4 *>((const T *)a.c.bounds + ((long long)page * a.c.hkv + kvh) * 2 * HD) + l;
+      lo[j] = b[0];
+      hi[j] = b[LANES];
     }
-    const T *lo = (const T *)a.c.bounds + ((long long)page * a.c.hkv + kvh) * 2 * a.hd, *hi = lo + a.hd;
-    float best = -INFINITY;
-    for (int g = 0; g < a.group; ++g) {
-      const T *q = (const T *)a.q + r * a.q_ld + (long long)(kvh * a.group + g) * a.hd;
-      double s = 0.0;
-      for (int d = lane; d < a.hd; d += 32) {
-        const float x = to_f(q[d]);
-        s += (double)x * (double)to_f(x >= 0.f ? hi[d] : lo[d]);
+  }
+  float best[NV > LANES ? NV / LANES : 1];
+#pragma unroll
+  for (int j = 0; j < (NV > LANES ? NV / LANES : 1); ++j) best[j] = -INFINITY;
+  for (int g0 = 0; g0 < a.group; g0 += GC) {
+    if (g0) __syncthreads();
+    for (int i = threadIdx.x; i < GC * HD / 2; i += CACHE_THREADS) {
+      const int g = i / (HD / 2), d = i % (HD / 2) * 2;                                // channels d and d + 1: lane d / 8, pair d % 8 / 2
+      double2 x = make_double2(0.0, 0.0);
+      if (g0 + g < a.group) {
+        const T *q = (const T *)a.q + r * a.q_ld + (long long)(kvh * a.group + g0 + g) * HD + d;
+        x = make_double2(scalbn((double)to_f(q[0]), CaWide<T>::UP), scalbn((double)to_f(q[1]), CaWide<T>::UP));
       }
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      best = fmaxf(best, (float)s);
+      q_s[g][d % 8 / 2][d / 8] = x;
     }
-    if (lane == 0) keys[p] = order_key(best);
+    __syncthreads();
+    double v[NV];                                          // v[g * SCORE_DEEP + j]
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = 0.0;
+#pragma unroll
+    for (int g = 0; g < GC; ++g) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const double2 q = q_s[g][e][l];
+        const bool nx = __double2hiint(q.x) < 0, ny = __double2hiint(q.y) < 0;
+#pragma unroll
+        for (int j = 0; j < SCORE_DEEP; ++j) {
+          const uint32_t L = e == 0 ? lo[j].x : e == 1 ? lo[j].y : e == 2 ? lo[j].z : lo[j].w, H = e == 0 ? hi[j].x : e == 1 ? hi[j].y : e == 2 ? hi[j].z : hi[j].w;
+          v[g * SCORE_DEEP + j] = fma(q.x, __hiloint2double(CaWide<T>::high((nx ? L : H) << 16), 0), v[g * SCORE_DEEP + j]);
+          v[g * SCORE_DEEP + j] = fma(q.y, __hiloint2double(CaWide<T>::high((ny ? L : H) & 0xffff0000u), 0), v[g * SCORE_DEEP + j]);
+        }
+      }
+    }
+    // across the lanes of a page: at each step a lane gives away one half of its sums and adds to the other
+    int width = NV;
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+      if (width > 1) {
+        width /= 2;
+        const bool up = (lane & o) != 0;
+#pragma unroll
+        for (int j = 0; j < NV / 2; ++j)
+          if (j < width) {
+            const double give = up ? v[j] : v[j + width], keep = up ? v[j + width] : v[j];
+            v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+          }
+      } else v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    }
+    // the largest of the group's heads: those past the group have no say.  Value i = g * SCORE_DEEP + j; its high bits were chosen by the lane's
+    constexpr int LEFT = NV > LANES ? NV / LANES : 1, STEPS = NV > LANES ? LANES : NV;
+    const int own = STEPS > 1 ? l / (LANES / STEPS) : 0;                                // the lane's value(s) are own * LEFT + (0 .. LEFT - 1)
+#pragma unroll
+    for (int j = 0; j < LEFT; ++j) {
+      float f = g0 + (own * LEFT + j) / SCORE_DEEP < a.group ? (float)v[j] : -INFINITY;
+      if (f != f) f = -INFINITY;
+#pragma unroll
+      for (int o = LANES / 2; o >= LANES / STEPS * (SCORE_DEEP / LEFT); o >>= 1) f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, o));
+      best[j] = fmaxf(best[j], f);
+    }
+  }
+  // lane l has the scores of page j = own * LEFT + (0 .. LEFT - 1), modulo SCORE_DEEP
+  constexpr int LEFT = NV > LANES ? NV / LANES : 1, STEPS = NV > LANES ? LANES : NV;
+  const int own = STEPS > 1 ? l / (LANES / STEPS) : 0;
+  uint32_t *keys = a.keys + (long long)blockIdx.x * a.c.pages_per_seq;
+#pragma unroll
+  for (int j = 0; j < LEFT; ++j) {
+    const int i = own * LEFT + j, deep = i % SCORE_DEEP, p = p0 + deep * PAGES;
+    bool b = bad[0];
+#pragma unroll
+    for (int k = 1; k < SCORE_DEEP; ++k) if (deep == k) b = bad[k];
+    if (i < SCORE_DEEP && l % (LANES / STEPS) == 0 && p >= a.keep_first && p < end) keys[p] = b ? 0u : order_key(best[j]);
   }
 }
 
-// grid (rows * KV heads).  Radix selection of the cut, eight bits a turn, then the kept pages in order.
+// grid (rows * KV heads), the keys in shared memory.  The cut: bins over the range of the keys, of equal width, so that they are filled evenly whatever the scores are; the bin in which
+// the cut falls is looked into again until it holds few keys, which are compared with each other.  Then the kept pages in order: a thread has a run of pages.
+#define SELECT_THREADS 512
+#define SELECT_BINS 2048
+#define SELECT_FEW 64
 __global__ void __launch_bounds__(SELECT_THREADS)
 k_cache_select(const __grid_constant__ CacheSelectArgs a) {
+  extern __shared__ uint32_t sel_keys[];
+  __shared__ int hist[SELECT_BINS], scan[SELECT_THREADS / 32], n_few, cut_bin, cut_above, cut_count, cut_ties;
+  __shared__ uint32_t few[SELECT_FEW], red[2], cut_key;
   kernel_entry(TR_k_cache_select);
-  const int r = blockIdx.x / a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos), tid = threadIdx.x;
+  const int r = blockIdx.x / a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int *ids = a.ids + (long long)blockIdx.x * a.budget;
   if (seq >= 0 && pos >= 0 && !n && tid == 0) cache_bad_index(a.status);
   if (n <= a.budget) {
     for (int i = tid; i < a.budget; i += SELECT_THREADS) ids[i] = i < n ? i : -1;
     return;
   }
-  __shared__ int hist[256], scan[SELECT_THREADS / 32], cut_bin, cut_left;
   const uint32_t *keys = a.keys + (long long)blockIdx.x * a.c.pages_per_seq;
-  const int p0 = a.keep_first, p1 = n - a.keep_last, lane = tid & 31, warp = tid >> 5;
-  int left = a.budget - a.keep_first - a.keep_last;             // to be taken by score: fewer than the p1 - p0 there are
-  uint32_t prefix = 0u, mask = 0u;
-  for (int shift = 24; shift >= 0 && left > 0; shift -= 8) {
-    hist[tid] = 0;
+  const int p0 = a.keep_first, m = n - a.keep_last - p0;        // candidates p0 .. p0 + m - 1
+  int left = a.budget - a.keep_first - a.keep_last;             // of which so many are taken: fewer than there are
+  uint32_t low = 0xffffffffu, high = 0u;
+  if (tid == 0) { red[0] = 0xffffffffu; red[1] = 0u; cut_key = 0u; cut_ties = 0; }
+  __syncthreads();
+  if (left) {
+    for (int i = tid; i < m; i += SELECT_THREADS) {
+      const uint32_t k = keys[p0 + i];
+      sel_keys[i] = k;
+      low = min(low, k); high = max(high, k);
+    }
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    if (lane == 0) { atomicMin(red, low); atomicMax(red + 1, high); }
     __syncthreads();
-    for (int p = p0 + tid; p < p1; p += SELECT_THREADS)
-      if ((keys[p] & mask) == prefix) atomicAdd(hist + (keys[p] >> shift & 255), 1);
+    low = red[0]; high = red[1];
+  }
+  while (left) {                                                // keys low .. high hold the cut: the left-th largest of them
+    int shift = 0;
+    while ((high - low) >> shift >= SELECT_BINS) ++shift;
+    for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) hist[i] = 0;
+    if (tid == 0) n_few = 0;
     __syncthreads();
-    // how many lie in this bin or above: the bin in which the cut falls
-    int own = hist[255 - tid], sum = own;
+    for (int i = tid; i < m; i += SELECT_THREADS) {
+      const uint32_t k = sel_keys[i];
+      if (k >= low && k <= high) atomicAdd(hist + ((k - low) >> shift), 1);
+    }
+    __syncthreads();
+    // from the top: bins 4 tid' .. 4 tid' + 3 with tid' = SELECT_THREADS - 1 - tid
+    constexpr int PER = SELECT_BINS / SELECT_THREADS;
+    int own = 0, sum;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) own += hist[(SELECT_THREADS - 1 - tid) * PER + k];
+    sum = own;
     for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
     if (lane == 31) scan[warp] = sum;
     __syncthreads();
     for (int w = 0; w < warp; ++w) sum += scan[w];
-    if (sum >= left && sum - own < left) { cut_bin = 255 - tid; cut_left = left - (sum - own); }
+    if (sum >= left && sum - own < left) {
+      int above = sum - own, b = (SELECT_THREADS - tid) * PER - 1;
+      while (above + hist[b] < left) above += hist[b--];
+      cut_bin = b; cut_above = above; cut_count = hist[b];
+    }
     __syncthreads();
-    prefix |= (uint32_t)cut_bin << shift;
-    mask |= 255u << shift;
-    left = cut_left;
+    left -= cut_above;
+    low += (uint32_t)cut_bin << shift;
+    high = min(high, low + (1u << shift) - 1u);
+    const int count = cut_count;
+    if (shift == 0) {                                           // a bin is a key
+      if (tid == 0) { cut_key = low; cut_ties = left; }
+      __syncthreads();
+      break;
+    }
+    if (count <= SELECT_FEW) {
+      for (int i = tid; i < m; i += SELECT_THREADS) {
+        const uint32_t k = sel_keys[i];
+        if (k >= low && k <= high) few[atomicAdd(&n_few, 1)] = k;
+      }
+      __syncthreads();
+      if (tid < count) {
+        int above = 0, same = 0;
+        for (int i = 0; i < count; ++i) { above += few[i] > few[tid]; same += few[i] == few[tid]; }
+        if (above < left && above + same >= left) { cut_key = few[tid]; cut_ties = left - above; }       // (equal keys write the same)
+      }
+      __syncthreads();
+      break;
+    }
     __syncthreads();
   }
-  // keys above the cut stay, and of those on it the first `left`; without a cut (nothing is taken by score) none
+  const uint32_t cut = cut_key;
+  const int take = cut_ties;                                    // of the keys on the cut, the first so many
   const bool none = a.budget == a.keep_first + a.keep_last;
-  int done = 0, ties = 0;                                       // pages written, pages on the cut passed
-  for (int base = 0; base < n; base += SELECT_THREADS) {
-    const int p = base + tid;
-    const uint32_t key = p >= p0 && p < p1 ? keys[p] : 0u;
-    const bool forced = p < n && (p < p0 || p >= p1), cand = p >= p0 && p < p1 && !none, tie = cand && key == prefix;
-    // two counts in one scan: ties in the upper half
-    int own = tie ? 1 << 16 : 0, sum = own;
-    for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
-    __syncthreads();
-    if (lane == 31) scan[warp] = sum;
-    __syncthreads();
-    int tie_at = ties + (sum - own >> 16), all = 0;
-    for (int w = 0; w < SELECT_THREADS / 32; ++w) { if (w < warp) tie_at += scan[w] >> 16; all += scan[w] >> 16; }
-    ties += all;
-    const bool keep = forced || (cand && key > prefix) || (tie && tie_at < left);
-    const unsigned b = __ballot_sync(0xffffffffu, keep);
-    __syncthreads();
-    if (lane == 0) scan[warp] = __popc(b);
-    __syncthreads();
-    int at = done + __popc(b & ((1u << lane) - 1u));
-    for (int w = 0; w < SELECT_THREADS / 32; ++w) { if (w < warp) at += scan[w]; done += scan[w]; }
-    if (keep) ids[at] = p;
-  }
+  // pages i0 .. i1 - 1 are this thread's
+  const int run = (m + SELECT_THREADS - 1) / SELECT_THREADS, i0 = min(m, tid * run), i1 = min(m, i0 + run);
+  int above = 0, ties = 0;
+  if (!none)
+    for (int i = i0; i < i1; ++i) { above += sel_keys[i] > cut; ties += sel_keys[i] == cut; }
+  int both = above | ties << 16, sum = both;                     // (no more than 32768 of each)
+  for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
+  if (lane == 31) scan[warp] = sum;
+  __syncthreads();
+  sum -= both;
+  for (int w = 0; w < warp; ++w) sum += scan[w];
+  int tie = sum >> 16 & 0xffff, at = a.keep_first + (sum & 0xffff) + min(tie, take);
+  if (!none)
+    for (int i = i0; i < i1; ++i) {
+      const uint32_t k = sel_keys[i];
+      if (k > cut || (k == cut && tie < take)) ids[at++] = p0 + i;
+      tie += k == cut;
+    }
+  for (int i = tid; i < a.keep_first; i += SELECT_THREADS) ids[i] = i;
+  for (int i = tid; i < a.keep_last; i += SELECT_THREADS) ids[a.budget - a.keep_last + i] = n - a.keep_last + i;
 }
