@@ -146,26 +146,43 @@ extern "C" dream_status dream_cache_append(const dream_cache *cache, const void 
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
 }
 
+// The parts of the selection's workspace; how many bytes they are.
+static size_t cache_select_room(const CacheView &v, int hd, int rows, void *workspace, CacheSelectArgs *a) {
+  // Blocks of the scores for each (row, KV head): as many as fill the GPU, three to an SM, and no more than there are pages for
+  const long long n = (long long)rows * v.hkv;
+  const int block = CACHE_THREADS / 32 * (32 / (hd / 8)) * SCORE_DEEP, most = (v.pages_per_seq + block - 1) / block;
+  const long long share = 148 * 3 / n;
+  const int blocks = share < 1 ? 1 : share < most ? (int)share : most;
+  const size_t scores = ((size_t)n * v.pages_per_seq * sizeof(float) + 255) / 256 * 256;
+  if (a) { a->scores = (float *)workspace; a->off = (float *)((char *)workspace + scores); a->score_blocks = blocks; }
+  return scores + ((size_t)n * blocks * sizeof(float) + 255) / 256 * 256;
+}
+
 extern "C" dream_status dream_cache_select_bytes(const dream_cache *cache, int32_t rows, size_t *bytes) {
   CacheView v;
   dream_status s = cache_view("dream_cache_select_bytes", cache, &v);
   if (!s) s = cache_heads("dream_cache_select_bytes", cache, rows, cache->n_kv_heads);
   if (s) return s;
   if (!bytes) return fail(nullptr, DREAM_E_ARG, "dream_cache_select_bytes: null argument");
-  *bytes = (size_t)rows * v.hkv * v.pages_per_seq * sizeof(uint32_t);
+  *bytes = cache_select_room(v, cache->head_dim, rows, nullptr, nullptr);
   return DREAM_OK;
 }
 
 template <typename T, int HD>
-static const char *cache_scores_run(const CacheSelectArgs &a, int rows, cudaStream_t stream) {
-  // as many heads of the group at a time as it has, up to four
-  void (*kernel)(CacheSelectArgs) = a.group == 1 ? k_cache_scores<T, HD, 1> : a.group == 2 ? k_cache_scores<T, HD, 2> : k_cache_scores<T, HD, 4>;
-  const int block = CACHE_THREADS / 32 * (32 / (HD / 8)) * SCORE_DEEP;
-  return cache_launch(kernel, dim3(rows * a.c.hkv, (a.c.pages_per_seq + block - 1) / block), CACHE_THREADS, 0, stream, a);
-}
-template <typename T>
-static const char *cache_scores(const CacheSelectArgs &a, int hd, int rows, cudaStream_t stream) {
-  return hd == 64 ? cache_scores_run<T, 64>(a, rows, stream) : hd == 128 ? cache_scores_run<T, 128>(a, rows, stream) : cache_scores_run<T, 256>(a, rows, stream);
+static const char *cache_select_run(const CacheSelectArgs &a, int rows, cudaStream_t stream) {
+  const char *why = nullptr;
+  size_t smem = 0;
+  if (a.c.pages_per_seq > a.budget) {
+    // as many heads of the group at a time as it has, up to four
+    void (*kernel)(CacheSelectArgs) = a.group == 1 ? k_cache_scores<T, HD, 1> : a.group == 2 ? k_cache_scores<T, HD, 2> : k_cache_scores<T, HD, 4>;
+    why = cache_launch(kernel, dim3(rows * a.c.hkv, a.score_blocks), CACHE_THREADS, 0, stream, a);
+    smem = (size_t)a.c.pages_per_seq * sizeof(uint32_t);      // of as many pages as a sequence may have
+  }
+  if (!why && smem > 32 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(k_cache_select<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, CACHE_MAX_SELECT * (int)sizeof(uint32_t));
+    if (e != cudaSuccess) { cudaGetLastError(); why = cudaGetErrorString(e); }
+  }
+  return why ? why : cache_launch(k_cache_select<T, HD>, dim3(rows * a.c.hkv), SELECT_THREADS, smem, stream, a);
 }
 
 extern "C" dream_status dream_cache_select(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *row_seq,
@@ -192,17 +209,13 @@ extern "C" dream_status dream_cache_select(const dream_cache *cache, const void 
   if (!s) s = cache_workspace(who, workspace, workspace_bytes, need);
   if (s) return s;
   a.q = q; a.q_ld = q_ld; a.row_seq = row_seq; a.row_pos = row_pos; a.group = n_heads / a.c.hkv;
-  a.budget = budget; a.keep_first = keep_first; a.keep_last = keep_last; a.keys = (uint32_t *)workspace; a.ids = ids; a.status = status;
-  const char *why = nullptr;
-  if (a.c.pages_per_seq > budget) why = cache->dtype == DREAM_BF16 ? cache_scores<bf16>(a, cache->head_dim, rows, (cudaStream_t)cuda_stream)
-                                                                  : cache_scores<f16>(a, cache->head_dim, rows, (cudaStream_t)cuda_stream);
-  // the keys of as many pages as a sequence may have are held in shared memory
-  const size_t smem = a.c.pages_per_seq > budget ? (size_t)a.c.pages_per_seq * sizeof(uint32_t) : 0;
-  if (!why && smem > 32 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(k_cache_select, cudaFuncAttributeMaxDynamicSharedMemorySize, CACHE_MAX_SELECT * (int)sizeof(uint32_t));
-    if (e != cudaSuccess) { cudaGetLastError(); why = cudaGetErrorString(e); }
-  }
-  if (!why) why = cache_launch(k_cache_select, dim3(rows * a.c.hkv), SELECT_THREADS, smem, (cudaStream_t)cuda_stream, a);
+  a.budget = budget; a.keep_first = keep_first; a.keep_last = keep_last; a.ids = ids; a.status = status;
+  cache_select_room(a.c, cache->head_dim, rows, workspace, &a);
+  const bool bf = cache->dtype == DREAM_BF16;
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  const char *why = cache->head_dim == 64 ? (bf ? cache_select_run<bf16, 64>(a, rows, stream) : cache_select_run<f16, 64>(a, rows, stream))
+                  : cache->head_dim == 128 ? (bf ? cache_select_run<bf16, 128>(a, rows, stream) : cache_select_run<f16, 128>(a, rows, stream))
+                                           : (bf ? cache_select_run<bf16, 256>(a, rows, stream) : cache_select_run<f16, 256>(a, rows, stream));
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
 }
 

@@ -167,7 +167,7 @@ __device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, i
 // bound_blocks blocks look for rows that fill a page, a few rows and one KV head each.  One unit a thread and a block of 256 per row and part of it, 88 registers:
 // 5871 rows of 32 heads of 256 215 us.
 template <typename T, int U>
-__global__ void __launch_bounds__(CACHE_THREADS, 4)
+__global__ void __launch_bounds__(CACHE_THREADS, U > 1 ? 3 : 4)
 k_cache_append(const __grid_constant__ CacheAppendArgs a) {
   kernel_entry(TR_k_cache_append);
   if ((int)blockIdx.x < a.bound_blocks) {
@@ -247,7 +247,9 @@ struct CacheSelectArgs {
   long long q_ld;
   const int *row_seq, *row_pos;
   int group, budget, keep_first, keep_last;
-  uint32_t *keys;                          // [row][KV head][pages_per_seq]
+  float *scores;                           // [row][KV head][pages_per_seq], as k_cache_scores has them ...
+  float *off;                              // [row][KV head][score_blocks]: ... each right to so much, by the block that made it
+  int score_blocks;
   int *ids;
   int *status;
 };
@@ -256,235 +258,352 @@ __device__ __forceinline__ uint32_t order_key(float v) {
   const uint32_t u = __float_as_uint(v + 0.f);
   return v == v ? u ^ (u & 0x80000000u ? 0xffffffffu : 0x80000000u) : 0u;
 }
+__device__ __forceinline__ float order_value(uint32_t k) { return __uint_as_float(k ^ (k & 0x80000000u ? 0x80000000u : 0xffffffffu)); }
 // Pages up to the row's own; 0 for a row without any.
 __device__ __forceinline__ int select_pages(const CacheSelectArgs &a, int seq, int pos) {
   return seq >= 0 && pos >= 0 && a.c.token_ok(seq, pos) ? (pos >> a.c.page_shift) + 1 : 0;
 }
-// The high word of a 64-bit number that is 2^-896 (bf16) or 2^-1008 (fp16) times the 16-bit one, exactly, subnormal ones included: its exponent and fraction moved into
-// place; the low word is 0.  x: the number in the upper 16 bits.  (A conversion instruction takes four times the time.)  The query's side of the product gets the
-// factor back.  Infinite numbers count as the next power of two above the largest.
-template <typename T> struct CaWide;
-template <> struct CaWide<bf16> {
-  static constexpr int UP = 896;
-  static __device__ __forceinline__ int high(uint32_t x) { return (int)((uint32_t)((int)x >> 3) & 0x8fffe000u); }
-};
-template <> struct CaWide<f16> {
-  static constexpr int UP = 1008;
-  static __device__ __forceinline__ int high(uint32_t x) { return (int)((x & 0x80000000u) | (x >> 6 & 0x01fffc00u)); }
-};
-
-// Bound by HBM, by arithmetic where many query heads share a KV head.  HD / 8 lanes take a page, eight channels each; a warp has SCORE_DEEP pages per lane under way at a time.  Every
-// product is exact in 64 bits (8 and 8, or 11 and 11, digits), and so is nearly every sum: in another order it comes out the same.  GC heads of the group at a time: a
-// lane has SCORE_DEEP * GC partial sums, which are added up across the lanes by halves, each step with half as many of them, and then compared.
+// Scores in 32 bits, with a bound on how far they are off.  (Which pages are kept is a matter of the scores in 64 bits, but only for the few near the cut, which
+// k_cache_select looks at again; in 64 bits for all, a score took four times the instructions, and 64 rows of 1024 pages 20 us.)  HD / 8 lanes take a page, eight
+// channels each; a warp has SCORE_DEEP pages per lane under way at a time, and GC heads of the group: a lane has SCORE_DEEP * GC partial sums,
+// which are added up across the lanes by halves, each step with half as many of them, and then compared.
+// The bound: a sum is eight fused steps in a lane and up to five additions across lanes, each wrong by 2^-24 of a partial sum, which is no larger than
+// sum |q_d| times the largest bound there is; one more such error for the rounding of the exact score, and three for the bound's own.
 #define SCORE_DEEP 4
+template <typename T> __device__ __forceinline__ float2 widen2(uint32_t w);
+template <> __device__ __forceinline__ float2 widen2<bf16>(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+template <> __device__ __forceinline__ float2 widen2<f16>(uint32_t w) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
+
 template <typename T, int HD, int GC>
-__global__ void __launch_bounds__(CACHE_THREADS)
+__global__ void __launch_bounds__(CACHE_THREADS, 3)
 k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
   constexpr int LANES = HD / 8, PAGES = 32 / LANES, NV = SCORE_DEEP * GC, BLOCK = CACHE_THREADS / 32 * PAGES * SCORE_DEEP;
-  __shared__ double2 q_s[GC][4][LANES];
+  constexpr int LEFT = NV > LANES ? NV / LANES : 1, STEPS = NV > LANES ? LANES : NV;
+  __shared__ float4 q_s[GC][2][LANES];                      // a lane's eight channels of a head
+  __shared__ uint4 m_s[GC][LANES];                          // and where they are negative: a mask for each pair
+  __shared__ uint32_t top_s[CACHE_THREADS / 32];
+  __shared__ float q1_s;
   kernel_entry(TR_k_cache_scores);
   const int r = blockIdx.x / a.c.hkv, kvh = blockIdx.x % a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LANES, end = n - a.keep_last;
-  const int p0 = blockIdx.y * BLOCK + warp * PAGES * SCORE_DEEP + lane / LANES;       // pages p0, p0 + PAGES, ...
-  if (n <= a.budget || (int)(blockIdx.y * BLOCK) >= end) return;                       // all are kept, or there are none here
-  uint4 lo[SCORE_DEEP], hi[SCORE_DEEP];
-  bool bad[SCORE_DEEP];
-#pragma unroll
-  for (int j = 0; j < SCORE_DEEP; ++j) {
-    const int p = p0 + j * PAGES;
-    const bool on = p >= a.keep_first && p < end;
-    const int page = on ? a.c.page(seq, p) : -1;
-    bad[j] = page < 0;
-    if (on && bad[j] && l == 0) cache_bad_index(a.status);
-    lo[j] = hi[j] = make_uint4(0u, 0u, 0u, 0u);
-    if (page >= 0) {
-      const uint4 *b = reinterpret_cast<const uint4 *>((const T *)a.c.bounds + ((long long)page * a.c.hkv + kvh) * 2 * HD) + l;
-      lo[j] = b[0];
-      hi[j] = b[LANES];
-    }
+  if (n <= a.budget) return;                               // all are kept
+  const T *q0 = (const T *)a.q + r * a.q_ld + (long long)kvh * a.group * HD;
+  // the largest sum |q_d| of the group's heads
+  if (threadIdx.x == 0) q1_s = 0.f;
+  __syncthreads();
+  for (int g = warp; g < a.group; g += CACHE_THREADS / 32) {
+    float sum = 0.f;
+    for (int d = lane; d < HD; d += 32) sum += fabsf(to_f(q0[g * HD + d]));
+    sum = warp_sum(sum);
+    if (lane == 0) atomicMax(reinterpret_cast<int *>(&q1_s), __float_as_int(sum));        // (floats above zero are ordered as integers are; NaN is above all)
   }
-  float best[NV > LANES ? NV / LANES : 1];
+  float *scores = a.scores + (long long)blockIdx.x * a.c.pages_per_seq;
+  uint32_t top = 0u;                                       // the largest magnitudes met, a pair
+  for (int base = blockIdx.y * BLOCK; base < end; base += gridDim.y * BLOCK) {
+    const int p0 = base + warp * PAGES * SCORE_DEEP + lane / LANES;                    // pages p0, p0 + PAGES, ...
+    uint4 lo[SCORE_DEEP], hi[SCORE_DEEP];
+    unsigned bad = 0;                                      // pages without a number: bit j
 #pragma unroll
-  for (int j = 0; j < (NV > LANES ? NV / LANES : 1); ++j) best[j] = -INFINITY;
-  for (int g0 = 0; g0 < a.group; g0 += GC) {
-    if (g0) __syncthreads();
-    for (int i = threadIdx.x; i < GC * HD / 2; i += CACHE_THREADS) {
-      const int g = i / (HD / 2), d = i % (HD / 2) * 2;                                // channels d and d + 1: lane d / 8, pair d % 8 / 2
-      double2 x = make_double2(0.0, 0.0);
-      if (g0 + g < a.group) {
-        const T *q = (const T *)a.q + r * a.q_ld + (long long)(kvh * a.group + g0 + g) * HD + d;
-        x = make_double2(scalbn((double)to_f(q[0]), CaWide<T>::UP), scalbn((double)to_f(q[1]), CaWide<T>::UP));
+    for (int j = 0; j < SCORE_DEEP; ++j) {
+      const int p = p0 + j * PAGES;
+      const bool on = p >= a.keep_first && p < end;
+      const int page = on ? a.c.page(seq, p) : -1;
+      if (on && page < 0) { bad |= 1u << j; cache_bad_index(a.status); }
+      lo[j] = hi[j] = make_uint4(0u, 0u, 0u, 0u);
+      if (page >= 0) {
+        const uint4 *b = reinterpret_cast<const uint4 *>((const T *)a.c.bounds + ((long long)page * a.c.hkv + kvh) * 2 * HD) + l;
+        lo[j] = b[0];
+        hi[j] = b[LANES];
       }
-      q_s[g][d % 8 / 2][d / 8] = x;
     }
-    __syncthreads();
-    double v[NV];                                          // v[g * SCORE_DEEP + j]
+    float best[LEFT];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = 0.0;
+    for (int j = 0; j < LEFT; ++j) best[j] = -INFINITY;
+    for (int g0 = 0; g0 < a.group; g0 += GC) {
+      if (base == (int)blockIdx.y * BLOCK || a.group > GC) {                             // (heads that fit stay where they are)
+        __syncthreads();
+        for (int i = threadIdx.x; i < GC * LANES; i += CACHE_THREADS) {
+          const int g = i / LANES, c = i % LANES;
+          const uint4 w = g0 + g < a.group ? *reinterpret_cast<const uint4 *>(q0 + (g0 + g) * HD + c * 8) : make_uint4(0u, 0u, 0u, 0u);
+          const float2 x = widen2<T>(w.x), y = widen2<T>(w.y), z = widen2<T>(w.z), u = widen2<T>(w.w);
+          q_s[g][0][c] = make_float4(x.x, x.y, y.x, y.y);
+          q_s[g][1][c] = make_float4(z.x, z.y, u.x, u.y);
+          const auto mask = [](uint32_t v) { return (v & 0x8000u ? 0xffffu : 0u) | (v & 0x80000000u ? 0xffff0000u : 0u); };
+          m_s[g][c] = make_uint4(mask(w.x), mask(w.y), mask(w.z), mask(w.w));
+        }
+        __syncthreads();
+      }
+      float v[NV];                                         // v[g * SCORE_DEEP + j]
 #pragma unroll
-    for (int g = 0; g < GC; ++g) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const double2 q = q_s[g][e][l];
-        const bool nx = __double2hiint(q.x) < 0, ny = __double2hiint(q.y) < 0;
+      for (int g = 0; g < GC; ++g) {
+        const float4 qa = q_s[g][0][l], qb = q_s[g][1][l];
+        const uint4 m = m_s[g][l];
 #pragma unroll
         for (int j = 0; j < SCORE_DEEP; ++j) {
-          const uint32_t L = e == 0 ? lo[j].x : e == 1 ? lo[j].y : e == 2 ? lo[j].z : lo[j].w, H = e == 0 ? hi[j].x : e == 1 ? hi[j].y : e == 2 ? hi[j].z : hi[j].w;
-          v[g * SCORE_DEEP + j] = fma(q.x, __hiloint2double(CaWide<T>::high((nx ? L : H) << 16), 0), v[g * SCORE_DEEP + j]);
-          v[g * SCORE_DEEP + j] = fma(q.y, __hiloint2double(CaWide<T>::high((ny ? L : H) & 0xffff0000u), 0), v[g * SCORE_DEEP + j]);
+          // the lower bound where q is negative, else the upper one
+          const float2 x = widen2<T>((lo[j].x & m.x) | (hi[j].x & ~m.x)), y = widen2<T>((lo[j].y & m.y) | (hi[j].y & ~m.y));
+          const float2 z = widen2<T>((lo[j].z & m.z) | (hi[j].z & ~m.z)), u = widen2<T>((lo[j].w & m.w) | (hi[j].w & ~m.w));
+          float t = qa.x * x.x;
+          t = fmaf(qa.y, x.y, t); t = fmaf(qa.z, y.x, t); t = fmaf(qa.w, y.y, t);
+          t = fmaf(qb.x, z.x, t); t = fmaf(qb.y, z.y, t); t = fmaf(qb.z, u.x, t);
+          v[g * SCORE_DEEP + j] = fmaf(qb.w, u.y, t);
         }
       }
-    }
-    // across the lanes of a page: at each step a lane gives away one half of its sums and adds to the other
-    int width = NV;
+      // across the lanes of a page: at each step a lane gives away one half of its sums and adds to the other
+      int width = NV;
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) {
-      if (width > 1) {
-        width /= 2;
-        const bool up = (lane & o) != 0;
+      for (int o = LANES / 2; o > 0; o >>= 1) {
+        if (width > 1) {
+          width /= 2;
+          const bool up = (lane & o) != 0;
 #pragma unroll
-        for (int j = 0; j < NV / 2; ++j)
-          if (j < width) {
-            const double give = up ? v[j] : v[j + width], keep = up ? v[j + width] : v[j];
-            v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-          }
-      } else v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+          for (int j = 0; j < NV / 2; ++j)
+            if (j < width) {
+              const float give = up ? v[j] : v[j + width], keep = up ? v[j + width] : v[j];
+              v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+        } else v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+      }
+      // A lane is left with the sums own * LEFT + (0 .. LEFT - 1), the bits of own being the lane's highest.  The largest of the group's heads: those past
+      // the group have no say, nor has NaN.
+      const int own = l / (LANES / STEPS);
+#pragma unroll
+      for (int j = 0; j < LEFT; ++j) {
+        float f = g0 + (own * LEFT + j) / SCORE_DEEP < a.group ? v[j] : -INFINITY;
+#pragma unroll
+        for (int o = LANES / 2; o >= LANES / STEPS * (SCORE_DEEP / LEFT); o >>= 1) f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, o));
+        best[j] = fmaxf(best[j], f);
+      }
     }
-    // the largest of the group's heads: those past the group have no say.  Value i = g * SCORE_DEEP + j; its high bits were chosen by the lane's
-    constexpr int LEFT = NV > LANES ? NV / LANES : 1, STEPS = NV > LANES ? LANES : NV;
-    const int own = STEPS > 1 ? l / (LANES / STEPS) : 0;                                // the lane's value(s) are own * LEFT + (0 .. LEFT - 1)
+#pragma unroll
+    for (int j = 0; j < SCORE_DEEP; ++j) {
+      const uint32_t w[8] = {lo[j].x, lo[j].y, lo[j].z, lo[j].w, hi[j].x, hi[j].y, hi[j].z, hi[j].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max_pair(top, w[i] & 0x7fff7fffu, T());
+    }
+    const int own = l / (LANES / STEPS);
 #pragma unroll
     for (int j = 0; j < LEFT; ++j) {
-      float f = g0 + (own * LEFT + j) / SCORE_DEEP < a.group ? (float)v[j] : -INFINITY;
-      if (f != f) f = -INFINITY;
-#pragma unroll
-      for (int o = LANES / 2; o >= LANES / STEPS * (SCORE_DEEP / LEFT); o >>= 1) f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, o));
-      best[j] = fmaxf(best[j], f);
+      const int i = own * LEFT + j, p = p0 + i % SCORE_DEEP * PAGES;
+      if (i < SCORE_DEEP && l % (LANES / STEPS) == 0 && p >= a.keep_first && p < end) scores[p] = bad >> i & 1u ? __int_as_float(0x7fffffff) : best[j];
     }
   }
-  // lane l has the scores of page j = own * LEFT + (0 .. LEFT - 1), modulo SCORE_DEEP
-  constexpr int LEFT = NV > LANES ? NV / LANES : 1, STEPS = NV > LANES ? LANES : NV;
-  const int own = STEPS > 1 ? l / (LANES / STEPS) : 0;
-  uint32_t *keys = a.keys + (long long)blockIdx.x * a.c.pages_per_seq;
-#pragma unroll
-  for (int j = 0; j < LEFT; ++j) {
-    const int i = own * LEFT + j, deep = i % SCORE_DEEP, p = p0 + deep * PAGES;
-    bool b = bad[0];
-#pragma unroll
-    for (int k = 1; k < SCORE_DEEP; ++k) if (deep == k) b = bad[k];
-    if (i < SCORE_DEEP && l % (LANES / STEPS) == 0 && p >= a.keep_first && p < end) keys[p] = b ? 0u : order_key(best[j]);
+  for (int o = 16; o > 0; o >>= 1) top = max_pair(top, __shfl_xor_sync(0xffffffffu, top, o), T());
+  if (lane == 0) top_s[warp] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < CACHE_THREADS / 32; ++w) top = max_pair(top, top_s[w], T());
+    const float2 t = widen2<T>(top);
+    // (and what products below the smallest normal number lose)
+    a.off[(long long)blockIdx.x * a.score_blocks + blockIdx.y] = 18.f * 0x1p-24f * q1_s * fmaxf(t.x, t.y) + 0x1p-140f;
   }
 }
 
-// grid (rows * KV heads), the keys in shared memory.  The cut: bins over the range of the keys, of equal width, so that they are filled evenly whatever the scores are; the bin in which
-// the cut falls is looked into again until it holds few keys, which are compared with each other.  Then the kept pages in order: a thread has a run of pages.
+// A page's score by the whole warp, from 64 bits: products are exact (8 and 8, or 11 and 11, digits), and so is nearly every sum of them.
+template <typename T, int HD>
+__device__ __forceinline__ float exact_score(const CacheSelectArgs &a, const T *q0, int page, int kvh, int lane) {
+  const T *lo = (const T *)a.c.bounds + ((long long)page * a.c.hkv + kvh) * 2 * HD, *hi = lo + HD;
+  float best = -INFINITY;
+  for (int g = 0; g < a.group; ++g) {
+    double s = 0.0;
+    for (int d = lane; d < HD; d += 32) {
+      const float x = to_f(q0[g * HD + d]);
+      s += (double)x * (double)to_f(x < 0.f ? lo[d] : hi[d]);
+    }
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    best = fmaxf(best, (float)s);
+  }
+  return best;
+}
+
+// grid (rows * KV heads), the scores in shared memory as 32-bit keys of the same order (0: a page without a number).  The cut, the left-th largest: bins over the range of
+// the keys, of equal width, so that they are filled evenly whatever the scores are; the bin in which the cut falls is looked into again until it holds few keys,
+// which are compared with each other.  Scores are off by up to E, and so is the cut: what lies above the cut by more than 2 E is kept, what lies below it by more is not, and where what lies
+// between (as a rule the cut's own page and nothing else) is not taken as a whole, it gets its exact scores and the cut is looked for again.  Then the kept pages in order: a
+// thread has a run of pages.
 #define SELECT_THREADS 512
 #define SELECT_BINS 2048
 #define SELECT_FEW 64
+struct SelectShared {
+  int hist[SELECT_BINS], scan[SELECT_THREADS / 32], n_few, bin, above, count, ties;
+  uint32_t few[SELECT_FEW], lowest, highest, key;
+};
+// The left-th largest (1 .. m) of keys[0 .. m - 1] in sh.key, and in sh.ties how many equal to it are among the left largest.
+__device__ __forceinline__ void select_cut(SelectShared &sh, const uint32_t *keys, int m, int left) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) { sh.lowest = 0xffffffffu; sh.highest = 0u; }
+  __syncthreads();
+  uint32_t low = 0xffffffffu, high = 0u;
+  for (int i = tid; i < m; i += SELECT_THREADS) { low = min(low, keys[i]); high = max(high, keys[i]); }
+  low = __reduce_min_sync(0xffffffffu, low);
+  high = __reduce_max_sync(0xffffffffu, high);
+  if (lane == 0) { atomicMin(&sh.lowest, low); atomicMax(&sh.highest, high); }
+  __syncthreads();
+  low = sh.lowest; high = sh.highest;
+  for (;;) {                                                    // keys low .. high hold the cut, the left-th largest of them
+    int shift = 0;
+    while ((high - low) >> shift >= SELECT_BINS) ++shift;
+    for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) sh.hist[i] = 0;
+    if (tid == 0) sh.n_few = 0;
+    __syncthreads();
+    for (int i = tid; i < m; i += SELECT_THREADS)
+      if (keys[i] >= low && keys[i] <= high) atomicAdd(sh.hist + ((keys[i] - low) >> shift), 1);
+    __syncthreads();
+    // from the top: bins PER t .. PER t + PER - 1 with t = SELECT_THREADS - 1 - tid
+    constexpr int PER = SELECT_BINS / SELECT_THREADS;
+    int own = 0, sum;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) own += sh.hist[(SELECT_THREADS - 1 - tid) * PER + k];
+    sum = own;
+    for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
+    if (lane == 31) sh.scan[warp] = sum;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) sum += sh.scan[w];
+    if (sum >= left && sum - own < left) {
+      int above = sum - own, b = (SELECT_THREADS - tid) * PER - 1;
+      while (above + sh.hist[b] < left) above += sh.hist[b--];
+      sh.bin = b; sh.above = above; sh.count = sh.hist[b];
+    }
+    __syncthreads();
+    left -= sh.above;
+    low += (uint32_t)sh.bin << shift;
+    high = min(high, low + (1u << shift) - 1u);
+    const int count = sh.count;
+    if (shift == 0) {                                           // a bin is a key
+      if (tid == 0) { sh.key = low; sh.ties = left; }
+      break;
+    }
+    if (count <= SELECT_FEW) {
+      for (int i = tid; i < m; i += SELECT_THREADS)
+        if (keys[i] >= low && keys[i] <= high) sh.few[atomicAdd(&sh.n_few, 1)] = keys[i];
+      __syncthreads();
+      if (tid < count) {
+        const uint32_t k = sh.few[tid];
+        int above = 0, same = 0;
+        for (int i = 0; i < count; ++i) { above += sh.few[i] > k; same += sh.few[i] == k; }
+        if (above < left && above + same >= left) { sh.key = k; sh.ties = left - above; }              // (equal keys write the same)
+      }
+      break;
+    }
+    __syncthreads();
+  }
+  __syncthreads();
+}
+
+template <typename T, int HD>
 __global__ void __launch_bounds__(SELECT_THREADS)
 k_cache_select(const __grid_constant__ CacheSelectArgs a) {
   extern __shared__ uint32_t sel_keys[];
-  __shared__ int hist[SELECT_BINS], scan[SELECT_THREADS / 32], n_few, cut_bin, cut_above, cut_count, cut_ties;
-  __shared__ uint32_t few[SELECT_FEW], red[2], cut_key;
+  __shared__ SelectShared sh;
+  __shared__ int n_in, n_border, border[SELECT_FEW], taken[SELECT_FEW];
+  __shared__ float off_s;
   kernel_entry(TR_k_cache_select);
-  const int r = blockIdx.x / a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r = blockIdx.x / a.c.hkv, kvh = blockIdx.x % a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int *ids = a.ids + (long long)blockIdx.x * a.budget;
   if (seq >= 0 && pos >= 0 && !n && tid == 0) cache_bad_index(a.status);
   if (n <= a.budget) {
     for (int i = tid; i < a.budget; i += SELECT_THREADS) ids[i] = i < n ? i : -1;
     return;
   }
-  const uint32_t *keys = a.keys + (long long)blockIdx.x * a.c.pages_per_seq;
+  const float *scores = a.scores + (long long)blockIdx.x * a.c.pages_per_seq;
   const int p0 = a.keep_first, m = n - a.keep_last - p0;        // candidates p0 .. p0 + m - 1
-  int left = a.budget - a.keep_first - a.keep_last;             // of which so many are taken: fewer than there are
-  uint32_t low = 0xffffffffu, high = 0u;
-  if (tid == 0) { red[0] = 0xffffffffu; red[1] = 0u; cut_key = 0u; cut_ties = 0; }
-  __syncthreads();
+  const int left = a.budget - a.keep_first - a.keep_last;       // of which so many are taken: fewer than there are
+  uint32_t cut = 0u;                                            // what is above it is kept, and of what is equal to it the first so many
+  int ties = 0;
+  if (tid == 0) { n_in = n_border = 0; off_s = 0.f; }
   if (left) {
-    for (int i = tid; i < m; i += SELECT_THREADS) {
-      const uint32_t k = keys[p0 + i];
-      sel_keys[i] = k;
-      low = min(low, k); high = max(high, k);
+    float off = 0.f;
+    for (int i = tid; i < a.score_blocks; i += SELECT_THREADS) {
+      const float f = a.off[(long long)blockIdx.x * a.score_blocks + i];
+      off = f > off || f != f ? (f != f ? INFINITY : f) : off;
     }
-    low = __reduce_min_sync(0xffffffffu, low);
-    high = __reduce_max_sync(0xffffffffu, high);
-    if (lane == 0) { atomicMin(red, low); atomicMax(red + 1, high); }
+    for (int i = tid; i < m; i += SELECT_THREADS) {
+      const uint32_t b = __float_as_uint(scores[p0 + i]);
+      sel_keys[i] = b == 0x7fffffffu ? 0u : order_key(__uint_as_float(b));
+    }
+    off = warp_max(off);
     __syncthreads();
-    low = red[0]; high = red[1];
+    if (lane == 0) atomicMax(reinterpret_cast<int *>(&off_s), __float_as_int(off));
+    select_cut(sh, sel_keys, m, left);
+    cut = sh.key;
+    ties = sh.ties;
   }
-  while (left) {                                                // keys low .. high hold the cut: the left-th largest of them
-    int shift = 0;
-    while ((high - low) >> shift >= SELECT_BINS) ++shift;
-    for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) hist[i] = 0;
-    if (tid == 0) n_few = 0;
-    __syncthreads();
+  if (left && cut) {                                            // (0: pages without a number are needed to fill the budget)
+    // ---- what is near the cut
+    const float at = order_value(cut), e2 = 2.f * off_s;
+    const auto side = [&](uint32_t k) {                         // 1: above the border, -1: below, 0: on it
+      const float s = order_value(k);
+      return k == 0u ? -1 : s - at > e2 ? 1 : at - s > e2 ? -1 : 0;
+    };
+    int in = 0;
     for (int i = tid; i < m; i += SELECT_THREADS) {
-      const uint32_t k = sel_keys[i];
-      if (k >= low && k <= high) atomicAdd(hist + ((k - low) >> shift), 1);
+      const int d = side(sel_keys[i]);
+      in += d > 0;
+      if (d == 0) { const int j = atomicAdd(&n_border, 1); if (j < SELECT_FEW) border[j] = i; }
     }
+    in = __reduce_add_sync(0xffffffffu, in);
+    if (lane == 0 && in) atomicAdd(&n_in, in);
     __syncthreads();
-    // from the top: bins 4 tid' .. 4 tid' + 3 with tid' = SELECT_THREADS - 1 - tid
-    constexpr int PER = SELECT_BINS / SELECT_THREADS;
-    int own = 0, sum;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) own += hist[(SELECT_THREADS - 1 - tid) * PER + k];
-    sum = own;
-    for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
-    if (lane == 31) scan[warp] = sum;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) sum += scan[w];
-    if (sum >= left && sum - own < left) {
-      int above = sum - own, b = (SELECT_THREADS - tid) * PER - 1;
-      while (above + hist[b] < left) above += hist[b--];
-      cut_bin = b; cut_above = above; cut_count = hist[b];
-    }
-    __syncthreads();
-    left -= cut_above;
-    low += (uint32_t)cut_bin << shift;
-    high = min(high, low + (1u << shift) - 1u);
-    const int count = cut_count;
-    if (shift == 0) {                                           // a bin is a key
-      if (tid == 0) { cut_key = low; cut_ties = left; }
+    const int nb = n_border, take = left - n_in;                // 1 .. nb of those on the border are taken
+    const bool few = nb <= SELECT_FEW, open = nb > take;
+    if (open && few) {
+      const T *q0 = (const T *)a.q + r * a.q_ld + (long long)kvh * a.group * HD;
+      for (int j = warp; j < nb; j += SELECT_THREADS / 32) {
+        const float s = exact_score<T, HD>(a, q0, a.c.page(seq, p0 + border[j]), kvh, lane);
+        if (lane == 0) sh.few[j] = order_key(s);
+      }
       __syncthreads();
-      break;
+      if (tid < nb) {
+        int before = 0;
+        for (int i = 0; i < nb; ++i) before += sh.few[i] > sh.few[tid] || (sh.few[i] == sh.few[tid] && border[i] < border[tid]);
+        taken[tid] = before < take;
+      }
+      __syncthreads();
     }
-    if (count <= SELECT_FEW) {
+    // kept pages become the highest key, the others 0; many on the border: these their exact one, and the cut is looked for again
+    const bool again = open && !few;
+    if (again) {
+      const T *q0 = (const T *)a.q + r * a.q_ld + (long long)kvh * a.group * HD;
+      for (int i = warp; i < m; i += SELECT_THREADS / 32) {
+        const int d = side(sel_keys[i]);
+        const float s = d ? 0.f : exact_score<T, HD>(a, q0, a.c.page(seq, p0 + i), kvh, lane);
+        __syncwarp();
+        if (lane == 0) sel_keys[i] = d > 0 ? 0xffffffffu : d < 0 ? 0u : order_key(s);
+      }
+      __syncthreads();
+      select_cut(sh, sel_keys, m, left);
+      cut = sh.key;
+      ties = sh.ties;
+    } else {
       for (int i = tid; i < m; i += SELECT_THREADS) {
-        const uint32_t k = sel_keys[i];
-        if (k >= low && k <= high) few[atomicAdd(&n_few, 1)] = k;
+        const int d = side(sel_keys[i]);
+        sel_keys[i] = d > 0 || (d == 0 && !open) ? 0xffffffffu : 0u;
       }
       __syncthreads();
-      if (tid < count) {
-        int above = 0, same = 0;
-        for (int i = 0; i < count; ++i) { above += few[i] > few[tid]; same += few[i] == few[tid]; }
-        if (above < left && above + same >= left) { cut_key = few[tid]; cut_ties = left - above; }       // (equal keys write the same)
-      }
-      __syncthreads();
-      break;
+      if (open && tid < nb && taken[tid]) sel_keys[border[tid]] = 0xffffffffu;
+      cut = 0xfffffffeu;
+      ties = 0;
     }
     __syncthreads();
   }
-  const uint32_t cut = cut_key;
-  const int take = cut_ties;                                    // of the keys on the cut, the first so many
-  const bool none = a.budget == a.keep_first + a.keep_last;
   // pages i0 .. i1 - 1 are this thread's
-  const int run = (m + SELECT_THREADS - 1) / SELECT_THREADS, i0 = min(m, tid * run), i1 = min(m, i0 + run);
-  int above = 0, ties = 0;
-  if (!none)
-    for (int i = i0; i < i1; ++i) { above += sel_keys[i] > cut; ties += sel_keys[i] == cut; }
-  int both = above | ties << 16, sum = both;                     // (no more than 32768 of each)
+  const int run = (m + SELECT_THREADS - 1) / SELECT_THREADS, i0 = min(m, tid * run), i1 = left ? min(m, i0 + run) : i0;
+  int above = 0, same = 0;
+  for (int i = i0; i < i1; ++i) { above += sel_keys[i] > cut; same += sel_keys[i] == cut; }
+  const int both = above | same << 16;                          // (no more than 32768 of each)
+  int sum = both;
   for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
-  if (lane == 31) scan[warp] = sum;
+  if (lane == 31) sh.scan[warp] = sum;
   __syncthreads();
   sum -= both;
-  for (int w = 0; w < warp; ++w) sum += scan[w];
-  int tie = sum >> 16 & 0xffff, at = a.keep_first + (sum & 0xffff) + min(tie, take);
-  if (!none)
-    for (int i = i0; i < i1; ++i) {
-      const uint32_t k = sel_keys[i];
-      if (k > cut || (k == cut && tie < take)) ids[at++] = p0 + i;
-      tie += k == cut;
-    }
+  for (int w = 0; w < warp; ++w) sum += sh.scan[w];
+  int tie = sum >> 16 & 0xffff, at = a.keep_first + (sum & 0xffff) + min(tie, ties);
+  for (int i = i0; i < i1; ++i) {
+    const uint32_t k = sel_keys[i];
+    if (k > cut || (k == cut && tie < ties)) ids[at++] = p0 + i;
+    tie += k == cut;
+  }
   for (int i = tid; i < a.keep_first; i += SELECT_THREADS) ids[i] = i;
   for (int i = tid; i < a.keep_last; i += SELECT_THREADS) ids[a.budget - a.keep_last + i] = n - a.keep_last + i;
 }
