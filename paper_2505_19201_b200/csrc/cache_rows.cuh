@@ -288,32 +288,45 @@ k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LANES, end = n - a.keep_last;
   if (n <= a.budget) return;                               // all are kept
   const T *q0 = (const T *)a.q + r * a.q_ld + (long long)kvh * a.group * HD;
-  // the largest sum |q_d| of the group's heads
-  if (threadIdx.x == 0) q1_s = 0.f;
-  __syncthreads();
-  for (int g = warp; g < a.group; g += CACHE_THREADS / 32) {
-    float sum = 0.f;
-    for (int d = lane; d < HD; d += 32) sum += fabsf(to_f(q0[g * HD + d]));
-    sum = warp_sum(sum);
-    if (lane == 0) atomicMax(reinterpret_cast<int *>(&q1_s), __float_as_int(sum));        // (floats above zero are ordered as integers are; NaN is above all)
-  }
   float *scores = a.scores + (long long)blockIdx.x * a.c.pages_per_seq;
   uint32_t top = 0u;                                       // the largest magnitudes met, a pair
-  for (int base = blockIdx.y * BLOCK; base < end; base += gridDim.y * BLOCK) {
-    const int p0 = base + warp * PAGES * SCORE_DEEP + lane / LANES;                    // pages p0, p0 + PAGES, ...
-    uint4 lo[SCORE_DEEP], hi[SCORE_DEEP];
-    unsigned bad = 0;                                      // pages without a number: bit j
+  int page[SCORE_DEEP];                                    // of the pages ahead; -1: not asked for, -2: no number
+  const auto look_up = [&](int base) {
 #pragma unroll
     for (int j = 0; j < SCORE_DEEP; ++j) {
-      const int p = p0 + j * PAGES;
-      const bool on = p >= a.keep_first && p < end;
-      const int page = on ? a.c.page(seq, p) : -1;
-      if (on && page < 0) { bad |= 1u << j; cache_bad_index(a.status); }
+      const int p = base + warp * PAGES * SCORE_DEEP + lane / LANES + j * PAGES;         // pages p0, p0 + PAGES, ...
+      page[j] = -1;
+      if (p >= a.keep_first && p < end) {
+        page[j] = a.c.page(seq, p);
+        if (page[j] < 0) { page[j] = -2; cache_bad_index(a.status); }
+      }
+    }
+  };
+  look_up(blockIdx.y * BLOCK);
+  if (threadIdx.x == 0) q1_s = 0.f;
+  for (int base = blockIdx.y * BLOCK; base < end; base += gridDim.y * BLOCK) {
+    const int p0 = base + warp * PAGES * SCORE_DEEP + lane / LANES;
+    uint4 lo[SCORE_DEEP], hi[SCORE_DEEP];
+    unsigned bad = 0, on = 0;                              // pages without a number, pages of this row: bit j
+#pragma unroll
+    for (int j = 0; j < SCORE_DEEP; ++j) {
       lo[j] = hi[j] = make_uint4(0u, 0u, 0u, 0u);
-      if (page >= 0) {
-        const uint4 *b = reinterpret_cast<const uint4 *>((const T *)a.c.bounds + ((long long)page * a.c.hkv + kvh) * 2 * HD) + l;
+      if (page[j] >= 0) {
+        const uint4 *b = reinterpret_cast<const uint4 *>((const T *)a.c.bounds + ((long long)page[j] * a.c.hkv + kvh) * 2 * HD) + l;
         lo[j] = b[0];
         hi[j] = b[LANES];
+      }
+      on |= (page[j] != -1) << j;
+      bad |= (page[j] == -2) << j;
+    }
+    look_up(base + gridDim.y * BLOCK);
+    if (base == (int)blockIdx.y * BLOCK) {                 // the largest sum |q_d| of the group's heads
+      __syncthreads();
+      for (int g = warp; g < a.group; g += CACHE_THREADS / 32) {
+        float sum = 0.f;
+        for (int d = lane; d < HD; d += 32) sum += fabsf(to_f(q0[g * HD + d]));
+        sum = warp_sum(sum);
+        if (lane == 0) atomicMax(reinterpret_cast<int *>(&q1_s), __float_as_int(sum));      // (floats above zero are ordered as integers are; NaN is above all)
       }
     }
     float best[LEFT];
@@ -385,7 +398,7 @@ k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
 #pragma unroll
     for (int j = 0; j < LEFT; ++j) {
       const int i = own * LEFT + j, p = p0 + i % SCORE_DEEP * PAGES;
-      if (i < SCORE_DEEP && l % (LANES / STEPS) == 0 && p >= a.keep_first && p < end) scores[p] = bad >> i & 1u ? __int_as_float(0x7fffffff) : best[j];
+      if (i < SCORE_DEEP && l % (LANES / STEPS) == 0 && on >> i & 1u) scores[p] = bad >> i & 1u ? __int_as_float(0x7fffffff) : best[j];
     }
   }
   for (int o = 16; o > 0; o >>= 1) top = max_pair(top, __shfl_xor_sync(0xffffffffu, top, o), T());
@@ -422,30 +435,31 @@ __device__ __forceinline__ float exact_score(const CacheSelectArgs &a, const T *
 // between (as a rule the cut's own page and nothing else) is not taken as a whole, it gets its exact scores and the cut is looked for again.  Then the kept pages in order: a
 // thread has a run of pages.
 #define SELECT_THREADS 512
-#define SELECT_BINS 2048
+#define SELECT_BINS 1024
 #define SELECT_FEW 64
 struct SelectShared {
   int hist[SELECT_BINS], scan[SELECT_THREADS / 32], n_few, bin, above, count, ties;
-  uint32_t few[SELECT_FEW], lowest, highest, key;
+  uint32_t few[SELECT_FEW], lows[SELECT_THREADS / 32], highs[SELECT_THREADS / 32], key;
 };
 // The left-th largest (1 .. m) of keys[0 .. m - 1] in sh.key, and in sh.ties how many equal to it are among the left largest.
-__device__ __forceinline__ void select_cut(SelectShared &sh, const uint32_t *keys, int m, int left) {
+// low, high: the lowest and the highest key of this thread's share.
+__device__ __forceinline__ void select_cut(SelectShared &sh, const uint32_t *keys, int m, int left, uint32_t low, uint32_t high) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) { sh.lowest = 0xffffffffu; sh.highest = 0u; }
-  __syncthreads();
-  uint32_t low = 0xffffffffu, high = 0u;
-  for (int i = tid; i < m; i += SELECT_THREADS) { low = min(low, keys[i]); high = max(high, keys[i]); }
   low = __reduce_min_sync(0xffffffffu, low);
   high = __reduce_max_sync(0xffffffffu, high);
-  if (lane == 0) { atomicMin(&sh.lowest, low); atomicMax(&sh.highest, high); }
+  if (lane == 0) { sh.lows[warp] = low; sh.highs[warp] = high; }
+  for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) sh.hist[i] = 0;
+  if (tid == 0) sh.n_few = 0;
   __syncthreads();
-  low = sh.lowest; high = sh.highest;
-  for (;;) {                                                    // keys low .. high hold the cut, the left-th largest of them
+  low = __reduce_min_sync(0xffffffffu, sh.lows[lane % (SELECT_THREADS / 32)]);
+  high = __reduce_max_sync(0xffffffffu, sh.highs[lane % (SELECT_THREADS / 32)]);
+  for (bool first = true;; first = false) {                     // keys low .. high hold the cut, the left-th largest of them
     int shift = 0;
     while ((high - low) >> shift >= SELECT_BINS) ++shift;
-    for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) sh.hist[i] = 0;
-    if (tid == 0) sh.n_few = 0;
-    __syncthreads();
+    if (!first) {
+      for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) sh.hist[i] = 0;
+      __syncthreads();
+    }
     for (int i = tid; i < m; i += SELECT_THREADS)
       if (keys[i] >= low && keys[i] <= high) atomicAdd(sh.hist + ((keys[i] - low) >> shift), 1);
     __syncthreads();
@@ -496,7 +510,7 @@ k_cache_select(const __grid_constant__ CacheSelectArgs a) {
   extern __shared__ uint32_t sel_keys[];
   __shared__ SelectShared sh;
   __shared__ int n_in, n_border, border[SELECT_FEW], taken[SELECT_FEW];
-  __shared__ float off_s;
+  __shared__ float offs[SELECT_THREADS / 32];
   kernel_entry(TR_k_cache_select);
   const int r = blockIdx.x / a.c.hkv, kvh = blockIdx.x % a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -511,27 +525,29 @@ k_cache_select(const __grid_constant__ CacheSelectArgs a) {
   const int left = a.budget - a.keep_first - a.keep_last;       // of which so many are taken: fewer than there are
   uint32_t cut = 0u;                                            // what is above it is kept, and of what is equal to it the first so many
   int ties = 0;
-  if (tid == 0) { n_in = n_border = 0; off_s = 0.f; }
+  if (tid == 0) n_in = n_border = 0;
   if (left) {
     float off = 0.f;
+    uint32_t low = 0xffffffffu, high = 0u;
     for (int i = tid; i < a.score_blocks; i += SELECT_THREADS) {
       const float f = a.off[(long long)blockIdx.x * a.score_blocks + i];
       off = f > off || f != f ? (f != f ? INFINITY : f) : off;
     }
     for (int i = tid; i < m; i += SELECT_THREADS) {
       const uint32_t b = __float_as_uint(scores[p0 + i]);
-      sel_keys[i] = b == 0x7fffffffu ? 0u : order_key(__uint_as_float(b));
+      const uint32_t k = b == 0x7fffffffu ? 0u : order_key(__uint_as_float(b));
+      sel_keys[i] = k;
+      low = min(low, k); high = max(high, k);
     }
     off = warp_max(off);
-    __syncthreads();
-    if (lane == 0) atomicMax(reinterpret_cast<int *>(&off_s), __float_as_int(off));
-    select_cut(sh, sel_keys, m, left);
+    if (lane == 0) offs[warp] = off;
+    select_cut(sh, sel_keys, m, left, low, high);
     cut = sh.key;
     ties = sh.ties;
   }
   if (left && cut) {                                            // (0: pages without a number are needed to fill the budget)
     // ---- what is near the cut
-    const float at = order_value(cut), e2 = 2.f * off_s;
+    const float at = order_value(cut), e2 = 2.f * warp_max(offs[lane % (SELECT_THREADS / 32)]);
     const auto side = [&](uint32_t k) {                         // 1: above the border, -1: below, 0: on it
       const float s = order_value(k);
       return k == 0u ? -1 : s - at > e2 ? 1 : at - s > e2 ? -1 : 0;
@@ -561,31 +577,32 @@ k_cache_select(const __grid_constant__ CacheSelectArgs a) {
       }
       __syncthreads();
     }
-    // kept pages become the highest key, the others 0; many on the border: these their exact one, and the cut is looked for again
-    const bool again = open && !few;
-    if (again) {
-      const T *q0 = (const T *)a.q + r * a.q_ld + (long long)kvh * a.group * HD;
-      for (int i = warp; i < m; i += SELECT_THREADS / 32) {
-        const int d = side(sel_keys[i]);
-        const float s = d ? 0.f : exact_score<T, HD>(a, q0, a.c.page(seq, p0 + i), kvh, lane);
-        __syncwarp();
-        if (lane == 0) sel_keys[i] = d > 0 ? 0xffffffffu : d < 0 ? 0u : order_key(s);
+    if (open) {
+      // Pages above become the highest key and those below 0; those on the border either, or their exact score, for which the cut is looked for again.  (Where they are
+      // all taken, what is kept is what the cut says already.)
+      uint32_t low = 0xffffffffu, high = 0u;
+      if (few) {
+        for (int i = tid; i < m; i += SELECT_THREADS) sel_keys[i] = side(sel_keys[i]) > 0 ? 0xffffffffu : 0u;
+        __syncthreads();
+        if (tid < nb && taken[tid]) sel_keys[border[tid]] = 0xffffffffu;
+        cut = 0xfffffffeu;
+        ties = 0;
+      } else {
+        const T *q0 = (const T *)a.q + r * a.q_ld + (long long)kvh * a.group * HD;
+        for (int i = warp; i < m; i += SELECT_THREADS / 32) {
+          const int d = side(sel_keys[i]);
+          const uint32_t k = d > 0 ? 0xffffffffu : d < 0 ? 0u : order_key(exact_score<T, HD>(a, q0, a.c.page(seq, p0 + i), kvh, lane));
+          __syncwarp();
+          if (lane == 0) sel_keys[i] = k;
+          low = min(low, k); high = max(high, k);
+        }
+        __syncthreads();
+        select_cut(sh, sel_keys, m, left, low, high);
+        cut = sh.key;
+        ties = sh.ties;
       }
       __syncthreads();
-      select_cut(sh, sel_keys, m, left);
-      cut = sh.key;
-      ties = sh.ties;
-    } else {
-      for (int i = tid; i < m; i += SELECT_THREADS) {
-        const int d = side(sel_keys[i]);
-        sel_keys[i] = d > 0 || (d == 0 && !open) ? 0xffffffffu : 0u;
-      }
-      __syncthreads();
-      if (open && tid < nb && taken[tid]) sel_keys[border[tid]] = 0xffffffffu;
-      cut = 0xfffffffeu;
-      ties = 0;
     }
-    __syncthreads();
   }
   // pages i0 .. i1 - 1 are this thread's
   const int run = (m + SELECT_THREADS - 1) / SELECT_THREADS, i0 = min(m, tid * run), i1 = left ? min(m, i0 + run) : i0;
