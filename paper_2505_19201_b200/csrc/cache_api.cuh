@@ -4,12 +4,13 @@
 #include <cudaTypedefs.h>
 
 #include "cache_attn.cuh"
+#include "cache_few.cuh"
 #include "cache_rows.cuh"
 
 #define CACHE_MAX_ROWS (1 << 20)
 #define CACHE_MAX_SEQS 4096
 #define CACHE_MAX_BUDGET 4096
-#define CACHE_MAX_CTAS 320                 // most CTAs of the attention
+#define CACHE_MAX_SMS 160
 #define CACHE_MAX_SELECT 32768             // pages of a sequence that dream_cache_select chooses from
 
 // The view of a cache, or what is wrong with it.
@@ -219,12 +220,14 @@ extern "C" dream_status dream_cache_select(const dream_cache *cache, const void 
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
 }
 
+// Most CTAs of the two attention kernels together, each of which may continue an item.
+static int cache_slots(int hd) { return CACHE_MAX_SMS * (hd == 64 ? 4 : hd == 128 ? 3 : 2); }
 // The parts of the attention's workspace; how many bytes they are.
 static size_t cache_attn_room(const dream_cache *c, int n_heads, int rows, void *workspace, CacheAttnArgs *a) {
   const size_t n = 2 * (size_t)rows * n_heads, hd = c->head_dim;
   size_t at = 0;
   auto take = [&](size_t bytes) { char *p = (char *)workspace + at; at += (bytes + 255) / 256 * 256; return p; };
-  char *po = take(n * hd * 4), *pm = take(n * 16), *co = take((size_t)CACHE_MAX_CTAS * 128 * hd * 4), *cm = take((size_t)CACHE_MAX_CTAS * 128 * 16);
+  char *po = take(n * hd * 4), *pm = take(n * 16), *co = take((size_t)cache_slots(c->head_dim) * 128 * hd * 4), *cm = take((size_t)cache_slots(c->head_dim) * 128 * 16);
   if (a) { a->part_o = (float *)po; a->part_ml = (float4 *)pm; a->cont_o = (float *)co; a->cont_ml = (float4 *)cm; }
   return at;
 }
@@ -257,7 +260,7 @@ static dream_status cache_attn_args(const char *who, const dream_cache *cache, C
   if (!s) s = cache_workspace(who, workspace, workspace_bytes, need);
   if (s) return s;
   a->q = q; a->q_ld = q_ld; a->out = out; a->out_ld = out_ld; a->lse = lse; a->rows = rows; a->heads = n_heads; a->group = n_heads / a->c.hkv;
-  a->scale_log2 = scale * 1.4426950408889634f; a->status = status; a->tile_rows = 128 / a->group;
+  a->scale_log2 = scale * 1.4426950408889634f; a->status = status;
   cache_attn_room(cache, n_heads, rows, const_cast<void *>(workspace), a);
   return DREAM_OK;
 }
@@ -275,11 +278,12 @@ static const char *cache_map(int dtype, const void *base, const cuuint64_t (&dim
                             step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? nullptr : "the strides make no tensor map";
 }
-// K or V: the keys of one page that go into a unit, and all panels of columns where they are the whole unit.
-static const char *cache_kv_map(const dream_cache *c, const CacheView &v, const void *base, CUtensorMap *out) {
-  const cuuint32_t sub = c->page_tokens < CA_BLK ? c->page_tokens : CA_BLK, panels = c->head_dim / 64;
+// K or V: the keys of one page that go into a unit of `unit`, and all panels of columns where they are the whole unit.
+static const char *cache_kv_map(const dream_cache *c, const CacheView &v, const void *base, int unit, CUtensorMap *out) {
+  const cuuint32_t sub = c->page_tokens < unit ? c->page_tokens : unit, panels = c->head_dim / 64;
   return cache_map(c->dtype, base, {64, (cuuint64_t)c->page_tokens, panels, (cuuint64_t)c->n_kv_heads, (cuuint64_t)c->n_pages},
-                   {(cuuint64_t)v.token_stride * 2, 128, (cuuint64_t)v.head_stride * 2, (cuuint64_t)v.page_stride * 2}, {64, sub, sub == CA_BLK ? panels : 1, 1, 1}, out);
+                   {(cuuint64_t)v.token_stride * 2, 128, (cuuint64_t)v.head_stride * 2, (cuuint64_t)v.page_stride * 2},
+                   {64, sub, sub == (cuuint32_t)unit ? panels : 1, 1, 1}, out);
 }
 // Q: a panel of so many rows' heads of one group, row after row, as a tile has its entries.
 static const char *cache_q_map(const dream_cache *c, const CacheAttnArgs &a, int rows, CUtensorMap *out) {
@@ -287,36 +291,77 @@ static const char *cache_q_map(const dream_cache *c, const CacheAttnArgs &a, int
   return cache_map(c->dtype, a.q, {64, hd / 64, (cuuint64_t)a.group, (cuuint64_t)c->n_kv_heads, (cuuint64_t)a.rows},
                    {128, hd * 2, a.group * hd * 2, (cuuint64_t)a.q_ld * 2}, {64, 1, (cuuint32_t)a.group, 1, (cuuint32_t)rows}, out);
 }
-template <typename T, int HD, bool PAGES>
-static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
-  struct Ready { int device, sms; };
-  static thread_local Ready ready[8];          // devices on which the kernel may use its shared memory, and their SMs
-  static thread_local int n_ready = 0;
-  auto *kernel = k_cache_attn<T, HD, PAGES>;
-  const size_t smem = CaShape<HD>::SMEM;
+// A kernel may use its shared memory on the current device from now on: once per device by a thread that calls again and again.  Returns the device's SMs, 0 with *e set
+// where something is wrong.  regs: registers per thread that the kernel counts on, or 0.
+template <typename... A>
+static int cache_allow(void (*kernel)(A...), size_t smem, int regs, cudaError_t *e) {
+  struct Ready { const void *kernel; int device, sms; };
+  static thread_local Ready ready[16];
+  static thread_local int next = 0;
   int device = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&device);
-  for (int i = 0; i < n_ready && i < 8; ++i) if (ready[i].device == device) sms = ready[i].sms;
-  if (e == cudaSuccess && !sms) {
-    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    cudaFuncAttributes fa = {};
-    if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, kernel);
-    if (e == cudaSuccess && CaShape<HD>::SPLIT && fa.numRegs != 80) return "the attention's warps share out 80 registers per thread and it was compiled with another number";
-    if (e == cudaSuccess) ready[n_ready++ % 8] = {device, sms};
-  }
-  if (e != cudaSuccess) { cudaGetLastError(); return cudaGetErrorString(e); }
+  if ((*e = cudaGetDevice(&device)) != cudaSuccess) return 0;
+  for (const Ready &r : ready) if (r.kernel == (const void *)kernel && r.device == device) return r.sms;
+  cudaFuncAttributes fa = {};
+  *e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+  if (*e == cudaSuccess) *e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (*e == cudaSuccess) *e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (*e == cudaSuccess) *e = cudaFuncGetAttributes(&fa, kernel);
+  if (*e == cudaSuccess && regs && fa.numRegs != regs) *e = cudaErrorInvalidKernelImage;
+  if (*e != cudaSuccess) return 0;
+  if (sms > CACHE_MAX_SMS) sms = CACHE_MAX_SMS;
+  ready[next] = {(const void *)kernel, device, sms};
+  next = (next + 1) % 16;
+  return sms;
+}
+// Tiles of up to 128 entries.
+template <typename T, int HD, bool PAGES>
+static const char *cache_attn_many(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
+  cudaError_t e = cudaSuccess;
+  const int sms = cache_allow(k_cache_attn<T, HD, PAGES>, CaShape<HD>::SMEM, CaShape<HD>::SPLIT ? 80 : 0, &e);
+  if (!sms) { cudaGetLastError(); return cudaGetErrorString(e); }
   CUtensorMap mk, mv, mq, ms;
-  const char *why = cache_kv_map(cache, a.c, a.c.k, &mk);
-  if (!why) why = cache_kv_map(cache, a.c, a.c.v, &mv);
+  a.tile_rows = 128 / a.group;
+  const char *why = cache_kv_map(cache, a.c, a.c.k, CA_BLK, &mk);
+  if (!why) why = cache_kv_map(cache, a.c, a.c.v, CA_BLK, &mv);
   // a copy takes a whole tile of query entries, or 16 where a segment has no more
   a.q_small = a.group < 16 ? 16 / a.group : 1;
   if (!why) why = cache_q_map(cache, a, a.tile_rows, &mq);
   if (!why) why = cache_q_map(cache, a, a.q_small, &ms);
   if (why) return why;
-  a.n_ctas = imin(sms * CaShape<HD>::CTAS_PER_SM, CACHE_MAX_CTAS);
-  why = cache_launch(kernel, dim3(a.n_ctas), CA_THREADS, smem, stream, mk, mv, mq, ms, a);
+  a.n_ctas = sms * CaShape<HD>::CTAS_PER_SM;
+  a.cont_base = 0;
+  return cache_launch(k_cache_attn<T, HD, PAGES>, dim3(a.n_ctas), CA_THREADS, CaShape<HD>::SMEM, stream, mk, mv, mq, ms, a);
+}
+// Tiles of up to 16.
+template <typename T, int HD, bool PAGES>
+static const char *cache_attn_few(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
+  using Sh = CfShape<HD>;
+  cudaError_t e = cudaSuccess;
+  const int sms = cache_allow(k_cache_attn_few<T, HD, PAGES>, Sh::SMEM, 0, &e);
+  if (!sms) { cudaGetLastError(); return cudaGetErrorString(e); }
+  CUtensorMap mk, mv, mq;
+  a.tile_rows = CF_N / a.group;
+  const char *why = cache_kv_map(cache, a.c, a.c.k, Sh::BLK, &mk);
+  if (!why) why = cache_kv_map(cache, a.c, a.c.v, Sh::BLK, &mv);
+  if (!why) why = cache_q_map(cache, a, a.tile_rows, &mq);
+  if (why) return why;
+  a.n_ctas = sms * Sh::CTAS_PER_SM;
+  a.cont_base = CACHE_MAX_SMS * CaShape<HD>::CTAS_PER_SM;
+  return cache_launch(k_cache_attn_few<T, HD, PAGES>, dim3(a.n_ctas), CF_THREADS, Sh::SMEM, stream, mk, mv, mq, a);
+}
+template <typename T, int HD, bool PAGES>
+static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
+  // A sequence's rows, or a listed row, have 16 entries or fewer (on the average: how many each has is on the device, and more go tile by tile); the shared keys meet all rows.
+  const bool own_few = a.group <= CF_N && (PAGES || (long long)a.rows * a.group <= (long long)CF_N * a.c.n_seqs);
+  const bool shared_few = (long long)a.rows * a.group <= CF_N, both = PAGES || !a.shared_tokens || shared_few == own_few;
+  const char *why = nullptr;
+  a.cont_slots = cache_slots(HD);
+  a.with_own = both || !own_few;
+  a.with_prefix = a.shared_tokens > 0;
+  if (!both || !own_few) why = cache_attn_many<T, HD, PAGES>(cache, a, stream);
+  a.with_own = 1;
+  a.with_prefix = both && a.shared_tokens > 0;
+  if (!why && own_few) why = cache_attn_few<T, HD, PAGES>(cache, a, stream);
   const long long merge = (long long)a.rows * a.heads * (HD / 8);
   return why ? why : cache_launch(k_cache_merge<T, HD, PAGES>, dim3((unsigned)((merge + 255) / 256)), 256, 0, stream, a);
 }
@@ -342,7 +387,7 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask; a.shared_tokens = shared_pages * cache->page_tokens;
   // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits
   const long long units = (long long)((cache->pages_per_seq * (long long)cache->page_tokens + CA_BLK - 1) / CA_BLK) * cache->n_kv_heads;
-  if (units > 0x7fffffffLL || (shared_pages && (units * shared_pages / cache->pages_per_seq + cache->n_kv_heads) * ((rows + a.tile_rows - 1) / a.tile_rows) > 0x7fffffffLL))
+  if (units > 0x7fffffffLL || (shared_pages && (units * shared_pages / cache->pages_per_seq + cache->n_kv_heads) * ((rows + 128 / a.group - 1) / (128 / a.group)) > 0x7fffffffLL))
     return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows over sequences of %d pages in one call", who, rows, cache->pages_per_seq);
   const char *why = cache_attn_launch<false>(cache, a, (cudaStream_t)cuda_stream);
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;

@@ -1,14 +1,7 @@
 // Attention over a paged cache that a program holds itself, on the tcgen05 tensor cores: a ragged batch whose sequences may begin with the
 // same pages (dream_cache_attn), and rows that read listed pages (dream_cache_attn_pages).
 //
-// Work.  An item is up to 128 query entries (entry = (row, query head of one KV-head group)) against a run of keys of one KV head, cut into
-// units of 64 keys.  Shared pages: the rows of all sequences stand together, in tiles of 128 entries, so that the prefix is read once for all of them (once per
-// tile).  A sequence's own tokens: its rows, tile by tile.  Listed pages: one row.  The units of all items, one behind the other, are dealt out to
-// the CTAs in equal contiguous ranges, by arithmetic on the lengths that each CTA does for itself (they are on the device), so long contexts
-// with few rows fill the GPU and short ones do not leave a tail.  An item counts CA_START units more than it has, for what starting and ending it costs.  A
-// range is a few segments, each in one item.  A segment leaves (m, l, O) of its keys; k_cache_merge adds up the
-// segments of a row, always in the same order.  The segment that starts an item has its place by row and head, a CTA's continuation
-// of an item the CTA's own.
+// Where a tile has more than 16 query entries; for fewer see cache_few.cuh, and for how the work is dealt out cache_work.cuh.
 //
 // A segment.  S = Q K^T (128 x 64, fp32 in TMEM, two to four buffers), softmax by eight warps of 16 rows each, the four lanes of a quad to a row (and to the
 // one eight further on): one pass with a running reference m that follows the
@@ -17,17 +10,15 @@
 // then moves the result by at most half a step of sum w |v - out|; the log-sum-exp has a sum of its own, of P as it was.  K and V come by TMA in two rings that
 // run on from segment to segment, so that the next one's keys are under way while one ends.  The producer alone works out what the segments are, ahead of
 // everybody else, and leaves them in a ring in shared memory.
-// Warps: 0 TMA and segments, 1 S, Q and TMEM, 2 O, 3 nothing, 4..11 softmax and epilogue.  Two CTAs share an SM's registers: 80 for each thread, of which
+// Warps: 0 K and segments, 1 Q, S and TMEM, 2 O, 3 V, 4..11 softmax and epilogue.  Two CTAs share an SM's registers: 80 for each thread, of which
 // the first four warps leave the others a part.
 #pragma once
 #include "attn_tc.cuh"
-#include "cache_rows.cuh"
+#include "cache_work.cuh"
 
 #define CA_THREADS 384
 #define CA_WARPS (CA_THREADS / 32)
 #define CA_BLK 64                        // keys of a unit
-#define CA_RING 16                       // units' key masks, and segments, that are known at once: more than the stages and the buffers of S together
-#define CA_START 1                       // units that starting and ending an item is worth
 
 template <int HD> struct CaShape {
   static constexpr int KP = HD / 64;                                   // 64-column panels of a row
@@ -38,43 +29,8 @@ template <int HD> struct CaShape {
   static constexpr int Q_BYTES = 128 * HD * 2, Q_PANEL = 128 * 128;
   static constexpr int STAGE = CA_BLK * HD * 2, PANEL = CA_BLK * 128;
   static constexpr bool SPLIT = CTAS_PER_SM == 2;                      // registers are moved between the warps: 4 x 32 x 64 + 8 x 32 x 88 = 384 x 80
-  static constexpr size_t SMEM = 1024 + Q_BYTES + 2 * STAGES * STAGE + 1536;
+  static constexpr size_t SMEM = 1024 + Q_BYTES + 2 * STAGES * STAGE + 2048;
 };
-
-struct CacheAttnArgs {
-  CacheView c;
-  const void *q;
-  long long q_ld, out_ld;
-  void *out;
-  float *lse;
-  const int *q_start, *kv_len;             // dense: rows by sequence
-  const uint32_t *tree;                    // dense: [rows][4], or null
-  const int *row_seq, *row_pos, *ids;      // pages
-  int budget, rows, heads, group, tile_rows;
-  int shared_tokens;                       // dense: keys [0, shared_tokens) are everybody's
-  float scale_log2;
-  float *part_o;                           // [phase][row][head][HD]: what the segment that starts an item leaves ...
-  float4 *part_ml;                         // [phase][row][head]: its (m, l, l before rounding, what follows: see pack_follow)
-  float *cont_o;                           // [CTA][128][HD], [CTA][128]: the segments that continue one
-  float4 *cont_ml;
-  int n_ctas;
-  int q_small;                             // query rows that the smaller of the two copies of Q takes
-  int *status;
-};
-
-// What the merge has to know about the segments behind an item's first: how many, from which CTA on, and the row's entry in the tile.
-#define CA_DONE 0x7ff                      // nothing is left to merge
-__device__ __forceinline__ float pack_follow(int entry, int n, int cta) { return __int_as_float(entry | n << 7 | cta << 18); }
-
-template <typename T> struct CaType;
-// The rounded P keeps all its digits between the largest value of the type and its smallest normal one: fp16's range ends 2^-14 below 1, so its P are
-// 2^10 times larger and the reference is followed sooner.
-template <> struct CaType<bf16> { static constexpr float SHIFT = 0.f, RESCALE = 8.f; static constexpr uint32_t IDESC = (1u << 7) | (1u << 10); };
-template <> struct CaType<f16> { static constexpr float SHIFT = 10.f, RESCALE = 4.f; static constexpr uint32_t IDESC = 0u; };
-__device__ __forceinline__ uint32_t pack2(float x, float y, bf16) { __nv_bfloat162 h = __floats2bfloat162_rn(x, y); return *reinterpret_cast<uint32_t *>(&h); }
-__device__ __forceinline__ uint32_t pack2(float x, float y, f16) { __half2 h = __floats2half2_rn(x, y); return *reinterpret_cast<uint32_t *>(&h); }
-__device__ __forceinline__ float2 unpack2(uint32_t w, bf16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ float2 unpack2(uint32_t w, f16) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
 
 // D += A B with A in TMEM (lane = row, a column holds two neighbouring elements of K).
 __device__ __forceinline__ void mma_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
@@ -90,88 +46,6 @@ __device__ __forceinline__ void tmem_st16x32(uint32_t taddr, const uint32_t (&r)
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
-// A sequence as the call gives it, held within the buffers whatever its numbers say.
-struct CaSeq {
-  int q0, n, len;                          // first row, rows, tokens
-  __device__ __forceinline__ CaSeq(const CacheAttnArgs &a, int s) {
-    q0 = min(max(a.q_start[s], 0), a.rows);
-    n = min(max(a.q_start[s + 1], q0), a.rows) - q0;
-    len = min(max(a.kv_len[s], 0), a.c.pages_per_seq << a.c.page_shift);
-  }
-  __device__ __forceinline__ int tiles(const CacheAttnArgs &a) const { return (n + a.tile_rows - 1) / a.tile_rows; }
-  // Tokens that some row of tile t sees (behind the last there may be anything), and units of its own ones: at least one, which leaves the row's
-  // place in the partials in order.
-  __device__ __forceinline__ int end(const CacheAttnArgs &a, int t) const { return a.tree ? len : max(0, len - n + min(n, (t + 1) * a.tile_rows)); }
-  __device__ __forceinline__ int units(const CacheAttnArgs &a, int t) const { return max(1, (end(a, t) - a.shared_tokens + CA_BLK - 1) / CA_BLK); }
-  __device__ __forceinline__ long long all_units(const CacheAttnArgs &a) const {
-    long long sum = 0;
-    for (int t = tiles(a) - 1; t >= 0; --t) sum += units(a, t) + CA_START;
-    return sum * a.c.hkv;
-  }
-};
-
-// A segment, as the producer leaves it for the others.
-struct CaSeg {
-  int row0, rows, kvh, seq;                // rows row0 .. row0 + rows - 1 against KV head kvh (phase 1: of sequence seq)
-  int phase;                               // 0: shared keys; 1: the rows' own
-  int end;                                 // keys from here on are nobody's (pages: the row's position)
-  int b0, n, key0;                         // units b0 .. b0 + n - 1 of the item, whose first key is key0; n = 0: there are no more segments
-  int follow;                              // CTAs that continue the item (of the segment that starts it)
-};
-
-// What a CTA has to do: units [u, u_end) of the call, as segments.
-template <bool PAGES> struct CaWalk {
-  long long u, u_end, u_first;
-  int upc;                                 // units per CTA
-  long long prefix_units;
-  int prefix_tiles, prefix_blocks, prefix_rows;
-  int seq, tile;
-  long long at;                            // where the units behind the prefix stand: those of (seq, tile) start here
-  // The part of this CTA in an item of so many blocks: behind CA_START units that stand for its start.  False where the range ends in front of the first.
-  __device__ __forceinline__ bool cut(CaSeg &s, long long item, int blocks) {
-    const int off = (int)(u - item) - CA_START;
-    s.b0 = max(off, 0);
-    const int b1 = (int)min((long long)blocks, u_end - item - CA_START);
-    s.n = b1 - s.b0;
-    s.follow = (int)(item + CA_START + blocks - 1 - u_first) / upc;
-    u = min(u_end, item + CA_START + blocks);
-    return s.n > 0;
-  }
-  __device__ __forceinline__ bool next(const CacheAttnArgs &a, CaSeg &s) {
-    if (PAGES) {
-      while (u < u_end) {
-        const int blocks = prefix_blocks, item = (int)(u / (blocks + CA_START));
-        s.phase = 1; s.row0 = item / a.c.hkv; s.rows = 1; s.kvh = item - s.row0 * a.c.hkv; s.seq = a.row_seq[s.row0]; s.key0 = 0; s.end = a.row_pos[s.row0];
-        if (cut(s, (long long)item * (blocks + CA_START), blocks)) return true;
-      }
-      return false;
-    }
-    while (u < min(u_end, prefix_units)) {
-      const int item = (int)u / (prefix_blocks + CA_START);
-      s.phase = 0; s.seq = 0; s.kvh = item / prefix_tiles;
-      s.row0 = (item - s.kvh * prefix_tiles) * a.tile_rows; s.rows = min(a.tile_rows, prefix_rows - s.row0);
-      s.end = a.shared_tokens; s.key0 = 0;
-      if (cut(s, (long long)item * (prefix_blocks + CA_START), prefix_blocks)) return true;
-    }
-    for (; u < u_end && seq < a.c.n_seqs; ++seq, tile = 0) {
-      const CaSeq q(a, seq);
-      for (const int tiles = q.tiles(a); tile < tiles; ++tile) {
-        const int blocks = q.units(a, tile), each = blocks + CA_START;
-        const long long sum = (long long)each * a.c.hkv;
-        while (u < u_end && u < at + sum) {
-          s.phase = 1; s.seq = seq; s.kvh = (int)(u - at) / each;
-          s.row0 = q.q0 + tile * a.tile_rows; s.rows = min(a.tile_rows, q.n - tile * a.tile_rows);
-          s.end = q.end(a, tile); s.key0 = a.shared_tokens;
-          if (cut(s, at + (long long)s.kvh * each, blocks)) return true;
-        }
-        if (u >= u_end) return false;
-        at += sum;
-      }
-    }
-    return false;
-  }
-};
-
 template <typename T, int HD, bool PAGES>
 __global__ void __launch_bounds__(CA_THREADS, (CaShape<HD>::CTAS_PER_SM))
 k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q,
@@ -184,12 +58,12 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   uint64_t *bars = (uint64_t *)(v_s + STAGES * Sh::STAGE);
   uint64_t *k_full = bars, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES;
   uint64_t *s_full = v_empty + STAGES, *p_full = s_full + SB, *o_done = p_full + SB, *q_full = o_done + SB, *o_free = q_full + 1, *seg_full = o_free + 1;
-  volatile uint64_t *masks = (volatile uint64_t *)(seg_full + CA_RING);    // [CA_RING] which keys of a unit there are
+  uint4 *masks = (uint4 *)(((uintptr_t)(seg_full + CA_RING) + 15) & ~(uintptr_t)15);                         // [CA_RING] which keys of a unit there are
   CaSeg *segs = (CaSeg *)(masks + CA_RING);                                // [CA_RING]
   uint32_t *tmem_base_p = (uint32_t *)(segs + CA_RING);
   volatile int *abort_flag = (volatile int *)(tmem_base_p + 1);
-  __shared__ long long sh_sum[CA_WARPS], sh_at;
-  __shared__ int sh_seq, sh_partial, sh_status[2];
+  __shared__ CaPlanShared plan;
+  __shared__ int sh_status[2];
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, cta = blockIdx.x;
   unsigned long long *tr = trace_open();
@@ -198,10 +72,10 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     else if (lane >= 8 && lane < 8 + SB) { mbar_init(s_full + lane - 8, 1); mbar_init(p_full + lane - 8, 8); mbar_init(o_done + lane - 8, 1); }
     else if (lane >= 16) mbar_init(seg_full + lane - 16, 1);
     if (lane == 12) { mbar_init(q_full, 1); mbar_init(o_free, 8); *abort_flag = 0; }
-    else if (lane == 13) { sh_partial = 0; sh_seq = 0; sh_at = 0; sh_status[0] = sh_status[1] = 0; }
+    else if (lane == 13) { plan.partial = plan.seq = 0; plan.at = 0; sh_status[0] = sh_status[1] = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 3 && lane == 0) {
+  if (warp == 4 && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
@@ -220,62 +94,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   trace_stamp(tr, TR_k_cache_attn);
   int *status = a.status ? a.status : sh_status;
 
-  // ---- this CTA's units
-  CaWalk<PAGES> w;
-  long long total;
-  w.seq = w.tile = 0;
-  w.at = 0;
-  if (PAGES) {
-    w.prefix_blocks = max(1, (a.budget * a.c.page_tokens + CA_BLK - 1) / CA_BLK);
-    total = (long long)a.rows * a.c.hkv * (w.prefix_blocks + CA_START);
-    w.upc = (int)max(1ll, (total + a.n_ctas - 1) / a.n_ctas);
-  } else {
-    w.prefix_rows = min(max(a.q_start[a.c.n_seqs], 0), a.rows);
-    w.prefix_blocks = (a.shared_tokens + CA_BLK - 1) / CA_BLK;
-    w.prefix_tiles = w.prefix_blocks ? (w.prefix_rows + a.tile_rows - 1) / a.tile_rows : 0;
-    w.prefix_units = (long long)w.prefix_tiles * (w.prefix_blocks + CA_START) * a.c.hkv;
-    // units in front of each sequence's, a sequence per thread at a time; once around for most batches, twice where there are more sequences than threads
-    const bool once = a.c.n_seqs <= CA_THREADS;
-    long long own = 0, sum = 0;
-    for (int s = threadIdx.x; s < a.c.n_seqs; s += CA_THREADS) {
-      const CaSeq q(a, s);
-      own = q.all_units(a);
-      sum += own;
-      if (q.n && q.len - q.n + (a.tree ? 0 : 1) < a.shared_tokens) sh_partial = 1;       // a row that does not see the whole prefix
-      if (cta == 0 && (q.q0 != a.q_start[s] || q.q0 + q.n != a.q_start[s + 1] || q.len != a.kv_len[s])) cache_bad_index(status);
-    }
-    for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
-    if (lane == 31) sh_sum[warp] = sum;
-    __syncthreads();
-    total = w.prefix_units;
-    long long before = w.prefix_units + sum - own;
-    for (int i = 0; i < CA_WARPS; ++i) { if (i < warp) before += sh_sum[i]; total += sh_sum[i]; }
-    w.upc = (int)max(1ll, (total + a.n_ctas - 1) / a.n_ctas);
-    // the sequence in which the units behind the prefix start for this CTA
-    const long long goal = max(min((long long)cta * w.upc, total), w.prefix_units);
-    if (once) {
-      if (goal >= before && goal < before + own) { sh_seq = threadIdx.x; sh_at = before; }
-    } else {
-      long long at = w.prefix_units;
-      for (int s0 = 0; s0 < a.c.n_seqs && at <= goal; s0 += CA_THREADS) {
-        const int s = s0 + threadIdx.x;
-        own = s < a.c.n_seqs ? CaSeq(a, s).all_units(a) : 0ll;
-        sum = own;
-        for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
-        __syncthreads();
-        if (lane == 31) sh_sum[warp] = sum;
-        __syncthreads();
-        before = at + sum - own;
-        for (int i = 0; i < CA_WARPS; ++i) { if (i < warp) before += sh_sum[i]; at += sh_sum[i]; }
-        if (goal >= before && goal < before + own) { sh_seq = s; sh_at = before; }
-      }
-    }
-    __syncthreads();
-    w.seq = sh_seq; w.at = sh_at;
-  }
-  w.u_first = (long long)cta * w.upc;
-  w.u = min(w.u_first, total);
-  w.u_end = min(w.u + w.upc, total);
+  CaWalk<CA_BLK, PAGES> w;
+  w.plan(a, plan, status);
   const uint32_t tmem_base = *tmem_base_p;
   int gave_up = WAIT_none;
   // Units of segment number i, once the producer has left it; 0: there is none, or a wait ran out.
@@ -289,97 +109,9 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
   }
   if (warp == 0) {
-    // ------------------------------------------------------------------ TMA producer
-    const uint64_t pol = policy_evict_normal();
-    const int sub = min(CA_BLK, a.c.page_tokens), n_sub = CA_BLK / sub;     // keys of one copy, copies of a unit
-    int ks = 0, vs = 0, g = 0, n_seg = 0;
-    uint32_t kph = 1, vph = 1;
-    for (;; ++n_seg) {
-      CaSeg s;
-      if (!w.next(a, s)) s.n = 0;
-      if (elect_one()) {
-        segs[n_seg % CA_RING] = s;
-        mbar_arrive(seg_full + n_seg % CA_RING);
-      }
-      __syncwarp();
-      if (!s.n) break;
-      // lane l holds the page of part p0 + l of the item's keys, and the first of these keys in the sequence
-      int p0 = -64, page = 0, token = 0;
-      for (int blk = s.b0; blk < s.b0 + s.n && !gave_up; ++blk, ++g) {
-        const int part = blk * n_sub;
-        if (part < p0 || part + n_sub > p0 + 32) {
-          p0 = part;
-          const int first = (p0 + lane) * sub;             // key of the item
-          page = -1;
-          token = 0;
-          bool bad = false;
-          if (PAGES) {
-            const int e = first >> a.c.page_shift;
-            const int *ids = a.ids + ((long long)s.row0 * a.c.hkv + s.kvh) * a.budget;
-            if (s.seq >= 0 && s.end >= 0) {
-              if (!a.c.token_ok(s.seq, s.end)) bad = true;
-              else if (e < a.budget) {
-                const int id = ids[e], before = e ? ids[e - 1] : -1;
-                if (id > before && id >= 0 && id <= s.end >> a.c.page_shift) {
-                  token = (id << a.c.page_shift) + (first & (a.c.page_tokens - 1));
-                  page = a.c.page(s.seq, id);
-                  bad = page < 0;
-                }
-              }
-            }
-          } else {
-            token = s.key0 + first;
-            if (token < s.end) {
-              page = a.c.page(s.seq, token >> a.c.page_shift);
-              bad = page < 0;
-            }
-          }
-          if (bad) cache_bad_index(status);
-        }
-        // which of the unit's keys there are: of its parts with a page, those in front of the end
-        uint32_t m0 = 0, m1 = 0;
-        const int i = lane - (part - p0);
-        if (i >= 0 && i < n_sub && page >= 0) {
-          const int n = min(sub, max(0, (PAGES ? s.end + 1 : s.end) - token));
-          const uint64_t m = (n >= 64 ? ~0ull : (1ull << n) - 1ull) << (i * sub);
-          m0 = (uint32_t)m; m1 = (uint32_t)(m >> 32);
-        }
-        m0 = __reduce_or_sync(0xffffffffu, m0);
-        m1 = __reduce_or_sync(0xffffffffu, m1);
-        for (int which = 0; which < 2 && !gave_up; ++which) {
-          int &st = which ? vs : ks;
-          uint32_t &ph = which ? vph : kph;
-          uint64_t *full = (which ? v_full : k_full) + st;
-          uint8_t *dst = (which ? v_s : k_s) + st * Sh::STAGE;
-          const CUtensorMap *map = which ? &map_v : &map_k;
-          if (!mbar_wait_warp((which ? v_empty : k_empty) + st, ph, abort_flag)) { gave_up = WAIT_cache_kv_ring; break; }
-          if (elect_one()) {
-            if (!which) masks[g % CA_RING] = (uint64_t)m0 | (uint64_t)m1 << 32;
-            mbar_expect_tx(full, (uint32_t)Sh::STAGE);
-          }
-          __syncwarp();
-          for (int j = 0; j < n_sub; ++j) {
-            // a part without a page is filled with zeros: its page number is past the last
-            const int pg = __shfl_sync(0xffffffffu, page, part - p0 + j), tk = __shfl_sync(0xffffffffu, token, part - p0 + j) & (a.c.page_tokens - 1);
-            if (elect_one()) {
-              if (n_sub == 1) tma_load_5d(dst, map, full, 0, tk, 0, s.kvh, pg < 0 ? a.c.n_pages : pg, pol);
-              else
-                for (int kp = 0; kp < KP; ++kp) tma_load_5d(dst + kp * Sh::PANEL + j * sub * 128, map, full, 0, tk, kp, s.kvh, pg < 0 ? a.c.n_pages : pg, pol);
-            }
-            __syncwarp();
-          }
-          if (++st == STAGES) { st = 0; ph ^= 1u; }
-        }
-      }
-      if (gave_up) break;
-    }
-    // Until the last releases have arrived: one that came in after this CTA has left would land in the shared memory of the next.
-#pragma unroll 1
-    for (int i = 0; i < STAGES && !gave_up; ++i) {
-      if (!mbar_wait_warp(k_empty + ks, kph, abort_flag) || !mbar_wait_warp(v_empty + vs, vph, abort_flag)) gave_up = WAIT_cache_last;
-      if (++ks == STAGES) { ks = 0; kph ^= 1u; }
-      if (++vs == STAGES) { vs = 0; vph ^= 1u; }
-    }
+    gave_up = ca_produce<HD, CA_BLK, STAGES, 0, PAGES>(a, w, CaRing{k_full, k_empty, seg_full, k_s, masks, segs, &map_k, abort_flag, status}, lane);
+  } else if (warp == 3) {
+    gave_up = ca_produce<HD, CA_BLK, STAGES, 1, PAGES>(a, w, CaRing{v_full, v_empty, nullptr, v_s, nullptr, nullptr, &map_v, abort_flag, status}, lane);
   } else if (warp == 1) {
     // ------------------------------------------------------------------ queries, and S = Q K^T: both operands K-major, N = 64
     constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | ((uint32_t)(CA_BLK >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -431,7 +163,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll 1
       for (int i = 0; i < n; ++i, ++g) {
         if (!__all_sync(0xffffffffu, mbar_wait(v_full + vs, vph, abort_flag) && mbar_wait(p_full + sb, pph, abort_flag))) { gave_up = WAIT_cache_p_v; break; }
-        const uint64_t m = masks[g % CA_RING];
+        const uint64_t m = masks[g % CA_RING].x | (uint64_t)masks[g % CA_RING].y << 32;
         if (m != ~0ull) {
           // values that are nobody's may be anything, and 0 times that not 0
           uint8_t *dst = v_s + vs * Sh::STAGE;
@@ -482,16 +214,15 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       int vis[2] = {0x7fffffff, 0x7fffffff};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        if (!PAGES && mine[k] && (s.phase || sh_partial)) {
+        if (!PAGES && mine[k] && (s.phase || plan.partial)) {
           const int r = s.row0 + (base + quad + 8 * k) / a.group;
-          int sq = s.seq;
+          int tail0 = s.tail0, q0 = s.q0;
           if (!s.phase) {                                                   // the sequence that has the row
-            int lo = 0, hi = a.c.n_seqs;
-            while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (a.q_start[m] <= r) lo = m; else hi = m; }
-            sq = lo;
+            const CaSeq q(a, ca_seq_of(a, r));
+            tail0 = q.len - q.n;
+            q0 = q.q0;
           }
-          const CaSeq q(a, sq);
-          vis[k] = q.len - q.n + (tree ? 0 : r - q.q0 + 1) - (s.key0 + s.b0 * CA_BLK);
+          vis[k] = tail0 + (tree ? 0 : r - q0 + 1) - (s.key0 + s.b0 * CA_BLK);
         }
       }
       float m_ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, l_true[2] = {0.f, 0.f};      // l: this lane's share of the sums
@@ -503,7 +234,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           const uint32_t s_col = lane_addr + (uint32_t)(HD + sb * CA_BLK);
           uint32_t sr[32];                                                  // sr[4 c + 2 k + j]: row k, key 8 c + 2 ql + j
           tmem_ld16x64(s_col, sr);
-          const uint64_t um = masks[g % CA_RING];
+          const uint64_t um = masks[g % CA_RING].x | (uint64_t)masks[g % CA_RING].y << 32;
           const bool all = um == ~0ull && vis[0] - i * CA_BLK >= CA_BLK && vis[1] - i * CA_BLK >= CA_BLK;
           tmem_ld_wait();
           if (!__all_sync(0xffffffffu, all)) {
@@ -597,11 +328,11 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         r[k] = s.row0 + e / a.group;
         h[k] = s.kvh * a.group + e % a.group;
         const long long rh = (long long)r[k] * a.heads + h[k];
-        at[k] = starts ? (PAGES ? rh : (long long)s.phase * a.rows * a.heads + rh) : (long long)cta * 128 + e;
+        at[k] = starts ? (PAGES ? rh : (long long)s.phase * a.rows * a.heads + rh) : (long long)(a.cont_base + cta) * 128 + e;
         if (mine[k] && ql == 0) {
           const float m = m_ref[k] == -INFINITY ? m_ref[k] : m_ref[k] - CaType<T>::SHIFT;
           if (starts) {
-            a.part_ml[at[k]] = make_float4(m, l[k], l_true[k], pack_follow(e, final || !row_on ? CA_DONE : s.follow, cta + 1));
+            a.part_ml[at[k]] = make_float4(m, l[k], l_true[k], pack_follow(e, final || !row_on ? CA_DONE : s.follow, a.cont_base + cta + 1));
             if (final && row_on && a.lse) a.lse[rh] = l[k] > 0.f ? (m + log2f(l_true[k])) * 0.6931471805599453f : -INFINITY;
           } else a.cont_ml[at[k]] = make_float4(m, l[k], l_true[k], 0.f);
         }
@@ -652,62 +383,4 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)Sh::TMEM_COLS) : "memory");
   }
-}
-
-// The segments of a (row, head), from the first to the last: out = sum w O / sum w l with w = 2^(m - max m).  A thread takes eight columns, and of the segments four
-// at a time, so that their loads are under way together.
-template <typename T, int HD, bool PAGES>
-__global__ void __launch_bounds__(256)
-k_cache_merge(const __grid_constant__ CacheAttnArgs a) {
-  kernel_entry(TR_k_cache_merge);
-  constexpr int V = HD / 8;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, rh = i / V;
-  const int c0 = (int)(i % V) * 8, r = (int)(rh / a.heads);
-  if (r >= a.rows || (!PAGES && r >= a.q_start[a.c.n_seqs])) return;
-  float M = -INFINITY, L = 0.f, Lt = 0.f, acc[8] = {};
-  auto add = [&](const float4 &ml, const float4 &x, const float4 &y) {
-    if (ml.x == -INFINITY) return;
-    const float Mn = fmaxf(M, ml.x), sc = ex2(M - Mn), w = ex2(ml.x - Mn);
-    L = L * sc + ml.y * w; Lt = Lt * sc + ml.z * w;
-    acc[0] = acc[0] * sc + x.x * w; acc[1] = acc[1] * sc + x.y * w; acc[2] = acc[2] * sc + x.z * w; acc[3] = acc[3] * sc + x.w * w;
-    acc[4] = acc[4] * sc + y.x * w; acc[5] = acc[5] * sc + y.y * w; acc[6] = acc[6] * sc + y.z * w; acc[7] = acc[7] * sc + y.w * w;
-    M = Mn;
-  };
-  // what starts the row's items, shared and own
-  const int first = PAGES || a.shared_tokens ? 0 : 1, last = PAGES ? 0 : 1;
-  float4 ml[2], x[2], y[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const long long at = (long long)k * a.rows * a.heads + rh;
-    const bool on = k >= first && k <= last;
-    ml[k] = on ? a.part_ml[at] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-    x[k] = on ? *reinterpret_cast<const float4 *>(a.part_o + at * HD + c0) : make_float4(0.f, 0.f, 0.f, 0.f);
-    y[k] = on ? *reinterpret_cast<const float4 *>(a.part_o + at * HD + c0 + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    if (k < first || k > last) continue;
-    const int f = __float_as_int(ml[k].w), entry = f & 127, cta = f >> 18 & 0x3ff;
-    int n = f >> 7 & 0x7ff;
-    if (n == CA_DONE) return;
-    n = min(n, a.n_ctas - cta);
-    add(ml[k], x[k], y[k]);
-    for (int j = 0; j < n; j += 4) {
-      float4 cm[4], cx[4], cy[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const long long c = (long long)(cta + min(j + q, n - 1)) * 128 + entry;
-        cm[q] = a.cont_ml[c];
-        cx[q] = *reinterpret_cast<const float4 *>(a.cont_o + c * HD + c0);
-        cy[q] = *reinterpret_cast<const float4 *>(a.cont_o + c * HD + c0 + 4);
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) if (j + q < n) add(cm[q], cx[q], cy[q]);
-    }
-  }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) acc[k] *= inv;
-  *reinterpret_cast<uint4 *>((T *)a.out + r * a.out_ld + (rh - (long long)r * a.heads) * HD + c0) = pack8<T>(acc);
-  if (a.lse && c0 == 0) a.lse[rh] = L > 0.f ? (M + log2f(Lt)) * 0.6931471805599453f : -INFINITY;
 }
