@@ -332,22 +332,22 @@ static const char *cache_attn_many(const dream_cache *cache, CacheAttnArgs &a, c
   a.cont_base = 0;
   return cache_launch(k_cache_attn<T, HD, PAGES>, dim3(a.n_ctas), CA_THREADS, CaShape<HD>::SMEM, stream, mk, mv, mq, ms, a);
 }
-// Tiles of up to 16.
-template <typename T, int HD, bool PAGES>
+// Tiles of up to NE.
+template <typename T, int HD, int NE, bool PAGES>
 static const char *cache_attn_few(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
   using Sh = CfShape<HD>;
   cudaError_t e = cudaSuccess;
-  const int sms = cache_allow(k_cache_attn_few<T, HD, PAGES>, Sh::SMEM, 0, &e);
+  const int sms = cache_allow(k_cache_attn_few<T, HD, NE, PAGES>, Sh::SMEM, 0, &e);
   if (!sms) { cudaGetLastError(); return cudaGetErrorString(e); }
   CUtensorMap mk, mv, mq;
-  a.tile_rows = CF_N / a.group;
+  a.tile_rows = NE / a.group;
   const char *why = cache_kv_map(cache, a.c, a.c.k, Sh::BLK, &mk);
   if (!why) why = cache_kv_map(cache, a.c, a.c.v, Sh::BLK, &mv);
   if (!why) why = cache_q_map(cache, a, a.tile_rows, &mq);
   if (why) return why;
   a.n_ctas = sms * Sh::CTAS_PER_SM;
   a.cont_base = CACHE_MAX_SMS * CaShape<HD>::CTAS_PER_SM;
-  return cache_launch(k_cache_attn_few<T, HD, PAGES>, dim3(a.n_ctas), CF_THREADS, Sh::SMEM, stream, mk, mv, mq, a);
+  return cache_launch(k_cache_attn_few<T, HD, NE, PAGES>, dim3(a.n_ctas), CF_THREADS, Sh::SMEM, stream, mk, mv, mq, a);
 }
 template <typename T, int HD, bool PAGES>
 static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
@@ -361,7 +361,11 @@ static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cu
   if (!both || !own_few) why = cache_attn_many<T, HD, PAGES>(cache, a, stream);
   a.with_own = 1;
   a.with_prefix = both && a.shared_tokens > 0;
-  if (!why && own_few) why = cache_attn_few<T, HD, PAGES>(cache, a, stream);
+  if (!why && own_few) {
+    // up to four entries, on the average, take a quarter of the code and of the registers
+    const bool four = a.group <= 4 && (PAGES || (long long)a.rows * a.group <= 4LL * a.c.n_seqs);
+    why = four ? cache_attn_few<T, HD, 4, PAGES>(cache, a, stream) : cache_attn_few<T, HD, CF_N, PAGES>(cache, a, stream);
+  }
   const long long merge = (long long)a.rows * a.heads * (HD / 8);
   return why ? why : cache_launch(k_cache_merge<T, HD, PAGES>, dim3((unsigned)((merge + 255) / 256)), 256, 0, stream, a);
 }

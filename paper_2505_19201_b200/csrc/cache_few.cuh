@@ -40,9 +40,23 @@ __device__ __forceinline__ bool cf_any(bool mine) {                    // ... of
   asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"((uint32_t)mine) : "memory");
   return r != 0;
 }
+// So many columns of a warp's 32 lanes, a lane to a thread.
+__device__ __forceinline__ void cf_ld(uint32_t taddr, uint32_t (&r)[16]) { tmem_ld16(taddr, r); }
+__device__ __forceinline__ void cf_ld(uint32_t taddr, uint32_t (&r)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void cf_st(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+                 "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void cf_st(uint32_t taddr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
 __device__ __forceinline__ void cf_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
 
-template <typename T, int HD, bool PAGES>
+// NE: entries of a tile at most.
+template <typename T, int HD, int NE, bool PAGES>
 __global__ void __launch_bounds__(CF_THREADS, (CfShape<HD>::CTAS_PER_SM))
 k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q,
                  const __grid_constant__ CacheAttnArgs a) {
@@ -62,10 +76,10 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   volatile int *abort_flag = (volatile int *)(tmem_base_p + 1);
   __shared__ CaPlanShared plan;
   __shared__ int sh_status[2];
-  __shared__ float red[4][CF_N];                                           // maxima of the warps
-  __shared__ float2 sums[4][CF_N];                                         // their sums of weights
-  __shared__ int e_vis[2][CF_N], e_row[2][CF_N];                           // of a segment's entries: what they see, their row
-  __shared__ long long e_at[2][CF_N];                                      // ... and row * heads + head
+  __shared__ float red[4][NE];                                           // maxima of the warps
+  __shared__ float2 sums[4][NE];                                         // their sums of weights
+  __shared__ int e_vis[2][NE], e_row[2][NE];                           // of a segment's entries: what they see, their row
+  __shared__ long long e_at[2][NE];                                      // ... and row * heads + head
   static_assert(CA_RING > STAGES + CF_S + 1, "what the producer leaves is read until a unit's P is done");
   static_assert(sizeof(uint64_t) * (4 * STAGES + 2 * CF_S + 10 + CA_RING) + sizeof(uint4) * CA_RING + sizeof(CaSeg) * CA_RING + 8 <= 2048, "room for the barriers and rings");
 
@@ -200,9 +214,9 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     const int q = warp & 3, t = q * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
     bool ok = true;
-    auto wait = [&](uint64_t *bar, uint32_t parity) {                       // one lane polls for the warp
+    auto wait = [&](uint64_t *bar, uint32_t parity, uint64_t *bar2 = nullptr, uint32_t parity2 = 0) {      // one lane polls for the warp
       int v = 1;
-      if (lane == 0 && (!ok || !mbar_wait(bar, parity, abort_flag))) v = 0;
+      if (lane == 0 && (!ok || !mbar_wait(bar, parity, abort_flag) || (bar2 && !mbar_wait(bar2, parity2, abort_flag)))) v = 0;
       if (!__shfl_sync(0xffffffffu, v, 0) && ok) {
         ok = false;
         if (lane == 0) wait_expired(status, WAIT_cache_softmax, abort_flag, -1);
@@ -218,7 +232,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const CaSeg &s = segs[seg % CA_RING];
       const int n_e = n > 0 ? s.rows * a.group : 0;
       // the entries' rows, and what they see: keys below vis (counted from the segment's first), in a tree their own ones as the mask has them
-      if (n > 0 && t < CF_N) {
+      if (n > 0 && t < NE) {
         const int r = s.row0 + min(t, n_e - 1) / a.group;
         int vis = 0x7fffffff;
         if (!PAGES && t < n_e && (s.phase || plan.partial)) {
@@ -237,17 +251,18 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       if (cf_any(n <= 0)) break;                            // (whatever a wait of one warp came to, they all go on or all leave: barriers follow)
       int least = e_vis[ob][0];                             // what every entry sees
 #pragma unroll
-      for (int e = 1; e < CF_N; ++e) least = min(least, e_vis[ob][e]);
-      float m_ref[CF_N], l[CF_N], l_true[CF_N];
+      for (int e = 1; e < NE; ++e) least = min(least, e_vis[ob][e]);
+      float m_ref[NE], l[NE], l_true[NE];
 #pragma unroll
-      for (int e = 0; e < CF_N; ++e) { m_ref[e] = -INFINITY; l[e] = l_true[e] = 0.f; }
+      for (int e = 0; e < NE; ++e) { m_ref[e] = -INFINITY; l[e] = l_true[e] = 0.f; }
 #pragma unroll 1
       for (int i = 0; i < n; ++i, ++g) {
         const int pb = g & 1;
-        wait(s_full + sb, sph);
+        // S of the unit, and room for its P: O of the unit before last (its barrier's phases are all waited for, one behind the other)
+        wait(s_full + sb, sph, g > 1 ? o_done + pb : nullptr, (uint32_t)((g >> 1) - 1) & 1u);
         tc_fence_after();
-        uint32_t sr[16];
-        tmem_ld16(tmem_base + lane_addr + (uint32_t)(sb * CF_N), sr);
+        uint32_t sr[NE];
+        cf_ld(tmem_base + lane_addr + (uint32_t)(sb * CF_N), sr);
         const uint4 um = masks[g % CA_RING];
         const bool all = least - i * BLK >= BLK && (um.x & um.y & (BLK == 128 ? um.z & um.w : 0xffffffffu)) == 0xffffffffu;
         tmem_ld_wait();
@@ -255,72 +270,62 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         __syncwarp();
         if (lane == 0) mbar_arrive(s_empty + sb);
         if (++sb == CF_S) { sb = 0; sph ^= 1u; }
-        float x[CF_N];
+        float x[NE];
 #pragma unroll
-        for (int e = 0; e < CF_N; ++e) x[e] = __uint_as_float(sr[e]);
+        for (int e = 0; e < NE; ++e) x[e] = __uint_as_float(sr[e]);
         bool there = has_key;
         if (!all) {
           const uint32_t mw = q == 0 ? um.x : q == 1 ? um.y : q == 2 ? um.z : um.w;
           there = has_key && (mw >> lane & 1u);
 #pragma unroll
-          for (int e = 0; e < CF_N; ++e) {
-            if (e >= n_e) break;
+          for (int e = 0; e < NE; ++e) {
             const int behind = t + i * BLK - e_vis[ob][e];                  // node of the key, in a tree
             bool sees = there && behind < 0;
-            if (tree && there && behind >= 0 && behind < 128) sees = a.tree[(long long)e_row[ob][e] * 4 + (behind >> 5)] >> (behind & 31) & 1u;
+            if (tree && there && behind >= 0 && behind < 128 && e < n_e) sees = a.tree[(long long)e_row[ob][e] * 4 + (behind >> 5)] >> (behind & 31) & 1u;
             x[e] = sees ? x[e] : -INFINITY;
           }
         }
         bool grow = false;
 #pragma unroll
-        for (int e = 0; e < CF_N; ++e)
-          if (e < n_e) grow = grow || (x[e] * scale > m_ref[e] + CaType<T>::RESCALE);
+        for (int e = 0; e < NE; ++e) grow = grow || (e < n_e && x[e] * scale > m_ref[e] + CaType<T>::RESCALE);
         if (cf_any(grow && has_key)) {
           // ---- the maxima of the unit, and new references where they have grown
 #pragma unroll
-          for (int e = 0; e < CF_N; ++e)
-            if (e < n_e) {
-              const float v = order_value(__reduce_max_sync(0xffffffffu, order_key(has_key ? x[e] : -INFINITY)));
-              if (lane == 0) red[q][e] = v;
-            }
+          for (int e = 0; e < NE; ++e) {
+            const float v = order_value(__reduce_max_sync(0xffffffffu, order_key(has_key ? x[e] : -INFINITY)));
+            if (lane == 0) red[q][e] = v;
+          }
           cf_sync();
-          float corr[CF_N];
+          float corr[NE];
 #pragma unroll
-          for (int e = 0; e < CF_N; ++e) {
-            corr[e] = 1.f;
-            if (e < n_e) {
-              const float bm = fmaxf(fmaxf(red[0][e], red[1][e]), fmaxf(red[2][e], red[3][e])) * scale;
-              if (bm > m_ref[e] + CaType<T>::RESCALE) {
-                corr[e] = ex2(m_ref[e] - bm);
-                l[e] *= corr[e]; l_true[e] *= corr[e];
-                m_ref[e] = bm;
-              }
-            }
+          for (int e = 0; e < NE; ++e) {                                    // (entries past n_e have scores of nothing in particular, and nobody reads what comes of them)
+            const float bm = fmaxf(fmaxf(red[0][e], red[1][e]), fmaxf(red[2][e], red[3][e])) * scale;
+            const bool more = bm > m_ref[e] + CaType<T>::RESCALE;
+            corr[e] = more ? ex2(m_ref[e] - bm) : 1.f;
+            l[e] *= corr[e]; l_true[e] *= corr[e];
+            m_ref[e] = more ? bm : m_ref[e];
           }
           if (i > 0) {                                                      // behind the O of every earlier unit
             wait(o_done + ((g - 1) & 1), (uint32_t)((g - 1) >> 1) & 1u);
             tc_fence_after();
 #pragma unroll
             for (int mt = 0; mt < Sh::MT; ++mt) {
-              uint32_t o[16];
+              uint32_t o[NE];
               const uint32_t at = o_base + lane_addr + (uint32_t)(ob * Sh::O_COLS + mt * CF_N);
-              tmem_ld16(at, o);
+              cf_ld(at, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < CF_N; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr[e]);
-              asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-                           ::"r"(at), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(o[8]), "r"(o[9]), "r"(o[10]),
-                             "r"(o[11]), "r"(o[12]), "r"(o[13]), "r"(o[14]), "r"(o[15]) : "memory");
+              for (int e = 0; e < NE; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr[e]);
+              cf_st(at, o);
             }
             tmem_st_wait();
           }
         }
-        if (g > 1) wait(o_done + pb, (uint32_t)((g >> 1) - 1) & 1u);        // the buffer of P is free
         if (has_key) {
           uint8_t *p = p_s + pb * Sh::P_BYTES + p_row;
 #pragma unroll
-          for (int e = 0; e < CF_N; ++e)
-            if (e < n_e) {
+          for (int e = 0; e < NE; ++e)
+            if (NE <= 4 || e < n_e) {
               const float w_true = ex2(fmaf(x[e], scale, (m_ref[e] == -INFINITY ? 0.f : -m_ref[e]) + CaType<T>::SHIFT));
               const T w = from_f<T>(w_true);
               *reinterpret_cast<T *>(p + e * 128 + ((p_chunk ^ (e & 7)) << 4)) = w;
@@ -342,24 +347,29 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full + pb);
       }
-      // ---- epilogue.  The sums of weights, across the lanes by halves: lane 2 e' ends up with those of entry e'
+      // ---- epilogue.  The sums of weights, across the lanes by halves: lane e (32 / NE) ends up with those of entry e
       {
-        float v[CF_N], u[CF_N];
+        float v[NE], u[NE];
 #pragma unroll
-        for (int e = 0; e < CF_N; ++e) { v[e] = l[e]; u[e] = l_true[e]; }
+        for (int e = 0; e < NE; ++e) { v[e] = l[e]; u[e] = l_true[e]; }
+        int width = NE;
 #pragma unroll
-        for (int o = 16, width = CF_N / 2; o > 1; o >>= 1, width /= 2) {
-          const bool up = (lane & o) != 0;
+        for (int o = 16; o > 0; o >>= 1) {
+          if (width > 1) {
+            width /= 2;
+            const bool up = (lane & o) != 0;
 #pragma unroll
-          for (int j = 0; j < CF_N / 2; ++j)
-            if (j < width) {
-              v[j] = (up ? v[j + width] : v[j]) + __shfl_xor_sync(0xffffffffu, up ? v[j] : v[j + width], o);
-              u[j] = (up ? u[j + width] : u[j]) + __shfl_xor_sync(0xffffffffu, up ? u[j] : u[j + width], o);
-            }
+            for (int j = 0; j < NE / 2; ++j)
+              if (j < width) {
+                v[j] = (up ? v[j + width] : v[j]) + __shfl_xor_sync(0xffffffffu, up ? v[j] : v[j + width], o);
+                u[j] = (up ? u[j + width] : u[j]) + __shfl_xor_sync(0xffffffffu, up ? u[j] : u[j + width], o);
+              }
+          } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+            u[0] += __shfl_xor_sync(0xffffffffu, u[0], o);
+          }
         }
-        v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
-        u[0] += __shfl_xor_sync(0xffffffffu, u[0], 1);
-        if (!(lane & 1)) sums[q][lane >> 1] = make_float2(v[0], u[0]);
+        if (lane % (32 / NE) == 0) sums[q][lane / (32 / NE)] = make_float2(v[0], u[0]);
       }
       cf_sync();
       const bool starts = s.b0 == 0, final = starts && !s.follow && (PAGES || !a.shared_tokens), row_on = !PAGES || s.seq >= 0;
@@ -367,15 +377,15 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const long long phase_at = PAGES ? 0 : (long long)s.phase * a.rows * a.heads, cont_at = (long long)(a.cont_base + cta) * 128;
       wait(o_done + ((g - 1) & 1), (uint32_t)((g - 1) >> 1) & 1u);
       tc_fence_after();
-      uint32_t o[Sh::MT][16];
+      uint32_t o[Sh::MT][NE];
 #pragma unroll
-      for (int mt = 0; mt < Sh::MT; ++mt) tmem_ld16(o_base + lane_addr + (uint32_t)(ob * Sh::O_COLS + mt * CF_N), o[mt]);
+      for (int mt = 0; mt < Sh::MT; ++mt) cf_ld(o_base + lane_addr + (uint32_t)(ob * Sh::O_COLS + mt * CF_N), o[mt]);
       tmem_ld_wait();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(o_free + ob);
 #pragma unroll
-      for (int e = 0; e < CF_N; ++e)
+      for (int e = 0; e < NE; ++e)
         if (e < n_e && ok) {
           const float2 s0 = sums[0][e], s1 = sums[1][e], s2 = sums[2][e], s3 = sums[3][e];
           const float sl = (s0.x + s1.x) + (s2.x + s3.x), st = (s0.y + s1.y) + (s2.y + s3.y), m = m_ref[e] == -INFINITY ? m_ref[e] : m_ref[e] - CaType<T>::SHIFT;
