@@ -388,7 +388,8 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   if (!s) s = cache_ints(who, "tree_mask", tree_mask, false);
   if (s) return s;
   if (shared_pages < 0 || shared_pages > cache->pages_per_seq) return fail(nullptr, DREAM_E_ARG, "%s: shared_pages = %d outside 0..pages_per_seq = %d", who, shared_pages, cache->pages_per_seq);
-  a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask; a.shared_tokens = shared_pages * cache->page_tokens;
+  a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask; // Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item with their own keys, whose parts need not be put together.
+  a.shared_tokens = (long long)rows * a.group >= 256LL * cache->n_seqs ? 0 : shared_pages * cache->page_tokens;
   // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits
   const long long units = (long long)((cache->pages_per_seq * (long long)cache->page_tokens + CA_BLK - 1) / CA_BLK) * cache->n_kv_heads;
   if (units > 0x7fffffffLL || (shared_pages && (units * shared_pages / cache->pages_per_seq + cache->n_kv_heads) * ((rows + 128 / a.group - 1) / (128 / a.group)) > 0x7fffffffLL))

@@ -38,12 +38,49 @@ __device__ __forceinline__ void mma_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uin
       "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
       ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
 }
-// 16 lanes x 32 columns: lane 4 i + j of the warp puts r[2 c] into column 4 c + j of TMEM lane i, r[2 c + 1] into that of lane i + 8.
-__device__ __forceinline__ void tmem_st16x32(uint32_t taddr, const uint32_t (&r)[16]) {
+// 16 lanes x 32 columns, as tmem_ld16x64 has them.
+__device__ __forceinline__ void tmem_ld16x32(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+// 16 lanes x 16 columns: lane 4 i + j of the warp puts r[2 c] into column 4 c + j of TMEM lane i, r[2 c + 1] into that of lane i + 8.
+__device__ __forceinline__ void tmem_st16x16(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_st16x32f(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+        "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// The first half of a unit's P, already stored, times a factor for each of the two rows: powers that end below 1, rounded once more.
+template <typename T> __device__ __forceinline__ void ca_rescale_p(uint32_t s_col, float corr0, float corr1) {
+  uint32_t p[8];
+  tmem_st_wait();
+  asm volatile("tcgen05.ld.sync.aligned.16x128b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(p[0]), "=r"(p[1]), "=r"(p[2]), "=r"(p[3]), "=r"(p[4]), "=r"(p[5]), "=r"(p[6]), "=r"(p[7]) : "r"(s_col) : "memory");
+  tmem_ld_wait();
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const float2 f = unpack2(p[c], T());
+    const float corr = c & 1 ? corr1 : corr0;
+    p[c] = pack2(f.x * corr, f.y * corr, T());
+  }
+  tmem_st16x16(s_col, p);
+}
+// Two at a time (an instruction for both).
+__device__ __forceinline__ float2 ca_add(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(r)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 ca_fma(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<unsigned long long &>(r)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)), "l"(reinterpret_cast<unsigned long long &>(c)));
+  return r;
 }
 
 template <typename T, int HD, bool PAGES>
@@ -72,7 +109,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     else if (lane >= 8 && lane < 8 + SB) { mbar_init(s_full + lane - 8, 1); mbar_init(p_full + lane - 8, 8); mbar_init(o_done + lane - 8, 1); }
     else if (lane >= 16) mbar_init(seg_full + lane - 16, 1);
     if (lane == 12) { mbar_init(q_full, 1); mbar_init(o_free, 8); *abort_flag = 0; }
-    else if (lane == 13) { plan.partial = plan.seq = 0; plan.at = 0; sh_status[0] = sh_status[1] = 0; }
+    else if (lane == 13) { plan.partial = 0; sh_status[0] = sh_status[1] = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 4 && lane == 0) {
@@ -225,86 +262,94 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           vis[k] = tail0 + (tree ? 0 : r - q0 + 1) - (s.key0 + s.b0 * CA_BLK);
         }
       }
-      float m_ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, l_true[2] = {0.f, 0.f};      // l: this lane's share of the sums
+      float m_ref[2] = {-INFINITY, -INFINITY};
+      float2 l2[2], t2[2];                                                  // this lane's share of the sums, rounded and as they were
+      l2[0] = l2[1] = t2[0] = t2[1] = make_float2(0.f, 0.f);
 #pragma unroll 1
       for (int i = 0; i < n; ++i, ++g) {
         wait(s_full + sb, sph);
         if (active) {
           tc_fence_after();
-          const uint32_t s_col = lane_addr + (uint32_t)(HD + sb * CA_BLK);
-          uint32_t sr[32];                                                  // sr[4 c + 2 k + j]: row k, key 8 c + 2 ql + j
-          tmem_ld16x64(s_col, sr);
-          const uint64_t um = masks[g % CA_RING].x | (uint64_t)masks[g % CA_RING].y << 32;
-          const bool all = um == ~0ull && vis[0] - i * CA_BLK >= CA_BLK && vis[1] - i * CA_BLK >= CA_BLK;
-          tmem_ld_wait();
-          if (!__all_sync(0xffffffffu, all)) {
+          // 32 keys at a time: what a whole unit takes in registers does not fit beside another CTA's
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t s_col = lane_addr + (uint32_t)(HD + sb * CA_BLK);
+            uint32_t sr[16];                                                // sr[4 c + 2 k + j]: row k, key 32 half + 8 c + 2 ql + j
+            tmem_ld16x32(s_col + (uint32_t)(half * 32), sr);
+            const uint32_t um = half ? masks[g % CA_RING].y : masks[g % CA_RING].x;
+            const int left0 = vis[0] - i * CA_BLK - half * 32, left1 = vis[1] - i * CA_BLK - half * 32;
+            const bool all = um == 0xffffffffu && left0 >= 32 && left1 >= 32;
+            tmem_ld_wait();
+            if (!__all_sync(0xffffffffu, all)) {
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int left = k ? left1 : left0;
+                uint32_t m = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u;
+                if (tree && left < 32 && mine[k]) {
+                  const uint32_t *t = a.tree + (long long)(s.row0 + (base + quad + 8 * k) / a.group) * 4;
+                  const int sh = -left, word = sh >> 5;                     // node of the first key; in front of the nodes: the bits come later
+                  const uint32_t w0 = word >= 0 && word < 4 ? t[word] : 0u, w1 = word >= -1 && word < 3 ? t[word + 1] : 0u;
+                  m |= __funnelshift_r(w0, w1, sh & 31);
+                }
+                m = (m & um) >> (2 * ql);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                  sr[4 * c + 2 * k] = m >> (8 * c) & 1u ? sr[4 * c + 2 * k] : 0xff800000u;
+                  sr[4 * c + 2 * k + 1] = m >> (8 * c) & 2u ? sr[4 * c + 2 * k + 1] : 0xff800000u;
+                }
+              }
+            }
+            float bm[2];
+            bool grow[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const int left = vis[k] - i * CA_BLK, npre = min(64, max(0, left));
-              unsigned long long m = npre >= 64 ? ~0ull : (1ull << npre) - 1ull;
-              if (tree && npre < 64 && mine[k]) {
-                const uint32_t *t = a.tree + (long long)(s.row0 + (base + quad + 8 * k) / a.group) * 4;
-                const unsigned long long mlo = t[0] | (unsigned long long)t[1] << 32, mhi = t[2] | (unsigned long long)t[3] << 32;
-                const int sh = -left;                                       // node of the unit's first key
-                if (sh < 0) m |= sh > -64 ? mlo << (-sh) : 0ull;
-                else if (sh < 64) m |= (mlo >> sh) | (sh ? mhi << (64 - sh) : 0ull);
-                else m |= sh < 128 ? mhi >> (sh - 64) : 0ull;
-              }
-              m = (m & um) >> (2 * ql);
-              const uint32_t v0 = (uint32_t)m, v1 = (uint32_t)(m >> 32);
+              float x = fmaxf(__uint_as_float(sr[2 * k]), __uint_as_float(sr[2 * k + 1]));
 #pragma unroll
-              for (int c = 0; c < 8; ++c) {
-                const uint32_t v = c < 4 ? v0 >> (8 * c) : v1 >> (8 * c - 32);
-                sr[4 * c + 2 * k] = v & 1u ? sr[4 * c + 2 * k] : 0xff800000u;
-                sr[4 * c + 2 * k + 1] = v & 2u ? sr[4 * c + 2 * k + 1] : 0xff800000u;
-              }
+              for (int c = 1; c < 4; ++c) x = fmaxf(x, fmaxf(__uint_as_float(sr[4 * c + 2 * k]), __uint_as_float(sr[4 * c + 2 * k + 1])));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+              bm[k] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2)) * scale;
+              grow[k] = mine[k] && bm[k] > m_ref[k] + CaType<T>::RESCALE;
             }
-          }
-          float bm[2];
-          bool grow[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float x = -INFINITY, y = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 8; ++c) { x = fmaxf(x, __uint_as_float(sr[4 * c + 2 * k])); y = fmaxf(y, __uint_as_float(sr[4 * c + 2 * k + 1])); }
-            x = fmaxf(x, y);
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-            bm[k] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2)) * scale;
-            grow[k] = mine[k] && bm[k] > m_ref[k] + CaType<T>::RESCALE && m_ref[k] != -INFINITY;
-          }
-          if (__any_sync(0xffffffffu, grow[0] || grow[1])) {
-            // the accumulator takes the new reference, behind the O of every earlier unit
-            wait(o_done + (g - 1) % SB, (uint32_t)((g - 1) / SB) & 1u);
-            tc_fence_after();
-            const float corr0 = grow[0] ? ex2(m_ref[0] - bm[0]) : 1.f, corr1 = grow[1] ? ex2(m_ref[1] - bm[1]) : 1.f;
+            if (__any_sync(0xffffffffu, grow[0] || grow[1])) {
+              // the accumulator, and the first half of P where this is the second, take the new reference, behind the O of every earlier unit
+              const float corr0 = grow[0] ? ex2(m_ref[0] - bm[0]) : 1.f, corr1 = grow[1] ? ex2(m_ref[1] - bm[1]) : 1.f;
+              if (i > 0) {
+                wait(o_done + (g - 1) % SB, (uint32_t)((g - 1) / SB) & 1u);
+                tc_fence_after();
 #pragma unroll 1
-            for (int c0 = 0; c0 < HD; c0 += 64) {
-              uint32_t o[32];
-              tmem_ld16x64(lane_addr + (uint32_t)c0, o);
-              tmem_ld_wait();
+                for (int c0 = 0; c0 < HD; c0 += 32) {
+                  uint32_t o[16];
+                  tmem_ld16x32(lane_addr + (uint32_t)c0, o);
+                  tmem_ld_wait();
 #pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * (c & 2 ? corr1 : corr0));
-              tmem_st16x64(lane_addr + (uint32_t)c0, o);
+                  for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * (c & 2 ? corr1 : corr0));
+                  tmem_st16x32f(lane_addr + (uint32_t)c0, o);
+                }
+                tmem_st_wait();
+              }
+              if (half) ca_rescale_p<T>(s_col, corr0, corr1);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float corr = k ? corr1 : corr0;
+                l2[k].x *= corr; l2[k].y *= corr; t2[k].x *= corr; t2[k].y *= corr;
+                if (grow[k]) m_ref[k] = bm[k];
+              }
             }
-            tmem_st_wait();
-            if (grow[0]) { l[0] *= corr0; l_true[0] *= corr0; m_ref[0] = bm[0]; }
-            if (grow[1]) { l[1] *= corr1; l_true[1] *= corr1; m_ref[1] = bm[1]; }
-          }
-          uint32_t p[16];
+            uint32_t p[8];
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if (m_ref[k] == -INFINITY) m_ref[k] = bm[k];
-            const float nbase = (m_ref[k] == -INFINITY ? 0.f : -m_ref[k]) + CaType<T>::SHIFT;
+            for (int k = 0; k < 2; ++k) {
+              const float nbase = (m_ref[k] == -INFINITY ? 0.f : -m_ref[k]) + CaType<T>::SHIFT;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              const float p0 = ex2(fmaf(__uint_as_float(sr[4 * c + 2 * k]), scale, nbase)), p1 = ex2(fmaf(__uint_as_float(sr[4 * c + 2 * k + 1]), scale, nbase));
-              p[2 * c + k] = pack2(p0, p1, T());
-              const float2 f = unpack2(p[2 * c + k], T());
-              l[k] += f.x + f.y;
-              l_true[k] += p0 + p1;
+              for (int c = 0; c < 4; ++c) {
+                const float2 d = ca_fma(make_float2(__uint_as_float(sr[4 * c + 2 * k]), __uint_as_float(sr[4 * c + 2 * k + 1])), make_float2(scale, scale), make_float2(nbase, nbase));
+                const float2 w = make_float2(ex2(d.x), ex2(d.y));
+                p[2 * c + k] = pack2(w.x, w.y, T());
+                l2[k] = ca_add(l2[k], unpack2(p[2 * c + k], T()));
+                t2[k] = ca_add(t2[k], w);
+              }
             }
+            tmem_st16x16(s_col + (uint32_t)(half * 16), p);
           }
-          tmem_st16x32(s_col, p);
           tmem_st_wait();
           tc_fence_before();
         }
@@ -312,6 +357,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (lane == 0) mbar_arrive(p_full + sb);
         if (++sb == SB) { sb = 0; sph ^= 1u; }
       }
+      float l[2] = {l2[0].x + l2[0].y, l2[1].x + l2[1].y}, l_true[2] = {t2[0].x + t2[0].y, t2[1].x + t2[1].y};
       // ---- epilogue
       const bool starts = s.b0 == 0, final = starts && !s.follow && (PAGES || !a.shared_tokens), row_on = !PAGES || s.seq >= 0;
       float inv[2];

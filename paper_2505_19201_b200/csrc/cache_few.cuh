@@ -79,7 +79,8 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ float red[4][NE];                                           // maxima of the warps
   __shared__ float2 sums[4][NE];                                         // their sums of weights
   __shared__ int e_vis[2][NE], e_row[2][NE];                           // of a segment's entries: what they see, their row
-  __shared__ long long e_at[2][NE];                                      // ... and row * heads + head
+  __shared__ void *e_to[NE];                                               // at its end: where O goes, the factor, the reference
+  __shared__ float e_inv[NE], refs[NE];
   static_assert(CA_RING > STAGES + CF_S + 1, "what the producer leaves is read until a unit's P is done");
   static_assert(sizeof(uint64_t) * (4 * STAGES + 2 * CF_S + 10 + CA_RING) + sizeof(uint4) * CA_RING + sizeof(CaSeg) * CA_RING + 8 <= 2048, "room for the barriers and rings");
 
@@ -92,7 +93,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const int i = lane - 8;
       mbar_init(p_full + i, 4); mbar_init(o_done + i, 1); mbar_init(o_free + i, 4); mbar_init(q_full + i, 1); mbar_init(q_empty + i, 1);
     } else if (lane >= 16) mbar_init(seg_full + lane - 16, 1);
-    if (lane == 12) { *abort_flag = 0; plan.partial = plan.seq = 0; plan.at = 0; sh_status[0] = sh_status[1] = 0; }
+    if (lane == 12) { *abort_flag = 0; plan.partial = 0; sh_status[0] = sh_status[1] = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 4 && lane == 0) {
@@ -246,7 +247,6 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         e_vis[ob][t] = vis;
         e_row[ob][t] = r;
-        e_at[ob][t] = (long long)r * a.heads + s.kvh * a.group + t % a.group;
       }
       if (cf_any(n <= 0)) break;                            // (whatever a wait of one warp came to, they all go on or all leave: barriers follow)
       int least = e_vis[ob][0];                             // what every entry sees
@@ -277,13 +277,19 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (!all) {
           const uint32_t mw = q == 0 ? um.x : q == 1 ? um.y : q == 2 ? um.z : um.w;
           there = has_key && (mw >> lane & 1u);
+          uint32_t sees = 0;
+          if (!tree) {
 #pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            const int behind = t + i * BLK - e_vis[ob][e];                  // node of the key, in a tree
-            bool sees = there && behind < 0;
-            if (tree && there && behind >= 0 && behind < 128 && e < n_e) sees = a.tree[(long long)e_row[ob][e] * 4 + (behind >> 5)] >> (behind & 31) & 1u;
-            x[e] = sees ? x[e] : -INFINITY;
+            for (int e = 0; e < NE; ++e) sees |= (uint32_t)(t + i * BLK < e_vis[ob][e]) << e;
+          } else {
+#pragma unroll 1
+            for (int e = 0; e < n_e; ++e) {
+              const int node = t + i * BLK - e_vis[ob][e];                  // of the key
+              if (node < 0 || (node < 128 && a.tree[(long long)e_row[ob][e] * 4 + (node >> 5)] >> (node & 31) & 1u)) sees |= 1u << e;
+            }
           }
+#pragma unroll
+          for (int e = 0; e < NE; ++e) x[e] = there && (sees >> e & 1u) ? x[e] : -INFINITY;
         }
         bool grow = false;
 #pragma unroll
@@ -371,10 +377,24 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         if (lane % (32 / NE) == 0) sums[q][lane / (32 / NE)] = make_float2(v[0], u[0]);
       }
+#pragma unroll
+      for (int e = 0; e < NE; ++e) if (t == e) refs[e] = m_ref[e];
       cf_sync();
-      const bool starts = s.b0 == 0, final = starts && !s.follow && (PAGES || !a.shared_tokens), row_on = !PAGES || s.seq >= 0;
-      const int follow = s.follow;
-      const long long phase_at = PAGES ? 0 : (long long)s.phase * a.rows * a.heads, cont_at = (long long)(a.cont_base + cta) * 128;
+      // a thread per entry: what the segment leaves of it, and where its O goes
+      const bool final = s.b0 == 0 && !s.follow && (PAGES || !a.shared_tokens);
+      if (t < n_e && t < NE) {
+        const float2 s0 = sums[0][t], s1 = sums[1][t], s2 = sums[2][t], s3 = sums[3][t];
+        const float sl = (s0.x + s1.x) + (s2.x + s3.x), st = (s0.y + s1.y) + (s2.y + s3.y), m = refs[t] == -INFINITY ? refs[t] : refs[t] - CaType<T>::SHIFT;
+        const int r = e_row[ob][t], h = s.kvh * a.group + t % a.group;
+        const bool starts = s.b0 == 0, row_on = !PAGES || s.seq >= 0;
+        const long long rh = (long long)r * a.heads + h, at = starts ? (PAGES ? rh : (long long)s.phase * a.rows * a.heads + rh) : (long long)(a.cont_base + cta) * 128 + t;
+        if (starts) {
+          a.part_ml[at] = make_float4(m, sl, st, pack_follow(t, final || !row_on ? CA_DONE : s.follow, a.cont_base + cta + 1));
+          if (final && row_on && a.lse) a.lse[rh] = sl > 0.f ? (m + log2f(st)) * 0.6931471805599453f : -INFINITY;
+        } else a.cont_ml[at] = make_float4(m, sl, st, 0.f);
+        e_to[t] = final ? (row_on ? (void *)((T *)a.out + r * a.out_ld + (long long)h * HD) : nullptr) : (void *)((starts ? a.part_o : a.cont_o) + at * HD);
+        e_inv[t] = sl > 0.f ? 1.f / sl : 0.f;
+      }
       wait(o_done + ((g - 1) & 1), (uint32_t)((g - 1) >> 1) & 1u);
       tc_fence_after();
       uint32_t o[Sh::MT][NE];
@@ -384,32 +404,19 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(o_free + ob);
+      cf_sync();
+      if (t < HD && ok) {
 #pragma unroll
-      for (int e = 0; e < NE; ++e)
-        if (e < n_e && ok) {
-          const float2 s0 = sums[0][e], s1 = sums[1][e], s2 = sums[2][e], s3 = sums[3][e];
-          const float sl = (s0.x + s1.x) + (s2.x + s3.x), st = (s0.y + s1.y) + (s2.y + s3.y), m = m_ref[e] == -INFINITY ? m_ref[e] : m_ref[e] - CaType<T>::SHIFT;
-          const long long rh = e_at[ob][e], at = starts ? phase_at + rh : cont_at + e;
-          if (t < HD) {
-            if (final) {
-              const float inv = sl > 0.f ? 1.f / sl : 0.f;
-              T *out = (T *)a.out + e_row[ob][e] * a.out_ld + (rh - (long long)e_row[ob][e] * a.heads) * HD;
-              if (row_on)
+        for (int e = 0; e < NE; ++e)
+          if (e < n_e) {
+            void *to = e_to[e];
 #pragma unroll
-                for (int mt = 0; mt < Sh::MT; ++mt) out[mt * 128 + t] = from_f<T>(__uint_as_float(o[mt][e]) * inv);
-            } else {
-              float *po = (starts ? a.part_o : a.cont_o) + at * HD;
-#pragma unroll
-              for (int mt = 0; mt < Sh::MT; ++mt) po[mt * 128 + t] = __uint_as_float(o[mt][e]);
+            for (int mt = 0; mt < Sh::MT; ++mt) {
+              if (!final) ((float *)to)[mt * 128 + t] = __uint_as_float(o[mt][e]);
+              else if (to) ((T *)to)[mt * 128 + t] = from_f<T>(__uint_as_float(o[mt][e]) * e_inv[e]);
             }
           }
-          if (t == e) {
-            if (starts) {
-              a.part_ml[at] = make_float4(m, sl, st, pack_follow(e, final || !row_on ? CA_DONE : follow, a.cont_base + cta + 1));
-              if (final && row_on && a.lse) a.lse[rh] = sl > 0.f ? (m + log2f(st)) * 0.6931471805599453f : -INFINITY;
-            } else a.cont_ml[at] = make_float4(m, sl, st, 0.f);
-          }
-        }
+      }
     }
     // the last O but one: nobody has waited for its arrival
     if (g > 1) wait(o_done + (g & 1), (uint32_t)((g - 2) >> 1) & 1u);

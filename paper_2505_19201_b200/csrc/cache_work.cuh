@@ -89,7 +89,10 @@ __device__ __forceinline__ int ca_seq_of(const CacheAttnArgs &a, int r) {
   return lo;
 }
 
-struct CaPlanShared { long long sum[32], at; int seq, partial; };      // partial, seq and at start as 0
+struct CaPlanShared { long long sum[32], at; CaSeq q; int seq, partial; };      // partial starts as 0
+
+// a / b for a from 0 and b from 1 on: a division of 64-bit numbers takes several times that of 32-bit ones, and hardly a call has as many units.
+__device__ __forceinline__ long long ca_div(long long a, int b) { return a >> 31 ? a / b : (long long)((int)a / b); }
 
 // What a CTA has to do: units [u, u_end) of the call, as segments.  Every item is reached from the one before it by counting on; lengths are read once per sequence.
 template <int BLK, bool PAGES> struct CaWalk {
@@ -108,16 +111,19 @@ template <int BLK, bool PAGES> struct CaWalk {
     s.row0 = q.q0 + tile * a.tile_rows; s.rows = min(a.tile_rows, q.n - tile * a.tile_rows);
     s.end = q.end(a, tile); s.tail0 = q.len - q.n; s.q0 = q.q0; s.kvh = 0;
   }
-  __device__ __forceinline__ void at_seq(const CacheAttnArgs &a, int seq) {               // ... the first tile of the first sequence from this one on that has rows
-    tiles = 0;
-    for (; seq < a.c.n_seqs; ++seq) {
-      q = CaSeq(a, seq);
-      if ((tiles = q.tiles(a)) > 0) break;
-    }
+  __device__ __forceinline__ void at_own(const CacheAttnArgs &a, int seq) {               // ... the first tile of this sequence
     s.phase = 1; s.seq = seq; s.key0 = a.shared_tokens;
     tile = 0;
+    tiles = q.tiles(a);
     if (tiles) at_tile(a);
     else u = u_end;                                          // (none: lengths that changed under way)
+  }
+  __device__ __forceinline__ void at_seq(const CacheAttnArgs &a, int seq) {               // ... of the first sequence from this one on that has rows
+    for (; seq < a.c.n_seqs; ++seq) {
+      q = CaSeq(a, seq);
+      if (q.n) break;
+    }
+    at_own(a, seq);
   }
   __device__ __forceinline__ void at_prefix(const CacheAttnArgs &a) {                     // shared keys: a tile of KV head s.kvh
     s.row0 = tile * a.tile_rows; s.rows = min(a.tile_rows, prefix_rows - tile * a.tile_rows);
@@ -160,6 +166,7 @@ template <int BLK, bool PAGES> struct CaWalk {
     if (PAGES) {
       blocks = max(1, (a.budget * a.c.page_tokens + BLK - 1) / BLK);
       total = (long long)a.rows * a.c.hkv * (blocks + CA_START);
+      upc = (int)max(1ll, ca_div(total + a.n_ctas - 1, a.n_ctas));
     } else {
       prefix_rows = min(max(a.q_start[a.c.n_seqs], 0), a.rows);
       prefix_blocks = (a.shared_tokens + BLK - 1) / BLK;
@@ -167,48 +174,50 @@ template <int BLK, bool PAGES> struct CaWalk {
       prefix_units = (long long)prefix_tiles * (prefix_blocks + CA_START) * a.c.hkv;
       // units in front of each sequence's, a sequence per thread at a time; once around for most batches, twice where there are more sequences than threads
       long long own = 0, sum = 0;
+      CaSeq t;
       for (int i = threadIdx.x; i < a.c.n_seqs; i += blockDim.x) {
-        const CaSeq t(a, i);
+        t = CaSeq(a, i);
         own = a.with_own ? t.template all_units<BLK>(a) : 0ll;
         sum += own;
         if (t.n && t.len - t.n + (a.tree ? 0 : 1) < a.shared_tokens) sh.partial = 1;       // a row that does not see the whole prefix
         if (cta == 0 && (t.q0 != a.q_start[i] || t.q0 + t.n != a.q_start[i + 1] || t.len != a.kv_len[i])) cache_bad_index(status);
       }
-      for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
+      for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += x; }
       if (lane == 31) sh.sum[warp] = sum;
       __syncthreads();
       total = prefix_units;
       long long before = prefix_units + sum - own;
       for (int i = 0; i < warps; ++i) { if (i < warp) before += sh.sum[i]; total += sh.sum[i]; }
       // the sequence in which the units behind the prefix start for this CTA
-      const long long per = max(1ll, (total + a.n_ctas - 1) / a.n_ctas), goal = max(min(cta * per, total), prefix_units);
+      upc = (int)max(1ll, ca_div(total + a.n_ctas - 1, a.n_ctas));
+      const long long goal = max(min((long long)cta * upc, total), prefix_units);
       if (a.c.n_seqs <= (int)blockDim.x) {
-        if (goal >= before && goal < before + own) { sh.seq = threadIdx.x; sh.at = before; }
+        if (goal >= before && goal < before + own) { sh.seq = threadIdx.x; sh.at = before; sh.q = t; }
       } else {
         long long next = prefix_units;
         for (int i0 = 0; i0 < a.c.n_seqs && next <= goal; i0 += blockDim.x) {
           const int i = i0 + threadIdx.x;
-          own = i < a.c.n_seqs && a.with_own ? CaSeq(a, i).template all_units<BLK>(a) : 0ll;
+          if (i < a.c.n_seqs) t = CaSeq(a, i);
+          own = i < a.c.n_seqs && a.with_own ? t.template all_units<BLK>(a) : 0ll;
           sum = own;
-          for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
+          for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += x; }
           __syncthreads();
           if (lane == 31) sh.sum[warp] = sum;
           __syncthreads();
           before = next + sum - own;
           for (int k = 0; k < warps; ++k) { if (k < warp) before += sh.sum[k]; next += sh.sum[k]; }
-          if (goal >= before && goal < before + own) { sh.seq = i; sh.at = before; }
+          if (goal >= before && goal < before + own) { sh.seq = i; sh.at = before; sh.q = t; }
         }
       }
       __syncthreads();
     }
-    upc = (int)max(1ll, (total + a.n_ctas - 1) / a.n_ctas);
     u_first = (long long)cta * upc;
     u = min(u_first, total);
     u_end = min(u + upc, total);
     if (u >= u_end) return;
     // ---- the item in which the range starts
     if (PAGES) {
-      const int i = (int)(u / (blocks + CA_START)), row = i / a.c.hkv;
+      const int i = (int)ca_div(u, blocks + CA_START), row = i / a.c.hkv;
       s.phase = 1; s.rows = 1;
       at_row(a, row);
       s.kvh = i - row * a.c.hkv;
@@ -222,7 +231,8 @@ template <int BLK, bool PAGES> struct CaWalk {
       at_prefix(a);
     } else {
       item = sh.at;
-      at_seq(a, sh.seq);
+      q = sh.q;
+      at_own(a, sh.seq);
       for (; tile < tiles; at_tile(a)) {                     // the tile, then the KV head
         const long long all = (long long)(blocks + CA_START) * a.c.hkv;
         if (u < item + all) break;
