@@ -221,7 +221,7 @@ extern "C" dream_status dream_cache_select(const dream_cache *cache, const void 
 }
 
 // Most CTAs of the two attention kernels together, each of which may continue an item.
-static int cache_slots(int hd) { return CACHE_MAX_SMS * (hd == 64 ? 4 : hd == 128 ? 3 : 2); }
+static int cache_slots(int hd) { return CACHE_MAX_SMS * (hd == 64 ? 3 : 2); }
 // The parts of the attention's workspace; how many bytes they are.
 static size_t cache_attn_room(const dream_cache *c, int n_heads, int rows, void *workspace, CacheAttnArgs *a) {
   const size_t n = 2 * (size_t)rows * n_heads, hd = c->head_dim;
@@ -292,21 +292,18 @@ static const char *cache_q_map(const dream_cache *c, const CacheAttnArgs &a, int
                    {128, hd * 2, a.group * hd * 2, (cuuint64_t)a.q_ld * 2}, {64, 1, (cuuint32_t)a.group, 1, (cuuint32_t)rows}, out);
 }
 // A kernel may use its shared memory on the current device from now on: once per device by a thread that calls again and again.  Returns the device's SMs, 0 with *e set
-// where something is wrong.  regs: registers per thread that the kernel counts on, or 0.
+// where something is wrong.
 template <typename... A>
-static int cache_allow(void (*kernel)(A...), size_t smem, int regs, cudaError_t *e) {
+static int cache_allow(void (*kernel)(A...), size_t smem, cudaError_t *e) {
   struct Ready { const void *kernel; int device, sms; };
   static thread_local Ready ready[16];
   static thread_local int next = 0;
   int device = 0, sms = 0;
   if ((*e = cudaGetDevice(&device)) != cudaSuccess) return 0;
   for (const Ready &r : ready) if (r.kernel == (const void *)kernel && r.device == device) return r.sms;
-  cudaFuncAttributes fa = {};
   *e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (*e == cudaSuccess) *e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (*e == cudaSuccess) *e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-  if (*e == cudaSuccess) *e = cudaFuncGetAttributes(&fa, kernel);
-  if (*e == cudaSuccess && regs && fa.numRegs != regs) *e = cudaErrorInvalidKernelImage;
   if (*e != cudaSuccess) return 0;
   if (sms > CACHE_MAX_SMS) sms = CACHE_MAX_SMS;
   ready[next] = {(const void *)kernel, device, sms};
@@ -317,18 +314,18 @@ static int cache_allow(void (*kernel)(A...), size_t smem, int regs, cudaError_t 
 template <typename T, int HD, bool PAGES>
 static const char *cache_attn_many(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
   cudaError_t e = cudaSuccess;
-  const int sms = cache_allow(k_cache_attn<T, HD, PAGES>, CaShape<HD>::SMEM, CaShape<HD>::SPLIT ? 80 : 0, &e);
+  const int sms = cache_allow(k_cache_attn<T, HD, PAGES>, CaShape<HD>::SMEM, &e);
   if (!sms) { cudaGetLastError(); return cudaGetErrorString(e); }
   CUtensorMap mk, mv, mq, ms;
   a.tile_rows = 128 / a.group;
-  const char *why = cache_kv_map(cache, a.c, a.c.k, CA_BLK, &mk);
-  if (!why) why = cache_kv_map(cache, a.c, a.c.v, CA_BLK, &mv);
+  const char *why = cache_kv_map(cache, a.c, a.c.k, CaShape<HD>::BLK, &mk);
+  if (!why) why = cache_kv_map(cache, a.c, a.c.v, CaShape<HD>::BLK, &mv);
   // a copy takes a whole tile of query entries, or 16 where a segment has no more
   a.q_small = a.group < 16 ? 16 / a.group : 1;
   if (!why) why = cache_q_map(cache, a, a.tile_rows, &mq);
   if (!why) why = cache_q_map(cache, a, a.q_small, &ms);
   if (why) return why;
-  a.n_ctas = sms * CaShape<HD>::CTAS_PER_SM;
+  a.n_ctas = sms;
   a.cont_base = 0;
   return cache_launch(k_cache_attn<T, HD, PAGES>, dim3(a.n_ctas), CA_THREADS, CaShape<HD>::SMEM, stream, mk, mv, mq, ms, a);
 }
@@ -337,7 +334,7 @@ template <typename T, int HD, int NE, bool PAGES>
 static const char *cache_attn_few(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
   using Sh = CfShape<HD>;
   cudaError_t e = cudaSuccess;
-  const int sms = cache_allow(k_cache_attn_few<T, HD, NE, PAGES>, Sh::SMEM, 0, &e);
+  const int sms = cache_allow(k_cache_attn_few<T, HD, NE, PAGES>, Sh::SMEM, &e);
   if (!sms) { cudaGetLastError(); return cudaGetErrorString(e); }
   CUtensorMap mk, mv, mq;
   a.tile_rows = NE / a.group;
@@ -346,7 +343,7 @@ static const char *cache_attn_few(const dream_cache *cache, CacheAttnArgs &a, cu
   if (!why) why = cache_q_map(cache, a, a.tile_rows, &mq);
   if (why) return why;
   a.n_ctas = sms * Sh::CTAS_PER_SM;
-  a.cont_base = CACHE_MAX_SMS * CaShape<HD>::CTAS_PER_SM;
+  a.cont_base = CACHE_MAX_SMS;
   return cache_launch(k_cache_attn_few<T, HD, NE, PAGES>, dim3(a.n_ctas), CF_THREADS, Sh::SMEM, stream, mk, mv, mq, a);
 }
 template <typename T, int HD, bool PAGES>
@@ -391,7 +388,7 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask; // Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item with their own keys, whose parts need not be put together.
   a.shared_tokens = (long long)rows * a.group >= 256LL * cache->n_seqs ? 0 : shared_pages * cache->page_tokens;
   // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits
-  const long long units = (long long)((cache->pages_per_seq * (long long)cache->page_tokens + CA_BLK - 1) / CA_BLK) * cache->n_kv_heads;
+  const long long units = (long long)((cache->pages_per_seq * (long long)cache->page_tokens + 63) / 64) * cache->n_kv_heads;
   if (units > 0x7fffffffLL || (shared_pages && (units * shared_pages / cache->pages_per_seq + cache->n_kv_heads) * ((rows + 128 / a.group - 1) / (128 / a.group)) > 0x7fffffffLL))
     return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows over sequences of %d pages in one call", who, rows, cache->pages_per_seq);
   const char *why = cache_attn_launch<false>(cache, a, (cudaStream_t)cuda_stream);

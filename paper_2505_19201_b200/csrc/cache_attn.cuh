@@ -3,32 +3,29 @@
 //
 // Where a tile has more than 16 query entries; for fewer see cache_few.cuh, and for how the work is dealt out cache_work.cuh.
 //
-// A segment.  S = Q K^T (128 x 64, fp32 in TMEM, two to four buffers), softmax by eight warps of 16 rows each, the four lanes of a quad to a row (and to the
-// one eight further on): one pass with a running reference m that follows the
-// row's maximum only when that has outgrown it (the accumulator is then rescaled, seldom), P = 2^(s - m) rounded to the cache's type into the columns
-// its scores came from, O += P V with P as the TMEM operand.  l sums the rounded P, so that the weights add up to 1 whatever their rounding, which
+// A segment.  S = Q K^T (128 x 128 keys, 64 at head_dim 256; fp32 in TMEM, two or three buffers), softmax by sixteen warps: a group of 16 rows has two, one for each half of the unit's
+// keys, and the four lanes of a quad share a row (and the one eight further on).  One pass with a running reference m that follows the
+// row's maximum only when that has outgrown it (the accumulator is then rescaled, seldom; whether it has is one barrier with a vote between the two warps), P = 2^(s - m)
+// rounded to the cache's type into the columns the scores came from, O += P V with P as the TMEM operand.  l sums the rounded P, so that the weights add up to 1 whatever their rounding, which
 // then moves the result by at most half a step of sum w |v - out|; the log-sum-exp has a sum of its own, of P as it was.  K and V come by TMA in two rings that
-// run on from segment to segment, so that the next one's keys are under way while one ends.  The producer alone works out what the segments are, ahead of
+// run on from segment to segment, so that the next one's keys are under way while one ends.  The producer of K alone says what the segments are, ahead of
 // everybody else, and leaves them in a ring in shared memory.
-// Warps: 0 K and segments, 1 Q, S and TMEM, 2 O, 3 V, 4..11 softmax and epilogue.  Two CTAs share an SM's registers: 80 for each thread, of which
-// the first four warps leave the others a part.
+// Warps: 0 K and segments, 1 Q, S and TMEM, 2 O, 3 V, 4..19 softmax and epilogue.
 #pragma once
 #include "attn_tc.cuh"
 #include "cache_work.cuh"
 
-#define CA_THREADS 384
-#define CA_WARPS (CA_THREADS / 32)
-#define CA_BLK 64                        // keys of a unit
+#define CA_SOFTMAX 16                    // softmax warps
+#define CA_THREADS (128 + 32 * CA_SOFTMAX)
 
 template <int HD> struct CaShape {
+  static constexpr int BLK = HD == 256 ? 64 : 128;                     // keys of a unit
   static constexpr int KP = HD / 64;                                   // 64-column panels of a row
   static constexpr int STAGES = HD == 64 ? 5 : 2;                      // units of K (and of V) in shared memory
-  static constexpr int S_BUFS = HD == 64 ? 3 : HD == 128 ? 2 : 4;      // what the TMEM columns hold beside O
-  static constexpr int TMEM_COLS = HD + S_BUFS * CA_BLK <= 256 ? 256 : 512;
-  static constexpr int CTAS_PER_SM = HD == 256 ? 1 : 2;                // one walks its keys while the other starts or ends a segment
+  static constexpr int S_BUFS = HD == 64 ? 3 : HD == 128 ? 3 : 4;      // what the 512 TMEM columns hold beside O
+  static constexpr int TMEM_COLS = 512;
   static constexpr int Q_BYTES = 128 * HD * 2, Q_PANEL = 128 * 128;
-  static constexpr int STAGE = CA_BLK * HD * 2, PANEL = CA_BLK * 128;
-  static constexpr bool SPLIT = CTAS_PER_SM == 2;                      // registers are moved between the warps: 4 x 32 x 64 + 8 x 32 x 88 = 384 x 80
+  static constexpr int STAGE = BLK * HD * 2, PANEL = BLK * 128;
   static constexpr size_t SMEM = 1024 + Q_BYTES + 2 * STAGES * STAGE + 2048;
 };
 
@@ -56,21 +53,6 @@ __device__ __forceinline__ void tmem_st16x32f(uint32_t taddr, const uint32_t (&r
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
         "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
-// The first half of a unit's P, already stored, times a factor for each of the two rows: powers that end below 1, rounded once more.
-template <typename T> __device__ __forceinline__ void ca_rescale_p(uint32_t s_col, float corr0, float corr1) {
-  uint32_t p[8];
-  tmem_st_wait();
-  asm volatile("tcgen05.ld.sync.aligned.16x128b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(p[0]), "=r"(p[1]), "=r"(p[2]), "=r"(p[3]), "=r"(p[4]), "=r"(p[5]), "=r"(p[6]), "=r"(p[7]) : "r"(s_col) : "memory");
-  tmem_ld_wait();
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    const float2 f = unpack2(p[c], T());
-    const float corr = c & 1 ? corr1 : corr0;
-    p[c] = pack2(f.x * corr, f.y * corr, T());
-  }
-  tmem_st16x16(s_col, p);
-}
 // Two at a time (an instruction for both).
 __device__ __forceinline__ float2 ca_add(float2 a, float2 b) {
   float2 r;
@@ -83,12 +65,20 @@ __device__ __forceinline__ float2 ca_fma(float2 a, float2 b, float2 c) {
   return r;
 }
 
+// The barrier of a pair of softmax warps, with and without a vote.
+__device__ __forceinline__ bool ca_any(int pair, bool mine) {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %2, 0;\n barrier.cta.red.or.pred q, %1, 64, p;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"(1 + pair), "r"((uint32_t)mine) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void ca_sync(int pair) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(1 + pair) : "memory"); }
+
 template <typename T, int HD, bool PAGES>
-__global__ void __launch_bounds__(CA_THREADS, (CaShape<HD>::CTAS_PER_SM))
+__global__ void __launch_bounds__(CA_THREADS, 1)
 k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q,
              const __grid_constant__ CUtensorMap map_q_small, const __grid_constant__ CacheAttnArgs a) {
   using Sh = CaShape<HD>;
-  constexpr int STAGES = Sh::STAGES, KP = Sh::KP, SB = Sh::S_BUFS;
+  constexpr int STAGES = Sh::STAGES, KP = Sh::KP, SB = Sh::S_BUFS, BLK = Sh::BLK;
   extern __shared__ uint8_t ca_smem_raw[];
   uint8_t *smem = (uint8_t *)(((uintptr_t)ca_smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t *q_s = smem, *k_s = q_s + Sh::Q_BYTES, *v_s = k_s + STAGES * Sh::STAGE;
@@ -101,14 +91,16 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   volatile int *abort_flag = (volatile int *)(tmem_base_p + 1);
   __shared__ CaPlanShared plan;
   __shared__ int sh_status[2];
+  __shared__ float pair_max[CA_SOFTMAX / 2][2][16];                        // what the halves of a pair tell each other: maxima of their rows ...
+  __shared__ float2 pair_sum[CA_SOFTMAX / 2][2][16];                       // ... and sums of weights
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, cta = blockIdx.x;
   unsigned long long *tr = trace_open();
   if (warp == 0) {
     if (lane < STAGES) { mbar_init(k_full + lane, 1); mbar_init(k_empty + lane, 1); mbar_init(v_full + lane, 1); mbar_init(v_empty + lane, 1); }
-    else if (lane >= 8 && lane < 8 + SB) { mbar_init(s_full + lane - 8, 1); mbar_init(p_full + lane - 8, 8); mbar_init(o_done + lane - 8, 1); }
+    else if (lane >= 8 && lane < 8 + SB) { mbar_init(s_full + lane - 8, 1); mbar_init(p_full + lane - 8, CA_SOFTMAX); mbar_init(o_done + lane - 8, 1); }
     else if (lane >= 16) mbar_init(seg_full + lane - 16, 1);
-    if (lane == 12) { mbar_init(q_full, 1); mbar_init(o_free, 8); *abort_flag = 0; }
+    if (lane == 12) { mbar_init(q_full, 1); mbar_init(o_free, CA_SOFTMAX); *abort_flag = 0; }
     else if (lane == 13) { plan.partial = 0; sh_status[0] = sh_status[1] = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -123,7 +115,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   static_assert(CA_RING == 16, "a lane inits each of the segments' barriers");
-  static_assert(CA_RING > STAGES + SB, "what the producer leaves is read until a unit's P is done");
+  static_assert(CA_RING > STAGES + SB + 1, "what the producer leaves is read until a unit's P is done");
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -131,7 +123,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   trace_stamp(tr, TR_k_cache_attn);
   int *status = a.status ? a.status : sh_status;
 
-  CaWalk<CA_BLK, PAGES> w;
+  CaWalk<BLK, PAGES> w;
   w.plan(a, plan, status);
   const uint32_t tmem_base = *tmem_base_p;
   int gave_up = WAIT_none;
@@ -141,17 +133,13 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     return segs[i % CA_RING].n;
   };
 
-  if (Sh::SPLIT) {
-    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
-  }
   if (warp == 0) {
-    gave_up = ca_produce<HD, CA_BLK, STAGES, 0, PAGES>(a, w, CaRing{k_full, k_empty, seg_full, k_s, masks, segs, &map_k, abort_flag, status}, lane);
+    gave_up = ca_produce<HD, BLK, STAGES, 0, PAGES>(a, w, CaRing{k_full, k_empty, seg_full, k_s, masks, segs, &map_k, abort_flag, status}, lane);
   } else if (warp == 3) {
-    gave_up = ca_produce<HD, CA_BLK, STAGES, 1, PAGES>(a, w, CaRing{v_full, v_empty, nullptr, v_s, nullptr, nullptr, &map_v, abort_flag, status}, lane);
+    gave_up = ca_produce<HD, BLK, STAGES, 1, PAGES>(a, w, CaRing{v_full, v_empty, nullptr, v_s, nullptr, nullptr, &map_v, abort_flag, status}, lane);
   } else if (warp == 1) {
     // ------------------------------------------------------------------ queries, and S = Q K^T: both operands K-major, N = 64
-    constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | ((uint32_t)(CA_BLK >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | ((uint32_t)(BLK >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     const uint64_t qd = smem_desc(smem_u32(q_s)), kd = smem_desc(smem_u32(k_s));
     const uint32_t s_addr = tmem_base + HD;
     const uint64_t pol = policy_evict_normal();
@@ -175,7 +163,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              mma_bf16(s_addr + (uint32_t)(sb * CA_BLK), qd + (uint64_t)((kp * Sh::Q_PANEL + k * 32) >> 4),
+              mma_bf16(s_addr + (uint32_t)(sb * BLK), qd + (uint64_t)((kp * Sh::Q_PANEL + k * 32) >> 4),
                        kd + (uint64_t)((ks * Sh::STAGE + kp * Sh::PANEL + k * 32) >> 4), idesc, (kp > 0 || k > 0) ? 1u : 0u);
           mma_commit(k_empty + ks);
           mma_commit(s_full + sb);
@@ -200,13 +188,16 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll 1
       for (int i = 0; i < n; ++i, ++g) {
         if (!__all_sync(0xffffffffu, mbar_wait(v_full + vs, vph, abort_flag) && mbar_wait(p_full + sb, pph, abort_flag))) { gave_up = WAIT_cache_p_v; break; }
-        const uint64_t m = masks[g % CA_RING].x | (uint64_t)masks[g % CA_RING].y << 32;
-        if (m != ~0ull) {
+        const uint4 m = masks[g % CA_RING];
+        if ((m.x & m.y & (BLK > 64 ? m.z & m.w : 0xffffffffu)) != 0xffffffffu) {
           // values that are nobody's may be anything, and 0 times that not 0
           uint8_t *dst = v_s + vs * Sh::STAGE;
 #pragma unroll 1
-          for (int j = lane; j < CA_BLK * KP * 8; j += 32)
-            if (!(m >> ((j >> 3) & (CA_BLK - 1)) & 1ull)) *reinterpret_cast<uint4 *>(dst + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+          for (int j = lane; j < BLK * KP * 8; j += 32)
+          {
+            const int key = (j >> 3) & (BLK - 1), word = key >> 5;
+            if (!((word == 0 ? m.x : word == 1 ? m.y : word == 2 ? m.z : m.w) >> (key & 31) & 1u)) *reinterpret_cast<uint4 *>(dst + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
           fence_proxy_async_smem();
           __syncwarp();
         }
@@ -214,8 +205,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (elect_one()) {
           const uint64_t bd = vd + (uint64_t)((vs * Sh::STAGE) >> 4);
 #pragma unroll
-          for (int k = 0; k < CA_BLK / 16; ++k)                             // 16 keys: eight columns of P, two groups of eight rows of V
-            mma_tmem_a(tmem_base, p_addr + (uint32_t)(sb * CA_BLK + k * 8), bd + (uint64_t)(k * 128), idesc, (i > 0 || k > 0) ? 1u : 0u);
+          for (int k = 0; k < BLK / 16; ++k)                             // 16 keys: eight columns of P, two groups of eight rows of V
+            mma_tmem_a(tmem_base, p_addr + (uint32_t)(sb * BLK + k * 8), bd + (uint64_t)(k * 128), idesc, (i > 0 || k > 0) ? 1u : 0u);
           mma_commit(v_empty + vs);
           mma_commit(o_done + sb);
         }
@@ -226,9 +217,10 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       if (gave_up) break;
     }
   } else if (warp >= 4) {
-    // ------------------------------------------------------------------ softmax and epilogue: warps 4..7 and 8..11 each take 16 lanes of a quarter; a
-    // lane has 16 of a unit's 64 keys for two rows of the tile, e[0] and e[1] = e[0] + 8
-    const int base = (warp & 3) * 32 + (warp >= 8 ? 16 : 0), quad = lane >> 2, ql = lane & 3;
+    // ------------------------------------------------------------------ softmax and epilogue: 16 rows of the tile have a warp for the first half of a unit's keys
+    // and one for the second; a lane has a quarter of the half's keys for two rows
+    constexpr int NC = BLK / 64;                            // runs of 32 keys in a half
+    const int ws = warp - 4, half = ws >> 3, pair = ws & 7, base = (warp & 3) * 32 + (ws & 4 ? 16 : 0), quad = lane >> 2, ql = lane & 3;
     const uint32_t lane_addr = tmem_base + ((uint32_t)base << 16);
     bool ok = true;
     auto wait = [&](uint64_t *bar, uint32_t parity) {                       // one lane polls for the warp
@@ -243,11 +235,13 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     const bool tree = !PAGES && a.tree;
     int g = 0, sb = 0;
     uint32_t sph = 0;
-    for (int seg = 0, n; (n = segment(seg, WAIT_cache_softmax)) > 0; ++seg) {
-      const CaSeg &s = segs[seg % CA_RING];              // read where it is needed: registers are short
+    for (int seg = 0;; ++seg) {
+      const int n = segment(seg, WAIT_cache_softmax);
+      if (ca_any(pair, n <= 0)) break;                      // (whatever a wait of one of the two came to, both go on or both leave: barriers follow)
+      const CaSeg &s = segs[seg % CA_RING];                 // read where it is needed: registers are short
       const int n_entries = s.rows * a.group;
       const bool active = base < n_entries, mine[2] = {base + quad < n_entries, base + quad + 8 < n_entries};
-      // a row sees the keys below vis (of the item's first, units counted from the segment's first), and in a tree its own ones as the mask has them
+      // a row sees the keys below vis (counted from this half of the segment's first unit), and in a tree its own ones as the mask has them
       int vis[2] = {0x7fffffff, 0x7fffffff};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -259,7 +253,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             tail0 = q.len - q.n;
             q0 = q.q0;
           }
-          vis[k] = tail0 + (tree ? 0 : r - q0 + 1) - (s.key0 + s.b0 * CA_BLK);
+          vis[k] = tail0 + (tree ? 0 : r - q0 + 1) - (s.key0 + s.b0 * BLK) - half * (BLK / 2);
         }
       }
       float m_ref[2] = {-INFINITY, -INFINITY};
@@ -270,20 +264,23 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         wait(s_full + sb, sph);
         if (active) {
           tc_fence_after();
-          // 32 keys at a time: what a whole unit takes in registers does not fit beside another CTA's
-#pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            const uint32_t s_col = lane_addr + (uint32_t)(HD + sb * CA_BLK);
-            uint32_t sr[16];                                                // sr[4 c + 2 k + j]: row k, key 32 half + 8 c + 2 ql + j
-            tmem_ld16x32(s_col + (uint32_t)(half * 32), sr);
-            const uint32_t um = half ? masks[g % CA_RING].y : masks[g % CA_RING].x;
-            const int left0 = vis[0] - i * CA_BLK - half * 32, left1 = vis[1] - i * CA_BLK - half * 32;
-            const bool all = um == 0xffffffffu && left0 >= 32 && left1 >= 32;
-            tmem_ld_wait();
-            if (!__all_sync(0xffffffffu, all)) {
+          const uint32_t s_col = lane_addr + (uint32_t)(HD + sb * BLK);
+          uint32_t sr[NC][16];                                              // sr[x][4 c + 2 k + j]: row k, key 32 x + 8 c + 2 ql + j of the half
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int left = k ? left1 : left0;
+          for (int x = 0; x < NC; ++x) tmem_ld16x32(s_col + (uint32_t)(half * (BLK / 2) + x * 32), sr[x]);
+          const uint4 um4 = masks[g % CA_RING];
+          uint32_t um[NC];
+          um[0] = NC == 2 ? (half ? um4.z : um4.x) : (half ? um4.y : um4.x);
+          if (NC == 2) um[NC - 1] = half ? um4.w : um4.y;
+          const int left0 = vis[0] - i * BLK, left1 = vis[1] - i * BLK;
+          const bool all = (um[0] & um[NC - 1]) == 0xffffffffu && left0 >= BLK / 2 && left1 >= BLK / 2;
+          tmem_ld_wait();
+          if (!__all_sync(0xffffffffu, all)) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int x = 0; x < NC; ++x) {
+                const int left = (k ? left1 : left0) - 32 * x;
                 uint32_t m = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u;
                 if (tree && left < 32 && mine[k]) {
                   const uint32_t *t = a.tree + (long long)(s.row0 + (base + quad + 8 * k) / a.group) * 4;
@@ -291,64 +288,71 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                   const uint32_t w0 = word >= 0 && word < 4 ? t[word] : 0u, w1 = word >= -1 && word < 3 ? t[word + 1] : 0u;
                   m |= __funnelshift_r(w0, w1, sh & 31);
                 }
-                m = (m & um) >> (2 * ql);
+                m = (m & um[x]) >> (2 * ql);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                  sr[4 * c + 2 * k] = m >> (8 * c) & 1u ? sr[4 * c + 2 * k] : 0xff800000u;
-                  sr[4 * c + 2 * k + 1] = m >> (8 * c) & 2u ? sr[4 * c + 2 * k + 1] : 0xff800000u;
+                  sr[x][4 * c + 2 * k] = m >> (8 * c) & 1u ? sr[x][4 * c + 2 * k] : 0xff800000u;
+                  sr[x][4 * c + 2 * k + 1] = m >> (8 * c) & 2u ? sr[x][4 * c + 2 * k + 1] : 0xff800000u;
                 }
               }
-            }
-            float bm[2];
-            bool grow[2];
+          }
+          float bm[2];
+          bool grow = false;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float x = -INFINITY;
+#pragma unroll
+            for (int y = 0; y < NC; ++y)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) x = fmaxf(x, fmaxf(__uint_as_float(sr[y][4 * c + 2 * k]), __uint_as_float(sr[y][4 * c + 2 * k + 1])));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            bm[k] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2)) * scale;
+            grow = grow || (mine[k] && bm[k] > m_ref[k] + CaType<T>::RESCALE);
+          }
+          // (and behind the vote both halves have their scores: P may take the columns of the first half's)
+          if (ca_any(pair, grow)) {
+            // the two halves' maxima; the accumulator takes the new reference, behind the O of every earlier unit, each half one half of its columns
+            if (ql == 0) { pair_max[pair][half][quad] = bm[0]; pair_max[pair][half][quad + 8] = bm[1]; }
+            ca_sync(pair);
+            float corr[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              float x = fmaxf(__uint_as_float(sr[2 * k]), __uint_as_float(sr[2 * k + 1]));
-#pragma unroll
-              for (int c = 1; c < 4; ++c) x = fmaxf(x, fmaxf(__uint_as_float(sr[4 * c + 2 * k]), __uint_as_float(sr[4 * c + 2 * k + 1])));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-              bm[k] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2)) * scale;
-              grow[k] = mine[k] && bm[k] > m_ref[k] + CaType<T>::RESCALE;
+              const float x = fmaxf(bm[k], pair_max[pair][half ^ 1][quad + 8 * k]);
+              const bool more = mine[k] && x > m_ref[k] + CaType<T>::RESCALE;
+              corr[k] = more ? ex2(m_ref[k] - x) : 1.f;
+              l2[k].x *= corr[k]; l2[k].y *= corr[k]; t2[k].x *= corr[k]; t2[k].y *= corr[k];
+              m_ref[k] = more ? x : m_ref[k];
             }
-            if (__any_sync(0xffffffffu, grow[0] || grow[1])) {
-              // the accumulator, and the first half of P where this is the second, take the new reference, behind the O of every earlier unit
-              const float corr0 = grow[0] ? ex2(m_ref[0] - bm[0]) : 1.f, corr1 = grow[1] ? ex2(m_ref[1] - bm[1]) : 1.f;
-              if (i > 0) {
-                wait(o_done + (g - 1) % SB, (uint32_t)((g - 1) / SB) & 1u);
-                tc_fence_after();
+            if (i > 0) {
+              wait(o_done + (g - 1) % SB, (uint32_t)((g - 1) / SB) & 1u);
+              tc_fence_after();
 #pragma unroll 1
-                for (int c0 = 0; c0 < HD; c0 += 32) {
-                  uint32_t o[16];
-                  tmem_ld16x32(lane_addr + (uint32_t)c0, o);
-                  tmem_ld_wait();
+              for (int c0 = half * (HD / 2); c0 < (half + 1) * (HD / 2); c0 += 32) {
+                uint32_t o[16];
+                tmem_ld16x32(lane_addr + (uint32_t)c0, o);
+                tmem_ld_wait();
 #pragma unroll
-                  for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * (c & 2 ? corr1 : corr0));
-                  tmem_st16x32f(lane_addr + (uint32_t)c0, o);
-                }
-                tmem_st_wait();
-              }
-              if (half) ca_rescale_p<T>(s_col, corr0, corr1);
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float corr = k ? corr1 : corr0;
-                l2[k].x *= corr; l2[k].y *= corr; t2[k].x *= corr; t2[k].y *= corr;
-                if (grow[k]) m_ref[k] = bm[k];
+                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * (c & 2 ? corr[1] : corr[0]));
+                tmem_st16x32f(lane_addr + (uint32_t)c0, o);
               }
             }
+          }
+#pragma unroll
+          for (int x = 0; x < NC; ++x) {
             uint32_t p[8];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               const float nbase = (m_ref[k] == -INFINITY ? 0.f : -m_ref[k]) + CaType<T>::SHIFT;
 #pragma unroll
               for (int c = 0; c < 4; ++c) {
-                const float2 d = ca_fma(make_float2(__uint_as_float(sr[4 * c + 2 * k]), __uint_as_float(sr[4 * c + 2 * k + 1])), make_float2(scale, scale), make_float2(nbase, nbase));
+                const float2 d = ca_fma(make_float2(__uint_as_float(sr[x][4 * c + 2 * k]), __uint_as_float(sr[x][4 * c + 2 * k + 1])), make_float2(scale, scale), make_float2(nbase, nbase));
                 const float2 w = make_float2(ex2(d.x), ex2(d.y));
                 p[2 * c + k] = pack2(w.x, w.y, T());
                 l2[k] = ca_add(l2[k], unpack2(p[2 * c + k], T()));
                 t2[k] = ca_add(t2[k], w);
               }
             }
-            tmem_st16x16(s_col + (uint32_t)(half * 16), p);
+            tmem_st16x16(s_col + (uint32_t)(half * (BLK / 4) + x * 16), p);
           }
           tmem_st_wait();
           tc_fence_before();
@@ -357,25 +361,35 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (lane == 0) mbar_arrive(p_full + sb);
         if (++sb == SB) { sb = 0; sph ^= 1u; }
       }
-      float l[2] = {l2[0].x + l2[0].y, l2[1].x + l2[1].y}, l_true[2] = {t2[0].x + t2[0].y, t2[1].x + t2[1].y};
-      // ---- epilogue
+      // ---- epilogue, each half one half of the columns
+      float l[2], l_true[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        l[k] = l2[k].x + l2[k].y;
+        l_true[k] = t2[k].x + t2[k].y;
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
+        l_true[k] += __shfl_xor_sync(0xffffffffu, l_true[k], 1);
+        l_true[k] += __shfl_xor_sync(0xffffffffu, l_true[k], 2);
+        if (ql == 0) pair_sum[pair][half][quad + 8 * k] = make_float2(l[k], l_true[k]);
+      }
+      ca_sync(pair);
       const bool starts = s.b0 == 0, final = starts && !s.follow && (PAGES || !a.shared_tokens), row_on = !PAGES || s.seq >= 0;
       float inv[2];
       long long at[2];
       int r[2], h[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
-        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
-        l_true[k] += __shfl_xor_sync(0xffffffffu, l_true[k], 1);
-        l_true[k] += __shfl_xor_sync(0xffffffffu, l_true[k], 2);
+        const float2 x = pair_sum[pair][0][quad + 8 * k], y = pair_sum[pair][1][quad + 8 * k];       // in this order in both
+        l[k] = x.x + y.x;
+        l_true[k] = x.y + y.y;
         inv[k] = l[k] > 0.f ? 1.f / l[k] : 0.f;
         const int e = base + quad + 8 * k;
         r[k] = s.row0 + e / a.group;
         h[k] = s.kvh * a.group + e % a.group;
         const long long rh = (long long)r[k] * a.heads + h[k];
         at[k] = starts ? (PAGES ? rh : (long long)s.phase * a.rows * a.heads + rh) : (long long)(a.cont_base + cta) * 128 + e;
-        if (mine[k] && ql == 0) {
+        if (mine[k] && ql == 0 && half == 0) {
           const float m = m_ref[k] == -INFINITY ? m_ref[k] : m_ref[k] - CaType<T>::SHIFT;
           if (starts) {
             a.part_ml[at[k]] = make_float4(m, l[k], l_true[k], pack_follow(e, final || !row_on ? CA_DONE : s.follow, a.cont_base + cta + 1));
@@ -387,30 +401,22 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       if (active && ok) {
         tc_fence_after();
 #pragma unroll 1
-        for (int c0 = 0; c0 < HD; c0 += 64) {
-          uint32_t o[32];                                                   // o[4 c + 2 k + j]: row k, column c0 + 8 c + 2 ql + j
-          tmem_ld16x64(lane_addr + (uint32_t)c0, o);
+        for (int c0 = half * (HD / 2); c0 < (half + 1) * (HD / 2); c0 += 32) {
+          uint32_t o[16];                                                   // o[4 c + 2 k + j]: row k, column c0 + 8 c + 2 ql + j
+          tmem_ld16x32(lane_addr + (uint32_t)c0, o);
           tmem_ld_wait();
-          if (final) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              T *out = (T *)a.out + (long long)r[k] * a.out_ld + (long long)h[k] * HD + c0;
+          for (int k = 0; k < 2; ++k) {
+            if (final) {
+              uint32_t z[4];
 #pragma unroll
-              for (int b = 0; b < 2; ++b) {
-                uint32_t z[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) z[c] = pack2(__uint_as_float(o[16 * b + 4 * c + 2 * k]) * inv[k], __uint_as_float(o[16 * b + 4 * c + 2 * k + 1]) * inv[k], T());
-                quad_transpose(z, lane);                                    // a lane now has eight columns that stand side by side
-                if (mine[k] && row_on) *reinterpret_cast<uint4 *>(out + 32 * b + 8 * ql) = make_uint4(z[0], z[1], z[2], z[3]);
-              }
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              if (!mine[k]) continue;
+              for (int c = 0; c < 4; ++c) z[c] = pack2(__uint_as_float(o[4 * c + 2 * k]) * inv[k], __uint_as_float(o[4 * c + 2 * k + 1]) * inv[k], T());
+              quad_transpose(z, lane);                                      // a lane now has eight columns that stand side by side
+              if (mine[k] && row_on) *reinterpret_cast<uint4 *>((T *)a.out + (long long)r[k] * a.out_ld + (long long)h[k] * HD + c0 + 8 * ql) = make_uint4(z[0], z[1], z[2], z[3]);
+            } else if (mine[k]) {
               float *po = (starts ? a.part_o : a.cont_o) + at[k] * HD + c0 + 2 * ql;
 #pragma unroll
-              for (int c = 0; c < 8; ++c) *reinterpret_cast<uint2 *>(po + 8 * c) = make_uint2(o[4 * c + 2 * k], o[4 * c + 2 * k + 1]);
+              for (int c = 0; c < 4; ++c) *reinterpret_cast<uint2 *>(po + 8 * c) = make_uint2(o[4 * c + 2 * k], o[4 * c + 2 * k + 1]);
             }
           }
         }
