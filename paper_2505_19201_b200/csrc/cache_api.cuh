@@ -130,20 +130,28 @@ extern "C" dream_status dream_cache_append(const dream_cache *cache, const void 
   a.q = q; a.q_ld = q_ld; a.k_new = k_new; a.k_ld = k_ld; a.v_new = v_new; a.v_ld = v_ld; a.q_out = q_out; a.q_out_ld = q_out_ld;
   a.row_seq = row_seq; a.slots = slots; a.positions = positions; a.rope = (const float2 *)rope; a.rows = rows; a.heads = q ? n_heads : 0; a.hd = hd;
   a.n_pos = n_pos; a.rot = rope ? rot_dim : 0; a.interleaved = interleaved != 0; a.status = status;
-  // Four units a thread where that fills the GPU; else one, so that more threads share the latency.
-  const long long units = (long long)rows * (a.heads + 2 * a.c.hkv) * (hd / 16);
-  const int deep = units >= 4LL * CACHE_THREADS * 148 * 4 ? 4 : 1;
-  const long long blocks = (units + CACHE_THREADS * deep - 1) / (CACHE_THREADS * deep);
+  // A thread takes one unit of one head where there are few rows, so that many share the latency; else that unit of several heads, whose rotary factors and place it looks up once.
+  const int per = CACHE_THREADS / (hd / 16), n_heads_all = a.heads + 2 * a.c.hkv;
+  const bool deep = (long long)rows * n_heads_all * (hd / 16) >= 4LL * CACHE_THREADS * 148 * 4;
+  a.head_lanes = deep ? 1 : per;
+  a.block_rows = per / a.head_lanes;
+  a.head_blocks = (n_heads_all + a.head_lanes * (deep ? APPEND_HEADS : 1) - 1) / (a.head_lanes * (deep ? APPEND_HEADS : 1));
+  a.bound_rows = 0;
+  int chunk_rows = a.block_rows;
+  a.bound_blocks = 0;
   if (a.c.bounds) {
-    // a block looks over so many rows for full pages: few where there are few rows, all of which may fill one at once
-    a.bound_rows = (int)((long long)rows * a.c.hkv / (148 * 4));
-    a.bound_rows = a.bound_rows < 1 ? 1 : a.bound_rows > 32 ? 32 : a.bound_rows;
-    a.bound_blocks = (rows + a.bound_rows - 1) / a.bound_rows * a.c.hkv;
+    // A block looks over so many rows for full pages (a power of two): few where there are few rows, all of which may fill one at once.
+    for (a.bound_rows = 1; a.bound_rows < 32 && (long long)rows * a.c.hkv >= 2LL * a.bound_rows * 148 * 4;) a.bound_rows *= 2;
+    if (a.bound_rows > chunk_rows) chunk_rows = a.bound_rows;
+    a.bound_blocks = chunk_rows / a.bound_rows * a.c.hkv;
   }
-  if (blocks + a.bound_blocks > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows of %d heads in one call", who, rows, a.heads);
-  void (*kernel)(CacheAppendArgs) = cache->dtype == DREAM_BF16 ? (deep > 1 ? k_cache_append<bf16, 4> : k_cache_append<bf16, 1>)
-                                                               : (deep > 1 ? k_cache_append<f16, 4> : k_cache_append<f16, 1>);
-  const char *why = cache_launch(kernel, dim3((unsigned)(blocks + a.bound_blocks)), CACHE_THREADS, 0, (cudaStream_t)cuda_stream, a);
+  a.chunk_rows = chunk_rows;
+  a.chunk_blocks = a.bound_blocks + chunk_rows / a.block_rows * a.head_blocks;
+  const long long blocks = (long long)((rows + chunk_rows - 1) / chunk_rows) * a.chunk_blocks;
+  if (blocks > 0x7fffffffLL) return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows of %d heads in one call", who, rows, a.heads);
+  void (*kernel)(CacheAppendArgs) = cache->dtype == DREAM_BF16 ? (deep ? k_cache_append<bf16, APPEND_HEADS> : k_cache_append<bf16, 1>)
+                                                               : (deep ? k_cache_append<f16, APPEND_HEADS> : k_cache_append<f16, 1>);
+  const char *why = cache_launch(kernel, dim3((unsigned)blocks), CACHE_THREADS, 0, (cudaStream_t)cuda_stream, a);
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
 }
 

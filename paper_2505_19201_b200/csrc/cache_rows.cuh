@@ -46,7 +46,9 @@ struct CacheAppendArgs {
   const int *row_seq, *slots, *positions;
   const float2 *rope;                      // [n_pos][rot / 2], or null (rot = 0 then)
   int rows, heads, hd, n_pos, rot, interleaved;
-  int bound_blocks, bound_rows;            // blocks that look for full pages, and rows of one of them
+  int chunk_rows, chunk_blocks;            // the grid: chunks of rows, the blocks of one
+  int bound_blocks, bound_rows;            // the first blocks of a chunk, which look for full pages, and rows of one of them
+  int head_lanes, block_rows, head_blocks; // of the others: threads of a row's unit, which take a head each at a time; rows of a block; blocks that share the heads
   int *status;
 };
 
@@ -57,17 +59,19 @@ __device__ __forceinline__ void append_unit(const CacheAppendArgs &a, int u, int
   ia = split ? u * 8 : u * 16;
   ib = split ? u * 8 + a.rot / 2 : u * 16 + 8;
 }
-// The rotation of unit u, in 32 bits, rounded once.
-template <typename T>
-__device__ __forceinline__ void append_rotate(const CacheAppendArgs &a, int u, int pos, uint4 &va, uint4 &vb) {
-  if (u * 16 >= a.rot) return;
+// The rotary factors of unit u at a position.
+__device__ __forceinline__ void append_factors(const CacheAppendArgs &a, int u, int pos, float (&cs)[16]) {
   const float4 *t = reinterpret_cast<const float4 *>(a.rope + (long long)pos * (a.rot / 2) + u * 8);
-  float x[8], y[8], cs[16];
 #pragma unroll
   for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(cs + 4 * i) = t[i];
+}
+// The rotation of a unit, in 32 bits, rounded once.
+template <typename T>
+__device__ __forceinline__ void append_rotate(bool interleaved, const float (&cs)[16], uint4 &va, uint4 &vb) {
+  float x[8], y[8];
   unpack8<T>(va, x);
   unpack8<T>(vb, y);
-  if (!a.interleaved) {
+  if (!interleaved) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float c = cs[2 * i], s = cs[2 * i + 1], p = x[i], q = y[i];
@@ -95,20 +99,18 @@ __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b, f16) { __ha
 // The bounds of one KV head of the page that row r fills, by a whole block: from the rows of this call (rotated once more: the same
 // values) and, for tokens that came earlier, from the cache.
 template <typename T>
-__device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, int kvh, int *from, uint32_t (*red)[CACHE_THREADS / 32][128], int *missing) {
+__device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, int kvh, int *from, uint32_t (*red)[CACHE_THREADS / 32][128]) {
   const int pt = a.c.page_tokens, seq = a.row_seq[r], slot = a.slots[r], first = slot - (pt - 1), tid = threadIdx.x, units = a.hd / 16;
   const int page = a.c.page(seq, slot >> a.c.page_shift);
   __syncthreads();                           // (the row before may still be read from)
-  if (tid == 0) *missing = 0;
-  __syncthreads();
+  int missing = 0;
   for (int t = tid; t < pt; t += CACHE_THREADS) {       // as a rule the rows of a sequence stand in order
     const int rr = r - (pt - 1) + t;
     const bool here = rr >= 0 && a.row_seq[rr] == seq && a.slots[rr] == first + t;
     from[t] = here ? rr : -1;                // -1: it is in the cache already
-    if (!here) *missing = 1;
+    missing |= !here;
   }
-  __syncthreads();
-  if (*missing) {
+  if (__syncthreads_or(missing)) {
     for (int rr = tid; rr < a.rows; rr += CACHE_THREADS)
       if (a.row_seq[rr] == seq && a.slots[rr] >= first && a.slots[rr] <= slot) from[a.slots[rr] - first] = rr;
     __syncthreads();
@@ -120,24 +122,34 @@ __device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, i
   const uint32_t plus = CaInf<T>::BITS * 0x10001u;         // two infinities
 #pragma unroll
   for (int i = 0; i < 8; ++i) { lo[i] = plus; hi[i] = plus | 0x80008000u; }
-  for (int t = tid / units; t < pt; t += groups) {
+  const auto load = [&](int t, uint4 &va, uint4 &vb) {
     const int rr = from[t];
-    uint4 va, vb;
-    if (rr >= 0) {
-      const int p = a.positions ? a.positions[rr] : first + t;
-      if (a.rot && (unsigned)p >= (unsigned)a.n_pos) continue;         // a row that is not written
-      const T *src = (const T *)a.k_new + rr * a.k_ld + (long long)kvh * a.hd;
-      va = *reinterpret_cast<const uint4 *>(src + ia);
-      vb = *reinterpret_cast<const uint4 *>(src + ib);
-      append_rotate<T>(a, u, p, va, vb);
-    } else {
-      const T *src = (const T *)a.c.k + a.c.at(page, kvh, t);
-      va = *reinterpret_cast<const uint4 *>(src + ia);
-      vb = *reinterpret_cast<const uint4 *>(src + ib);
-    }
-    const uint32_t w[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
+    const T *src = rr >= 0 ? (const T *)a.k_new + rr * a.k_ld + (long long)kvh * a.hd : (const T *)a.c.k + a.c.at(page, kvh, t);
+    va = *reinterpret_cast<const uint4 *>(src + ia);
+    vb = *reinterpret_cast<const uint4 *>(src + ib);
+  };
+  for (int t0 = tid / units; t0 < pt; t0 += 2 * groups) {
+    uint4 va[2], vb[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { lo[i] = min_pair(lo[i], w[i], T()); hi[i] = max_pair(hi[i], w[i], T()); }
+    for (int j = 0; j < 2; ++j) if (t0 + j * groups < pt) load(t0 + j * groups, va[j], vb[j]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int t = t0 + j * groups;
+      if (t >= pt) continue;
+      const int rr = from[t];
+      if (rr >= 0 && a.rot) {
+        const int p = a.positions ? a.positions[rr] : first + t;
+        if ((unsigned)p >= (unsigned)a.n_pos) continue;                // a row that is not written
+        if (u * 16 < a.rot) {
+          float cs[16];
+          append_factors(a, u, p, cs);
+          append_rotate<T>(a.interleaved, cs, va[j], vb[j]);
+        }
+      }
+      const uint32_t w[8] = {va[j].x, va[j].y, va[j].z, va[j].w, vb[j].x, vb[j].y, vb[j].z, vb[j].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { lo[i] = min_pair(lo[i], w[i], T()); hi[i] = max_pair(hi[i], w[i], T()); }
+    }
   }
   for (int o = units; o < 32; o <<= 1)
 #pragma unroll
@@ -162,18 +174,21 @@ __device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, i
   }
 }
 
-// Bound by HBM, or by latency where there are few rows.  Blocks from bound_blocks on move rows: a thread takes U units of the heads of consecutive rows (queries,
-// then keys, then values), whose loads are under way together; rows, positions and pages are looked up behind them.  The first
-// bound_blocks blocks look for rows that fill a page, a few rows and one KV head each.  One unit a thread and a block of 256 per row and part of it, 88 registers:
-// 5871 rows of 32 heads of 256 215 us.
-template <typename T, int U>
-__global__ void __launch_bounds__(CACHE_THREADS, U > 1 ? 3 : 4)
+// Bound by HBM, or by latency where there are few rows.  The grid is in chunks of rows.  The first blocks of a chunk look for rows that fill a page, a few rows and one
+// KV head each; the others move rows: a thread has one unit of a row and takes it from HEADS heads (queries, then keys, then values), two at a time; the row's place and
+// the unit's rotary factors it looks up once.  Measured with 5871 rows of 16 + 2 x 8 heads of 256, 193 MB: 42.9 us (4.5 TB/s), 37.5 of them without bounds; with 16 heads
+// a thread 46.2 (one and a quarter waves of blocks), with 4 heads 44.3 (more look-ups); with four units of any heads a thread, each with factors and divisions of its own,
+// 54; with all the blocks that look for pages at the grid's start, four times the rows take 155 us in place of 145 (their rows are read from HBM twice).
+#define APPEND_HEADS 8
+template <typename T, int HEADS>
+__global__ void __launch_bounds__(CACHE_THREADS, 4)
 k_cache_append(const __grid_constant__ CacheAppendArgs a) {
   kernel_entry(TR_k_cache_append);
-  if ((int)blockIdx.x < a.bound_blocks) {
-    __shared__ int from[256], missing;
+  const int chunk = blockIdx.x / a.chunk_blocks, at = blockIdx.x - chunk * a.chunk_blocks;
+  if (at < a.bound_blocks) {
+    __shared__ int from[256];
     __shared__ uint32_t red[2][CACHE_THREADS / 32][128];
-    const int kvh = blockIdx.x % a.c.hkv, r0 = blockIdx.x / a.c.hkv * a.bound_rows, lane = threadIdx.x & 31, pt = a.c.page_tokens;
+    const int kvh = at % a.c.hkv, r0 = chunk * a.chunk_rows + at / a.c.hkv * a.bound_rows, lane = threadIdx.x & 31, pt = a.c.page_tokens;
     // which of the rows fill a page: the same in every warp
     const int r = r0 + lane;
     bool fills = false;
@@ -181,59 +196,56 @@ k_cache_append(const __grid_constant__ CacheAppendArgs a) {
       const int seq = a.row_seq[r], slot = a.slots[r], pos = a.positions ? a.positions[r] : slot;
       fills = seq >= 0 && a.c.token_ok(seq, slot) && (slot & (pt - 1)) == pt - 1 && (!a.rot || (unsigned)pos < (unsigned)a.n_pos) && a.c.page(seq, slot >> a.c.page_shift) >= 0;
     }
-    for (unsigned left = __ballot_sync(0xffffffffu, fills); left; left &= left - 1) append_bounds<T>(a, r0 + __ffs(left) - 1, kvh, from, red, &missing);
+    for (unsigned left = __ballot_sync(0xffffffffu, fills); left; left &= left - 1) append_bounds<T>(a, r0 + __ffs(left) - 1, kvh, from, red);
     return;
   }
-  const int units = a.hd / 16, per_row = (a.heads + 2 * a.c.hkv) * units;
-  const long long first = (long long)(blockIdx.x - a.bound_blocks) * (CACHE_THREADS * U), row0 = first / per_row;
-  const unsigned off = (unsigned)(first - row0 * per_row) + threadIdx.x;
-  uint4 va[U], vb[U];
-  int row[U], hh[U], u[U], ia[U], ib[U];
+  const int units = a.hd / 16, block = at - a.bound_blocks, rows_at = block / a.head_blocks, part = block - rows_at * a.head_blocks;
+  const int u = threadIdx.x % units, rest = threadIdx.x / units, hl = rest % a.head_lanes;
+  const long long r = (long long)chunk * a.chunk_rows + rows_at * a.block_rows + rest / a.head_lanes;
+  if (r >= a.rows) return;
+  const int n_heads = a.heads + 2 * a.c.hkv, h0 = part * (a.head_lanes * HEADS) + hl;      // heads h0, h0 + head_lanes, ...
+  int ia, ib;
+  append_unit(a, u, ia, ib);
+  // where a head's unit comes from
+  const auto load = [&](int hh, uint4 &va, uint4 &vb) {
+    const bool is_v = hh >= a.heads + a.c.hkv;
+    const T *src = hh < a.heads ? (const T *)a.q + r * a.q_ld + (long long)hh * a.hd
+                   : !is_v ? (const T *)a.k_new + r * a.k_ld + (long long)(hh - a.heads) * a.hd
+                           : (const T *)a.v_new + r * a.v_ld + (long long)(hh - a.heads - a.c.hkv) * a.hd;
+    va = *reinterpret_cast<const uint4 *>(src + (is_v ? u * 16 : ia));                    // (values are not rotated: sixteen elements as they stand)
+    vb = *reinterpret_cast<const uint4 *>(src + (is_v ? u * 16 + 8 : ib));
+  };
+  constexpr int AT_ONCE = HEADS > 1 ? 2 : 1;
+  uint4 va[AT_ONCE], vb[AT_ONCE];
 #pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const unsigned i = off + j * CACHE_THREADS, rr = i / (unsigned)per_row, w = i - rr * (unsigned)per_row;
-    row[j] = (int)(row0 + rr);
-    hh[j] = (int)(w / (unsigned)units);
-    u[j] = (int)w - hh[j] * units;
-    ia[j] = u[j] * 16; ib[j] = ia[j] + 8;
-    if (hh[j] < a.heads + a.c.hkv) append_unit(a, u[j], ia[j], ib[j]);
-    if (row[j] < a.rows) {
-      const T *src = hh[j] < a.heads ? (const T *)a.q + row[j] * a.q_ld + (long long)hh[j] * a.hd
-                     : hh[j] < a.heads + a.c.hkv ? (const T *)a.k_new + row[j] * a.k_ld + (long long)(hh[j] - a.heads) * a.hd
-                                                 : (const T *)a.v_new + row[j] * a.v_ld + (long long)(hh[j] - a.heads - a.c.hkv) * a.hd;
-      va[j] = *reinterpret_cast<const uint4 *>(src + ia[j]);
-      vb[j] = *reinterpret_cast<const uint4 *>(src + ib[j]);
-    }
+  for (int j = 0; j < AT_ONCE; ++j) if (h0 + j * a.head_lanes < n_heads) load(h0 + j * a.head_lanes, va[j], vb[j]);
+  const int seq = a.row_seq[r], slot = a.slots[r], pos = a.positions ? a.positions[r] : slot;
+  if (seq < 0) return;
+  if (!a.c.token_ok(seq, slot) || (a.rot && (unsigned)pos >= (unsigned)a.n_pos)) {
+    if (u == 0) cache_bad_index(a.status);
+    return;
   }
-  int seq[U], slot[U], pos[U];
+  const int page = a.c.page(seq, slot >> a.c.page_shift);
+  const bool turn = u * 16 < a.rot;
+  float cs[16];
+  if (turn) append_factors(a, u, pos, cs);
+  if (page < 0 && u == 0 && hl == 0) cache_bad_index(a.status);
+#pragma unroll 1
+  for (int j0 = 0; j0 < HEADS; j0 += AT_ONCE) {
+    if (j0 > 0)
 #pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const bool on = row[j] < a.rows;
-    seq[j] = on ? a.row_seq[row[j]] : -1;
-    slot[j] = on ? a.slots[row[j]] : 0;
-    pos[j] = on && a.positions ? a.positions[row[j]] : slot[j];
-  }
+      for (int j = 0; j < AT_ONCE; ++j) if (h0 + (j0 + j) * a.head_lanes < n_heads) load(h0 + (j0 + j) * a.head_lanes, va[j], vb[j]);
 #pragma unroll
-  for (int j = 0; j < U; ++j) {
-    if (seq[j] < 0) continue;
-    if (!a.c.token_ok(seq[j], slot[j]) || (a.rot && (unsigned)pos[j] >= (unsigned)a.n_pos)) {
-      if (u[j] == 0) cache_bad_index(a.status);
-      continue;
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int hh = h0 + (j0 + j) * a.head_lanes;
+      if (hh >= n_heads || (hh >= a.heads && page < 0)) continue;
+      const bool is_v = hh >= a.heads + a.c.hkv;
+      T *dst = hh < a.heads ? (T *)a.q_out + r * a.q_out_ld + (long long)hh * a.hd
+                            : (T *)(is_v ? a.c.v : a.c.k) + a.c.at(page, hh - a.heads - (is_v ? a.c.hkv : 0), slot & (a.c.page_tokens - 1));
+      if (turn && !is_v) append_rotate<T>(a.interleaved, cs, va[j], vb[j]);
+      *reinterpret_cast<uint4 *>(dst + (is_v ? u * 16 : ia)) = va[j];
+      *reinterpret_cast<uint4 *>(dst + (is_v ? u * 16 + 8 : ib)) = vb[j];
     }
-    T *dst;
-    if (hh[j] < a.heads) dst = (T *)a.q_out + row[j] * a.q_out_ld + (long long)hh[j] * a.hd;
-    else {
-      const bool is_v = hh[j] >= a.heads + a.c.hkv;
-      const int page = a.c.page(seq[j], slot[j] >> a.c.page_shift);
-      if (page < 0) {
-        if (u[j] == 0) cache_bad_index(a.status);
-        continue;
-      }
-      dst = (T *)(is_v ? a.c.v : a.c.k) + a.c.at(page, hh[j] - a.heads - (is_v ? a.c.hkv : 0), slot[j] & (a.c.page_tokens - 1));
-    }
-    if (hh[j] < a.heads + a.c.hkv) append_rotate<T>(a, u[j], pos[j], va[j], vb[j]);
-    *reinterpret_cast<uint4 *>(dst + ia[j]) = va[j];
-    *reinterpret_cast<uint4 *>(dst + ib[j]) = vb[j];
   }
 }
 
