@@ -65,6 +65,11 @@ __device__ __forceinline__ float2 ca_fma(float2 a, float2 b, float2 c) {
   return r;
 }
 
+// Eight floats to a 32-byte boundary: even columns in x, odd ones in y.  (Four lanes store a whole line: in pieces of eight bytes a tile's partial result took 4000 cycles.)
+__device__ __forceinline__ void st_global8(float *p, const uint32_t (&x)[4], const uint32_t (&y)[4]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(x[0]), "r"(y[0]), "r"(x[1]), "r"(y[1]), "r"(x[2]), "r"(y[2]), "r"(x[3]), "r"(y[3]) : "memory");
+}
 // The barrier of a pair of softmax warps, with and without a vote.
 __device__ __forceinline__ bool ca_any(int pair, bool mine) {
   uint32_t r;
@@ -123,7 +128,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   trace_stamp(tr, TR_k_cache_attn);
   int *status = a.status ? a.status : sh_status;
 
-  CaWalk<BLK, PAGES> w;
+  CaWalk<BLK, 1, PAGES> w;
   w.plan(a, plan, status);
   const uint32_t tmem_base = *tmem_base_p;
   int gave_up = WAIT_none;
@@ -134,9 +139,9 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   };
 
   if (warp == 0) {
-    gave_up = ca_produce<HD, BLK, STAGES, 0, PAGES>(a, w, CaRing{k_full, k_empty, seg_full, k_s, masks, segs, &map_k, abort_flag, status}, lane);
+    gave_up = ca_produce<HD, STAGES, 0>(a, w, CaRing{k_full, k_empty, seg_full, k_s, masks, segs, &map_k, abort_flag, status}, lane);
   } else if (warp == 3) {
-    gave_up = ca_produce<HD, BLK, STAGES, 1, PAGES>(a, w, CaRing{v_full, v_empty, nullptr, v_s, nullptr, nullptr, &map_v, abort_flag, status}, lane);
+    gave_up = ca_produce<HD, STAGES, 1>(a, w, CaRing{v_full, v_empty, nullptr, v_s, nullptr, nullptr, &map_v, abort_flag, status}, lane);
   } else if (warp == 1) {
     // ------------------------------------------------------------------ queries, and S = Q K^T: both operands K-major, N = 64
     constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | ((uint32_t)(BLK >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -188,19 +193,6 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll 1
       for (int i = 0; i < n; ++i, ++g) {
         if (!__all_sync(0xffffffffu, mbar_wait(v_full + vs, vph, abort_flag) && mbar_wait(p_full + sb, pph, abort_flag))) { gave_up = WAIT_cache_p_v; break; }
-        const uint4 m = masks[g % CA_RING];
-        if ((m.x & m.y & (BLK > 64 ? m.z & m.w : 0xffffffffu)) != 0xffffffffu) {
-          // values that are nobody's may be anything, and 0 times that not 0
-          uint8_t *dst = v_s + vs * Sh::STAGE;
-#pragma unroll 1
-          for (int j = lane; j < BLK * KP * 8; j += 32)
-          {
-            const int key = (j >> 3) & (BLK - 1), word = key >> 5;
-            if (!((word == 0 ? m.x : word == 1 ? m.y : word == 2 ? m.z : m.w) >> (key & 31) & 1u)) *reinterpret_cast<uint4 *>(dst + j * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
         tc_fence_after();
         if (elect_one()) {
           const uint64_t bd = vd + (uint64_t)((vs * Sh::STAGE) >> 4);
@@ -262,13 +254,24 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll 1
       for (int i = 0; i < n; ++i, ++g) {
         wait(s_full + sb, sph);
+        const uint4 um4 = masks[g % CA_RING];
+        if ((um4.x & um4.y & (BLK > 64 ? um4.z & um4.w : 0xffffffffu)) != 0xffffffffu) {
+          // values that are nobody's may be anything, and 0 times that not 0: all the warps' lanes, some to a key
+          constexpr int LANES = 32 * CA_SOFTMAX / BLK;
+          const int key = (ws * 32 + lane) / LANES, word = key >> 5;
+          if (!((word == 0 ? um4.x : word == 1 ? um4.y : word == 2 ? um4.z : um4.w) >> (key & 31) & 1u) && mbar_wait(v_full + g % STAGES, (uint32_t)(g / STAGES) & 1u, abort_flag)) {
+            uint8_t *v = v_s + (g % STAGES) * Sh::STAGE + key * 128;
+#pragma unroll 1
+            for (int j = lane % LANES; j < KP * 8; j += LANES) *reinterpret_cast<uint4 *>(v + (j >> 3) * Sh::PANEL + (j & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+        }
         if (active) {
           tc_fence_after();
           const uint32_t s_col = lane_addr + (uint32_t)(HD + sb * BLK);
           uint32_t sr[NC][16];                                              // sr[x][4 c + 2 k + j]: row k, key 32 x + 8 c + 2 ql + j of the half
 #pragma unroll
           for (int x = 0; x < NC; ++x) tmem_ld16x32(s_col + (uint32_t)(half * (BLK / 2) + x * 32), sr[x]);
-          const uint4 um4 = masks[g % CA_RING];
           uint32_t um[NC];
           um[0] = NC == 2 ? (half ? um4.z : um4.x) : (half ? um4.y : um4.x);
           if (NC == 2) um[NC - 1] = half ? um4.w : um4.y;
@@ -407,16 +410,18 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           tmem_ld_wait();
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
+            uint32_t z[4], y[4];                                            // turned within the quad, a lane has eight columns that stand side by side
             if (final) {
-              uint32_t z[4];
 #pragma unroll
               for (int c = 0; c < 4; ++c) z[c] = pack2(__uint_as_float(o[4 * c + 2 * k]) * inv[k], __uint_as_float(o[4 * c + 2 * k + 1]) * inv[k], T());
-              quad_transpose(z, lane);                                      // a lane now has eight columns that stand side by side
+              quad_transpose(z, lane);
               if (mine[k] && row_on) *reinterpret_cast<uint4 *>((T *)a.out + (long long)r[k] * a.out_ld + (long long)h[k] * HD + c0 + 8 * ql) = make_uint4(z[0], z[1], z[2], z[3]);
-            } else if (mine[k]) {
-              float *po = (starts ? a.part_o : a.cont_o) + at[k] * HD + c0 + 2 * ql;
+            } else {
 #pragma unroll
-              for (int c = 0; c < 4; ++c) *reinterpret_cast<uint2 *>(po + 8 * c) = make_uint2(o[4 * c + 2 * k], o[4 * c + 2 * k + 1]);
+              for (int c = 0; c < 4; ++c) { z[c] = o[4 * c + 2 * k]; y[c] = o[4 * c + 2 * k + 1]; }
+              quad_transpose(z, lane);
+              quad_transpose(y, lane);
+              if (mine[k]) st_global8((starts ? a.part_o : a.cont_o) + at[k] * HD + c0 + 8 * ql, z, y);
             }
           }
         }

@@ -21,6 +21,7 @@
 #define CF_THREADS 256
 #define CF_N 16                          // entries of a tile: the N of the instructions
 #define CF_S 4                           // buffers of S
+#define CF_START 3                       // units that starting and ending an item is worth: 128 sequences of up to 1000 tokens, 32 heads of 64, with 1, 2, 3: 179, 154, 151 us
 
 template <int HD> struct CfShape {
   static constexpr int BLK = HD == 256 ? 64 : 128;                     // keys of a unit
@@ -111,7 +112,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   pdl_wait();
   trace_stamp(tr, TR_k_cache_attn);
   int *status = a.status ? a.status : sh_status;
-  CaWalk<BLK, PAGES> w;
+  CaWalk<BLK, CF_START, PAGES> w;
   w.plan(a, plan, status);
   const uint32_t tmem_base = *tmem_base_p, o_base = tmem_base + CF_S * CF_N;
   int gave_up = WAIT_none;
@@ -122,9 +123,9 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   };
 
   if (warp == 0) {
-    gave_up = ca_produce<HD, BLK, STAGES, 0, PAGES>(a, w, CaRing{k_full, k_empty, seg_full, k_s, masks, segs, &map_k, abort_flag, status}, lane);
+    gave_up = ca_produce<HD, STAGES, 0>(a, w, CaRing{k_full, k_empty, seg_full, k_s, masks, segs, &map_k, abort_flag, status}, lane);
   } else if (warp == 3) {
-    gave_up = ca_produce<HD, BLK, STAGES, 1, PAGES>(a, w, CaRing{v_full, v_empty, nullptr, v_s, nullptr, nullptr, &map_v, abort_flag, status}, lane);
+    gave_up = ca_produce<HD, STAGES, 1>(a, w, CaRing{v_full, v_empty, nullptr, v_s, nullptr, nullptr, &map_v, abort_flag, status}, lane);
   } else if (warp == 1) {
     // ------------------------------------------------------------------ queries, a segment ahead, and S^T = K Q^T
     constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | ((uint32_t)(CF_N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);

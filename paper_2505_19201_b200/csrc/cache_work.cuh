@@ -4,7 +4,7 @@
 // units of 64 or 128 keys.  Shared pages: the rows of all sequences stand together, in full tiles, so that the prefix is read once for all of them (once per
 // tile).  A sequence's own tokens: its rows, tile by tile.  Listed pages: one row.  The units of all items, one behind the other, are dealt out to
 // the CTAs in equal contiguous ranges, by arithmetic on the lengths that each CTA does for itself (they are on the device), so long contexts
-// with few rows fill the GPU and short ones do not leave a tail.  An item counts CA_START units more than it has, for what starting and ending it costs.  A
+// with few rows fill the GPU and short ones do not leave a tail.  An item counts START units more than it has, for what starting and ending it costs.  A
 // range is a few segments, each in one item.  A segment leaves (m, l, O) of its keys; k_cache_merge adds up the
 // segments of a row, always in the same order.  The segment that starts an item has its place by row and head, a CTA's continuation
 // of an item the CTA's own.
@@ -13,7 +13,6 @@
 #include "cache_rows.cuh"
 
 #define CA_RING 16                       // units' key masks, and segments, that are known at once: more than the stages and the buffers of S together
-#define CA_START 1                       // units that starting and ending an item is worth
 
 struct CacheAttnArgs {
   CacheView c;
@@ -65,9 +64,9 @@ struct CaSeq {
   // place in the partials in order.
   __device__ __forceinline__ int end(const CacheAttnArgs &a, int t) const { return a.tree ? len : max(0, len - n + min(n, (t + 1) * a.tile_rows)); }
   template <int BLK> __device__ __forceinline__ int units(const CacheAttnArgs &a, int t) const { return max(1, (end(a, t) - a.shared_tokens + BLK - 1) / BLK); }
-  template <int BLK> __device__ __forceinline__ long long all_units(const CacheAttnArgs &a) const {
+  template <int BLK, int START> __device__ __forceinline__ long long all_units(const CacheAttnArgs &a) const {
     long long sum = 0;
-    for (int t = tiles(a) - 1; t >= 0; --t) sum += units<BLK>(a, t) + CA_START;
+    for (int t = tiles(a) - 1; t >= 0; --t) sum += units<BLK>(a, t) + START;
     return sum * a.c.hkv;
   }
 };
@@ -95,8 +94,8 @@ struct CaPlanShared { long long sum[32], at; CaSeq q; int seq, partial; };      
 __device__ __forceinline__ long long ca_div(long long a, int b) { return a >> 31 ? a / b : (long long)((int)a / b); }
 
 // What a CTA has to do: units [u, u_end) of the call, as segments.  Every item is reached from the one before it by counting on; lengths are read once per sequence.
-template <int BLK, bool PAGES> struct CaWalk {
-  long long u, u_end, u_first, item;       // item: the first unit of the item at hand, which has CA_START + blocks
+template <int BLK, int START, bool PAGES> struct CaWalk {
+  long long u, u_end, u_first, item;       // item: the first unit of the item at hand, which has START + blocks
   int upc, blocks, tile, tiles;
   int prefix_tiles, prefix_blocks, prefix_rows;
   CaSeq q;
@@ -129,7 +128,7 @@ template <int BLK, bool PAGES> struct CaWalk {
     s.row0 = tile * a.tile_rows; s.rows = min(a.tile_rows, prefix_rows - tile * a.tile_rows);
   }
   __device__ __forceinline__ void next_item(const CacheAttnArgs &a) {
-    item += CA_START + blocks;
+    item += START + blocks;
     if (PAGES) {
       if (++s.kvh == a.c.hkv) at_row(a, s.row0 + 1);
     } else if (s.phase) {
@@ -145,12 +144,12 @@ template <int BLK, bool PAGES> struct CaWalk {
   // The next segment, in s.
   __device__ __forceinline__ bool next(const CacheAttnArgs &a) {
     while (u < u_end) {
-      if (u >= item + CA_START + blocks) { next_item(a); continue; }
-      // behind CA_START units that stand for the item's start; nothing where the range ends among them
-      s.b0 = max((int)(u - item) - CA_START, 0);
-      s.n = (int)min((long long)blocks, u_end - item - CA_START) - s.b0;
-      s.follow = (int)(item + CA_START + blocks - 1 - u_first) / upc;
-      u = min(u_end, item + CA_START + blocks);
+      if (u >= item + START + blocks) { next_item(a); continue; }
+      // behind START units that stand for the item's start; nothing where the range ends among them
+      s.b0 = max((int)(u - item) - START, 0);
+      s.n = (int)min((long long)blocks, u_end - item - START) - s.b0;
+      s.follow = (int)(item + START + blocks - 1 - u_first) / upc;
+      u = min(u_end, item + START + blocks);
       if (s.n > 0) return true;
     }
     s.n = 0;
@@ -165,19 +164,19 @@ template <int BLK, bool PAGES> struct CaWalk {
     s.key0 = s.seq = s.kvh = s.tail0 = s.q0 = 0;
     if (PAGES) {
       blocks = max(1, (a.budget * a.c.page_tokens + BLK - 1) / BLK);
-      total = (long long)a.rows * a.c.hkv * (blocks + CA_START);
+      total = (long long)a.rows * a.c.hkv * (blocks + START);
       upc = (int)max(1ll, ca_div(total + a.n_ctas - 1, a.n_ctas));
     } else {
       prefix_rows = min(max(a.q_start[a.c.n_seqs], 0), a.rows);
       prefix_blocks = (a.shared_tokens + BLK - 1) / BLK;
       prefix_tiles = prefix_blocks && a.with_prefix ? (prefix_rows + a.tile_rows - 1) / a.tile_rows : 0;
-      prefix_units = (long long)prefix_tiles * (prefix_blocks + CA_START) * a.c.hkv;
+      prefix_units = (long long)prefix_tiles * (prefix_blocks + START) * a.c.hkv;
       // units in front of each sequence's, a sequence per thread at a time; once around for most batches, twice where there are more sequences than threads
       long long own = 0, sum = 0;
       CaSeq t;
       for (int i = threadIdx.x; i < a.c.n_seqs; i += blockDim.x) {
         t = CaSeq(a, i);
-        own = a.with_own ? t.template all_units<BLK>(a) : 0ll;
+        own = a.with_own ? t.template all_units<BLK, START>(a) : 0ll;
         sum += own;
         if (t.n && t.len - t.n + (a.tree ? 0 : 1) < a.shared_tokens) sh.partial = 1;       // a row that does not see the whole prefix
         if (cta == 0 && (t.q0 != a.q_start[i] || t.q0 + t.n != a.q_start[i + 1] || t.len != a.kv_len[i])) cache_bad_index(status);
@@ -198,7 +197,7 @@ template <int BLK, bool PAGES> struct CaWalk {
         for (int i0 = 0; i0 < a.c.n_seqs && next <= goal; i0 += blockDim.x) {
           const int i = i0 + threadIdx.x;
           if (i < a.c.n_seqs) t = CaSeq(a, i);
-          own = i < a.c.n_seqs && a.with_own ? t.template all_units<BLK>(a) : 0ll;
+          own = i < a.c.n_seqs && a.with_own ? t.template all_units<BLK, START>(a) : 0ll;
           sum = own;
           for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += x; }
           __syncthreads();
@@ -217,30 +216,30 @@ template <int BLK, bool PAGES> struct CaWalk {
     if (u >= u_end) return;
     // ---- the item in which the range starts
     if (PAGES) {
-      const int i = (int)ca_div(u, blocks + CA_START), row = i / a.c.hkv;
+      const int i = (int)ca_div(u, blocks + START), row = i / a.c.hkv;
       s.phase = 1; s.rows = 1;
       at_row(a, row);
       s.kvh = i - row * a.c.hkv;
-      item = (long long)i * (blocks + CA_START);
+      item = (long long)i * (blocks + START);
     } else if (u < prefix_units) {
-      const int i = (int)u / (prefix_blocks + CA_START);
+      const int i = (int)u / (prefix_blocks + START);
       s.phase = 0; s.end = a.shared_tokens;
       blocks = prefix_blocks;
       s.kvh = i / prefix_tiles; tile = i - s.kvh * prefix_tiles;
-      item = (long long)i * (prefix_blocks + CA_START);
+      item = (long long)i * (prefix_blocks + START);
       at_prefix(a);
     } else {
       item = sh.at;
       q = sh.q;
       at_own(a, sh.seq);
       for (; tile < tiles; at_tile(a)) {                     // the tile, then the KV head
-        const long long all = (long long)(blocks + CA_START) * a.c.hkv;
+        const long long all = (long long)(blocks + START) * a.c.hkv;
         if (u < item + all) break;
         item += all;
         if (++tile == tiles) break;
       }
-      s.kvh = (int)(u - item) / (blocks + CA_START);
-      item += (long long)s.kvh * (blocks + CA_START);
+      s.kvh = (int)(u - item) / (blocks + START);
+      item += (long long)s.kvh * (blocks + START);
     }
   }
 };
@@ -254,8 +253,8 @@ __device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity) {
 
 // K (WHICH = 0) or V (1) of all units, by a warp of its own, with what goes with a unit and a segment for the others (WHICH = 0 alone).  Returns the wait that ran out.
 struct CaRing { uint64_t *full, *empty, *seg_full; uint8_t *data; uint4 *masks; CaSeg *segs; const CUtensorMap *map; volatile int *abort_flag; int *status; };
-template <int HD, int BLK, int STAGES, int WHICH, bool PAGES>
-__device__ __forceinline__ int ca_produce(const CacheAttnArgs &a, CaWalk<BLK, PAGES> &w, const CaRing &ring, int lane) {
+template <int HD, int STAGES, int WHICH, int BLK, int START, bool PAGES>
+__device__ __forceinline__ int ca_produce(const CacheAttnArgs &a, CaWalk<BLK, START, PAGES> &w, const CaRing &ring, int lane) {
   constexpr int KP = HD / 64, STAGE = BLK * HD * 2, PANEL = BLK * 128;
   const uint64_t pol = policy_evict_normal();
   const int sub = min(BLK, a.c.page_tokens), n_sub = BLK / sub;             // keys of one copy, copies of a unit
