@@ -365,6 +365,7 @@ static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cu
   a.with_prefix = a.shared_tokens > 0;
   if (!both || !own_few) why = cache_attn_many<T, HD, PAGES>(cache, a, stream);
   a.with_own = 1;
+  a.early = !both || !own_few;
   a.with_prefix = both && a.shared_tokens > 0;
   if (!why && own_few) {
     // up to four entries, on the average, take a quarter of the code and of the registers

@@ -215,7 +215,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     const int ws = warp - 4, half = ws >> 3, pair = ws & 7, base = (warp & 3) * 32 + (ws & 4 ? 16 : 0), quad = lane >> 2, ql = lane & 3;
     const uint32_t lane_addr = tmem_base + ((uint32_t)base << 16);
     bool ok = true;
-    auto wait = [&](uint64_t *bar, uint32_t parity) {                       // one lane polls for the warp
+    auto wait = [&](uint64_t *bar, uint32_t parity) {                       // one lane polls for the warp, where it has to wait at all (64 readers of 32768 keys, 64 wide: 92 -> 87 us)
+      if (__all_sync(0xffffffffu, ok && mbar_test(bar, parity))) return;
       int v = 1;
       if (lane == 0 && (!ok || !mbar_wait(bar, parity, abort_flag))) v = 0;
       if (!__shfl_sync(0xffffffffu, v, 0) && ok) {

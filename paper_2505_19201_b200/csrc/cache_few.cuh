@@ -109,7 +109,10 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  pdl_wait();
+  // Behind the launch of this call for full tiles there is nothing to wait for: that one has waited for all in front of it before it let this one start.  (64 readers of a
+  // prefix of 32768 keys, 64 wide: 226 -> 218 us.  Were this launch let start when the other one has begun, so that its CTAs follow those that leave one by one, it would
+  // be no faster, and questions on one image slower, 36.3 us in place of 35.2.)
+  if (!a.early) pdl_wait();
   trace_stamp(tr, TR_k_cache_attn);
   int *status = a.status ? a.status : sh_status;
   CaWalk<BLK, CF_START, PAGES> w;
@@ -216,7 +219,8 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     const int q = warp & 3, t = q * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
     bool ok = true;
-    auto wait = [&](uint64_t *bar, uint32_t parity, uint64_t *bar2 = nullptr, uint32_t parity2 = 0) {      // one lane polls for the warp
+    auto wait = [&](uint64_t *bar, uint32_t parity, uint64_t *bar2 = nullptr, uint32_t parity2 = 0) {      // one lane polls for the warp, where it has to wait at all
+      if (__all_sync(0xffffffffu, ok && mbar_test(bar, parity) && (!bar2 || mbar_test(bar2, parity2)))) return;
       int v = 1;
       if (lane == 0 && (!ok || !mbar_wait(bar, parity, abort_flag) || (bar2 && !mbar_wait(bar2, parity2, abort_flag)))) v = 0;
       if (!__shfl_sync(0xffffffffu, v, 0) && ok) {
@@ -424,6 +428,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
   if (gave_up && lane == 0) wait_expired(status, gave_up, abort_flag, -1);
   drain_if_aborted(abort_flag);
+  if (a.early) pdl_wait();                   // the end of this launch is the end of both
   pdl_trigger();
   tc_fence_before();
   __syncthreads();

@@ -32,6 +32,7 @@ struct CacheAttnArgs {
   float4 *cont_ml;
   int with_prefix, with_own;               // dense: which keys this launch takes, the shared ones, the rows' own, or both
   int n_ctas, cont_base, cont_slots;       // CTAs of this launch, where its continuations' slots start, and slots of all launches
+  int early;                               // the launch in front is the other one of this call, of which this one needs nothing
   int q_small;                             // query rows that the smaller of the two copies of Q takes
   int *status;
 };
