@@ -372,8 +372,11 @@ static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cu
     const bool four = a.group <= 4 && (PAGES || (long long)a.rows * a.group <= 4LL * a.c.n_seqs);
     why = four ? cache_attn_few<T, HD, 4, PAGES>(cache, a, stream) : cache_attn_few<T, HD, CF_N, PAGES>(cache, a, stream);
   }
-  const long long merge = (long long)a.rows * a.heads * (HD / 8);
-  return why ? why : cache_launch(k_cache_merge<T, HD, PAGES>, dim3((unsigned)((merge + 255) / 256)), 256, 0, stream, a);
+  // more (row, head)s than threads that merge them are resident at once: a CTA continues one item at most, so most of them are done already, unless each has two parts
+  const long long rh = (long long)a.rows * a.heads, per = 256 / (HD / 4);
+  a.look = (PAGES || !a.shared_tokens) && rh > 148 * 8 * per;
+  const long long blocks = a.look ? (rh + MERGE_LOOK - 1) / MERGE_LOOK : (rh + per - 1) / per;
+  return why ? why : cache_launch(k_cache_merge<T, HD, PAGES>, dim3((unsigned)blocks), 256, 0, stream, a);
 }
 template <bool PAGES>
 static const char *cache_attn_launch(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
