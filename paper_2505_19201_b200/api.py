@@ -318,19 +318,24 @@ class Cache:
         n, h, pt, d = k.shape
         self.k, self.v, self.page_table, self.bounds, self.device = k, v, page_table, bounds, dev
         b = _side("bounds", bounds, k.dtype, (n, h, 2, d), dev)
-        self.heads, self.dim, self.seqs = h, d, page_table.shape[0]
+        self.heads, self.dim, self.seqs, self.dtype = h, d, page_table.shape[0], k.dtype
         self.c = dream_cache(k.data_ptr(), v.data_ptr(), b, page_table.data_ptr(), k.stride(0), k.stride(1), k.stride(2), page_table.stride(0),
                              kind, n, pt, h, d, page_table.shape[0], page_table.shape[1])
         self.p = C.addressof(self.c)
 
     def rows(self, name, t, heads=None):
         """Address, elements from row to row, rows and heads of a tensor [rows, heads, head_dim] whose heads are consecutive."""
-        _need(name, t)
-        if t.dtype is not self.k.dtype or t.get_device() != self.device or t.dim() != 3:
-            _bad(f"{name} must be {self.k.dtype} [rows, heads, head_dim] on cuda:{self.device}")
-        (R, H, d), (ld, hs, es) = t.shape, t.stride()
+        if t is None:
+            _need(name, t)
+        shape = t.shape
+        if t.dtype is not self.dtype or len(shape) != 3 or t.get_device() != self.device:
+            _bad(f"{name} must be {self.dtype} [rows, heads, head_dim] on cuda:{self.device}")
+        R, H, d = shape
         if d != self.dim or (heads is not None and H != heads):
             _bad(f"{name} must have {'heads' if heads is None else heads} x {self.dim} elements in a row")
+        if t.is_contiguous():                        # (most are; a contiguous tensor's strides need not be asked for)
+            return t.data_ptr(), H * d, R, H
+        ld, hs, es = t.stride()
         if es != 1 or (hs != d and H > 1):
             _bad(f"{name} must have consecutive heads in a row")
         return t.data_ptr(), ld if R > 1 else H * d, R, H
