@@ -393,7 +393,8 @@ dream_status dream_distill_grad(const void *logits, int32_t dtype, int32_t rows,
  *            they are then; until then they are not looked at, so a page may be rewritten as often as drafted tokens are refused.
  *   rows, n_heads : at least 1 each; query head h reads KV head h / (n_heads / n_kv_heads); n_heads a multiple of n_kv_heads, at most 128 times it
  *   q, k_new, v_new, q_out, out : device, rows of heads x head_dim consecutive elements of the cache's dtype, `*_ld` elements from row to row (a multiple
- *            of 8, at least the row), 16-byte aligned: parts of a fused projection's rows will do
+ *            of 8, at least the row), 16-byte aligned: parts of a fused projection's rows will do.  What a call writes overlaps nothing that it reads
+ *            (but q_out may be q)
  *   workspace : device, 256-byte aligned, of the size that dream_cache_attn_bytes (dream_cache_select_bytes) says; what it holds does not
  *            outlive the call, and two calls that may run at the same time need one each (so do two captured graphs that may)
  *   status : device int32[2], zeroed by the caller once, or NULL.  Word 0 becomes 1 when a bounded wait in a kernel ran out (word 1: which), 2
@@ -414,7 +415,8 @@ typedef struct {
 dream_status dream_rope_table(float *table, int32_t n_pos, int32_t rot_dim, float theta, void *cuda_stream);
 
 /* Appends rows: row r is token slots[r] of sequence row_seq[r] (device int32 [rows]; a negative sequence is padding, its row is skipped).  Its queries are
- * rotated to q_out, its keys rotated into the cache, its values copied there.  The order of the rows is free; no sequence's slot comes twice.
+ * rotated to q_out, its keys rotated into the cache, its values copied there.  The order of the rows is free; no sequence's slot, and no token of a page,
+ * comes twice.
  *   q, q_out : n_heads x head_dim per row, or both NULL with n_heads = 0; q_out may be q itself (q_out_ld = q_ld then)
  *   rope : device float [n_pos][rot_dim / 2][2] as dream_rope_table makes it, or NULL (no rotation).  The first rot_dim channels of a head are rotated (a
  *            multiple of 16, at most head_dim): (a, b) -> (a cos - b sin, b cos + a sin), where a, b are channels i and i + rot_dim / 2, or with

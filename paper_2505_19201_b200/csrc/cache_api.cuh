@@ -3,6 +3,8 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <atomic>
+
 #include "cache_attn.cuh"
 #include "cache_few.cuh"
 #include "cache_rows.cuh"
@@ -274,13 +276,14 @@ static dream_status cache_attn_args(const char *who, const dream_cache *cache, C
 }
 // A tensor of five dimensions as the copies take it, 64 columns (128 bytes, swizzled) at a time.
 static const char *cache_map(int dtype, const void *base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4], const cuuint32_t (&box)[5], CUtensorMap *out) {
-  static PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
-  if (!encode) {
-    void *fn = nullptr;
+  static std::atomic<void *> found(nullptr);               // (by whichever thread comes first)
+  void *fn = found.load(std::memory_order_acquire);
+  if (!fn) {
     cudaDriverEntryPointQueryResult qr;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qr) != cudaSuccess || !fn) return "cuTensorMapEncodeTiled not available";
-    encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qr) != cudaSuccess || !fn) { cudaGetLastError(); return "cuTensorMapEncodeTiled not available"; }
+    found.store(fn, std::memory_order_release);
   }
+  const PFN_cuTensorMapEncodeTiled_v12000 encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
   const cuuint32_t step[5] = {1, 1, 1, 1, 1};
   const CUresult r = encode(out, dtype == DREAM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void *>(base), dims, strides, box,
                             step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -397,11 +400,13 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   if (!s) s = cache_ints(who, "tree_mask", tree_mask, false);
   if (s) return s;
   if (shared_pages < 0 || shared_pages > cache->pages_per_seq) return fail(nullptr, DREAM_E_ARG, "%s: shared_pages = %d outside 0..pages_per_seq = %d", who, shared_pages, cache->pages_per_seq);
-  a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask; // Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item with their own keys, whose parts need not be put together.
+  a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask;
+  // Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item with their own keys, whose parts need not be put together.
   a.shared_tokens = (long long)rows * a.group >= 256LL * cache->n_seqs ? 0 : shared_pages * cache->page_tokens;
-  // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits
-  const long long units = (long long)((cache->pages_per_seq * (long long)cache->page_tokens + 63) / 64) * cache->n_kv_heads;
-  if (units > 0x7fffffffLL || (shared_pages && (units * shared_pages / cache->pages_per_seq + cache->n_kv_heads) * ((rows + 128 / a.group - 1) / (128 / a.group)) > 0x7fffffffLL))
+  // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits (with what an item's start counts)
+  auto units = [&](long long n_pages) { return (n_pages * cache->page_tokens / 64 + 1 + CF_START) * cache->n_kv_heads; };
+  const int tile = (long long)rows * a.group <= CF_N ? 1 : 128 / a.group;               // rows of one, at least
+  if (units(cache->pages_per_seq) > 0x7fffffffLL || (shared_pages && units(shared_pages) * ((rows + tile - 1) / tile) > 0x7fffffffLL))
     return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows over sequences of %d pages in one call", who, rows, cache->pages_per_seq);
   const char *why = cache_attn_launch<false>(cache, a, (cudaStream_t)cuda_stream);
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;

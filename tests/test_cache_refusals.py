@@ -98,6 +98,15 @@ def test_selection_needs_bounds_and_has_room_for_so_many_pages():
     assert all(call(None) == E_ARG for call in CALLS)
 
 
+@pytest.mark.parametrize("over,rows", [(dict(page_tokens=256, pages_per_seq=1 << 22, n_kv_heads=64), 16), (dict(page_tokens=256, pages_per_seq=1 << 22, n_kv_heads=128), 1),
+                                       (dict(page_tokens=16, pages_per_seq=1 << 23, n_kv_heads=2), 1 << 20)])
+def test_work_that_is_not_counted_in_32_bits(over, rows):
+    """A prefix of so many keys in so many tiles; a table may well name one page over and over."""
+    h = over["n_kv_heads"]
+    c = cache(**over, table_stride=1 << 23, head_stride=256 * 128, page_stride=256 * 128 * h)
+    assert attn(c, heads=h, q_ld=h * 128, out_ld=h * 128, rows=rows, out=1 << 50, shared=over["pages_per_seq"], n=1 << 60) == E_CAPACITY
+
+
 def test_strides_that_nothing_steps_along_do_not_count():
     n = C.c_size_t()
     for ok in (dict(n_pages=1, page_stride=0), dict(n_kv_heads=1, head_stride=-5), dict(n_seqs=1, table_stride=0), dict(page_stride=128, token_stride=50 * 128, head_stride=64 * 50 * 128)):
