@@ -132,9 +132,10 @@ extern "C" dream_status dream_cache_append(const dream_cache *cache, const void 
   a.q = q; a.q_ld = q_ld; a.k_new = k_new; a.k_ld = k_ld; a.v_new = v_new; a.v_ld = v_ld; a.q_out = q_out; a.q_out_ld = q_out_ld;
   a.row_seq = row_seq; a.slots = slots; a.positions = positions; a.rope = (const float2 *)rope; a.rows = rows; a.heads = q ? n_heads : 0; a.hd = hd;
   a.n_pos = n_pos; a.rot = rope ? rot_dim : 0; a.interleaved = interleaved != 0; a.status = status;
-  // A thread takes one unit of one head where there are few rows, so that many share the latency; else that unit of several heads, whose rotary factors and place it looks up once.
+  // A thread takes one unit of one head where there are few rows, so that many share the latency; else that unit of several heads, whose rotary factors and place it looks up
+  // once.  (32 + 2 x 8 heads of 128, with bounds, one head or several: 512 rows 9.1 or 9.3 us, 1024 rows 13.3 or 10.9, 3200 rows 32.6 or 19.4.)
   const int per = CACHE_THREADS / (hd / 16), n_heads_all = a.heads + 2 * a.c.hkv;
-  const bool deep = (long long)rows * n_heads_all * (hd / 16) >= 4LL * CACHE_THREADS * 148 * 4;
+  const bool deep = (long long)rows * n_heads_all * (hd / 16) >= 2LL * CACHE_THREADS * 148 * 4;
   a.head_lanes = deep ? 1 : per;
   a.block_rows = per / a.head_lanes;
   a.head_blocks = (n_heads_all + a.head_lanes * (deep ? APPEND_HEADS : 1) - 1) / (a.head_lanes * (deep ? APPEND_HEADS : 1));
@@ -340,28 +341,29 @@ static const char *cache_attn_many(const dream_cache *cache, CacheAttnArgs &a, c
   a.cont_base = 0;
   return cache_launch(k_cache_attn<T, HD, PAGES>, dim3(a.n_ctas), CA_THREADS, CaShape<HD>::SMEM, stream, mk, mv, mq, ms, a);
 }
-// Tiles of up to NE.
-template <typename T, int HD, int NE, bool PAGES>
+// Tiles of up to CF_ENTRIES.
+template <typename T, int HD, bool PAGES>
 static const char *cache_attn_few(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
   using Sh = CfShape<HD>;
   cudaError_t e = cudaSuccess;
-  const int sms = cache_allow(k_cache_attn_few<T, HD, NE, PAGES>, Sh::SMEM, &e);
+  const int sms = cache_allow(k_cache_attn_few<T, HD, PAGES>, Sh::SMEM, &e);
   if (!sms) { cudaGetLastError(); return cudaGetErrorString(e); }
   CUtensorMap mk, mv, mq;
-  a.tile_rows = NE / a.group;
+  a.tile_rows = CF_ENTRIES / a.group;
   const char *why = cache_kv_map(cache, a.c, a.c.k, Sh::BLK, &mk);
   if (!why) why = cache_kv_map(cache, a.c, a.c.v, Sh::BLK, &mv);
   if (!why) why = cache_q_map(cache, a, a.tile_rows, &mq);
   if (why) return why;
   a.n_ctas = sms * Sh::CTAS_PER_SM;
   a.cont_base = CACHE_MAX_SMS;
-  return cache_launch(k_cache_attn_few<T, HD, NE, PAGES>, dim3(a.n_ctas), CF_THREADS, Sh::SMEM, stream, mk, mv, mq, a);
+  return cache_launch(k_cache_attn_few<T, HD, PAGES>, dim3(a.n_ctas), CF_THREADS, Sh::SMEM, stream, mk, mv, mq, a);
 }
 template <typename T, int HD, bool PAGES>
 static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
-  // A sequence's rows, or a listed row, have 16 entries or fewer (on the average: how many each has is on the device, and more go tile by tile); the shared keys meet all rows.
-  const bool own_few = a.group <= CF_N && (PAGES || (long long)a.rows * a.group <= (long long)CF_N * a.c.n_seqs);
-  const bool shared_few = (long long)a.rows * a.group <= CF_N, both = PAGES || !a.shared_tokens || shared_few == own_few;
+  // A sequence's rows, or a listed row, have four entries or fewer (on the average: how many each has is on the device, and more go tile by tile); the shared keys meet all rows.
+  // Both sides: at the kernel for few.
+  const bool own_few = a.group <= CF_ENTRIES && (PAGES || (long long)a.rows * a.group <= (long long)CF_ENTRIES * a.c.n_seqs);
+  const bool shared_few = (long long)a.rows * a.group <= CF_ENTRIES, both = PAGES || !a.shared_tokens || shared_few == own_few;
   const char *why = nullptr;
   a.cont_slots = cache_slots(HD);
   a.with_own = both || !own_few;
@@ -370,12 +372,9 @@ static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cu
   a.with_own = 1;
   a.early = !both || !own_few;
   a.with_prefix = both && a.shared_tokens > 0;
-  if (!why && own_few) {
-    // up to four entries, on the average, take a quarter of the code and of the registers
-    const bool four = a.group <= 4 && (PAGES || (long long)a.rows * a.group <= 4LL * a.c.n_seqs);
-    why = four ? cache_attn_few<T, HD, 4, PAGES>(cache, a, stream) : cache_attn_few<T, HD, CF_N, PAGES>(cache, a, stream);
-  }
-  // more (row, head)s than threads that merge them are resident at once: a CTA continues one item at most, so most of them are done already, unless each has two parts
+  if (!why && own_few) why = cache_attn_few<T, HD, PAGES>(cache, a, stream);
+  // More (row, head)s than threads that merge them are resident at once: a CTA continues one item at most, so most of them are done already, unless each has two parts.  (Seven
+  // sequences of 500 rows behind 4096 tokens 297 us, without the look 325; of 128 rows 90 and 88.)
   const long long rh = (long long)a.rows * a.heads, per = 256 / (HD / 4);
   a.look = (PAGES || !a.shared_tokens) && rh > 148 * 8 * per;
   const long long blocks = a.look ? (rh + MERGE_LOOK - 1) / MERGE_LOOK : (rh + per - 1) / per;
@@ -401,11 +400,13 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   if (s) return s;
   if (shared_pages < 0 || shared_pages > cache->pages_per_seq) return fail(nullptr, DREAM_E_ARG, "%s: shared_pages = %d outside 0..pages_per_seq = %d", who, shared_pages, cache->pages_per_seq);
   a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask;
-  // Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item with their own keys, whose parts need not be put together.
+  // Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item with their own keys, whose parts need not be put together.  (Seven
+  // sequences behind 4096 tokens, 16 heads over 8 of 256, with 128 rows each 90 us, and 110 with the prefix by itself; with 64 rows 61 and 64, but their last tiles are full, which at
+  // other lengths they are not; with 32 rows 46 and 40.)
   a.shared_tokens = (long long)rows * a.group >= 256LL * cache->n_seqs ? 0 : shared_pages * cache->page_tokens;
   // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits (with what an item's start counts)
   auto units = [&](long long n_pages) { return (n_pages * cache->page_tokens / 64 + 1 + CF_START) * cache->n_kv_heads; };
-  const int tile = (long long)rows * a.group <= CF_N ? 1 : 128 / a.group;               // rows of one, at least
+  const int tile = (long long)rows * a.group <= CF_ENTRIES ? CF_ENTRIES / a.group : 128 / a.group;     // rows of one
   if (units(cache->pages_per_seq) > 0x7fffffffLL || (shared_pages && units(shared_pages) * ((rows + tile - 1) / tile) > 0x7fffffffLL))
     return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows over sequences of %d pages in one call", who, rows, cache->pages_per_seq);
   const char *why = cache_attn_launch<false>(cache, a, (cudaStream_t)cuda_stream);

@@ -1,7 +1,7 @@
 // Attention over a paged cache that a program holds itself, on the tcgen05 tensor cores: a ragged batch whose sequences may begin with the
 // same pages (dream_cache_attn), and rows that read listed pages (dream_cache_attn_pages).
 //
-// Where a tile has more than 16 query entries; for fewer see cache_few.cuh, and for how the work is dealt out cache_work.cuh.
+// Where a tile has more than four query entries; for fewer see cache_few.cuh, and for how the work is dealt out cache_work.cuh.
 //
 // A segment.  S = Q K^T (128 x 128 keys, 64 at head_dim 256; fp32 in TMEM, two or three buffers), softmax by sixteen warps: a group of 16 rows has two, one for each half of the unit's
 // keys, and the four lanes of a quad share a row (and the one eight further on).  One pass with a running reference m that follows the

@@ -1,9 +1,10 @@
-// Attention over a paged cache for few query entries per item (up to 16: a token of one sequence and its KV head's group, listed pages, a small batch on a
-// shared prefix), on the tcgen05 tensor cores.  How the work is dealt out: cache_work.cuh.
+// Attention over a paged cache for up to four query entries per item (a token of one sequence and its KV head's group, a listed row), on the tcgen05 tensor
+// cores.  How the work is dealt out: cache_work.cuh.
 //
-// The keys stand on the matrix instruction's long side:  S^T = K Q^T  (keys x 16), O^T += V^T P^T  (head_dim x 16).  Then every lane of every softmax warp has a key, a few
-// entries each, and nothing is computed for rows that are not there; with the entries on the long side (cache_attn.cuh) one warp in eight had all
-// of a unit's softmax, 1.6k to 2k cycles of latency for 64 keys, and a sequence of 64 tokens took 8k cycles from start to end.
+// The keys stand on the matrix instruction's long side:  S^T = K Q^T  (keys x 16), O^T += V^T P^T  (head_dim x 16).  Then every lane of every softmax warp has a key, four
+// entries each, and nothing is computed for rows that are not there.  Against the kernel with the entries on the long side (cache_attn.cuh), whose two softmax warps of sixteen rows
+// have all there is to do: 64 sequences of 2000 tokens, 32 heads over 8 of 128 wide, 88 us and 92; 12 heads of 64, 70 and 102; 16 over 8 of 256, 172 and 170; one of 833 tokens, 32
+// heads of 128, 12.5 and 13.9.  A form for up to 16 entries lost to the other kernel: 28 over 4 heads of 128 65 us against 53, 32 over 2 43 against 33, 24 over 3 of 64 38 against 35.
 //   S^T   tcgen05.mma 128 x 16 x 16 over head_dim, A = the unit's keys and B = Q, both K-major; fp32 in TMEM, a ring of four 16-column buffers
 //   softmax   four warps, a key per thread: P = 2^(s - m) with a running reference m per entry, the same in all threads.  Whether some score has outgrown its reference
 //         by more than a power of two is one barrier with a vote per unit; only then (in the first unit of a segment, and seldom later) the maxima are taken, across lanes and warps, and
@@ -19,7 +20,8 @@
 #include "cache_work.cuh"
 
 #define CF_THREADS 256
-#define CF_N 16                          // entries of a tile: the N of the instructions
+#define CF_ENTRIES 4                     // entries of a tile at most
+#define CF_N 16                          // the N of the instructions: no fewer
 #define CF_S 4                           // buffers of S
 #define CF_START 3                       // units that starting and ending an item is worth: 128 sequences of up to 1000 tokens, 32 heads of 64, with 1, 2, 3: 179, 154, 151 us
 
@@ -41,28 +43,21 @@ __device__ __forceinline__ bool cf_any(bool mine) {                    // ... of
   asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"((uint32_t)mine) : "memory");
   return r != 0;
 }
-// So many columns of a warp's 32 lanes, a lane to a thread.
-__device__ __forceinline__ void cf_ld(uint32_t taddr, uint32_t (&r)[16]) { tmem_ld16(taddr, r); }
+// Four columns of a warp's 32 lanes, a lane to a thread.
 __device__ __forceinline__ void cf_ld(uint32_t taddr, uint32_t (&r)[4]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void cf_st(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
-                 "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 __device__ __forceinline__ void cf_st(uint32_t taddr, const uint32_t (&r)[4]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 __device__ __forceinline__ void cf_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
 
-// NE: entries of a tile at most.
-template <typename T, int HD, int NE, bool PAGES>
+template <typename T, int HD, bool PAGES>
 __global__ void __launch_bounds__(CF_THREADS, (CfShape<HD>::CTAS_PER_SM))
 k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q,
                  const __grid_constant__ CacheAttnArgs a) {
   using Sh = CfShape<HD>;
-  constexpr int STAGES = Sh::STAGES, KP = Sh::KP, BLK = Sh::BLK;
+  constexpr int STAGES = Sh::STAGES, KP = Sh::KP, BLK = Sh::BLK, NE = CF_ENTRIES;
   extern __shared__ uint8_t cf_smem_raw[];
   uint8_t *smem = (uint8_t *)(((uintptr_t)cf_smem_raw + 1023) & ~(uintptr_t)1023);
   // V in front of K in front of Q: what an instruction reads past its rows (see above) is there
@@ -335,8 +330,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (has_key) {
           uint8_t *p = p_s + pb * Sh::P_BYTES + p_row;
 #pragma unroll
-          for (int e = 0; e < NE; ++e)
-            if (NE <= 4 || e < n_e) {
+          for (int e = 0; e < NE; ++e) {
               const float w_true = ex2(fmaf(x[e], scale, (m_ref[e] == -INFINITY ? 0.f : -m_ref[e]) + CaType<T>::SHIFT));
               const T w = from_f<T>(w_true);
               *reinterpret_cast<T *>(p + e * 128 + ((p_chunk ^ (e & 7)) << 4)) = w;

@@ -1,6 +1,6 @@
 // How the work of the attention over a paged cache is dealt out, and how its parts come together again.
 //
-// Work.  An item is a tile of query entries (entry = (row, query head of one KV-head group)), up to 128 or up to 16 by kernel, against a run of keys of one KV head, cut into
+// Work.  An item is a tile of query entries (entry = (row, query head of one KV-head group)), up to 128 or up to 4 by kernel, against a run of keys of one KV head, cut into
 // units of 64 or 128 keys.  Shared pages: the rows of all sequences stand together, in full tiles, so that the prefix is read once for all of them (once per
 // tile).  A sequence's own tokens: its rows, tile by tile.  Listed pages: one row.  The units of all items, one behind the other, are dealt out to
 // the CTAs in equal contiguous ranges, by arithmetic on the lengths that each CTA does for itself (they are on the device), so long contexts
