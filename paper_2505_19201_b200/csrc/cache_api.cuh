@@ -160,10 +160,10 @@ extern "C" dream_status dream_cache_append(const dream_cache *cache, const void 
 
 // The parts of the selection's workspace; how many bytes they are.
 static size_t cache_select_room(const CacheView &v, int hd, int rows, void *workspace, CacheSelectArgs *a) {
-  // Blocks of the scores for each (row, KV head): as many as fill the GPU, three to an SM, and no more than there are pages for
+  // Blocks of the scores for each (row, KV head): as many as fill the GPU, and no more than there are pages for
   const long long n = (long long)rows * v.hkv;
-  const int block = CACHE_THREADS / 32 * (32 / (hd / 8)) * SCORE_DEEP, most = (v.pages_per_seq + block - 1) / block;
-  const long long share = 148 * 3 / n;
+  const int most = (v.pages_per_seq + SCORE_PAGES - 1) / SCORE_PAGES;
+  const long long share = 148 * SCORE_BLOCKS / n;
   const int blocks = share < 1 ? 1 : share < most ? (int)share : most;
   const size_t scores = ((size_t)n * v.pages_per_seq * sizeof(float) + 255) / 256 * 256;
   if (a) { a->scores = (float *)workspace; a->off = (float *)((char *)workspace + scores); a->score_blocks = blocks; }
@@ -185,9 +185,7 @@ static const char *cache_select_run(const CacheSelectArgs &a, int rows, cudaStre
   const char *why = nullptr;
   size_t smem = 0;
   if (a.c.pages_per_seq > a.budget) {
-    // as many heads of the group at a time as it has, up to four
-    void (*kernel)(CacheSelectArgs) = a.group == 1 ? k_cache_scores<T, HD, 1> : a.group == 2 ? k_cache_scores<T, HD, 2> : k_cache_scores<T, HD, 4>;
-    why = cache_launch(kernel, dim3(rows * a.c.hkv, a.score_blocks), CACHE_THREADS, 0, stream, a);
+    why = cache_launch(k_cache_scores<T, HD>, dim3(rows * a.c.hkv, a.score_blocks), CACHE_THREADS, 0, stream, a);
     smem = (size_t)a.c.pages_per_seq * sizeof(uint32_t);      // of as many pages as a sequence may have
   }
   if (!why && smem > 32 * 1024) {
@@ -406,7 +404,7 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   a.shared_tokens = (long long)rows * a.group >= 256LL * cache->n_seqs ? 0 : shared_pages * cache->page_tokens;
   // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits (with what an item's start counts)
   auto units = [&](long long n_pages) { return (n_pages * cache->page_tokens / 64 + 1 + CF_START) * cache->n_kv_heads; };
-  const int tile = (long long)rows * a.group <= CF_ENTRIES ? CF_ENTRIES / a.group : 128 / a.group;     // rows of one
+  const int tile = 128 / a.group;                          // rows of one (CF_ENTRIES or fewer are one tile in either kernel)
   if (units(cache->pages_per_seq) > 0x7fffffffLL || (shared_pages && units(shared_pages) * ((rows + tile - 1) / tile) > 0x7fffffffLL))
     return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows over sequences of %d pages in one call", who, rows, cache->pages_per_seq);
   const char *why = cache_attn_launch<false>(cache, a, (cudaStream_t)cuda_stream);

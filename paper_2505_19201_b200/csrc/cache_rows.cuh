@@ -275,155 +275,6 @@ __device__ __forceinline__ float order_value(uint32_t k) { return __uint_as_floa
 __device__ __forceinline__ int select_pages(const CacheSelectArgs &a, int seq, int pos) {
   return seq >= 0 && pos >= 0 && a.c.token_ok(seq, pos) ? (pos >> a.c.page_shift) + 1 : 0;
 }
-// Scores in 32 bits, with a bound on how far they are off.  (Which pages are kept is a matter of the scores in 64 bits, but only for the few near the cut, which
-// k_cache_select looks at again; in 64 bits for all, a score took four times the instructions, and 64 rows of 1024 pages 20 us.)  HD / 8 lanes take a page, eight
-// channels each; a warp has SCORE_DEEP pages per lane under way at a time, and GC heads of the group: a lane has SCORE_DEEP * GC partial sums,
-// which are added up across the lanes by halves, each step with half as many of them, and then compared.
-// The bound: a sum is eight fused steps in a lane and up to five additions across lanes, each wrong by 2^-24 of a partial sum, which is no larger than
-// sum |q_d| times the largest bound there is; one more such error for the rounding of the exact score, and three for the bound's own.
-#define SCORE_DEEP 4
-template <typename T> __device__ __forceinline__ float2 widen2(uint32_t w);
-template <> __device__ __forceinline__ float2 widen2<bf16>(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-template <> __device__ __forceinline__ float2 widen2<f16>(uint32_t w) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
-
-template <typename T, int HD, int GC>
-__global__ void __launch_bounds__(CACHE_THREADS, 3)
-k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
-  constexpr int LANES = HD / 8, PAGES = 32 / LANES, NV = SCORE_DEEP * GC, BLOCK = CACHE_THREADS / 32 * PAGES * SCORE_DEEP;
-  constexpr int LEFT = NV > LANES ? NV / LANES : 1, STEPS = NV > LANES ? LANES : NV;
-  __shared__ float4 q_s[GC][2][LANES];                      // a lane's eight channels of a head
-  __shared__ uint4 m_s[GC][LANES];                          // and where they are negative: a mask for each pair
-  __shared__ uint32_t top_s[CACHE_THREADS / 32];
-  __shared__ float q1_s;
-  kernel_entry(TR_k_cache_scores);
-  const int r = blockIdx.x / a.c.hkv, kvh = blockIdx.x % a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LANES, end = n - a.keep_last;
-  if (n <= a.budget) return;                               // all are kept
-  const T *q0 = (const T *)a.q + r * a.q_ld + (long long)kvh * a.group * HD;
-  float *scores = a.scores + (long long)blockIdx.x * a.c.pages_per_seq;
-  uint32_t top = 0u;                                       // the largest magnitudes met, a pair
-  int page[SCORE_DEEP];                                    // of the pages ahead; -1: not asked for, -2: no number
-  const auto look_up = [&](int base) {
-#pragma unroll
-    for (int j = 0; j < SCORE_DEEP; ++j) {
-      const int p = base + warp * PAGES * SCORE_DEEP + lane / LANES + j * PAGES;         // pages p0, p0 + PAGES, ...
-      page[j] = -1;
-      if (p >= a.keep_first && p < end) {
-        page[j] = a.c.page(seq, p);
-        if (page[j] < 0) { page[j] = -2; cache_bad_index(a.status); }
-      }
-    }
-  };
-  look_up(blockIdx.y * BLOCK);
-  if (threadIdx.x == 0) q1_s = 0.f;
-  for (int base = blockIdx.y * BLOCK; base < end; base += gridDim.y * BLOCK) {
-    const int p0 = base + warp * PAGES * SCORE_DEEP + lane / LANES;
-    uint4 lo[SCORE_DEEP], hi[SCORE_DEEP];
-    unsigned bad = 0, on = 0;                              // pages without a number, pages of this row: bit j
-#pragma unroll
-    for (int j = 0; j < SCORE_DEEP; ++j) {
-      lo[j] = hi[j] = make_uint4(0u, 0u, 0u, 0u);
-      if (page[j] >= 0) {
-        const uint4 *b = reinterpret_cast<const uint4 *>((const T *)a.c.bounds + ((long long)page[j] * a.c.hkv + kvh) * 2 * HD) + l;
-        lo[j] = b[0];
-        hi[j] = b[LANES];
-      }
-      on |= (page[j] != -1) << j;
-      bad |= (page[j] == -2) << j;
-    }
-    look_up(base + gridDim.y * BLOCK);
-    if (base == (int)blockIdx.y * BLOCK) {                 // the largest sum |q_d| of the group's heads
-      __syncthreads();
-      for (int g = warp; g < a.group; g += CACHE_THREADS / 32) {
-        float sum = 0.f;
-        for (int d = lane; d < HD; d += 32) sum += fabsf(to_f(q0[g * HD + d]));
-        sum = warp_sum(sum);
-        if (lane == 0) atomicMax(reinterpret_cast<int *>(&q1_s), __float_as_int(sum));      // (floats above zero are ordered as integers are; NaN is above all)
-      }
-    }
-    float best[LEFT];
-#pragma unroll
-    for (int j = 0; j < LEFT; ++j) best[j] = -INFINITY;
-    for (int g0 = 0; g0 < a.group; g0 += GC) {
-      if (base == (int)blockIdx.y * BLOCK || a.group > GC) {                             // (heads that fit stay where they are)
-        __syncthreads();
-        for (int i = threadIdx.x; i < GC * LANES; i += CACHE_THREADS) {
-          const int g = i / LANES, c = i % LANES;
-          const uint4 w = g0 + g < a.group ? *reinterpret_cast<const uint4 *>(q0 + (g0 + g) * HD + c * 8) : make_uint4(0u, 0u, 0u, 0u);
-          const float2 x = widen2<T>(w.x), y = widen2<T>(w.y), z = widen2<T>(w.z), u = widen2<T>(w.w);
-          q_s[g][0][c] = make_float4(x.x, x.y, y.x, y.y);
-          q_s[g][1][c] = make_float4(z.x, z.y, u.x, u.y);
-          const auto mask = [](uint32_t v) { return (v & 0x8000u ? 0xffffu : 0u) | (v & 0x80000000u ? 0xffff0000u : 0u); };
-          m_s[g][c] = make_uint4(mask(w.x), mask(w.y), mask(w.z), mask(w.w));
-        }
-        __syncthreads();
-      }
-      float v[NV];                                         // v[g * SCORE_DEEP + j]
-#pragma unroll
-      for (int g = 0; g < GC; ++g) {
-        const float4 qa = q_s[g][0][l], qb = q_s[g][1][l];
-        const uint4 m = m_s[g][l];
-#pragma unroll
-        for (int j = 0; j < SCORE_DEEP; ++j) {
-          // the lower bound where q is negative, else the upper one
-          const float2 x = widen2<T>((lo[j].x & m.x) | (hi[j].x & ~m.x)), y = widen2<T>((lo[j].y & m.y) | (hi[j].y & ~m.y));
-          const float2 z = widen2<T>((lo[j].z & m.z) | (hi[j].z & ~m.z)), u = widen2<T>((lo[j].w & m.w) | (hi[j].w & ~m.w));
-          float t = qa.x * x.x;
-          t = fmaf(qa.y, x.y, t); t = fmaf(qa.z, y.x, t); t = fmaf(qa.w, y.y, t);
-          t = fmaf(qb.x, z.x, t); t = fmaf(qb.y, z.y, t); t = fmaf(qb.z, u.x, t);
-          v[g * SCORE_DEEP + j] = fmaf(qb.w, u.y, t);
-        }
-      }
-      // across the lanes of a page: at each step a lane gives away one half of its sums and adds to the other
-      int width = NV;
-#pragma unroll
-      for (int o = LANES / 2; o > 0; o >>= 1) {
-        if (width > 1) {
-          width /= 2;
-          const bool up = (lane & o) != 0;
-#pragma unroll
-          for (int j = 0; j < NV / 2; ++j)
-            if (j < width) {
-              const float give = up ? v[j] : v[j + width], keep = up ? v[j + width] : v[j];
-              v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-            }
-        } else v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
-      }
-      // A lane is left with the sums own * LEFT + (0 .. LEFT - 1), the bits of own being the lane's highest.  The largest of the group's heads: those past
-      // the group have no say, nor has NaN.
-      const int own = l / (LANES / STEPS);
-#pragma unroll
-      for (int j = 0; j < LEFT; ++j) {
-        float f = g0 + (own * LEFT + j) / SCORE_DEEP < a.group ? v[j] : -INFINITY;
-#pragma unroll
-        for (int o = LANES / 2; o >= LANES / STEPS * (SCORE_DEEP / LEFT); o >>= 1) f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, o));
-        best[j] = fmaxf(best[j], f);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < SCORE_DEEP; ++j) {
-      const uint32_t w[8] = {lo[j].x, lo[j].y, lo[j].z, lo[j].w, hi[j].x, hi[j].y, hi[j].z, hi[j].w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = max_pair(top, w[i] & 0x7fff7fffu, T());
-    }
-    const int own = l / (LANES / STEPS);
-#pragma unroll
-    for (int j = 0; j < LEFT; ++j) {
-      const int i = own * LEFT + j, p = p0 + i % SCORE_DEEP * PAGES;
-      if (i < SCORE_DEEP && l % (LANES / STEPS) == 0 && on >> i & 1u) scores[p] = bad >> i & 1u ? __int_as_float(0x7fffffff) : best[j];
-    }
-  }
-  for (int o = 16; o > 0; o >>= 1) top = max_pair(top, __shfl_xor_sync(0xffffffffu, top, o), T());
-  if (lane == 0) top_s[warp] = top;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < CACHE_THREADS / 32; ++w) top = max_pair(top, top_s[w], T());
-    const float2 t = widen2<T>(top);
-    // (and what products below the smallest normal number lose)
-    a.off[(long long)blockIdx.x * a.score_blocks + blockIdx.y] = 18.f * 0x1p-24f * q1_s * fmaxf(t.x, t.y) + 0x1p-140f;
-  }
-}
-
 // A page's score by the whole warp, from 64 bits: products are exact (8 and 8, or 11 and 11, digits), and so is nearly every sum of them.
 template <typename T, int HD>
 __device__ __forceinline__ float exact_score(const CacheSelectArgs &a, const T *q0, int page, int kvh, int lane) {
@@ -439,6 +290,156 @@ __device__ __forceinline__ float exact_score(const CacheSelectArgs &a, const T *
     best = fmaxf(best, (float)s);
   }
   return best;
+}
+
+// D = A B + 0, 16 x 8 over 16: a lane has of A the pairs 2 j, 2 j + 1 (a[0], a[1]) and 2 j + 8, 2 j + 9 (a[2], a[3]) of rows i and i + 8, of B those of column i, of D
+// columns 2 j and 2 j + 1 of both rows (lane = 4 i + j).
+__device__ __forceinline__ void score_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, bf16) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void score_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, f16) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ float2 widen2(uint32_t w, bf16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ float2 widen2(uint32_t w, f16) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
+
+// Scores in 32 bits, with a bound on how far they are off.  (Which pages are kept is a matter of the scores in 64 bits, but only for the few near the cut, which
+// k_cache_select looks at again.)  sum_d max(q_d lo_d, q_d hi_d) is a product of the bounds with q's positive part and its negative one, [hi | lo] [q+ ; q-]: a
+// warp takes 16 pages against up to eight heads of the group (more in another pass) with the warp's own matrix instruction; eight columns are too few for the others, and what
+// bounds this is the bounds' way from memory.  A row of A is a page, and its channels come in any order, the same in q, so that a lane reads 16 bytes at a time.
+// Selection as a whole, with 64 pages kept, before (a lane had eight channels of a page, multiplied, added one by one and across lanes: six times the instructions) and now: 8 rows
+// against 1024 pages, 32 heads over 8 of 128, 23.9 and 18.8 us; 64 rows 93 and 70; one row against 2048 pages 15.2 and 11.7; 9 rows against 1876 pages of 16 tokens, 16 over 8 of 256, 35 and 28.
+// (Two or four runs of 32 channels under way in a lane take registers from blocks: 64 rows 91 us and 69, 8 rows 19.0 and 21.6.)
+// A sum that is no number, as infinite bounds times 0 make it, is formed again from 64 bits.
+// The bound.  Each of HD / 8 instructions adds 16 exact products to zero; of each product it may lose 2^-23 of the largest, and of its result, no larger than 16 of these, as much:
+// 32 x 2^-23 = 2^-18 of the largest product there may be, max |q_d| times the largest bound there is (met in 2.5 million sums: 2^-21).  The sums are added in 32 bits, each time wrong by
+// 2^-24 of a partial sum, which is no larger than sum |q_d| times the largest bound; one more such error for the rounding of the exact score, and four for the bound's own.
+#define SCORE_PAGES (CACHE_THREADS / 32 * 16)              // pages that a block has under way
+#define SCORE_BLOCKS 4                                     // to an SM: few registers a thread and many blocks; see below
+template <typename T, int HD>
+__global__ void __launch_bounds__(CACHE_THREADS, SCORE_BLOCKS)
+k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
+  constexpr int CHUNKS = HD / 32;                           // 32 channels: a lane's 16 bytes, four lanes to a page
+  __shared__ uint4 q_s[2][CHUNKS][32];                      // positive and negative parts, as the lanes take them
+  __shared__ uint32_t top_s[CACHE_THREADS / 32];
+  __shared__ float q1_s, q_top_s;
+  kernel_entry(TR_k_cache_scores);
+  const int r = blockIdx.x / a.c.hkv, kvh = blockIdx.x % a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, end = n - a.keep_last;
+  if (n <= a.budget) return;                               // all are kept
+  const T *q0 = (const T *)a.q + r * a.q_ld + (long long)kvh * a.group * HD;
+  float *scores = a.scores + (long long)blockIdx.x * a.c.pages_per_seq;
+  const uint32_t inf = CaInf<T>::BITS * 0x10001u;
+  uint32_t high = inf | 0x80008000u, low = inf;            // the largest upper and the smallest lower bound met, a pair
+  const int step = gridDim.y * SCORE_PAGES;
+  int page;                                                // of the pages ahead, a lane and its neighbour 16 further on have one; -1: not asked for, -2: no number
+  const auto look_up = [&](int base) {
+    const int p = base + warp * 16 + (lane & 15);
+    page = -1;
+    if (p >= a.keep_first && p < end) {
+      page = a.c.page(seq, p);
+      if (page < 0) { page = -2; cache_bad_index(a.status); }
+    }
+  };
+  if (threadIdx.x == 0) q1_s = q_top_s = 0.f;
+  for (int g0 = 0; g0 < a.group; g0 += 8) {
+    look_up(blockIdx.y * SCORE_PAGES);
+    __syncthreads();
+    for (int i = threadIdx.x; i < CHUNKS * 32; i += CACHE_THREADS) {
+      const int g = g0 + (i & 31) / 4;
+      const uint4 w = g < a.group ? *reinterpret_cast<const uint4 *>(q0 + g * HD + (i >> 5) * 32 + (i & 3) * 8) : make_uint4(0u, 0u, 0u, 0u);
+      const auto mask = [](uint32_t v) { return (v & 0x8000u ? 0xffffu : 0u) | (v & 0x80000000u ? 0xffff0000u : 0u); };
+      const uint4 m = make_uint4(mask(w.x), mask(w.y), mask(w.z), mask(w.w));
+      q_s[0][i >> 5][i & 31] = make_uint4(w.x & ~m.x, w.y & ~m.y, w.z & ~m.z, w.w & ~m.w);
+      q_s[1][i >> 5][i & 31] = make_uint4(w.x & m.x, w.y & m.y, w.z & m.z, w.w & m.w);
+    }
+    for (int g = g0 + warp; g < min(g0 + 8, a.group); g += CACHE_THREADS / 32) {
+      float sum = 0.f, most = 0.f;                         // sum |q_d| and max |q_d|
+      for (int d = lane; d < HD; d += 32) {
+        const float x = fabsf(to_f(q0[g * HD + d]));
+        sum += x;
+        most = fmaxf(most, x);
+      }
+      sum = warp_sum(sum);
+      most = warp_max(most);
+      // (floats above zero are ordered as integers are; NaN is above all)
+      if (lane == 0) { atomicMax(reinterpret_cast<int *>(&q1_s), __float_as_int(sum)); atomicMax(reinterpret_cast<int *>(&q_top_s), __float_as_int(most)); }
+    }
+    __syncthreads();
+    for (int base = blockIdx.y * SCORE_PAGES; base < end; base += step) {
+      const int now = page, p0 = base + warp * 16;
+      look_up(base + step);
+      const int pa = __shfl_sync(0xffffffffu, now, lane / 4), pb = __shfl_sync(0xffffffffu, now, lane / 4 + 8);
+      const uint4 *lo_a = reinterpret_cast<const uint4 *>((const T *)a.c.bounds + ((long long)max(pa, 0) * a.c.hkv + kvh) * 2 * HD) + (lane & 3);
+      const uint4 *lo_b = reinterpret_cast<const uint4 *>((const T *)a.c.bounds + ((long long)max(pb, 0) * a.c.hkv + kvh) * 2 * HD) + (lane & 3);
+      float v[4] = {};
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        uint4 x[4];                                         // upper and lower bounds of both pages
+        x[0] = x[1] = x[2] = x[3] = make_uint4(0u, 0u, 0u, 0u);
+        if (pa >= 0) { x[0] = lo_a[HD / 8 + c * 4]; x[2] = lo_a[c * 4]; }
+        if (pb >= 0) { x[1] = lo_b[HD / 8 + c * 4]; x[3] = lo_b[c * 4]; }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {                       // the positive part with the upper bounds, the negative one with the lower
+          const uint4 b = q_s[s][c][lane], &ya = x[2 * s], &yb = x[2 * s + 1];
+          float d[4], e[4];
+          score_mma(d, ya.x, yb.x, ya.y, yb.y, b.x, b.y, T());
+          score_mma(e, ya.z, yb.z, ya.w, yb.w, b.z, b.w, T());
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = (v[i] + d[i]) + e[i];
+          if (g0 == 0) {
+            const uint32_t w[8] = {ya.x, ya.y, ya.z, ya.w, yb.x, yb.y, yb.z, yb.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              if (s == 0) high = max_pair(high, w[i], T());
+              else low = min_pair(low, w[i], T());
+            }
+          }
+        }
+      }
+      // the largest of the group's heads, across the four lanes of a page
+      float best[2];
+      bool odd[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int g = g0 + 2 * (lane & 3);
+        const float s0 = g < a.group ? v[2 * k] : -INFINITY, s1 = g + 1 < a.group ? v[2 * k + 1] : -INFINITY;
+        odd[k] = s0 != s0 || s1 != s1;
+        float f = fmaxf(s0, s1);
+        f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, 1));
+        best[k] = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, 2));
+      }
+      const unsigned odd_a = __ballot_sync(0xffffffffu, odd[0] && pa >= 0), odd_b = __ballot_sync(0xffffffffu, odd[1] && pb >= 0);
+      if (odd_a | odd_b)
+        for (int i = 0; i < 16; ++i)
+          if ((i < 8 ? odd_a >> 4 * i : odd_b >> 4 * (i - 8)) & 15u) {
+            const float s = exact_score<T, HD>(a, q0, __shfl_sync(0xffffffffu, now, i), kvh, lane);
+            if (lane / 4 == i % 8) best[i / 8] = s;
+          }
+      if ((lane & 3) == 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int pg = k ? pb : pa, p = p0 + lane / 4 + 8 * k;
+          if (pg != -1) scores[p] = pg == -2 ? __int_as_float(0x7fffffff) : g0 ? fmaxf(scores[p], best[k]) : best[k];
+        }
+      }
+    }
+  }
+  for (int o = 16; o > 0; o >>= 1) {
+    high = max_pair(high, __shfl_xor_sync(0xffffffffu, high, o), T());
+    low = min_pair(low, __shfl_xor_sync(0xffffffffu, low, o), T());
+  }
+  if (lane == 0) top_s[warp] = max_pair(max_pair(high, low ^ 0x80008000u, T()), 0u, T());
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t top = top_s[0];
+    for (int w = 1; w < CACHE_THREADS / 32; ++w) top = max_pair(top, top_s[w], T());
+    const float2 t = widen2(top, T());
+    // (and what products below the smallest normal number lose)
+    a.off[(long long)blockIdx.x * a.score_blocks + blockIdx.y] = ((HD / 8) * 0x1p-18f * q_top_s + (HD / 8 + 5) * 0x1p-24f * q1_s) * fmaxf(t.x, t.y) + 0x1p-116f;
+  }
 }
 
 // grid (rows * KV heads), the scores in shared memory as 32-bit keys of the same order (0: a page without a number).  The cut, the left-th largest: bins over the range of

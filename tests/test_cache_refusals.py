@@ -98,7 +98,7 @@ def test_selection_needs_bounds_and_has_room_for_so_many_pages():
     assert all(call(None) == E_ARG for call in CALLS)
 
 
-@pytest.mark.parametrize("over,rows", [(dict(page_tokens=256, pages_per_seq=1 << 22, n_kv_heads=64), 16), (dict(page_tokens=256, pages_per_seq=1 << 22, n_kv_heads=128), 1),
+@pytest.mark.parametrize("over,rows", [(dict(page_tokens=256, pages_per_seq=1 << 22, n_kv_heads=64), 129), (dict(page_tokens=256, pages_per_seq=1 << 22, n_kv_heads=128), 1),
                                        (dict(page_tokens=16, pages_per_seq=1 << 23, n_kv_heads=2), 1 << 20)])
 def test_work_that_is_not_counted_in_32_bits(over, rows):
     """A prefix of so many keys in so many tiles; a table may well name one page over and over."""

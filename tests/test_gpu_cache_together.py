@@ -339,3 +339,27 @@ def test_wrappers_refuse_what_does_not_fit():
     with pytest.raises((ValueError, TypeError, RuntimeError)):                    # a cache without bounds
         api.dream_cache_select(pg.cache, q, seq, pos, ids, space)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("heads,hkv,d,dtype", [(4, 2, 128, "bf16"), (24, 2, 64, "f16"), (1, 1, 256, "bf16"), (9, 1, 128, "f16")])
+def test_selection_with_infinite_bounds(heads, hkv, d, dtype):
+    """A channel that is unbounded on the side that a query does not ask about says nothing; on the other side the page comes first."""
+    from paper_2505_19201_b200 import api
+    g = torch.Generator(device="cuda").manual_seed(d + heads)
+    n, pt, budget = 300, 16, 40
+    k = torch.randn(n, hkv, pt, d, generator=g, device="cuda").to(TYPES[dtype])
+    bounds = torch.stack((k.amin(2), k.amax(2)), 2).contiguous()
+    at = torch.randperm(n, generator=g, device="cuda")[:60]
+    bounds[at[:30], :, 0, 3] = -float("inf")
+    bounds[at[30:45], :, 1, 5] = float("inf")
+    tab = torch.randperm(n, generator=g, device="cuda").int().view(1, n)
+    cache = api.Cache(k, torch.zeros_like(k), tab, bounds)
+    q = torch.randn(3, heads, d, generator=g, device="cuda").to(TYPES[dtype])
+    q[q == 0] = 1.0
+    q[0, :, 3], q[0, :, 5] = q[0, :, 3].abs(), -q[0, :, 5].abs()                 # row 0: nothing unbounded counts
+    pos, seq = [n * pt - 1, 290 * pt, 200 * pt + 3], i32([0, 0, 0])
+    ids, status = torch.full((3, hkv, budget), 99, dtype=torch.int32, device="cuda"), i32([0, 0])
+    api.dream_cache_select(cache, q, seq, i32(pos), ids, room(api.dream_cache_select_bytes(cache, 3)), keep_first=1, keep_last=1, status=status)
+    for r in range(3):
+        assert torch.equal(ids[r].cpu(), best_pages(cache, tab[0], q[r], pos[r], budget, 1, 1))
+    assert status.tolist() == [0, 0]
