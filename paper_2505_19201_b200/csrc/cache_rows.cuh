@@ -448,7 +448,8 @@ k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
 // between (as a rule the cut's own page and nothing else) is not taken as a whole, it gets its exact scores and the cut is looked for again.  Then the kept pages in order: a
 // thread has a run of pages.
 #define SELECT_THREADS 512
-#define SELECT_BINS 1024
+#define SELECT_BITS 10
+#define SELECT_BINS (1 << SELECT_BITS)
 #define SELECT_FEW 64
 struct SelectShared {
   int hist[SELECT_BINS], scan[SELECT_THREADS / 32], n_few, bin, above, count, ties;
@@ -467,8 +468,7 @@ __device__ __forceinline__ void select_cut(SelectShared &sh, const uint32_t *key
   low = __reduce_min_sync(0xffffffffu, sh.lows[lane % (SELECT_THREADS / 32)]);
   high = __reduce_max_sync(0xffffffffu, sh.highs[lane % (SELECT_THREADS / 32)]);
   for (bool first = true;; first = false) {                     // keys low .. high hold the cut, the left-th largest of them
-    int shift = 0;
-    while ((high - low) >> shift >= SELECT_BINS) ++shift;
+    const int shift = max(0, 32 - __clz(high - low) - SELECT_BITS);
     if (!first) {
       for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) sh.hist[i] = 0;
       __syncthreads();
@@ -485,7 +485,7 @@ __device__ __forceinline__ void select_cut(SelectShared &sh, const uint32_t *key
     for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += t; }
     if (lane == 31) sh.scan[warp] = sum;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) sum += sh.scan[w];
+    sum += __reduce_add_sync(0xffffffffu, lane < warp ? sh.scan[lane] : 0);
     if (sum >= left && sum - own < left) {
       int above = sum - own, b = (SELECT_THREADS - tid) * PER - 1;
       while (above + sh.hist[b] < left) above += sh.hist[b--];
@@ -627,7 +627,7 @@ k_cache_select(const __grid_constant__ CacheSelectArgs a) {
   if (lane == 31) sh.scan[warp] = sum;
   __syncthreads();
   sum -= both;
-  for (int w = 0; w < warp; ++w) sum += sh.scan[w];
+  sum += __reduce_add_sync(0xffffffffu, lane < warp ? sh.scan[lane] : 0);
   int tie = sum >> 16 & 0xffff, at = a.keep_first + (sum & 0xffff) + min(tie, ties);
   for (int i = i0; i < i1; ++i) {
     const uint32_t k = sel_keys[i];
