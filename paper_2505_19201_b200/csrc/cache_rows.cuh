@@ -310,7 +310,7 @@ __device__ __forceinline__ float2 widen2(uint32_t w, f16) { return __half22float
 // warp takes 16 pages against up to eight heads of the group (more in another pass) with the warp's own matrix instruction; eight columns are too few for the others, and what
 // bounds this is the bounds' way from memory.  A row of A is a page, and its channels come in any order, the same in q, so that a lane reads 16 bytes at a time.
 // Selection as a whole, with 64 pages kept, before (a lane had eight channels of a page, multiplied, added one by one and across lanes: six times the instructions) and now: 8 rows
-// against 1024 pages, 32 heads over 8 of 128, 23.9 and 18.8 us; 64 rows 93 and 70; one row against 2048 pages 15.2 and 11.7; 9 rows against 1876 pages of 16 tokens, 16 over 8 of 256, 35 and 28.
+// against 1024 pages, 32 heads over 8 of 128, 23.9 and 17.9 us; 64 rows 93 and 68; one row against 2048 pages 15.2 and 10.6; 9 rows against 1876 pages of 16 tokens, 16 over 8 of 256, 35 and 28.
 // (Two or four runs of 32 channels under way in a lane take registers from blocks: 64 rows 91 us and 69, 8 rows 19.0 and 21.6.)
 // A sum that is no number, as infinite bounds times 0 make it, is formed again from 64 bits.
 // The bound.  Each of HD / 8 instructions adds 16 exact products to zero; of each product it may lose 2^-23 of the largest, and of its result, no larger than 16 of these, as much:
@@ -325,7 +325,9 @@ k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
   __shared__ uint4 q_s[2][CHUNKS][32];                      // positive and negative parts, as the lanes take them
   __shared__ uint32_t top_s[CACHE_THREADS / 32];
   __shared__ float q1_s, q_top_s;
-  kernel_entry(TR_k_cache_scores);
+  unsigned long long *tr = trace_open();
+  pdl_wait();
+  trace_stamp(tr, TR_k_cache_scores);
   const int r = blockIdx.x / a.c.hkv, kvh = blockIdx.x % a.c.hkv, seq = a.row_seq[r], pos = a.row_pos[r], n = select_pages(a, seq, pos);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, end = n - a.keep_last;
   if (n <= a.budget) return;                               // all are kept
@@ -433,6 +435,7 @@ k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
   }
   if (lane == 0) top_s[warp] = max_pair(max_pair(high, low ^ 0x80008000u, T()), 0u, T());
   __syncthreads();
+  pdl_trigger();                             // (at the start, the blocks of k_cache_select would crowd the SMs that have room then: 8 rows 21 us for 18)
   if (threadIdx.x == 0) {
     uint32_t top = top_s[0];
     for (int w = 1; w < CACHE_THREADS / 32; ++w) top = max_pair(top, top_s[w], T());
