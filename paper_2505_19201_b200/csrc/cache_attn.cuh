@@ -184,6 +184,12 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       // the next queries take these ones' place when S of the last unit is done
       if (!mbar_wait_warp(s_full + (g - 1) % SB, (uint32_t)((g - 1) / SB) & 1u, abort_flag)) { gave_up = WAIT_cache_k; break; }
     }
+    // the last O of each buffer: the softmax waits for that of a segment's last unit, and for the others' arrivals nobody does
+#pragma unroll 1
+    for (int i = 0; i < SB && !gave_up; ++i) {
+      if (!mbar_wait_warp(o_done + sb, sph, abort_flag)) gave_up = WAIT_cache_last;
+      if (++sb == SB) { sb = 0; sph ^= 1u; }
+    }
   } else if (warp == 2) {
     // ------------------------------------------------------------------ O += P V: P in TMEM, V MN-major, N = head_dim
     constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
