@@ -266,10 +266,13 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         wait(s_full + sb, sph);
         const uint4 um4 = masks[g % CA_RING];
         if ((um4.x & um4.y & (BLK > 64 ? um4.z & um4.w : 0xffffffffu)) != 0xffffffffu) {
-          // values that are nobody's may be anything, and 0 times that not 0: all the warps' lanes, some to a key
+          // values that are nobody's may be anything, and 0 times that not 0: all the warps' lanes, some to a key.  With fewer stages than buffers of S a unit's scores may be here before
+          // the values of the unit STAGES back, and then the parity of their barrier is that of the unit before that one; behind its O it says what it is asked
           constexpr int LANES = 32 * CA_SOFTMAX / BLK;
           const int key = (ws * 32 + lane) / LANES, word = key >> 5;
-          if (!((word == 0 ? um4.x : word == 1 ? um4.y : word == 2 ? um4.z : um4.w) >> (key & 31) & 1u) && mbar_wait(v_full + g % STAGES, (uint32_t)(g / STAGES) & 1u, abort_flag)) {
+          if (!((word == 0 ? um4.x : word == 1 ? um4.y : word == 2 ? um4.z : um4.w) >> (key & 31) & 1u) &&
+              (STAGES >= SB || g < STAGES || mbar_wait(o_done + (g - STAGES) % SB, (uint32_t)((g - STAGES) / SB) & 1u, abort_flag)) &&
+              mbar_wait(v_full + g % STAGES, (uint32_t)(g / STAGES) & 1u, abort_flag)) {
             uint8_t *v = v_s + (g % STAGES) * Sh::STAGE + key * 128;
 #pragma unroll 1
             for (int j = lane % LANES; j < KP * 8; j += LANES) *reinterpret_cast<uint4 *>(v + (j >> 3) * Sh::PANEL + (j & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);

@@ -17,18 +17,23 @@ FEW = {64: (3, 4), 128: (3, 4), 256: (3, 4)}
 class Committer:
     """tcgen05.commit: arrives behind the MMAs issued before it, and when it arrives beyond that nothing says, later commits' arrivals on other barriers included."""
 
-    def __init__(self, clock):
-        self.clock, self.last = clock, 0.0
+    def __init__(self, clock, late=()):
+        self.clock, self.late, self.last = clock, late, 0.0
 
     def __call__(self, *barriers):
         self.last = max(self.last, self.clock.now) + self.clock.rng.uniform(0.05, 0.6)
         for b in barriers:
-            self.clock.at(self.last + self.clock.rng.uniform(0, 1.5) ** 5, b.arrive)
+            self.clock.at(self.last + self.clock.rng.uniform(0, 10 if b in self.late else 1), b.arrive)
 
 
 def closing_waits(path):
     """Whether the kernel waits at its end for the arrivals that nothing else waits for, as its source has it."""
     return bool(re.search(r"// the last O [^\n]*\n[^}]*?\(o_done \+", open(os.path.join(CSRC, path)).read()))
+
+
+def clears_behind_o():
+    """Whether k_cache_attn clears values that are nobody's behind the O that left their stage, as its source has it."""
+    return "mbar_wait(o_done + (g - STAGES) % SB, (uint32_t)((g - STAGES) / SB) & 1u, abort_flag)" in open(os.path.join(CSRC, "cache_attn.cuh")).read()
 
 
 def bars(n, count=1):
@@ -63,7 +68,7 @@ def segment(i, seg_full):
     return until(lambda: seg_full[i % RING].done(i // RING & 1))
 
 
-def many(hd, segments, seed, closing=True):
+def many(hd, segments, seed, closing=True, behind_o=True):
     stages, SB = MANY[hd]
     rng = random.Random(seed)
     clock = Clock(rng)
@@ -99,7 +104,7 @@ def many(hd, segments, seed, closing=True):
             sb, sph = step(sb, sph, SB)
 
     def o_issuer():
-        commit = Committer(clock)
+        commit = Committer(clock, o_done)
         vs = vph = sb = pph = g = 0
         for seg in range(len(segments) + 1):
             yield from segment(seg, seg_full)
@@ -141,6 +146,11 @@ def many(hd, segments, seed, closing=True):
             for u in range(n):
                 yield from until(lambda: s_full[sb].done(sph))
                 assert held["s"][sb] == g and ring["mask"][g % RING] == g
+                if rng.random() < 0.3:                          # values that are cleared
+                    if stages < SB and g >= stages and behind_o:
+                        yield from until(lambda: o_done[(g - stages) % SB].done((g - stages) // SB & 1))
+                    yield from until(lambda: v_full[g % stages].done(g // stages & 1))
+                    assert held["v"][g % stages] == g and v_full[g % stages].phase == g // stages + 1
                 yield from meet(w % 8)
                 if moves.random() < 0.3:
                     yield from meet(w % 8)
@@ -220,7 +230,7 @@ def few(hd, segments, seed, closing=True):
             seg += 1
 
     def o_issuer():
-        commit = Committer(clock)
+        commit = Committer(clock, o_done)
         st = ph = g = 0
         for seg in range(len(segments) + 1):
             yield from segment(seg, seg_full)
@@ -270,9 +280,9 @@ def few(hd, segments, seed, closing=True):
                         yield from until(lambda: o_done[(g - 1) & 1].done((g - 1) >> 1 & 1))
                         assert held["o"][seg & 1] == g - 1
                 held["p"][pb][w] = g
-                if rng.random() < 0.2:
+                if rng.random() < 0.3:
                     yield from until(lambda: v_full[g % stages].done(g // stages & 1))
-                    assert held["v"][g % stages] == g
+                    assert held["v"][g % stages] == g and v_full[g % stages].phase == g // stages + 1
                 yield from some(rng, 3)
                 p_full[pb].arrive()
                 g += 1
@@ -292,6 +302,20 @@ def few(hd, segments, seed, closing=True):
 
 
 SEGMENTS = [[], [1], [2], [3], [4], [5], [9], [1, 1], [3, 1, 2], [1] * 20, [1, 7, 1, 4], [2] * 18 + [5]]
+
+
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_values_are_cleared_where_they_have_come(hd):
+    for segments in SEGMENTS:
+        for seed in range(12, 36):
+            many(hd, list(segments), seed, behind_o=clears_behind_o())
+
+
+def test_values_cleared_by_their_barrier_alone():
+    with pytest.raises(AssertionError):
+        for segments in SEGMENTS:
+            for seed in range(12, 36):
+                many(256, list(segments), seed, behind_o=False)
 
 
 @pytest.mark.parametrize("hd", [64, 128, 256])
