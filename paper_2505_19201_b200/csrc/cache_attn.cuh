@@ -109,7 +109,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     else if (lane >= 8 && lane < 8 + SB) { mbar_init(s_full + lane - 8, 1); mbar_init(p_full + lane - 8, CA_SOFTMAX); mbar_init(o_done + lane - 8, 1); }
     else if (lane >= 16) mbar_init(seg_full + lane - 16, 1);
     if (lane == 12) { mbar_init(q_full, 1); mbar_init(o_free, CA_SOFTMAX); *abort_flag = 0; }
-    else if (lane == 13) { plan.partial = 0; sh_status[0] = sh_status[1] = 0; }
+    else if (lane == 13) { plan.partial = plan.longest = 0; sh_status[0] = sh_status[1] = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 4 && lane == 0) {

@@ -90,7 +90,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const int i = lane - 8;
       mbar_init(p_full + i, 4); mbar_init(o_done + i, 1); mbar_init(o_free + i, 4); mbar_init(q_full + i, 1); mbar_init(q_empty + i, 1);
     } else if (lane >= 16) mbar_init(seg_full + lane - 16, 1);
-    if (lane == 12) { *abort_flag = 0; plan.partial = 0; sh_status[0] = sh_status[1] = 0; }
+    if (lane == 12) { *abort_flag = 0; plan.partial = plan.longest = 0; sh_status[0] = sh_status[1] = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 4 && lane == 0) {

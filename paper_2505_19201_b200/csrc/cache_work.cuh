@@ -90,7 +90,7 @@ __device__ __forceinline__ int ca_seq_of(const CacheAttnArgs &a, int r) {
   return lo;
 }
 
-struct CaPlanShared { long long sum[32], at; CaSeq q; int seq, partial; };      // partial starts as 0
+struct CaPlanShared { long long sum[32], at; CaSeq q; int seq, partial, longest; };      // partial and longest start as 0
 
 // a / b for a from 0 and b from 1 on: a division of 64-bit numbers takes several times that of 32-bit ones, and hardly a call has as many units.
 __device__ __forceinline__ long long ca_div(long long a, int b) { return a >> 31 ? a / b : (long long)((int)a / b); }
@@ -175,16 +175,19 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
       prefix_units = (long long)prefix_tiles * (prefix_blocks + START) * a.c.hkv;
       // units in front of each sequence's, a sequence per thread at a time; once around for most batches, twice where there are more sequences than threads
       long long own = 0, sum = 0;
+      int longest = 0;
       CaSeq t;
       for (int i = threadIdx.x; i < a.c.n_seqs; i += blockDim.x) {
         t = CaSeq(a, i);
         own = a.with_own ? t.template all_units<BLK, START>(a) : 0ll;
         sum += own;
         if (t.n && t.len - t.n + (a.tree ? 0 : 1) < a.shared_tokens) sh.partial = 1;       // a row that does not see the whole prefix
+        if (t.n) longest = max(longest, t.len);
         if (cta == 0 && (t.q0 != a.q_start[i] || t.q0 + t.n != a.q_start[i + 1] || t.len != a.kv_len[i])) cache_bad_index(status);
       }
       for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += x; }
-      if (lane == 31) sh.sum[warp] = sum;
+      longest = __reduce_max_sync(0xffffffffu, longest);
+      if (lane == 31) { sh.sum[warp] = sum; if (longest) atomicMax(&sh.longest, longest); }
       __syncthreads();
       total = prefix_units;
       long long before = prefix_units + sum - own;
@@ -225,7 +228,7 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
       item = (long long)i * (blocks + START);
     } else if (u < prefix_units) {
       const int i = (int)u / (prefix_blocks + START);
-      s.phase = 0; s.end = a.shared_tokens;
+      s.phase = 0; s.end = min(a.shared_tokens, sh.longest);                               // behind everybody's last token there may be anything
       blocks = prefix_blocks;
       s.kvh = i / prefix_tiles; tile = i - s.kvh * prefix_tiles;
       item = (long long)i * (prefix_blocks + START);
