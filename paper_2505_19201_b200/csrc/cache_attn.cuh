@@ -303,6 +303,10 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                   const int sh = -left, word = sh >> 5;                     // node of the first key; in front of the nodes: the bits come later
                   const uint32_t w0 = word >= 0 && word < 4 ? t[word] : 0u, w1 = word >= -1 && word < 3 ? t[word + 1] : 0u;
                   m |= __funnelshift_r(w0, w1, sh & 31);
+                  if (!s.phase) {                                           // (shared pages do not end where the row's sequence does: no bits past its nodes)
+                    const int past = left + CaSeq(a, ca_seq_of(a, s.row0 + (base + quad + 8 * k) / a.group)).n;
+                    m &= past >= 32 ? 0xffffffffu : past > 0 ? (1u << past) - 1u : 0u;
+                  }
                 }
                 m = (m & um[x]) >> (2 * ql);
 #pragma unroll

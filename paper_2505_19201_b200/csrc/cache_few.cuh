@@ -75,7 +75,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ int sh_status[2];
   __shared__ float red[4][NE];                                           // maxima of the warps
   __shared__ float2 sums[4][NE];                                         // their sums of weights
-  __shared__ int e_vis[2][NE], e_row[2][NE];                           // of a segment's entries: what they see, their row
+  __shared__ int e_vis[2][NE], e_row[2][NE], e_nodes[2][NE];           // of a segment's entries: what they see, their row, and its tree's nodes
   __shared__ void *e_to[NE];                                               // at its end: where O goes, the factor, the reference
   __shared__ float e_inv[NE], refs[NE];
   static_assert(CA_RING > STAGES + CF_S + 1, "what the producer leaves is read until a unit's P is done");
@@ -236,18 +236,20 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       // the entries' rows, and what they see: keys below vis (counted from the segment's first), in a tree their own ones as the mask has them
       if (n > 0 && t < NE) {
         const int r = s.row0 + min(t, n_e - 1) / a.group;
-        int vis = 0x7fffffff;
+        int vis = 0x7fffffff, nodes = 128;                  // (own keys end with the nodes anyway, shared ones do not)
         if (!PAGES && t < n_e && (s.phase || plan.partial)) {
           int tail0 = s.tail0, q0 = s.q0;
           if (!s.phase) {
             const CaSeq sq(a, ca_seq_of(a, r));
             tail0 = sq.len - sq.n;
             q0 = sq.q0;
+            nodes = min(sq.n, 128);
           }
           vis = tail0 + (tree ? 0 : r - q0 + 1) - (s.key0 + s.b0 * BLK);
         }
         e_vis[ob][t] = vis;
         e_row[ob][t] = r;
+        e_nodes[ob][t] = nodes;
       }
       if (cf_any(n <= 0)) break;                            // (whatever a wait of one warp came to, they all go on or all leave: barriers follow)
       int least = e_vis[ob][0];                             // what every entry sees
@@ -286,7 +288,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll 1
             for (int e = 0; e < n_e; ++e) {
               const int node = t + i * BLK - e_vis[ob][e];                  // of the key
-              if (node < 0 || (node < 128 && a.tree[(long long)e_row[ob][e] * 4 + (node >> 5)] >> (node & 31) & 1u)) sees |= 1u << e;
+              if (node < 0 || (node < e_nodes[ob][e] && a.tree[(long long)e_row[ob][e] * 4 + (node >> 5)] >> (node & 31) & 1u)) sees |= 1u << e;
             }
           }
 #pragma unroll

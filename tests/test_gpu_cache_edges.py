@@ -33,3 +33,11 @@ def test_nobody_fills_the_shared_pages(heads, hkv, T, d, pt, shared, lengths, tr
     pg.table[:, (max(lengths) + pt - 1) // pt:] = -1
     dense(pg, T, heads, tree=sum((chain(n, False) for n in T), []) if tree else None)
 
+
+@pytest.mark.parametrize("heads,hkv,T", FORMS)
+@pytest.mark.parametrize("d,pt,shared,lengths", [(128, 64, 2, [128, 90]), (64, 16, 8, [127, 100]), (256, 64, 2, [140, 100])])
+def test_bits_of_nodes_that_are_not_there(heads, hkv, T, d, pt, shared, lengths):
+    """A tree inside the shared pages, in front of tokens that are another sequence's: bits past its last node say nothing."""
+    T, lengths = T[::-1], lengths[::-1][:len(T)]
+    pg = Pages([max(lengths)] + lengths, hkv, d, pt, shared=shared, seed=heads)
+    dense(pg, [1] + T, heads, tree=chain(1, True) + sum((chain(n, True) for n in T), []))
