@@ -1,8 +1,12 @@
 """Calls on a paged cache at the edges of what they allow."""
+import random
+
 import pytest
+import torch
 
 from .test_gpu_cache_attn import dense
-from .util_cache import Pages, tree_words
+from .test_gpu_cache_rows import i32, table
+from .util_cache import NAN, Pages, pools, tree_words
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +45,32 @@ def test_bits_of_nodes_that_are_not_there(heads, hkv, T, d, pt, shared, lengths)
     T, lengths = T[::-1], lengths[::-1][:len(T)]
     pg = Pages([max(lengths)] + lengths, hkv, d, pt, shared=shared, seed=heads)
     dense(pg, [1] + T, heads, tree=chain(1, True) + sum((chain(n, True) for n in T), []))
+
+
+@pytest.mark.parametrize("hkv,d,pt,dtype,rot,more", [(2, 128, 64, "bf16", 128, 0), (1, 64, 16, "f16", 0, 0), (3, 256, 32, "bf16", 96, 0), (8, 128, 256, "bf16", 128, 0), (8, 128, 32, "f16", 64, 3000)])
+def test_bounds_of_a_page_that_several_sequences_write(hkv, d, pt, dtype, rot, more):
+    """Rows of three sequences that name one page, at places of their own in it and at entries of their own in the table, in any order; `more` rows of a fourth."""
+    from paper_2505_19201_b200 import api
+    rng = random.Random(pt)
+    n_pages = 8 + more // pt + 1
+    k, v = pools(n_pages, hkv, pt, d, dtype)
+    tab = torch.full((4, n_pages), -1, dtype=torch.int32)
+    tab[0, 0], tab[1, 2], tab[2, 1] = 5, 5, 5
+    tab[3, :n_pages - 8] = torch.arange(8, n_pages)
+    bounds = torch.full((n_pages, hkv, 2, d), NAN, dtype=k.dtype, device="cuda")
+    cache = api.Cache(k, v, tab.cuda(), bounds)
+    rope = table(3 * pt + more, rot) if rot else None
+    g = torch.Generator(device="cuda").manual_seed(pt)
+    for turn in range(8):
+        owner = [rng.choice([0, 1, 2, None]) for _ in range(pt)]                # None: it stays as it is, which the first time is nothing
+        owner[-1] = turn % 3
+        rows = [(s, (0, 2 * pt, pt)[s] + t) for t, s in enumerate(owner) if s is not None] + [(3, t) for t in range(more)]
+        if turn % 2:
+            rng.shuffle(rows)
+        x = (8.0 - turn) * torch.randn(len(rows), hkv, d, generator=g, device="cuda")
+        x, status = x.to(k.dtype), i32([0, 0])
+        api.dream_cache_append(cache, None, x, x, i32([s for s, _ in rows]), i32([t for _, t in rows]), None, rope=rope, status=status)
+        assert status.tolist() == [0, 0]
+        page = k[5].float().nan_to_num(nan=0.0)
+        there = ~torch.isnan(k[5]).any(2).any(0)
+        assert torch.equal(bounds[5].float(), torch.stack((page[:, there].amin(1), page[:, there].amax(1)), 1))
