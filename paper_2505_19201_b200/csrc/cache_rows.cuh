@@ -96,6 +96,8 @@ __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b, bf16) { __n
 __device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b, f16) { __half2 r = __hmin2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b)); return *reinterpret_cast<uint32_t *>(&r); }
 __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b, f16) { __half2 r = __hmax2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b)); return *reinterpret_cast<uint32_t *>(&r); }
 
+// Whether a row has a position that there are factors for (it is not written otherwise).
+__device__ __forceinline__ bool append_position_ok(const CacheAppendArgs &a, int r, int slot) { return !a.rot || (unsigned)(a.positions ? a.positions[r] : slot) < (unsigned)a.n_pos; }
 // The bounds of one KV head of the page that row r fills, by a whole block: from the rows of this call (rotated once more: the same
 // values) and, for tokens that came earlier, from the cache.
 template <typename T>
@@ -106,7 +108,7 @@ __device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, i
   int missing = 0;
   for (int t = tid; t < pt; t += CACHE_THREADS) {       // as a rule the rows of a sequence stand in order
     const int rr = r - (pt - 1) + t;
-    const bool here = rr >= 0 && a.row_seq[rr] == seq && a.slots[rr] == first + t;
+    const bool here = rr >= 0 && a.row_seq[rr] == seq && a.slots[rr] == first + t && append_position_ok(a, rr, first + t);
     from[t] = here ? rr : -1;                // -1: it is in the cache already
     missing |= !here;
   }
@@ -123,7 +125,8 @@ __device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, i
         at[j] = rr < a.rows ? a.slots[rr] : 0;
       }
 #pragma unroll
-      for (int j = 0; j < AT_ONCE; ++j) other[j] = other[j] >= 0 && a.c.token_ok(other[j], at[j]) && from[at[j] & (pt - 1)] < 0 ? a.c.page(other[j], at[j] >> a.c.page_shift) : -1;
+      for (int j = 0; j < AT_ONCE; ++j) other[j] = other[j] >= 0 && a.c.token_ok(other[j], at[j]) && from[at[j] & (pt - 1)] < 0 && append_position_ok(a, r0 + j * CACHE_THREADS, at[j])
+                                                          ? a.c.page(other[j], at[j] >> a.c.page_shift) : -1;
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j) if (other[j] == page) from[at[j] & (pt - 1)] = r0 + j * CACHE_THREADS;
     }
@@ -151,14 +154,10 @@ __device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, i
       const int t = t0 + j * groups;
       if (t >= pt) continue;
       const int rr = from[t];
-      if (rr >= 0 && a.rot) {
-        const int p = a.positions ? a.positions[rr] : a.slots[rr];
-        if ((unsigned)p >= (unsigned)a.n_pos) continue;                // a row that is not written
-        if (u * 16 < a.rot) {
-          float cs[16];
-          append_factors(a, u, p, cs);
-          append_rotate<T>(a.interleaved, cs, va[j], vb[j]);
-        }
+      if (rr >= 0 && u * 16 < a.rot) {
+        float cs[16];
+        append_factors(a, u, a.positions ? a.positions[rr] : a.slots[rr], cs);
+        append_rotate<T>(a.interleaved, cs, va[j], vb[j]);
       }
       const uint32_t w[8] = {va[j].x, va[j].y, va[j].z, va[j].w, vb[j].x, vb[j].y, vb[j].z, vb[j].w};
 #pragma unroll

@@ -74,3 +74,19 @@ def test_bounds_of_a_page_that_several_sequences_write(hkv, d, pt, dtype, rot, m
         page = k[5].float().nan_to_num(nan=0.0)
         there = ~torch.isnan(k[5]).any(2).any(0)
         assert torch.equal(bounds[5].float(), torch.stack((page[:, there].amin(1), page[:, there].amax(1)), 1))
+
+
+@pytest.mark.parametrize("order", [1, -1])
+def test_bounds_hold_what_a_refused_row_leaves(order):
+    """A row whose position is out of range is not written: the page's bounds count the token that is there."""
+    from paper_2505_19201_b200 import api
+    k, v = pools(1, 2, 16, 64, "bf16")
+    bounds = torch.full((1, 2, 2, 64), NAN, dtype=torch.bfloat16, device="cuda")
+    cache = api.Cache(k, v, i32([[0]]), bounds)
+    rope, slots = table(20, 64), list(range(16))[::order]
+    old = 50 * torch.randn(16, 2, 64, device="cuda").bfloat16()
+    api.dream_cache_append(cache, None, old, old, i32([0] * 16), i32(slots), None, rope=rope)
+    was, new, status = k[0, :, 6].clone(), torch.randn(16, 2, 64, device="cuda").bfloat16(), i32([0, 0])
+    api.dream_cache_append(cache, None, new, new, i32([0] * 16), i32(slots), None, positions=i32([20 if t == 6 else t for t in slots]), rope=rope, status=status)
+    assert status[0] == 2 and torch.equal(k[0, :, 6], was)
+    assert torch.equal(bounds[0], torch.stack((k[0].amin(1), k[0].amax(1)), 1))
