@@ -119,10 +119,21 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
     if (tiles) at_tile(a);
     else u = u_end;                                          // (none: lengths that changed under way)
   }
-  __device__ __forceinline__ void at_seq(const CacheAttnArgs &a, int seq) {               // ... of the first sequence from this one on that has rows
-    for (; seq < a.c.n_seqs; ++seq) {
-      q = CaSeq(a, seq);
-      if (q.n) break;
+  // ... of the first sequence from this one on that has rows; by a whole warp, which looks at 32 sequences at a time (8 of 4096 slots with a row each: 33 us; one by one 65).
+  __device__ __forceinline__ void at_seq(const CacheAttnArgs &a, int seq) {
+    q.n = 0;
+    for (; seq < a.c.n_seqs; seq += 32) {
+      const int i = seq + (threadIdx.x & 31);
+      CaSeq t;
+      t.q0 = t.n = t.len = 0;
+      if (i < a.c.n_seqs) t = CaSeq(a, i);
+      const unsigned some = __ballot_sync(0xffffffffu, t.n > 0);
+      if (some) {
+        const int first = __ffs(some) - 1;
+        seq += first;
+        q.q0 = __shfl_sync(0xffffffffu, t.q0, first); q.n = __shfl_sync(0xffffffffu, t.n, first); q.len = __shfl_sync(0xffffffffu, t.len, first);
+        break;
+      }
     }
     at_own(a, seq);
   }

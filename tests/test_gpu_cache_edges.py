@@ -90,3 +90,15 @@ def test_bounds_hold_what_a_refused_row_leaves(order):
     api.dream_cache_append(cache, None, new, new, i32([0] * 16), i32(slots), None, positions=i32([20 if t == 6 else t for t in slots]), rope=rope, status=status)
     assert status[0] == 2 and torch.equal(k[0, :, 6], was)
     assert torch.equal(bounds[0], torch.stack((k[0].amin(1), k[0].amax(1)), 1))
+
+
+@pytest.mark.parametrize("n_seqs,busy,T", [(4096, [3, 700, 701, 2500, 4095], [1, 1, 1, 1, 1]), (4096, [0, 1999, 4094], [20, 3, 130]), (65, [64], [1]), (33, [0, 32], [2, 40]), (640, [31, 32, 639], [1, 7, 1])])
+@pytest.mark.parametrize("shared", [0, 2])
+def test_slots_without_rows(n_seqs, busy, T, shared):
+    """Slots of a batch of which few have rows in a call, at any distance from each other."""
+    lengths, rows = [0] * n_seqs, [0] * n_seqs
+    for i, (b, t) in enumerate(zip(busy, T)):
+        lengths[b], rows[b] = 32 + t + 150 * i, t
+    pg = Pages(lengths, 2, 64, 16, shared=shared, seed=n_seqs)
+    pg.table[:, :shared] = pg.table[busy[0], :shared]
+    dense(pg, rows, 4)
