@@ -438,7 +438,9 @@ dream_status dream_cache_attn_bytes(const dream_cache *cache, int32_t n_heads, i
  *            read once for all rows instead of once per sequence.  0: nothing is shared.
  *   scale : finite, above zero (as a rule head_dim^-1/2)
  *   lse : device float [rows][n_heads], log-sum-exp of the scaled scores (-inf for a row that sees nothing), or NULL
- * What lies in a page behind a sequence's last token may be anything, NaN included; the tokens themselves are finite. */
+ * What lies in a page behind a sequence's last token may be anything, NaN included; the tokens themselves are finite.
+ * Sequences with a token each, with many, and with none may stand in one batch in any mixture.  (Only a call with rows = n_seqs, nothing shared and up to four query heads to a KV head
+ * is laid out for a row of each sequence: one that has many is right there, but slow.) */
 dream_status dream_cache_attn(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *q_start,
                               const int32_t *kv_len, int32_t shared_pages, const uint32_t *tree_mask, float scale, void *out, int64_t out_ld,
                               float *lse, void *workspace, size_t workspace_bytes, int32_t *status, void *cuda_stream);

@@ -4,6 +4,7 @@
 #include <cudaTypedefs.h>
 
 #include <atomic>
+#include <climits>
 
 #include "cache_attn.cuh"
 #include "cache_few.cuh"
@@ -358,19 +359,39 @@ static const char *cache_attn_few(const dream_cache *cache, CacheAttnArgs &a, cu
 }
 template <typename T, int HD, bool PAGES>
 static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cudaStream_t stream) {
-  // A sequence's rows, or a listed row, have four entries or fewer (on the average: how many each has is on the device, and more go tile by tile); the shared keys meet all rows.
-  // Both sides: at the kernel for few.
-  const bool own_few = a.group <= CF_ENTRIES && (PAGES || (long long)a.rows * a.group <= (long long)CF_ENTRIES * a.c.n_seqs);
-  const bool shared_few = (long long)a.rows * a.group <= CF_ENTRIES, both = PAGES || !a.shared_tokens || shared_few == own_few;
+  // Query entries to a KV head: those of a listed row, or of all rows of a sequence.  How many rows a sequence has is on the device, so where sequences of up to four entries may stand
+  // beside others (no more than four to a sequence on the average) both kernels are launched and each takes its own; but a call with as many rows as sequences and nothing shared is
+  // taken to have a row of each.  (8 sequences of 20 rows in 256 slots, 32 heads over 8 of 128 behind 2000 tokens: 32 us, and 134 by the kernel for few alone; 63 tokens and a prompt
+  // of 192 rows, 32 heads, 339 and 395.  What the other launch costs where it finds nothing: 64 slots with 8 rows 21.5 and 18, 16 sequences of 4 rows 55 and 52.)
+  const long long entries = (long long)a.rows * a.group;
+  const bool few = a.group <= CF_ENTRIES && (PAGES || entries <= (long long)CF_ENTRIES * a.c.n_seqs);
+  const bool many = !few || (!PAGES && entries > CF_ENTRIES && (a.shared_tokens || a.rows != a.c.n_seqs));
   const char *why = nullptr;
   a.cont_slots = cache_slots(HD);
-  a.with_own = both || !own_few;
-  a.with_prefix = a.shared_tokens > 0;
-  if (!both || !own_few) why = cache_attn_many<T, HD, PAGES>(cache, a, stream);
-  a.with_own = 1;
-  a.early = !both || !own_few;
-  a.with_prefix = both && a.shared_tokens > 0;
-  if (!why && own_few) why = cache_attn_few<T, HD, PAGES>(cache, a, stream);
+  auto launch_many = [&]() {
+    if (why || !many) return;
+    a.own_from = few ? CF_ENTRIES + 1 : 1; a.own_to = INT_MAX;
+    a.with_prefix = a.shared_tokens > 0;
+    why = cache_attn_many<T, HD, PAGES>(cache, a, stream);
+  };
+  auto launch_few = [&]() {
+    if (why || !few) return;
+    a.own_from = 1; a.own_to = many ? CF_ENTRIES : INT_MAX;
+    a.with_prefix = !many && a.shared_tokens > 0;
+    why = cache_attn_few<T, HD, PAGES>(cache, a, stream);
+  };
+  // In front, what there is most of: the shared keys, or those of single tokens.
+  if (a.shared_tokens) {
+    launch_many();
+    a.early = few && many;
+    launch_few();
+  } else {
+    a.let = few && many;
+    launch_few();
+    a.let = 0;
+    a.early = few && many;
+    launch_many();
+  }
   // More (row, head)s than threads that merge them are resident at once: a CTA continues one item at most, so most of them are done already, unless each has two parts.  (Seven
   // sequences of 500 rows behind 4096 tokens 297 us, without the look 325; of 128 rows 90 and 88.)
   const long long rh = (long long)a.rows * a.heads, per = 256 / (HD / 4);

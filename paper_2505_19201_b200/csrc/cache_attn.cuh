@@ -103,6 +103,15 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   __shared__ float2 pair_sum[CA_SOFTMAX / 2][2][16];                       // ... and sums of weights
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, cta = blockIdx.x;
+  if (a.early) {                             // no sequence has more entries than the other kernel's tiles: there is nothing to set up, and what follows need not wait for it
+    bool some = false;
+    for (int i = threadIdx.x; i < a.c.n_seqs; i += CA_THREADS) some = some || CaSeq(a, i).taken(a);
+    if (!__syncthreads_or(some)) {
+      pdl_trigger();
+      pdl_wait();
+      return;
+    }
+  }
   unsigned long long *tr = trace_open();
   if (warp == 0) {
     if (lane < STAGES) { mbar_init(k_full + lane, 1); mbar_init(k_empty + lane, 1); mbar_init(v_full + lane, 1); mbar_init(v_empty + lane, 1); }
@@ -127,7 +136,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  pdl_wait();
+  if (!a.early) pdl_wait();
+  if (a.let) pdl_trigger();
   trace_stamp(tr, TR_k_cache_attn);
   int *status = a.status ? a.status : sh_status;
 
@@ -450,6 +460,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   }
   if (gave_up && lane == 0) wait_expired(status, gave_up, abort_flag, -1);
   drain_if_aborted(abort_flag);
+  if (a.early) pdl_wait();                   // the end of this launch is the end of both
   pdl_trigger();
   tc_fence_before();
   __syncthreads();

@@ -109,6 +109,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   // prefix of 32768 keys, 64 wide: 226 -> 218 us.  Were this launch let start when the other one has begun, so that its CTAs follow those that leave one by one, it would
   // be no faster, and questions on one image slower, 36.3 us in place of 35.2.)
   if (!a.early) pdl_wait();
+  if (a.let) pdl_trigger();
   trace_stamp(tr, TR_k_cache_attn);
   int *status = a.status ? a.status : sh_status;
   CaWalk<BLK, CF_START, PAGES> w;

@@ -30,9 +30,10 @@ struct CacheAttnArgs {
   float4 *part_ml;                         // [phase][row][head]: its (m, l, l before rounding, what follows: see pack_follow)
   float *cont_o;                           // [CTA][128][HD], [CTA][128]: the segments that continue one
   float4 *cont_ml;
-  int with_prefix, with_own;               // dense: which keys this launch takes, the shared ones, the rows' own, or both
+  int with_prefix, own_from, own_to;       // dense: what this launch takes, the shared keys or not, and the own keys of sequences with so many query entries to a KV head
   int n_ctas, cont_base, cont_slots;       // CTAs of this launch, where its continuations' slots start, and slots of all launches
-  int early;                               // the launch in front is the other one of this call, of which this one needs nothing
+  int early;                               // the launch in front is the other one of this call, of which this one needs nothing ...
+  int let;                                 // ... and this one has the other behind it, which may begin where blocks of this one have left
   int look;                                // merge: most rows are one segment, and done
   int q_small;                             // query rows that the smaller of the two copies of Q takes
   int *status;
@@ -61,6 +62,7 @@ struct CaSeq {
     n = min(max(a.q_start[s + 1], q0), a.rows) - q0;
     len = min(max(a.kv_len[s], 0), a.c.pages_per_seq << a.c.page_shift);
   }
+  __device__ __forceinline__ bool taken(const CacheAttnArgs &a) const { return n * a.group >= a.own_from && n * a.group <= a.own_to; }      // by this launch
   __device__ __forceinline__ int tiles(const CacheAttnArgs &a) const { return (n + a.tile_rows - 1) / a.tile_rows; }
   // Tokens that some row of tile t sees (behind the last there may be anything), and units of its own ones: at least one, which leaves the row's
   // place in the partials in order.
@@ -119,7 +121,7 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
     if (tiles) at_tile(a);
     else u = u_end;                                          // (none: lengths that changed under way)
   }
-  // ... of the first sequence from this one on that has rows; by a whole warp, which looks at 32 sequences at a time (8 of 4096 slots with a row each: 33 us; one by one 65).
+  // ... of the first sequence from this one on that this launch takes; by a whole warp, which looks at 32 sequences at a time (8 of 4096 slots with a row each: 33 us; one by one 65).
   __device__ __forceinline__ void at_seq(const CacheAttnArgs &a, int seq) {
     q.n = 0;
     for (; seq < a.c.n_seqs; seq += 32) {
@@ -127,7 +129,7 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
       CaSeq t;
       t.q0 = t.n = t.len = 0;
       if (i < a.c.n_seqs) t = CaSeq(a, i);
-      const unsigned some = __ballot_sync(0xffffffffu, t.n > 0);
+      const unsigned some = __ballot_sync(0xffffffffu, t.taken(a));
       if (some) {
         const int first = __ffs(some) - 1;
         seq += first;
@@ -190,7 +192,7 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
       CaSeq t;
       for (int i = threadIdx.x; i < a.c.n_seqs; i += blockDim.x) {
         t = CaSeq(a, i);
-        own = a.with_own ? t.template all_units<BLK, START>(a) : 0ll;
+        own = t.taken(a) ? t.template all_units<BLK, START>(a) : 0ll;
         sum += own;
         if (t.n && t.len - t.n + (a.tree ? 0 : 1) < a.shared_tokens) sh.partial = 1;       // a row that does not see the whole prefix
         if (t.n) longest = max(longest, t.len);
@@ -213,7 +215,7 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
         for (int i0 = 0; i0 < a.c.n_seqs && next <= goal; i0 += blockDim.x) {
           const int i = i0 + threadIdx.x;
           if (i < a.c.n_seqs) t = CaSeq(a, i);
-          own = i < a.c.n_seqs && a.with_own ? t.template all_units<BLK, START>(a) : 0ll;
+          own = i < a.c.n_seqs && t.taken(a) ? t.template all_units<BLK, START>(a) : 0ll;
           sum = own;
           for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += x; }
           __syncthreads();

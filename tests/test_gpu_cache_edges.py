@@ -6,7 +6,7 @@ import torch
 
 from .test_gpu_cache_attn import dense
 from .test_gpu_cache_rows import i32, table
-from .util_cache import NAN, Pages, pools, tree_words
+from .util_cache import NAN, Pages, close, dense_reference, pools, tree_words
 
 pytestmark = pytest.mark.gpu
 
@@ -102,3 +102,51 @@ def test_slots_without_rows(n_seqs, busy, T, shared):
     pg = Pages(lengths, 2, 64, 16, shared=shared, seed=n_seqs)
     pg.table[:, :shared] = pg.table[busy[0], :shared]
     dense(pg, rows, 4)
+
+
+MIXED = [[1] * 7 + [40], [40, 0, 1, 0, 2, 0, 0, 3, 0, 0, 0, 0], [0] * 30 + [33, 1], [5, 0, 4, 0, 3, 0, 2, 0, 1, 0, 0, 0, 0, 0, 0, 0], [9] + [0] * 8, [4, 1, 0, 1], [200] + [1] * 60 + [0] * 200]
+
+
+@pytest.mark.parametrize("heads,hkv,d", [(2, 2, 64), (4, 2, 128), (3, 1, 256), (4, 1, 64), (8, 2, 128)])
+@pytest.mark.parametrize("T", MIXED)
+@pytest.mark.parametrize("shared", [0, 2])
+def test_prompts_beside_single_tokens(heads, hkv, d, T, shared):
+    lengths = [(0 if t == 0 and b % 2 else 32 + t + 37 * (b % 5)) for b, t in enumerate(T)]
+    pg = Pages(lengths, hkv, d, 16, shared=shared, seed=len(T))
+    pg.table[:, :shared] = pg.table[0, :shared]
+    dense(pg, T, heads)
+
+
+def test_prompts_beside_single_tokens_in_graphs():
+    """One captured call serves batches of every mixture, replayed one behind another with nothing between: the same bits as calls alone."""
+    from paper_2505_19201_b200 import api
+    most, heads = 48, 4
+    pg = Pages([200 + 7 * b for b in range(24)], 2, 128, 16, seed=3)
+    q = pg.queries(most, heads)
+    start, work = i32([0] * 25), torch.empty(api.dream_cache_attn_bytes(pg.cache, most, heads), dtype=torch.uint8, device="cuda")
+    lens, out = i32(pg.lengths), torch.zeros_like(q)
+    call = lambda o: api.dream_cache_attn(pg.cache, q, start, lens, o, work)  # noqa: E731
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        call(out)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call(out)
+    for T in ([1] * 24, [2] * 24, [40] + [0] * 20 + [1, 2, 3], [0] * 24, [0] * 23 + [48], [1] * 20 + [5, 5, 5, 5]):
+        starts = [sum(T[:b]) for b in range(25)]
+        start.copy_(i32(starts))
+        alone = torch.full_like(q, 7.0)
+        call(alone)
+        torch.cuda.synchronize()
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            for _ in range(5):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, alone)
+        if starts[-1]:
+            want, _, size = dense_reference(pg, q, starts)
+            close(out[:starts[-1]], want, size, "bf16")
+        assert (out[starts[-1]:] == 7.0).all()
