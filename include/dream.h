@@ -435,7 +435,8 @@ dream_status dream_cache_attn_bytes(const dream_cache *cache, int32_t n_heads, i
  * tokens up to its own, kv_len - T + i; with tree_mask (device uint32 [rows][4], the layout of dream_tree.mask; T <= 128) the tokens in front of the
  * T and those of the T whose bit is set.  Rows behind q_start[n_seqs] are left as they were.  A row that sees nothing gets zeros.
  *   shared_pages : the first so many entries of the page table are the same in every sequence (those of sequence 0 are read): their keys are
- *            read once for all rows instead of once per sequence.  0: nothing is shared.
+ *            read once for all rows instead of once per sequence.  0: nothing is shared.  ("Once": for each tile of up to 128 query entries of a KV head.  Where the sequences have
+ *            256 entries on the average each reads the shared keys with its own, tile by tile, which is at most half as many times again.)
  *   scale : finite, above zero (as a rule head_dim^-1/2)
  *   lse : device float [rows][n_heads], log-sum-exp of the scaled scores (-inf for a row that sees nothing), or NULL
  * What lies in a page behind a sequence's last token may be anything, NaN included; the tokens themselves are finite.

@@ -395,7 +395,7 @@ static const char *cache_attn_run(const dream_cache *cache, CacheAttnArgs &a, cu
   // More (row, head)s than threads that merge them are resident at once: a CTA continues one item at most, so most of them are done already, unless each has two parts.  (Seven
   // sequences of 500 rows behind 4096 tokens 297 us, without the look 325; of 128 rows 90 and 88.)
   const long long rh = (long long)a.rows * a.heads, per = 256 / (HD / 4);
-  a.look = (PAGES || !a.shared_tokens) && rh > 148 * 8 * per;
+  a.look = (PAGES || !a.shared_tokens || entries >= 256LL * a.c.n_seqs) && rh > 148 * 8 * per;
   const long long blocks = a.look ? (rh + MERGE_LOOK - 1) / MERGE_LOOK : (rh + per - 1) / per;
   return why ? why : cache_launch(k_cache_merge<T, HD, PAGES>, dim3((unsigned)blocks), 256, 0, stream, a);
 }
@@ -419,10 +419,7 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   if (s) return s;
   if (shared_pages < 0 || shared_pages > cache->pages_per_seq) return fail(nullptr, DREAM_E_ARG, "%s: shared_pages = %d outside 0..pages_per_seq = %d", who, shared_pages, cache->pages_per_seq);
   a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask;
-  // Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item with their own keys, whose parts need not be put together.  (Seven
-  // sequences behind 4096 tokens, 16 heads over 8 of 256, with 128 rows each 90 us, and 110 with the prefix by itself; with 64 rows 61 and 64, but their last tiles are full, which at
-  // other lengths they are not; with 32 rows 46 and 40.)
-  a.shared_tokens = (long long)rows * a.group >= 256LL * cache->n_seqs ? 0 : shared_pages * cache->page_tokens;
+  a.shared_tokens = shared_pages * cache->page_tokens;
   // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits (with what an item's start counts)
   auto units = [&](long long n_pages) { return (n_pages * cache->page_tokens / 64 + 1 + CF_START) * cache->n_kv_heads; };
   const int tile = 128 / a.group;                          // rows of one (CF_ENTRIES or fewer are one tile in either kernel)

@@ -404,7 +404,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (ql == 0) pair_sum[pair][half][quad + 8 * k] = make_float2(l[k], l_true[k]);
       }
       ca_sync(pair);
-      const bool starts = s.b0 == 0, final = starts && !s.follow && (PAGES || !a.shared_tokens), row_on = !PAGES || s.seq >= 0;
+      const bool starts = s.b0 == 0, final = starts && !s.follow && (PAGES || !plan.shared), row_on = !PAGES || s.seq >= 0;
       float inv[2];
       long long at[2];
       int r[2], h[2];

@@ -384,7 +384,7 @@ k_cache_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       for (int e = 0; e < NE; ++e) if (t == e) refs[e] = m_ref[e];
       cf_sync();
       // a thread per entry: what the segment leaves of it, and where its O goes
-      const bool final = s.b0 == 0 && !s.follow && (PAGES || !a.shared_tokens);
+      const bool final = s.b0 == 0 && !s.follow && (PAGES || !plan.shared);
       if (t < n_e && t < NE) {
         const float2 s0 = sums[0][t], s1 = sums[1][t], s2 = sums[2][t], s3 = sums[3][t];
         const float sl = (s0.x + s1.x) + (s2.x + s3.x), st = (s0.y + s1.y) + (s2.y + s3.y), m = refs[t] == -INFINITY ? refs[t] : refs[t] - CaType<T>::SHIFT;

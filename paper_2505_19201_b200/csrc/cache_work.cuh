@@ -24,7 +24,7 @@ struct CacheAttnArgs {
   const uint32_t *tree;                    // dense: [rows][4], or null
   const int *row_seq, *row_pos, *ids;      // pages
   int budget, rows, heads, group, tile_rows;
-  int shared_tokens;                       // dense: keys [0, shared_tokens) are everybody's
+  int shared_tokens;                       // dense: keys [0, shared_tokens) are everybody's (see ca_shared)
   float scale_log2;
   float *part_o;                           // [phase][row][head][HD]: what the segment that starts an item leaves ...
   float4 *part_ml;                         // [phase][row][head]: its (m, l, l before rounding, what follows: see pack_follow)
@@ -53,6 +53,14 @@ __device__ __forceinline__ uint32_t pack2(float x, float y, f16) { __half2 h = _
 __device__ __forceinline__ float2 unpack2(uint32_t w, bf16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 __device__ __forceinline__ float2 unpack2(uint32_t w, f16) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
 
+// The shared keys that are an item of their own, against the rows of all sequences.  Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item
+// with their own keys, whose parts need not be put together: 0.  (Seven sequences behind 4096 tokens, 16 heads over 8 of 256, with 128 rows each 90 us, and 110 with the prefix by itself;
+// with 64 rows 61 and 64, but their last tiles are full, which at other lengths they are not; with 32 rows 46 and 40.)  From two tiles to a sequence on, on the average over the
+// sequences, the tiles by sequence are at most half as many again as those of all rows together, however the rows are spread: one more for each sequence.  The rows counted are those there
+// are, not those that a captured call has room for.
+__device__ __forceinline__ int ca_shared(const CacheAttnArgs &a, int n_rows) { return (long long)n_rows * a.group >= 256ll * a.c.n_seqs ? 0 : a.shared_tokens; }
+__device__ __forceinline__ int ca_rows(const CacheAttnArgs &a) { return min(max(a.q_start[a.c.n_seqs], 0), a.rows); }
+
 // A sequence as the call gives it, held within the buffers whatever its numbers say.
 struct CaSeq {
   int q0, n, len;                          // first row, rows, tokens
@@ -67,10 +75,10 @@ struct CaSeq {
   // Tokens that some row of tile t sees (behind the last there may be anything), and units of its own ones: at least one, which leaves the row's
   // place in the partials in order.
   __device__ __forceinline__ int end(const CacheAttnArgs &a, int t) const { return a.tree ? len : max(0, len - n + min(n, (t + 1) * a.tile_rows)); }
-  template <int BLK> __device__ __forceinline__ int units(const CacheAttnArgs &a, int t) const { return max(1, (end(a, t) - a.shared_tokens + BLK - 1) / BLK); }
-  template <int BLK, int START> __device__ __forceinline__ long long all_units(const CacheAttnArgs &a) const {
+  template <int BLK> __device__ __forceinline__ int units(const CacheAttnArgs &a, int t, int shared) const { return max(1, (end(a, t) - shared + BLK - 1) / BLK); }
+  template <int BLK, int START> __device__ __forceinline__ long long all_units(const CacheAttnArgs &a, int shared) const {
     long long sum = 0;
-    for (int t = tiles(a) - 1; t >= 0; --t) sum += units<BLK>(a, t) + START;
+    for (int t = tiles(a) - 1; t >= 0; --t) sum += units<BLK>(a, t, shared) + START;
     return sum * a.c.hkv;
   }
 };
@@ -92,7 +100,7 @@ __device__ __forceinline__ int ca_seq_of(const CacheAttnArgs &a, int r) {
   return lo;
 }
 
-struct CaPlanShared { long long sum[32], at; CaSeq q; int seq, partial, longest; };      // partial and longest start as 0
+struct CaPlanShared { long long sum[32], at; CaSeq q; int seq, partial, longest, shared; };      // partial and longest start as 0
 
 // a / b for a from 0 and b from 1 on: a division of 64-bit numbers takes several times that of 32-bit ones, and hardly a call has as many units.
 __device__ __forceinline__ long long ca_div(long long a, int b) { return a >> 31 ? a / b : (long long)((int)a / b); }
@@ -100,7 +108,7 @@ __device__ __forceinline__ long long ca_div(long long a, int b) { return a >> 31
 // What a CTA has to do: units [u, u_end) of the call, as segments.  Every item is reached from the one before it by counting on; lengths are read once per sequence.
 template <int BLK, int START, bool PAGES> struct CaWalk {
   long long u, u_end, u_first, item;       // item: the first unit of the item at hand, which has START + blocks
-  int upc, blocks, tile, tiles;
+  int upc, blocks, tile, tiles, shared;
   int prefix_tiles, prefix_blocks, prefix_rows;
   CaSeq q;
   CaSeg s;
@@ -110,12 +118,12 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
     if (row < a.rows) { s.seq = a.row_seq[row]; s.end = a.row_pos[row]; }
   }
   __device__ __forceinline__ void at_tile(const CacheAttnArgs &a) {                       // own keys: the first KV head of a tile of sequence s.seq
-    blocks = q.template units<BLK>(a, tile);
+    blocks = q.template units<BLK>(a, tile, shared);
     s.row0 = q.q0 + tile * a.tile_rows; s.rows = min(a.tile_rows, q.n - tile * a.tile_rows);
     s.end = q.end(a, tile); s.tail0 = q.len - q.n; s.q0 = q.q0; s.kvh = 0;
   }
   __device__ __forceinline__ void at_own(const CacheAttnArgs &a, int seq) {               // ... the first tile of this sequence
-    s.phase = 1; s.seq = seq; s.key0 = a.shared_tokens;
+    s.phase = 1; s.seq = seq; s.key0 = shared;
     tile = 0;
     tiles = q.tiles(a);
     if (tiles) at_tile(a);
@@ -175,15 +183,17 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
   __device__ __forceinline__ void plan(const CacheAttnArgs &a, CaPlanShared &sh, int *status) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, cta = blockIdx.x;
     long long total, prefix_units = 0;
-    tile = tiles = 0;
+    tile = tiles = shared = 0;
     s.key0 = s.seq = s.kvh = s.tail0 = s.q0 = 0;
     if (PAGES) {
       blocks = max(1, (a.budget * a.c.page_tokens + BLK - 1) / BLK);
       total = (long long)a.rows * a.c.hkv * (blocks + START);
       upc = (int)max(1ll, ca_div(total + a.n_ctas - 1, a.n_ctas));
     } else {
-      prefix_rows = min(max(a.q_start[a.c.n_seqs], 0), a.rows);
-      prefix_blocks = (a.shared_tokens + BLK - 1) / BLK;
+      prefix_rows = ca_rows(a);
+      shared = ca_shared(a, prefix_rows);
+      if (threadIdx.x == 0) sh.shared = shared;
+      prefix_blocks = (shared + BLK - 1) / BLK;
       prefix_tiles = prefix_blocks && a.with_prefix ? (prefix_rows + a.tile_rows - 1) / a.tile_rows : 0;
       prefix_units = (long long)prefix_tiles * (prefix_blocks + START) * a.c.hkv;
       // units in front of each sequence's, a sequence per thread at a time; once around for most batches, twice where there are more sequences than threads
@@ -192,9 +202,9 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
       CaSeq t;
       for (int i = threadIdx.x; i < a.c.n_seqs; i += blockDim.x) {
         t = CaSeq(a, i);
-        own = t.taken(a) ? t.template all_units<BLK, START>(a) : 0ll;
+        own = t.taken(a) ? t.template all_units<BLK, START>(a, shared) : 0ll;
         sum += own;
-        if (t.n && t.len - t.n + (a.tree ? 0 : 1) < a.shared_tokens) sh.partial = 1;       // a row that does not see the whole prefix
+        if (t.n && t.len - t.n + (a.tree ? 0 : 1) < shared) sh.partial = 1;       // a row that does not see the whole prefix
         if (t.n) longest = max(longest, t.len);
         if (cta == 0 && (t.q0 != a.q_start[i] || t.q0 + t.n != a.q_start[i + 1] || t.len != a.kv_len[i])) cache_bad_index(status);
       }
@@ -215,7 +225,7 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
         for (int i0 = 0; i0 < a.c.n_seqs && next <= goal; i0 += blockDim.x) {
           const int i = i0 + threadIdx.x;
           if (i < a.c.n_seqs) t = CaSeq(a, i);
-          own = i < a.c.n_seqs && t.taken(a) ? t.template all_units<BLK, START>(a) : 0ll;
+          own = i < a.c.n_seqs && t.taken(a) ? t.template all_units<BLK, START>(a, shared) : 0ll;
           sum = own;
           for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += x; }
           __syncthreads();
@@ -241,7 +251,7 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
       item = (long long)i * (blocks + START);
     } else if (u < prefix_units) {
       const int i = (int)u / (prefix_blocks + START);
-      s.phase = 0; s.end = min(a.shared_tokens, sh.longest);                               // behind everybody's last token there may be anything
+      s.phase = 0; s.end = min(shared, sh.longest);                               // behind everybody's last token there may be anything
       blocks = prefix_blocks;
       s.kvh = i / prefix_tiles; tile = i - s.kvh * prefix_tiles;
       item = (long long)i * (prefix_blocks + START);
@@ -374,7 +384,7 @@ __device__ __forceinline__ int ca_produce(const CacheAttnArgs &a, CaWalk<BLK, ST
 // Where most rows are one segment, and done, a block looks over MERGE_LOOK of them first (look), and does not load the partial results that are not there.
 #define MERGE_LOOK 32                    // of a block's first warp, a lane each
 template <typename T, int HD, bool PAGES>
-__device__ __forceinline__ void merge_row(const CacheAttnArgs &a, long long rh, int r, int c0) {
+__device__ __forceinline__ void merge_row(const CacheAttnArgs &a, bool shared, long long rh, int r, int c0) {
   float M = -INFINITY, L = 0.f, Lt = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](const float4 &ml, const float4 &x) {
@@ -385,7 +395,7 @@ __device__ __forceinline__ void merge_row(const CacheAttnArgs &a, long long rh, 
     M = Mn;
   };
   // what starts the row's items, shared and own
-  const int first = PAGES || a.shared_tokens ? 0 : 1, last = PAGES ? 0 : 1;
+  const int first = PAGES || shared ? 0 : 1, last = PAGES ? 0 : 1;
   float4 ml[2], x[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -427,12 +437,13 @@ __global__ void __launch_bounds__(256, 4)
 k_cache_merge(const __grid_constant__ CacheAttnArgs a) {
   kernel_entry(TR_k_cache_merge);
   constexpr int V = HD / 4, PER = 256 / V;
-  const int rows = PAGES ? a.rows : min(a.rows, a.q_start[a.c.n_seqs]);
+  const int rows = PAGES ? a.rows : ca_rows(a);
+  const bool shared = !PAGES && ca_shared(a, rows) > 0;
   const int c0 = (int)(threadIdx.x % V) * 4;
   if (!a.look) {
     const long long rh = (long long)blockIdx.x * PER + threadIdx.x / V;
     const int r = (int)ca_div(rh, a.heads);
-    if (r < rows) merge_row<T, HD, PAGES>(a, rh, r, c0);
+    if (r < rows) merge_row<T, HD, PAGES>(a, shared, rh, r, c0);
     return;
   }
   __shared__ int list[MERGE_LOOK], n_list;
@@ -449,6 +460,6 @@ k_cache_merge(const __grid_constant__ CacheAttnArgs a) {
   const int n = n_list;
   for (int j = t / V; j < n; j += PER) {
     const long long rh = base + list[j];
-    merge_row<T, HD, PAGES>(a, rh, (int)ca_div(rh, a.heads), c0);
+    merge_row<T, HD, PAGES>(a, shared, rh, (int)ca_div(rh, a.heads), c0);
   }
 }

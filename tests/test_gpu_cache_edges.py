@@ -150,3 +150,11 @@ def test_prompts_beside_single_tokens_in_graphs():
             want, _, size = dense_reference(pg, q, starts)
             close(out[:starts[-1]], want, size, "bf16")
         assert (out[starts[-1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("T", [[1] * 4, [64, 64, 64, 63], [64] * 4, [1, 254, 0, 1], [3, 250, 0, 3]])
+@pytest.mark.parametrize("behind", [0, 3, 600])
+def test_rows_behind_the_last_do_not_say_how_the_prefix_is_read(T, behind):
+    """Around 256 query entries to a sequence, with room for more rows than there are."""
+    pg = Pages([64 + max(t, 1) + 5 * b for b, t in enumerate(T)], 2, 128, 32, shared=2, seed=sum(T))
+    dense(pg, T, 8, behind=behind)
