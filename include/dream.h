@@ -398,7 +398,7 @@ dream_status dream_distill_grad(const void *logits, int32_t dtype, int32_t rows,
  *   workspace : device, 256-byte aligned, of the size that dream_cache_attn_bytes (dream_cache_select_bytes) says; what it holds does not
  *            outlive the call, and two calls that may run at the same time need one each (so do two captured graphs that may)
  *   status : device int32[2], zeroed by the caller once, or NULL.  Word 0 becomes 1 when a bounded wait in a kernel ran out (word 1: which), 2
- *            when a sequence, token, position or page number was out of range.  What such a number stands for is left out: rows are not written, keys not seen.
+ *            when a sequence, token, position, row or page number was out of range.  What such a number stands for is left out: rows are not written, keys not seen.
  *   cuda_stream : a cudaStream_t of the current device (NULL = legacy default stream)
  * Asynchronous; nothing is allocated; errors are reported through dream_last_error(NULL), before anything is enqueued. */
 typedef struct {

@@ -206,7 +206,7 @@ template <int BLK, int START, bool PAGES> struct CaWalk {
         sum += own;
         if (t.n && t.len - t.n + (a.tree ? 0 : 1) < shared) sh.partial = 1;       // a row that does not see the whole prefix
         if (t.n) longest = max(longest, t.len);
-        if (cta == 0 && (t.q0 != a.q_start[i] || t.q0 + t.n != a.q_start[i + 1] || t.len != a.kv_len[i])) cache_bad_index(status);
+        if (cta == 0 && (t.q0 != a.q_start[i] || (i == 0 && t.q0) || t.q0 + t.n != a.q_start[i + 1] || t.len != a.kv_len[i])) cache_bad_index(status);
       }
       for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += x; }
       longest = __reduce_max_sync(0xffffffffu, longest);
@@ -437,13 +437,13 @@ __global__ void __launch_bounds__(256, 4)
 k_cache_merge(const __grid_constant__ CacheAttnArgs a) {
   kernel_entry(TR_k_cache_merge);
   constexpr int V = HD / 4, PER = 256 / V;
-  const int rows = PAGES ? a.rows : ca_rows(a);
+  const int rows = PAGES ? a.rows : ca_rows(a), first = PAGES ? 0 : a.q_start[0];      // (rows in front of the first sequence are nobody's, and have no parts)
   const bool shared = !PAGES && ca_shared(a, rows) > 0;
   const int c0 = (int)(threadIdx.x % V) * 4;
   if (!a.look) {
     const long long rh = (long long)blockIdx.x * PER + threadIdx.x / V;
     const int r = (int)ca_div(rh, a.heads);
-    if (r < rows) merge_row<T, HD, PAGES>(a, shared, rh, r, c0);
+    if (r >= first && r < rows) merge_row<T, HD, PAGES>(a, shared, rh, r, c0);
     return;
   }
   __shared__ int list[MERGE_LOOK], n_list;
@@ -451,7 +451,7 @@ k_cache_merge(const __grid_constant__ CacheAttnArgs a) {
   const int t = threadIdx.x;
   if (t < 32) {
     const long long rh = base + t;
-    const bool open = t < MERGE_LOOK && ca_div(rh, a.heads) < rows && (__float_as_int(a.part_ml[(PAGES ? 0ll : (long long)a.rows * a.heads) + rh].w) >> 7 & 0x7ff) != CA_DONE;
+    const bool open = t < MERGE_LOOK && ca_div(rh, a.heads) < rows && ca_div(rh, a.heads) >= first && (__float_as_int(a.part_ml[(PAGES ? 0ll : (long long)a.rows * a.heads) + rh].w) >> 7 & 0x7ff) != CA_DONE;
     const unsigned b = __ballot_sync(0xffffffffu, open);
     if (open) list[__popc(b & ((1u << t) - 1u))] = t;
     if (t == 0) n_list = __popc(b);

@@ -6,7 +6,7 @@ import torch
 
 from .test_gpu_cache_attn import dense
 from .test_gpu_cache_rows import i32, table
-from .util_cache import NAN, Pages, close, dense_reference, pools, tree_words
+from .util_cache import NAN, Pages, close, close_lse, dense_reference, pools, tree_words
 
 pytestmark = pytest.mark.gpu
 
@@ -158,3 +158,19 @@ def test_rows_behind_the_last_do_not_say_how_the_prefix_is_read(T, behind):
     """Around 256 query entries to a sequence, with room for more rows than there are."""
     pg = Pages([64 + max(t, 1) + 5 * b for b, t in enumerate(T)], 2, 128, 32, shared=2, seed=sum(T))
     dense(pg, T, 8, behind=behind)
+
+
+@pytest.mark.parametrize("T,heads,shared", [([3, 1], 4, 0), ([1, 1], 4, 2), ([90, 70], 8, 2), ([300, 400], 8, 0)])
+def test_rows_in_front_of_the_first_sequence_are_nobodys(T, heads, shared):
+    """Starts that do not begin at 0 are out of range: reported, and the rows in front are left as they were."""
+    from paper_2505_19201_b200 import api
+    pg = Pages([t + 64 for t in T], 2, 64, 32, shared=shared)
+    front, n = 2, sum(T)
+    q = pg.queries(front + n, heads)
+    out, lse, status = torch.full_like(q, 77.0), torch.full((front + n, heads), 77.0, device="cuda"), i32([0, 0])
+    work = torch.full((api.dream_cache_attn_bytes(pg.cache, front + n, heads),), 255, dtype=torch.uint8, device="cuda")
+    api.dream_cache_attn(pg.cache, q, i32([front, front + T[0], front + n]), i32(pg.lengths), out, work, shared_pages=shared, lse=lse, status=status)
+    want, wl, size = dense_reference(pg, q[front:], [0, T[0], n])
+    close(out[front:], want, size, "bf16")
+    close_lse(lse[front:], wl)
+    assert (out[:front] == 77.0).all() and (lse[:front] == 77.0).all() and status[0] == 2
