@@ -420,10 +420,12 @@ extern "C" dream_status dream_cache_attn(const dream_cache *cache, const void *q
   if (shared_pages < 0 || shared_pages > cache->pages_per_seq) return fail(nullptr, DREAM_E_ARG, "%s: shared_pages = %d outside 0..pages_per_seq = %d", who, shared_pages, cache->pages_per_seq);
   a.q_start = q_start; a.kv_len = kv_len; a.tree = tree_mask;
   a.shared_tokens = shared_pages * cache->page_tokens;
-  // the units of the prefix, and those of one tile of a sequence, are counted in 32 bits (with what an item's start counts)
+  // The units of the prefix, those of one tile of a sequence and those of a CTA are counted in 32 bits (with what an item's start counts).
   auto units = [&](long long n_pages) { return (n_pages * cache->page_tokens / 64 + 1 + CF_START) * cache->n_kv_heads; };
   const int tile = 128 / a.group;                          // rows of one (CF_ENTRIES or fewer are one tile in either kernel)
-  if (units(cache->pages_per_seq) > 0x7fffffffLL || (shared_pages && units(shared_pages) * ((rows + tile - 1) / tile) > 0x7fffffffLL))
+  const long long tiles = (rows + tile - 1) / tile, few_tiles = a.group <= CF_ENTRIES && rows == cache->n_seqs ? rows : 0;      // (the kernel for few alone takes up to a row at a time)
+  const long long own = units(cache->pages_per_seq), all = own * (tiles + cache->n_seqs + few_tiles) + (shared_pages ? units(shared_pages) * tiles : 0);
+  if (own > 0x7fffffffLL || (shared_pages && units(shared_pages) * tiles > 0x7fffffffLL) || all / 128 > 0x7fffffffLL)      // (no fewer CTAs than that)
     return fail(nullptr, DREAM_E_CAPACITY, "%s: %d rows over sequences of %d pages in one call", who, rows, cache->pages_per_seq);
   const char *why = cache_attn_launch<false>(cache, a, (cudaStream_t)cuda_stream);
   return why ? fail(nullptr, DREAM_E_CUDA, "%s: %s", who, why) : DREAM_OK;
