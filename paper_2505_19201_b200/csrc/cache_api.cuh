@@ -160,7 +160,7 @@ extern "C" dream_status dream_cache_append(const dream_cache *cache, const void 
 }
 
 // The parts of the selection's workspace; how many bytes they are.
-static size_t cache_select_room(const CacheView &v, int hd, int rows, void *workspace, CacheSelectArgs *a) {
+static size_t cache_select_room(const CacheView &v, int rows, void *workspace, CacheSelectArgs *a) {
   // Blocks of the scores for each (row, KV head): as many as fill the GPU, and no more than there are pages for
   const long long n = (long long)rows * v.hkv;
   const int most = (v.pages_per_seq + SCORE_PAGES - 1) / SCORE_PAGES;
@@ -177,7 +177,7 @@ extern "C" dream_status dream_cache_select_bytes(const dream_cache *cache, int32
   if (!s) s = cache_heads("dream_cache_select_bytes", cache, rows, cache->n_kv_heads);
   if (s) return s;
   if (!bytes) return fail(nullptr, DREAM_E_ARG, "dream_cache_select_bytes: null argument");
-  *bytes = cache_select_room(v, cache->head_dim, rows, nullptr, nullptr);
+  *bytes = cache_select_room(v, rows, nullptr, nullptr);
   return DREAM_OK;
 }
 
@@ -221,7 +221,7 @@ extern "C" dream_status dream_cache_select(const dream_cache *cache, const void 
   if (s) return s;
   a.q = q; a.q_ld = q_ld; a.row_seq = row_seq; a.row_pos = row_pos; a.group = n_heads / a.c.hkv;
   a.budget = budget; a.keep_first = keep_first; a.keep_last = keep_last; a.ids = ids; a.status = status;
-  cache_select_room(a.c, cache->head_dim, rows, workspace, &a);
+  cache_select_room(a.c, rows, workspace, &a);
   const bool bf = cache->dtype == DREAM_BF16;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   const char *why = cache->head_dim == 64 ? (bf ? cache_select_run<bf16, 64>(a, rows, stream) : cache_select_run<f16, 64>(a, rows, stream))

@@ -133,6 +133,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   }
   static_assert(CA_RING == 16, "a lane inits each of the segments' barriers");
   static_assert(CA_RING > STAGES + SB + 1, "what the producer leaves is read until a unit's P is done");
+  static_assert(sizeof(uint64_t) * (4 * STAGES + 3 * SB + 2 + CA_RING) + 16 + sizeof(uint4) * CA_RING + sizeof(CaSeg) * CA_RING + 8 <= 2048, "room for the barriers and rings");
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -156,7 +157,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   } else if (warp == 3) {
     gave_up = ca_produce<HD, STAGES, 1>(a, w, CaRing{v_full, v_empty, nullptr, v_s, nullptr, nullptr, &map_v, abort_flag, status}, lane);
   } else if (warp == 1) {
-    // ------------------------------------------------------------------ queries, and S = Q K^T: both operands K-major, N = 64
+    // ------------------------------------------------------------------ queries, and S = Q K^T: both operands K-major, N = BLK
     constexpr uint32_t idesc = (1u << 4) | CaType<T>::IDESC | ((uint32_t)(BLK >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     const uint64_t qd = smem_desc(smem_u32(q_s)), kd = smem_desc(smem_u32(k_s));
     const uint32_t s_addr = tmem_base + HD;

@@ -34,6 +34,10 @@ template <typename T> __device__ __forceinline__ uint4 pack8(const float (&f)[8]
   return q;
 }
 
+// A pair in 32 bits.
+__device__ __forceinline__ float2 unpack2(uint32_t w, bf16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ float2 unpack2(uint32_t w, f16) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
+
 template <typename T> struct CaInf;
 template <> struct CaInf<bf16> { static constexpr uint32_t BITS = 0x7f80u; };
 template <> struct CaInf<f16> { static constexpr uint32_t BITS = 0x7c00u; };
@@ -113,9 +117,9 @@ __device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, i
     missing |= !here;
   }
   if (__syncthreads_or(missing)) {
-    // By the page, which another sequence may name too.  Eight look-ups of a thread under way together: 16900 rows of 20 sequences, each of which begins inside a page, take 151 us (one by
+    // By the page, which another sequence may name too.  Four look-ups of a thread under way together: 16900 rows of 20 sequences, each of which begins inside a page, take 154 us (one by
     // one 178; by the sequence alone, which is not enough, 145).
-    constexpr int AT_ONCE = 8;
+    constexpr int AT_ONCE = 4;
     for (int r0 = tid; r0 < a.rows; r0 += AT_ONCE * CACHE_THREADS) {
       int other[AT_ONCE], at[AT_ONCE];
 #pragma unroll
@@ -189,7 +193,8 @@ __device__ __forceinline__ void append_bounds(const CacheAppendArgs &a, int r, i
 
 // Bound by HBM, or by latency where there are few rows.  The grid is in chunks of rows.  The first blocks of a chunk look for rows that fill a page, a few rows and one
 // KV head each; the others move rows: a thread has one unit of a row and takes it from HEADS heads (queries, then keys, then values), two at a time; the row's place and
-// the unit's rotary factors it looks up once.  Measured with 5871 rows of 16 + 2 x 8 heads of 256, 193 MB: 42.9 us (4.5 TB/s), 37.5 of them without bounds; with 16 heads
+// the unit's rotary factors it looks up once.  Four blocks to an SM, which takes 12 to 36 bytes of a thread's registers to memory and back; with three, and none, 44.0 us for the 42.4
+// below, 163 for the 154 above.  Measured with 5871 rows of 16 + 2 x 8 heads of 256, 193 MB: 42.4 us (4.5 TB/s), 37.1 without bounds; with 16 heads
 // a thread 46.2 (one and a quarter waves of blocks), with 4 heads 44.3 (more look-ups); with four units of any heads a thread, each with factors and divisions of its own,
 // 54; with all the blocks that look for pages at the grid's start, four times the rows take 155 us in place of 145 (their rows are read from HBM twice).
 #define APPEND_HEADS 8
@@ -315,8 +320,6 @@ __device__ __forceinline__ void score_mma(float (&d)[4], uint32_t a0, uint32_t a
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
                : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-__device__ __forceinline__ float2 widen2(uint32_t w, bf16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ float2 widen2(uint32_t w, f16) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
 
 // Scores in 32 bits, with a bound on how far they are off.  (Which pages are kept is a matter of the scores in 64 bits, but only for the few near the cut, which
 // k_cache_select looks at again.)  sum_d max(q_d lo_d, q_d hi_d) is a product of the bounds with q's positive part and its negative one, [hi | lo] [q+ ; q-]: a
@@ -330,7 +333,9 @@ __device__ __forceinline__ float2 widen2(uint32_t w, f16) { return __half22float
 // 32 x 2^-23 = 2^-18 of the largest product there may be, max |q_d| times the largest bound there is (met in 2.5 million sums: 2^-21).  The sums are added in 32 bits, each time wrong by
 // 2^-24 of a partial sum, which is no larger than sum |q_d| times the largest bound; one more such error for the rounding of the exact score, and four for the bound's own.
 #define SCORE_PAGES (CACHE_THREADS / 32 * 16)              // pages that a block has under way
-#define SCORE_BLOCKS 4                                     // to an SM: few registers a thread and many blocks; see below
+// Blocks to an SM: few registers a thread, 12 to 20 bytes of which go to memory and back, and many blocks (three, and none: 64 rows 82.7 us for 67.7, 8 rows 19.6 for 18.0, 9 rows of
+// small pages 32.4 for 28.4).
+#define SCORE_BLOCKS 4
 template <typename T, int HD>
 __global__ void __launch_bounds__(CACHE_THREADS, SCORE_BLOCKS)
 k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
@@ -452,7 +457,7 @@ k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
   if (threadIdx.x == 0) {
     uint32_t top = top_s[0];
     for (int w = 1; w < CACHE_THREADS / 32; ++w) top = max_pair(top, top_s[w], T());
-    const float2 t = widen2(top, T());
+    const float2 t = unpack2(top, T());
     // (and what products below the smallest normal number lose)
     a.off[(long long)blockIdx.x * a.score_blocks + blockIdx.y] = ((HD / 8) * 0x1p-18f * q_top_s + (HD / 8 + 5) * 0x1p-24f * q1_s) * fmaxf(t.x, t.y) + 0x1p-116f;
   }

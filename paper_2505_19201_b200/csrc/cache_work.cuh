@@ -50,8 +50,6 @@ template <> struct CaType<bf16> { static constexpr float SHIFT = 0.f, RESCALE = 
 template <> struct CaType<f16> { static constexpr float SHIFT = 10.f, RESCALE = 4.f; static constexpr uint32_t IDESC = 0u; };
 __device__ __forceinline__ uint32_t pack2(float x, float y, bf16) { __nv_bfloat162 h = __floats2bfloat162_rn(x, y); return *reinterpret_cast<uint32_t *>(&h); }
 __device__ __forceinline__ uint32_t pack2(float x, float y, f16) { __half2 h = __floats2half2_rn(x, y); return *reinterpret_cast<uint32_t *>(&h); }
-__device__ __forceinline__ float2 unpack2(uint32_t w, bf16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ float2 unpack2(uint32_t w, f16) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
 
 // The shared keys that are an item of their own, against the rows of all sequences.  Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item
 // with their own keys, whose parts need not be put together: 0.  (Seven sequences behind 4096 tokens, 16 heads over 8 of 256, with 128 rows each 90 us, and 110 with the prefix by itself;
