@@ -328,7 +328,7 @@ __device__ __forceinline__ void score_mma(float (&d)[4], uint32_t a0, uint32_t a
 // Selection as a whole, with 64 pages kept, before (a lane had eight channels of a page, multiplied, added one by one and across lanes: six times the instructions) and now: 8 rows
 // against 1024 pages, 32 heads over 8 of 128, 23.9 and 17.9 us; 64 rows 93 and 68; one row against 2048 pages 15.2 and 10.6; 9 rows against 1876 pages of 16 tokens, 16 over 8 of 256, 35 and 28.
 // (Two or four runs of 32 channels under way in a lane take registers from blocks: 64 rows 91 us and 69, 8 rows 19.0 and 21.6.)
-// A sum that is no number, as infinite bounds times 0 make it, is formed again from 64 bits.
+// A sum that is no finite number, as infinite bounds make it or a part of it past the largest number of 32 bits, is formed again from 64 bits.
 // The bound.  Each of HD / 8 instructions adds 16 exact products to zero; of each product it may lose 2^-23 of the largest, and of its result, no larger than 16 of these, as much:
 // 32 x 2^-23 = 2^-18 of the largest product there may be, max |q_d| times the largest bound there is (met in 2.5 million sums: 2^-21).  The sums are added in 32 bits, each time wrong by
 // 2^-24 of a partial sum, which is no larger than sum |q_d| times the largest bound; one more such error for the rounding of the exact score, and four for the bound's own.
@@ -426,7 +426,7 @@ k_cache_scores(const __grid_constant__ CacheSelectArgs a) {
       for (int k = 0; k < 2; ++k) {
         const int g = g0 + 2 * (lane & 3);
         const float s0 = g < a.group ? v[2 * k] : -INFINITY, s1 = g + 1 < a.group ? v[2 * k + 1] : -INFINITY;
-        odd[k] = s0 != s0 || s1 != s1;
+        odd[k] = (g < a.group && !(fabsf(s0) < INFINITY)) || (g + 1 < a.group && !(fabsf(s1) < INFINITY));
         float f = fmaxf(s0, s1);
         f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, 1));
         best[k] = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, 2));

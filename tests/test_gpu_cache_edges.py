@@ -174,3 +174,21 @@ def test_rows_in_front_of_the_first_sequence_are_nobodys(T, heads, shared):
     close(out[front:], want, size, "bf16")
     close_lse(lse[front:], wl)
     assert (out[:front] == 77.0).all() and (lse[:front] == 77.0).all() and status[0] == 2
+
+
+def test_selection_with_sums_past_the_largest_number_on_the_way():
+    """A part of a page's sum is past the largest number of 32 bits, the sum itself is not: another page's is larger."""
+    from paper_2505_19201_b200 import api
+    n, big = 40, 2.0 ** 63
+    k = torch.zeros(n, 1, 16, 64, dtype=torch.bfloat16, device="cuda")
+    bounds = torch.zeros(n, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    bounds[7, 0, :, [0, 8]], bounds[7, 0, :, 40] = big, -big                    # 2^127 + 2^127 - 2^127
+    bounds[30, 0, :, 0] = 1.5 * big
+    cache = api.Cache(k, k.clone(), i32([list(range(n))]), bounds)
+    q = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    q[0, 0, [0, 8, 40]] = 2.0 ** 64
+    for budget, want in ((3, [0, 30, 39]), (4, [0, 7, 30, 39])):
+        ids = torch.zeros(1, 1, budget, dtype=torch.int32, device="cuda")
+        work = torch.full((api.dream_cache_select_bytes(cache, 1),), 255, dtype=torch.uint8, device="cuda")
+        api.dream_cache_select(cache, q, i32([0]), i32([n * 16 - 1]), ids, work, keep_first=1, keep_last=1)
+        assert ids[0, 0].tolist() == want
