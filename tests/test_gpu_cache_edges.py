@@ -192,3 +192,92 @@ def test_selection_with_sums_past_the_largest_number_on_the_way():
         work = torch.full((api.dream_cache_select_bytes(cache, 1),), 255, dtype=torch.uint8, device="cuda")
         api.dream_cache_select(cache, q, i32([0]), i32([n * 16 - 1]), ids, work, keep_first=1, keep_last=1)
         assert ids[0, 0].tolist() == want
+
+
+def test_wrappers_refuse_before_anything_is_enqueued():
+    """Every refusal is the library's or the wrapper's own, with its code, and leaves the output and the device as they were."""
+    from paper_2505_19201_b200 import api
+    E_ARG, E_NOMEM = -1, -3
+    pg = Pages([40, 20], 2, 64, 16)
+    q, n, start = pg.queries(2, 4), i32([40, 20]), i32([0, 1, 2])
+    room = torch.empty(api.dream_cache_attn_bytes(pg.cache, 2, 4), dtype=torch.uint8, device="cuda")
+    out, ids, seq, pos = torch.full_like(q, 5.0), i32([[[0, 1]] * 2] * 2), i32([0, 1]), i32([39, 19])
+    kv = torch.zeros(2, 2, 64, dtype=q.dtype, device="cuda")
+    calls = [
+        (api.dream_cache_attn, dict(cache=pg.cache, q=q, q_start=start, kv_len=n, out=out, workspace=room),
+         [dict(q=q.half()), dict(q=q.cpu()), dict(q=q[:, :, :32]), dict(q=q[:, ::2]), dict(q=None), dict(q=q[0]), dict(out=out[:1]), dict(out=out[:, :2]), dict(out=q),
+          dict(q_start=start[:2]), dict(q_start=start.long()), dict(q_start=None), dict(kv_len=n[:1]), dict(kv_len=None), dict(workspace=None),
+          dict(tree_mask=torch.zeros(2, 3, dtype=torch.int32, device="cuda")), dict(lse=torch.zeros(2, 3, device="cuda")), dict(scale=0.0), dict(scale=float("nan")),
+          dict(shared_pages=99), dict(q=q[:0], out=out[:0]), dict(cache=None), dict(workspace=room[16:])], [dict(workspace=room[:-256])]),
+        (api.dream_cache_attn_pages, dict(cache=pg.cache, q=q, row_seq=seq, row_pos=pos, ids=ids, out=out, workspace=room),
+         [dict(ids=ids[:, :1]), dict(ids=ids.long()), dict(ids=None), dict(row_seq=seq[:1]), dict(row_pos=None), dict(ids=ids[:, :, :0])], [dict(workspace=room[:256])]),
+        (api.dream_cache_append, dict(cache=pg.cache, q=q, k_new=kv, v_new=kv, row_seq=seq, slots=i32([0, 0]), q_out=out),
+         [dict(k_new=kv[:1]), dict(v_new=kv.half()), dict(v_new=None), dict(slots=None), dict(slots=pos[:1]), dict(q_out=None), dict(q=None), dict(q_out=out[:, :2]),
+          dict(rope=torch.zeros(4, 32, device="cuda")), dict(rope=torch.zeros(4, 64, 2, device="cuda")), dict(positions=pos.long())], [])]
+    k, v = pg.k.clone(), pg.v.clone()
+    for call, good, bad_args, short in calls:
+        for some, code in ((bad_args, E_ARG), (short, E_NOMEM)):
+            for bad in some:
+                with pytest.raises(api.DreamError) as e:
+                    call(**dict(good, **bad))
+                assert e.value.code == code, (call.__name__, bad.keys(), str(e.value))
+    with pytest.raises(api.DreamError) as e:                                    # a cache without bounds
+        api.dream_cache_select(pg.cache, q, seq, pos, ids, room)
+    assert e.value.code == E_ARG
+    torch.cuda.synchronize()
+    assert (out == 5.0).all() and torch.equal(k.nan_to_num(9.0), pg.k.nan_to_num(9.0)) and torch.equal(v.nan_to_num(9.0), pg.v.nan_to_num(9.0))
+    calls[0][0](**calls[0][1])
+    want, _, size = dense_reference(pg, q, [0, 1, 2])
+    close(out, want, size, "bf16")
+
+
+def test_several_host_threads():
+    """Threads that each append, attend, select and attend to the selected on a stream, a cache and a workspace of their own: the same bits as one behind the other."""
+    import threading
+
+    from paper_2505_19201_b200 import api
+    heads, hkv, rows = 8, 2, 3
+
+    def work(i, out, times):
+        d, pt = (64, 128, 256, 128)[i % 4], (16, 32, 64, 16)[i % 4]
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            pg = Pages([700 + i, 90, 1300], hkv, d, pt, seed=i, extra_entries=2)
+            bounds = torch.stack((pg.k.contiguous().amin(2), pg.k.contiguous().amax(2)), 2).nan_to_num(0.0)
+            cache = api.Cache(pg.k, pg.v, pg.table, bounds)
+            room = torch.empty(max(api.dream_cache_attn_bytes(cache, rows, heads), api.dream_cache_select_bytes(cache, rows)), dtype=torch.uint8, device="cuda")
+            x = pg.queries(rows, heads + 2 * hkv)
+            seq, pos, status = i32([0, 1, 2]), i32([n - 1 for n in pg.lengths]), i32([0, 0])
+            for _ in range(times):
+                q, dense_out, few = (torch.zeros(rows, heads, d, dtype=x.dtype, device="cuda") for _ in range(3))
+                ids = torch.zeros(rows, hkv, 4, dtype=torch.int32, device="cuda")
+                api.dream_cache_append(cache, x[:, :heads], x[:, heads:heads + hkv], x[:, heads + hkv:], seq, pos, q, status=status)
+                api.dream_cache_attn(cache, q, i32([0, 1, 2, 3]), pos + 1, dense_out, room, status=status)
+                api.dream_cache_select(cache, q, seq, pos, ids, room, status=status)
+                api.dream_cache_attn_pages(cache, q, seq, pos, ids, few, room, status=status)
+                out.append((dense_out, ids, few))
+            stream.synchronize()
+            assert status.tolist() == [0, 0]
+
+    alone, together = [[] for _ in range(6)], [[] for _ in range(6)]
+    for i in range(6):
+        work(i, alone[i], 1)
+    threads = [threading.Thread(target=work, args=(i, together[i], 8)) for i in range(6)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for a, b in zip(alone, together):
+        assert len(b) == 8
+        for got in b:
+            assert all(torch.equal(x, y) for x, y in zip(a[0], got))
+
+
+@pytest.mark.parametrize("heads", [1, 4, 16])
+@pytest.mark.parametrize("tree", [False, True])
+def test_more_rows_than_tokens_behind_shared_pages(heads, tree):
+    """Rows in front of a sequence's first token see nothing, whatever the others share."""
+    T, lengths = [2, 10, 4, 0], [100, 3, 0, 70]
+    out, lse = dense(Pages(lengths, 1, 64, 32, shared=2), T, heads, tree=sum((chain(n, True) for n in T), []) if tree else None)
+    if not tree:
+        assert (out[2:9] == 0).all() and (out[12:16] == 0).all() and torch.isinf(lse[2:9]).all() and torch.isinf(lse[12:16]).all()
