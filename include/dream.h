@@ -396,7 +396,8 @@ dream_status dream_distill_grad(const void *logits, int32_t dtype, int32_t rows,
  *            of 8, at least the row), 16-byte aligned: parts of a fused projection's rows will do.  What a call writes overlaps nothing that it reads
  *            (but q_out may be q)
  *   workspace : device, 256-byte aligned, of the size that dream_cache_attn_bytes (dream_cache_select_bytes) says; what it holds does not
- *            outlive the call, and two calls that may run at the same time need one each (so do two captured graphs that may)
+ *            outlive the call, and two calls that may run at the same time need one each (so do two captured graphs that may).  Attention's is 16 MB at head_dim 64, 21 at 128 and
+ *            42 at 256 for the parts of work that is dealt out, and 8 head_dim + 32 bytes for each row and head.
  *   status : device int32[2], zeroed by the caller once, or NULL.  Word 0 becomes 1 when a bounded wait in a kernel ran out (word 1: which), 2
  *            when a sequence, token, position, row or page number was out of range.  What such a number stands for is left out: rows are not written, keys not seen.
  *   cuda_stream : a cudaStream_t of the current device (NULL = legacy default stream)
@@ -411,7 +412,8 @@ typedef struct {
   int32_t n_seqs, pages_per_seq;  /* rows of the page table (at most 4096), and pages in one of them */
 } dream_cache;
 
-/* Rotary factors: table[p][i] = (cos, sin)(p * theta^(-2 i / rot_dim)), float [n_pos][rot_dim / 2][2] on the device, from angles taken in 64 bits. */
+/* Rotary factors: table[p][i] = (cos, sin)(p * theta^(-2 i / rot_dim)), float [n_pos][rot_dim / 2][2] on the device, from angles taken in 64 bits.  A program does this once: 131072
+ * positions of 128 channels take 79 us (their bytes would take 10; it is the 64-bit arithmetic). */
 dream_status dream_rope_table(float *table, int32_t n_pos, int32_t rot_dim, float theta, void *cuda_stream);
 
 /* Appends rows: row r is token slots[r] of sequence row_seq[r] (device int32 [rows]; a negative sequence is padding, its row is skipped).  Its queries are
@@ -439,7 +441,9 @@ dream_status dream_cache_attn_bytes(const dream_cache *cache, int32_t n_heads, i
  *            256 entries on the average each reads the shared keys with its own, tile by tile, which is at most half as many times again.)
  *   scale : finite, above zero (as a rule head_dim^-1/2)
  *   lse : device float [rows][n_heads], log-sum-exp of the scaled scores (-inf for a row that sees nothing), or NULL
- * What lies in a page behind a sequence's last token may be anything, NaN included; the tokens themselves are finite.
+ * What lies in a page behind a sequence's last token may be anything, NaN included; the tokens themselves are finite, and so small that the sums in 32 bits are finite too: scores below
+ * 2^127, and values below 2^119 divided by the number of keys (weights are up to 2^8 before they are divided by their sum; fp16 values are always so small).
+ * Weights are rounded to the cache's dtype for their product with V, and divided by the sum of the rounded ones, which moves a result by at most half a step of sum w |v - out|.
  * Sequences with a token each, with many, and with none may stand in one batch in any mixture.  (Only a call with rows = n_seqs, nothing shared and up to four query heads to a KV head
  * is laid out for a row of each sequence: one that has many is right there, but slow.) */
 dream_status dream_cache_attn(const dream_cache *cache, const void *q, int64_t q_ld, int32_t n_heads, int32_t rows, const int32_t *q_start,

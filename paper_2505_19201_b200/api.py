@@ -399,7 +399,8 @@ def dream_cache_attn_bytes(cache, rows, n_heads):
 
 def dream_cache_attn(cache, q, q_start, kv_len, out, workspace, shared_pages=0, tree_mask=None, scale=None, lse=None, status=None, stream=None):
     """Attention of a ragged batch: rows q_start[s] .. q_start[s + 1] - 1 of q [rows, heads, head_dim] are the last tokens of sequence s, which has
-    kv_len[s] in all; causal, or under tree_mask [rows, 4] int32.  The first shared_pages pages are the same in every sequence and are read once.  out like
+    kv_len[s] in all; causal, or under tree_mask [rows, 4] int32.  The first shared_pages pages are the same in every sequence and are read once.  Weights are
+    rounded to the cache's type for their product with V.  out like
     q; lse [rows, heads] float32 or None; workspace: a CUDA tensor of dream_cache_attn_bytes bytes; scale: head_dim^-1/2 unless given."""
     c = _cache(cache)
     dev, i32 = c.device, torch.int32

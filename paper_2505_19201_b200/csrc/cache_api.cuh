@@ -134,7 +134,7 @@ extern "C" dream_status dream_cache_append(const dream_cache *cache, const void 
   a.row_seq = row_seq; a.slots = slots; a.positions = positions; a.rope = (const float2 *)rope; a.rows = rows; a.heads = q ? n_heads : 0; a.hd = hd;
   a.n_pos = n_pos; a.rot = rope ? rot_dim : 0; a.interleaved = interleaved != 0; a.status = status;
   // A thread takes one unit of one head where there are few rows, so that many share the latency; else that unit of several heads, whose rotary factors and place it looks up
-  // once.  (32 + 2 x 8 heads of 128, with bounds, one head or several: 512 rows 9.1 or 9.3 us, 1024 rows 13.3 or 10.9, 3200 rows 32.6 or 19.4.)
+  // once.  (32 + 2 x 8 heads of 128, with bounds, one head or several: 512 rows 9.5 or 9.2 us, 1024 rows 13.9 or 10.9, 3200 rows 35.1 or 21.5.)
   const int per = CACHE_THREADS / (hd / 16), n_heads_all = a.heads + 2 * a.c.hkv;
   const bool deep = (long long)rows * n_heads_all * (hd / 16) >= 2LL * CACHE_THREADS * 148 * 4;
   a.head_lanes = deep ? 1 : per;

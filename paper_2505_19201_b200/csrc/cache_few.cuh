@@ -3,8 +3,8 @@
 //
 // The keys stand on the matrix instruction's long side:  S^T = K Q^T  (keys x 16), O^T += V^T P^T  (head_dim x 16).  Then every lane of every softmax warp has a key, four
 // entries each, and nothing is computed for rows that are not there.  Against the kernel with the entries on the long side (cache_attn.cuh), whose two softmax warps of sixteen rows
-// have all there is to do: 64 sequences of 2000 tokens, 32 heads over 8 of 128 wide, 88 us and 92; 12 heads of 64, 70 and 102; 16 over 8 of 256, 172 and 170; one of 833 tokens, 32
-// heads of 128, 12.5 and 13.9.  A form for up to 16 entries lost to the other kernel: 28 over 4 heads of 128 65 us against 53, 32 over 2 43 against 33, 24 over 3 of 64 38 against 35.
+// have all there is to do: 64 sequences of 2000 tokens, 32 heads over 8 of 128 wide, 89 us and 92 to 108; 12 heads of 64, 70 and 102 to 108; one of 833 tokens, 32 heads of 128, 13.0 and
+// 14.4.  At 256 wide neither is ahead (16 over 8: 171 and 170 to 175; of 1000 tokens, two rows each, 94 and 92), and the rule is the same for all widths.  A form for up to 16 entries lost to the other kernel: 28 over 4 heads of 128 65 us against 53, 32 over 2 43 against 33, 24 over 3 of 64 38 against 35.
 //   S^T   tcgen05.mma 128 x 16 x 16 over head_dim, A = the unit's keys and B = Q, both K-major; fp32 in TMEM, a ring of four 16-column buffers
 //   softmax   four warps, a key per thread: P = 2^(s - m) with a running reference m per entry, the same in all threads.  Whether some score has outgrown its reference
 //         by more than a power of two is one barrier with a vote per unit; only then (in the first unit of a segment, and seldom later) the maxima are taken, across lanes and warps, and

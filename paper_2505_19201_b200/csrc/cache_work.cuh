@@ -2,7 +2,7 @@
 //
 // Work.  An item is a tile of query entries (entry = (row, query head of one KV-head group)), up to 128 or up to 4 by kernel, against a run of keys of one KV head, cut into
 // units of 64 or 128 keys.  Shared pages: the rows of all sequences stand together, in full tiles, so that the prefix is read once for all of them (once per
-// tile).  A sequence's own tokens: its rows, tile by tile.  Listed pages: one row.  The units of all items, one behind the other, are dealt out to
+// tile; see ca_shared).  A sequence's own tokens: its rows, tile by tile, in the launch for its number of entries.  Listed pages: one row.  The units of all items, one behind the other, are dealt out to
 // the CTAs in equal contiguous ranges, by arithmetic on the lengths that each CTA does for itself (they are on the device), so long contexts
 // with few rows fill the GPU and short ones do not leave a tail.  An item counts START units more than it has, for what starting and ending it costs.  A
 // range is a few segments, each in one item.  A segment leaves (m, l, O) of its keys; k_cache_merge adds up the
@@ -52,7 +52,7 @@ __device__ __forceinline__ uint32_t pack2(float x, float y, bf16) { __nv_bfloat1
 __device__ __forceinline__ uint32_t pack2(float x, float y, f16) { __half2 h = __floats2half2_rn(x, y); return *reinterpret_cast<uint32_t *>(&h); }
 
 // The shared keys that are an item of their own, against the rows of all sequences.  Sequences whose own rows fill tiles read the prefix once per tile either way, and then it is one item
-// with their own keys, whose parts need not be put together: 0.  (Seven sequences behind 4096 tokens, 16 heads over 8 of 256, with 128 rows each 90 us, and 110 with the prefix by itself;
+// with their own keys, whose parts need not be put together: 0.  (Seven sequences behind 4096 tokens, 16 heads over 8 of 256, with 128 rows each 89 us, and 113 with the prefix by itself;
 // with 64 rows 61 and 64, but their last tiles are full, which at other lengths they are not; with 32 rows 46 and 40.)  From two tiles to a sequence on, on the average over the
 // sequences, the tiles by sequence are at most half as many again as those of all rows together, however the rows are spread: one more for each sequence.  The rows counted are those there
 // are, not those that a captured call has room for.

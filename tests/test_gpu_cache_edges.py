@@ -281,3 +281,12 @@ def test_more_rows_than_tokens_behind_shared_pages(heads, tree):
     out, lse = dense(Pages(lengths, 1, 64, 32, shared=2), T, heads, tree=sum((chain(n, True) for n in T), []) if tree else None)
     if not tree:
         assert (out[2:9] == 0).all() and (out[12:16] == 0).all() and torch.isinf(lse[2:9]).all() and torch.isinf(lse[12:16]).all()
+
+
+@pytest.mark.parametrize("heads,T", [(1, 1), (8, 3), (4, 130)])
+def test_values_as_large_as_may_be(heads, T):
+    """Values of 2^119 over the number of keys: sums of weights up to 2^8 times such values are finite."""
+    pg = Pages([512], 1, 128, 64)
+    pg.k *= torch.linspace(0.1, 2, 64, device="cuda").bfloat16()[:, None]
+    pg.v.copy_(torch.sign(pg.v) * 2.0 ** 110)
+    dense(pg, [T], heads, gain=2.0, spread=100.0)
